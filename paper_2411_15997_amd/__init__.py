@@ -2,7 +2,8 @@
 
 Argument marshalling only: every step of the path runs in the HIP kernels of
 ``libfairserve.so``; torch supplies device memory and the current stream.
-The functions carry the C entry points' names (include/fairserve.h).  There
+The functions carry the C entry points' names (include/fairserve.h; those of an engine
+step, include/fairserve_engine.h, are in ``engine``).  There
 is no CPU fallback: loading fails loudly when the library is missing.
 """
 from __future__ import annotations
@@ -13,6 +14,12 @@ from dataclasses import dataclass
 from typing import Optional, Sequence
 
 import numpy as np
+
+from . import engine
+from .engine import (FS_BF16, FS_F16, FS_F32, FS_ROPE_BASE, FS_ROPE_LINEAR,  # noqa: F401
+                     FS_ROPE_PARTS, FS_ROPE_PLAIN, Adapters, KVCache, Rope, Sampling, Step,
+                     cleared_err_word, fs_adapter_linear, fs_clear_status, fs_paged_attention,
+                     fs_rope_append, fs_rope_frequencies, fs_sample)
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libfairserve.so")
@@ -110,6 +117,7 @@ def _lib():
             "fs_sync_status": ([S, P], I32),
             "fs_status_string": ([I32], C.c_char_p),
         }
+        sig.update(engine.signatures())
         for name, (args, res) in sig.items():
             f = getattr(L, name)
             f.argtypes = args
@@ -122,7 +130,7 @@ EXPORTED = ("fs_cost", "fs_history_workspace", "fs_weights_from_history", "fs_th
             "fs_schedule_step", "fs_run_trace_workspace", "fs_run_trace", "fs_metrics_workspace",
             "fs_fairness_metrics", "fs_metrics_noalloc_limit", "fs_fairness_metrics_noalloc",
             "fs_workload_workspace", "fs_workload_stats",
-            "fs_coef_from_expectations", "fs_sync_status", "fs_status_string")
+            "fs_coef_from_expectations", "fs_sync_status", "fs_status_string") + engine.EXPORTED_ENGINE
 
 
 def _check(code: int, where: str):

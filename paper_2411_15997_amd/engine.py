@@ -1,0 +1,359 @@
+"""Binding of the engine-step operators (include/fairserve_engine.h): descriptors over the
+caller's tensors and the calls, on torch's current stream.
+
+Argument marshalling only.  A descriptor (Step, KVCache, Adapters, Rope, Sampling) checks
+its tensors once and keeps them alive; a serving loop makes it once and calls with it.
+The calls raise the status word `err` and do not clear it: pass one cleared word
+(cleared_err_word, fs_clear_status) to every call of a step with check=False and look at
+it once with sync_check.  Without `err` a call takes a cleared word of its own.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+import numpy as np
+
+FS_BF16, FS_F16, FS_F32 = 0, 1, 2
+FS_ROPE_PLAIN, FS_ROPE_LINEAR, FS_ROPE_BASE, FS_ROPE_PARTS = 0, 1, 2, 3
+ALIGN = 256
+
+EXPORTED_ENGINE = ("fs_clear_status", "fs_adapter_workspace", "fs_adapter_linear",
+                   "fs_rope_frequencies", "fs_rope_append", "fs_attention_workspace",
+                   "fs_paged_attention", "fs_sample_workspace", "fs_sample")
+
+
+class fs_step(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("q_off_h", C.c_void_p), ("q_off", C.c_void_p),
+                ("kv_len", C.c_void_p), ("max_kv", C.c_int32)]
+
+
+class fs_kv_cache(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("page_size", C.c_int32), ("n_pages", C.c_int64), ("k", C.c_void_p),
+                ("v", C.c_void_p), ("page_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("token_stride", C.c_int64), ("table", C.c_void_p), ("table_stride", C.c_int64)]
+
+
+class fs_adapters(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("in_features", C.c_int32), ("out_features", C.c_int32),
+                ("n_adapters", C.c_int32), ("max_rank", C.c_int32), ("a", C.c_void_p),
+                ("b", C.c_void_p), ("rank", C.c_void_p), ("scale", C.c_void_p),
+                ("adapter", C.c_void_p)]
+
+
+class fs_rope(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("inv_freq", C.c_void_p),
+                ("factor", C.c_float), ("pos", C.c_void_p)]
+
+
+class fs_sampling(C.Structure):
+    _fields_ = [("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p),
+                ("min_p", C.c_void_p)]
+
+
+def signatures():
+    P, I32, I64, SZ, F, D = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t, C.c_float, C.c_double
+    S, K, A, R, G = (C.POINTER(t) for t in (fs_step, fs_kv_cache, fs_adapters, fs_rope,
+                                            fs_sampling))
+    return {
+        "fs_clear_status": ([P, P], I32),
+        "fs_adapter_workspace": ([S, A], SZ),
+        "fs_adapter_linear": ([S, A, P, I64, P, P, I64, P, SZ, P, P], I32),
+        "fs_rope_frequencies": ([I32, D, I32, D, I32, D, D, P, P], I32),
+        "fs_rope_append": ([S, K, R, I32, P, I64, P, I64, P, I64, P, I64, P, P], I32),
+        "fs_attention_workspace": ([S, K, I32, I32], SZ),
+        "fs_paged_attention": ([S, K, I32, F, I32, P, I64, P, I64, P, P, SZ, P, P], I32),
+        "fs_sample_workspace": ([I32, I32, I32], SZ),
+        "fs_sample": ([I32, I32, I32, P, I64, G, P, P, P, P, P, SZ, P, P], I32),
+    }
+
+
+_fns = None
+
+
+def _lib():
+    """The loaded library's entry points (looked up once)."""
+    global _fns
+    if _fns is None:
+        from . import _lib as load
+        _fns = load()
+    return _fns
+
+
+_torch_mod = None
+
+
+def _torch():
+    global _torch_mod
+    if _torch_mod is None:
+        import torch
+        _torch_mod = torch
+    return _torch_mod
+
+
+def _fail(code, where):
+    from . import FairServeError
+    raise FairServeError(code, where)
+
+
+def _dtype_code(t):
+    torch = _torch()
+    code = {torch.bfloat16: FS_BF16, torch.float16: FS_F16, torch.float32: FS_F32}.get(t.dtype)
+    if code is None:
+        raise TypeError(f"dtype {t.dtype} is not supported (bfloat16, float16, float32)")
+    return code
+
+
+def _want(cond, what):
+    if not cond:
+        raise ValueError(what)
+
+
+def _stream(t):
+    return _torch()._C._cuda_getCurrentRawStream(t.device.index)
+
+
+def _vector(t, dtype, n, name):
+    """A contiguous device vector of `n` values of `dtype`, or None."""
+    if t is None:
+        return None
+    _want(t.dtype == dtype and t.is_contiguous() and t.dim() == 1 and t.shape[0] >= n,
+          f"{name}: a contiguous {dtype} vector of {n} values")
+    return t.data_ptr()
+
+
+def _rows(t, name, *shape):
+    """Pointer and row stride of a tensor of rows whose inner dimensions are packed."""
+    _want(tuple(t.shape) == shape, f"{name}: shape {tuple(t.shape)}, wanted {shape}")
+    inner = 1
+    for d in range(t.dim() - 1, 0, -1):
+        _want(t.shape[d] == 1 or t.stride(d) == inner, f"{name}: inner dimensions are not packed")
+        inner *= t.shape[d]
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else inner)
+
+
+def _workspace(ws, need, like):
+    if need == 0:
+        return None, None, 0
+    if ws is None:
+        ws = _torch().empty(need, dtype=_torch().uint8, device=like.device)
+    return ws, ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def cleared_err_word(device="cuda"):
+    return _torch().zeros(1, dtype=_torch().int32, device=device)
+
+
+def fs_clear_status(err):
+    code = _lib().fs_clear_status(err.data_ptr(), _stream(err))
+    if code:
+        _fail(code, "fs_clear_status")
+
+
+def _done(code, where, err, check):
+    if code:
+        _fail(code, where)
+    if check:
+        from . import sync_check
+        sync_check(err, where)
+
+
+class Step:
+    """The requests of one engine step: q_off (host sequence and its int32 device copy,
+    made when not given), kv_len [n] int32 on the device and the host bound max_kv."""
+
+    def __init__(self, q_off_h, q_off=None, kv_len=None, max_kv=0, device="cuda"):
+        torch = _torch()
+        self.q_off_h = np.ascontiguousarray(q_off_h, np.int32)
+        n = self.q_off_h.shape[0] - 1
+        _want(n >= 0, "q_off: at least one value")
+        self.n, self.rows = n, int(self.q_off_h[-1])
+        self.q_off = torch.from_numpy(self.q_off_h.copy()).to(device) if q_off is None else q_off
+        self.kv_len = kv_len
+        self.s = fs_step(n, self.q_off_h.ctypes.data,
+                         _vector(self.q_off, torch.int32, n + 1, "q_off"),
+                         _vector(kv_len, torch.int32, n, "kv_len"), int(max_kv))
+        self.ref = C.byref(self.s)
+
+
+class KVCache:
+    """A paged cache: k and v [pages][kv_heads][page_size][head_dim] (any strides with the
+    last dimension packed; k and v alike), table [n][width] int32 of page ids."""
+
+    def __init__(self, k, v, table):
+        torch = _torch()
+        _want(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and
+              k.dtype == v.dtype, "k and v: four dimensions, alike in shape, strides and dtype")
+        _want(k.shape[3] == 1 or k.stride(3) == 1, "k, v: the last dimension is not packed")
+        _want(table.dim() == 2 and table.dtype == torch.int32 and
+              (table.shape[1] <= 1 or table.stride(1) == 1), "table: int32 [n][width]")
+        self.k, self.v, self.table = k, v, table
+        self.n_kv_heads, self.head_dim, self.dtype = k.shape[1], k.shape[3], k.dtype
+        self.s = fs_kv_cache(_dtype_code(k), k.shape[1], k.shape[3], k.shape[2], k.shape[0],
+                             k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
+                             table.data_ptr(), self._table_stride(table))
+        self.ref = C.byref(self.s)
+
+    @staticmethod
+    def _table_stride(table):
+        if table.shape[0] > 1:
+            _want(table.stride(0) >= table.shape[1], "table: rows overlap")
+            return table.stride(0) if table.stride(0) == table.shape[1] else table.stride(0)
+        return table.shape[1]
+
+
+class Adapters:
+    """Low-rank adapters: a [n][max_rank][K], b [n][N][max_rank] (packed), adapter [n_seqs]
+    int32 (-1: none), rank [n] int32 and scale [n] float (each may be None)."""
+
+    def __init__(self, a, b, adapter, rank=None, scale=None):
+        torch = _torch()
+        _want(a.dim() == 3 and b.dim() == 3 and a.is_contiguous() and b.is_contiguous() and
+              a.dtype == b.dtype and a.shape[0] == b.shape[0] and a.shape[1] == b.shape[2],
+              "a [n][max_rank][K] and b [n][N][max_rank]: packed, of one dtype")
+        n, r, k = a.shape
+        self.keep = (a, b, adapter, rank, scale)
+        self.dtype, self.K, self.N, self.n_seqs = a.dtype, k, b.shape[1], adapter.shape[0]
+        self.s = fs_adapters(_dtype_code(a), k, b.shape[1], n, r, a.data_ptr(), b.data_ptr(),
+                             _vector(rank, torch.int32, n, "rank"),
+                             _vector(scale, torch.float32, n, "scale"),
+                             _vector(adapter, torch.int32, 0, "adapter"))
+        self.ref = C.byref(self.s)
+
+
+class Rope:
+    """Rotary positions: inv_freq [rotary_dim / 2] float on the device, the pair layout, the
+    factor of long-context scaling and, when not the cache positions, pos [rows] int32."""
+
+    def __init__(self, inv_freq, interleaved=False, factor=1.0, pos=None):
+        torch = _torch()
+        self.inv_freq, self.pos = inv_freq, pos
+        n = inv_freq.shape[0]
+        self.s = fs_rope(2 * n, int(bool(interleaved)), _vector(inv_freq, torch.float32, n, "inv_freq"),
+                         float(factor), _vector(pos, torch.int32, 0, "pos"))
+        self.ref = C.byref(self.s)
+
+
+class Sampling:
+    """Per-row sampling settings on the device (each may be None)."""
+
+    def __init__(self, temperature=None, top_k=None, top_p=None, min_p=None):
+        torch = _torch()
+        self.keep = (temperature, top_k, top_p, min_p)
+        self.rows = min((t.shape[0] for t in self.keep if t is not None), default=None)
+        self.s = fs_sampling(_vector(temperature, torch.float32, 0, "temperature"),
+                             _vector(top_k, torch.int32, 0, "top_k"),
+                             _vector(top_p, torch.float32, 0, "top_p"),
+                             _vector(min_p, torch.float32, 0, "min_p"))
+        self.ref = C.byref(self.s)
+
+
+def fs_adapter_linear(step: Step, adapters: Adapters, x, w, y=None, ws=None, err=None, check=True):
+    """y = x w^T plus every request's adapter; x [rows][K], w [N][K], returns y [rows][N]."""
+    K, N = adapters.K, adapters.N
+    xp, xs = _rows(x, "x", step.rows, K)
+    _want(tuple(w.shape) == (N, K) and w.is_contiguous(), "w: packed [N][K]")
+    _want(x.dtype == adapters.dtype and w.dtype == adapters.dtype, "x, w and adapters: one dtype")
+    _want(adapters.n_seqs >= step.n, "adapter: an id for every request")
+    if y is None:
+        y = _torch().empty((step.rows, N), dtype=x.dtype, device=x.device)
+    _want(y.dtype == x.dtype, "y: the dtype of x")
+    yp, ys = _rows(y, "y", step.rows, N)
+    err = cleared_err_word(x.device) if err is None else err
+    L = _lib()
+    ws, wp, wn = _workspace(ws, L.fs_adapter_workspace(step.ref, adapters.ref), x)
+    _done(L.fs_adapter_linear(step.ref, adapters.ref, xp, xs, w.data_ptr(), yp, ys, wp, wn,
+                              err.data_ptr(), _stream(x)), "fs_adapter_linear", err, check)
+    return y
+
+
+def fs_rope_frequencies(rotary_dim, theta0=10000.0, scaling=FS_ROPE_PLAIN, scale=1.0,
+                        original_len=4096, beta_fast=32.0, beta_slow=1.0):
+    """Host helper: (inv_freq [rotary_dim / 2] float32, factor)."""
+    f = np.zeros(max(1, rotary_dim // 2), np.float32)
+    m = np.zeros(1, np.float32)
+    code = _lib().fs_rope_frequencies(int(rotary_dim), float(theta0), int(scaling), float(scale),
+                                      int(original_len), float(beta_fast), float(beta_slow),
+                                      f.ctypes.data, m.ctypes.data)
+    if code:
+        _fail(code, "fs_rope_frequencies")
+    return f[:rotary_dim // 2], float(m[0])
+
+
+def fs_rope_append(step: Step, cache: KVCache, rope: Rope, q, k, v, q_out=None, err=None,
+                   check=True):
+    """Turns q [rows][heads][dim] and k, appends k and v [rows][kv_heads][dim] to the cache;
+    returns the turned q (q_out, which may be q itself)."""
+    T, HK, D = step.rows, cache.n_kv_heads, cache.head_dim
+    _want(k.dtype == cache.dtype and v.dtype == cache.dtype and
+          (q is None or q.dtype == cache.dtype), "q, k, v: the cache's dtype")
+    _want(cache.table.shape[0] >= step.n, "table: a row for every request")
+    _want(rope.pos is None or rope.pos.shape[0] >= T, "pos: a position for every row")
+    kp, ks = _rows(k, "k", T, HK, D)
+    vp, vs = _rows(v, "v", T, HK, D)
+    H, qp, qs, op, os_ = 0, None, 0, None, 0
+    if q is not None:
+        H = q.shape[1]
+        qp, qs = _rows(q, "q", T, H, D)
+        if q_out is None:
+            q_out = _torch().empty((T, H, D), dtype=q.dtype, device=q.device)
+        _want(q_out.dtype == q.dtype, "q_out: the dtype of q")
+        op, os_ = _rows(q_out, "q_out", T, H, D)
+    err = cleared_err_word(k.device) if err is None else err
+    _done(_lib().fs_rope_append(step.ref, cache.ref, rope.ref, H, qp, qs, kp, ks, vp, vs, op, os_,
+                                err.data_ptr(), _stream(k)), "fs_rope_append", err, check)
+    return q_out
+
+
+def fs_paged_attention(step: Step, cache: KVCache, q, scale, window=0, out=None, lse=None,
+                       want_lse=False, ws=None, err=None, check=True):
+    """Attention of q [rows][heads][dim] over the cache; returns out, or (out, lse) when the
+    log-sum-exp [rows][heads] is wanted."""
+    T, H, D = q.shape
+    _want(q.dtype == cache.dtype and D == cache.head_dim, "q: the cache's dtype and head_dim")
+    _want(cache.table.shape[0] >= step.n, "table: a row for every request")
+    qp, qs = _rows(q, "q", step.rows, H, D)
+    torch = _torch()
+    if out is None:
+        out = torch.empty((T, H, D), dtype=q.dtype, device=q.device)
+    _want(out.dtype == q.dtype, "out: the dtype of q")
+    op, os_ = _rows(out, "out", T, H, D)
+    if lse is None and want_lse:
+        lse = torch.empty((T, H), dtype=torch.float32, device=q.device)
+    if lse is not None:
+        _want(lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == T * H,
+              "lse: packed float32 [rows][heads]")
+    err = cleared_err_word(q.device) if err is None else err
+    L = _lib()
+    ws, wp, wn = _workspace(ws, L.fs_attention_workspace(step.ref, cache.ref, H, int(window)), q)
+    _done(L.fs_paged_attention(step.ref, cache.ref, H, scale, int(window), qp, qs, op, os_,
+                               None if lse is None else lse.data_ptr(), wp, wn, err.data_ptr(),
+                               _stream(q)), "fs_paged_attention", err, check)
+    return out if lse is None else (out, lse)
+
+
+def fs_sample(logits, u, sampling: Sampling, token=None, logprob=None, kept=None, ws=None,
+              err=None, check=True):
+    """The next token of each row of logits [rows][vocab] for the random numbers u [rows];
+    returns (token int32, logprob float32, kept int32), each [rows]."""
+    torch = _torch()
+    n, V = logits.shape
+    _want(n <= 1 or logits.stride(0) >= V, "logits: rows overlap")
+    _want(V == 1 or logits.stride(1) == 1, "logits: rows are not packed")
+    _want(sampling.rows is None or sampling.rows >= n, "sampling: a setting for every row")
+    up = _vector(u, torch.float32, n, "u")
+    dev = logits.device
+    token = torch.empty(n, dtype=torch.int32, device=dev) if token is None else token
+    logprob = torch.empty(n, dtype=torch.float32, device=dev) if logprob is None else logprob
+    kept = torch.empty(n, dtype=torch.int32, device=dev) if kept is None else kept
+    tp, lp, kp = (_vector(token, torch.int32, n, "token"),
+                  _vector(logprob, torch.float32, n, "logprob"),
+                  _vector(kept, torch.int32, n, "kept"))
+    err = cleared_err_word(dev) if err is None else err
+    code = _dtype_code(logits)
+    L = _lib()
+    ws, wp, wn = _workspace(ws, L.fs_sample_workspace(code, n, V), logits)
+    _done(L.fs_sample(code, n, V, logits.data_ptr(), logits.stride(0) if n > 1 else V,
+                      sampling.ref, up, tp, lp, kp, wp, wn, err.data_ptr(), _stream(logits)),
+          "fs_sample", err, check)
+    return token, logprob, kept
