@@ -1,97 +1,610 @@
-// Attention of the step's rows over the paged cache (one pass over the keys with the
-// running maximum and sum of the softmax).  One wave per row and head.
+// Attention of the step's rows over the paged cache: one pass over the keys with the
+// running maximum and sum of the softmax.
+//
+// The G = n_heads / n_kv_heads query heads that share a key/value head are rows of one
+// matrix product: a request's n tokens are n * G rows (token-major) per key/value head.
+//   k_attn_few    requests of at most 64 rows (single tokens, small chunks): bound by the
+//                 cache's bytes.  Keys are spread over the four waves of a work-group and
+//                 over work-groups (splits); each wave streams its own 32 keys at a time.
+//   k_attn_chunk  larger chunks: bound by the matrix cores.  128 rows a work-group, 64
+//                 keys at a time through LDS.
+//   k_attn_join   joins the splits' results with their maxima and sums, in split order.
+// Both products run with the keys as rows of the first operand (S^T = K Q^T,
+// O^T = V^T P^T): a lane then holds scores of one query row only, its probabilities are
+// the second product's operand as they lie in registers, and the running factors are one
+// number per lane.  The second product takes the keys in the order in which the first
+// one leaves them; V is read from LDS transposed, in that same order.
 #include "fs_engine.h"
 
 namespace fs {
 
 namespace {
 
+constexpr int kFewRows = 64;    // rows (tokens times group) that k_attn_few takes
+constexpr int kChunkRows = 128;  // rows of a work-group of k_attn_chunk
+constexpr float kLn2 = 0.693147180559945309f;
+
 struct AttnArgs {
   const int32_t *q_off, *kv_len;
-  int32_t n_seqs, max_kv, rows, n_heads, window;
+  int32_t n_seqs, max_kv, rows, n_heads, window, group;
   DevCache c;
   const short *q;
   short *out;
   int64_t q_stride, out_stride;
   float *lse;
-  float scale;
+  float c2;            // |scale| * log2(e)
+  uint32_t flip;       // sign of the scale, applied to the queries
+  int32_t few_split;   // keys of a split (k_attn_few), splits
+  int32_t few_splits;
+  int32_t few_tokens;  // most tokens of a request that k_attn_few takes
+  int32_t chunk_split, chunk_splits, chunk_tiles;
+  float *few_o, *few_ml;      // [splits][n_seqs][few_tokens][heads][D], [..][2]
+  float *chunk_o, *chunk_ml;  // [splits][rows][heads][D], [..][2]
   int32_t *err;
 };
 
-template <bool BF, int D>
-__global__ void __launch_bounds__(256) k_attention(AttnArgs a) {
-  __shared__ float qs[4][D];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t rh = int64_t(blockIdx.x) * 4 + wave;
-  const bool live = rh < int64_t(a.rows) * a.n_heads;
-  const int32_t t = live ? int32_t(rh / a.n_heads) : 0, h = live ? int32_t(rh % a.n_heads) : 0;
-  for (int d = lane; d < D; d += 64)
-    qs[wave][d] = to_f32<BF>(a.q[t * a.q_stride + h * D + d]) * a.scale;
-  __syncthreads();
-  if (!live) return;
+// Keys that the rows [r0, r1) of a request with n tokens and kv cached ones see.
+struct KeyRange {
+  int32_t lo, hi;
+};
+__device__ inline KeyRange key_range(const AttnArgs &a, int32_t n, int32_t kv, int32_t tok0,
+                                     int32_t tok1) {
+  KeyRange r;
+  r.lo = a.window ? max(0, kv - n + tok0 - a.window + 1) : 0;
+  r.hi = max(0, kv - n + tok1 + 1);
+  return r;
+}
+
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+// Four keys by sixteen columns of V per 16 lanes, transposed: lane i of the 16 names the
+// 8 bytes (key i / 4, columns 4 (i % 4) ..) and gets column i of the four keys.
+__device__ inline s16x4 read_tr(const short *p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (lds_s16x4 *)(__attribute__((address_space(3))) short *)(p));
+}
+
+// Where 16-byte chunk `c` of key row `r` lies in an LDS tile with D-element rows: chunks
+// are exchanged so that 16 rows' chunks, and 4 rows' transposed reads, fall on different
+// banks.
+template <int D>
+__device__ inline int tile_at(int r, int c) {
+  if constexpr (D == 128)
+    return r * 128 + ((c ^ ((r & 3) << 2 | ((r >> 2) & 3))) * 8);
+  else
+    return r * 64 + ((c ^ (((r >> 1) & 1) << 2 | ((r >> 2) & 3))) * 8);
+}
+
+template <bool BF>
+__device__ inline s16x8 pack8(const float *p) {
+  s16x8 v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = to_16<BF>(p[i]);
+  return v;
+}
+
+// Element offset of a key's row in the cache (either of k and v).
+__device__ inline int64_t key_at(const DevCache &c, const int32_t *table, int32_t j, int64_t head,
+                                 int32_t &code) {
+  const int64_t page = checked_page(c, table + (j >> c.page_shift), code);
+  return page * c.page_stride + head + (j & ((1 << c.page_shift) - 1)) * c.token_stride;
+}
+
+// ---- few rows: NT tiles of 16 rows
+template <bool BF, int D, int NT>
+__global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
+  constexpr int KS = D / 32;  // matrix steps of a score, and 16-byte chunks of a lane's row
+  constexpr int DB = D / 16;  // 16-column blocks of an output row
+  __shared__ __align__(16) short vt[4][32 * D];
+  __shared__ float wm[4][NT * 16], wl[4][NT * 16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int r16 = lane & 15, g4 = lane >> 4;
+  const int s = blockIdx.x, hk = blockIdx.y;
+  const int32_t q0 = __ldg(a.q_off + s), n = __ldg(a.q_off + s + 1) - q0;
+  const int G = a.group, R = n * G;
+  if (R <= 0 || R > kFewRows) return;
   int32_t code = 0;
-  const int32_t s = seq_of_row(a.q_off, a.n_seqs, t);
   const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
-  const int32_t p = kv - (__ldg(a.q_off + s + 1) - t);
-  const int32_t first = a.window ? max(0, p - a.window + 1) : 0;
-  const int64_t head = (h / (a.n_heads / a.c.n_kv_heads)) * a.c.head_stride;
+  const KeyRange kr = key_range(a, n, kv, 0, n - 1);
+  const bool single = kr.hi - kr.lo <= a.few_split;
+  const int32_t lo = kr.lo + blockIdx.z * a.few_split;
+  if (blockIdx.z > 0 && lo >= kr.hi) return;
+  const int32_t hi = min(kr.hi, lo + a.few_split);
   const int32_t *table = a.c.table + s * a.c.table_stride;
-  const int32_t in_page = (1 << a.c.page_shift) - 1;
-  float m = -INFINITY, l = 0.f, o[D / 64] = {};
-  for (int32_t j0 = first; j0 <= p; j0 += 64) {
-    const int32_t j = j0 + lane;
-    const bool see = j <= p;
-    int64_t at = 0;
-    float sc = -INFINITY;
-    if (see) {
-      at = checked_page(a.c, table + (j >> a.c.page_shift), code) * a.c.page_stride + head +
-           (j & in_page) * a.c.token_stride;
-      const short *kp = reinterpret_cast<const short *>(a.c.k) + at;
-      sc = 0.f;
-      for (int d = 0; d < D; d += 8) {
-        const s16x8 kv8 = *reinterpret_cast<const s16x8 *>(kp + d);
+  const int64_t head = hk * a.c.head_stride;
+  const short *kp = reinterpret_cast<const short *>(a.c.k) + g4 * 8;
+  const short *vp = reinterpret_cast<const short *>(a.c.v) + g4 * 8;
+
+  // queries: row r16 of each tile, this lane's 8 elements of each step
+  s16x8 qf[NT][KS];
+  int32_t pos[NT];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sc += to_f32<BF>(kv8[i]) * qs[wave][d + i];
-      }
-    }
-    float top = sc;
-    for (int w = 32; w; w >>= 1) top = fmaxf(top, __shfl_xor(top, w, 64));
-    const float m2 = fmaxf(m, top);
-    if (m2 == -INFINITY) continue;
-    const float f = expf(m - m2), e = expf(sc - m2);
-    float sum = e;
-    for (int w = 32; w; w >>= 1) sum += __shfl_xor(sum, w, 64);
-    l = l * f + sum;
-    m = m2;
+  for (int t = 0; t < NT; ++t) {
+    const int r = min(t * 16 + r16, R - 1), tok = r / G, h = hk * G + (r - tok * G);
+    pos[t] = t * 16 + r16 < R ? kv - n + tok : -1;
+    const short *qp = a.q + (q0 + tok) * a.q_stride + h * D + g4 * 8;
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) o[i] *= f;
-    const int n = min(64, p - j0 + 1);
-    for (int i = 0; i < n; ++i) {
-      const float w = __shfl(e, i, 64);
-      const int64_t vat = __shfl(at, i, 64);
-      const short *vp = reinterpret_cast<const short *>(a.c.v) + vat;
-#pragma unroll
-      for (int d = 0; d < D / 64; ++d) o[d] += w * to_f32<BF>(vp[d * 64 + lane]);
+    for (int k = 0; k < KS; ++k) {
+      qf[t][k] = *reinterpret_cast<const s16x8 *>(qp + k * 32);
+      if (a.flip) qf[t][k] ^= short(0x8000);
     }
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  f32x4 o[NT][DB] = {};
+  float m[NT], l[NT];
 #pragma unroll
-  for (int d = 0; d < D / 64; ++d)
-    a.out[t * a.out_stride + h * D + d * 64 + lane] = to_16<BF>(o[d] * inv);
-  if (a.lse && lane == 0) a.lse[int64_t(t) * a.n_heads + h] = m + logf(l);
+  for (int t = 0; t < NT; ++t) m[t] = -INFINITY, l[t] = 0.f;
+
+  s16x8 kf[2][KS], vf[2][KS];
+  int64_t at[2];
+  const int32_t first = lo + wave * 32;
+  short *tile = vt[wave];
+  if (first < hi) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      at[b] = key_at(a.c, table, min(first + b * 16 + r16, hi - 1), head, code);
+#pragma unroll
+      for (int k = 0; k < KS; ++k) kf[b][k] = *reinterpret_cast<const s16x8 *>(kp + at[b] + k * 32);
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int k = 0; k < KS; ++k) vf[b][k] = *reinterpret_cast<const s16x8 *>(vp + at[b] + k * 32);
+    // the next tile's places, one tile ahead of its rows
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+      at[b] = key_at(a.c, table, min(first + 128 + b * 16 + r16, hi - 1), head, code);
+  }
+  for (int32_t j0 = first; j0 < hi; j0 += 128) {
+    f32x4 sc[NT][2] = {};
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int k = 0; k < KS; ++k) sc[t][b] = mfma_16x16x32<BF>(kf[b][k], qf[t][k], sc[t][b]);
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+        *reinterpret_cast<s16x8 *>(tile + tile_at<D>(b * 16 + r16, k * 4 + g4)) = vf[b][k];
+    if (j0 + 128 < hi) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+          kf[b][k] = *reinterpret_cast<const s16x8 *>(kp + at[b] + k * 32);
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+          vf[b][k] = *reinterpret_cast<const s16x8 *>(vp + at[b] + k * 32);
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+        at[b] = key_at(a.c, table, min(j0 + 256 + b * 16 + r16, hi - 1), head, code);
+    }
+    s16x8 pf[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      float p[8], top = -INFINITY;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int32_t j = j0 + b * 16 + g4 * 4 + i;
+          const bool see = j <= pos[t] && j < hi && (a.window == 0 || j > pos[t] - a.window);
+          p[b * 4 + i] = see ? sc[t][b][i] : -INFINITY;
+          top = fmaxf(top, p[b * 4 + i]);
+        }
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float m2 = fmaxf(m[t], top);
+      if (__any(m2 > m[t])) {
+        const float f = m[t] == -INFINITY ? 0.f : exp2_fast((m[t] - m2) * a.c2);
+        l[t] *= f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[t][d] *= f;
+        m[t] = m2;
+      }
+      const float mc = m[t] == -INFINITY ? 0.f : m[t] * a.c2;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        p[i] = exp2_fast(fmaf(p[i], a.c2, -mc));
+        l[t] += p[i];
+      }
+      pf[t] = pack8<BF>(p);
+    }
+    // keys 4 g4 .. + 3 and 16 + 4 g4 .. + 3 of the tile, 16 columns at a time
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+      const int row = 4 * g4 + (r16 >> 2), col = d * 16 + (r16 & 3) * 4;
+      const s16x4 v0 = read_tr(tile + tile_at<D>(row, col >> 3) + (col & 7));
+      const s16x4 v1 = read_tr(tile + tile_at<D>(row + 16, col >> 3) + (col & 7));
+      const s16x8 vv = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) o[t][d] = mfma_16x16x32<BF>(vv, pf[t], o[t][d]);
+    }
+  }
   raise_err(a.err, code);
+
+  // the four waves' results, joined in LDS a tile of rows at a time
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    l[t] += __shfl_xor(l[t], 16, 64);
+    l[t] += __shfl_xor(l[t], 32, 64);
+    if (g4 == 0) wm[wave][t * 16 + r16] = m[t], wl[wave][t * 16 + r16] = l[t];
+  }
+  float *buf = reinterpret_cast<float *>(vt);  // [4][16][D / 2]: half of the columns at a time
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    if (t * 16 >= R) break;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      __syncthreads();
+#pragma unroll
+      for (int d = 0; d < DB / 2; ++d)
+        *reinterpret_cast<f32x4 *>(buf + (wave * 16 + r16) * (D / 2) +
+                                   ((d * 16 + g4 * 4) ^ ((r16 & 3) * 4))) = o[t][half * (DB / 2) + d];
+      __syncthreads();
+      for (int e = tid; e < 16 * D / 8; e += 256) {
+        const int r = e / (D / 8), col = (e - r * (D / 8)) * 4;
+        if (t * 16 + r >= R) continue;
+        const int tr = t * 16 + r;
+        const float top = fmaxf(fmaxf(wm[0][tr], wm[1][tr]), fmaxf(wm[2][tr], wm[3][tr]));
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const float f = wm[w][tr] == -INFINITY ? 0.f : exp2_fast((wm[w][tr] - top) * a.c2);
+          sum += f * wl[w][tr];
+          acc += f * *reinterpret_cast<const f32x4 *>(buf + (w * 16 + r) * (D / 2) +
+                                                      (col ^ ((r & 3) * 4)));
+        }
+        const int tok = tr / G, h = hk * G + (tr - tok * G), cc = half * (D / 2) + col;
+        if (single) {
+          const float inv = sum > 0.f ? 1.f / sum : 0.f;
+          s16x4 v;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = to_16<BF>(acc[i] * inv);
+          *reinterpret_cast<s16x4 *>(a.out + (q0 + tok) * a.out_stride + h * D + cc) = v;
+          if (cc == 0 && a.lse)
+            a.lse[int64_t(q0 + tok) * a.n_heads + h] =
+                sum > 0.f ? (top * a.c2 + __log2f(sum)) * kLn2 : -INFINITY;
+        } else {
+          const int64_t idx =
+              ((int64_t(blockIdx.z) * a.n_seqs + s) * a.few_tokens + tok) * a.n_heads + h;
+          *reinterpret_cast<f32x4 *>(a.few_o + idx * D + cc) = acc;
+          if (cc == 0) a.few_ml[idx * 2] = top, a.few_ml[idx * 2 + 1] = sum;
+        }
+      }
+    }
+  }
+}
+
+// Row tiles of k_attn_chunk: request s owns tile numbers from q_off[s] * G / 128 + s on.
+__device__ inline void chunk_tile(const AttnArgs &a, int32_t b, int32_t &s, int32_t &r0) {
+  int32_t lo = 0, hi = a.n_seqs - 1;
+  while (lo < hi) {
+    const int32_t mid = (lo + hi + 1) >> 1;
+    if (__ldg(a.q_off + mid) * a.group / kChunkRows + mid <= b)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  s = lo;
+  r0 = (b - __ldg(a.q_off + lo) * a.group / kChunkRows - lo) * kChunkRows;
+}
+
+// ---- chunks: four waves of 32 rows, 64 keys at a time
+template <bool BF, int D>
+__global__ void __launch_bounds__(256, 2) k_attn_chunk(AttnArgs a) {
+  constexpr int KS = D / 16;       // matrix steps of a score
+  constexpr int DB = D / 32;       // 32-column blocks of an output row
+  constexpr int CH = D / 8;        // 16-byte chunks of a key row
+  constexpr int LD = 64 * CH / 256;  // chunks a thread loads of K, and of V
+  __shared__ __align__(16) short kt[64 * D], vt[64 * D];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int r32 = lane & 31, h2 = lane >> 5;
+  const int hk = blockIdx.x % a.c.n_kv_heads;
+  // the last tiles of a request see the most keys: they go first
+  const int32_t b = a.chunk_tiles - 1 - int32_t(blockIdx.x / a.c.n_kv_heads);
+  int32_t s, r0;
+  chunk_tile(a, b, s, r0);
+  const int32_t q0 = __ldg(a.q_off + s), n = __ldg(a.q_off + s + 1) - q0;
+  const int G = a.group, R = n * G;
+  if (r0 >= R || R <= kFewRows) return;
+  int32_t code = 0;
+  const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
+  const KeyRange kr = key_range(a, n, kv, r0 / G, (min(r0 + kChunkRows, R) - 1) / G);
+  const bool single = kr.hi - kr.lo <= a.chunk_split;
+  const int32_t lo = kr.lo + blockIdx.y * a.chunk_split;
+  if (blockIdx.y > 0 && lo >= kr.hi) return;
+  const int32_t hi = min(kr.hi, lo + a.chunk_split);
+  const int32_t *table = a.c.table + s * a.c.table_stride;
+  const int64_t head = hk * a.c.head_stride;
+
+  const int row = r0 + wave * 32 + r32;
+  const int tok = min(row, R - 1) / G, h = hk * G + (min(row, R - 1) - tok * G);
+  const int32_t pos = kv - n + tok;
+  const int32_t pos_lo = kv - n + min(r0 + wave * 32, R - 1) / G;  // the wave's first row
+  s16x8 qf[KS];
+  {
+    const short *qp = a.q + (q0 + tok) * a.q_stride + h * D + h2 * 8;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      qf[k] = *reinterpret_cast<const s16x8 *>(qp + k * 16);
+      if (a.flip) qf[k] ^= short(0x8000);
+    }
+  }
+  f32x16 o[DB] = {};
+  float m = -INFINITY, l = 0.f;
+
+  const int lr = tid / CH, lc = tid % CH;  // this thread's row (of 256 / CH) and chunk
+  s16x8 kreg[LD], vreg[LD];
+  auto load = [&](int32_t j0) {
+#pragma unroll
+    for (int i = 0; i < LD; ++i) {
+      const int64_t at =
+          key_at(a.c, table, min(j0 + i * (256 / CH) + lr, hi - 1), head, code) + lc * 8;
+      kreg[i] = *reinterpret_cast<const s16x8 *>(reinterpret_cast<const short *>(a.c.k) + at);
+      vreg[i] = *reinterpret_cast<const s16x8 *>(reinterpret_cast<const short *>(a.c.v) + at);
+    }
+  };
+  if (lo < hi) load(lo);
+  for (int32_t j0 = lo; j0 < hi; j0 += 64) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < LD; ++i) {
+      const int at = tile_at<D>(i * (256 / CH) + lr, lc);
+      *reinterpret_cast<s16x8 *>(kt + at) = kreg[i];
+      *reinterpret_cast<s16x8 *>(vt + at) = vreg[i];
+    }
+    __syncthreads();
+    if (j0 + 64 < hi) load(j0 + 64);
+    f32x16 sc[2] = {};
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        sc[c] = mfma_32x32x16<BF>(
+            *reinterpret_cast<const s16x8 *>(kt + tile_at<D>(c * 32 + r32, k * 2 + h2)), qf[k],
+            sc[c]);
+    // keys that some row of the wave does not see
+    if (j0 + 63 > pos_lo || j0 + 64 > hi || a.window) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int32_t j = j0 + c * 32 + 8 * (i >> 2) + 4 * h2 + (i & 3);
+          if (j > pos || j >= hi || (a.window && j <= pos - a.window)) sc[c][i] = -INFINITY;
+        }
+    }
+    float top = sc[0][0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[0][i]);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[1][i]);
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    const float m2 = fmaxf(m, top);
+    if (__any(m2 > m)) {
+      const float f = m == -INFINITY ? 0.f : exp2_fast((m - m2) * a.c2);
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) o[d] *= f;
+      m = m2;
+    }
+    const float mc = m == -INFINITY ? 0.f : m * a.c2;
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          p[i] = exp2_fast(fmaf(sc[c][u * 8 + i], a.c2, -mc));
+          l += p[i];
+        }
+        const s16x8 pf = pack8<BF>(p);
+        // keys 4 h2 .. + 3 and 8 + 4 h2 .. + 3 of this 16
+        const int vr = c * 32 + u * 16 + 4 * h2 + ((lane & 15) >> 2);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const int col = d * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+          const s16x4 v0 = read_tr(vt + tile_at<D>(vr, col >> 3) + (col & 7));
+          const s16x4 v1 = read_tr(vt + tile_at<D>(vr + 8, col >> 3) + (col & 7));
+          o[d] = mfma_32x32x16<BF>(__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7), pf,
+                                   o[d]);
+        }
+      }
+  }
+  raise_err(a.err, code);
+  l += __shfl_xor(l, 32, 64);
+  if (row >= R) return;
+  if (single) {
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    short *op = a.out + (q0 + tok) * a.out_stride + h * D;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s16x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = to_16<BF>(o[d][i * 4 + e] * inv);
+        *reinterpret_cast<s16x4 *>(op + d * 32 + i * 8 + h2 * 4) = v;
+      }
+    if (h2 == 0 && a.lse)
+      a.lse[int64_t(q0 + tok) * a.n_heads + h] =
+          l > 0.f ? (m * a.c2 + __log2f(l)) * kLn2 : -INFINITY;
+  } else {
+    const int64_t idx = (int64_t(blockIdx.y) * a.rows + q0 + tok) * a.n_heads + h;
+    float *op = a.chunk_o + idx * D;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4 *>(op + d * 32 + i * 8 + h2 * 4) =
+            f32x4{o[d][i * 4], o[d][i * 4 + 1], o[d][i * 4 + 2], o[d][i * 4 + 3]};
+    if (h2 == 0) a.chunk_ml[idx * 2] = m, a.chunk_ml[idx * 2 + 1] = l;
+  }
+}
+
+// ---- the splits of one row and head, joined in split order: a work-group each
+template <bool BF, int D>
+__global__ void __launch_bounds__(256) k_attn_join(AttnArgs a) {
+  constexpr int PER = 256 / (D / 4);  // splits in flight
+  __shared__ f32x4 part[PER][D / 4];
+  __shared__ float ls[PER];
+  const int32_t t = blockIdx.x / a.n_heads, h = blockIdx.x - t * a.n_heads;
+  const int32_t s = seq_of_row(a.q_off, a.n_seqs, t);
+  const int32_t q0 = __ldg(a.q_off + s), n = __ldg(a.q_off + s + 1) - q0, tok = t - q0;
+  int32_t code = 0;
+  const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
+  const bool few = n * a.group <= kFewRows;
+  int32_t tok0 = 0, tok1 = n - 1;
+  if (!few) {
+    const int32_t r0 = (tok * a.group + h % a.group) / kChunkRows * kChunkRows;
+    tok0 = r0 / a.group;
+    tok1 = (min(r0 + kChunkRows, n * a.group) - 1) / a.group;
+  }
+  const KeyRange kr = key_range(a, n, kv, tok0, tok1);
+  const int32_t len = kr.hi - kr.lo, split = few ? a.few_split : a.chunk_split;
+  if (len <= split) return;  // written whole
+  const int splits = (len + split - 1) / split;
+  const float *po = few ? a.few_o : a.chunk_o, *pml = few ? a.few_ml : a.chunk_ml;
+  const int64_t idx0 = few ? (int64_t(s) * a.few_tokens + tok) * a.n_heads + h
+                           : int64_t(t) * a.n_heads + h;
+  const int64_t step = (few ? int64_t(a.n_seqs) * a.few_tokens : int64_t(a.rows)) * a.n_heads;
+  float top = -INFINITY;
+  for (int i = threadIdx.x & 63; i < splits; i += 64)
+    top = fmaxf(top, pml[(idx0 + i * step) * 2]);
+  for (int w = 32; w; w >>= 1) top = fmaxf(top, __shfl_xor(top, w, 64));
+  const int g = threadIdx.x / (D / 4), c = threadIdx.x % (D / 4);
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  float sum = 0.f;
+  for (int i = g; i < splits; i += PER) {
+    const int64_t idx = idx0 + i * step;
+    const float mi = pml[idx * 2];
+    const float f = mi == -INFINITY ? 0.f : exp2_fast((mi - top) * a.c2);
+    sum += f * pml[idx * 2 + 1];
+    acc += f * *reinterpret_cast<const f32x4 *>(po + idx * D + c * 4);
+  }
+  part[g][c] = acc;
+  if (c == 0) ls[g] = sum;
+  __syncthreads();
+  if (g) return;
+  sum = 0.f;
+  acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < PER; ++i) acc += part[i][c], sum += ls[i];
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  s16x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = to_16<BF>(acc[i] * inv);
+  *reinterpret_cast<s16x4 *>(a.out + t * a.out_stride + h * D + c * 4) = v;
+  if (c == 0 && a.lse)
+    a.lse[int64_t(t) * a.n_heads + h] = sum > 0.f ? (top * a.c2 + __log2f(sum)) * kLn2 : -INFINITY;
+}
+
+// How a call's work is split: from the step's shape and the bound on lengths alone.
+struct Plan {
+  int32_t few_seqs, few_rows, few_tokens, few_split, few_splits;
+  int32_t chunk_seqs, chunk_tiles, chunk_split, chunk_splits;
+};
+
+Plan plan(const fs_step *s, const fs_kv_cache *c, int32_t n_heads, int32_t window) {
+  Plan p = {};
+  const int32_t G = n_heads / c->n_kv_heads;
+  int32_t most = 0;
+  for (int32_t i = 0; i < s->n_seqs; ++i) {
+    const int32_t n = s->q_off_h[i + 1] - s->q_off_h[i];
+    if (n == 0) continue;
+    if (int64_t(n) * G <= kFewRows) {
+      ++p.few_seqs;
+      p.few_tokens = n > p.few_tokens ? n : p.few_tokens;
+    } else {
+      ++p.chunk_seqs;
+      most = n > most ? n : most;
+    }
+  }
+  p.few_rows = p.few_tokens * G;
+  auto keys = [&](int32_t tokens) {  // most keys that a tile of rows sees
+    const int64_t k = window ? int64_t(window) + tokens : s->max_kv;
+    return int32_t(k < s->max_kv ? k : s->max_kv);
+  };
+  auto split_of = [&](int64_t blocks, int32_t len, int32_t want, int32_t least, int32_t &split,
+                      int32_t &splits) {
+    int64_t each = (int64_t(len) * blocks + want - 1) / want;
+    each = (each + 127) / 128 * 128;
+    split = int32_t(each < least ? least : each);
+    splits = len > split ? (len + split - 1) / split : 1;
+  };
+  if (p.few_seqs > 0)
+    split_of(int64_t(p.few_seqs) * c->n_kv_heads, keys(p.few_tokens), 2048, 512, p.few_split,
+             p.few_splits);
+  if (p.chunk_seqs > 0) {
+    p.chunk_tiles =
+        int32_t(int64_t(s->q_off_h[s->n_seqs]) * G / kChunkRows + s->n_seqs);
+    const int32_t toks = kChunkRows / G + 2;
+    split_of(int64_t(p.chunk_tiles) * c->n_kv_heads, keys(most < toks ? most : toks), 512, 1024,
+             p.chunk_split, p.chunk_splits);
+  }
+  return p;
+}
+
+size_t round256(size_t x) { return (x + 255) / 256 * 256; }
+
+// Bytes of the partial results: [rows][D] and [rows][2] floats of each kind.
+struct Space {
+  size_t few_o, few_ml, chunk_o, chunk_ml;
+  size_t total() const { return few_o + few_ml + chunk_o + chunk_ml; }
+};
+Space space(const Plan &p, const fs_step *s, const fs_kv_cache *c, int32_t n_heads) {
+  Space w = {};
+  if (p.few_splits > 1) {
+    const size_t r = size_t(p.few_splits) * s->n_seqs * p.few_tokens * n_heads;
+    w.few_o = round256(r * c->head_dim * 4);
+    w.few_ml = round256(r * 8);
+  }
+  if (p.chunk_splits > 1) {
+    const size_t r = size_t(p.chunk_splits) * s->q_off_h[s->n_seqs] * n_heads;
+    w.chunk_o = round256(r * c->head_dim * 4);
+    w.chunk_ml = round256(r * 8);
+  }
+  return w;
+}
+
+template <bool BF, int D>
+void run(const AttnArgs &a, const Plan &p, hipStream_t stream) {
+  const dim3 block(256);
+  if (p.few_seqs > 0) {
+    const dim3 grid(a.n_seqs, a.c.n_kv_heads, p.few_splits);
+    if (p.few_rows <= 16)
+      hipLaunchKernelGGL((k_attn_few<BF, D, 1>), grid, block, 0, stream, a);
+    else if (p.few_rows <= 32)
+      hipLaunchKernelGGL((k_attn_few<BF, D, 2>), grid, block, 0, stream, a);
+    else
+      hipLaunchKernelGGL((k_attn_few<BF, D, 4>), grid, block, 0, stream, a);
+  }
+  if (p.chunk_seqs > 0)
+    hipLaunchKernelGGL((k_attn_chunk<BF, D>), dim3(p.chunk_tiles * a.c.n_kv_heads, p.chunk_splits),
+                       block, 0, stream, a);
+  if (p.few_splits > 1 || p.chunk_splits > 1)
+    hipLaunchKernelGGL((k_attn_join<BF, D>), dim3(a.rows * a.n_heads), block, 0, stream, a);
 }
 
 }  // namespace
 
-size_t attention_workspace_bytes(const fs_step *, const fs_kv_cache *, int32_t, int32_t) {
-  return 0;
+size_t attention_workspace_bytes(const fs_step *s, const fs_kv_cache *c, int32_t n_heads,
+                                 int32_t window) {
+  return space(plan(s, c, n_heads, window), s, c, n_heads).total();
 }
 
 hipError_t launch_attention(const fs_step *s, const fs_kv_cache *c, int32_t n_heads, float scale,
                             int32_t window, const void *q, int64_t q_stride, void *out,
                             int64_t out_stride, float *lse, void *ws, int32_t *err,
                             hipStream_t stream) {
+  const Plan p = plan(s, c, n_heads, window);
+  const Space w = space(p, s, c, n_heads);
   AttnArgs a;
   a.q_off = s->q_off;
   a.kv_len = s->kv_len;
@@ -100,24 +613,38 @@ hipError_t launch_attention(const fs_step *s, const fs_kv_cache *c, int32_t n_he
   a.rows = s->q_off_h[s->n_seqs];
   a.n_heads = n_heads;
   a.window = window;
+  a.group = n_heads / c->n_kv_heads;
   a.c = dev_cache(c);
   a.q = static_cast<const short *>(q);
   a.out = static_cast<short *>(out);
   a.q_stride = q_stride;
   a.out_stride = out_stride;
   a.lse = lse;
-  a.scale = scale;
+  // a scale of 0 makes every visible score equal; a factor of 0 would turn -inf into NaN
+  const float c2 = (scale < 0.f ? -scale : scale) * 1.44269504088896341f;
+  a.c2 = c2 > 1.2e-38f ? c2 : 1.2e-38f;
+  a.flip = scale < 0.f;
+  a.few_split = p.few_split;
+  a.few_splits = p.few_splits;
+  a.few_tokens = p.few_tokens;
+  a.chunk_split = p.chunk_split;
+  a.chunk_splits = p.chunk_splits;
+  a.chunk_tiles = p.chunk_tiles;
+  char *at = static_cast<char *>(ws);
+  a.few_o = reinterpret_cast<float *>(at);
+  a.few_ml = reinterpret_cast<float *>(at + w.few_o);
+  a.chunk_o = reinterpret_cast<float *>(at + w.few_o + w.few_ml);
+  a.chunk_ml = reinterpret_cast<float *>(at + w.few_o + w.few_ml + w.chunk_o);
   a.err = err;
-  const dim3 grid((int64_t(a.rows) * n_heads + 3) / 4), block(256);
   const bool bf = c->dtype == FS_BF16;
   if (bf && c->head_dim == 128)
-    hipLaunchKernelGGL((k_attention<true, 128>), grid, block, 0, stream, a);
+    run<true, 128>(a, p, stream);
   else if (bf)
-    hipLaunchKernelGGL((k_attention<true, 64>), grid, block, 0, stream, a);
+    run<true, 64>(a, p, stream);
   else if (c->head_dim == 128)
-    hipLaunchKernelGGL((k_attention<false, 128>), grid, block, 0, stream, a);
+    run<false, 128>(a, p, stream);
   else
-    hipLaunchKernelGGL((k_attention<false, 64>), grid, block, 0, stream, a);
+    run<false, 64>(a, p, stream);
   return hipGetLastError();
 }
 
