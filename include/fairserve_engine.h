@@ -33,6 +33,7 @@ typedef enum fs_dtype { FS_BF16 = 0, FS_F16 = 1, FS_F32 = 2 } fs_dtype;
 
 /* The requests of one engine step.  Request s brings the rows q_off[s] .. q_off[s+1]-1 of
  * the step's token matrices (a chunk of its prompt, one decoded token, or none).
+ *   n_seqs   in [0, 65535]
  *   q_off_h  host   [n_seqs+1] int32, q_off_h[0] = 0, non-decreasing
  *   q_off    device [n_seqs+1] int32, same values
  *   kv_len   device [n_seqs] int32: the request's tokens in the cache once this step's

@@ -326,7 +326,10 @@ __global__ void __launch_bounds__(256, 2) k_attn_chunk(AttnArgs a) {
   const int row = r0 + wave * 32 + r32;
   const int tok = min(row, R - 1) / G, h = hk * G + (min(row, R - 1) - tok * G);
   const int32_t pos = kv - n + tok;
-  const int32_t pos_lo = kv - n + min(r0 + wave * 32, R - 1) / G;  // the wave's first row
+  // the wave's first and last row, and the first key that its last row's window leaves
+  const int32_t pos_lo = kv - n + min(r0 + wave * 32, R - 1) / G;
+  const int32_t win_hi =
+      a.window ? kv - n + min(r0 + wave * 32 + 31, R - 1) / G - a.window : INT32_MIN;
   s16x8 qf[KS];
   {
     const short *qp = a.q + (q0 + tok) * a.q_stride + h * D + h2 * 8;
@@ -370,7 +373,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_chunk(AttnArgs a) {
             *reinterpret_cast<const s16x8 *>(kt + tile_at<D>(c * 32 + r32, k * 2 + h2)), qf[k],
             sc[c]);
     // keys that some row of the wave does not see
-    if (j0 + 63 > pos_lo || j0 + 64 > hi || a.window) {
+    if (j0 + 63 > pos_lo || j0 + 64 > hi || j0 <= win_hi) {
 #pragma unroll
       for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -449,31 +452,50 @@ __global__ void __launch_bounds__(256, 2) k_attn_chunk(AttnArgs a) {
 }
 
 // ---- the splits of one row and head, joined in split order: a work-group each
-template <bool BF, int D>
+template <bool BF, int D, bool FEW>
 __global__ void __launch_bounds__(256) k_attn_join(AttnArgs a) {
-  constexpr int PER = 256 / (D / 4);  // splits in flight
+  constexpr int PER = 256 / (D / 4);  // splits side by side
   __shared__ f32x4 part[PER][D / 4];
   __shared__ float ls[PER];
-  const int32_t t = blockIdx.x / a.n_heads, h = blockIdx.x - t * a.n_heads;
-  const int32_t s = seq_of_row(a.q_off, a.n_seqs, t);
-  const int32_t q0 = __ldg(a.q_off + s), n = __ldg(a.q_off + s + 1) - q0, tok = t - q0;
+  const int32_t h = blockIdx.x;
+  int32_t s, tok, q0, n, split;
+  int64_t idx0, step;
+  const float *po, *pml;
+  if constexpr (FEW) {
+    s = blockIdx.y;
+    tok = blockIdx.z;
+    q0 = __ldg(a.q_off + s);
+    n = __ldg(a.q_off + s + 1) - q0;
+    if (tok >= n || n * a.group > kFewRows) return;
+    split = a.few_split;
+    po = a.few_o, pml = a.few_ml;
+    idx0 = (int64_t(s) * a.few_tokens + tok) * a.n_heads + h;
+    step = int64_t(a.n_seqs) * a.few_tokens * a.n_heads;
+  } else {
+    const int32_t t = blockIdx.y * 65535 + blockIdx.z;
+    if (t >= a.rows) return;
+    s = seq_of_row(a.q_off, a.n_seqs, t);
+    q0 = __ldg(a.q_off + s);
+    n = __ldg(a.q_off + s + 1) - q0;
+    tok = t - q0;
+    if (n * a.group <= kFewRows) return;
+    split = a.chunk_split;
+    po = a.chunk_o, pml = a.chunk_ml;
+    idx0 = int64_t(t) * a.n_heads + h;
+    step = int64_t(a.rows) * a.n_heads;
+  }
   int32_t code = 0;
   const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
-  const bool few = n * a.group <= kFewRows;
   int32_t tok0 = 0, tok1 = n - 1;
-  if (!few) {
+  if (!FEW) {
     const int32_t r0 = (tok * a.group + h % a.group) / kChunkRows * kChunkRows;
     tok0 = r0 / a.group;
     tok1 = (min(r0 + kChunkRows, n * a.group) - 1) / a.group;
   }
   const KeyRange kr = key_range(a, n, kv, tok0, tok1);
-  const int32_t len = kr.hi - kr.lo, split = few ? a.few_split : a.chunk_split;
+  const int32_t len = kr.hi - kr.lo;
   if (len <= split) return;  // written whole
   const int splits = (len + split - 1) / split;
-  const float *po = few ? a.few_o : a.chunk_o, *pml = few ? a.few_ml : a.chunk_ml;
-  const int64_t idx0 = few ? (int64_t(s) * a.few_tokens + tok) * a.n_heads + h
-                           : int64_t(t) * a.n_heads + h;
-  const int64_t step = (few ? int64_t(a.n_seqs) * a.few_tokens : int64_t(a.rows)) * a.n_heads;
   float top = -INFINITY;
   for (int i = threadIdx.x & 63; i < splits; i += 64)
     top = fmaxf(top, pml[(idx0 + i * step) * 2]);
@@ -481,6 +503,7 @@ __global__ void __launch_bounds__(256) k_attn_join(AttnArgs a) {
   const int g = threadIdx.x / (D / 4), c = threadIdx.x % (D / 4);
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   float sum = 0.f;
+#pragma unroll 4
   for (int i = g; i < splits; i += PER) {
     const int64_t idx = idx0 + i * step;
     const float mi = pml[idx * 2];
@@ -497,12 +520,13 @@ __global__ void __launch_bounds__(256) k_attn_join(AttnArgs a) {
 #pragma unroll
   for (int i = 0; i < PER; ++i) acc += part[i][c], sum += ls[i];
   const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  const int64_t t = q0 + tok;
   s16x4 v;
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = to_16<BF>(acc[i] * inv);
   *reinterpret_cast<s16x4 *>(a.out + t * a.out_stride + h * D + c * 4) = v;
   if (c == 0 && a.lse)
-    a.lse[int64_t(t) * a.n_heads + h] = sum > 0.f ? (top * a.c2 + __log2f(sum)) * kLn2 : -INFINITY;
+    a.lse[t * a.n_heads + h] = sum > 0.f ? (top * a.c2 + __log2f(sum)) * kLn2 : -INFINITY;
 }
 
 // How a call's work is split: from the step's shape and the bound on lengths alone.
@@ -531,22 +555,22 @@ Plan plan(const fs_step *s, const fs_kv_cache *c, int32_t n_heads, int32_t windo
     const int64_t k = window ? int64_t(window) + tokens : s->max_kv;
     return int32_t(k < s->max_kv ? k : s->max_kv);
   };
-  auto split_of = [&](int64_t blocks, int32_t len, int32_t want, int32_t least, int32_t &split,
-                      int32_t &splits) {
+  auto split_of = [&](int64_t blocks, int32_t len, int32_t want, int32_t least, int32_t most,
+                      int32_t &split, int32_t &splits) {
     int64_t each = (int64_t(len) * blocks + want - 1) / want;
     each = (each + 127) / 128 * 128;
-    split = int32_t(each < least ? least : each);
+    split = int32_t(each < least ? least : each > most ? most : each);
     splits = len > split ? (len + split - 1) / split : 1;
   };
   if (p.few_seqs > 0)
-    split_of(int64_t(p.few_seqs) * c->n_kv_heads, keys(p.few_tokens), 2048, 512, p.few_split,
+    split_of(int64_t(p.few_seqs) * c->n_kv_heads, keys(p.few_tokens), 1024, 512, 1024, p.few_split,
              p.few_splits);
   if (p.chunk_seqs > 0) {
     p.chunk_tiles =
         int32_t(int64_t(s->q_off_h[s->n_seqs]) * G / kChunkRows + s->n_seqs);
     const int32_t toks = kChunkRows / G + 2;
     split_of(int64_t(p.chunk_tiles) * c->n_kv_heads, keys(most < toks ? most : toks), 512, 1024,
-             p.chunk_split, p.chunk_splits);
+             1 << 30, p.chunk_split, p.chunk_splits);
   }
   return p;
 }
@@ -588,8 +612,13 @@ void run(const AttnArgs &a, const Plan &p, hipStream_t stream) {
   if (p.chunk_seqs > 0)
     hipLaunchKernelGGL((k_attn_chunk<BF, D>), dim3(p.chunk_tiles * a.c.n_kv_heads, p.chunk_splits),
                        block, 0, stream, a);
-  if (p.few_splits > 1 || p.chunk_splits > 1)
-    hipLaunchKernelGGL((k_attn_join<BF, D>), dim3(a.rows * a.n_heads), block, 0, stream, a);
+  if (p.few_splits > 1)
+    hipLaunchKernelGGL((k_attn_join<BF, D, true>), dim3(a.n_heads, a.n_seqs, p.few_tokens), block, 0,
+                       stream, a);
+  if (p.chunk_splits > 1)
+    hipLaunchKernelGGL((k_attn_join<BF, D, false>),
+                       dim3(a.n_heads, (a.rows + 65534) / 65535, min(a.rows, 65535)), block, 0,
+                       stream, a);
 }
 
 }  // namespace

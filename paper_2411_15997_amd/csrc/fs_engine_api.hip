@@ -16,7 +16,7 @@ fs_status status_of(hipError_t e) { return e == hipSuccess ? FS_OK : FS_E_HIP; }
 int32_t rows_of(const fs_step *s) { return s->q_off_h[s->n_seqs]; }
 
 fs_status check_step(const fs_step *s, bool lengths) {
-  if (!s || s->n_seqs < 0 || !s->q_off_h || s->q_off_h[0] != 0) return FS_E_ARG;
+  if (!s || s->n_seqs < 0 || s->n_seqs > 65535 || !s->q_off_h || s->q_off_h[0] != 0) return FS_E_ARG;
   for (int32_t i = 0; i < s->n_seqs; ++i)
     if (s->q_off_h[i + 1] < s->q_off_h[i]) return FS_E_ARG;
   if (rows_of(s) > (1 << 30)) return FS_E_ARG;
