@@ -22,6 +22,7 @@ namespace {
 
 constexpr int kFewRows = 64;    // rows (tokens times group) that k_attn_few takes
 constexpr int kChunkRows = 128;  // rows of a work-group of k_attn_chunk
+constexpr int64_t kMostPartial = int64_t(1) << 28;  // bytes of partial results, about
 constexpr float kLn2 = 0.693147180559945309f;
 
 struct AttnArgs {
@@ -100,7 +101,10 @@ __global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
   __shared__ float wm[4][NT * 16], wl[4][NT * 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int r16 = lane & 15, g4 = lane >> 4;
-  const int s = blockIdx.x, hk = blockIdx.y;
+  // Work-groups go to the 8 dies in turn: heads fastest, and each split shifts the
+  // requests by one, so a long request's splits do not gather on one die.
+  const int hk = blockIdx.x % a.c.n_kv_heads, sz = blockIdx.x / a.c.n_kv_heads;
+  const int z = sz / a.n_seqs, s = (sz + z) % a.n_seqs;
   const int32_t q0 = __ldg(a.q_off + s), n = __ldg(a.q_off + s + 1) - q0;
   const int G = a.group, R = n * G;
   if (R <= 0 || R > kFewRows) return;
@@ -108,8 +112,8 @@ __global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
   const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
   const KeyRange kr = key_range(a, n, kv, 0, n - 1);
   const bool single = kr.hi - kr.lo <= a.few_split;
-  const int32_t lo = kr.lo + blockIdx.z * a.few_split;
-  if (blockIdx.z > 0 && lo >= kr.hi) return;
+  const int32_t lo = kr.lo + z * a.few_split;
+  if (z > 0 && lo >= kr.hi) return;
   const int32_t hi = min(kr.hi, lo + a.few_split);
   const int32_t *table = a.c.table + s * a.c.table_stride;
   const int64_t head = hk * a.c.head_stride;
@@ -272,7 +276,7 @@ __global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
                 sum > 0.f ? (top * a.c2 + __log2f(sum)) * kLn2 : -INFINITY;
         } else {
           const int64_t idx =
-              ((int64_t(blockIdx.z) * a.n_seqs + s) * a.few_tokens + tok) * a.n_heads + h;
+              ((int64_t(z) * a.n_seqs + s) * a.few_tokens + tok) * a.n_heads + h;
           *reinterpret_cast<f32x4 *>(a.few_o + idx * D + cc) = acc;
           if (cc == 0) a.few_ml[idx * 2] = top, a.few_ml[idx * 2 + 1] = sum;
         }
@@ -556,21 +560,28 @@ Plan plan(const fs_step *s, const fs_kv_cache *c, int32_t n_heads, int32_t windo
     return int32_t(k < s->max_kv ? k : s->max_kv);
   };
   auto split_of = [&](int64_t blocks, int32_t len, int32_t want, int32_t least, int32_t most,
-                      int32_t &split, int32_t &splits) {
+                      int64_t rows, int32_t &split, int32_t &splits) {
+    const int64_t bytes = rows * n_heads * (c->head_dim + 2) * 4;  // of one split
+    int64_t most_splits = kMostPartial / bytes;
+    most_splits = most_splits < 4 ? 4 : most_splits > 512 ? 512 : most_splits;
     int64_t each = (int64_t(len) * blocks + want - 1) / want;
     each = (each + 127) / 128 * 128;
-    split = int32_t(each < least ? least : each > most ? most : each);
+    each = each < least ? least : each > most ? most : each;
+    // no more splits than their partial results may take, whatever the bound on lengths
+    const int64_t few = (int64_t(len) + most_splits - 1) / most_splits;
+    if (each < few) each = (few + 127) / 128 * 128;
+    split = int32_t(each);
     splits = len > split ? (len + split - 1) / split : 1;
   };
   if (p.few_seqs > 0)
-    split_of(int64_t(p.few_seqs) * c->n_kv_heads, keys(p.few_tokens), 1024, 512, 1024, p.few_split,
-             p.few_splits);
+    split_of(int64_t(p.few_seqs) * c->n_kv_heads, keys(p.few_tokens), 1024, 512, 1024,
+             int64_t(s->n_seqs) * p.few_tokens, p.few_split, p.few_splits);
   if (p.chunk_seqs > 0) {
     p.chunk_tiles =
         int32_t(int64_t(s->q_off_h[s->n_seqs]) * G / kChunkRows + s->n_seqs);
     const int32_t toks = kChunkRows / G + 2;
     split_of(int64_t(p.chunk_tiles) * c->n_kv_heads, keys(most < toks ? most : toks), 512, 1024,
-             1 << 30, p.chunk_split, p.chunk_splits);
+             1 << 30, s->q_off_h[s->n_seqs], p.chunk_split, p.chunk_splits);
   }
   return p;
 }
@@ -601,7 +612,7 @@ template <bool BF, int D>
 void run(const AttnArgs &a, const Plan &p, hipStream_t stream) {
   const dim3 block(256);
   if (p.few_seqs > 0) {
-    const dim3 grid(a.n_seqs, a.c.n_kv_heads, p.few_splits);
+    const dim3 grid(uint32_t(a.n_seqs) * a.c.n_kv_heads * p.few_splits);
     if (p.few_rows <= 16)
       hipLaunchKernelGGL((k_attn_few<BF, D, 1>), grid, block, 0, stream, a);
     else if (p.few_rows <= 32)

@@ -28,7 +28,7 @@ fs_status check_step(const fs_step *s, bool lengths) {
 
 fs_status check_cache(const fs_step *s, const fs_kv_cache *c, int32_t most_dim) {
   if (!c || (c->dtype != FS_BF16 && c->dtype != FS_F16)) return FS_E_ARG;
-  if (c->n_kv_heads < 1 || c->n_kv_heads > 65535 || c->head_dim < 8 || c->head_dim > most_dim ||
+  if (c->n_kv_heads < 1 || c->n_kv_heads > 1024 || c->head_dim < 8 || c->head_dim > most_dim ||
       !mult8(c->head_dim))
     return FS_E_ARG;
   if (c->page_size < 1 || c->page_size > 4096 || (c->page_size & (c->page_size - 1)))

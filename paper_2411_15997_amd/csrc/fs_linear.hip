@@ -1,9 +1,14 @@
 // A projection with every request's own low-rank adapter beside the shared weight:
 //   y = x W^T + scale_a (x A_a^T) B_a^T,   a = the row's request's adapter.
-// Two launches: k_shrink makes h = scale x A_a^T per request in fp32 and stores it as the
-// sum of two 16-bit values; k_linear runs the product over K and then goes on over the
-// few columns of h against B_a in the same accumulators, so y is written once and never
-// read.
+// Two launches.  k_shrink makes h = scale x A_a^T per request in fp32 and stores it as the
+// sum of two 16-bit values, with the row's adapter beside it.  The product then runs over
+// K and goes on over the few columns of h against B_a in the same accumulators, so y is
+// written once and never read:
+//   k_linear_few   up to 256 rows: bound by the bytes of W.  A work-group takes 16 or 32
+//                  columns of y; its eight waves share out K and join in LDS.
+//   k_linear_tile  more rows: bound by the matrix cores.  W and x go through LDS in tiles.
+// W is the first operand (its rows are y's columns), so a lane holds neighbouring columns
+// of one row of y.
 #include "fs_engine.h"
 
 namespace fs {
@@ -16,7 +21,8 @@ struct LinArgs {
   int32_t n_seqs, rows, K, N, n_adapters, R;  // R: max_rank (0: no adapters)
   const short *x, *w, *a, *b;
   short *y;
-  short *h;  // [rows][2R]: high parts, low parts
+  short *h;         // [rows][2R]: high parts, low parts
+  int32_t *row_ad;  // [rows]: the row's adapter, -1 when it has none
   int64_t x_stride, y_stride;
   int32_t *err;
 };
@@ -38,118 +44,352 @@ __device__ inline int32_t adapter_of(const LinArgs &g, int32_t s, int32_t &rank,
   return a;
 }
 
-// One request's rows, 16 at a time, against 16 of its adapter's A rows; the four waves
-// share out K and join in LDS.
-template <bool BF>
-__global__ void __launch_bounds__(256) k_shrink(LinArgs g) {
-  __shared__ float part[4][16][17];
+// One request's rows, 16 at a time, against its adapter's A; the waves share out K and
+// join in LDS.  JT: 16-column tiles of h.
+template <bool BF, int JT, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64) k_shrink(LinArgs g) {
+  __shared__ float part[WAVES][16][JT * 16 + 1];
   const RowTile t = row_tile<4>(g.q_off, g.n_seqs, blockIdx.x);
   if (t.rows <= 0) return;
   int32_t code = 0, rank;
   const int32_t ad = adapter_of(g, t.s, rank, code);
-  if (threadIdx.x == 0 && blockIdx.y == 0) raise_err(g.err, code);
-  const int j0 = blockIdx.y * 16;
-  if (ad < 0) return;  // k_linear does not look at h for such rows
+  if (threadIdx.x == 0) raise_err(g.err, code);
+  if (threadIdx.x < t.rows) g.row_ad[t.row0 + threadIdx.x] = rank > 0 ? ad : -1;
+  if (ad < 0 || rank == 0) return;  // h of such rows is not looked at
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int r = lane & 15, kq = (lane >> 4) * 8;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  if (j0 < rank) {
-    const short *xp = g.x + int64_t(t.row0 + min(r, t.rows - 1)) * g.x_stride;
-    const short *ap = g.a + (int64_t(ad) * g.R + min(j0 + r, rank - 1)) * g.K;
-    const s16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (int k = wave * 32 + kq; k < (g.K + 31) / 32 * 32; k += 128) {
-      const s16x8 xv = k < g.K ? *reinterpret_cast<const s16x8 *>(xp + k) : zero;
-      const s16x8 av = k < g.K ? *reinterpret_cast<const s16x8 *>(ap + k) : zero;
-      acc = mfma_16x16x32<BF>(xv, av, acc);
+  f32x4 acc[JT] = {};
+  const short *xp = g.x + int64_t(t.row0 + min(r, t.rows - 1)) * g.x_stride;
+  const short *ap[JT];
+#pragma unroll
+  for (int j = 0; j < JT; ++j) ap[j] = g.a + (int64_t(ad) * g.R + min(j * 16 + r, rank - 1)) * g.K;
+  const s16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+  // a wave takes 128 of K at a time
+  for (int k0 = wave * 128; k0 < g.K; k0 += WAVES * 128) {
+    s16x8 xv[4], av[JT][4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int k = k0 + u * 32 + kq;
+      xv[u] = k < g.K ? *reinterpret_cast<const s16x8 *>(xp + k) : zero;
+#pragma unroll
+      for (int j = 0; j < JT; ++j)
+        av[j][u] = k < g.K ? *reinterpret_cast<const s16x8 *>(ap[j] + k) : zero;
     }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int j = 0; j < JT; ++j) acc[j] = mfma_16x16x32<BF>(xv[u], av[j][u], acc[j]);
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) part[wave][(lane >> 4) * 4 + i][r] = acc[i];
+  for (int j = 0; j < JT; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) part[wave][(lane >> 4) * 4 + i][j * 16 + r] = acc[j][i];
   __syncthreads();
-  const int row = threadIdx.x >> 4, j = threadIdx.x & 15;
-  if (row < t.rows && j0 + j < g.R) {
-    float v = (part[0][row][j] + part[1][row][j]) + (part[2][row][j] + part[3][row][j]);
-    v = j0 + j < rank ? v * (g.scale ? __ldg(g.scale + ad) : 1.f) : 0.f;
+  const float scale = g.scale ? __ldg(g.scale + ad) : 1.f;
+  for (int e = threadIdx.x; e < 16 * JT * 16; e += WAVES * 64) {
+    const int row = e / (JT * 16), j = e % (JT * 16);
+    if (row >= t.rows || j >= g.R) continue;
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) v += part[w][row][j];
+    v = j < rank ? v * scale : 0.f;
     const short hi = to_16<BF>(v);
-    short *hp = g.h + int64_t(t.row0 + row) * (2 * g.R) + j0 + j;
+    short *hp = g.h + int64_t(t.row0 + row) * (2 * g.R) + j;
     hp[0] = hi;
     hp[g.R] = to_16<BF>(v - to_f32<BF>(hi));
   }
 }
 
-// One wave: 16 rows by 64 columns, operands straight from memory in the matrix cores'
-// layout.
-template <bool BF>
-__global__ void __launch_bounds__(256) k_linear(LinArgs g) {
+// B_a[n][j .. j + 7], columns at and beyond the rank as 0.
+__device__ inline s16x8 load_b(const LinArgs &g, int32_t ad, int32_t rank, int32_t n, int j) {
+  s16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (j < rank) {
+    v = *reinterpret_cast<const s16x8 *>(g.b + (int64_t(ad) * g.N + n) * g.R + j);
+    if (j + 8 > rank)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = j + i < rank ? v[i] : short(0);
+  }
+  return v;
+}
+__device__ inline int32_t rank_of(const LinArgs &g, int32_t ad) {
+  return g.rank ? min(__ldg(g.rank + ad), g.R) : g.R;
+}
+
+// ---- few rows: MT tiles of 16 rows by NT tiles of 16 columns
+template <bool BF, int MT, int NT>
+__global__ void __launch_bounds__(512) k_linear_few(LinArgs g) {
+  __shared__ f32x4 part[8][MT * NT][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int r = lane & 15, kq = (lane >> 4) * 8;
-  const int n0 = (blockIdx.x * 4 + wave) * 64, m0 = blockIdx.y * 16;
-  if (n0 >= g.N) return;
-  const int row = min(m0 + r, g.rows - 1);
+  const int n0 = blockIdx.x * (NT * 16), m0 = blockIdx.y * (MT * 16);
   const s16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
-  f32x4 acc[4] = {};
-  const short *xp = g.x + int64_t(row) * g.x_stride;
-  const short *wp[4];
+  f32x4 acc[MT][NT] = {};
+  const short *xp[MT], *wp[NT];
 #pragma unroll
-  for (int c = 0; c < 4; ++c) wp[c] = g.w + int64_t(min(n0 + 16 * c + r, g.N - 1)) * g.K;
-  for (int k = kq; k < (g.K + 31) / 32 * 32; k += 32) {
-    const s16x8 xv = k < g.K ? *reinterpret_cast<const s16x8 *>(xp + k) : zero;
+  for (int m = 0; m < MT; ++m)
+    xp[m] = g.x + int64_t(min(m0 + m * 16 + r, g.rows - 1)) * g.x_stride + kq;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const s16x8 wv = k < g.K ? *reinterpret_cast<const s16x8 *>(wp[c] + k) : zero;
-      acc[c] = mfma_16x16x32<BF>(xv, wv, acc[c]);
+  for (int n = 0; n < NT; ++n) wp[n] = g.w + int64_t(min(n0 + n * 16 + r, g.N - 1)) * g.K + kq;
+  // a wave takes 128 of K at a time
+  int k0 = wave * 128;
+  for (; k0 + 128 <= g.K; k0 += 1024) {
+    s16x8 wv[NT][4], xv[MT][4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        wv[n][u] = *reinterpret_cast<const s16x8 *>(wp[n] + k0 + u * 32);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+        xv[m][u] = *reinterpret_cast<const s16x8 *>(xp[m] + k0 + u * 32);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[m][n] = mfma_16x16x32<BF>(wv[n][u], xv[m][u], acc[m][n]);
+  }
+  if (k0 < g.K) {
+    for (int u = 0; u < 4; ++u) {
+      const int k = k0 + u * 32;
+      const bool in = k + kq < g.K;
+      s16x8 wv[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        wv[n] = in ? *reinterpret_cast<const s16x8 *>(wp[n] + k) : zero;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const s16x8 xv = in ? *reinterpret_cast<const s16x8 *>(xp[m] + k) : zero;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[m][n] = mfma_16x16x32<BF>(wv[n], xv, acc[m][n]);
+      }
     }
   }
   if (g.n_adapters > 0) {
-    const int last = min(m0 + 15, g.rows - 1);
-    for (int s = seq_of_row(g.q_off, g.n_seqs, m0); s < g.n_seqs && __ldg(g.q_off + s) <= last;
-         ++s) {
-      int32_t code = 0, rank;
-      const int32_t ad = adapter_of(g, s, rank, code);
-      if (ad < 0 || rank == 0) continue;
-      const bool mine = m0 + r >= __ldg(g.q_off + s) && m0 + r < __ldg(g.q_off + s + 1);
-      const short *hp = g.h + int64_t(row) * (2 * g.R);
-      // chunks of 8 columns: R/8 high ones, then R/8 low ones
-      for (int c8 = lane >> 4; c8 < (g.R / 4 + 3) / 4 * 4; c8 += 4) {
-        const bool in = c8 < g.R / 4;
-        const s16x8 hv = mine && in ? *reinterpret_cast<const s16x8 *>(hp + c8 * 8) : zero;
-        const int j = (c8 < g.R / 8 ? c8 : c8 - g.R / 8) * 8;
+    // the distinct adapters of a tile's rows, shared out over the waves that hold the tile
+    const int chunks = g.R / 8;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          s16x8 bv = zero;
-          if (in && j < rank) {
-            bv = *reinterpret_cast<const s16x8 *>(
-                g.b + (int64_t(ad) * g.N + min(n0 + 16 * c + r, g.N - 1)) * g.R + j);
+    for (int m = 0; m < MT; ++m) {
+      if (wave % MT != m) continue;
+      const int row = m0 + m * 16 + r;
+      const int32_t ad = row < g.rows ? __ldg(g.row_ad + row) : -1;
+      const short *hp = g.h + int64_t(min(row, g.rows - 1)) * (2 * g.R);
+      uint64_t left = __ballot(ad >= 0);
+      for (int turn = 0; left; ++turn) {
+        const int32_t a = __builtin_amdgcn_readlane(ad, __builtin_ctzll(left));
+        const bool mine = ad == a;
+        left &= ~__ballot(mine);
+        if (turn % (8 / MT) != wave / MT) continue;
+        const int32_t rank = rank_of(g, a);
+        // chunks of 8 columns: R/8 high ones, then R/8 low ones
+        for (int c = lane >> 4; c < (2 * chunks + 3) / 4 * 4; c += 4) {
+          const bool in = c < 2 * chunks;
+          const s16x8 hv = mine && in ? *reinterpret_cast<const s16x8 *>(hp + c * 8) : zero;
+          const int j = in ? (c < chunks ? c : c - chunks) * 8 : g.R;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) bv[i] = j + i < rank ? bv[i] : short(0);
-          }
-          acc[c] = mfma_16x16x32<BF>(hv, bv, acc[c]);
+          for (int n = 0; n < NT; ++n)
+            acc[m][n] = mfma_16x16x32<BF>(
+                load_b(g, a, rank, min(n0 + n * 16 + r, g.N - 1), j), hv, acc[m][n]);
         }
       }
     }
   }
 #pragma unroll
-  for (int c = 0; c < 4; ++c)
+  for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int m = m0 + (lane >> 4) * 4 + i, n = n0 + 16 * c + r;
-      if (m < g.rows && n < g.N) g.y[int64_t(m) * g.y_stride + n] = to_16<BF>(acc[c][i]);
+    for (int n = 0; n < NT; ++n) part[wave][m * NT + n][lane] = acc[m][n];
+  __syncthreads();
+  for (int t = wave; t < MT * NT; t += 8) {
+    f32x4 v = part[0][t][lane];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) v += part[w][t][lane];
+    const int row = m0 + (t / NT) * 16 + r, n = n0 + (t % NT) * 16 + (lane >> 4) * 4;
+    if (row < g.rows && n < g.N) {
+      s16x4 o;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = to_16<BF>(v[i]);
+      *reinterpret_cast<s16x4 *>(g.y + int64_t(row) * g.y_stride + n) = o;
     }
+  }
+}
+
+// Where 16-byte chunk c of row r lies in an LDS tile of 64-element rows.
+__device__ inline int gemm_at(int r, int c) { return r * 64 + ((c ^ ((r >> 1) & 7)) * 8); }
+
+// ---- many rows: BM rows by BN columns a work-group, K in steps of 64 through two LDS
+// buffers; a wave takes WM rows by WN columns.
+template <bool BF, int BM, int BN, int WM, int WN>
+__global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) k_linear_tile(LinArgs g) {
+  constexpr int THREADS = (BM / WM) * (BN / WN) * 64;
+  constexpr int MT = WM / 32, NT = WN / 32;
+  constexpr int LX = BM * 8 / THREADS, LW = BN * 8 / THREADS;  // 16-byte chunks a thread loads
+  __shared__ __align__(16) short xs[2][BM * 64], wsm[2][BN * 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int r32 = lane & 31, h2 = lane >> 5;
+
+  // Work-groups go to the 8 dies in turn: each die takes a run of neighbouring tiles, in
+  // strips of 8 row tiles, so that its L2 serves the x and W they share.
+  const int tm = (g.rows + BM - 1) / BM, tn = (g.N + BN - 1) / BN, total = tm * tn;
+  int id = blockIdx.x;
+  {
+    const int die = id & 7, per = total >> 3, extra = total & 7;
+    id = die * per + min(die, extra) + (id >> 3);
+  }
+  const int strip = 8 * tn, first = id / strip * 8, width = min(8, tm - first);
+  const int m0 = (first + (id % strip) % width) * BM, n0 = (id % strip) / width * BN;
+
+  const int wm = (wave % (BM / WM)) * WM, wn = (wave / (BM / WM)) * WN;
+  f32x16 acc[MT][NT] = {};
+  s16x8 xr[LX], wr[LW];
+  const int lrow = tid >> 3, lc = tid & 7;
+  const s16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+  const short *xp[LX], *wp[LW];
+#pragma unroll
+  for (int i = 0; i < LX; ++i)
+    xp[i] = g.x + int64_t(min(m0 + lrow + i * (THREADS / 8), g.rows - 1)) * g.x_stride + lc * 8;
+#pragma unroll
+  for (int i = 0; i < LW; ++i)
+    wp[i] = g.w + int64_t(min(n0 + lrow + i * (THREADS / 8), g.N - 1)) * g.K + lc * 8;
+  auto load = [&](int k) {
+    const bool in = k + lc * 8 < g.K;
+#pragma unroll
+    for (int i = 0; i < LX; ++i) xr[i] = in ? *reinterpret_cast<const s16x8 *>(xp[i] + k) : zero;
+#pragma unroll
+    for (int i = 0; i < LW; ++i) wr[i] = in ? *reinterpret_cast<const s16x8 *>(wp[i] + k) : zero;
+  };
+  auto store = [&](int b) {
+#pragma unroll
+    for (int i = 0; i < LX; ++i)
+      *reinterpret_cast<s16x8 *>(&xs[b][gemm_at(lrow + i * (THREADS / 8), lc)]) = xr[i];
+#pragma unroll
+    for (int i = 0; i < LW; ++i)
+      *reinterpret_cast<s16x8 *>(&wsm[b][gemm_at(lrow + i * (THREADS / 8), lc)]) = wr[i];
+  };
+  load(0);
+  store(0);
+  __syncthreads();
+  int b = 0;
+  for (int k = 0; k < g.K; k += 64, b ^= 1) {
+    if (k + 64 < g.K) load(k + 64);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      s16x8 xf[MT], wf[NT];
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+        xf[m] = *reinterpret_cast<const s16x8 *>(&xs[b][gemm_at(wm + m * 32 + r32, u * 2 + h2)]);
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        wf[n] = *reinterpret_cast<const s16x8 *>(&wsm[b][gemm_at(wn + n * 32 + r32, u * 2 + h2)]);
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[m][n] = mfma_32x32x16<BF>(wf[n], xf[m], acc[m][n]);
+    }
+    if (k + 64 < g.K) store(b ^ 1);
+    __syncthreads();
+  }
+  if (g.n_adapters > 0) {
+    const int chunks = g.R / 8;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const int row = m0 + wm + m * 32 + r32;
+      const int32_t ad = row < g.rows ? __ldg(g.row_ad + row) : -1;
+      const short *hp = g.h + int64_t(min(row, g.rows - 1)) * (2 * g.R);
+      uint64_t left = __ballot(ad >= 0);
+      while (left) {
+        const int32_t a = __builtin_amdgcn_readlane(ad, __builtin_ctzll(left));
+        const bool mine = ad == a;
+        left &= ~__ballot(mine);
+        const int32_t rank = rank_of(g, a);
+        for (int c = h2; c < 2 * chunks; c += 2) {
+          const s16x8 hv = mine ? *reinterpret_cast<const s16x8 *>(hp + c * 8) : zero;
+          const int j = (c < chunks ? c : c - chunks) * 8;
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            acc[m][n] = mfma_32x32x16<BF>(
+                load_b(g, a, rank, min(n0 + wn + n * 32 + r32, g.N - 1), j), hv, acc[m][n]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int row = m0 + wm + m * 32 + r32;
+    if (row >= g.rows) continue;
+    short *yp = g.y + int64_t(row) * g.y_stride;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int col = n0 + wn + n * 32 + i * 8 + h2 * 4;
+        s16x4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = to_16<BF>(acc[m][n][i * 4 + e]);
+        if (col < g.N) *reinterpret_cast<s16x4 *>(yp + col) = o;
+      }
+  }
+}
+
+template <bool BF, int JT>
+void shrink(const LinArgs &g, int64_t tiles, hipStream_t stream) {
+  // few tiles: more waves share out K, so that one tile's time is short
+  if (tiles <= 512 && JT <= 4)
+    hipLaunchKernelGGL((k_shrink<BF, JT, 16>), dim3(tiles), dim3(1024), 0, stream, g);
+  else
+    hipLaunchKernelGGL((k_shrink<BF, JT, 4>), dim3(tiles), dim3(256), 0, stream, g);
+}
+
+template <bool BF, int MT>
+void few(const LinArgs &g, hipStream_t stream) {
+  const int mb = (g.rows + MT * 16 - 1) / (MT * 16);
+  // 16 columns a work-group while that does not exceed the compute units
+  if ((g.N + 15) / 16 * mb <= 256)
+    hipLaunchKernelGGL((k_linear_few<BF, MT, 1>), dim3((g.N + 15) / 16, mb), dim3(512), 0, stream,
+                       g);
+  else
+    hipLaunchKernelGGL((k_linear_few<BF, MT, 2>), dim3((g.N + 31) / 32, mb), dim3(512), 0, stream,
+                       g);
 }
 
 template <bool BF>
 void run(const LinArgs &g, int64_t tiles, hipStream_t stream) {
-  if (g.n_adapters > 0)
-    hipLaunchKernelGGL(k_shrink<BF>, dim3(tiles, (g.R + 15) / 16), dim3(256), 0, stream, g);
-  hipLaunchKernelGGL(k_linear<BF>, dim3((g.N + 255) / 256, (g.rows + 15) / 16), dim3(256), 0,
-                     stream, g);
+  if (g.n_adapters > 0) {
+    if (g.R <= 16)
+      shrink<BF, 1>(g, tiles, stream);
+    else if (g.R <= 32)
+      shrink<BF, 2>(g, tiles, stream);
+    else if (g.R <= 64)
+      shrink<BF, 4>(g, tiles, stream);
+    else
+      shrink<BF, 8>(g, tiles, stream);
+  }
+  if (g.rows <= 256) {
+    if (g.rows <= 16)
+      few<BF, 1>(g, stream);
+    else if (g.rows <= 32)
+      few<BF, 2>(g, stream);
+    else
+      few<BF, 4>(g, stream);
+    return;
+  }
+  const int64_t big = int64_t((g.rows + 255) / 256) * ((g.N + 255) / 256);
+  if (big >= 256) {
+    hipLaunchKernelGGL((k_linear_tile<BF, 256, 256, 128, 64>), dim3(big), dim3(512), 0, stream, g);
+  } else {
+    const int64_t n = int64_t((g.rows + 127) / 128) * ((g.N + 127) / 128);
+    hipLaunchKernelGGL((k_linear_tile<BF, 128, 128, 64, 64>), dim3(n), dim3(256), 0, stream, g);
+  }
 }
 
 }  // namespace
 
 size_t adapter_workspace_bytes(const fs_step *s, const fs_adapters *ad) {
   if (ad->n_adapters == 0) return 0;
-  return size_t(s->q_off_h[s->n_seqs]) * ad->max_rank * 4;
+  return size_t(s->q_off_h[s->n_seqs]) * (ad->max_rank + 1) * 4;
 }
 
 hipError_t launch_adapter_linear(const fs_step *s, const fs_adapters *ad, const void *x,
@@ -172,6 +412,7 @@ hipError_t launch_adapter_linear(const fs_step *s, const fs_adapters *ad, const 
   g.b = static_cast<const short *>(ad->b);
   g.y = static_cast<short *>(y);
   g.h = static_cast<short *>(ws);
+  g.row_ad = static_cast<int32_t *>(ws) + size_t(g.rows) * g.R;
   g.x_stride = x_stride;
   g.y_stride = y_stride;
   g.err = err;
