@@ -27,6 +27,8 @@ struct SampleArgs {
 };
 
 constexpr int kThreads = 1024;
+constexpr int kWaves = kThreads / 64;
+constexpr int kAhead = 4;  // 16-byte loads of a thread in flight
 constexpr double kOne = 1099511627776.0;  // 2^40
 
 // Order-preserving key: larger logit, larger key; -0 as 0; NaN as -inf.  -inf is kLow.
@@ -48,11 +50,12 @@ __device__ inline float load_logit(const char *row, int32_t i) {
     return to_f32<DT == FS_BF16>(reinterpret_cast<const short *>(row)[i]);
 }
 
-// A row as groups of consecutive tokens: the ones before the first 16-byte boundary, the
-// 16-byte vectors, the ones after the last vector.
+// A row as the tokens before the first 16-byte boundary, 16-byte vectors, and the tokens
+// after the last vector.
 template <int DT>
 struct Row {
   static constexpr int kVec = DT == FS_F32 ? 4 : 8;
+  typedef s16x8 Raw;  // 16 bytes
   const char *p;
   int32_t head, vecs, vocab;
   __device__ Row(const char *base, int32_t V) : p(base), vocab(V) {
@@ -60,73 +63,129 @@ struct Row {
     head = min(V, int32_t((16 - (reinterpret_cast<uintptr_t>(base) & 15)) & 15) / size);
     vecs = (V - head) / kVec;
   }
-  __device__ int32_t groups() const { return vecs + 2; }
-  // f(id, logit) for the tokens of a group, in order
+  __device__ int32_t tail() const { return head + vecs * kVec; }
+  __device__ Raw load(int32_t v) const {  // vector v, or any other when there is no such
+    const int32_t i = head + min(v, vecs - 1) * kVec;
+    return *reinterpret_cast<const Raw *>(p + int64_t(i) * (16 / kVec));
+  }
+  __device__ static float at(const Raw &v, int e) {  // e known at compile time
+    if constexpr (DT == FS_F32)
+      return __builtin_bit_cast(f32x4, v)[e];
+    else
+      return to_f32<DT == FS_BF16>(v[e]);
+  }
+  __device__ static float pick(const Raw &v, int e) {  // e from 0 to kVec - 1
+    typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+    const u32x4 w = __builtin_bit_cast(u32x4, v);
+    const int d = DT == FS_F32 ? e : e >> 1;
+    const uint32_t lo = d & 1 ? w[1] : w[0], hi = d & 1 ? w[3] : w[2];
+    const uint32_t x = d & 2 ? hi : lo;
+    if constexpr (DT == FS_F32)
+      return __uint_as_float(x);
+    else
+      return to_f32<DT == FS_BF16>(short(e & 1 ? x >> 16 : x));
+  }
+  // f(id, logit) for every token of the row, in no order; the next loads are in flight
+  // while a batch is worked on
   template <class F>
-  __device__ void visit(int32_t g, F f) const {
-    if (g >= 1 && g <= vecs) {
-      const int32_t i0 = head + (g - 1) * kVec;
-      if constexpr (DT == FS_F32) {
-        const f32x4 v = *reinterpret_cast<const f32x4 *>(p + int64_t(i0) * 4);
+  __device__ void each(F f) const {
+    const int tid = threadIdx.x, odd = head + vocab - tail();
+    if (tid < odd) {
+      const int32_t i = tid < head ? tid : tail() + tid - head;
+      f(i, load_logit<DT>(p, i));
+    }
+    if (vecs == 0) return;
+    Raw q[kAhead];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f(i0 + e, v[e]);
-      } else {
-        const s16x8 v = *reinterpret_cast<const s16x8 *>(p + int64_t(i0) * 2);
+    for (int u = 0; u < kAhead; ++u) q[u] = load(tid + u * kThreads);
+    // the body once, not once for each load in flight: the passes' code then stays in the
+    // instruction cache
+#pragma unroll 1
+    for (int32_t v = tid; v < vecs; v += kThreads) {
+      const Raw x = q[0];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f(i0 + e, to_f32<DT == FS_BF16>(v[e]));
-      }
-    } else if (g < groups()) {
-      const int32_t i0 = g == 0 ? 0 : head + vecs * kVec, i1 = g == 0 ? head : vocab;
-      for (int32_t i = i0; i < i1; ++i) f(i, load_logit<DT>(p, i));
+      for (int u = 0; u + 1 < kAhead; ++u) q[u] = q[u + 1];
+      q[kAhead - 1] = load(v + kAhead * kThreads);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) f(head + v * kVec + e, at(x, e));
     }
   }
 };
 
-// 2^-y for y >= 0 times 2^40, rounded down.  2^f for |f| <= 1/2 by the Taylor series of
-// exp(f ln 2) (degree 12: below 2e-16 of the value).
-__device__ inline uint64_t weight_of(double y) {
-  const double k = rint(-y), z = (-y - k) * 0.693147180559945309417;
-  double p = 2.08767569878680989792e-9;  // 1/12!
-  p = fma(p, z, 2.50521083854417187751e-8);
-  p = fma(p, z, 2.75573192239858906526e-7);
-  p = fma(p, z, 2.75573192239858906526e-6);
-  p = fma(p, z, 2.48015873015873015873e-5);
-  p = fma(p, z, 1.98412698412698412698e-4);
-  p = fma(p, z, 1.38888888888888888889e-3);
-  p = fma(p, z, 8.33333333333333333333e-3);
-  p = fma(p, z, 4.16666666666666666667e-2);
-  p = fma(p, z, 1.66666666666666666667e-1);
-  p = fma(p, z, 0.5);
-  p = fma(p, z, 1.0);
-  p = fma(p, z, 1.0);
-  // a whole number below 2^52 lies in the low bits of its sum with 2^52
-  const double w = floor(ldexp(p, int(k) + 40)) + 4503599627370496.0;
-  return y < 41.0 ? uint64_t(__double_as_longlong(w)) & ((uint64_t(1) << 52) - 1) : 0;
-}
-
+// The weight of a logit: floor(2^(40 - y)), y = (largest - x) * per >= 0.  2^-y is taken as
+// 2^-n * 2^-(j/64) * e^z with a table of the 64 middle factors and |z| <= ln(2) / 128, whose
+// series ends below 4e-17 of the value at degree 5.
 struct Weigh {
-  uint32_t top;  // key of the largest logit
+  float top;  // the largest logit
   double best, per;
-  // the exponent: weight 2^(40 - y); 0 for the largest logit, whatever it is
-  __device__ double y_of(uint32_t key) const {
-    return key == top ? 0.0 : __dmul_rn(__dsub_rn(best, double(value_of(key))), per);
+  const double *table;  // 2^(-j/64)
+  __device__ double y_of(float x) const {
+    return x == top ? 0.0 : __dmul_rn(__dsub_rn(best, double(x)), per);
   }
-  __device__ uint64_t operator()(uint32_t key) const { return weight_of(y_of(key)); }
+  __device__ uint64_t of_y(double y) const {
+    // the nearest multiple of 1/64: the sum's low bits are its number of 64ths
+    const double s = fma(y, 64.0, 6755399441055744.0);  // 1.5 * 2^52
+    const int q = int(uint32_t(__double_as_longlong(s)));
+    const double z = fma(s - 6755399441055744.0, 0.015625, -y) * 0.693147180559945309417;
+    double p = 8.33333333333333333333e-3;
+    p = fma(p, z, 4.16666666666666666667e-2);
+    p = fma(p, z, 1.66666666666666666667e-1);
+    p = fma(p, z, 0.5);
+    p = fma(p, z, 1.0);
+    p = fma(p, z, 1.0);
+    // 2^(40 - q/64) times it, rounded down: its mantissa shifted right
+    const uint64_t bits = uint64_t(__double_as_longlong(p * table[q & 63]));
+    const uint64_t mant = (bits & 0xfffffffffffffull) | 0x10000000000000ull;
+    const int shift = 12 + (q >> 6) + 1023 - int(bits >> 52);
+    return y < 41.0 ? mant >> (shift & 63) : 0;
+  }
+  __device__ uint64_t operator()(float x) const { return of_y(y_of(x)); }
+  __device__ uint64_t operator()(uint32_t key) const { return of_y(y_of(value_of(key))); }
 };
 
-template <class T>
-__device__ T block_sum(T v, T *red) {
-  for (int w = 32; w; w >>= 1) v += __shfl_xor(v, w, 64);
+// Sum over the wave, in lane 63: four steps inside rows of 16 lanes, two across them.
+template <int CTRL, int ROWS>
+__device__ inline uint64_t add_dpp(uint64_t x) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, uint32_t(x), CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, uint32_t(x >> 32), CTRL, ROWS, 0xf, false);
+  return x + (uint64_t(hi) << 32 | lo);
+}
+__device__ inline uint64_t wave_sum_last(uint64_t x) {
+  x = add_dpp<0x111, 0xf>(x);  // row_shr 1, 2, 4, 8
+  x = add_dpp<0x112, 0xf>(x);
+  x = add_dpp<0x114, 0xf>(x);
+  x = add_dpp<0x118, 0xf>(x);
+  x = add_dpp<0x142, 0xa>(x);  // lane 15 of a row to the next row
+  return add_dpp<0x143, 0xc>(x);  // lane 31 to the upper half
+}
+
+template <int CTRL, int ROWS>
+__device__ inline float max_dpp(float x) {
+  return fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(
+                      0xff800000u, __float_as_uint(x), CTRL, ROWS, 0xf, false)));
+}
+__device__ inline float wave_max_last(float x) {
+  x = max_dpp<0x111, 0xf>(x);
+  x = max_dpp<0x112, 0xf>(x);
+  x = max_dpp<0x114, 0xf>(x);
+  x = max_dpp<0x118, 0xf>(x);
+  x = max_dpp<0x142, 0xa>(x);
+  return max_dpp<0x143, 0xc>(x);
+}
+
+__device__ inline uint64_t block_sum(uint64_t v, uint64_t *red) {
+  v = wave_sum_last(v);
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  if ((threadIdx.x & 63) == 63) red[threadIdx.x >> 6] = v;
   __syncthreads();
-  T s = 0;
-  for (int i = 0; i < kThreads / 64; ++i) s += red[i];
+  uint64_t s = 0;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) s += red[i];
   return s;
 }
 
 // Exclusive prefix sum over the block's threads.
-__device__ inline uint64_t block_scan(uint64_t v, uint64_t *red) {
+__device__ inline uint64_t block_scan(uint64_t v, uint64_t *red, uint64_t *total = nullptr) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   uint64_t x = v;
   for (int w = 1; w < 64; w <<= 1) {
@@ -136,8 +195,13 @@ __device__ inline uint64_t block_scan(uint64_t v, uint64_t *red) {
   __syncthreads();
   if (lane == 63) red[wave] = x;
   __syncthreads();
-  uint64_t before = 0;
-  for (int i = 0; i < wave; ++i) before += red[i];
+  uint64_t before = 0, all = 0;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    before += i < wave ? red[i] : 0;
+    all += red[i];
+  }
+  if (total) *total = all;
   return before + x - v;
 }
 
@@ -162,7 +226,7 @@ __device__ void sort_down(uint64_t *v, int n2) {
 
 constexpr int kList = 4096;       // candidates that are sorted in LDS
 constexpr int kBins = 41 * 32;    // of y: 32 to an octave of weight
-constexpr int kSegs = (1 << 20) / 4 / 64 + 2;
+constexpr int kSegs = (1 << 20) / 4 / 64 + 2;  // sums of 64 groups of tokens
 
 struct Shared {
   union {
@@ -170,8 +234,9 @@ struct Shared {
     uint64_t seg[kSegs];
   };
   uint64_t hist[kBins];
-  uint64_t red[16];
+  uint64_t red[kWaves];
   uint64_t val[2];
+  double table[64];
   int32_t n;
 };
 
@@ -181,51 +246,105 @@ __device__ inline uint64_t pair_of(uint32_t key, int32_t id) {
 __device__ inline uint32_t key_in(uint64_t pair) { return uint32_t(pair >> 32); }
 __device__ inline int32_t id_in(uint64_t pair) { return int32_t(~uint32_t(pair)); }
 
+// A lower bound on the k-th largest of the threads' keys: its upper 16 bits, digit by digit.
+__device__ uint32_t kth_of_threads(uint32_t key, int32_t k, Shared &sh) {
+  const int tid = threadIdx.x;
+  uint32_t *h = reinterpret_cast<uint32_t *>(sh.hist);
+  uint32_t prefix = 0;
+#pragma unroll
+  for (int shift = 24; shift >= 16; shift -= 8) {
+    __syncthreads();
+    if (tid < 256) h[tid] = 0;
+    __syncthreads();
+    if (shift == 24 || (key >> 24) == (prefix >> 24)) atomicAdd(&h[(key >> shift) & 255], 1u);
+    __syncthreads();
+    if (tid < 64) {
+      // four digits a lane, from the largest down
+      uint32_t c[4], sum = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum += c[e] = h[255 - (tid * 4 + e)];
+      uint32_t x = sum;
+      for (int w = 1; w < 64; w <<= 1) {
+        const uint32_t y = __shfl_up(x, w, 64);
+        if (tid >= w) x += y;
+      }
+      uint32_t before = x - sum;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (before < uint32_t(k) && before + c[e] >= uint32_t(k)) {
+          sh.val[0] = prefix | uint32_t(255 - (tid * 4 + e)) << shift;
+          sh.val[1] = uint32_t(k) - before;
+        }
+        before += c[e];
+      }
+    }
+    __syncthreads();
+    prefix = uint32_t(sh.val[0]);
+    k = int32_t(sh.val[1]);
+  }
+  return prefix;
+}
+
 // Appends to the list the tokens that `take` accepts; false when they are more than kList.
 template <int DT, class F>
 __device__ bool collect(const Row<DT> &row, Shared &sh, F take) {
-  const int lane = threadIdx.x & 63;
   __syncthreads();
   if (threadIdx.x == 0) sh.n = 0;
   __syncthreads();
-  const int32_t rounds = (row.groups() + kThreads - 1) / kThreads;
-  for (int32_t r = 0; r < rounds; ++r) {
-    const int32_t g = r * kThreads + threadIdx.x;
-    uint64_t got[8];
-    int n = 0;
-    row.visit(g, [&](int32_t id, float x) {
-      const uint32_t key = key_of(x);
-      if (take(key)) {
-        // n is at most kVec: the unrolled choice keeps got[] in registers
-#pragma unroll
-        for (int e = 0; e < 8; ++e) got[e] = e == n ? pair_of(key, id) : got[e];
-        ++n;
-      }
-    });
-    if (__any(n > 0)) {
-      int x = n;
-      for (int w = 1; w < 64; w <<= 1) {
-        const int y = __shfl_up(x, w, 64);
-        if (lane >= w) x += y;
-      }
-      int base = 0;
-      if (lane == 63) base = atomicAdd(&sh.n, x);
-      base = __shfl(base, 63, 64) + x - n;
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < n && base + e < kList) sh.list[base + e] = got[e];
+  row.each([&](int32_t id, float x) {
+    if (take(x)) {
+      const int at = atomicAdd(&sh.n, 1);
+      if (at < kList) sh.list[at] = pair_of(key_of(x), id);
     }
-  }
+  });
   __syncthreads();
   return sh.n <= kList;
 }
 
-// Fills the list up to a power of two and sorts it; returns its length.
+// The number of values above x in a run of 64 that is sorted downward.
+__device__ inline int above_in_run(const uint64_t *run, uint64_t x) {
+  int n = 0;
+#pragma unroll
+  for (int d = 32; d; d >>= 1) n += run[n + d - 1] > x ? d : 0;
+  return n + (run[n] > x);
+}
+
+// Sorts the list downward (its values differ) and returns its length.  Up to kThreads
+// values: each wave sorts 64 in registers, then a value's place is the count of larger
+// ones over all runs; more go through sort_down.
 __device__ int sort_list(Shared &sh) {
-  const int n = sh.n;
+  const int n = sh.n, tid = threadIdx.x, lane = tid & 63;
+  if (n <= kThreads) {
+    const int runs = (n + 63) >> 6;
+    uint64_t x = tid < n ? sh.list[tid] : 0;
+    if (tid < runs * 64) {
+      for (int size = 2; size <= 64; size <<= 1)
+        for (int d = size >> 1; d; d >>= 1) {
+          const uint64_t y = __shfl_xor(x, d, 64);
+          const bool larger = ((lane & d) == 0) == ((lane & size) == 0);
+          x = (x > y) == larger ? x : y;
+        }
+    }
+    if (runs > 1) {
+      __syncthreads();
+      if (tid < runs * 64) sh.list[tid] = x;
+      __syncthreads();
+      int place = lane;
+      if (x)
+        for (int r = 0; r < runs; ++r)
+          if (r != tid >> 6) place += above_in_run(sh.list + r * 64, x);
+      __syncthreads();
+      if (x) sh.list[place] = x;
+    } else {
+      __syncthreads();
+      if (x) sh.list[tid] = x;
+    }
+    __syncthreads();
+    return n;
+  }
   int n2 = 64;
   while (n2 < n) n2 <<= 1;
-  for (int i = n + threadIdx.x; i < n2; i += kThreads) sh.list[i] = 0;
+  for (int i = n + tid; i < n2; i += kThreads) sh.list[i] = 0;
   __syncthreads();
   sort_down(sh.list, n2);
   return n;
@@ -237,6 +356,7 @@ __device__ void sample_slow(const SampleArgs &a, const char *base, int32_t row, 
 
 template <int DT>
 __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
+  constexpr int kVec = Row<DT>::kVec, kPer = kList / kThreads;
   __shared__ Shared sh;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t row = blockIdx.x, V = a.vocab;
@@ -249,63 +369,98 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
   const int32_t k_in = a.top_k ? a.top_k[row] : 0;
   const bool bad = !(T >= 0.f) || !(T < INFINITY) || !(tp >= 0.f && tp <= 1.f) ||
                    !(mp >= 0.f && mp <= 1.f) || !(u >= 0.f && u < 1.f);
+  if (tid < 64) sh.table[tid] = exp2(double(-tid) * 0.015625);
 
-  // the largest logit and its lowest id
-  uint64_t mine = 0;
-  for (int32_t g = tid; g < r.groups(); g += kThreads)
-    r.visit(g, [&](int32_t id, float x) {
-      const uint64_t c = pair_of(key_of(x), id);
-      mine = c > mine ? c : mine;
-    });
-  uint64_t best = mine;
-  for (int w = 32; w; w >>= 1) {
-    const uint64_t o = __shfl_xor(best, w, 64);
-    best = o > best ? o : best;
-  }
-  if (lane == 0) sh.red[wave] = best;
+  // the largest logit (NaN loses every comparison)
+  float mine = -INFINITY;
+  r.each([&](int32_t, float x) { mine = fmaxf(mine, x); });
+  float top = wave_max_last(mine);
+  float *fred = reinterpret_cast<float *>(sh.red);
+  if (lane == 63) fred[wave] = top;
   __syncthreads();
-  for (int i = 0; i < kThreads / 64; ++i) best = sh.red[i] > best ? sh.red[i] : best;
-  const uint32_t top = key_in(best);
-  if (bad || top <= kLow || T == 0.f) {
+  top = fred[0];
+#pragma unroll
+  for (int i = 1; i < kWaves; ++i) top = fmaxf(top, fred[i]);
+  if (bad || top == -INFINITY) {
     if (tid == 0) {
-      const bool none = bad || top <= kLow;
-      a.token[row] = none ? -1 : id_in(best);
-      if (a.logprob) a.logprob[row] = none ? -INFINITY : 0.f;
-      if (a.kept) a.kept[row] = none ? 0 : 1;
+      a.token[row] = -1;
+      if (a.logprob) a.logprob[row] = -INFINITY;
+      if (a.kept) a.kept[row] = 0;
       if (bad) raise_err(a.err, FS_E_RANGE);
     }
     return;
   }
-  const Weigh weigh{top, double(value_of(top)), 1.4426950408889634 / double(T)};
+  if (T == 0.f) {  // the lowest id of the largest logit
+    if (tid == 0) sh.n = V;
+    __syncthreads();
+    if (mine == top) r.each([&](int32_t id, float x) {
+      if (x == top) atomicMin(&sh.n, id);
+    });
+    __syncthreads();
+    if (tid == 0) {
+      a.token[row] = sh.n;
+      if (a.logprob) a.logprob[row] = 0.f;
+      if (a.kept) a.kept[row] = 1;
+    }
+    return;
+  }
+  const Weigh weigh{top, double(top), 1.4426950408889634 / double(T), sh.table};
   uint64_t least = uint64_t(ceil(__dmul_rn(double(mp), kOne)));
   if (least < 1) least = 1;
 
   // kept: pairs (key, ~id) of at least `cut`, with a weight of at least `least`
-  uint64_t cut = uint64_t(kLow + 1) << 32;
+  uint64_t cut = pair_of(kLow + 1, INT32_MAX);
   if (k_in > 0 && k_in < V) {
-    // The k-th largest of the threads' own largest keys is no larger than the k-th
-    // largest key: what is at least that holds the first k tokens.
-    if (k_in > kThreads)
-      return sample_slow<DT>(a, base, row, weigh, tp, least, k_in, u, sh);
-    __syncthreads();
-    sh.list[tid] = mine;
-    __syncthreads();
-    sort_down(sh.list, kThreads);
-    const uint32_t bound = max(key_in(sh.list[k_in - 1]), kLow + 1);
-    if (!collect<DT>(r, sh, [&](uint32_t key) { return key >= bound; }))
-      return sample_slow<DT>(a, base, row, weigh, tp, least, k_in, u, sh);
+    bool fits;
+    if (k_in <= kThreads) {
+      // The k-th largest of the threads' own largest logits is no larger than the k-th
+      // largest logit: what is at least that holds the first k tokens.
+      const float bound = value_of(max(kth_of_threads(key_of(mine), k_in, sh), kLow + 1));
+      fits = collect<DT>(r, sh, [&](float x) { return x >= bound; });
+    } else {
+      // the bin of y in which the k-th logit lies; what lies beyond the bins has no weight
+      for (int i = tid; i < kBins; i += kThreads) sh.hist[i] = 0;
+      __syncthreads();
+      r.each([&](int32_t, float x) {
+        const double y = weigh.y_of(x);
+        if (y < 41.0) atomicAdd(reinterpret_cast<unsigned int *>(&sh.hist[int(y * 32.0)]), 1u);
+      });
+      __syncthreads();
+      constexpr int kB = (kBins + kThreads - 1) / kThreads;
+      uint64_t h[kB], sum = 0;
+#pragma unroll
+      for (int e = 0; e < kB; ++e) {
+        h[e] = tid * kB + e < kBins ? sh.hist[tid * kB + e] : 0;
+        sum += h[e];
+      }
+      uint64_t before = block_scan(sum, sh.red);
+      if (tid == 0) sh.val[1] = kBins - 1;
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < kB; ++e) {
+        if (before < uint64_t(k_in) && before + h[e] >= uint64_t(k_in)) sh.val[1] = tid * kB + e;
+        before += h[e];
+      }
+      __syncthreads();
+      const int bin = int(sh.val[1]);
+      fits = collect<DT>(r, sh, [&](float x) {
+        const double y = weigh.y_of(x);
+        return y < 41.0 && int(y * 32.0) <= bin;
+      });
+    }
+    if (!fits) return sample_slow<DT>(a, base, row, weigh, tp, least, k_in, u, sh);
     const int n = sort_list(sh);
     // the list's order is the definition's: every cut is a prefix of it
     const int per = (n + kThreads - 1) / kThreads, i0 = min(tid * per, n), i1 = min(i0 + per, n);
-    uint64_t w[kList / kThreads], sum = 0;
+    uint64_t w[kPer], sum = 0;
 #pragma unroll
-    for (int e = 0; e < kList / kThreads; ++e) {
+    for (int e = 0; e < kPer; ++e) {
       const int i = i0 + e;
       w[e] = i < i1 && i < k_in ? weigh(key_in(sh.list[i])) : 0;
       sum += w[e];
     }
-    uint64_t before = block_scan(sum, sh.red);
-    const uint64_t W = block_sum(sum, sh.red);
+    uint64_t W;
+    uint64_t before = block_scan(sum, sh.red, &W);
     uint64_t limit = ~uint64_t(0);
     if (tp < 1.f) {
       const double lim = ceil(__dmul_rn(double(tp), double(W)));
@@ -313,7 +468,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
     }
     uint64_t kept = 0, kept_n = 0;
 #pragma unroll
-    for (int e = 0; e < kList / kThreads; ++e) {
+    for (int e = 0; e < kPer; ++e) {
       const bool in = w[e] >= least && before < limit;
       before += w[e];
       w[e] = in ? w[e] : 0;
@@ -324,14 +479,12 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
     const int m = int(block_sum(kept_n, sh.red));
     uint64_t goal = uint64_t(__dmul_rn(double(u), double(S)));
     if (goal > S - 1) goal = S - 1;
-    // the kept ones by id, with their weights: ids sort upward as ~id downward
-    __syncthreads();
+    // the kept ones by id, with their keys: ids sort upward as ~id downward
 #pragma unroll
-    for (int e = 0; e < kList / kThreads; ++e) {
+    for (int e = 0; e < kPer; ++e) {
       const int i = i0 + e;
       if (i < i1 && w[e]) sh.list[i] = uint64_t(uint32_t(sh.list[i])) << 32 | key_in(sh.list[i]);
     }
-    __syncthreads();
     if (tid == 0) sh.n = m;
     __syncthreads();
     sort_list(sh);
@@ -339,7 +492,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
               j1 = min(j0 + per2, m);
     sum = 0;
 #pragma unroll
-    for (int e = 0; e < kList / kThreads; ++e) {
+    for (int e = 0; e < kPer; ++e) {
       w[e] = j0 + e < j1 ? weigh(uint32_t(sh.list[j0 + e])) : 0;
       sum += w[e];
     }
@@ -347,11 +500,11 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
     if (run <= goal && goal < run + sum) {
       bool found = false;
 #pragma unroll
-      for (int e = 0; e < kList / kThreads; ++e) {
+      for (int e = 0; e < kPer; ++e) {
         run += w[e];
         if (!found && w[e] && run > goal) {
           found = true;
-          a.token[row] = int32_t(~key_in(sh.list[j0 + e]));
+          a.token[row] = id_in(key_in(sh.list[j0 + e]));
           if (a.logprob) a.logprob[row] = float(log(double(w[e]) / double(S)));
           if (a.kept) a.kept[row] = m;
         }
@@ -364,88 +517,138 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
     // weights by bin of y, 32 bins to an octave
     for (int i = tid; i < kBins; i += kThreads) sh.hist[i] = 0;
     __syncthreads();
-    for (int32_t g = tid; g < r.groups(); g += kThreads)
-      r.visit(g, [&](int32_t, float x) {
-        const double y = weigh.y_of(key_of(x));
-        const uint64_t w = weight_of(y);
-        if (w)
-          atomicAdd(reinterpret_cast<unsigned long long *>(&sh.hist[int(y * 32.0)]),
-                    (unsigned long long)w);
-      });
+    r.each([&](int32_t, float x) {
+      const double y = weigh.y_of(x);
+      if (y < 41.0)
+        atomicAdd(reinterpret_cast<unsigned long long *>(&sh.hist[int(y * 32.0)]),
+                  (unsigned long long)weigh.of_y(y));
+    });
     __syncthreads();
     // the bin in which the running sum reaches the limit
-    constexpr int kPer = (kBins + kThreads - 1) / kThreads;
-    uint64_t h[kPer], sum = 0;
+    constexpr int kB = (kBins + kThreads - 1) / kThreads;
+    uint64_t h[kB], sum = 0;
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-      h[e] = tid * kPer + e < kBins ? sh.hist[tid * kPer + e] : 0;
+    for (int e = 0; e < kB; ++e) {
+      h[e] = tid * kB + e < kBins ? sh.hist[tid * kB + e] : 0;
       sum += h[e];
     }
-    uint64_t before = block_scan(sum, sh.red);
-    const uint64_t W = block_sum(sum, sh.red);
+    uint64_t W;
+    uint64_t before = block_scan(sum, sh.red, &W);
     const double lim = ceil(__dmul_rn(double(tp), double(W)));
     const uint64_t limit = lim < 1.0 ? 1 : uint64_t(lim);
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
+    for (int e = 0; e < kB; ++e) {
       if (before < limit && before + h[e] >= limit) {
         sh.val[0] = before;
-        sh.val[1] = tid * kPer + e;
+        sh.val[1] = tid * kB + e;
       }
       before += h[e];
     }
     __syncthreads();
     const uint64_t above = sh.val[0];
     const int bin = int(sh.val[1]);
-    if (!collect<DT>(r, sh, [&](uint32_t key) {
-          if (key <= kLow) return false;
-          const double y = weigh.y_of(key);
+    // the bin's logits, a little widened, so that few need the exact test
+    const float slack = 1e-6f * (fabsf(top) + float(42.0 / weigh.per));
+    const float from = float(double(top) - (bin + 1) * 0.03125 / weigh.per) - slack;
+    const float to = float(double(top) - bin * 0.03125 / weigh.per) + slack;
+    const bool narrow = isfinite(from) && isfinite(to);
+    if (!collect<DT>(r, sh, [&](float x) {
+          if (narrow && !(x >= from && x <= to)) return false;
+          const double y = weigh.y_of(x);
           return y < 41.0 && int(y * 32.0) == bin;
         }))
       return sample_slow<DT>(a, base, row, weigh, tp, least, k_in, u, sh);
     const int n = sort_list(sh);
     const int per = (n + kThreads - 1) / kThreads, i0 = min(tid * per, n), i1 = min(i0 + per, n);
-    uint64_t w[kList / kThreads];
+    uint64_t w[kPer];
     sum = 0;
 #pragma unroll
-    for (int e = 0; e < kList / kThreads; ++e) {
+    for (int e = 0; e < kPer; ++e) {
       w[e] = i0 + e < i1 ? weigh(key_in(sh.list[i0 + e])) : 0;
       sum += w[e];
     }
     before = above + block_scan(sum, sh.red);
     // the last token whose predecessors stay below the limit
 #pragma unroll
-    for (int e = 0; e < kList / kThreads; ++e) {
+    for (int e = 0; e < kPer; ++e) {
       if (w[e] && before < limit && before + w[e] >= limit) sh.val[0] = sh.list[i0 + e];
       before += w[e];
     }
     __syncthreads();
     cut = sh.val[0];
+    __syncthreads();
   }
 
-  // the kept weights in the order of ids: a sum for each 64 groups, then the one that
-  // holds the goal, token by token
-  __syncthreads();
-  const int32_t segs = (r.groups() + 63) / 64;
+  // The kept weights in the order of ids: a sum for each 64 groups (the tokens before the
+  // first vector, each vector, the tokens after the last), then the one that holds the
+  // goal, token by token.  Where few are kept a lane weighs its own one after another, so
+  // a round costs as many weights as its fullest lane keeps, not a whole vector.
+  const float cut_x = value_of(key_in(cut));
+  const int32_t cut_id = id_in(cut);
+  // below `low` a weight is surely under `least` (and under 1)
+  const double reach = 40.0 - log2(double(least)) + 0.01;
+  const float low = float(double(top) - reach / weigh.per) -
+                    1e-6f * (fabsf(top) + float(reach / weigh.per));
+  const float bound = isfinite(low) ? fmaxf(cut_x, low) : cut_x;
+  auto group = [&](int32_t g, const s16x8 &raw, auto take) {
+    if (g >= 1 && g <= r.vecs) {
+      const int32_t i0 = r.head + (g - 1) * kVec;
+      uint32_t mask = 0;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const float x = Row<DT>::at(raw, e);
+        mask |= (x > bound || (x == bound && (x > cut_x || i0 + e <= cut_id))) ? 1u << e : 0;
+      }
+      if (__any(__popc(mask) > kVec / 2)) {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+          const uint64_t w = weigh(Row<DT>::at(raw, e));
+          take(i0 + e, w >= least && (mask >> e & 1) ? w : 0);
+        }
+      } else {
+        while (mask) {
+          const int e = __builtin_ctz(mask);
+          mask &= mask - 1;
+          const uint64_t w = weigh(Row<DT>::pick(raw, e));
+          take(i0 + e, w >= least ? w : 0);
+        }
+      }
+    } else if (g == 0 || g == r.vecs + 1) {
+      const int32_t i0 = g == 0 ? 0 : r.tail(), i1 = g == 0 ? r.head : V;
+      for (int32_t i = i0; i < i1; ++i) {
+        const float x = load_logit<DT>(base, i);
+        const uint64_t w =
+            x > bound || (x == bound && (x > cut_x || i <= cut_id)) ? weigh(x) : 0;
+        take(i, w >= least ? w : 0);
+      }
+    }
+  };
+  const int32_t segs = (r.vecs + 2 + 63) / 64;
   uint64_t total = 0;
   uint32_t count = 0;
-  auto kept_weight = [&](int32_t id, float x) -> uint64_t {
-    const uint32_t key = key_of(x);
-    if (pair_of(key, id) < cut) return 0;
-    const uint64_t w = weigh(key);
-    return w >= least ? w : 0;
-  };
-  for (int32_t s = wave; s < segs; s += kThreads / 64) {
-    uint64_t sum = 0;
-    r.visit(s * 64 + lane, [&](int32_t id, float x) {
-      const uint64_t w = kept_weight(id, x);
-      sum += w;
-      count += w != 0;
-    });
-    for (int w = 32; w; w >>= 1) sum += __shfl_xor(sum, w, 64);
-    if (lane == 0) sh.seg[s] = sum;
-    total += sum;
+  {
+    s16x8 q[kAhead] = {};
+    const bool any = r.vecs > 0;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (any) q[i] = r.load(max(0, (wave + i * kWaves) * 64 + lane - 1));
+#pragma unroll 1
+    for (int32_t s = wave; s < segs; s += kWaves) {
+      const s16x8 raw = q[0];
+#pragma unroll
+      for (int i = 0; i + 1 < kAhead; ++i) q[i] = q[i + 1];
+      if (any) q[kAhead - 1] = r.load((s + kAhead * kWaves) * 64 + lane - 1);
+      uint64_t sum = 0;
+      group(s * 64 + lane, raw, [&](int32_t, uint64_t w) {
+        sum += w;
+        count += w != 0;
+      });
+      total += sum;
+      sum = wave_sum_last(sum);
+      if (lane == 63) sh.seg[s] = sum;
+    }
   }
-  const uint64_t S = block_sum(lane == 0 ? total : uint64_t(0), sh.red);
+  const uint64_t S = block_sum(total, sh.red);
   const int32_t m = int32_t(block_sum(uint64_t(count), sh.red));
   uint64_t goal = uint64_t(__dmul_rn(double(u), double(S)));
   if (goal > S - 1) goal = S - 1;
@@ -468,8 +671,10 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
   if (wave) return;
   run = sh.val[0];
   const int32_t g = int32_t(sh.val[1]) * 64 + lane;
+  s16x8 raw = {};
+  if (r.vecs > 0) raw = r.load(max(0, g - 1));
   sum = 0;
-  r.visit(g, [&](int32_t id, float x) { sum += kept_weight(id, x); });
+  group(g, raw, [&](int32_t, uint64_t w) { sum += w; });
   uint64_t x = sum;
   for (int w = 1; w < 64; w <<= 1) {
     const uint64_t y = __shfl_up(x, w, 64);
@@ -478,8 +683,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
   run += x - sum;
   if (run <= goal && goal < run + sum) {
     bool found = false;
-    r.visit(g, [&](int32_t id, float v) {
-      const uint64_t w = kept_weight(id, v);
+    group(g, raw, [&](int32_t id, uint64_t w) {
       run += w;
       if (!found && run > goal) {
         found = true;

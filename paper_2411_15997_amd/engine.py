@@ -98,7 +98,9 @@ def _fail(code, where):
 
 def _dtype_code(t):
     torch = _torch()
-    code = {torch.bfloat16: FS_BF16, torch.float16: FS_F16, torch.float32: FS_F32}.get(t.dtype)
+    d = t.dtype
+    code = FS_BF16 if d == torch.bfloat16 else FS_F16 if d == torch.float16 else \
+        FS_F32 if d == torch.float32 else None
     if code is None:
         raise TypeError(f"dtype {t.dtype} is not supported (bfloat16, float16, float32)")
     return code
@@ -117,19 +119,22 @@ def _vector(t, dtype, n, name):
     """A contiguous device vector of `n` values of `dtype`, or None."""
     if t is None:
         return None
-    _want(t.dtype == dtype and t.is_contiguous() and t.dim() == 1 and t.shape[0] >= n,
-          f"{name}: a contiguous {dtype} vector of {n} values")
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] < n or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} vector of {n} values")
     return t.data_ptr()
 
 
-def _rows(t, name, *shape):
+def _rows(t, name, shape):
     """Pointer and row stride of a tensor of rows whose inner dimensions are packed."""
-    _want(tuple(t.shape) == shape, f"{name}: shape {tuple(t.shape)}, wanted {shape}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, wanted {shape}")
+    st = t.stride()
     inner = 1
-    for d in range(t.dim() - 1, 0, -1):
-        _want(t.shape[d] == 1 or t.stride(d) == inner, f"{name}: inner dimensions are not packed")
-        inner *= t.shape[d]
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else inner)
+    for d in range(len(shape) - 1, 0, -1):
+        if st[d] != inner and shape[d] != 1:
+            raise ValueError(f"{name}: inner dimensions are not packed")
+        inner *= shape[d]
+    return t.data_ptr(), (st[0] if shape[0] > 1 else inner)
 
 
 def _workspace(ws, need, like):
@@ -251,14 +256,14 @@ class Sampling:
 def fs_adapter_linear(step: Step, adapters: Adapters, x, w, y=None, ws=None, err=None, check=True):
     """y = x w^T plus every request's adapter; x [rows][K], w [N][K], returns y [rows][N]."""
     K, N = adapters.K, adapters.N
-    xp, xs = _rows(x, "x", step.rows, K)
-    _want(tuple(w.shape) == (N, K) and w.is_contiguous(), "w: packed [N][K]")
+    xp, xs = _rows(x, "x", (step.rows, K))
+    _want(w.shape == (N, K) and w.is_contiguous(), "w: packed [N][K]")
     _want(x.dtype == adapters.dtype and w.dtype == adapters.dtype, "x, w and adapters: one dtype")
     _want(adapters.n_seqs >= step.n, "adapter: an id for every request")
     if y is None:
         y = _torch().empty((step.rows, N), dtype=x.dtype, device=x.device)
     _want(y.dtype == x.dtype, "y: the dtype of x")
-    yp, ys = _rows(y, "y", step.rows, N)
+    yp, ys = _rows(y, "y", (step.rows, N))
     err = cleared_err_word(x.device) if err is None else err
     L = _lib()
     ws, wp, wn = _workspace(ws, L.fs_adapter_workspace(step.ref, adapters.ref), x)
@@ -289,16 +294,16 @@ def fs_rope_append(step: Step, cache: KVCache, rope: Rope, q, k, v, q_out=None, 
           (q is None or q.dtype == cache.dtype), "q, k, v: the cache's dtype")
     _want(cache.table.shape[0] >= step.n, "table: a row for every request")
     _want(rope.pos is None or rope.pos.shape[0] >= T, "pos: a position for every row")
-    kp, ks = _rows(k, "k", T, HK, D)
-    vp, vs = _rows(v, "v", T, HK, D)
+    kp, ks = _rows(k, "k", (T, HK, D))
+    vp, vs = _rows(v, "v", (T, HK, D))
     H, qp, qs, op, os_ = 0, None, 0, None, 0
     if q is not None:
         H = q.shape[1]
-        qp, qs = _rows(q, "q", T, H, D)
+        qp, qs = _rows(q, "q", (T, H, D))
         if q_out is None:
             q_out = _torch().empty((T, H, D), dtype=q.dtype, device=q.device)
         _want(q_out.dtype == q.dtype, "q_out: the dtype of q")
-        op, os_ = _rows(q_out, "q_out", T, H, D)
+        op, os_ = _rows(q_out, "q_out", (T, H, D))
     err = cleared_err_word(k.device) if err is None else err
     _done(_lib().fs_rope_append(step.ref, cache.ref, rope.ref, H, qp, qs, kp, ks, vp, vs, op, os_,
                                 err.data_ptr(), _stream(k)), "fs_rope_append", err, check)
@@ -312,12 +317,12 @@ def fs_paged_attention(step: Step, cache: KVCache, q, scale, window=0, out=None,
     T, H, D = q.shape
     _want(q.dtype == cache.dtype and D == cache.head_dim, "q: the cache's dtype and head_dim")
     _want(cache.table.shape[0] >= step.n, "table: a row for every request")
-    qp, qs = _rows(q, "q", step.rows, H, D)
+    qp, qs = _rows(q, "q", (step.rows, H, D))
     torch = _torch()
     if out is None:
         out = torch.empty((T, H, D), dtype=q.dtype, device=q.device)
     _want(out.dtype == q.dtype, "out: the dtype of q")
-    op, os_ = _rows(out, "out", T, H, D)
+    op, os_ = _rows(out, "out", (T, H, D))
     if lse is None and want_lse:
         lse = torch.empty((T, H), dtype=torch.float32, device=q.device)
     if lse is not None:
