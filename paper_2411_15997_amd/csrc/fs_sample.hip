@@ -28,7 +28,7 @@ struct SampleArgs {
 
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
-constexpr int kAhead = 4;  // 16-byte loads of a thread in flight
+constexpr int kAhead = 2;  // 16-byte loads of a thread in flight in the ordered pass
 constexpr double kOne = 1099511627776.0;  // 2^40
 
 // Order-preserving key: larger logit, larger key; -0 as 0; NaN as -inf.  -inf is kLow.
@@ -66,7 +66,8 @@ struct Row {
   __device__ int32_t tail() const { return head + vecs * kVec; }
   __device__ Raw load(int32_t v) const {  // vector v, or any other when there is no such
     const int32_t i = head + min(v, vecs - 1) * kVec;
-    return *reinterpret_cast<const Raw *>(p + int64_t(i) * (16 / kVec));
+    typedef const __attribute__((address_space(1))) Raw *Global;
+    return *(Global)(p + int64_t(i) * (16 / kVec));
   }
   __device__ static float at(const Raw &v, int e) {  // e known at compile time
     if constexpr (DT == FS_F32)
@@ -85,62 +86,84 @@ struct Row {
     else
       return to_f32<DT == FS_BF16>(short(e & 1 ? x >> 16 : x));
   }
-  // f(id, logit) for every token of the row, in no order; the next loads are in flight
-  // while a batch is worked on
-  template <class F>
-  __device__ void each(F f) const {
+  // The whole row in no order: vec(first id, 16 bytes) for the vectors, one(id, logit) for
+  // the other tokens.  AHEAD loads are in flight; the body is written out as often, so
+  // long bodies take few.
+  template <int AHEAD, class F, class G>
+  __device__ void each(F vec, G one) const {
     const int tid = threadIdx.x, odd = head + vocab - tail();
     if (tid < odd) {
       const int32_t i = tid < head ? tid : tail() + tid - head;
-      f(i, load_logit<DT>(p, i));
+      one(i, load_logit<DT>(p, i));
     }
     if (vecs == 0) return;
-    Raw q[kAhead];
+    Raw q[AHEAD];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) q[u] = load(tid + u * kThreads);
-    // the body once, not once for each load in flight: the passes' code then stays in the
-    // instruction cache
+    for (int u = 0; u < AHEAD; ++u) q[u] = load(tid + u * kThreads);
 #pragma unroll 1
-    for (int32_t v = tid; v < vecs; v += kThreads) {
-      const Raw x = q[0];
+    for (int32_t v0 = tid; v0 < vecs; v0 += AHEAD * kThreads)
 #pragma unroll
-      for (int u = 0; u + 1 < kAhead; ++u) q[u] = q[u + 1];
-      q[kAhead - 1] = load(v + kAhead * kThreads);
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) f(head + v * kVec + e, at(x, e));
-    }
+      for (int u = 0; u < AHEAD; ++u) {
+        const int32_t v = v0 + u * kThreads;
+        const Raw x = q[u];
+        q[u] = load(v + AHEAD * kThreads);
+        if (v < vecs) vec(head + v * kVec, x);
+      }
   }
 };
 
-// The weight of a logit: floor(2^(40 - y)), y = (largest - x) * per >= 0.  2^-y is taken as
-// 2^-n * 2^-(j/64) * e^z with a table of the 64 middle factors and |z| <= ln(2) / 128, whose
-// series ends below 4e-17 of the value at degree 5.
+// The weight of a logit: floor(2^(40 - y)), y = (largest - x) * per >= 0.  With q the nearest
+// whole number to 256 y, 2^-y = 2^-(q >> 8) * 2^-((q & 255) / 256) * 2^(r / 256), |r| <= 1/2:
+// a table of the 256 middle factors, and a series that ends below 4e-17 of the value at
+// degree 4.  (Full passes over a row are bound by these instructions.)
 struct Weigh {
-  float top;  // the largest logit
-  double best, per;
-  const double *table;  // 2^(-j/64)
+  float top;            // the largest logit
+  double best, per;     // per: 256 log2(e) / T
+  const double *table;  // 2^(-j/256)
+  static constexpr double kMagic = 6755399441055744.0 + 11 * 256;  // 1.5 * 2^52 + 11 * 256
+  // 256 y, at most 13,030 (no weight is left from 41 * 256 on); NaN as -inf
   __device__ double y_of(float x) const {
-    return x == top ? 0.0 : __dmul_rn(__dsub_rn(best, double(x)), per);
+    return fmin(__dmul_rn(__dsub_rn(best, double(fmaxf(x, -INFINITY))), per), 13030.0);
+  }
+  // q + 11 * 256, in the low bits of the sum
+  __device__ static uint32_t place(double y) {
+    return uint32_t(__double_as_longlong(y + kMagic));
+  }
+  __device__ static int bin_of(uint32_t place) { return int(place >> 3) - 11 * 32; }
+  // N weights side by side: the table is read for all of them at once
+  template <int N>
+  __device__ void many(const double *y, uint64_t *w) const {
+    double r[N], mid[N];
+    uint32_t at[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const double s = y[e] + kMagic;
+      at[e] = uint32_t(__double_as_longlong(s));
+      mid[e] = table[at[e] & 255];
+      r[e] = (s - kMagic) - y[e];
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      double p = 2.23939519087515698716e-12;
+      p = fma(p, r[e], 3.30830268054137129301e-09);
+      p = fma(p, r[e], 3.66556559691010622906e-06);
+      p = fma(p, r[e], 2.70760617406228627432e-03);
+      p = fma(p, r[e], 1.0);
+      // above 2 the product's bits stand still: its mantissa holds it times 2^51
+      const uint64_t bits = uint64_t(__double_as_longlong(fma(p, mid[e], 2.0)));
+      w[e] = (bits & 0xfffffffffffffull) >> (at[e] >> 8);
+    }
   }
   __device__ uint64_t of_y(double y) const {
-    // the nearest multiple of 1/64: the sum's low bits are its number of 64ths
-    const double s = fma(y, 64.0, 6755399441055744.0);  // 1.5 * 2^52
-    const int q = int(uint32_t(__double_as_longlong(s)));
-    const double z = fma(s - 6755399441055744.0, 0.015625, -y) * 0.693147180559945309417;
-    double p = 8.33333333333333333333e-3;
-    p = fma(p, z, 4.16666666666666666667e-2);
-    p = fma(p, z, 1.66666666666666666667e-1);
-    p = fma(p, z, 0.5);
-    p = fma(p, z, 1.0);
-    p = fma(p, z, 1.0);
-    // 2^(40 - q/64) times it, rounded down: its mantissa shifted right
-    const uint64_t bits = uint64_t(__double_as_longlong(p * table[q & 63]));
-    const uint64_t mant = (bits & 0xfffffffffffffull) | 0x10000000000000ull;
-    const int shift = 12 + (q >> 6) + 1023 - int(bits >> 52);
-    return y < 41.0 ? mant >> (shift & 63) : 0;
+    uint64_t w;
+    many<1>(&y, &w);
+    return w;
   }
   __device__ uint64_t operator()(float x) const { return of_y(y_of(x)); }
-  __device__ uint64_t operator()(uint32_t key) const { return of_y(y_of(value_of(key))); }
+  __device__ uint64_t operator()(uint32_t key) const {
+    const float x = value_of(key);
+    return x == top ? uint64_t(1) << 40 : of_y(y_of(x));  // the largest may be infinite
+  }
 };
 
 // Sum over the wave, in lane 63: four steps inside rows of 16 lanes, two across them.
@@ -236,7 +259,7 @@ struct Shared {
   uint64_t hist[kBins];
   uint64_t red[kWaves];
   uint64_t val[2];
-  double table[64];
+  double table[256];
   int32_t n;
 };
 
@@ -291,12 +314,25 @@ __device__ bool collect(const Row<DT> &row, Shared &sh, F take) {
   __syncthreads();
   if (threadIdx.x == 0) sh.n = 0;
   __syncthreads();
-  row.each([&](int32_t id, float x) {
+  auto one = [&](int32_t id, float x) {
     if (take(x)) {
       const int at = atomicAdd(&sh.n, 1);
       if (at < kList) sh.list[at] = pair_of(key_of(x), id);
     }
-  });
+  };
+  row.template each<4>(
+      [&](int32_t id0, const s16x8 &v) {
+        uint32_t mask = 0;
+#pragma unroll
+        for (int e = 0; e < Row<DT>::kVec; ++e) mask |= take(Row<DT>::at(v, e)) ? 1u << e : 0;
+        while (mask) {
+          const int e = __builtin_ctz(mask);
+          mask &= mask - 1;
+          const int at = atomicAdd(&sh.n, 1);
+          if (at < kList) sh.list[at] = pair_of(key_of(Row<DT>::pick(v, e)), id0 + e);
+        }
+      },
+      one);
   __syncthreads();
   return sh.n <= kList;
 }
@@ -369,11 +405,16 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
   const int32_t k_in = a.top_k ? a.top_k[row] : 0;
   const bool bad = !(T >= 0.f) || !(T < INFINITY) || !(tp >= 0.f && tp <= 1.f) ||
                    !(mp >= 0.f && mp <= 1.f) || !(u >= 0.f && u < 1.f);
-  if (tid < 64) sh.table[tid] = exp2(double(-tid) * 0.015625);
+  if (tid < 256) sh.table[tid] = exp2(double(-tid) * 0.00390625);
 
   // the largest logit (NaN loses every comparison)
   float mine = -INFINITY;
-  r.each([&](int32_t, float x) { mine = fmaxf(mine, x); });
+  r.template each<4>(
+      [&](int32_t, const s16x8 &v) {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) mine = fmaxf(mine, Row<DT>::at(v, e));
+      },
+      [&](int32_t, float x) { mine = fmaxf(mine, x); });
   float top = wave_max_last(mine);
   float *fred = reinterpret_cast<float *>(sh.red);
   if (lane == 63) fred[wave] = top;
@@ -393,9 +434,16 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
   if (T == 0.f) {  // the lowest id of the largest logit
     if (tid == 0) sh.n = V;
     __syncthreads();
-    if (mine == top) r.each([&](int32_t id, float x) {
-      if (x == top) atomicMin(&sh.n, id);
-    });
+    if (mine == top)
+      r.template each<2>(
+          [&](int32_t id0, const s16x8 &v) {
+#pragma unroll
+            for (int e = kVec - 1; e >= 0; --e)
+              if (Row<DT>::at(v, e) == top) atomicMin(&sh.n, id0 + e);
+          },
+          [&](int32_t id, float x) {
+            if (x == top) atomicMin(&sh.n, id);
+          });
     __syncthreads();
     if (tid == 0) {
       a.token[row] = sh.n;
@@ -404,12 +452,14 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
     }
     return;
   }
-  const Weigh weigh{top, double(top), 1.4426950408889634 / double(T), sh.table};
+  const Weigh weigh{top, double(top), 256.0 * (1.4426950408889634 / double(T)), sh.table};
   uint64_t least = uint64_t(ceil(__dmul_rn(double(mp), kOne)));
   if (least < 1) least = 1;
 
   // kept: pairs (key, ~id) of at least `cut`, with a weight of at least `least`
   uint64_t cut = pair_of(kLow + 1, INT32_MAX);
+  // an infinite logit leaves no finite distances: the general way deals with it
+  if (top == INFINITY) return sample_slow<DT>(a, base, row, weigh, tp, least, k_in, u, sh);
   if (k_in > 0 && k_in < V) {
     bool fits;
     if (k_in <= kThreads) {
@@ -421,10 +471,16 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
       // the bin of y in which the k-th logit lies; what lies beyond the bins has no weight
       for (int i = tid; i < kBins; i += kThreads) sh.hist[i] = 0;
       __syncthreads();
-      r.each([&](int32_t, float x) {
-        const double y = weigh.y_of(x);
-        if (y < 41.0) atomicAdd(reinterpret_cast<unsigned int *>(&sh.hist[int(y * 32.0)]), 1u);
-      });
+      auto one = [&](int32_t, float x) {
+        const int bin = Weigh::bin_of(Weigh::place(weigh.y_of(x)));
+        if (bin < kBins) atomicAdd(reinterpret_cast<unsigned int *>(&sh.hist[bin]), 1u);
+      };
+      r.template each<2>(
+          [&](int32_t id0, const s16x8 &v) {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) one(id0 + e, Row<DT>::at(v, e));
+          },
+          one);
       __syncthreads();
       constexpr int kB = (kBins + kThreads - 1) / kThreads;
       uint64_t h[kB], sum = 0;
@@ -444,8 +500,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
       __syncthreads();
       const int bin = int(sh.val[1]);
       fits = collect<DT>(r, sh, [&](float x) {
-        const double y = weigh.y_of(x);
-        return y < 41.0 && int(y * 32.0) <= bin;
+        return Weigh::bin_of(Weigh::place(weigh.y_of(x))) <= bin;
       });
     }
     if (!fits) return sample_slow<DT>(a, base, row, weigh, tp, least, k_in, u, sh);
@@ -517,12 +572,25 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
     // weights by bin of y, 32 bins to an octave
     for (int i = tid; i < kBins; i += kThreads) sh.hist[i] = 0;
     __syncthreads();
-    r.each([&](int32_t, float x) {
-      const double y = weigh.y_of(x);
-      if (y < 41.0)
-        atomicAdd(reinterpret_cast<unsigned long long *>(&sh.hist[int(y * 32.0)]),
-                  (unsigned long long)weigh.of_y(y));
-    });
+    auto add = [&](double y, uint64_t w) {
+      const int bin = Weigh::bin_of(Weigh::place(y));
+      if (bin < kBins)
+        atomicAdd(reinterpret_cast<unsigned long long *>(&sh.hist[bin]), (unsigned long long)w);
+    };
+    r.template each<2>(
+        [&](int32_t, const s16x8 &v) {
+          double y[kVec];
+          uint64_t w[kVec];
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) y[e] = weigh.y_of(Row<DT>::at(v, e));
+          weigh.template many<kVec>(y, w);
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) add(y[e], w[e]);
+        },
+        [&](int32_t, float x) {
+          const double y = weigh.y_of(x);
+          add(y, weigh.of_y(y));
+        });
     __syncthreads();
     // the bin in which the running sum reaches the limit
     constexpr int kB = (kBins + kThreads - 1) / kThreads;
@@ -548,14 +616,13 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
     const uint64_t above = sh.val[0];
     const int bin = int(sh.val[1]);
     // the bin's logits, a little widened, so that few need the exact test
-    const float slack = 1e-6f * (fabsf(top) + float(42.0 / weigh.per));
-    const float from = float(double(top) - (bin + 1) * 0.03125 / weigh.per) - slack;
-    const float to = float(double(top) - bin * 0.03125 / weigh.per) + slack;
+    const float slack = 1e-6f * (fabsf(top) + float(42.0 * 256.0 / weigh.per));
+    const float from = float(double(top) - ((bin + 1) * 8 + 1) / weigh.per) - slack;
+    const float to = float(double(top) - (bin * 8 - 1) / weigh.per) + slack;
     const bool narrow = isfinite(from) && isfinite(to);
     if (!collect<DT>(r, sh, [&](float x) {
           if (narrow && !(x >= from && x <= to)) return false;
-          const double y = weigh.y_of(x);
-          return y < 41.0 && int(y * 32.0) == bin;
+          return Weigh::bin_of(Weigh::place(weigh.y_of(x))) == bin;
         }))
       return sample_slow<DT>(a, base, row, weigh, tp, least, k_in, u, sh);
     const int n = sort_list(sh);
@@ -586,7 +653,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
   const float cut_x = value_of(key_in(cut));
   const int32_t cut_id = id_in(cut);
   // below `low` a weight is surely under `least` (and under 1)
-  const double reach = 40.0 - log2(double(least)) + 0.01;
+  const double reach = 256.0 * (40.0 - log2(double(least)) + 0.01);
   const float low = float(double(top) - reach / weigh.per) -
                     1e-6f * (fabsf(top) + float(reach / weigh.per));
   const float bound = isfinite(low) ? fmaxf(cut_x, low) : cut_x;
@@ -600,11 +667,14 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
         mask |= (x > bound || (x == bound && (x > cut_x || i0 + e <= cut_id))) ? 1u << e : 0;
       }
       if (__any(__popc(mask) > kVec / 2)) {
+        double y[kVec];
+        uint64_t w[kVec];
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-          const uint64_t w = weigh(Row<DT>::at(raw, e));
-          take(i0 + e, w >= least && (mask >> e & 1) ? w : 0);
-        }
+        for (int e = 0; e < kVec; ++e) y[e] = weigh.y_of(Row<DT>::at(raw, e));
+        weigh.template many<kVec>(y, w);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e)
+          take(i0 + e, w[e] >= least && (mask >> e & 1) ? w[e] : 0);
       } else {
         while (mask) {
           const int e = __builtin_ctz(mask);
@@ -633,20 +703,23 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
     for (int i = 0; i < kAhead; ++i)
       if (any) q[i] = r.load(max(0, (wave + i * kWaves) * 64 + lane - 1));
 #pragma unroll 1
-    for (int32_t s = wave; s < segs; s += kWaves) {
-      const s16x8 raw = q[0];
+    for (int32_t s0 = wave; s0 < segs; s0 += kAhead * kWaves)
 #pragma unroll
-      for (int i = 0; i + 1 < kAhead; ++i) q[i] = q[i + 1];
-      if (any) q[kAhead - 1] = r.load((s + kAhead * kWaves) * 64 + lane - 1);
-      uint64_t sum = 0;
-      group(s * 64 + lane, raw, [&](int32_t, uint64_t w) {
-        sum += w;
-        count += w != 0;
-      });
-      total += sum;
-      sum = wave_sum_last(sum);
-      if (lane == 63) sh.seg[s] = sum;
-    }
+      for (int i = 0; i < kAhead; ++i) {
+        const int32_t s = s0 + i * kWaves;
+        const s16x8 raw = q[i];
+        if (any) q[i] = r.load((s + kAhead * kWaves) * 64 + lane - 1);
+        if (s < segs) {
+          uint64_t sum = 0;
+          group(s * 64 + lane, raw, [&](int32_t, uint64_t w) {
+            sum += w;
+            count += w != 0;
+          });
+          total += sum;
+          sum = wave_sum_last(sum);
+          if (lane == 63) sh.seg[s] = sum;
+        }
+      }
   }
   const uint64_t S = block_sum(total, sh.red);
   const int32_t m = int32_t(block_sum(uint64_t(count), sh.red));
