@@ -77,6 +77,7 @@ fs_status fs_clear_status(int32_t *err, hipStream_t stream);
  *   a [n_adapters][max_rank][K], b [n_adapters][N][max_rank]; entries at and after
  *   rank[a] are not used.  rank NULL: max_rank; scale NULL: 1
  * K, N, max_rank and the strides are multiples of 8, bases 16-byte aligned, max_rank <= 128,
+ * K, N <= 2^20, x_stride <= 2^21,
  * n_adapters may be 0 (adapter is then not read).  Sums are held in fp32; scale * h enters the
  * second product as the sum of two dtype values (its rounding is below fp32's of the sum).
  * ws: fs_adapter_workspace(s, ad) bytes, 256-byte aligned.  err: FS_E_RANGE for an

@@ -58,6 +58,27 @@ __device__ inline f32x16 mfma_32x32x16(s16x8 a, s16x8 b, f32x16 c) {
                                                   __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
+// 16 bytes for each lane from `base` (the same for the wave) plus its own offset in bytes
+// straight into LDS, at address `at` (the same for the wave) plus 16 times the lane.
+// Counted by vmcnt, in order; wait_loads() before use.  Written out because the compiler
+// would wait for all such loads before any LDS read.  No register is loaded: nothing of
+// the wave's own can be overwritten while it is under way.
+__device__ inline void load_to_lds(const void *base, uint32_t offset, uint32_t at) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at),
+               "v"(offset), "s"(base)
+               : "memory");
+}
+__device__ inline uint32_t lds_address(const void *p) {
+  return __builtin_amdgcn_readfirstlane(
+      uint32_t(uintptr_t((__attribute__((address_space(3))) const void *)p)));
+}
+// Waits until at most LEFT of the wave's newest loads are under way and its LDS reads are
+// done, then for the other waves: what they loaded is there, what they read may be replaced.
+template <int LEFT>
+__device__ inline void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
+
 // The request whose rows contain row t: the last s with q_off[s] <= t (t < q_off[n]).
 __device__ inline int32_t seq_of_row(const int32_t *q_off, int32_t n, int32_t t) {
   int32_t lo = 0, hi = n - 1;

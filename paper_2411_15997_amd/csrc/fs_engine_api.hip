@@ -104,7 +104,7 @@ fs_status fs_adapter_linear(const fs_step *s, const fs_adapters *ad, const void 
   if (rows_of(s) == 0) return FS_OK;
   if (!x || !w || !y || !aligned_to(x, 16) || !aligned_to(w, 16) || !aligned_to(y, 16) ||
       !mult8(x_stride) || !mult8(y_stride) || x_stride < ad->in_features ||
-      y_stride < ad->out_features)
+      y_stride < ad->out_features || x_stride > (1 << 21))
     return FS_E_ARG;
   const size_t need = adapter_workspace_bytes(s, ad);
   if (need > 0 && (!ws || !aligned_to(ws, 256) || ws_bytes < need)) return FS_E_WORKSPACE;

@@ -217,18 +217,23 @@ __global__ void __launch_bounds__(512) k_linear_few(LinArgs g) {
   }
 }
 
-// Where 16-byte chunk c of row r lies in an LDS tile of 64-element rows.
-__device__ inline int gemm_at(int r, int c) { return r * 64 + ((c ^ ((r >> 1) & 7)) * 8); }
+// Which 16-byte chunk of its row lies in place c of row r of an LDS tile (and the other way
+// round): 16 rows' chunks of one column fall on different banks.
+template <int BK>
+__device__ inline int place_of(int r, int c) {
+  return BK == 64 ? c ^ ((r >> 1) & 7) : c ^ ((r >> 2) & 3);
+}
 
-// ---- many rows: BM rows by BN columns a work-group, K in steps of 64 through two LDS
-// buffers; a wave takes WM rows by WN columns.
-template <bool BF, int BM, int BN, int WM, int WN>
-__global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) k_linear_tile(LinArgs g) {
-  constexpr int THREADS = (BM / WM) * (BN / WN) * 64;
+// ---- many rows: BM rows by BN columns a work-group, K in steps of BK through STAGES LDS
+// buffers that are filled STAGES - 1 steps ahead; a wave takes WM rows by WN columns.
+template <bool BF, int BM, int BN, int WM, int WN, int BK, int STAGES>
+__global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) k_linear_tile(LinArgs g) {
+  constexpr int WAVES = (BM / WM) * (BN / WN);
   constexpr int MT = WM / 32, NT = WN / 32;
-  constexpr int LX = BM * 8 / THREADS, LW = BN * 8 / THREADS;  // 16-byte chunks a thread loads
-  __shared__ __align__(16) short xs[2][BM * 64], wsm[2][BN * 64];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int CH = BK / 8, RW = 64 / CH;  // chunks of a row, rows of a wave's load
+  constexpr int LX = BM / RW / WAVES, LW = BN / RW / WAVES;  // a wave's loads of a step
+  __shared__ __align__(16) short xs[STAGES][BM * BK], ws[STAGES][BN * BK];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r32 = lane & 31, h2 = lane >> 5;
 
   // Work-groups go to the 8 dies in turn: each die takes a run of neighbouring tiles, in
@@ -244,54 +249,92 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) k_linear_tile(L
 
   const int wm = (wave % (BM / WM)) * WM, wn = (wave / (BM / WM)) * WN;
   f32x16 acc[MT][NT] = {};
-  s16x8 xr[LX], wr[LW];
-  const int lrow = tid >> 3, lc = tid & 7;
-  const s16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
-  const short *xp[LX], *wp[LW];
+  // this lane's row and chunk of each of the wave's loads, as bytes from the tile's start
+  uint32_t xo[LX], wo[LW];
+  int xc[LX], wc[LW];
 #pragma unroll
-  for (int i = 0; i < LX; ++i)
-    xp[i] = g.x + int64_t(min(m0 + lrow + i * (THREADS / 8), g.rows - 1)) * g.x_stride + lc * 8;
+  for (int i = 0; i < LX; ++i) {
+    const int r = (wave * LX + i) * RW + lane / CH;
+    xc[i] = place_of<BK>(r, lane % CH) * 8;
+    xo[i] = uint32_t((min(m0 + r, g.rows - 1) - m0) * g.x_stride + xc[i]) * 2;
+  }
 #pragma unroll
-  for (int i = 0; i < LW; ++i)
-    wp[i] = g.w + int64_t(min(n0 + lrow + i * (THREADS / 8), g.N - 1)) * g.K + lc * 8;
-  auto load = [&](int k) {
-    const bool in = k + lc * 8 < g.K;
+  for (int i = 0; i < LW; ++i) {
+    const int r = (wave * LW + i) * RW + lane / CH;
+    wc[i] = place_of<BK>(r, lane % CH) * 8;
+    wo[i] = uint32_t((min(n0 + r, g.N - 1) - n0) * g.K + wc[i]) * 2;
+  }
+  const short *x0 = g.x + int64_t(m0) * g.x_stride, *w0 = g.w + int64_t(n0) * g.K;
+  const uint32_t xs_at = lds_address(&xs[0][wave * LX * RW * BK]),
+                 ws_at = lds_address(&ws[0][wave * LW * RW * BK]);
+  auto issue = [&](int step) {
+    const int k = step * BK, s = step % STAGES;
+    if (k + BK <= g.K) {
 #pragma unroll
-    for (int i = 0; i < LX; ++i) xr[i] = in ? *reinterpret_cast<const s16x8 *>(xp[i] + k) : zero;
+      for (int i = 0; i < LX; ++i)
+        load_to_lds(x0 + k, xo[i], xs_at + (s * BM + i * RW) * BK * 2);
 #pragma unroll
-    for (int i = 0; i < LW; ++i) wr[i] = in ? *reinterpret_cast<const s16x8 *>(wp[i] + k) : zero;
+      for (int i = 0; i < LW; ++i)
+        load_to_lds(w0 + k, wo[i], ws_at + (s * BN + i * RW) * BK * 2);
+    } else {  // past the end of K: the last chunk of the row, its products are masked
+#pragma unroll
+      for (int i = 0; i < LX; ++i)
+        load_to_lds(x0 + k, xo[i] + 2 * min(0, g.K - 8 - k - xc[i]),
+                    xs_at + (s * BM + i * RW) * BK * 2);
+#pragma unroll
+      for (int i = 0; i < LW; ++i)
+        load_to_lds(w0 + k, wo[i] + 2 * min(0, g.K - 8 - k - wc[i]),
+                    ws_at + (s * BN + i * RW) * BK * 2);
+    }
   };
-  auto store = [&](int b) {
+  auto multiply = [&](int step, bool whole) {
+    const short *xt = xs[step % STAGES], *wt = ws[step % STAGES];
 #pragma unroll
-    for (int i = 0; i < LX; ++i)
-      *reinterpret_cast<s16x8 *>(&xs[b][gemm_at(lrow + i * (THREADS / 8), lc)]) = xr[i];
-#pragma unroll
-    for (int i = 0; i < LW; ++i)
-      *reinterpret_cast<s16x8 *>(&wsm[b][gemm_at(lrow + i * (THREADS / 8), lc)]) = wr[i];
-  };
-  load(0);
-  store(0);
-  __syncthreads();
-  int b = 0;
-  for (int k = 0; k < g.K; k += 64, b ^= 1) {
-    if (k + 64 < g.K) load(k + 64);
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < BK / 16; ++u) {
       s16x8 xf[MT], wf[NT];
+      const int c = u * 2 + h2;
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
-        xf[m] = *reinterpret_cast<const s16x8 *>(&xs[b][gemm_at(wm + m * 32 + r32, u * 2 + h2)]);
+      for (int n = 0; n < NT; ++n) {
+        const int r = wn + n * 32 + r32;
+        wf[n] = *reinterpret_cast<const s16x8 *>(wt + r * BK + place_of<BK>(r, c) * 8);
+      }
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-        wf[n] = *reinterpret_cast<const s16x8 *>(&wsm[b][gemm_at(wn + n * 32 + r32, u * 2 + h2)]);
+      for (int m = 0; m < MT; ++m) {
+        const int r = wm + m * 32 + r32;
+        xf[m] = *reinterpret_cast<const s16x8 *>(xt + r * BK + place_of<BK>(r, c) * 8);
+      }
+      if (!whole) {
+        const s16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+        const bool in = step * BK + c * 8 < g.K;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) xf[m] = in ? xf[m] : zero;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) wf[n] = in ? wf[n] : zero;
+      }
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int n = 0; n < NT; ++n) acc[m][n] = mfma_32x32x16<BF>(wf[n], xf[m], acc[m][n]);
     }
-    if (k + 64 < g.K) store(b ^ 1);
-    __syncthreads();
+  };
+  const int steps = (g.K + BK - 1) / BK, full = g.K / BK;
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s)
+    if (s < steps) issue(s);
+  int step = 0;
+  for (; step + STAGES - 1 < steps; ++step) {
+    wait_loads<(STAGES - 2) * (LX + LW)>();
+    issue(step + STAGES - 1);
+    multiply(step, true);
   }
+  for (; step < steps; ++step) {
+    wait_loads<0>();
+    if (step < full)
+      multiply(step, true);
+    else
+      multiply(step, false);
+  }
+  const s16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
   if (g.n_adapters > 0) {
     const int chunks = g.R / 8;
 #pragma unroll
@@ -337,8 +380,9 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) k_linear_tile(L
 template <bool BF, int JT>
 void shrink(const LinArgs &g, int64_t tiles, hipStream_t stream) {
   // few tiles: more waves share out K, so that one tile's time is short
-  if (tiles <= 512 && JT <= 4)
-    hipLaunchKernelGGL((k_shrink<BF, JT, 16>), dim3(tiles), dim3(1024), 0, stream, g);
+  constexpr int kMost = JT <= 4 ? 16 : 8;  // by registers
+  if (tiles <= 512)
+    hipLaunchKernelGGL((k_shrink<BF, JT, kMost>), dim3(tiles), dim3(kMost * 64), 0, stream, g);
   else
     hipLaunchKernelGGL((k_shrink<BF, JT, 4>), dim3(tiles), dim3(256), 0, stream, g);
 }
@@ -378,10 +422,12 @@ void run(const LinArgs &g, int64_t tiles, hipStream_t stream) {
   }
   const int64_t big = int64_t((g.rows + 255) / 256) * ((g.N + 255) / 256);
   if (big >= 256) {
-    hipLaunchKernelGGL((k_linear_tile<BF, 256, 256, 128, 64>), dim3(big), dim3(512), 0, stream, g);
+    hipLaunchKernelGGL((k_linear_tile<BF, 256, 256, 128, 64, 64, 2>), dim3(big), dim3(512), 0,
+                       stream, g);
   } else {
     const int64_t n = int64_t((g.rows + 127) / 128) * ((g.N + 127) / 128);
-    hipLaunchKernelGGL((k_linear_tile<BF, 128, 128, 64, 64>), dim3(n), dim3(256), 0, stream, g);
+    hipLaunchKernelGGL((k_linear_tile<BF, 128, 128, 64, 64, 64, 2>), dim3(n), dim3(256), 0, stream,
+                       g);
   }
 }
 
