@@ -287,16 +287,10 @@ __global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
 
 // Row tiles of k_attn_chunk: request s owns tile numbers from q_off[s] * G / 128 + s on.
 __device__ inline void chunk_tile(const AttnArgs &a, int32_t b, int32_t &s, int32_t &r0) {
-  int32_t lo = 0, hi = a.n_seqs - 1;
-  while (lo < hi) {
-    const int32_t mid = (lo + hi + 1) >> 1;
-    if (__ldg(a.q_off + mid) * a.group / kChunkRows + mid <= b)
-      lo = mid;
-    else
-      hi = mid - 1;
-  }
-  s = lo;
-  r0 = (b - __ldg(a.q_off + lo) * a.group / kChunkRows - lo) * kChunkRows;
+  s = last_at_most(a.n_seqs, b, [&](int32_t i) {
+    return __ldg(a.q_off + i) * a.group / kChunkRows + i;
+  });
+  r0 = (b - __ldg(a.q_off + s) * a.group / kChunkRows - s) * kChunkRows;
 }
 
 // ---- chunks: four waves of 32 rows, 64 keys at a time

@@ -79,17 +79,31 @@ __device__ inline void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
 }
 
-// The request whose rows contain row t: the last s with q_off[s] <= t (t < q_off[n]).
-__device__ inline int32_t seq_of_row(const int32_t *q_off, int32_t n, int32_t t) {
-  int32_t lo = 0, hi = n - 1;
-  while (lo < hi) {
-    int32_t mid = (lo + hi + 1) >> 1;
-    if (__ldg(q_off + mid) <= t)
-      lo = mid;
-    else
-      hi = mid - 1;
+// The same for a wave that reads only what it loaded itself: reads_done() before a buffer
+// is loaded again, wait_own() before one is read.
+__device__ inline void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+template <int LEFT>
+__device__ inline void wait_own() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
+}
+
+// The last of the requests 0 .. n - 1 whose first(s) is at most b, by the whole wave: 64
+// probes a round instead of one.  first is non-decreasing and first(0) <= b.
+template <class F>
+__device__ inline int32_t last_at_most(int32_t n, int32_t b, F first) {
+  int32_t lo = 0, len = n;
+  while (len > 1) {
+    const int32_t step = (len + 63) >> 6, at = int32_t(__lane_id()) * step;
+    const int32_t hits = __popcll(__ballot(at < len && first(lo + at) <= b));
+    const int32_t from = lo + (hits - 1) * step;
+    len = min(step, lo + len - from);
+    lo = from;
   }
   return lo;
+}
+// The request whose rows contain row t (t < q_off[n]), by the whole wave.
+__device__ inline int32_t seq_of_row(const int32_t *q_off, int32_t n, int32_t t) {
+  return last_at_most(n, t, [&](int32_t s) { return __ldg(q_off + s); });
 }
 
 // Row tiles that never span two requests.  Request s owns the tile numbers from
@@ -100,14 +114,8 @@ struct RowTile {
 };
 template <int SHIFT>
 __device__ inline RowTile row_tile(const int32_t *q_off, int32_t n, int32_t b) {
-  int32_t lo = 0, hi = n - 1;
-  while (lo < hi) {
-    int32_t mid = (lo + hi + 1) >> 1;
-    if ((__ldg(q_off + mid) >> SHIFT) + mid <= b)
-      lo = mid;
-    else
-      hi = mid - 1;
-  }
+  const int32_t lo =
+      last_at_most(n, b, [&](int32_t s) { return (__ldg(q_off + s) >> SHIFT) + s; });
   const int32_t q0 = __ldg(q_off + lo), q1 = __ldg(q_off + lo + 1);
   RowTile t;
   t.s = lo;

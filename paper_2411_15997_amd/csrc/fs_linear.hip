@@ -44,11 +44,95 @@ __device__ inline int32_t adapter_of(const LinArgs &g, int32_t s, int32_t &rank,
   return a;
 }
 
-// One request's rows, 16 at a time, against its adapter's A; the waves share out K and
-// join in LDS.  JT: 16-column tiles of h.
-template <bool BF, int JT, int WAVES>
+// Which 16-byte chunk of its row lies in place c of row r of an LDS tile (and the other way
+// round): 16 rows' chunks of one column fall on different banks.
+template <int BK>
+__device__ inline int place_of(int r, int c) {
+  return BK == 64 ? c ^ ((r >> 1) & 7) : c ^ ((r >> 2) & 3);
+}
+
+// acc[m][n] += W x^T over this wave's share of K: MT tiles of 16 rows of x, NT of 16 rows of
+// w.  The waves take 64 of K in turn, each through STAGES buffers of its own that are filled
+// STAGES - 1 steps ahead, so they never wait for each other.  (Straight from memory in the
+// matrix cores' layout, 16 lanes would touch 16 rows: a quarter of the cache's rate.)
+template <bool BF, int MT, int NT, int WAVES, int STAGES>
+__device__ void share_of_k(const short *x, int64_t x_stride, int x_rows, const short *w, int w_rows,
+                           int K, int wave, short *lds, f32x4 (&acc)[MT][NT]) {
+  constexpr int TILE = 16 * 64, STEP = (MT + NT) * TILE, LOADS = 2 * (MT + NT);
+  const int lane = threadIdx.x & 63, r16 = lane & 15, g4 = lane >> 4;
+  short *mine = lds + wave * (STAGES * STEP);
+  const uint32_t at = lds_address(mine);
+  uint32_t off[LOADS];
+  int col[2];
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int r = i * 8 + (lane >> 3);  // of x's tiles, then w's
+    col[i & 1] = place_of<64>(r & 15, lane & 7) * 8;
+    off[i] = i < 2 * MT ? uint32_t(min(r, x_rows - 1) * x_stride + col[i & 1]) * 2
+                        : uint32_t(min(r - MT * 16, w_rows - 1) * K + col[i & 1]) * 2;
+  }
+  const int slices = (K + 63) / 64, n = slices > wave ? (slices - wave + WAVES - 1) / WAVES : 0;
+  auto issue = [&](int t) {
+    const int k = (wave + t * WAVES) * 64;
+    const uint32_t to = at + (t % STAGES) * STEP * 2;
+    if (k + 64 <= K) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) load_to_lds((i < 2 * MT ? x : w) + k, off[i], to + i * 1024);
+    } else {  // past the end of K: the last chunk of the row, its products are masked
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i)
+        load_to_lds((i < 2 * MT ? x : w) + k, off[i] + 2 * min(0, K - 8 - k - col[i & 1]),
+                    to + i * 1024);
+    }
+  };
+  auto multiply = [&](int t, bool whole) {
+    const short *b = mine + (t % STAGES) * STEP;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int c = u * 4 + g4, place = r16 * 64 + place_of<64>(r16, c) * 8;
+      s16x8 xf[MT], wf[NT];
+#pragma unroll
+      for (int m = 0; m < MT; ++m) xf[m] = *reinterpret_cast<const s16x8 *>(b + m * TILE + place);
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        wf[j] = *reinterpret_cast<const s16x8 *>(b + (MT + j) * TILE + place);
+      if (!whole) {
+        const s16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+        const bool in = (wave + t * WAVES) * 64 + c * 8 < K;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) xf[m] = in ? xf[m] : zero;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) wf[j] = in ? wf[j] : zero;
+      }
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[m][j] = mfma_16x16x32<BF>(wf[j], xf[m], acc[m][j]);
+    }
+  };
+#pragma unroll
+  for (int t = 0; t < STAGES - 1; ++t)
+    if (t < n) issue(t);
+  int t = 0;
+  for (; t + STAGES - 1 < n; ++t) {
+    reads_done();
+    issue(t + STAGES - 1);
+    wait_own<(STAGES - 1) * LOADS>();
+    multiply(t, true);
+  }
+  wait_own<0>();
+  for (; t < n; ++t) {
+    multiply(t, (wave + t * WAVES + 1) * 64 <= K);
+  }
+}
+
+// One request's rows, 16 at a time, against its adapter's A; the waves share out K and join
+// in LDS.  JT: 16-column tiles of h.
+template <bool BF, int JT, int WAVES, int STAGES>
 __global__ void __launch_bounds__(WAVES * 64) k_shrink(LinArgs g) {
-  __shared__ float part[WAVES][16][JT * 16 + 1];
+  constexpr int LOADED = WAVES * STAGES * (1 + JT) * 16 * 64;
+  __shared__ __align__(16) short lds[LOADED];
+  static_assert(LOADED >= WAVES * JT * 256 * 2, "room for the partial sums");
   const RowTile t = row_tile<4>(g.q_off, g.n_seqs, blockIdx.x);
   if (t.rows <= 0) return;
   int32_t code = 0, rank;
@@ -56,157 +140,121 @@ __global__ void __launch_bounds__(WAVES * 64) k_shrink(LinArgs g) {
   if (threadIdx.x == 0) raise_err(g.err, code);
   if (threadIdx.x < t.rows) g.row_ad[t.row0 + threadIdx.x] = rank > 0 ? ad : -1;
   if (ad < 0 || rank == 0) return;  // h of such rows is not looked at
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int r = lane & 15, kq = (lane >> 4) * 8;
-  f32x4 acc[JT] = {};
-  const short *xp = g.x + int64_t(t.row0 + min(r, t.rows - 1)) * g.x_stride;
-  const short *ap[JT];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  f32x4 acc[1][JT] = {};
+  share_of_k<BF, 1, JT, WAVES, STAGES>(g.x + int64_t(t.row0) * g.x_stride, g.x_stride, t.rows,
+                                        g.a + int64_t(ad) * g.R * g.K, rank, g.K, wave, lds, acc);
+  __syncthreads();
+  f32x4 *part = reinterpret_cast<f32x4 *>(lds);
 #pragma unroll
-  for (int j = 0; j < JT; ++j) ap[j] = g.a + (int64_t(ad) * g.R + min(j * 16 + r, rank - 1)) * g.K;
-  const s16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
-  // a wave takes 128 of K at a time
-  for (int k0 = wave * 128; k0 < g.K; k0 += WAVES * 128) {
-    s16x8 xv[4], av[JT][4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int k = k0 + u * 32 + kq;
-      xv[u] = k < g.K ? *reinterpret_cast<const s16x8 *>(xp + k) : zero;
-#pragma unroll
-      for (int j = 0; j < JT; ++j)
-        av[j][u] = k < g.K ? *reinterpret_cast<const s16x8 *>(ap[j] + k) : zero;
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-#pragma unroll
-      for (int j = 0; j < JT; ++j) acc[j] = mfma_16x16x32<BF>(xv[u], av[j][u], acc[j]);
-  }
-#pragma unroll
-  for (int j = 0; j < JT; ++j)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) part[wave][(lane >> 4) * 4 + i][j * 16 + r] = acc[j][i];
+  for (int j = 0; j < JT; ++j) part[(wave * JT + j) * 64 + lane] = acc[0][j];
   __syncthreads();
   const float scale = g.scale ? __ldg(g.scale + ad) : 1.f;
-  for (int e = threadIdx.x; e < 16 * JT * 16; e += WAVES * 64) {
-    const int row = e / (JT * 16), j = e % (JT * 16);
-    if (row >= t.rows || j >= g.R) continue;
-    float v = 0.f;
+  for (int e = threadIdx.x; e < JT * 64; e += WAVES * 64) {
+    f32x4 v = part[e];
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) v += part[w][row][j];
-    v = j < rank ? v * scale : 0.f;
-    const short hi = to_16<BF>(v);
-    short *hp = g.h + int64_t(t.row0 + row) * (2 * g.R) + j;
-    hp[0] = hi;
-    hp[g.R] = to_16<BF>(v - to_f32<BF>(hi));
+    for (int w = 1; w < WAVES; ++w) v += part[w * JT * 64 + e];
+    const int row = e & 15, j0 = (e >> 4) * 4;
+    if (row >= t.rows || j0 >= g.R) continue;
+    s16x4 hi, lo;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float f = j0 + i < rank ? v[i] * scale : 0.f;
+      hi[i] = to_16<BF>(f);
+      lo[i] = to_16<BF>(f - to_f32<BF>(hi[i]));
+    }
+    short *hp = g.h + int64_t(t.row0 + row) * (2 * g.R) + j0;
+    *reinterpret_cast<s16x4 *>(hp) = hi;
+    *reinterpret_cast<s16x4 *>(hp + g.R) = lo;
   }
 }
 
-// B_a[n][j .. j + 7], columns at and beyond the rank as 0.
+// B_a[n][j .. j + 7], columns at and beyond the rank as 0 (j at most R; loaded before the
+// rank is looked at, so that the two loads go side by side).
 __device__ inline s16x8 load_b(const LinArgs &g, int32_t ad, int32_t rank, int32_t n, int j) {
-  s16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
-  if (j < rank) {
-    v = *reinterpret_cast<const s16x8 *>(g.b + (int64_t(ad) * g.N + n) * g.R + j);
-    if (j + 8 > rank)
+  s16x8 v = *reinterpret_cast<const s16x8 *>(g.b + (int64_t(ad) * g.N + n) * g.R + min(j, g.R - 8));
+  if (j + 8 > rank)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = j + i < rank ? v[i] : short(0);
-  }
+    for (int i = 0; i < 8; ++i) v[i] = j + i < rank ? v[i] : short(0);
   return v;
 }
 __device__ inline int32_t rank_of(const LinArgs &g, int32_t ad) {
   return g.rank ? min(__ldg(g.rank + ad), g.R) : g.R;
 }
 
-// ---- few rows: MT tiles of 16 rows by NT tiles of 16 columns
-template <bool BF, int MT, int NT>
-__global__ void __launch_bounds__(512) k_linear_few(LinArgs g) {
-  __shared__ f32x4 part[8][MT * NT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int r = lane & 15, kq = (lane >> 4) * 8;
+// ---- few rows: MT tiles of 16 rows by NT tiles of 16 columns, four waves
+template <bool BF, int MT, int NT, int STAGES>
+__global__ void __launch_bounds__(256) k_linear_few(LinArgs g) {
+  __shared__ __align__(16) short lds[4 * STAGES * (MT + NT) * 16 * 64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15;
   const int n0 = blockIdx.x * (NT * 16), m0 = blockIdx.y * (MT * 16);
   const s16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+  // the adapters of the tile of rows that this wave deals with
+  const int my = wave % MT, my_row = m0 + my * 16 + r;
+  const int32_t ad = g.n_adapters > 0 && my_row < g.rows ? __ldg(g.row_ad + my_row) : -1;
   f32x4 acc[MT][NT] = {};
-  const short *xp[MT], *wp[NT];
-#pragma unroll
-  for (int m = 0; m < MT; ++m)
-    xp[m] = g.x + int64_t(min(m0 + m * 16 + r, g.rows - 1)) * g.x_stride + kq;
-#pragma unroll
-  for (int n = 0; n < NT; ++n) wp[n] = g.w + int64_t(min(n0 + n * 16 + r, g.N - 1)) * g.K + kq;
-  // a wave takes 128 of K at a time
-  int k0 = wave * 128;
-  for (; k0 + 128 <= g.K; k0 += 1024) {
-    s16x8 wv[NT][4], xv[MT][4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-        wv[n][u] = *reinterpret_cast<const s16x8 *>(wp[n] + k0 + u * 32);
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-        xv[m][u] = *reinterpret_cast<const s16x8 *>(xp[m] + k0 + u * 32);
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc[m][n] = mfma_16x16x32<BF>(wv[n][u], xv[m][u], acc[m][n]);
-  }
-  if (k0 < g.K) {
-    for (int u = 0; u < 4; ++u) {
-      const int k = k0 + u * 32;
-      const bool in = k + kq < g.K;
-      s16x8 wv[NT];
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-        wv[n] = in ? *reinterpret_cast<const s16x8 *>(wp[n] + k) : zero;
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        const s16x8 xv = in ? *reinterpret_cast<const s16x8 *>(xp[m] + k) : zero;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc[m][n] = mfma_16x16x32<BF>(wv[n], xv, acc[m][n]);
-      }
-    }
-  }
-  if (g.n_adapters > 0) {
-    // the distinct adapters of a tile's rows, shared out over the waves that hold the tile
+  share_of_k<BF, MT, NT, 4, STAGES>(g.x + int64_t(m0) * g.x_stride, g.x_stride, g.rows - m0,
+                                    g.w + int64_t(n0) * g.K, g.N - n0, g.K, wave, lds, acc);
+  // The distinct adapters of a tile's rows, shared out over the 4 / MT waves that hold the
+  // tile: four adapters' loads side by side, 4 chunks of 8 columns at a time (R/8 high
+  // ones, then R/8 low ones).
+  uint64_t left = __ballot(ad >= 0);
+  if (left) {
     const int chunks = g.R / 8;
+    const short *hp = g.h + int64_t(min(my_row, g.rows - 1)) * (2 * g.R);
+    f32x4 sum[NT] = {};
+    for (int turn = 0; left;) {
+      int32_t who[4] = {-1, -1, -1, -1}, rank[4] = {0, 0, 0, 0};
+      int found = 0;
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      if (wave % MT != m) continue;
-      const int row = m0 + m * 16 + r;
-      const int32_t ad = row < g.rows ? __ldg(g.row_ad + row) : -1;
-      const short *hp = g.h + int64_t(min(row, g.rows - 1)) * (2 * g.R);
-      uint64_t left = __ballot(ad >= 0);
-      for (int turn = 0; left; ++turn) {
-        const int32_t a = __builtin_amdgcn_readlane(ad, __builtin_ctzll(left));
-        const bool mine = ad == a;
-        left &= ~__ballot(mine);
-        if (turn % (8 / MT) != wave / MT) continue;
-        const int32_t rank = rank_of(g, a);
-        // chunks of 8 columns: R/8 high ones, then R/8 low ones
-        for (int c = lane >> 4; c < (2 * chunks + 3) / 4 * 4; c += 4) {
-          const bool in = c < 2 * chunks;
-          const s16x8 hv = mine && in ? *reinterpret_cast<const s16x8 *>(hp + c * 8) : zero;
-          const int j = in ? (c < chunks ? c : c - chunks) * 8 : g.R;
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-            acc[m][n] = mfma_16x16x32<BF>(
-                load_b(g, a, rank, min(n0 + n * 16 + r, g.N - 1), j), hv, acc[m][n]);
+      for (int i = 0; i < 4; ++i) {
+        while (left) {
+          const int32_t a = __builtin_amdgcn_readlane(ad, __builtin_ctzll(left));
+          left &= ~__ballot(ad == a);
+          if (turn++ % (4 / MT) == wave / MT) {
+            who[i] = a;
+            rank[i] = rank_of(g, a);
+            ++found;
+            break;
+          }
         }
       }
+      if (found == 0) break;
+      for (int c = lane >> 4; c < (2 * chunks + 3) / 4 * 4; c += 4) {
+        const bool in = c < 2 * chunks;
+        const s16x8 hv = in ? *reinterpret_cast<const s16x8 *>(hp + c * 8) : zero;
+        const int j = in ? (c < chunks ? c : c - chunks) * 8 : g.R;
+        s16x8 bv[4][NT];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            bv[i][n] = load_b(g, max(who[i], 0), rank[i], min(n0 + n * 16 + r, g.N - 1), j);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            sum[n] = mfma_16x16x32<BF>(bv[i][n], ad >= 0 && ad == who[i] ? hv : zero, sum[n]);
+      }
     }
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        if (m == my) acc[m][n] += sum[n];
   }
+  __syncthreads();
+  f32x4 *part = reinterpret_cast<f32x4 *>(lds);
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int n = 0; n < NT; ++n) part[wave][m * NT + n][lane] = acc[m][n];
+    for (int n = 0; n < NT; ++n) part[(wave * MT * NT + m * NT + n) * 64 + lane] = acc[m][n];
   __syncthreads();
-  for (int t = wave; t < MT * NT; t += 8) {
-    f32x4 v = part[0][t][lane];
+  for (int t = wave; t < MT * NT; t += 4) {
+    f32x4 v = part[t * 64 + lane];
 #pragma unroll
-    for (int w = 1; w < 8; ++w) v += part[w][t][lane];
+    for (int w = 1; w < 4; ++w) v += part[(w * MT * NT + t) * 64 + lane];
     const int row = m0 + (t / NT) * 16 + r, n = n0 + (t % NT) * 16 + (lane >> 4) * 4;
     if (row < g.rows && n < g.N) {
       s16x4 o;
@@ -215,13 +263,6 @@ __global__ void __launch_bounds__(512) k_linear_few(LinArgs g) {
       *reinterpret_cast<s16x4 *>(g.y + int64_t(row) * g.y_stride + n) = o;
     }
   }
-}
-
-// Which 16-byte chunk of its row lies in place c of row r of an LDS tile (and the other way
-// round): 16 rows' chunks of one column fall on different banks.
-template <int BK>
-__device__ inline int place_of(int r, int c) {
-  return BK == 64 ? c ^ ((r >> 1) & 7) : c ^ ((r >> 2) & 3);
 }
 
 // ---- many rows: BM rows by BN columns a work-group, K in steps of BK through STAGES LDS
@@ -289,32 +330,38 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) k_linear_tile(LinA
   };
   auto multiply = [&](int step, bool whole) {
     const short *xt = xs[step % STAGES], *wt = ws[step % STAGES];
-#pragma unroll
-    for (int u = 0; u < BK / 16; ++u) {
-      s16x8 xf[MT], wf[NT];
+    s16x8 xf[2][MT], wf[2][NT];
+    auto operands = [&](int u) {
       const int c = u * 2 + h2;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         const int r = wn + n * 32 + r32;
-        wf[n] = *reinterpret_cast<const s16x8 *>(wt + r * BK + place_of<BK>(r, c) * 8);
+        wf[u & 1][n] = *reinterpret_cast<const s16x8 *>(wt + r * BK + place_of<BK>(r, c) * 8);
       }
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         const int r = wm + m * 32 + r32;
-        xf[m] = *reinterpret_cast<const s16x8 *>(xt + r * BK + place_of<BK>(r, c) * 8);
+        xf[u & 1][m] = *reinterpret_cast<const s16x8 *>(xt + r * BK + place_of<BK>(r, c) * 8);
       }
       if (!whole) {
         const s16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
         const bool in = step * BK + c * 8 < g.K;
 #pragma unroll
-        for (int m = 0; m < MT; ++m) xf[m] = in ? xf[m] : zero;
+        for (int m = 0; m < MT; ++m) xf[u & 1][m] = in ? xf[u & 1][m] : zero;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) wf[n] = in ? wf[n] : zero;
+        for (int n = 0; n < NT; ++n) wf[u & 1][n] = in ? wf[u & 1][n] : zero;
       }
+    };
+    // the next 16 columns' operands are read while these are multiplied
+    operands(0);
+#pragma unroll
+    for (int u = 0; u < BK / 16; ++u) {
+      if (u + 1 < BK / 16) operands(u + 1);
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) acc[m][n] = mfma_32x32x16<BF>(wf[n], xf[m], acc[m][n]);
+        for (int n = 0; n < NT; ++n) acc[m][n] = mfma_32x32x16<BF>(wf[u & 1][n], xf[u & 1][m], acc[m][n]);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
   const int steps = (g.K + BK - 1) / BK, full = g.K / BK;
@@ -329,10 +376,7 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) k_linear_tile(LinA
   }
   for (; step < steps; ++step) {
     wait_loads<0>();
-    if (step < full)
-      multiply(step, true);
-    else
-      multiply(step, false);
+    multiply(step, step < full);
   }
   const s16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
   if (g.n_adapters > 0) {
@@ -378,40 +422,44 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) k_linear_tile(LinA
 }
 
 template <bool BF, int JT>
-void shrink(const LinArgs &g, int64_t tiles, hipStream_t stream) {
-  // few tiles: more waves share out K, so that one tile's time is short
-  constexpr int kMost = JT <= 4 ? 16 : 8;  // by registers
+void shrink(const LinArgs &g, const fs_step *st, hipStream_t stream) {
+  const int64_t tiles = row_tiles(st, 4);
+  // few tiles: more waves share out K, so that one tile's time is short (as LDS allows);
+  // many: the loads of several steps are under way
+  constexpr int kMost = JT == 1 ? 16 : JT <= 4 ? 8 : 4;
+  constexpr int kStages = JT == 1 ? 4 : JT == 2 ? 3 : 2;
   if (tiles <= 512)
-    hipLaunchKernelGGL((k_shrink<BF, JT, kMost>), dim3(tiles), dim3(kMost * 64), 0, stream, g);
+    hipLaunchKernelGGL((k_shrink<BF, JT, kMost, 2>), dim3(tiles), dim3(kMost * 64), 0, stream, g);
   else
-    hipLaunchKernelGGL((k_shrink<BF, JT, 4>), dim3(tiles), dim3(256), 0, stream, g);
+    hipLaunchKernelGGL((k_shrink<BF, JT, 4, kStages>), dim3(tiles), dim3(256), 0, stream, g);
 }
 
 template <bool BF, int MT>
 void few(const LinArgs &g, hipStream_t stream) {
   const int mb = (g.rows + MT * 16 - 1) / (MT * 16);
-  // 16 columns a work-group while that does not exceed the compute units
-  if ((g.N + 15) / 16 * mb <= 256)
-    hipLaunchKernelGGL((k_linear_few<BF, MT, 1>), dim3((g.N + 15) / 16, mb), dim3(512), 0, stream,
-                       g);
+  constexpr int kStages = MT == 4 ? 2 : MT == 2 ? 3 : 4;  // 64 to 80 KB of LDS for 16 columns
+  // 16 columns a work-group while two of them on each compute unit hold them all
+  if ((g.N + 15) / 16 * mb <= 512)
+    hipLaunchKernelGGL((k_linear_few<BF, MT, 1, kStages>), dim3((g.N + 15) / 16, mb), dim3(256), 0,
+                       stream, g);
   else
-    hipLaunchKernelGGL((k_linear_few<BF, MT, 2>), dim3((g.N + 31) / 32, mb), dim3(512), 0, stream,
-                       g);
+    hipLaunchKernelGGL((k_linear_few<BF, MT, 2, kStages>), dim3((g.N + 31) / 32, mb), dim3(256), 0,
+                       stream, g);
 }
 
 template <bool BF>
-void run(const LinArgs &g, int64_t tiles, hipStream_t stream) {
+void run(const LinArgs &g, const fs_step *st, hipStream_t stream) {
   if (g.n_adapters > 0) {
     if (g.R <= 16)
-      shrink<BF, 1>(g, tiles, stream);
+      shrink<BF, 1>(g, st, stream);
     else if (g.R <= 32)
-      shrink<BF, 2>(g, tiles, stream);
+      shrink<BF, 2>(g, st, stream);
     else if (g.R <= 64)
-      shrink<BF, 4>(g, tiles, stream);
+      shrink<BF, 4>(g, st, stream);
     else
-      shrink<BF, 8>(g, tiles, stream);
+      shrink<BF, 8>(g, st, stream);
   }
-  if (g.rows <= 256) {
+  if (g.rows <= 64) {
     if (g.rows <= 16)
       few<BF, 1>(g, stream);
     else if (g.rows <= 32)
@@ -420,15 +468,17 @@ void run(const LinArgs &g, int64_t tiles, hipStream_t stream) {
       few<BF, 4>(g, stream);
     return;
   }
-  const int64_t big = int64_t((g.rows + 255) / 256) * ((g.N + 255) / 256);
-  if (big >= 256) {
-    hipLaunchKernelGGL((k_linear_tile<BF, 256, 256, 128, 64, 64, 2>), dim3(big), dim3(512), 0,
+  // The largest tiles that still occupy three quarters of the compute units.
+  auto tiles = [&](int64_t t) { return ((g.rows + t - 1) / t) * ((g.N + t - 1) / t); };
+  if (tiles(256) >= 192)
+    hipLaunchKernelGGL((k_linear_tile<BF, 256, 256, 128, 64, 64, 2>), dim3(tiles(256)), dim3(512),
+                       0, stream, g);
+  else if (tiles(128) >= 192)
+    hipLaunchKernelGGL((k_linear_tile<BF, 128, 128, 64, 64, 64, 2>), dim3(tiles(128)), dim3(256), 0,
                        stream, g);
-  } else {
-    const int64_t n = int64_t((g.rows + 127) / 128) * ((g.N + 127) / 128);
-    hipLaunchKernelGGL((k_linear_tile<BF, 128, 128, 64, 64, 64, 2>), dim3(n), dim3(256), 0, stream,
-                       g);
-  }
+  else
+    hipLaunchKernelGGL((k_linear_tile<BF, 64, 64, 32, 32, 64, 4>), dim3(tiles(64)), dim3(256), 0,
+                       stream, g);
 }
 
 }  // namespace
@@ -462,11 +512,10 @@ hipError_t launch_adapter_linear(const fs_step *s, const fs_adapters *ad, const 
   g.x_stride = x_stride;
   g.y_stride = y_stride;
   g.err = err;
-  const int64_t tiles = row_tiles(s, 4);
   if (ad->dtype == FS_BF16)
-    run<true>(g, tiles, stream);
+    run<true>(g, s, stream);
   else
-    run<false>(g, tiles, stream);
+    run<false>(g, s, stream);
   return hipGetLastError();
 }
 

@@ -48,23 +48,26 @@ __global__ void __launch_bounds__(256) k_rope_append(RopeArgs a) {
   const int32_t t0 = blockIdx.x * kTok;
   const int32_t nt = min(kTok, a.rows - t0);
   const int tid = threadIdx.x;
-  if (tid < nt) {
-    int32_t code = 0;
-    const int32_t t = t0 + tid;
+  // a wave for each token
+  if (tid >> 6 < nt) {
+    const int32_t i = tid >> 6, t = t0 + i;
     const int32_t s = seq_of_row(a.q_off, a.n_seqs, t);
-    const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
-    const int32_t p = kv - (__ldg(a.q_off + s + 1) - t);
-    int64_t at = -1;
-    if (p >= 0) {
-      const int32_t id = __ldg(a.c.table + s * a.c.table_stride + (p >> a.c.page_shift));
-      if (uint32_t(id) < uint64_t(a.c.n_pages))
-        at = id * a.c.page_stride + (p & ((1 << a.c.page_shift) - 1)) * a.c.token_stride;
-      else
-        code = FS_E_RANGE;
+    if ((tid & 63) == 0) {
+      int32_t code = 0;
+      const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
+      const int32_t p = kv - (__ldg(a.q_off + s + 1) - t);
+      int64_t at = -1;
+      if (p >= 0) {
+        const int32_t id = __ldg(a.c.table + s * a.c.table_stride + (p >> a.c.page_shift));
+        if (uint32_t(id) < uint64_t(a.c.n_pages))
+          at = id * a.c.page_stride + (p & ((1 << a.c.page_shift) - 1)) * a.c.token_stride;
+        else
+          code = FS_E_RANGE;
+      }
+      slot[i] = at;
+      where[i] = a.pos ? __ldg(a.pos + t) : max(p, 0);
+      raise_err(a.err, code);
     }
-    slot[tid] = at;
-    where[tid] = a.pos ? __ldg(a.pos + t) : max(p, 0);
-    raise_err(a.err, code);
   }
   __syncthreads();
   const int half = a.rotary / 2;
