@@ -55,8 +55,9 @@ typedef struct fs_step {
  * and the same for v (strides in elements; d contiguous).  Pages may be shared between
  * requests (a common prompt prefix), in any order.  dtype FS_BF16 or FS_F16;
  * page_size a power of two in [1, 4096]; page ids in [0, n_pages), else FS_E_RANGE.
- * k, v and the strides must keep rows 16-byte aligned.  Slots at and after kv_len are
- * never used, whatever they hold. */
+ * k, v and the strides must keep rows 16-byte aligned; strides below 2^31, a page's own rows
+ * within 2^30 elements (a cache of any size).  Slots at and after kv_len are never used,
+ * whatever they hold. */
 typedef struct fs_kv_cache {
   int32_t dtype, n_kv_heads, head_dim, page_size;
   int64_t n_pages;

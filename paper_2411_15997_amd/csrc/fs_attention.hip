@@ -85,20 +85,25 @@ __device__ inline s16x8 pack8(const float *p) {
   return v;
 }
 
-// Element offset of a key's row in the cache (either of k and v).
-__device__ inline int64_t key_at(const DevCache &c, const int32_t *table, int32_t j, int64_t head,
-                                 int32_t &code) {
-  const int64_t page = checked_page(c, table + (j >> c.page_shift), code);
-  return page * c.page_stride + head + (j & ((1 << c.page_shift) - 1)) * c.token_stride;
+// A row keeps the reference of its exponentials until a score passes it by 2^kSlack, so
+// that its sums are seldom scaled; probabilities then reach 2^kSlack, which costs no
+// precision.
+constexpr float kSlack = 8.f;
+
+// The larger of the two halves' values, in both.
+__device__ inline float max_of_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
 // ---- few rows: NT tiles of 16 rows
-template <bool BF, int D, int NT>
-__global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
+template <bool BF, int D, int NT, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64) k_attn_few(AttnArgs a) {
+  constexpr int STEP = WAVES * 32;  // keys of the work-group's waves side by side
   constexpr int KS = D / 32;  // matrix steps of a score, and 16-byte chunks of a lane's row
   constexpr int DB = D / 16;  // 16-column blocks of an output row
-  __shared__ __align__(16) short vt[4][32 * D];
-  __shared__ float wm[4][NT * 16], wl[4][NT * 16];
+  __shared__ __align__(16) short vt[WAVES][32 * D];
+  __shared__ float wm[WAVES][NT * 16], wl[WAVES][NT * 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int r16 = lane & 15, g4 = lane >> 4;
   // Work-groups go to the 8 dies in turn: heads fastest, and each split shifts the
@@ -116,7 +121,7 @@ __global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
   if (z > 0 && lo >= kr.hi) return;
   const int32_t hi = min(kr.hi, lo + a.few_split);
   const int32_t *table = a.c.table + s * a.c.table_stride;
-  const int64_t head = hk * a.c.head_stride;
+  const uint32_t head = hk * a.c.head_stride;
   const short *kp = reinterpret_cast<const short *>(a.c.k) + g4 * 8;
   const short *vp = reinterpret_cast<const short *>(a.c.v) + g4 * 8;
 
@@ -140,13 +145,16 @@ __global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
   for (int t = 0; t < NT; ++t) m[t] = -INFINITY, l[t] = 0.f;
 
   s16x8 kf[2][KS], vf[2][KS];
-  int64_t at[2];
+  uint64_t at[2];
+  auto key_at = [&](int32_t j) {
+    return row_at(a.c, __ldg(table + (j >> a.c.page_shift)), j, head, code);
+  };
   const int32_t first = lo + wave * 32;
   short *tile = vt[wave];
   if (first < hi) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      at[b] = key_at(a.c, table, min(first + b * 16 + r16, hi - 1), head, code);
+      at[b] = key_at(min(first + b * 16 + r16, hi - 1));
 #pragma unroll
       for (int k = 0; k < KS; ++k) kf[b][k] = *reinterpret_cast<const s16x8 *>(kp + at[b] + k * 32);
     }
@@ -157,9 +165,9 @@ __global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
     // the next tile's places, one tile ahead of its rows
 #pragma unroll
     for (int b = 0; b < 2; ++b)
-      at[b] = key_at(a.c, table, min(first + 128 + b * 16 + r16, hi - 1), head, code);
+      at[b] = key_at(min(first + STEP + b * 16 + r16, hi - 1));
   }
-  for (int32_t j0 = first; j0 < hi; j0 += 128) {
+  for (int32_t j0 = first; j0 < hi; j0 += STEP) {
     f32x4 sc[NT][2] = {};
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -172,7 +180,7 @@ __global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
 #pragma unroll
       for (int k = 0; k < KS; ++k)
         *reinterpret_cast<s16x8 *>(tile + tile_at<D>(b * 16 + r16, k * 4 + g4)) = vf[b][k];
-    if (j0 + 128 < hi) {
+    if (j0 + STEP < hi) {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -185,7 +193,7 @@ __global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
           vf[b][k] = *reinterpret_cast<const s16x8 *>(vp + at[b] + k * 32);
 #pragma unroll
       for (int b = 0; b < 2; ++b)
-        at[b] = key_at(a.c, table, min(j0 + 256 + b * 16 + r16, hi - 1), head, code);
+        at[b] = key_at(min(j0 + 2 * STEP + b * 16 + r16, hi - 1));
     }
     s16x8 pf[NT];
 #pragma unroll
@@ -200,10 +208,10 @@ __global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
           p[b * 4 + i] = see ? sc[t][b][i] : -INFINITY;
           top = fmaxf(top, p[b * 4 + i]);
         }
-      top = fmaxf(top, __shfl_xor(top, 16, 64));
-      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      top = max_of_halves(fmaxf(top, __shfl_xor(top, 16, 64)));
       const float m2 = fmaxf(m[t], top);
-      if (__any(m2 > m[t])) {
+      // (-inf less -inf is no number and asks for nothing)
+      if (__any((m2 - m[t]) * a.c2 > kSlack)) {
         const float f = m[t] == -INFINITY ? 0.f : exp2_fast((m[t] - m2) * a.c2);
         l[t] *= f;
 #pragma unroll
@@ -231,14 +239,14 @@ __global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
   }
   raise_err(a.err, code);
 
-  // the four waves' results, joined in LDS a tile of rows at a time
+  // the waves' results, joined in LDS a tile of rows at a time
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     l[t] += __shfl_xor(l[t], 16, 64);
     l[t] += __shfl_xor(l[t], 32, 64);
     if (g4 == 0) wm[wave][t * 16 + r16] = m[t], wl[wave][t * 16 + r16] = l[t];
   }
-  float *buf = reinterpret_cast<float *>(vt);  // [4][16][D / 2]: half of the columns at a time
+  float *buf = reinterpret_cast<float *>(vt);  // [WAVES][16][D / 2]: half of the columns at a time
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     if (t * 16 >= R) break;
@@ -250,15 +258,17 @@ __global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
         *reinterpret_cast<f32x4 *>(buf + (wave * 16 + r16) * (D / 2) +
                                    ((d * 16 + g4 * 4) ^ ((r16 & 3) * 4))) = o[t][half * (DB / 2) + d];
       __syncthreads();
-      for (int e = tid; e < 16 * D / 8; e += 256) {
+      for (int e = tid; e < 16 * D / 8; e += WAVES * 64) {
         const int r = e / (D / 8), col = (e - r * (D / 8)) * 4;
         if (t * 16 + r >= R) continue;
         const int tr = t * 16 + r;
-        const float top = fmaxf(fmaxf(wm[0][tr], wm[1][tr]), fmaxf(wm[2][tr], wm[3][tr]));
+        float top = wm[0][tr];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, wm[w][tr]);
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
         float sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
           const float f = wm[w][tr] == -INFINITY ? 0.f : exp2_fast((wm[w][tr] - top) * a.c2);
           sum += f * wl[w][tr];
           acc += f * *reinterpret_cast<const f32x4 *>(buf + (w * 16 + r) * (D / 2) +
@@ -299,9 +309,10 @@ __global__ void __launch_bounds__(256, 2) k_attn_chunk(AttnArgs a) {
   constexpr int KS = D / 16;       // matrix steps of a score
   constexpr int DB = D / 32;       // 32-column blocks of an output row
   constexpr int CH = D / 8;        // 16-byte chunks of a key row
-  constexpr int LD = 64 * CH / 256;  // chunks a thread loads of K, and of V
-  __shared__ __align__(16) short kt[64 * D], vt[64 * D];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int RW = 64 / CH;      // rows of a wave's load
+  constexpr int LD = 16 / RW;      // a wave's loads of K, and of V, for 64 keys
+  __shared__ __align__(16) short kt[2][64 * D], vt[2][64 * D];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r32 = lane & 31, h2 = lane >> 5;
   const int hk = blockIdx.x % a.c.n_kv_heads;
   // the last tiles of a request see the most keys: they go first
@@ -319,7 +330,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_chunk(AttnArgs a) {
   if (blockIdx.y > 0 && lo >= kr.hi) return;
   const int32_t hi = min(kr.hi, lo + a.chunk_split);
   const int32_t *table = a.c.table + s * a.c.table_stride;
-  const int64_t head = hk * a.c.head_stride;
+  const uint32_t head = hk * a.c.head_stride;
 
   const int row = r0 + wave * 32 + r32;
   const int tok = min(row, R - 1) / G, h = hk * G + (min(row, R - 1) - tok * G);
@@ -340,35 +351,50 @@ __global__ void __launch_bounds__(256, 2) k_attn_chunk(AttnArgs a) {
   f32x16 o[DB] = {};
   float m = -INFINITY, l = 0.f;
 
-  const int lr = tid / CH, lc = tid % CH;  // this thread's row (of 256 / CH) and chunk
-  s16x8 kreg[LD], vreg[LD];
-  auto load = [&](int32_t j0) {
+  // This lane's row and 16-byte chunk of each of the wave's loads: a wave loads the keys
+  // 16 * wave .. + 15 of K and V, RW rows at a time.
+  int32_t lrow[LD];
+  uint32_t lcol[LD], page[LD];
+#pragma unroll
+  for (int i = 0; i < LD; ++i) {
+    lrow[i] = wave * 16 + i * RW + lane / CH;
+    lcol[i] = head + (tile_at<D>(lrow[i], lane % CH) - lrow[i] * D);
+  }
+  // page ids are loaded one tile ahead of the rows
+  auto pages = [&](int32_t j0) {
+#pragma unroll
+    for (int i = 0; i < LD; ++i)
+      page[i] = __ldg(table + (min(j0 + lrow[i], hi - 1) >> a.c.page_shift));
+  };
+  const uint32_t k_to = lds_address(kt[0] + wave * 16 * D), v_to = lds_address(vt[0] + wave * 16 * D);
+  auto issue = [&](int32_t j0, int buf) {
 #pragma unroll
     for (int i = 0; i < LD; ++i) {
-      const int64_t at =
-          key_at(a.c, table, min(j0 + i * (256 / CH) + lr, hi - 1), head, code) + lc * 8;
-      kreg[i] = *reinterpret_cast<const s16x8 *>(reinterpret_cast<const short *>(a.c.k) + at);
-      vreg[i] = *reinterpret_cast<const s16x8 *>(reinterpret_cast<const short *>(a.c.v) + at);
+      const uint64_t at = 2 * row_at(a.c, page[i], min(j0 + lrow[i], hi - 1), lcol[i], code);
+      load_to_lds(a.c.k + at, k_to + (buf * 64 + i * RW) * D * 2);
+      load_to_lds(a.c.v + at, v_to + (buf * 64 + i * RW) * D * 2);
     }
   };
-  if (lo < hi) load(lo);
-  for (int32_t j0 = lo; j0 < hi; j0 += 64) {
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < LD; ++i) {
-      const int at = tile_at<D>(i * (256 / CH) + lr, lc);
-      *reinterpret_cast<s16x8 *>(kt + at) = kreg[i];
-      *reinterpret_cast<s16x8 *>(vt + at) = vreg[i];
+  if (lo < hi) {
+    pages(lo);
+    issue(lo, 0);
+    pages(lo + 64);
+  }
+  int buf = 0;
+  for (int32_t j0 = lo; j0 < hi; j0 += 64, buf ^= 1) {
+    wait_loads<0>();
+    if (j0 + 64 < hi) {
+      issue(j0 + 64, buf ^ 1);
+      pages(j0 + 128);
     }
-    __syncthreads();
-    if (j0 + 64 < hi) load(j0 + 64);
+    const short *kb = kt[buf], *vb = vt[buf];
     f32x16 sc[2] = {};
 #pragma unroll
     for (int k = 0; k < KS; ++k)
 #pragma unroll
       for (int c = 0; c < 2; ++c)
         sc[c] = mfma_32x32x16<BF>(
-            *reinterpret_cast<const s16x8 *>(kt + tile_at<D>(c * 32 + r32, k * 2 + h2)), qf[k],
+            *reinterpret_cast<const s16x8 *>(kb + tile_at<D>(c * 32 + r32, k * 2 + h2)), qf[k],
             sc[c]);
     // keys that some row of the wave does not see
     if (j0 + 63 > pos_lo || j0 + 64 > hi || j0 <= win_hi) {
@@ -385,9 +411,8 @@ __global__ void __launch_bounds__(256, 2) k_attn_chunk(AttnArgs a) {
     for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[0][i]);
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[1][i]);
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    const float m2 = fmaxf(m, top);
-    if (__any(m2 > m)) {
+    const float m2 = fmaxf(m, max_of_halves(top));
+    if (__any((m2 - m) * a.c2 > kSlack)) {
       const float f = m == -INFINITY ? 0.f : exp2_fast((m - m2) * a.c2);
       l *= f;
 #pragma unroll
@@ -411,8 +436,8 @@ __global__ void __launch_bounds__(256, 2) k_attn_chunk(AttnArgs a) {
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
           const int col = d * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-          const s16x4 v0 = read_tr(vt + tile_at<D>(vr, col >> 3) + (col & 7));
-          const s16x4 v1 = read_tr(vt + tile_at<D>(vr + 8, col >> 3) + (col & 7));
+          const s16x4 v0 = read_tr(vb + tile_at<D>(vr, col >> 3) + (col & 7));
+          const s16x4 v1 = read_tr(vb + tile_at<D>(vr + 8, col >> 3) + (col & 7));
           o[d] = mfma_32x32x16<BF>(__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7), pf,
                                    o[d]);
         }
@@ -608,11 +633,14 @@ void run(const AttnArgs &a, const Plan &p, hipStream_t stream) {
   if (p.few_seqs > 0) {
     const dim3 grid(uint32_t(a.n_seqs) * a.c.n_kv_heads * p.few_splits);
     if (p.few_rows <= 16)
-      hipLaunchKernelGGL((k_attn_few<BF, D, 1>), grid, block, 0, stream, a);
+      if (grid.x <= 256)  // one work-group a compute unit at most: twice the waves in it
+        hipLaunchKernelGGL((k_attn_few<BF, D, 1, 8>), grid, dim3(512), 0, stream, a);
+      else
+        hipLaunchKernelGGL((k_attn_few<BF, D, 1, 4>), grid, block, 0, stream, a);
     else if (p.few_rows <= 32)
-      hipLaunchKernelGGL((k_attn_few<BF, D, 2>), grid, block, 0, stream, a);
+      hipLaunchKernelGGL((k_attn_few<BF, D, 2, 4>), grid, block, 0, stream, a);
     else
-      hipLaunchKernelGGL((k_attn_few<BF, D, 4>), grid, block, 0, stream, a);
+      hipLaunchKernelGGL((k_attn_few<BF, D, 4, 4>), grid, block, 0, stream, a);
   }
   if (p.chunk_seqs > 0)
     hipLaunchKernelGGL((k_attn_chunk<BF, D>), dim3(p.chunk_tiles * a.c.n_kv_heads, p.chunk_splits),

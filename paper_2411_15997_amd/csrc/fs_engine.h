@@ -68,6 +68,11 @@ __device__ inline void load_to_lds(const void *base, uint32_t offset, uint32_t a
                "v"(offset), "s"(base)
                : "memory");
 }
+// The same from each lane's own 64-bit address.
+__device__ inline void load_to_lds(const void *from, uint32_t at) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from)
+               : "memory");
+}
 __device__ inline uint32_t lds_address(const void *p) {
   return __builtin_amdgcn_readfirstlane(
       uint32_t(uintptr_t((__attribute__((address_space(3))) const void *)p)));
@@ -127,11 +132,11 @@ inline int64_t row_tiles(const fs_step *s, int shift) {
   return (int64_t(s->q_off_h[s->n_seqs]) >> shift) + s->n_seqs;
 }
 
-// A cache as kernels see it (page_size = 1 << page_shift).
+// A cache as kernels see it (page_size = 1 << page_shift).  Offsets are in elements; one
+// inside a page fits 31 bits, as the page stride does (checked on the host).
 struct DevCache {
   const char *k, *v;
-  int64_t page_stride, head_stride, token_stride;  // elements
-  int64_t n_pages;
+  uint32_t page_stride, head_stride, token_stride, n_pages;
   const int32_t *table;
   int64_t table_stride;
   int32_t page_shift, n_kv_heads, head_dim;
@@ -141,10 +146,10 @@ inline DevCache dev_cache(const fs_kv_cache *c) {
   DevCache d;
   d.k = static_cast<const char *>(c->k);
   d.v = static_cast<const char *>(c->v);
-  d.page_stride = c->page_stride;
-  d.head_stride = c->head_stride;
-  d.token_stride = c->token_stride;
-  d.n_pages = c->n_pages;
+  d.page_stride = uint32_t(c->page_stride);
+  d.head_stride = uint32_t(c->head_stride);
+  d.token_stride = uint32_t(c->token_stride);
+  d.n_pages = uint32_t(c->n_pages);
   d.table = c->table;
   d.table_stride = c->table_stride;
   d.page_shift = __builtin_ctz(unsigned(c->page_size));
@@ -165,14 +170,16 @@ __device__ inline int32_t checked_len(const int32_t *kv_len, int32_t s, int32_t 
   return n;
 }
 
-// Page id of a table entry: one outside the cache raises *code and becomes page 0.
-__device__ inline int64_t checked_page(const DevCache &c, const int32_t *entry, int32_t &code) {
-  const int32_t p = __ldg(entry);
-  if (uint32_t(p) >= uint64_t(c.n_pages)) {
+// Offset of a token's row: its page (an id outside the cache raises *code and becomes page
+// 0), its slot, and the head's offset inside a page.
+__device__ inline uint64_t row_at(const DevCache &c, uint32_t page, int32_t j, uint32_t head,
+                                  int32_t &code) {
+  if (page >= c.n_pages) {
     code = FS_E_RANGE;
-    return 0;
+    page = 0;
   }
-  return p;
+  return uint64_t(page) * c.page_stride +
+         (head + uint32_t(j & ((1 << c.page_shift) - 1)) * c.token_stride);
 }
 
 // ---- launchers

@@ -35,7 +35,8 @@ fs_status check_cache(const fs_step *s, const fs_kv_cache *c, int32_t most_dim) 
     return FS_E_ARG;
   if (c->n_pages < 1 || c->n_pages > INT32_MAX) return FS_E_ARG;
   if (c->page_stride < 0 || c->head_stride < 0 || c->token_stride < 0 || !mult8(c->page_stride) ||
-      !mult8(c->head_stride) || !mult8(c->token_stride))
+      !mult8(c->head_stride) || !mult8(c->token_stride) || c->page_stride > INT32_MAX ||
+      c->head_stride > INT32_MAX || c->token_stride > INT32_MAX)
     return FS_E_ARG;
   // the offset inside a page, in elements, is computed in 32 bits
   if ((c->page_size - 1) * c->token_stride + (c->n_kv_heads - 1) * c->head_stride + c->head_dim >

@@ -58,9 +58,9 @@ __global__ void __launch_bounds__(256) k_rope_append(RopeArgs a) {
       const int32_t p = kv - (__ldg(a.q_off + s + 1) - t);
       int64_t at = -1;
       if (p >= 0) {
-        const int32_t id = __ldg(a.c.table + s * a.c.table_stride + (p >> a.c.page_shift));
-        if (uint32_t(id) < uint64_t(a.c.n_pages))
-          at = id * a.c.page_stride + (p & ((1 << a.c.page_shift) - 1)) * a.c.token_stride;
+        const uint32_t id = __ldg(a.c.table + s * a.c.table_stride + (p >> a.c.page_shift));
+        if (id < a.c.n_pages)
+          at = row_at(a.c, id, p, 0, code);
         else
           code = FS_E_RANGE;
       }
@@ -107,14 +107,14 @@ __global__ void __launch_bounds__(256) k_rope_append(RopeArgs a) {
         } else {
           if (at < 0) continue;
           src = a.k + 2 * (t * a.k_stride + (h - a.n_heads) * D);
-          dst = a.kw + 2 * (at + (h - a.n_heads) * a.c.head_stride);
+          dst = a.kw + 2 * (at + int64_t(h - a.n_heads) * a.c.head_stride);
         }
       } else {
         if (at < 0) continue;
         const int r = it - rot_items, h = r / vper;
         j = r - h * vper;
         src = a.v + 2 * (t * a.v_stride + h * D);
-        dst = a.vw + 2 * (at + h * a.c.head_stride);
+        dst = a.vw + 2 * (at + int64_t(h) * a.c.head_stride);
         copy = true;
       }
       if constexpr (VEC) {
