@@ -97,14 +97,17 @@ __device__ inline float max_of_halves(float x) {
 }
 
 // ---- few rows: NT tiles of 16 rows
-template <bool BF, int D, int NT, int WAVES>
-__global__ void __launch_bounds__(WAVES * 64) k_attn_few(AttnArgs a) {
-  constexpr int STEP = WAVES * 32;  // keys of the work-group's waves side by side
-  constexpr int KS = D / 32;  // matrix steps of a score, and 16-byte chunks of a lane's row
+template <bool BF, int D, int NT>
+__global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
+  constexpr int KS = D / 32;  // matrix steps of a score
   constexpr int DB = D / 16;  // 16-column blocks of an output row
-  __shared__ __align__(16) short vt[WAVES][32 * D];
-  __shared__ float wm[WAVES][NT * 16], wl[WAVES][NT * 16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int CH = D / 8;   // 16-byte chunks of a key row
+  constexpr int RW = 64 / CH, LD = 32 / RW;  // rows of a wave's load, loads of 32 keys' K (or V)
+  constexpr int kIds = 512;   // page ids kept in LDS
+  __shared__ __align__(16) short kv_lds[4][2][32 * D];  // a wave's K and V
+  __shared__ float wm[4][NT * 16], wl[4][NT * 16];
+  __shared__ uint32_t ids[kIds];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, g4 = lane >> 4;
   // Work-groups go to the 8 dies in turn: heads fastest, and each split shifts the
   // requests by one, so a long request's splits do not gather on one die.
@@ -122,8 +125,6 @@ __global__ void __launch_bounds__(WAVES * 64) k_attn_few(AttnArgs a) {
   const int32_t hi = min(kr.hi, lo + a.few_split);
   const int32_t *table = a.c.table + s * a.c.table_stride;
   const uint32_t head = hk * a.c.head_stride;
-  const short *kp = reinterpret_cast<const short *>(a.c.k) + g4 * 8;
-  const short *vp = reinterpret_cast<const short *>(a.c.v) + g4 * 8;
 
   // queries: row r16 of each tile, this lane's 8 elements of each step
   s16x8 qf[NT][KS];
@@ -144,98 +145,105 @@ __global__ void __launch_bounds__(WAVES * 64) k_attn_few(AttnArgs a) {
 #pragma unroll
   for (int t = 0; t < NT; ++t) m[t] = -INFINITY, l[t] = 0.f;
 
-  s16x8 kf[2][KS], vf[2][KS];
-  uint64_t at[2];
-  auto key_at = [&](int32_t j) {
-    return row_at(a.c, __ldg(table + (j >> a.c.page_shift)), j, head, code);
-  };
-  const int32_t first = lo + wave * 32;
-  short *tile = vt[wave];
-  if (first < hi) {
+  // This lane's row and 16-byte chunk of each load.  (Straight into registers in the matrix
+  // cores' layout, 16 lanes would touch 16 rows: a quarter of the cache's rate.)
+  uint32_t lcol[LD];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      at[b] = key_at(min(first + b * 16 + r16, hi - 1));
-#pragma unroll
-      for (int k = 0; k < KS; ++k) kf[b][k] = *reinterpret_cast<const s16x8 *>(kp + at[b] + k * 32);
-    }
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int k = 0; k < KS; ++k) vf[b][k] = *reinterpret_cast<const s16x8 *>(vp + at[b] + k * 32);
-    // the next tile's places, one tile ahead of its rows
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-      at[b] = key_at(min(first + STEP + b * 16 + r16, hi - 1));
+  for (int i = 0; i < LD; ++i) {
+    const int r = i * RW + lane / CH;
+    lcol[i] = head + (tile_at<D>(r, lane % CH) - r * D);
   }
-  for (int32_t j0 = first; j0 < hi; j0 += STEP) {
-    f32x4 sc[NT][2] = {};
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int k = 0; k < KS; ++k) sc[t][b] = mfma_16x16x32<BF>(kf[b][k], qf[t][k], sc[t][b]);
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int k = 0; k < KS; ++k)
-        *reinterpret_cast<s16x8 *>(tile + tile_at<D>(b * 16 + r16, k * 4 + g4)) = vf[b][k];
-    if (j0 + STEP < hi) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int k = 0; k < KS; ++k)
-          kf[b][k] = *reinterpret_cast<const s16x8 *>(kp + at[b] + k * 32);
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int k = 0; k < KS; ++k)
-          vf[b][k] = *reinterpret_cast<const s16x8 *>(vp + at[b] + k * 32);
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-        at[b] = key_at(min(j0 + 2 * STEP + b * 16 + r16, hi - 1));
+  const uint32_t to = lds_address(kv_lds[wave][0]);
+
+  // the page ids of up to kIds pages at a time
+  for (int32_t from = lo; from < hi;) {
+    const int32_t p0 = from >> a.c.page_shift;
+    const int32_t end = int32_t(min(int64_t(hi), int64_t(p0 + kIds) << a.c.page_shift));
+    __syncthreads();
+    for (int i = tid; i < ((end - 1) >> a.c.page_shift) - p0 + 1; i += 256) {
+      const uint32_t page = __ldg(table + p0 + i);
+      if (page >= a.c.n_pages) code = FS_E_RANGE;
+      ids[i] = page < a.c.n_pages ? page : 0;
     }
-    s16x8 pf[NT];
+    __syncthreads();
+    // the waves take 32 keys in turn
+    const int32_t first = from + wave * 32;
+    const int32_t tiles = first < end ? (end - first + 127) / 128 : 0;
+    auto issue = [&](int32_t t) {
+      const int32_t j0 = first + t * 128;
+      uint64_t at[LD];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      float p[8], top = -INFINITY;
+      for (int i = 0; i < LD; ++i) {
+        const int32_t j = min(j0 + i * RW + lane / CH, end - 1);
+        at[i] = 2 * row_at(a.c, ids[(j >> a.c.page_shift) - p0], j, lcol[i], code);
+      }
+#pragma unroll
+      for (int i = 0; i < LD; ++i) load_to_lds(a.c.k + at[i], to + i * 1024);
+#pragma unroll
+      for (int i = 0; i < LD; ++i) load_to_lds(a.c.v + at[i], to + 32 * D * 2 + i * 1024);
+    };
+    if (tiles > 0) issue(0);
+    for (int32_t t = 0; t < tiles; ++t) {
+      const int32_t j0 = first + t * 128;
+      wait_own<0>();
+      const short *kb = kv_lds[wave][0], *vb = kv_lds[wave][1];
+      f32x4 sc[NT][2] = {};
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int32_t j = j0 + b * 16 + g4 * 4 + i;
-          const bool see = j <= pos[t] && j < hi && (a.window == 0 || j > pos[t] - a.window);
-          p[b * 4 + i] = see ? sc[t][b][i] : -INFINITY;
-          top = fmaxf(top, p[b * 4 + i]);
+        for (int k = 0; k < KS; ++k) {
+          const s16x8 kf =
+              *reinterpret_cast<const s16x8 *>(kb + tile_at<D>(b * 16 + r16, k * 4 + g4));
+#pragma unroll
+          for (int r = 0; r < NT; ++r) sc[r][b] = mfma_16x16x32<BF>(kf, qf[r][k], sc[r][b]);
         }
-      top = max_of_halves(fmaxf(top, __shfl_xor(top, 16, 64)));
-      const float m2 = fmaxf(m[t], top);
-      // (-inf less -inf is no number and asks for nothing)
-      if (__any((m2 - m[t]) * a.c2 > kSlack)) {
-        const float f = m[t] == -INFINITY ? 0.f : exp2_fast((m[t] - m2) * a.c2);
-        l[t] *= f;
+      s16x8 pf[NT];
 #pragma unroll
-        for (int d = 0; d < DB; ++d) o[t][d] *= f;
-        m[t] = m2;
+      for (int r = 0; r < NT; ++r) {
+        float p[8], top = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int32_t j = j0 + b * 16 + g4 * 4 + i;
+            const bool see = j <= pos[r] && j < end && (a.window == 0 || j > pos[r] - a.window);
+            p[b * 4 + i] = see ? sc[r][b][i] : -INFINITY;
+            top = fmaxf(top, p[b * 4 + i]);
+          }
+        top = max_of_halves(fmaxf(top, __shfl_xor(top, 16, 64)));
+        const float m2 = fmaxf(m[r], top);
+        // (-inf less -inf is no number and asks for nothing)
+        if (__any((m2 - m[r]) * a.c2 > kSlack)) {
+          const float f = m[r] == -INFINITY ? 0.f : exp2_fast((m[r] - m2) * a.c2);
+          l[r] *= f;
+#pragma unroll
+          for (int d = 0; d < DB; ++d) o[r][d] *= f;
+          m[r] = m2;
+        }
+        const float mc = m[r] == -INFINITY ? 0.f : m[r] * a.c2;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          p[i] = exp2_fast(fmaf(p[i], a.c2, -mc));
+          l[r] += p[i];
+        }
+        pf[r] = pack8<BF>(p);
       }
-      const float mc = m[t] == -INFINITY ? 0.f : m[t] * a.c2;
+      // keys 4 g4 .. + 3 and 16 + 4 g4 .. + 3 of the tile, 16 columns at a time
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        p[i] = exp2_fast(fmaf(p[i], a.c2, -mc));
-        l[t] += p[i];
+      for (int d = 0; d < DB; ++d) {
+        const int row = 4 * g4 + (r16 >> 2), col = d * 16 + (r16 & 3) * 4;
+        const s16x4 v0 = read_tr(vb + tile_at<D>(row, col >> 3) + (col & 7));
+        const s16x4 v1 = read_tr(vb + tile_at<D>(row + 16, col >> 3) + (col & 7));
+        const s16x8 vv = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+        for (int r = 0; r < NT; ++r) o[r][d] = mfma_16x16x32<BF>(vv, pf[r], o[r][d]);
       }
-      pf[t] = pack8<BF>(p);
+      if (t + 1 < tiles) {
+        reads_done();
+        issue(t + 1);
+      }
     }
-    // keys 4 g4 .. + 3 and 16 + 4 g4 .. + 3 of the tile, 16 columns at a time
-#pragma unroll
-    for (int d = 0; d < DB; ++d) {
-      const int row = 4 * g4 + (r16 >> 2), col = d * 16 + (r16 & 3) * 4;
-      const s16x4 v0 = read_tr(tile + tile_at<D>(row, col >> 3) + (col & 7));
-      const s16x4 v1 = read_tr(tile + tile_at<D>(row + 16, col >> 3) + (col & 7));
-      const s16x8 vv = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) o[t][d] = mfma_16x16x32<BF>(vv, pf[t], o[t][d]);
-    }
+    from = end;
   }
   raise_err(a.err, code);
 
@@ -246,7 +254,7 @@ __global__ void __launch_bounds__(WAVES * 64) k_attn_few(AttnArgs a) {
     l[t] += __shfl_xor(l[t], 32, 64);
     if (g4 == 0) wm[wave][t * 16 + r16] = m[t], wl[wave][t * 16 + r16] = l[t];
   }
-  float *buf = reinterpret_cast<float *>(vt);  // [WAVES][16][D / 2]: half of the columns at a time
+  float *buf = reinterpret_cast<float *>(kv_lds);  // [4][16][D / 2]: half of the columns at a time
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     if (t * 16 >= R) break;
@@ -258,17 +266,17 @@ __global__ void __launch_bounds__(WAVES * 64) k_attn_few(AttnArgs a) {
         *reinterpret_cast<f32x4 *>(buf + (wave * 16 + r16) * (D / 2) +
                                    ((d * 16 + g4 * 4) ^ ((r16 & 3) * 4))) = o[t][half * (DB / 2) + d];
       __syncthreads();
-      for (int e = tid; e < 16 * D / 8; e += WAVES * 64) {
+      for (int e = tid; e < 16 * D / 8; e += 256) {
         const int r = e / (D / 8), col = (e - r * (D / 8)) * 4;
         if (t * 16 + r >= R) continue;
         const int tr = t * 16 + r;
         float top = wm[0][tr];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, wm[w][tr]);
+        for (int w = 1; w < 4; ++w) top = fmaxf(top, wm[w][tr]);
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
         float sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
+        for (int w = 0; w < 4; ++w) {
           const float f = wm[w][tr] == -INFINITY ? 0.f : exp2_fast((wm[w][tr] - top) * a.c2);
           sum += f * wl[w][tr];
           acc += f * *reinterpret_cast<const f32x4 *>(buf + (w * 16 + r) * (D / 2) +
@@ -633,25 +641,22 @@ void run(const AttnArgs &a, const Plan &p, hipStream_t stream) {
   if (p.few_seqs > 0) {
     const dim3 grid(uint32_t(a.n_seqs) * a.c.n_kv_heads * p.few_splits);
     if (p.few_rows <= 16)
-      if (grid.x <= 256)  // one work-group a compute unit at most: twice the waves in it
-        hipLaunchKernelGGL((k_attn_few<BF, D, 1, 8>), grid, dim3(512), 0, stream, a);
-      else
-        hipLaunchKernelGGL((k_attn_few<BF, D, 1, 4>), grid, block, 0, stream, a);
+      hipLaunchKernelGGL((k_attn_few<BF, D, 1>), grid, block, 0, stream, a);
     else if (p.few_rows <= 32)
-      hipLaunchKernelGGL((k_attn_few<BF, D, 2, 4>), grid, block, 0, stream, a);
+      hipLaunchKernelGGL((k_attn_few<BF, D, 2>), grid, block, 0, stream, a);
     else
-      hipLaunchKernelGGL((k_attn_few<BF, D, 4, 4>), grid, block, 0, stream, a);
+      hipLaunchKernelGGL((k_attn_few<BF, D, 4>), grid, block, 0, stream, a);
   }
   if (p.chunk_seqs > 0)
     hipLaunchKernelGGL((k_attn_chunk<BF, D>), dim3(p.chunk_tiles * a.c.n_kv_heads, p.chunk_splits),
                        block, 0, stream, a);
   if (p.few_splits > 1)
-    hipLaunchKernelGGL((k_attn_join<BF, D, true>), dim3(a.n_heads, a.n_seqs, p.few_tokens), block, 0,
-                       stream, a);
+    hipLaunchKernelGGL((k_attn_join<BF, D, true>), dim3(a.n_heads, a.n_seqs, p.few_tokens), dim3(256),
+                       0, stream, a);
   if (p.chunk_splits > 1)
     hipLaunchKernelGGL((k_attn_join<BF, D, false>),
-                       dim3(a.n_heads, (a.rows + 65534) / 65535, min(a.rows, 65535)), block, 0,
-                       stream, a);
+                       dim3(a.n_heads, (a.rows + 65534) / 65535, min(a.rows, 65535)), dim3(256),
+                       0, stream, a);
 }
 
 }  // namespace
