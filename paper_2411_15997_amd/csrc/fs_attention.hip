@@ -21,7 +21,6 @@ namespace fs {
 namespace {
 
 constexpr int kFewRows = 64;    // rows (tokens times group) that k_attn_few takes
-constexpr int kChunkRows = 128;  // rows of a work-group of k_attn_chunk
 constexpr int64_t kMostPartial = int64_t(1) << 28;  // bytes of partial results, about
 constexpr float kLn2 = 0.693147180559945309f;
 
@@ -38,6 +37,7 @@ struct AttnArgs {
   int32_t few_split;   // keys of a split (k_attn_few), splits
   int32_t few_splits;
   int32_t few_tokens;  // most tokens of a request that k_attn_few takes
+  int32_t chunk_rows;  // rows of a work-group of k_attn_chunk
   int32_t chunk_split, chunk_splits, chunk_tiles;
   float *few_o, *few_ml;      // [splits][n_seqs][few_tokens][heads][D], [..][2]
   float *chunk_o, *chunk_ml;  // [splits][rows][heads][D], [..][2]
@@ -303,36 +303,38 @@ __global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
   }
 }
 
-// Row tiles of k_attn_chunk: request s owns tile numbers from q_off[s] * G / 128 + s on.
+// Row tiles of k_attn_chunk: request s owns tile numbers from q_off[s] * G / chunk_rows + s
+// on, its last rows (which see the most keys) first.  r0 < 0: no rows.
 __device__ inline void chunk_tile(const AttnArgs &a, int32_t b, int32_t &s, int32_t &r0) {
   s = last_at_most(a.n_seqs, b, [&](int32_t i) {
-    return __ldg(a.q_off + i) * a.group / kChunkRows + i;
+    return __ldg(a.q_off + i) * a.group / a.chunk_rows + i;
   });
-  r0 = (b - __ldg(a.q_off + s) * a.group / kChunkRows - s) * kChunkRows;
+  const int32_t q0 = __ldg(a.q_off + s), R = (__ldg(a.q_off + s + 1) - q0) * a.group;
+  const int32_t tiles = (R + a.chunk_rows - 1) / a.chunk_rows;
+  r0 = (tiles - 1 - (b - q0 * a.group / a.chunk_rows - s)) * a.chunk_rows;
 }
 
-// ---- chunks: four waves of 32 rows, 64 keys at a time
-template <bool BF, int D>
-__global__ void __launch_bounds__(256, 2) k_attn_chunk(AttnArgs a) {
+// ---- chunks: WAVES waves of 32 rows, 64 keys at a time through two buffers
+template <bool BF, int D, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64, 2) k_attn_chunk(AttnArgs a) {
   constexpr int KS = D / 16;       // matrix steps of a score
   constexpr int DB = D / 32;       // 32-column blocks of an output row
   constexpr int CH = D / 8;        // 16-byte chunks of a key row
   constexpr int RW = 64 / CH;      // rows of a wave's load
-  constexpr int LD = 16 / RW;      // a wave's loads of K, and of V, for 64 keys
+  constexpr int LD = 64 / WAVES / RW;  // a wave's loads of K, and of V, for 64 keys
+  static_assert(LD >= 1, "a wave loads whole rows");
   __shared__ __align__(16) short kt[2][64 * D], vt[2][64 * D];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r32 = lane & 31, h2 = lane >> 5;
   const int hk = blockIdx.x % a.c.n_kv_heads;
-  // the last tiles of a request see the most keys: they go first
-  const int32_t b = a.chunk_tiles - 1 - int32_t(blockIdx.x / a.c.n_kv_heads);
   int32_t s, r0;
-  chunk_tile(a, b, s, r0);
+  chunk_tile(a, blockIdx.x / a.c.n_kv_heads, s, r0);
   const int32_t q0 = __ldg(a.q_off + s), n = __ldg(a.q_off + s + 1) - q0;
   const int G = a.group, R = n * G;
-  if (r0 >= R || R <= kFewRows) return;
+  if (r0 < 0 || R <= kFewRows) return;
   int32_t code = 0;
   const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
-  const KeyRange kr = key_range(a, n, kv, r0 / G, (min(r0 + kChunkRows, R) - 1) / G);
+  const KeyRange kr = key_range(a, n, kv, r0 / G, (min(r0 + WAVES * 32, R) - 1) / G);
   const bool single = kr.hi - kr.lo <= a.chunk_split;
   const int32_t lo = kr.lo + blockIdx.y * a.chunk_split;
   if (blockIdx.y > 0 && lo >= kr.hi) return;
@@ -359,13 +361,12 @@ __global__ void __launch_bounds__(256, 2) k_attn_chunk(AttnArgs a) {
   f32x16 o[DB] = {};
   float m = -INFINITY, l = 0.f;
 
-  // This lane's row and 16-byte chunk of each of the wave's loads: a wave loads the keys
-  // 16 * wave .. + 15 of K and V, RW rows at a time.
+  // This lane's row and 16-byte chunk of each of the wave's loads, RW rows at a time.
   int32_t lrow[LD];
   uint32_t lcol[LD], page[LD];
 #pragma unroll
   for (int i = 0; i < LD; ++i) {
-    lrow[i] = wave * 16 + i * RW + lane / CH;
+    lrow[i] = (wave * LD + i) * RW + lane / CH;
     lcol[i] = head + (tile_at<D>(lrow[i], lane % CH) - lrow[i] * D);
   }
   // page ids are loaded one tile ahead of the rows
@@ -374,7 +375,8 @@ __global__ void __launch_bounds__(256, 2) k_attn_chunk(AttnArgs a) {
     for (int i = 0; i < LD; ++i)
       page[i] = __ldg(table + (min(j0 + lrow[i], hi - 1) >> a.c.page_shift));
   };
-  const uint32_t k_to = lds_address(kt[0] + wave * 16 * D), v_to = lds_address(vt[0] + wave * 16 * D);
+  const uint32_t k_to = lds_address(kt[0] + wave * LD * RW * D),
+                 v_to = lds_address(vt[0] + wave * LD * RW * D);
   auto issue = [&](int32_t j0, int buf) {
 #pragma unroll
     for (int i = 0; i < LD; ++i) {
@@ -519,9 +521,9 @@ __global__ void __launch_bounds__(256) k_attn_join(AttnArgs a) {
   const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
   int32_t tok0 = 0, tok1 = n - 1;
   if (!FEW) {
-    const int32_t r0 = (tok * a.group + h % a.group) / kChunkRows * kChunkRows;
+    const int32_t r0 = (tok * a.group + h % a.group) / a.chunk_rows * a.chunk_rows;
     tok0 = r0 / a.group;
-    tok1 = (min(r0 + kChunkRows, n * a.group) - 1) / a.group;
+    tok1 = (min(r0 + a.chunk_rows, n * a.group) - 1) / a.group;
   }
   const KeyRange kr = key_range(a, n, kv, tok0, tok1);
   const int32_t len = kr.hi - kr.lo;
@@ -563,7 +565,7 @@ __global__ void __launch_bounds__(256) k_attn_join(AttnArgs a) {
 // How a call's work is split: from the step's shape and the bound on lengths alone.
 struct Plan {
   int32_t few_seqs, few_rows, few_tokens, few_split, few_splits;
-  int32_t chunk_seqs, chunk_tiles, chunk_split, chunk_splits;
+  int32_t chunk_seqs, chunk_rows, chunk_tiles, chunk_split, chunk_splits;
 };
 
 Plan plan(const fs_step *s, const fs_kv_cache *c, int32_t n_heads, int32_t window) {
@@ -604,9 +606,15 @@ Plan plan(const fs_step *s, const fs_kv_cache *c, int32_t n_heads, int32_t windo
     split_of(int64_t(p.few_seqs) * c->n_kv_heads, keys(p.few_tokens), 1024, 512, 1024,
              int64_t(s->n_seqs) * p.few_tokens, p.few_split, p.few_splits);
   if (p.chunk_seqs > 0) {
-    p.chunk_tiles =
-        int32_t(int64_t(s->q_off_h[s->n_seqs]) * G / kChunkRows + s->n_seqs);
-    const int32_t toks = kChunkRows / G + 2;
+    auto tiles = [&](int32_t rows) {
+      return int32_t(int64_t(s->q_off_h[s->n_seqs]) * G / rows + s->n_seqs);
+    };
+    // 256 rows share each key tile where that still gives every compute unit a work-group
+    // (head_dim 128: 4,096 rows over 32,768 keys 2.03 ms with 128 rows, 1.89 ms with 256; the
+    // lighter tiles of head_dim 64 gain more from four work-groups a unit, 145 against 109 us)
+    p.chunk_rows = c->head_dim == 128 && int64_t(tiles(256)) * c->n_kv_heads >= 256 ? 256 : 128;
+    p.chunk_tiles = tiles(p.chunk_rows);
+    const int32_t toks = p.chunk_rows / G + 2;
     split_of(int64_t(p.chunk_tiles) * c->n_kv_heads, keys(most < toks ? most : toks), 512, 1024,
              1 << 30, s->q_off_h[s->n_seqs], p.chunk_split, p.chunk_splits);
   }
@@ -647,9 +655,16 @@ void run(const AttnArgs &a, const Plan &p, hipStream_t stream) {
     else
       hipLaunchKernelGGL((k_attn_few<BF, D, 4>), grid, block, 0, stream, a);
   }
-  if (p.chunk_seqs > 0)
-    hipLaunchKernelGGL((k_attn_chunk<BF, D>), dim3(p.chunk_tiles * a.c.n_kv_heads, p.chunk_splits),
-                       block, 0, stream, a);
+  if (p.chunk_seqs > 0) {
+    if constexpr (D == 128)
+      if (p.chunk_rows == 256)
+        hipLaunchKernelGGL((k_attn_chunk<BF, D, 8>),
+                           dim3(p.chunk_tiles * a.c.n_kv_heads, p.chunk_splits), dim3(512), 0,
+                           stream, a);
+    if (p.chunk_rows == 128)
+      hipLaunchKernelGGL((k_attn_chunk<BF, D, 4>),
+                         dim3(p.chunk_tiles * a.c.n_kv_heads, p.chunk_splits), block, 0, stream, a);
+  }
   if (p.few_splits > 1)
     hipLaunchKernelGGL((k_attn_join<BF, D, true>), dim3(a.n_heads, a.n_seqs, p.few_tokens), dim3(256),
                        0, stream, a);
@@ -694,6 +709,7 @@ hipError_t launch_attention(const fs_step *s, const fs_kv_cache *c, int32_t n_he
   a.few_split = p.few_split;
   a.few_splits = p.few_splits;
   a.few_tokens = p.few_tokens;
+  a.chunk_rows = p.chunk_rows;
   a.chunk_split = p.chunk_split;
   a.chunk_splits = p.chunk_splits;
   a.chunk_tiles = p.chunk_tiles;
