@@ -129,7 +129,7 @@ struct Weigh {
   __device__ static uint32_t place(double y) {
     return uint32_t(__double_as_longlong(y + kMagic));
   }
-  __device__ static int bin_of(uint32_t place) { return int(place >> 3) - 11 * 32; }
+  __device__ static int bin_of(uint32_t place) { return int(place >> 3); }
   // N weights side by side: the table is read for all of them at once
   template <int N>
   __device__ void many(const double *y, uint64_t *w) const {
@@ -248,14 +248,13 @@ __device__ void sort_down(uint64_t *v, int n2) {
 }
 
 constexpr int kList = 4096;       // candidates that are sorted in LDS
-constexpr int kBins = 41 * 32;    // of y: 32 to an octave of weight
+constexpr int kBase = 11 * 32;    // the first bin
+constexpr int kBins = kBase + 51 * 32;  // of y: 32 to an octave of weight (none is left from 41 on)
 constexpr int kSegs = (1 << 20) / 4 / 64 + 2;  // sums of 64 groups of tokens
 
 struct Shared {
-  union {
-    uint64_t list[kList];
-    uint64_t seg[kSegs];
-  };
+  uint64_t list[kList];
+  uint64_t seg[kSegs];
   uint64_t hist[kBins];
   uint64_t red[kWaves];
   uint64_t val[2];
@@ -473,7 +472,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
       __syncthreads();
       auto one = [&](int32_t, float x) {
         const int bin = Weigh::bin_of(Weigh::place(weigh.y_of(x)));
-        if (bin < kBins) atomicAdd(reinterpret_cast<unsigned int *>(&sh.hist[bin]), 1u);
+        atomicAdd(reinterpret_cast<unsigned int *>(&sh.hist[bin]), 1u);
       };
       r.template each<2>(
           [&](int32_t id0, const s16x8 &v) {
@@ -568,14 +567,18 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
     return;
   }
 
-  if (tp < 1.f) {
+  // top-p: the bin of y in which the cut lies, and what lies above it
+  const bool nucleus = tp < 1.f;
+  uint64_t limit = 0, above = 0;
+  int bin = 0;
+  float from = INFINITY, to = -INFINITY;  // the bin's logits, a little widened
+  if (nucleus) {
     // weights by bin of y, 32 bins to an octave
     for (int i = tid; i < kBins; i += kThreads) sh.hist[i] = 0;
     __syncthreads();
     auto add = [&](double y, uint64_t w) {
-      const int bin = Weigh::bin_of(Weigh::place(y));
-      if (bin < kBins)
-        atomicAdd(reinterpret_cast<unsigned long long *>(&sh.hist[bin]), (unsigned long long)w);
+      atomicAdd(reinterpret_cast<unsigned long long *>(&sh.hist[Weigh::bin_of(Weigh::place(y))]),
+                (unsigned long long)w);
     };
     r.template each<2>(
         [&](int32_t, const s16x8 &v) {
@@ -603,7 +606,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
     uint64_t W;
     uint64_t before = block_scan(sum, sh.red, &W);
     const double lim = ceil(__dmul_rn(double(tp), double(W)));
-    const uint64_t limit = lim < 1.0 ? 1 : uint64_t(lim);
+    limit = lim < 1.0 ? 1 : uint64_t(lim);
 #pragma unroll
     for (int e = 0; e < kB; ++e) {
       if (before < limit && before + h[e] >= limit) {
@@ -613,75 +616,58 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
       before += h[e];
     }
     __syncthreads();
-    const uint64_t above = sh.val[0];
-    const int bin = int(sh.val[1]);
-    // the bin's logits, a little widened, so that few need the exact test
+    above = sh.val[0];
+    bin = int(sh.val[1]);
     const float slack = 1e-6f * (fabsf(top) + float(42.0 * 256.0 / weigh.per));
-    const float from = float(double(top) - ((bin + 1) * 8 + 1) / weigh.per) - slack;
-    const float to = float(double(top) - (bin * 8 - 1) / weigh.per) + slack;
-    const bool narrow = isfinite(from) && isfinite(to);
-    if (!collect<DT>(r, sh, [&](float x) {
-          if (narrow && !(x >= from && x <= to)) return false;
-          return Weigh::bin_of(Weigh::place(weigh.y_of(x))) == bin;
-        }))
-      return sample_slow<DT>(a, base, row, weigh, tp, least, k_in, u, sh);
-    const int n = sort_list(sh);
-    const int per = (n + kThreads - 1) / kThreads, i0 = min(tid * per, n), i1 = min(i0 + per, n);
-    uint64_t w[kPer];
-    sum = 0;
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-      w[e] = i0 + e < i1 ? weigh(key_in(sh.list[i0 + e])) : 0;
-      sum += w[e];
-    }
-    before = above + block_scan(sum, sh.red);
-    // the last token whose predecessors stay below the limit
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-      if (w[e] && before < limit && before + w[e] >= limit) sh.val[0] = sh.list[i0 + e];
-      before += w[e];
-    }
-    __syncthreads();
-    cut = sh.val[0];
+    from = float(double(top) - ((bin - kBase + 1) * 8 + 1) / weigh.per) - slack;
+    to = float(double(top) - ((bin - kBase) * 8 - 1) / weigh.per) + slack;
+    if (!isfinite(from) || !isfinite(to)) from = -INFINITY, to = INFINITY;
+    if (tid == 0) sh.n = 0;
     __syncthreads();
   }
 
   // The kept weights in the order of ids: a sum for each 64 groups (the tokens before the
   // first vector, each vector, the tokens after the last), then the one that holds the
-  // goal, token by token.  Where few are kept a lane weighs its own one after another, so
-  // a round costs as many weights as its fullest lane keeps, not a whole vector.
-  const float cut_x = value_of(key_in(cut));
-  const int32_t cut_id = id_in(cut);
+  // goal, token by token.  Where not all are kept a lane weighs its own one after another,
+  // so a round costs as many weights as its fullest lane keeps, not a whole vector.
+  // Under top-p the logits above the cut's bin are summed so and the bin's own are listed
+  // in the same pass; once sorted, those that stay are added to their groups' sums.
+  float cut_x = nucleus ? to : value_of(key_in(cut));
+  int32_t cut_id = nucleus ? -1 : id_in(cut);
   // below `low` a weight is surely under `least` (and under 1)
   const double reach = 256.0 * (40.0 - log2(double(least)) + 0.01);
   const float low = float(double(top) - reach / weigh.per) -
                     1e-6f * (fabsf(top) + float(reach / weigh.per));
-  const float bound = isfinite(low) ? fmaxf(cut_x, low) : cut_x;
+  float bound = isfinite(low) ? fmaxf(cut_x, low) : cut_x;
+  const bool whole = !nucleus && least == 1;  // every token with a weight is kept
   auto group = [&](int32_t g, const s16x8 &raw, auto take) {
     if (g >= 1 && g <= r.vecs) {
       const int32_t i0 = r.head + (g - 1) * kVec;
-      uint32_t mask = 0;
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const float x = Row<DT>::at(raw, e);
-        mask |= (x > bound || (x == bound && (x > cut_x || i0 + e <= cut_id))) ? 1u << e : 0;
-      }
-      if (__any(__popc(mask) > kVec / 2)) {
+      if (whole) {
         double y[kVec];
         uint64_t w[kVec];
 #pragma unroll
         for (int e = 0; e < kVec; ++e) y[e] = weigh.y_of(Row<DT>::at(raw, e));
         weigh.template many<kVec>(y, w);
 #pragma unroll
-        for (int e = 0; e < kVec; ++e)
-          take(i0 + e, w[e] >= least && (mask >> e & 1) ? w[e] : 0);
-      } else {
-        while (mask) {
-          const int e = __builtin_ctz(mask);
-          mask &= mask - 1;
-          const uint64_t w = weigh(Row<DT>::pick(raw, e));
-          take(i0 + e, w >= least ? w : 0);
-        }
+        for (int e = 0; e < kVec; ++e) take(i0 + e, w[e]);
+        return;
+      }
+      // equal to the bound: kept up to the cut's own id
+      const int32_t ties = bound > cut_x ? kVec : max(0, min(kVec, cut_id - i0 + 1));
+      uint32_t above = 0, equal = 0;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const float x = Row<DT>::at(raw, e);
+        above |= x > bound ? 1u << e : 0;
+        equal |= x == bound ? 1u << e : 0;
+      }
+      uint32_t mask = above | (equal & ((1u << ties) - 1));
+      while (mask) {
+        const int e = __builtin_ctz(mask);
+        mask &= mask - 1;
+        const uint64_t w = weigh(Row<DT>::pick(raw, e));
+        take(i0 + e, w >= least ? w : 0);
       }
     } else if (g == 0 || g == r.vecs + 1) {
       const int32_t i0 = g == 0 ? 0 : r.tail(), i1 = g == 0 ? r.head : V;
@@ -696,6 +682,44 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
   const int32_t segs = (r.vecs + 2 + 63) / 64;
   uint64_t total = 0;
   uint32_t count = 0;
+  // A logit near the cut's bin: the weight of one above it, a place in the list for its own.
+  auto doubtful = [&](int32_t id, float x) -> uint64_t {
+    const double y = weigh.y_of(x);
+    const int at_bin = Weigh::bin_of(Weigh::place(y));
+    if (at_bin < bin) {
+      const uint64_t w = weigh.of_y(y);
+      count += w >= least;
+      return w >= least ? w : 0;
+    }
+    if (at_bin == bin) {
+      const int at = atomicAdd(&sh.n, 1);
+      if (at < kList) sh.list[at] = pair_of(key_of(x), id);
+    }
+    return 0;
+  };
+  auto near_cut = [&](int32_t g, const s16x8 &raw) -> uint64_t {
+    uint64_t sum = 0;
+    if (g >= 1 && g <= r.vecs) {
+      uint32_t mask = 0;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const float x = Row<DT>::at(raw, e);
+        mask |= x >= from && x <= to ? 1u << e : 0;
+      }
+      while (mask) {
+        const int e = __builtin_ctz(mask);
+        mask &= mask - 1;
+        sum += doubtful(r.head + (g - 1) * kVec + e, Row<DT>::pick(raw, e));
+      }
+    } else if (g == 0 || g == r.vecs + 1) {
+      const int32_t i0 = g == 0 ? 0 : r.tail(), i1 = g == 0 ? r.head : V;
+      for (int32_t i = i0; i < i1; ++i) {
+        const float x = load_logit<DT>(base, i);
+        if (x >= from && x <= to) sum += doubtful(i, x);
+      }
+    }
+    return sum;
+  };
   {
     s16x8 q[kAhead] = {};
     const bool any = r.vecs > 0;
@@ -715,11 +739,45 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
             sum += w;
             count += w != 0;
           });
+          if (nucleus) sum += near_cut(s * 64 + lane, raw);
           total += sum;
           sum = wave_sum_last(sum);
           if (lane == 63) sh.seg[s] = sum;
         }
       }
+  }
+  if (nucleus) {
+    __syncthreads();
+    if (sh.n > kList) return sample_slow<DT>(a, base, row, weigh, tp, least, k_in, u, sh);
+    const int n = sort_list(sh);
+    const int per = (n + kThreads - 1) / kThreads, i0 = min(tid * per, n), i1 = min(i0 + per, n);
+    uint64_t w[kPer], sum = 0;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      w[e] = i0 + e < i1 ? weigh(key_in(sh.list[i0 + e])) : 0;
+      sum += w[e];
+    }
+    uint64_t before = above + block_scan(sum, sh.red);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      if (w[e] && before < limit) {
+        const uint64_t pair = sh.list[i0 + e];
+        if (before + w[e] >= limit) sh.val[0] = pair;  // the last one that stays
+        if (w[e] >= least) {
+          const int32_t id = id_in(pair);
+          const int32_t g = id < r.head ? 0 : (id - r.head) / kVec + 1;
+          atomicAdd(reinterpret_cast<unsigned long long *>(&sh.seg[g >> 6]),
+                    (unsigned long long)w[e]);
+          total += w[e];
+          ++count;
+        }
+      }
+      before += w[e];
+    }
+    __syncthreads();
+    cut_x = value_of(key_in(sh.val[0]));
+    cut_id = id_in(sh.val[0]);
+    bound = isfinite(low) ? fmaxf(cut_x, low) : cut_x;
   }
   const uint64_t S = block_sum(total, sh.red);
   const int32_t m = int32_t(block_sum(uint64_t(count), sh.red));

@@ -129,12 +129,20 @@ def _rows(t, name, shape):
     if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, wanted {shape}")
     st = t.stride()
-    inner = 1
-    for d in range(len(shape) - 1, 0, -1):
-        if st[d] != inner and shape[d] != 1:
-            raise ValueError(f"{name}: inner dimensions are not packed")
-        inner *= shape[d]
-    return t.data_ptr(), (st[0] if shape[0] > 1 else inner)
+    if len(shape) == 3:
+        packed = (st[2] == 1 or shape[2] == 1) and (st[1] == shape[2] or shape[1] == 1)
+        row = shape[1] * shape[2]
+    else:
+        packed = st[1] == 1 or shape[1] == 1
+        row = shape[1]
+    if not packed:
+        raise ValueError(f"{name}: inner dimensions are not packed")
+    return t.data_ptr(), (st[0] if shape[0] > 1 else row)
+
+
+def _new(shape, dtype, device):
+    """A packed tensor (two dimensions); empty_strided is torch's cheapest way to one."""
+    return _torch().empty_strided(shape, (shape[1], 1), dtype=dtype, device=device)
 
 
 def _workspace(ws, need, like):
@@ -203,7 +211,7 @@ class KVCache:
     def _table_stride(table):
         if table.shape[0] > 1:
             _want(table.stride(0) >= table.shape[1], "table: rows overlap")
-            return table.stride(0) if table.stride(0) == table.shape[1] else table.stride(0)
+            return table.stride(0)
         return table.shape[1]
 
 
@@ -261,7 +269,7 @@ def fs_adapter_linear(step: Step, adapters: Adapters, x, w, y=None, ws=None, err
     _want(x.dtype == adapters.dtype and w.dtype == adapters.dtype, "x, w and adapters: one dtype")
     _want(adapters.n_seqs >= step.n, "adapter: an id for every request")
     if y is None:
-        y = _torch().empty((step.rows, N), dtype=x.dtype, device=x.device)
+        y = _new((step.rows, N), x.dtype, x.device)
     _want(y.dtype == x.dtype, "y: the dtype of x")
     yp, ys = _rows(y, "y", (step.rows, N))
     err = cleared_err_word(x.device) if err is None else err
@@ -301,7 +309,7 @@ def fs_rope_append(step: Step, cache: KVCache, rope: Rope, q, k, v, q_out=None, 
         H = q.shape[1]
         qp, qs = _rows(q, "q", (T, H, D))
         if q_out is None:
-            q_out = _torch().empty((T, H, D), dtype=q.dtype, device=q.device)
+            q_out = _torch().empty_like(q)  # packed: a strided q is not copied in its strides
         _want(q_out.dtype == q.dtype, "q_out: the dtype of q")
         op, os_ = _rows(q_out, "q_out", (T, H, D))
     err = cleared_err_word(k.device) if err is None else err
@@ -320,11 +328,11 @@ def fs_paged_attention(step: Step, cache: KVCache, q, scale, window=0, out=None,
     qp, qs = _rows(q, "q", (step.rows, H, D))
     torch = _torch()
     if out is None:
-        out = torch.empty((T, H, D), dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q)
     _want(out.dtype == q.dtype, "out: the dtype of q")
     op, os_ = _rows(out, "out", (T, H, D))
     if lse is None and want_lse:
-        lse = torch.empty((T, H), dtype=torch.float32, device=q.device)
+        lse = _new((T, H), torch.float32, q.device)
     if lse is not None:
         _want(lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == T * H,
               "lse: packed float32 [rows][heads]")
@@ -343,14 +351,16 @@ def fs_sample(logits, u, sampling: Sampling, token=None, logprob=None, kept=None
     returns (token int32, logprob float32, kept int32), each [rows]."""
     torch = _torch()
     n, V = logits.shape
-    _want(n <= 1 or logits.stride(0) >= V, "logits: rows overlap")
-    _want(V == 1 or logits.stride(1) == 1, "logits: rows are not packed")
+    stride = logits.stride()
+    _want(n <= 1 or stride[0] >= V, "logits: rows overlap")
+    _want(V == 1 or stride[1] == 1, "logits: rows are not packed")
     _want(sampling.rows is None or sampling.rows >= n, "sampling: a setting for every row")
     up = _vector(u, torch.float32, n, "u")
     dev = logits.device
-    token = torch.empty(n, dtype=torch.int32, device=dev) if token is None else token
-    logprob = torch.empty(n, dtype=torch.float32, device=dev) if logprob is None else logprob
-    kept = torch.empty(n, dtype=torch.int32, device=dev) if kept is None else kept
+    like = u if u.shape[0] == n else u[:n]
+    token = torch.empty_like(like, dtype=torch.int32) if token is None else token
+    logprob = torch.empty_like(like) if logprob is None else logprob
+    kept = torch.empty_like(like, dtype=torch.int32) if kept is None else kept
     tp, lp, kp = (_vector(token, torch.int32, n, "token"),
                   _vector(logprob, torch.float32, n, "logprob"),
                   _vector(kept, torch.int32, n, "kept"))
@@ -358,7 +368,7 @@ def fs_sample(logits, u, sampling: Sampling, token=None, logprob=None, kept=None
     code = _dtype_code(logits)
     L = _lib()
     ws, wp, wn = _workspace(ws, L.fs_sample_workspace(code, n, V), logits)
-    _done(L.fs_sample(code, n, V, logits.data_ptr(), logits.stride(0) if n > 1 else V,
+    _done(L.fs_sample(code, n, V, logits.data_ptr(), stride[0] if n > 1 else V,
                       sampling.ref, up, tp, lp, kp, wp, wn, err.data_ptr(), _stream(logits)),
           "fs_sample", err, check)
     return token, logprob, kept
