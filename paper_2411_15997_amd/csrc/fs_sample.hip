@@ -250,12 +250,14 @@ __device__ void sort_down(uint64_t *v, int n2) {
 constexpr int kList = 4096;       // candidates that are sorted in LDS
 constexpr int kBase = 11 * 32;    // the first bin
 constexpr int kBins = kBase + 51 * 32;  // of y: 32 to an octave of weight (none is left from 41 on)
+constexpr int kQueue = 64 * 8 + 16;  // logits of a wave that wait to be weighed
 constexpr int kSegs = (1 << 20) / 4 / 64 + 2;  // sums of 64 groups of tokens
 
 struct Shared {
   uint64_t list[kList];
   uint64_t seg[kSegs];
   uint64_t hist[kBins];
+  uint64_t queue[kWaves][kQueue];
   uint64_t red[kWaves];
   uint64_t val[2];
   double table[256];
@@ -682,47 +684,45 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
   const int32_t segs = (r.vecs + 2 + 63) / 64;
   uint64_t total = 0;
   uint32_t count = 0;
-  // A logit near the cut's bin: the weight of one above it, a place in the list for its own.
-  auto doubtful = [&](int32_t id, float x) -> uint64_t {
-    const double y = weigh.y_of(x);
-    const int at_bin = Weigh::bin_of(Weigh::place(y));
-    if (at_bin < bin) {
-      const uint64_t w = weigh.of_y(y);
-      count += w >= least;
-      return w >= least ? w : 0;
+  // Not all are kept: a sum's logits that may be are gathered, and weighed 64 at a time with
+  // every lane at work.
+  const float gate = nucleus ? from : bound;
+  uint64_t *queue = sh.queue[wave];
+  int waiting = 0;  // the same for the wave
+  auto gather = [&](int32_t id, float x, bool have) {
+    const bool take = have && x >= gate;
+    const uint64_t takers = __ballot(take);
+    if (takers) {
+      if (take)
+        queue[waiting + __builtin_amdgcn_mbcnt_hi(uint32_t(takers >> 32),
+                                                  __builtin_amdgcn_mbcnt_lo(uint32_t(takers), 0))] =
+            pair_of(key_of(x), id);
+      waiting += __popcll(takers);
     }
-    if (at_bin == bin) {
-      const int at = atomicAdd(&sh.n, 1);
-      if (at < kList) sh.list[at] = pair_of(key_of(x), id);
-    }
-    return 0;
   };
-  auto near_cut = [&](int32_t g, const s16x8 &raw) -> uint64_t {
+  auto weigh_gathered = [&]() -> uint64_t {
     uint64_t sum = 0;
-    if (g >= 1 && g <= r.vecs) {
-      uint32_t mask = 0;
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const float x = Row<DT>::at(raw, e);
-        mask |= x >= from && x <= to ? 1u << e : 0;
-      }
-      while (mask) {
-        const int e = __builtin_ctz(mask);
-        mask &= mask - 1;
-        sum += doubtful(r.head + (g - 1) * kVec + e, Row<DT>::pick(raw, e));
-      }
-    } else if (g == 0 || g == r.vecs + 1) {
-      const int32_t i0 = g == 0 ? 0 : r.tail(), i1 = g == 0 ? r.head : V;
-      for (int32_t i = i0; i < i1; ++i) {
-        const float x = load_logit<DT>(base, i);
-        if (x >= from && x <= to) sum += doubtful(i, x);
+    for (int from_slot = 0; from_slot < waiting; from_slot += 64) {
+      if (from_slot + lane >= waiting) continue;
+      const uint64_t pair = queue[from_slot + lane];
+      const double y = weigh.y_of(value_of(key_in(pair)));
+      const int at_bin = Weigh::bin_of(Weigh::place(y));
+      if (nucleus && at_bin == bin) {
+        const int at = atomicAdd(&sh.n, 1);
+        if (at < kList) sh.list[at] = pair;
+      } else if (!nucleus || at_bin < bin) {
+        const uint64_t w = weigh.of_y(y);
+        sum += w >= least ? w : 0;
+        count += w >= least;
       }
     }
+    waiting = 0;
     return sum;
   };
   {
     s16x8 q[kAhead] = {};
     const bool any = r.vecs > 0;
+    const int32_t last_seg = (r.vecs + 1) >> 6;
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
       if (any) q[i] = r.load(max(0, (wave + i * kWaves) * 64 + lane - 1));
@@ -733,17 +733,31 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
         const int32_t s = s0 + i * kWaves;
         const s16x8 raw = q[i];
         if (any) q[i] = r.load((s + kAhead * kWaves) * 64 + lane - 1);
-        if (s < segs) {
-          uint64_t sum = 0;
-          group(s * 64 + lane, raw, [&](int32_t, uint64_t w) {
+        if (s >= segs) continue;
+        const int32_t g = s * 64 + lane;
+        uint64_t sum = 0;
+        if (whole) {
+          group(g, raw, [&](int32_t, uint64_t w) {
             sum += w;
             count += w != 0;
           });
-          if (nucleus) sum += near_cut(s * 64 + lane, raw);
-          total += sum;
-          sum = wave_sum_last(sum);
-          if (lane == 63) sh.seg[s] = sum;
+        } else {
+          const bool vec = g >= 1 && g <= r.vecs;
+#pragma unroll
+          for (int e = 0; e < kVec; ++e)
+            gather(r.head + (g - 1) * kVec + e, Row<DT>::at(raw, e), vec);
+          if (s == 0 || s == last_seg) {  // the tokens outside the vectors
+            const int32_t i0 = g == 0 ? 0 : r.tail(),
+                          n = g == 0 ? r.head : g == r.vecs + 1 ? V - r.tail() : 0;
+#pragma unroll 1
+            for (int e = 0; e < kVec; ++e)
+              gather(i0 + e, e < n ? load_logit<DT>(base, i0 + e) : 0.f, e < n);
+          }
+          sum = weigh_gathered();
         }
+        total += sum;
+        sum = wave_sum_last(sum);
+        if (lane == 63) sh.seg[s] = sum;
       }
   }
   if (nucleus) {
