@@ -303,9 +303,34 @@ __global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
   }
 }
 
-// Row tiles of k_attn_chunk: request s owns tile numbers from q_off[s] * G / chunk_rows + s
-// on, its last rows (which see the most keys) first.  r0 < 0: no rows.
+// Row tile number b of k_attn_chunk, a request's last rows (which see the most keys) first.
+// Up to 64 requests are taken in the order of the keys they see, the most first, so that
+// the work ends evenly; more in their own order, request s owning the tile numbers from
+// q_off[s] * G / chunk_rows + s on.  r0 < 0: no rows.
 __device__ inline void chunk_tile(const AttnArgs &a, int32_t b, int32_t &s, int32_t &r0) {
+  if (a.n_seqs <= 64) {
+    const int32_t i = min(int32_t(__lane_id()), a.n_seqs - 1);
+    const int32_t n = __ldg(a.q_off + i + 1) - __ldg(a.q_off + i), R = n * a.group;
+    const int32_t kv = __ldg(a.kv_len + i);
+    const int32_t keys = a.window ? min(kv, a.window + n) : kv;
+    const int32_t mine = R > kFewRows ? (R + a.chunk_rows - 1) / a.chunk_rows : 0;
+    int32_t before = 0;
+    for (int j = 0; j < a.n_seqs; ++j) {
+      const int32_t other = __builtin_amdgcn_readlane(keys, j);
+      if (other > keys || (other == keys && j < i)) before += __builtin_amdgcn_readlane(mine, j);
+    }
+    const uint64_t hit =
+        __ballot(int32_t(__lane_id()) < a.n_seqs && before <= b && b < before + mine);
+    if (!hit) {
+      s = 0;
+      r0 = -1;
+      return;
+    }
+    s = __builtin_ctzll(hit);
+    r0 = (__builtin_amdgcn_readlane(mine, s) - 1 - (b - __builtin_amdgcn_readlane(before, s))) *
+         a.chunk_rows;
+    return;
+  }
   s = last_at_most(a.n_seqs, b, [&](int32_t i) {
     return __ldg(a.q_off + i) * a.group / a.chunk_rows + i;
   });
@@ -378,6 +403,9 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attn_chunk(AttnArgs a) {
   const uint32_t k_to = lds_address(kt[0] + wave * LD * RW * D),
                  v_to = lds_address(vt[0] + wave * LD * RW * D);
   auto issue = [&](int32_t j0, int buf) {
+    // all ids are waited for here: a wait between the loads would be for those loads too
+#pragma unroll
+    for (int i = 0; i < LD; ++i) asm volatile("" : "+v"(page[i]));
 #pragma unroll
     for (int i = 0; i < LD; ++i) {
       const uint64_t at = 2 * row_at(a.c, page[i], min(j0 + lrow[i], hi - 1), lcol[i], code);
