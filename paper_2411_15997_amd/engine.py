@@ -270,8 +270,10 @@ def fs_adapter_linear(step: Step, adapters: Adapters, x, w, y=None, ws=None, err
     _want(adapters.n_seqs >= step.n, "adapter: an id for every request")
     if y is None:
         y = _new((step.rows, N), x.dtype, x.device)
-    _want(y.dtype == x.dtype, "y: the dtype of x")
-    yp, ys = _rows(y, "y", (step.rows, N))
+        yp, ys = y.data_ptr(), N
+    else:
+        _want(y.dtype == x.dtype, "y: the dtype of x")
+        yp, ys = _rows(y, "y", (step.rows, N))
     err = cleared_err_word(x.device) if err is None else err
     L = _lib()
     ws, wp, wn = _workspace(ws, L.fs_adapter_workspace(step.ref, adapters.ref), x)
@@ -309,9 +311,11 @@ def fs_rope_append(step: Step, cache: KVCache, rope: Rope, q, k, v, q_out=None, 
         H = q.shape[1]
         qp, qs = _rows(q, "q", (T, H, D))
         if q_out is None:
-            q_out = _torch().empty_like(q)  # packed: a strided q is not copied in its strides
-        _want(q_out.dtype == q.dtype, "q_out: the dtype of q")
-        op, os_ = _rows(q_out, "q_out", (T, H, D))
+            q_out = _torch().empty_like(q)  # packed, whatever q's row stride
+            op, os_ = q_out.data_ptr(), H * D
+        else:
+            _want(q_out.dtype == q.dtype, "q_out: the dtype of q")
+            op, os_ = _rows(q_out, "q_out", (T, H, D))
     err = cleared_err_word(k.device) if err is None else err
     _done(_lib().fs_rope_append(step.ref, cache.ref, rope.ref, H, qp, qs, kp, ks, vp, vs, op, os_,
                                 err.data_ptr(), _stream(k)), "fs_rope_append", err, check)
@@ -328,12 +332,14 @@ def fs_paged_attention(step: Step, cache: KVCache, q, scale, window=0, out=None,
     qp, qs = _rows(q, "q", (step.rows, H, D))
     torch = _torch()
     if out is None:
-        out = torch.empty_like(q)
-    _want(out.dtype == q.dtype, "out: the dtype of q")
-    op, os_ = _rows(out, "out", (T, H, D))
-    if lse is None and want_lse:
-        lse = _new((T, H), torch.float32, q.device)
-    if lse is not None:
+        out = torch.empty_like(q)  # packed, whatever q's row stride
+        op, os_ = out.data_ptr(), H * D
+    else:
+        _want(out.dtype == q.dtype, "out: the dtype of q")
+        op, os_ = _rows(out, "out", (T, H, D))
+    if lse is None:
+        lse = _new((T, H), torch.float32, q.device) if want_lse else None
+    else:
         _want(lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == T * H,
               "lse: packed float32 [rows][heads]")
     err = cleared_err_word(q.device) if err is None else err
@@ -358,12 +364,16 @@ def fs_sample(logits, u, sampling: Sampling, token=None, logprob=None, kept=None
     up = _vector(u, torch.float32, n, "u")
     dev = logits.device
     like = u if u.shape[0] == n else u[:n]
-    token = torch.empty_like(like, dtype=torch.int32) if token is None else token
-    logprob = torch.empty_like(like) if logprob is None else logprob
-    kept = torch.empty_like(like, dtype=torch.int32) if kept is None else kept
-    tp, lp, kp = (_vector(token, torch.int32, n, "token"),
-                  _vector(logprob, torch.float32, n, "logprob"),
-                  _vector(kept, torch.int32, n, "kept"))
+
+    def output(t, dtype, name):
+        if t is None:
+            t = torch.empty_like(like, dtype=dtype)
+            return t, t.data_ptr()
+        return t, _vector(t, dtype, n, name)
+
+    token, tp = output(token, torch.int32, "token")
+    logprob, lp = output(logprob, torch.float32, "logprob")
+    kept, kp = output(kept, torch.int32, "kept")
     err = cleared_err_word(dev) if err is None else err
     code = _dtype_code(logits)
     L = _lib()
