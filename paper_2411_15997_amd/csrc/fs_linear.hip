@@ -305,6 +305,12 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) k_linear_tile(LinA
     wc[i] = place_of<BK>(r, lane % CH) * 8;
     wo[i] = uint32_t((min(n0 + r, g.N - 1) - n0) * g.K + wc[i]) * 2;
   }
+  int32_t ad[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int row = m0 + wm + m * 32 + r32;
+    ad[m] = g.n_adapters > 0 && row < g.rows ? __ldg(g.row_ad + row) : -1;
+  }
   const short *x0 = g.x + int64_t(m0) * g.x_stride, *w0 = g.w + int64_t(n0) * g.K;
   const uint32_t xs_at = lds_address(&xs[0][wave * LX * RW * BK]),
                  ws_at = lds_address(&ws[0][wave * LW * RW * BK]);
@@ -379,27 +385,50 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) k_linear_tile(LinA
     multiply(step, step < full);
   }
   const s16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
-  if (g.n_adapters > 0) {
-    const int chunks = g.R / 8;
+  // The distinct adapters of a tile's rows, two at a time: the loads of both, and of two
+  // chunks of 8 columns (R/8 high ones, then R/8 low ones), go side by side.
+  const int chunks = g.R / 8;
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      const int row = m0 + wm + m * 32 + r32;
-      const int32_t ad = row < g.rows ? __ldg(g.row_ad + row) : -1;
-      const short *hp = g.h + int64_t(min(row, g.rows - 1)) * (2 * g.R);
-      uint64_t left = __ballot(ad >= 0);
-      while (left) {
-        const int32_t a = __builtin_amdgcn_readlane(ad, __builtin_ctzll(left));
-        const bool mine = ad == a;
-        left &= ~__ballot(mine);
-        const int32_t rank = rank_of(g, a);
-        for (int c = h2; c < 2 * chunks; c += 2) {
-          const s16x8 hv = mine ? *reinterpret_cast<const s16x8 *>(hp + c * 8) : zero;
-          const int j = (c < chunks ? c : c - chunks) * 8;
+  for (int m = 0; m < MT; ++m) {
+    const int row = m0 + wm + m * 32 + r32;
+    const short *hp = g.h + int64_t(min(row, g.rows - 1)) * (2 * g.R);
+    uint64_t left = __ballot(ad[m] >= 0);
+    while (left) {
+      int32_t who[2] = {-1, -1}, rank[2] = {0, 0};
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
-            acc[m][n] = mfma_32x32x16<BF>(
-                load_b(g, a, rank, min(n0 + wn + n * 32 + r32, g.N - 1), j), hv, acc[m][n]);
+      for (int i = 0; i < 2; ++i)
+        if (left) {
+          who[i] = __builtin_amdgcn_readlane(ad[m], __builtin_ctzll(left));
+          left &= ~__ballot(ad[m] == who[i]);
+          rank[i] = rank_of(g, who[i]);
         }
+      for (int c0 = h2; c0 < 2 * chunks; c0 += 4) {
+        s16x8 hv[2], bv[2][2][NT];
+        int j[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int c = c0 + u * 2;
+          const bool in = c < 2 * chunks;
+          hv[u] = in ? *reinterpret_cast<const s16x8 *>(hp + c * 8) : zero;
+          j[u] = in ? (c < chunks ? c : c - chunks) * 8 : g.R;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (who[i] >= 0)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int n = 0; n < NT; ++n)
+                bv[i][u][n] =
+                    load_b(g, who[i], rank[i], min(n0 + wn + n * 32 + r32, g.N - 1), j[u]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (who[i] >= 0)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int n = 0; n < NT; ++n)
+                acc[m][n] = mfma_32x32x16<BF>(bv[i][u][n], ad[m] == who[i] ? hv[u] : zero, acc[m][n]);
       }
     }
   }
