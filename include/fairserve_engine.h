@@ -33,14 +33,14 @@ typedef enum fs_dtype { FS_BF16 = 0, FS_F16 = 1, FS_F32 = 2 } fs_dtype;
 
 /* The requests of one engine step.  Request s brings the rows q_off[s] .. q_off[s+1]-1 of
  * the step's token matrices (a chunk of its prompt, one decoded token, or none).
- *   n_seqs   in [0, 65535]
+ *   n_seqs   in [0, 65535]; at most 2^24 rows in all
  *   q_off_h  host   [n_seqs+1] int32, q_off_h[0] = 0, non-decreasing
  *   q_off    device [n_seqs+1] int32, same values
  *   kv_len   device [n_seqs] int32: the request's tokens in the cache once this step's
  *            are appended; row i of its n rows has position kv_len - n + i.  A negative
  *            position marks a padding row: nothing is appended for it and its attention
  *            output is 0.  FS_E_RANGE unless 0 <= kv_len <= max_kv
- *   max_kv   host bound of every kv_len (sizes the work split, not the result) */
+ *   max_kv   host bound of every kv_len, at most 2^30 (sizes the work split, not the result) */
 typedef struct fs_step {
   int32_t n_seqs;
   const int32_t *q_off_h;
@@ -144,7 +144,8 @@ fs_status fs_rope_append(const fs_step *s, const fs_kv_cache *c, const fs_rope *
  * such token gets 0 (lse -inf).  lse [T][n_heads] fp32 (NULL: not wanted) is
  * ln sum_j exp(scale q . k_j), which joins results over parts of a context.
  *   q, out: [T][n_heads][head_dim] of the cache's dtype (token strides q_stride,
- *   out_stride); head_dim 64 or 128; n_heads a multiple of n_kv_heads, at most 64 times it.
+ *   out_stride); head_dim 64 or 128; n_heads a multiple of n_kv_heads, at most 64 times it;
+ *   rows times n_heads at most 2^30, n_seqs times n_kv_heads at most 2^21.
  * Scores, softmax statistics and sums are fp32; the probabilities enter the second
  * product in the cache's dtype.  Values at positions that a row's mask excludes have to
  * be finite if they lie below kv_len (they meet a probability of 0).
@@ -169,7 +170,8 @@ fs_status fs_paged_attention(const fs_step *s, const fs_kv_cache *c, int32_t n_h
  * order of ids) whose running sum of kept weights exceeds min(floor(u * S), S - 1).
  * Temperature 0: the first token of the order.  A row without a logit above -inf:
  * token -1, logprob -inf, kept 0.
- *   logits [rows][vocab] dtype (row stride `stride` elements), vocab in [1, 2^20]
+ *   logits [rows][vocab] dtype (row stride `stride` elements), vocab in [1, 2^20],
+ *   rows at most 2^21
  *   temperature, top_p, min_p float, top_k int32: device [rows], each may be NULL
  *   (1, 1, 0, all); temperature finite and >= 0, top_p and min_p in [0, 1], u in [0, 1):
  *   FS_E_RANGE otherwise (NaN included), and token -1

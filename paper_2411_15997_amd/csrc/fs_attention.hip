@@ -4,10 +4,15 @@
 // The G = n_heads / n_kv_heads query heads that share a key/value head are rows of one
 // matrix product: a request's n tokens are n * G rows (token-major) per key/value head.
 //   k_attn_few    requests of at most 64 rows (single tokens, small chunks): bound by the
-//                 cache's bytes.  Keys are spread over the four waves of a work-group and
-//                 over work-groups (splits); each wave streams its own 32 keys at a time.
-//   k_attn_chunk  larger chunks: bound by the matrix cores.  128 rows a work-group, 64
-//                 keys at a time through LDS.
+//                 cache's bytes (64 requests of up to 16,384 tokens: 121 us, 4.97 TB/s; one of
+//                 200,001: 80 us and 7 for the join, 5.1 TB/s).  The keys are spread over
+//                 work-groups (splits of up to 1,024) and over the four waves of each, which
+//                 load 32 keys at a time into LDS of their own and never wait for each other.
+//   k_attn_chunk  larger chunks: bound by the waits of a tile's chain (scores, maximum,
+//                 exponentials, products) at two waves a SIMD; the matrix cores are busy for
+//                 57 % of the cycles (4,096 rows over 32,768 keys, head_dim 128: 1.9 ms, 1.08
+//                 PFLOP/s; head_dim 64: 0.84).  128 or 256 rows a work-group share each tile
+//                 of 64 keys.
 //   k_attn_join   joins the splits' results with their maxima and sums, in split order.
 // Both products run with the keys as rows of the first operand (S^T = K Q^T,
 // O^T = V^T P^T): a lane then holds scores of one query row only, its probabilities are
@@ -34,17 +39,16 @@ struct AttnArgs {
   float *lse;
   float c2;            // |scale| * log2(e)
   uint32_t flip;       // sign of the scale, applied to the queries
-  int32_t few_split;   // keys of a split (k_attn_few), splits
-  int32_t few_splits;
+  int32_t few_split;   // keys of a split (k_attn_few)
   int32_t few_tokens;  // most tokens of a request that k_attn_few takes
   int32_t chunk_rows;  // rows of a work-group of k_attn_chunk
-  int32_t chunk_split, chunk_splits, chunk_tiles;
+  int32_t chunk_split;
   float *few_o, *few_ml;      // [splits][n_seqs][few_tokens][heads][D], [..][2]
   float *chunk_o, *chunk_ml;  // [splits][rows][heads][D], [..][2]
   int32_t *err;
 };
 
-// Keys that the rows [r0, r1) of a request with n tokens and kv cached ones see.
+// Keys that the tokens tok0 .. tok1 of a request with n new and kv cached ones see.
 struct KeyRange {
   int32_t lo, hi;
 };
@@ -92,7 +96,8 @@ constexpr float kSlack = 8.f;
 
 // The larger of the two halves' values, in both.
 __device__ inline float max_of_halves(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  const uint32_t b = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
@@ -263,8 +268,9 @@ __global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
       __syncthreads();
 #pragma unroll
       for (int d = 0; d < DB / 2; ++d)
-        *reinterpret_cast<f32x4 *>(buf + (wave * 16 + r16) * (D / 2) +
-                                   ((d * 16 + g4 * 4) ^ ((r16 & 3) * 4))) = o[t][half * (DB / 2) + d];
+        *reinterpret_cast<f32x4 *>(
+            buf + (wave * 16 + r16) * (D / 2) + ((d * 16 + g4 * 4) ^ ((r16 & 3) * 4))) =
+            o[t][half * (DB / 2) + d];
       __syncthreads();
       for (int e = tid; e < 16 * D / 8; e += 256) {
         const int r = e / (D / 8), col = (e - r * (D / 8)) * 4;
@@ -596,7 +602,11 @@ struct Plan {
   int32_t chunk_seqs, chunk_rows, chunk_tiles, chunk_split, chunk_splits;
 };
 
+// A window that no length can fill is none (and positions less a window stay in 32 bits).
+int32_t limited(int32_t window, const fs_step *s) { return window >= s->max_kv ? 0 : window; }
+
 Plan plan(const fs_step *s, const fs_kv_cache *c, int32_t n_heads, int32_t window) {
+  window = limited(window, s);
   Plan p = {};
   const int32_t G = n_heads / c->n_kv_heads;
   int32_t most = 0;
@@ -694,8 +704,8 @@ void run(const AttnArgs &a, const Plan &p, hipStream_t stream) {
                          dim3(p.chunk_tiles * a.c.n_kv_heads, p.chunk_splits), block, 0, stream, a);
   }
   if (p.few_splits > 1)
-    hipLaunchKernelGGL((k_attn_join<BF, D, true>), dim3(a.n_heads, a.n_seqs, p.few_tokens), dim3(256),
-                       0, stream, a);
+    hipLaunchKernelGGL((k_attn_join<BF, D, true>), dim3(a.n_heads, a.n_seqs, p.few_tokens),
+                       dim3(256), 0, stream, a);
   if (p.chunk_splits > 1)
     hipLaunchKernelGGL((k_attn_join<BF, D, false>),
                        dim3(a.n_heads, (a.rows + 65534) / 65535, min(a.rows, 65535)), dim3(256),
@@ -722,7 +732,7 @@ hipError_t launch_attention(const fs_step *s, const fs_kv_cache *c, int32_t n_he
   a.max_kv = s->max_kv;
   a.rows = s->q_off_h[s->n_seqs];
   a.n_heads = n_heads;
-  a.window = window;
+  a.window = limited(window, s);
   a.group = n_heads / c->n_kv_heads;
   a.c = dev_cache(c);
   a.q = static_cast<const short *>(q);
@@ -735,12 +745,9 @@ hipError_t launch_attention(const fs_step *s, const fs_kv_cache *c, int32_t n_he
   a.c2 = c2 > 1.2e-38f ? c2 : 1.2e-38f;
   a.flip = scale < 0.f;
   a.few_split = p.few_split;
-  a.few_splits = p.few_splits;
   a.few_tokens = p.few_tokens;
   a.chunk_rows = p.chunk_rows;
   a.chunk_split = p.chunk_split;
-  a.chunk_splits = p.chunk_splits;
-  a.chunk_tiles = p.chunk_tiles;
   char *at = static_cast<char *>(ws);
   a.few_o = reinterpret_cast<float *>(at);
   a.few_ml = reinterpret_cast<float *>(at + w.few_o);

@@ -16,10 +16,11 @@ fs_status status_of(hipError_t e) { return e == hipSuccess ? FS_OK : FS_E_HIP; }
 int32_t rows_of(const fs_step *s) { return s->q_off_h[s->n_seqs]; }
 
 fs_status check_step(const fs_step *s, bool lengths) {
-  if (!s || s->n_seqs < 0 || s->n_seqs > 65535 || !s->q_off_h || s->q_off_h[0] != 0) return FS_E_ARG;
+  if (!s || s->n_seqs < 0 || s->n_seqs > 65535 || !s->q_off_h || s->q_off_h[0] != 0)
+    return FS_E_ARG;
   for (int32_t i = 0; i < s->n_seqs; ++i)
     if (s->q_off_h[i + 1] < s->q_off_h[i]) return FS_E_ARG;
-  if (rows_of(s) > (1 << 30)) return FS_E_ARG;
+  if (rows_of(s) > (1 << 24)) return FS_E_ARG;
   if (rows_of(s) > 0 && !s->q_off) return FS_E_ARG;
   if (lengths && (s->max_kv < 0 || s->max_kv > (1 << 30) || (rows_of(s) > 0 && !s->kv_len)))
     return FS_E_ARG;
@@ -73,8 +74,10 @@ fs_status check_attention(const fs_step *s, const fs_kv_cache *c, int32_t n_head
   if (c->head_dim != 64 && c->head_dim != 128) return FS_E_ARG;
   if (n_heads < 1 || n_heads % c->n_kv_heads || n_heads / c->n_kv_heads > 64 || window < 0)
     return FS_E_ARG;
-  // rows times heads, and with them every count of work-groups, stay in 31 bits
-  if (int64_t(rows_of(s)) * n_heads > (int64_t(1) << 30)) return FS_E_ARG;
+  // keeps every count of work-items in 32 bits
+  if (int64_t(rows_of(s)) * n_heads > (int64_t(1) << 30) ||
+      int64_t(s->n_seqs) * c->n_kv_heads > (int64_t(1) << 21))
+    return FS_E_ARG;
   return FS_OK;
 }
 
@@ -202,7 +205,7 @@ size_t fs_sample_workspace(int32_t dtype, int32_t rows, int32_t vocab) {
 fs_status fs_sample(int32_t dtype, int32_t rows, int32_t vocab, const void *logits, int64_t stride,
                     const fs_sampling *p, const float *u, int32_t *token, float *logprob,
                     int32_t *kept, void *ws, size_t ws_bytes, int32_t *err, hipStream_t stream) {
-  if (dtype < FS_BF16 || dtype > FS_F32 || rows < 0 || rows > (1 << 24) || vocab < 1 ||
+  if (dtype < FS_BF16 || dtype > FS_F32 || rows < 0 || rows > (1 << 21) || vocab < 1 ||
       vocab > (1 << 20) || !p || !err || stride < vocab)
     return FS_E_ARG;
   if (rows == 0) return FS_OK;

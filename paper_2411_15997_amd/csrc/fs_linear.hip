@@ -366,7 +366,8 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) k_linear_tile(LinA
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) acc[m][n] = mfma_32x32x16<BF>(wf[u & 1][n], xf[u & 1][m], acc[m][n]);
+        for (int n = 0; n < NT; ++n)
+          acc[m][n] = mfma_32x32x16<BF>(wf[u & 1][n], xf[u & 1][m], acc[m][n]);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
@@ -428,7 +429,8 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) k_linear_tile(LinA
             for (int u = 0; u < 2; ++u)
 #pragma unroll
               for (int n = 0; n < NT; ++n)
-                acc[m][n] = mfma_32x32x16<BF>(bv[i][u][n], ad[m] == who[i] ? hv[u] : zero, acc[m][n]);
+                acc[m][n] =
+                    mfma_32x32x16<BF>(bv[i][u][n], ad[m] == who[i] ? hv[u] : zero, acc[m][n]);
       }
     }
   }

@@ -38,7 +38,8 @@ def test_step_and_cache_arguments():
                                       None, ws, wsb, err, None)
 
     for s in (step((1, 2)), step((0, 2, 1)), step(max_kv=-1), step(q_dev=None), step(kv=None),
-              step((0, 1 << 30), max_kv=16)):
+              step((0, 1 << 30), max_kv=16), step((0, (1 << 24) + 1)),
+              step([0] * 65537 + [1])):
         assert attn(s=s) == A
     for kw in (dict(dtype=2), dict(dtype=-1), dict(n_kv_heads=0), dict(head_dim=96),
                dict(head_dim=60), dict(head_dim=256), dict(page_size=0), dict(page_size=24),
@@ -113,6 +114,20 @@ def test_sample_arguments():
         assert sample(**kw) == A, kw
     assert sample(rows=0) == fs.FS_OK
     assert lib.fs_clear_status(None, None) == A
+
+
+def test_binding_wants_one_device():
+    m = torch.device("meta")
+    k = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
+    t = torch.zeros(2, 4, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        fs.KVCache(k, k, t.to(m))
+    with pytest.raises(ValueError):
+        fs.Sampling(torch.zeros(4), None, torch.zeros(4, device=m))
+    step = fs.Step([0, 1], kv_len=t[0, :1].clone(), max_kv=5, device="cpu")
+    with pytest.raises(ValueError):
+        fs.fs_paged_attention(step, fs.KVCache(k, k, t), torch.zeros(1, 2, 64, dtype=k.dtype, device=m),
+                              1.0)
 
 
 def test_binding_refuses_what_it_would_misread():

@@ -287,6 +287,29 @@ def test_attention_large_scores_and_a_loose_bound(lens, kv):
     within(l, lse, ltol, "lse")
 
 
+@pytest.mark.parametrize("lens,kv", [([1, 1], [300, 0]), ([90, 70, 3], [200, 40, 3])])
+def test_attention_window_beyond_every_length(lens, kv):
+    """The largest window there is, with padding rows: as without a window."""
+    g = gen(17)
+    k, v, table = make_cache(g, kv, 2, 64, 16, HF)
+    q = normal(g, sum(lens), 6, 64, dtype=HF).cuda()
+    step, cache = step_of(lens, kv), on_gpu(k, v, table)
+    plain = fs.fs_paged_attention(step, cache, q, 0.2)
+    for window in (2 ** 31 - 1, 300, 1 << 30):
+        assert torch.equal(fs.fs_paged_attention(step, cache, q, 0.2, window=window), plain)
+
+
+@pytest.mark.parametrize("lens", [[1] * 70, [80] * 3 + [1] * 67])
+def test_attention_of_many_requests(lens):
+    g = gen(18)
+    kv = [n + int(x) for n, x in zip(lens, torch.randint(0, 150, (len(lens),), generator=g))]
+    k, v, table = make_cache(g, kv, 1, 128, 16, BF)
+    q_off = offsets(lens)
+    q = normal(g, q_off[-1], 3, 128)
+    want, tol, _, _ = ref.attention(q, k, v, table, q_off, kv, 0.1, 0)
+    within(fs.fs_paged_attention(step_of(lens, kv), on_gpu(k, v, table), q.cuda(), 0.1), want, tol, "out")
+
+
 @pytest.mark.parametrize("lens", [[1, 1, 1], [50, 1, 20]])
 def test_attention_offsets_beyond_32_bits_and_shared_pages(lens):
     g = gen(12)
@@ -438,6 +461,16 @@ def test_sample_shapes_and_strides(rows, vocab, dtype):
         assert (int(tok[i]), int(kept[i])) == (a[0], a[2]), i
         assert (int(tok2[i]), int(kept2[i])) == (b[0], b[2]), i
         assert (int(tok3[i]), int(kept3[i])) == (c[0], c[2]), i
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_sample_large_k(dtype):
+    """k beyond the work-group's threads, and beyond what is sorted in LDS."""
+    g = gen(91)
+    x = normal(g, 4, 60000, dtype=dtype, std=2.0)
+    u = torch.rand(4, generator=g).tolist()
+    check_sample(x, u, k=[513, 1500, 3900, 20000])
+    check_sample(x, u, t=[0.3, 2.0, 1.0, 0.7], k=[1025, 4096, 59999, 5000], p=[0.9, 0.999, 0.5, 1.0])
 
 
 def test_sample_bad_settings():
