@@ -13,7 +13,7 @@
 //                 57 % of the cycles (4,096 rows over 32,768 keys, head_dim 128: 1.9 ms, 1.08
 //                 PFLOP/s; head_dim 64: 0.84).  128 or 256 rows a work-group share each tile
 //                 of 64 keys.
-//   k_attn_join   joins the splits' results with their maxima and sums, in split order.
+//   k_attn_join_* join the splits' results with their maxima and sums, in split order.
 // Both products run with the keys as rows of the first operand (S^T = K Q^T,
 // O^T = V^T P^T): a lane then holds scores of one query row only, its probabilities are
 // the second product's operand as they lie in registers, and the running factors are one
@@ -518,66 +518,70 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attn_chunk(AttnArgs a) {
   }
 }
 
-// ---- the splits of one row and head, joined in split order: a work-group each
-template <bool BF, int D, bool FEW>
-__global__ void __launch_bounds__(256) k_attn_join(AttnArgs a) {
+// ---- the splits of a row and head, joined in split order by 16-byte columns.
+// A row's splits, `step` rows apart from idx0 on.
+struct Parts {
+  const float *o, *ml;
+  int64_t idx0, step;
+  int splits;
+};
+// Adds every PER-th split from `first` on to the four columns of `acc`.
+template <int D, int PER>
+__device__ inline void add_splits(const AttnArgs &a, const Parts &p, int first, int c, float top,
+                                  f32x4 &acc, float &sum) {
+#pragma unroll 4
+  for (int i = first; i < p.splits; i += PER) {
+    const int64_t idx = p.idx0 + i * p.step;
+    const float mi = p.ml[idx * 2];
+    const float f = mi == -INFINITY ? 0.f : exp2_fast((mi - top) * a.c2);
+    sum += f * p.ml[idx * 2 + 1];
+    acc += f * *reinterpret_cast<const f32x4 *>(p.o + idx * D + c * 4);
+  }
+}
+// The largest of the splits' maxima, by LANES neighbouring lanes.
+template <int LANES>
+__device__ inline float top_of(const Parts &p) {
+  float top = -INFINITY;
+  for (int i = threadIdx.x % LANES; i < p.splits; i += LANES)
+    top = fmaxf(top, p.ml[(p.idx0 + i * p.step) * 2]);
+#pragma unroll
+  for (int w = LANES / 2; w; w >>= 1) top = fmaxf(top, __shfl_xor(top, w, 64));
+  return top;
+}
+template <bool BF, int D>
+__device__ inline void put_joined(const AttnArgs &a, int64_t t, int32_t h, int c, f32x4 acc,
+                                  float sum, float top) {
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  s16x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = to_16<BF>(acc[i] * inv);
+  *reinterpret_cast<s16x4 *>(a.out + t * a.out_stride + h * D + c * 4) = v;
+  if (c == 0 && a.lse)
+    a.lse[t * a.n_heads + h] = sum > 0.f ? (top * a.c2 + __log2f(sum)) * kLn2 : -INFINITY;
+}
+
+// Few rows, often many splits: a work-group for a row and head, the splits side by side.
+template <bool BF, int D>
+__global__ void __launch_bounds__(256) k_attn_join_few(AttnArgs a) {
   constexpr int PER = 256 / (D / 4);  // splits side by side
   __shared__ f32x4 part[PER][D / 4];
   __shared__ float ls[PER];
-  const int32_t h = blockIdx.x;
-  int32_t s, tok, q0, n, split;
-  int64_t idx0, step;
-  const float *po, *pml;
-  if constexpr (FEW) {
-    s = blockIdx.y;
-    tok = blockIdx.z;
-    q0 = __ldg(a.q_off + s);
-    n = __ldg(a.q_off + s + 1) - q0;
-    if (tok >= n || n * a.group > kFewRows) return;
-    split = a.few_split;
-    po = a.few_o, pml = a.few_ml;
-    idx0 = (int64_t(s) * a.few_tokens + tok) * a.n_heads + h;
-    step = int64_t(a.n_seqs) * a.few_tokens * a.n_heads;
-  } else {
-    const int32_t t = blockIdx.y * 65535 + blockIdx.z;
-    if (t >= a.rows) return;
-    s = seq_of_row(a.q_off, a.n_seqs, t);
-    q0 = __ldg(a.q_off + s);
-    n = __ldg(a.q_off + s + 1) - q0;
-    tok = t - q0;
-    if (n * a.group <= kFewRows) return;
-    split = a.chunk_split;
-    po = a.chunk_o, pml = a.chunk_ml;
-    idx0 = int64_t(t) * a.n_heads + h;
-    step = int64_t(a.rows) * a.n_heads;
-  }
+  const int32_t h = blockIdx.x, s = blockIdx.y, tok = blockIdx.z;
+  const int32_t q0 = __ldg(a.q_off + s), n = __ldg(a.q_off + s + 1) - q0;
+  if (tok >= n || n * a.group > kFewRows) return;
   int32_t code = 0;
   const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
-  int32_t tok0 = 0, tok1 = n - 1;
-  if (!FEW) {
-    const int32_t r0 = (tok * a.group + h % a.group) / a.chunk_rows * a.chunk_rows;
-    tok0 = r0 / a.group;
-    tok1 = (min(r0 + a.chunk_rows, n * a.group) - 1) / a.group;
-  }
-  const KeyRange kr = key_range(a, n, kv, tok0, tok1);
+  const KeyRange kr = key_range(a, n, kv, 0, n - 1);
   const int32_t len = kr.hi - kr.lo;
-  if (len <= split) return;  // written whole
-  const int splits = (len + split - 1) / split;
-  float top = -INFINITY;
-  for (int i = threadIdx.x & 63; i < splits; i += 64)
-    top = fmaxf(top, pml[(idx0 + i * step) * 2]);
-  for (int w = 32; w; w >>= 1) top = fmaxf(top, __shfl_xor(top, w, 64));
+  if (len <= a.few_split) return;  // written whole
+  const Parts p{a.few_o, a.few_ml, (int64_t(s) * a.few_tokens + tok) * a.n_heads + h,
+                int64_t(a.n_seqs) * a.few_tokens * a.n_heads,
+                (len + a.few_split - 1) / a.few_split};
+  const float top = top_of<64>(p);
   const int g = threadIdx.x / (D / 4), c = threadIdx.x % (D / 4);
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   float sum = 0.f;
-#pragma unroll 4
-  for (int i = g; i < splits; i += PER) {
-    const int64_t idx = idx0 + i * step;
-    const float mi = pml[idx * 2];
-    const float f = mi == -INFINITY ? 0.f : exp2_fast((mi - top) * a.c2);
-    sum += f * pml[idx * 2 + 1];
-    acc += f * *reinterpret_cast<const f32x4 *>(po + idx * D + c * 4);
-  }
+  add_splits<D, PER>(a, p, g, c, top, acc, sum);
   part[g][c] = acc;
   if (c == 0) ls[g] = sum;
   __syncthreads();
@@ -586,14 +590,34 @@ __global__ void __launch_bounds__(256) k_attn_join(AttnArgs a) {
   acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < PER; ++i) acc += part[i][c], sum += ls[i];
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
-  const int64_t t = q0 + tok;
-  s16x4 v;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = to_16<BF>(acc[i] * inv);
-  *reinterpret_cast<s16x4 *>(a.out + t * a.out_stride + h * D + c * 4) = v;
-  if (c == 0 && a.lse)
-    a.lse[t * a.n_heads + h] = sum > 0.f ? (top * a.c2 + __log2f(sum)) * kLn2 : -INFINITY;
+  put_joined<BF, D>(a, q0 + tok, h, c, acc, sum, top);
+}
+
+// Many rows, few splits: D / 4 lanes for a row and head.  (1,000 tokens of 32 heads in 2
+// splits, head_dim 128: 10.5 us; with a work-group for each row and head 43.)
+template <bool BF, int D>
+__global__ void __launch_bounds__(256) k_attn_join_chunk(AttnArgs a) {
+  constexpr int LANES = D / 4;
+  const int32_t it = blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+  if (it >= a.rows * a.n_heads) return;
+  const int32_t t = it / a.n_heads, h = it - t * a.n_heads, c = threadIdx.x % LANES;
+  const int32_t s = seq_of_row(a.q_off, a.n_seqs, t);
+  const int32_t q0 = __ldg(a.q_off + s), n = __ldg(a.q_off + s + 1) - q0;
+  if (n * a.group <= kFewRows) return;
+  int32_t code = 0;
+  const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
+  const int32_t r0 = ((t - q0) * a.group + h % a.group) / a.chunk_rows * a.chunk_rows;
+  const KeyRange kr = key_range(a, n, kv, r0 / a.group,
+                                (min(r0 + a.chunk_rows, n * a.group) - 1) / a.group);
+  const int32_t len = kr.hi - kr.lo;
+  if (len <= a.chunk_split) return;  // written whole
+  const Parts p{a.chunk_o, a.chunk_ml, it, int64_t(a.rows) * a.n_heads,
+                (len + a.chunk_split - 1) / a.chunk_split};
+  const float top = top_of<LANES>(p);
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  float sum = 0.f;
+  add_splits<D, 1>(a, p, 0, c, top, acc, sum);
+  put_joined<BF, D>(a, t, h, c, acc, sum, top);
 }
 
 // How a call's work is split: from the step's shape and the bound on lengths alone.
@@ -704,12 +728,12 @@ void run(const AttnArgs &a, const Plan &p, hipStream_t stream) {
                          dim3(p.chunk_tiles * a.c.n_kv_heads, p.chunk_splits), block, 0, stream, a);
   }
   if (p.few_splits > 1)
-    hipLaunchKernelGGL((k_attn_join<BF, D, true>), dim3(a.n_heads, a.n_seqs, p.few_tokens),
-                       dim3(256), 0, stream, a);
-  if (p.chunk_splits > 1)
-    hipLaunchKernelGGL((k_attn_join<BF, D, false>),
-                       dim3(a.n_heads, (a.rows + 65534) / 65535, min(a.rows, 65535)), dim3(256),
-                       0, stream, a);
+    hipLaunchKernelGGL((k_attn_join_few<BF, D>), dim3(a.n_heads, a.n_seqs, p.few_tokens), block, 0,
+                       stream, a);
+  if (p.chunk_splits > 1) {
+    const int64_t lanes = int64_t(a.rows) * a.n_heads * (D / 4);
+    hipLaunchKernelGGL((k_attn_join_chunk<BF, D>), dim3((lanes + 255) / 256), block, 0, stream, a);
+  }
 }
 
 }  // namespace

@@ -4,9 +4,18 @@
 // sum of two 16-bit values, with the row's adapter beside it.  The product then runs over
 // K and goes on over the few columns of h against B_a in the same accumulators, so y is
 // written once and never read:
-//   k_linear_few   up to 256 rows: bound by the bytes of W.  A work-group takes 16 or 32
-//                  columns of y; its eight waves share out K and join in LDS.
-//   k_linear_tile  more rows: bound by the matrix cores.  W and x go through LDS in tiles.
+//   k_shrink       16 rows of one request a work-group; its waves share out K and join in
+//                  LDS.  Bound by the bytes of x where there are many rows (16,384 rows of
+//                  4,096: 134 MB in 38 us, 3.6 TB/s), by one tile's chain where there are few
+//                  (5.6 us).
+//   k_linear_few   up to 64 rows: bound by the bytes of W, and at a few MB by what a
+//                  work-group can have under way (64 rows, 4,096 x 6,144: 50 MB in 17 to 20
+//                  us).  A work-group takes 16 or 32 columns of y; its four waves share out K
+//                  and join in LDS.
+//   k_linear_tile  more rows: bound by the matrix cores and LDS together.  W and x go through
+//                  LDS in tiles (16,384 x 4,096 x 4,096: 490 to 530 us, 1.04 to 1.12 PFLOP/s, the matrix cores busy for 58 % of the
+//                  cycles; its loads alone take 404 us, its products alone 419).  Eight waves
+//                  with tiles of 128 x 64 each read LDS least for a product.
 // W is the first operand (its rows are y's columns), so a lane holds neighbouring columns
 // of one row of y.
 #include "fs_engine.h"
