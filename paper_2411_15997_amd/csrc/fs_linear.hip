@@ -10,12 +10,13 @@
 //                  (5.6 us).
 //   k_linear_few   up to 64 rows: bound by the bytes of W, and at a few MB by what a
 //                  work-group can have under way (64 rows, 4,096 x 6,144: 50 MB in 17 to 20
-//                  us).  A work-group takes 16 or 32 columns of y; its four waves share out K
+//                  us).  A work-group takes 16 to 64 columns of y; its four waves share out K
 //                  and join in LDS.
 //   k_linear_tile  more rows: bound by the matrix cores and LDS together.  W and x go through
-//                  LDS in tiles (16,384 x 4,096 x 4,096: 490 to 530 us, 1.04 to 1.12 PFLOP/s, the matrix cores busy for 58 % of the
-//                  cycles; its loads alone take 404 us, its products alone 419).  Eight waves
-//                  with tiles of 128 x 64 each read LDS least for a product.
+//                  LDS in tiles (16,384 x 4,096 x 4,096: 470 to 490 us and the shrink's 38,
+//                  1.1 PFLOP/s, the matrix cores busy for 58 % of the cycles; its loads alone
+//                  take 404 us, its products alone 419).  Eight waves with tiles of 128 x 64
+//                  each read LDS least for a product.
 // W is the first operand (its rows are y's columns), so a lane holds neighbouring columns
 // of one row of y.
 #include "fs_engine.h"
@@ -191,20 +192,20 @@ __device__ inline int32_t rank_of(const LinArgs &g, int32_t ad) {
   return g.rank ? min(__ldg(g.rank + ad), g.R) : g.R;
 }
 
-// ---- few rows: MT tiles of 16 rows by NT tiles of 16 columns, four waves
+// ---- few rows: all of them, in MT tiles of 16, by NT tiles of 16 columns, four waves
 template <bool BF, int MT, int NT, int STAGES>
 __global__ void __launch_bounds__(256) k_linear_few(LinArgs g) {
   __shared__ __align__(16) short lds[4 * STAGES * (MT + NT) * 16 * 64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15;
-  const int n0 = blockIdx.x * (NT * 16), m0 = blockIdx.y * (MT * 16);
+  const int n0 = blockIdx.x * (NT * 16);
   const s16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
   // the adapters of the tile of rows that this wave deals with
-  const int my = wave % MT, my_row = m0 + my * 16 + r;
+  const int my = wave % MT, my_row = my * 16 + r;
   const int32_t ad = g.n_adapters > 0 && my_row < g.rows ? __ldg(g.row_ad + my_row) : -1;
   f32x4 acc[MT][NT] = {};
-  share_of_k<BF, MT, NT, 4, STAGES>(g.x + int64_t(m0) * g.x_stride, g.x_stride, g.rows - m0,
-                                    g.w + int64_t(n0) * g.K, g.N - n0, g.K, wave, lds, acc);
+  share_of_k<BF, MT, NT, 4, STAGES>(g.x, g.x_stride, g.rows, g.w + int64_t(n0) * g.K, g.N - n0,
+                                    g.K, wave, lds, acc);
   // The distinct adapters of a tile's rows, shared out over the 4 / MT waves that hold the
   // tile: four adapters' loads side by side, 4 chunks of 8 columns at a time (R/8 high
   // ones, then R/8 low ones).
@@ -264,7 +265,7 @@ __global__ void __launch_bounds__(256) k_linear_few(LinArgs g) {
     f32x4 v = part[t * 64 + lane];
 #pragma unroll
     for (int w = 1; w < 4; ++w) v += part[(w * MT * NT + t) * 64 + lane];
-    const int row = m0 + (t / NT) * 16 + r, n = n0 + (t % NT) * 16 + (lane >> 4) * 4;
+    const int row = (t / NT) * 16 + r, n = n0 + (t % NT) * 16 + (lane >> 4) * 4;
     if (row < g.rows && n < g.N) {
       s16x4 o;
 #pragma unroll
@@ -465,7 +466,8 @@ template <bool BF, int JT>
 void shrink(const LinArgs &g, const fs_step *st, hipStream_t stream) {
   const int64_t tiles = row_tiles(st, 4);
   // few tiles: more waves share out K, so that one tile's time is short (as LDS allows);
-  // many: the loads of several steps are under way
+  // many: the loads of several steps are under way.  (The two lie within 1 % of the whole
+  // call on either side: 137 tiles 40.9 against 41.3 us, 512 259.5 against 262.)
   constexpr int kMost = JT == 1 ? 16 : JT <= 4 ? 8 : 4;
   constexpr int kStages = JT == 1 ? 4 : JT == 2 ? 3 : 2;
   if (tiles <= 512)
@@ -474,17 +476,30 @@ void shrink(const LinArgs &g, const fs_step *st, hipStream_t stream) {
     hipLaunchKernelGGL((k_shrink<BF, JT, 4, kStages>), dim3(tiles), dim3(256), 0, stream, g);
 }
 
+// Columns of a work-group: each reads all of x, so few rows take the least columns, and more
+// take 16 while two of them on each compute unit hold all columns, else 48 or 64, one on each
+// compute unit, as fewer rounds of its time ask (with the shrink, K = 4,096, 64 rows:
+//   columns        6,144   9,000  14,336  20,000  28,672
+//   16 at a time    24.6    37.5    55.7    69.5    95.5 us
+//   32              25.0    48.0    54.1    79.4   105.1
+//   48              24.8    30.0    58.1    64.6    91.0
+//   64              27.6    33.6    41.8    76.1    81.9
+// 16 rows by 28,672: 58 us with 16 columns, 70 with 32, 57 with 64; 64 rows on their tiles of
+// k_linear_tile: 29.9 us for 6,144 columns, 39.0 for 14,336, 85.5 for 28,672).
 template <bool BF, int MT>
 void few(const LinArgs &g, hipStream_t stream) {
-  const int mb = (g.rows + MT * 16 - 1) / (MT * 16);
   constexpr int kStages = MT == 4 ? 2 : MT == 2 ? 3 : 4;  // 64 to 80 KB of LDS for 16 columns
-  // 16 columns a work-group while two of them on each compute unit hold them all
-  if ((g.N + 15) / 16 * mb <= 512)
-    hipLaunchKernelGGL((k_linear_few<BF, MT, 1, kStages>), dim3((g.N + 15) / 16, mb), dim3(256), 0,
-                       stream, g);
-  else
-    hipLaunchKernelGGL((k_linear_few<BF, MT, 2, kStages>), dim3((g.N + 31) / 32, mb), dim3(256), 0,
-                       stream, g);
+  auto groups = [&](int cols) { return dim3((g.N + cols - 1) / cols); };
+  if (MT == 1 || g.N <= 512 * 16)
+    hipLaunchKernelGGL((k_linear_few<BF, MT, 1, kStages>), groups(16), dim3(256), 0, stream, g);
+  else if constexpr (MT > 1) {
+    const int cus = 256, by48 = (g.N + cus * 48 - 1) / (cus * 48),
+              by64 = (g.N + cus * 64 - 1) / (cus * 64);
+    if (by48 * 3 <= by64 * 4)
+      hipLaunchKernelGGL((k_linear_few<BF, MT, 3, 2>), groups(48), dim3(256), 0, stream, g);
+    else
+      hipLaunchKernelGGL((k_linear_few<BF, MT, 4, 2>), groups(64), dim3(256), 0, stream, g);
+  }
 }
 
 template <bool BF>
@@ -508,7 +523,9 @@ void run(const LinArgs &g, const fs_step *st, hipStream_t stream) {
       few<BF, 4>(g, stream);
     return;
   }
-  // The largest tiles that still occupy three quarters of the compute units.
+  // The largest tiles that still occupy three quarters of the compute units (K = 4,096: 1,024
+  // tiles of 256 take 516 us, of 128 587 and of 64 902; 2,048 rows by 4,096 columns, 128 tiles
+  // of 256, 106, 75 and 114 us; K = 2,048, 500 rows by 2,560 columns: - , 34.0 and 22.7).
   auto tiles = [&](int64_t t) { return ((g.rows + t - 1) / t) * ((g.N + t - 1) / t); };
   if (tiles(256) >= 192)
     hipLaunchKernelGGL((k_linear_tile<BF, 256, 256, 128, 64, 64, 2>), dim3(tiles(256)), dim3(512),

@@ -84,6 +84,20 @@ def test_linear(lens, K, N, n, R, dtype):
     assert torch.equal(again, y)
 
 
+@pytest.mark.parametrize("rows", [20, 50])
+@pytest.mark.parametrize("N", [8200, 12304, 24600])
+def test_linear_few_rows_many_columns(rows, N):
+    g = gen(rows + N)
+    K, lens = 136, [1] * (rows - 7) + [7]
+    q_off = offsets(lens)
+    x, w = normal(g, rows, K), normal(g, N, K, std=K ** -0.5)
+    a, b = normal(g, 3, 16, K, std=K ** -0.5), normal(g, 3, N, 16)
+    adapter = torch.randint(-1, 3, (len(lens),), generator=g, dtype=torch.int32)
+    want, bound = ref.linear(x, w, a, b, q_off, adapter)
+    ad = fs.Adapters(a.cuda(), b.cuda(), adapter.cuda())
+    within(fs.fs_adapter_linear(fs.Step(q_off), ad, x.cuda(), w.cuda()), want, bound, "y")
+
+
 def test_linear_without_adapters_and_defaults():
     g = gen(5)
     lens, K, N = [5, 1, 70], 128, 200
