@@ -112,14 +112,22 @@ def _want(cond, what):
 
 
 def _stream(t):
-    return _torch()._C._cuda_getCurrentRawStream(t.device.index)
+    return _torch()._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _one_device(*tensors):
-    """The device of the tensors given (None among them is left out)."""
+    """The index of the device of the tensors given (None among them is left out)."""
     devices = {t.device for t in tensors if t is not None}
     _want(len(devices) == 1, f"tensors on one device, not on {sorted(map(str, devices))}")
-    return devices.pop()
+    return devices.pop().index
+
+
+def _on(index, *tensors):
+    """The tensors given are on the GPU of that index (what the host could not read the GPU
+    would fault on)."""
+    for t in tensors:
+        if t is not None and t.get_device() != index or index is None:
+            raise ValueError("every tensor of a call on one GPU")
 
 
 def _vector(t, dtype, n, name):
@@ -136,15 +144,10 @@ def _rows(t, name, shape):
     if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, wanted {shape}")
     st = t.stride()
-    if len(shape) == 3:
-        packed = (st[2] == 1 or shape[2] == 1) and (st[1] == shape[2] or shape[1] == 1)
-        row = shape[1] * shape[2]
-    else:
-        packed = st[1] == 1 or shape[1] == 1
-        row = shape[1]
-    if not packed:
+    inner = shape[-1]
+    if st[-1] != 1 and inner != 1 or len(st) == 3 and st[1] != inner and shape[1] != 1:
         raise ValueError(f"{name}: inner dimensions are not packed")
-    return t.data_ptr(), (st[0] if shape[0] > 1 else row)
+    return t.data_ptr(), (st[0] if shape[0] > 1 else inner if len(st) == 2 else inner * shape[1])
 
 
 def _new(shape, dtype, device):
@@ -190,7 +193,7 @@ class Step:
         self.n, self.rows = n, int(self.q_off_h[-1])
         self.q_off = torch.from_numpy(self.q_off_h.copy()).to(device) if q_off is None else q_off
         self.kv_len = kv_len
-        self.device = _one_device(self.q_off, kv_len)
+        self.gpu = _one_device(self.q_off, kv_len)
         self.s = fs_step(n, self.q_off_h.ctypes.data,
                          _vector(self.q_off, torch.int32, n + 1, "q_off"),
                          _vector(kv_len, torch.int32, n, "kv_len"), int(max_kv))
@@ -208,7 +211,7 @@ class KVCache:
         _want(k.shape[3] == 1 or k.stride(3) == 1, "k, v: the last dimension is not packed")
         _want(table.dim() == 2 and table.dtype == torch.int32 and
               (table.shape[1] <= 1 or table.stride(1) == 1), "table: int32 [n][width]")
-        self.k, self.v, self.table, self.device = k, v, table, _one_device(k, v, table)
+        self.k, self.v, self.table, self.gpu = k, v, table, _one_device(k, v, table)
         self.n_kv_heads, self.head_dim, self.dtype = k.shape[1], k.shape[3], k.dtype
         self.s = fs_kv_cache(_dtype_code(k), k.shape[1], k.shape[3], k.shape[2], k.shape[0],
                              k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
@@ -234,7 +237,7 @@ class Adapters:
               "a [n][max_rank][K] and b [n][N][max_rank]: packed, of one dtype")
         n, r, k = a.shape
         self.keep = (a, b, adapter, rank, scale)
-        self.device = _one_device(*self.keep)
+        self.gpu = _one_device(*self.keep)
         self.dtype, self.K, self.N, self.n_seqs = a.dtype, k, b.shape[1], adapter.shape[0]
         self.s = fs_adapters(_dtype_code(a), k, b.shape[1], n, r, a.data_ptr(), b.data_ptr(),
                              _vector(rank, torch.int32, n, "rank"),
@@ -249,7 +252,7 @@ class Rope:
 
     def __init__(self, inv_freq, interleaved=False, factor=1.0, pos=None):
         torch = _torch()
-        self.inv_freq, self.pos, self.device = inv_freq, pos, _one_device(inv_freq, pos)
+        self.inv_freq, self.pos, self.gpu = inv_freq, pos, _one_device(inv_freq, pos)
         n = inv_freq.shape[0]
         self.s = fs_rope(2 * n, int(bool(interleaved)), _vector(inv_freq, torch.float32, n, "inv_freq"),
                          float(factor), _vector(pos, torch.int32, 0, "pos"))
@@ -263,7 +266,7 @@ class Sampling:
         torch = _torch()
         self.keep = (temperature, top_k, top_p, min_p)
         self.rows = min((t.shape[0] for t in self.keep if t is not None), default=None)
-        self.device = _one_device(*self.keep) if self.rows is not None else None
+        self.gpu = _one_device(*self.keep) if self.rows is not None else None
         self.s = fs_sampling(_vector(temperature, torch.float32, 0, "temperature"),
                              _vector(top_k, torch.int32, 0, "top_k"),
                              _vector(top_p, torch.float32, 0, "top_p"),
@@ -278,7 +281,8 @@ def fs_adapter_linear(step: Step, adapters: Adapters, x, w, y=None, ws=None, err
     _want(w.shape == (N, K) and w.is_contiguous(), "w: packed [N][K]")
     _want(x.dtype == adapters.dtype and w.dtype == adapters.dtype, "x, w and adapters: one dtype")
     _want(adapters.n_seqs >= step.n, "adapter: an id for every request")
-    _want(x.device == w.device == adapters.device == step.device, "x, w, adapters, step: one device")
+    _on(step.gpu, x, w, y, ws, err)
+    _want(adapters.gpu == step.gpu, "adapters and step: one GPU")
     if y is None:
         y = _new((step.rows, N), x.dtype, x.device)
         yp, ys = y.data_ptr(), N
@@ -315,8 +319,8 @@ def fs_rope_append(step: Step, cache: KVCache, rope: Rope, q, k, v, q_out=None, 
           (q is None or q.dtype == cache.dtype), "q, k, v: the cache's dtype")
     _want(cache.table.shape[0] >= step.n, "table: a row for every request")
     _want(rope.pos is None or rope.pos.shape[0] >= T, "pos: a position for every row")
-    _want(k.device == v.device == cache.device == rope.device == step.device and
-          (q is None or q.device == k.device), "q, k, v, cache, rope, step: one device")
+    _on(step.gpu, q, k, v, q_out, err)
+    _want(cache.gpu == rope.gpu == step.gpu, "cache, rope and step: one GPU")
     kp, ks = _rows(k, "k", (T, HK, D))
     vp, vs = _rows(v, "v", (T, HK, D))
     H, qp, qs, op, os_ = 0, None, 0, None, 0
@@ -342,7 +346,8 @@ def fs_paged_attention(step: Step, cache: KVCache, q, scale, window=0, out=None,
     T, H, D = q.shape
     _want(q.dtype == cache.dtype and D == cache.head_dim, "q: the cache's dtype and head_dim")
     _want(cache.table.shape[0] >= step.n, "table: a row for every request")
-    _want(q.device == cache.device == step.device, "q, cache, step: one device")
+    _on(step.gpu, q, out, lse, ws, err)
+    _want(cache.gpu == step.gpu, "cache and step: one GPU")
     qp, qs = _rows(q, "q", (step.rows, H, D))
     torch = _torch()
     if out is None:
@@ -377,7 +382,8 @@ def fs_sample(logits, u, sampling: Sampling, token=None, logprob=None, kept=None
     _want(sampling.rows is None or sampling.rows >= n, "sampling: a setting for every row")
     up = _vector(u, torch.float32, n, "u")
     dev = logits.device
-    _want(u.device == dev and sampling.device in (None, dev), "logits, u, sampling: one device")
+    _on(dev.index, u, token, logprob, kept, ws, err)
+    _want(sampling.gpu is None or sampling.gpu == dev.index, "logits and sampling: one GPU")
     like = u if u.shape[0] == n else u[:n]
 
     def output(t, dtype, name):

@@ -128,6 +128,13 @@ def test_binding_wants_one_device():
     with pytest.raises(ValueError):
         fs.fs_paged_attention(step, fs.KVCache(k, k, t), torch.zeros(1, 2, 64, dtype=k.dtype, device=m),
                               1.0)
+    q = torch.zeros(1, 2, 64, dtype=k.dtype)
+    rope = fs.Rope(torch.ones(32))
+    for call in (lambda: fs.fs_paged_attention(step, fs.KVCache(k, k, t), q, 1.0),
+                 lambda: fs.fs_rope_append(step, fs.KVCache(k, k, t), rope, q, q, q),
+                 lambda: fs.fs_sample(q[0].float(), torch.zeros(2), fs.Sampling())):
+        with pytest.raises(ValueError):                    # nothing of it is on a GPU
+            call()
 
 
 def test_binding_refuses_what_it_would_misread():
