@@ -145,7 +145,7 @@ fs_status fs_rope_append(const fs_step *s, const fs_kv_cache *c, const fs_rope *
  * ln sum_j exp(scale q . k_j), which joins results over parts of a context.
  *   q, out: [T][n_heads][head_dim] of the cache's dtype (token strides q_stride,
  *   out_stride); head_dim 64 or 128; n_heads a multiple of n_kv_heads, at most 64 times it;
- *   rows times n_heads at most 2^30, n_seqs times n_kv_heads at most 2^21.
+ *   rows times n_heads at most 2^30, n_seqs times n_kv_heads at most 2^20.
  * Scores, softmax statistics and sums are fp32; the probabilities enter the second
  * product in the cache's dtype.  Values at positions that a row's mask excludes have to
  * be finite if they lie below kv_len (they meet a probability of 0).

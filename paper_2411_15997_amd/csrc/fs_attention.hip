@@ -19,6 +19,8 @@
 // the second product's operand as they lie in registers, and the running factors are one
 // number per lane.  The second product takes the keys in the order in which the first
 // one leaves them; V is read from LDS transposed, in that same order.
+#include <type_traits>
+
 #include "fs_engine.h"
 
 namespace fs {
@@ -103,20 +105,20 @@ __device__ inline float max_of_halves(float x) {
 
 // ---- few rows: NT tiles of 16 rows
 template <bool BF, int D, int NT>
-__global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
+__device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *lds) {
   constexpr int KS = D / 32;  // matrix steps of a score
   constexpr int DB = D / 16;  // 16-column blocks of an output row
   constexpr int CH = D / 8;   // 16-byte chunks of a key row
   constexpr int RW = 64 / CH, LD = 32 / RW;  // rows of a wave's load, loads of 32 keys' K (or V)
   constexpr int kIds = 512;   // page ids kept in LDS
-  __shared__ __align__(16) short kv_lds[4][2][32 * D];  // a wave's K and V
+  auto kv_lds = reinterpret_cast<short(*)[2][32 * D]>(lds);  // a wave's K and V
   __shared__ float wm[4][NT * 16], wl[4][NT * 16];
   __shared__ uint32_t ids[kIds];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, g4 = lane >> 4;
   // Work-groups go to the 8 dies in turn: heads fastest, and each split shifts the
   // requests by one, so a long request's splits do not gather on one die.
-  const int hk = blockIdx.x % a.c.n_kv_heads, sz = blockIdx.x / a.c.n_kv_heads;
+  const int hk = block % a.c.n_kv_heads, sz = block / a.c.n_kv_heads;
   const int z = sz / a.n_seqs, s = (sz + z) % a.n_seqs;
   const int32_t q0 = __ldg(a.q_off + s), n = __ldg(a.q_off + s + 1) - q0;
   const int G = a.group, R = n * G;
@@ -347,19 +349,19 @@ __device__ inline void chunk_tile(const AttnArgs &a, int32_t b, int32_t &s, int3
 
 // ---- chunks: WAVES waves of 32 rows, 64 keys at a time through two buffers
 template <bool BF, int D, int WAVES>
-__global__ void __launch_bounds__(WAVES * 64, 2) k_attn_chunk(AttnArgs a) {
+__device__ __forceinline__ void attn_chunk(const AttnArgs &a, int block, int z, short *lds) {
   constexpr int KS = D / 16;       // matrix steps of a score
   constexpr int DB = D / 32;       // 32-column blocks of an output row
   constexpr int CH = D / 8;        // 16-byte chunks of a key row
   constexpr int RW = 64 / CH;      // rows of a wave's load
   constexpr int LD = 64 / WAVES / RW;  // a wave's loads of K, and of V, for 64 keys
   static_assert(LD >= 1, "a wave loads whole rows");
-  __shared__ __align__(16) short kt[2][64 * D], vt[2][64 * D];
+  auto kt = reinterpret_cast<short(*)[64 * D]>(lds), vt = kt + 2;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r32 = lane & 31, h2 = lane >> 5;
-  const int hk = blockIdx.x % a.c.n_kv_heads;
+  const int hk = block % a.c.n_kv_heads;
   int32_t s, r0;
-  chunk_tile(a, blockIdx.x / a.c.n_kv_heads, s, r0);
+  chunk_tile(a, block / a.c.n_kv_heads, s, r0);
   const int32_t q0 = __ldg(a.q_off + s), n = __ldg(a.q_off + s + 1) - q0;
   const int G = a.group, R = n * G;
   if (r0 < 0 || R <= kFewRows) return;
@@ -367,8 +369,8 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attn_chunk(AttnArgs a) {
   const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
   const KeyRange kr = key_range(a, n, kv, r0 / G, (min(r0 + WAVES * 32, R) - 1) / G);
   const bool single = kr.hi - kr.lo <= a.chunk_split;
-  const int32_t lo = kr.lo + blockIdx.y * a.chunk_split;
-  if (blockIdx.y > 0 && lo >= kr.hi) return;
+  const int32_t lo = kr.lo + z * a.chunk_split;
+  if (z > 0 && lo >= kr.hi) return;
   const int32_t hi = min(kr.hi, lo + a.chunk_split);
   const int32_t *table = a.c.table + s * a.c.table_stride;
   const uint32_t head = hk * a.c.head_stride;
@@ -506,7 +508,7 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attn_chunk(AttnArgs a) {
       a.lse[int64_t(q0 + tok) * a.n_heads + h] =
           l > 0.f ? (m * a.c2 + __log2f(l)) * kLn2 : -INFINITY;
   } else {
-    const int64_t idx = (int64_t(blockIdx.y) * a.rows + q0 + tok) * a.n_heads + h;
+    const int64_t idx = (int64_t(z) * a.rows + q0 + tok) * a.n_heads + h;
     float *op = a.chunk_o + idx * D;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -516,6 +518,31 @@ __global__ void __launch_bounds__(WAVES * 64, 2) k_attn_chunk(AttnArgs a) {
             f32x4{o[d][i * 4], o[d][i * 4 + 1], o[d][i * 4 + 2], o[d][i * 4 + 3]};
     if (h2 == 0) a.chunk_ml[idx * 2] = m, a.chunk_ml[idx * 2 + 1] = l;
   }
+}
+
+template <bool BF, int D, int NT>
+__global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
+  __shared__ __align__(16) short lds[256 * D];
+  attn_few<BF, D, NT>(a, blockIdx.x, lds);
+}
+template <bool BF, int D, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64, 2) k_attn_chunk(AttnArgs a) {
+  __shared__ __align__(16) short lds[256 * D];
+  attn_chunk<BF, D, WAVES>(a, blockIdx.x, blockIdx.y, lds);
+}
+// Both kinds of requests in one launch: the single tokens' loads fill what the chunks' last
+// work-groups leave of the card.  (24 requests of up to 8,192 tokens, 16 heads of 64, a window
+// of 3,000: 82 us, 99 one after the other, 102 with the chunks last; 24 of up to 16,000, most
+// of them chunks of 400 or less: 216 us, 232 one after the other, 301 with the chunks last,
+// 275 with the two evenly mixed.)
+template <bool BF, int D, int NT>
+__global__ void __launch_bounds__(256, 2) k_attn_mixed(AttnArgs a, int chunk, int tiles) {
+  __shared__ __align__(16) short lds[256 * D];
+  const int block = blockIdx.x;
+  if (block < chunk)
+    attn_chunk<BF, D, 4>(a, block % tiles, block / tiles, lds);
+  else
+    attn_few<BF, D, NT>(a, block - chunk, lds);
 }
 
 // ---- the splits of a row and head, joined in split order by 16-byte columns.
@@ -708,24 +735,30 @@ Space space(const Plan &p, const fs_step *s, const fs_kv_cache *c, int32_t n_hea
 template <bool BF, int D>
 void run(const AttnArgs &a, const Plan &p, hipStream_t stream) {
   const dim3 block(256);
-  if (p.few_seqs > 0) {
-    const dim3 grid(uint32_t(a.n_seqs) * a.c.n_kv_heads * p.few_splits);
-    if (p.few_rows <= 16)
-      hipLaunchKernelGGL((k_attn_few<BF, D, 1>), grid, block, 0, stream, a);
-    else if (p.few_rows <= 32)
-      hipLaunchKernelGGL((k_attn_few<BF, D, 2>), grid, block, 0, stream, a);
-    else
-      hipLaunchKernelGGL((k_attn_few<BF, D, 4>), grid, block, 0, stream, a);
-  }
-  if (p.chunk_seqs > 0) {
+  const int few = p.few_seqs > 0 ? a.n_seqs * a.c.n_kv_heads * p.few_splits : 0;
+  const int tiles = p.chunk_tiles * a.c.n_kv_heads;
+  const int chunk = p.chunk_seqs > 0 ? tiles * p.chunk_splits : 0;
+  auto by_rows = [&](auto nt) {
+    constexpr int NT = decltype(nt)::value;
+    if (few > 0 && chunk > 0 && p.chunk_rows == 128)
+      hipLaunchKernelGGL((k_attn_mixed<BF, D, NT>), dim3(chunk + few), block, 0, stream, a, chunk,
+                         tiles);
+    else if (few > 0)
+      hipLaunchKernelGGL((k_attn_few<BF, D, NT>), dim3(few), block, 0, stream, a);
+  };
+  if (p.few_rows <= 16)
+    by_rows(std::integral_constant<int, 1>());
+  else if (p.few_rows <= 32)
+    by_rows(std::integral_constant<int, 2>());
+  else
+    by_rows(std::integral_constant<int, 4>());
+  if (chunk > 0) {
+    const dim3 grid(tiles, p.chunk_splits);
     if constexpr (D == 128)
       if (p.chunk_rows == 256)
-        hipLaunchKernelGGL((k_attn_chunk<BF, D, 8>),
-                           dim3(p.chunk_tiles * a.c.n_kv_heads, p.chunk_splits), dim3(512), 0,
-                           stream, a);
-    if (p.chunk_rows == 128)
-      hipLaunchKernelGGL((k_attn_chunk<BF, D, 4>),
-                         dim3(p.chunk_tiles * a.c.n_kv_heads, p.chunk_splits), block, 0, stream, a);
+        hipLaunchKernelGGL((k_attn_chunk<BF, D, 8>), grid, dim3(512), 0, stream, a);
+    if (few == 0 && p.chunk_rows == 128)
+      hipLaunchKernelGGL((k_attn_chunk<BF, D, 4>), grid, block, 0, stream, a);
   }
   if (p.few_splits > 1)
     hipLaunchKernelGGL((k_attn_join_few<BF, D>), dim3(a.n_heads, a.n_seqs, p.few_tokens), block, 0,

@@ -76,7 +76,7 @@ fs_status check_attention(const fs_step *s, const fs_kv_cache *c, int32_t n_head
     return FS_E_ARG;
   // keeps every count of work-items in 32 bits
   if (int64_t(rows_of(s)) * n_heads > (int64_t(1) << 30) ||
-      int64_t(s->n_seqs) * c->n_kv_heads > (int64_t(1) << 21))
+      int64_t(s->n_seqs) * c->n_kv_heads > (int64_t(1) << 20))
     return FS_E_ARG;
   return FS_OK;
 }
