@@ -10,7 +10,7 @@
 //                 load 32 keys at a time into LDS of their own and never wait for each other.
 //   k_attn_chunk  larger chunks: bound by the waits of a tile's chain (scores, maximum,
 //                 exponentials, products) at two waves a SIMD; the matrix cores are busy for
-//                 57 % of the cycles (4,096 rows over 32,768 keys, head_dim 128: 1.9 ms, 1.08
+//                 half of the cycles (4,096 rows over 32,768 keys, head_dim 128: 1.9 ms, 1.08
 //                 PFLOP/s; head_dim 64: 0.84).  128 or 256 rows a work-group share each tile
 //                 of 64 keys.
 //   k_attn_join_* join the splits' results with their maxima and sums, in split order.
@@ -691,6 +691,10 @@ Plan plan(const fs_step *s, const fs_kv_cache *c, int32_t n_heads, int32_t windo
     split = int32_t(each);
     splits = len > split ? (len + split - 1) / split : 1;
   };
+  // few rows: 1,024 work-groups wanted, of 512 to 1,024 keys (4 requests of up to 500 keys,
+  // 8 heads: 9.7 us whole, 13.0 in two splits of 256, and 3,000 keys 15.5 and 14.1; 64 of up
+  // to 16,384: 121 us with 1,024 keys at most, 125 with 512, 127 with 2,048; one of 200,001
+  // over 4 heads: 86 us, 94 with 2,048 work-groups, 90 with 512)
   if (p.few_seqs > 0)
     split_of(int64_t(p.few_seqs) * c->n_kv_heads, keys(p.few_tokens), 1024, 512, 1024,
              int64_t(s->n_seqs) * p.few_tokens, p.few_split, p.few_splits);
@@ -701,8 +705,16 @@ Plan plan(const fs_step *s, const fs_kv_cache *c, int32_t n_heads, int32_t windo
     // 256 rows share each key tile where that still gives every compute unit a work-group
     // (head_dim 128: 4,096 rows over 32,768 keys 2.03 ms with 128 rows, 1.89 ms with 256; the
     // lighter tiles of head_dim 64 gain more from four work-groups a unit, 145 against 109 us)
-    p.chunk_rows = c->head_dim == 128 && int64_t(tiles(256)) * c->n_kv_heads >= 256 ? 256 : 128;
+    // and no request of few rows is there to run beside them (100 requests, chunks of up to
+    // 300 of 8 x 4 heads and single tokens: 466 us with 256 rows, 356 with 128 and one launch;
+    // chunks of up to 4,000 over 20,000 keys: 2.23 ms and 2.30)
+    p.chunk_rows = c->head_dim == 128 && p.few_seqs == 0 &&
+                           int64_t(tiles(256)) * c->n_kv_heads >= 256
+                       ? 256
+                       : 128;
     p.chunk_tiles = tiles(p.chunk_rows);
+    // 512 work-groups wanted, of at least 1,024 keys (300 rows over 20,000 keys: 134 us, 154
+    // with 256 work-groups, 144 with 1,024)
     const int32_t toks = p.chunk_rows / G + 2;
     split_of(int64_t(p.chunk_tiles) * c->n_kv_heads, keys(most < toks ? most : toks), 512, 1024,
              1 << 30, s->q_off_h[s->n_seqs], p.chunk_split, p.chunk_splits);

@@ -324,6 +324,20 @@ def test_attention_of_many_requests(lens):
     within(fs.fs_paged_attention(step_of(lens, kv), on_gpu(k, v, table), q.cuda(), 0.1), want, tol, "out")
 
 
+@pytest.mark.parametrize("window", [0, 150])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_attention_of_many_rows_without_small_requests(dtype, window):
+    """Chunks alone, and so many heads that 256 rows share a tile of keys."""
+    g = gen(19 + window)
+    lens, kv = [261, 0, 77], [500, 9, 333]
+    k, v, table = make_cache(g, kv, 16, 128, 16, dtype)
+    q = normal(g, sum(lens), 256, 128, dtype=dtype)
+    q_off = offsets(lens)
+    want, tol, _, _ = ref.attention(q, k, v, table, q_off, kv, 0.09, window)
+    got = fs.fs_paged_attention(step_of(lens, kv), on_gpu(k, v, table), q.cuda(), 0.09, window=window)
+    within(got, want, tol, "out")
+
+
 @pytest.mark.parametrize("lens", [[1, 1, 1], [50, 1, 20]])
 def test_attention_offsets_beyond_32_bits_and_shared_pages(lens):
     g = gen(12)
