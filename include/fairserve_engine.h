@@ -80,7 +80,9 @@ fs_status fs_clear_status(int32_t *err, hipStream_t stream);
  * K, N, max_rank and the strides are multiples of 8, bases 16-byte aligned, max_rank <= 128,
  * K, N <= 2^20, x_stride <= 2^21,
  * n_adapters may be 0 (adapter is then not read).  Sums are held in fp32; scale * h enters the
- * second product as the sum of two dtype values (its rounding is below fp32's of the sum).
+ * second product as the sum of two dtype values (its rounding is below fp32's of the sum; in
+ * FS_F16 in units of a power of two of the row's own, so that it may exceed the type's range).
+ * What is not finite in one adapter reaches its own requests' rows alone.
  * ws: fs_adapter_workspace(s, ad) bytes, 256-byte aligned.  err: FS_E_RANGE for an
  * adapter outside [-1, n_adapters) or a rank outside [0, max_rank]. */
 typedef struct fs_adapters {

@@ -1,9 +1,9 @@
 // A projection with every request's own low-rank adapter beside the shared weight:
 //   y = x W^T + scale_a (x A_a^T) B_a^T,   a = the row's request's adapter.
 // Two launches.  k_shrink makes h = scale x A_a^T per request in fp32 and stores it as the
-// sum of two 16-bit values, with the row's adapter beside it.  The product then runs over
-// K and goes on over the few columns of h against B_a in the same accumulators, so y is
-// written once and never read:
+// sum of two 16-bit values (in half precision in units of a power of two of the row's own),
+// with the row's adapter and rank beside it.  The product then runs over K and goes on over
+// the few columns of h against B_a, so y is written once and never read:
 //   k_shrink       16 rows of one request a work-group; its waves share out K and join in
 //                  LDS.  Bound by the bytes of x where there are many rows (16,384 rows of
 //                  4,096: 134 MB in 38 us, 3.6 TB/s), by one tile's chain where there are few
@@ -32,7 +32,8 @@ struct LinArgs {
   const short *x, *w, *a, *b;
   short *y;
   short *h;         // [rows][2R]: high parts, low parts
-  int32_t *row_ad;  // [rows]: the row's adapter, -1 when it has none
+  int2 *row_ad;     // [rows up to a multiple of 16]: the row's adapter (-1: none), its rank
+  float *row_unit;  // [rows]: what h counts in (half precision; 1 in bfloat16)
   int64_t x_stride, y_stride;
   int32_t *err;
 };
@@ -142,13 +143,14 @@ template <bool BF, int JT, int WAVES, int STAGES>
 __global__ void __launch_bounds__(WAVES * 64) k_shrink(LinArgs g) {
   constexpr int LOADED = WAVES * STAGES * (1 + JT) * 16 * 64;
   __shared__ __align__(16) short lds[LOADED];
-  static_assert(LOADED >= WAVES * JT * 256 * 2, "room for the partial sums");
+  static_assert(LOADED >= WAVES * JT * 256 * 2 + 32, "room for the partial sums and `most`");
+  uint32_t *most = reinterpret_cast<uint32_t *>(lds + LOADED) - 16;  // rows' largest, as bits
   const RowTile t = row_tile<4>(g.q_off, g.n_seqs, blockIdx.x);
   if (t.rows <= 0) return;
   int32_t code = 0, rank;
   const int32_t ad = adapter_of(g, t.s, rank, code);
   if (threadIdx.x == 0) raise_err(g.err, code);
-  if (threadIdx.x < t.rows) g.row_ad[t.row0 + threadIdx.x] = rank > 0 ? ad : -1;
+  if (threadIdx.x < t.rows) g.row_ad[t.row0 + threadIdx.x] = {rank > 0 ? ad : -1, rank};
   if (ad < 0 || rank == 0) return;  // h of such rows is not looked at
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   f32x4 acc[1][JT] = {};
@@ -158,59 +160,83 @@ __global__ void __launch_bounds__(WAVES * 64) k_shrink(LinArgs g) {
   f32x4 *part = reinterpret_cast<f32x4 *>(lds);
 #pragma unroll
   for (int j = 0; j < JT; ++j) part[(wave * JT + j) * 64 + lane] = acc[0][j];
+  if (threadIdx.x < 16) most[threadIdx.x] = 0;
   __syncthreads();
   const float scale = g.scale ? __ldg(g.scale + ad) : 1.f;
-  for (int e = threadIdx.x; e < JT * 64; e += WAVES * 64) {
-    f32x4 v = part[e];
+  constexpr int PER = (JT + WAVES - 1) / WAVES;
+  f32x4 v[PER];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) v += part[w * JT * 64 + e];
-    const int row = e & 15, j0 = (e >> 4) * 4;
-    if (row >= t.rows || j0 >= g.R) continue;
+  for (int p = 0; p < PER; ++p) {
+    const int e = threadIdx.x + p * WAVES * 64, row = e & 15, j0 = (e >> 4) * 4;
+    if (e >= JT * 64) continue;
+    v[p] = part[e];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) v[p] += part[w * JT * 64 + e];
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[p][i] = j0 + i < rank ? v[p][i] * scale : 0.f;
+      m = fmaxf(m, fabsf(v[p][i]));
+    }
+    if (!BF) atomicMax(&most[row], __float_as_uint(m));
+  }
+  if (!BF) __syncthreads();
+#pragma unroll
+  for (int p = 0; p < PER; ++p) {
+    const int e = threadIdx.x + p * WAVES * 64, row = e & 15, j0 = (e >> 4) * 4;
+    if (e >= JT * 64 || row >= t.rows || j0 >= g.R) continue;
+    // half precision: a power of two brings the row's largest to between 2^14 and 2^15, so
+    // that none is beyond the range and the low parts are not below it
+    // (a unit of at least 2^-40: sums are divided by it)
+    const uint32_t top = BF ? 0 : most[row] >> 23, ex = top < 101 ? 101 : top;
+    const float up = BF || ex == 255 ? 1.f : __uint_as_float((268 - ex) << 23);
+    const float unit = BF || ex == 255 ? 1.f : __uint_as_float((ex - 14) << 23);
     s16x4 hi, lo;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float f = j0 + i < rank ? v[i] * scale : 0.f;
+      const float f = v[p][i] * up;
       hi[i] = to_16<BF>(f);
-      lo[i] = to_16<BF>(f - to_f32<BF>(hi[i]));
+      const float left = f - to_f32<BF>(hi[i]);
+      lo[i] = to_16<BF>(fabsf(left) < INFINITY ? left : 0.f);  // an infinite h has no low part
     }
     short *hp = g.h + int64_t(t.row0 + row) * (2 * g.R) + j0;
     *reinterpret_cast<s16x4 *>(hp) = hi;
     *reinterpret_cast<s16x4 *>(hp + g.R) = lo;
+    if (!BF && j0 == 0) g.row_unit[t.row0 + row] = unit;
   }
 }
 
-// B_a[n][j .. j + 7], columns at and beyond the rank as 0 (j at most R; loaded before the
-// rank is looked at, so that the two loads go side by side).
-__device__ inline s16x8 load_b(const LinArgs &g, int32_t ad, int32_t rank, int32_t n, int j) {
-  s16x8 v = *reinterpret_cast<const s16x8 *>(g.b + (int64_t(ad) * g.N + n) * g.R + min(j, g.R - 8));
+// B_a[n][j .. j + 7] (another place's at j = R), and 0 for its columns at and beyond the rank.
+__device__ inline s16x8 load_b(const LinArgs &g, int32_t ad, int32_t n, int j) {
+  return *reinterpret_cast<const s16x8 *>(g.b + (int64_t(ad) * g.N + n) * g.R + min(j, g.R - 8));
+}
+__device__ inline s16x8 within_rank(s16x8 v, int j, int32_t rank) {
   if (j + 8 > rank)
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = j + i < rank ? v[i] : short(0);
   return v;
 }
-__device__ inline int32_t rank_of(const LinArgs &g, int32_t ad) {
-  return g.rank ? min(__ldg(g.rank + ad), g.R) : g.R;
-}
-
 // ---- few rows: all of them, in MT tiles of 16, by NT tiles of 16 columns, four waves
 template <bool BF, int MT, int NT, int STAGES>
 __global__ void __launch_bounds__(256) k_linear_few(LinArgs g) {
   __shared__ __align__(16) short lds[4 * STAGES * (MT + NT) * 16 * 64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = lane & 15;
+  const int r = lane & 15, g4 = lane >> 4;
   const int n0 = blockIdx.x * (NT * 16);
   const s16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
   // the adapters of the tile of rows that this wave deals with
   const int my = wave % MT, my_row = my * 16 + r;
-  const int32_t ad = g.n_adapters > 0 && my_row < g.rows ? __ldg(g.row_ad + my_row) : -1;
+  const int2 ad = g.n_adapters > 0 && my_row < g.rows ? g.row_ad[my_row] : int2{-1, 0};
   f32x4 acc[MT][NT] = {};
   share_of_k<BF, MT, NT, 4, STAGES>(g.x, g.x_stride, g.rows, g.w + int64_t(n0) * g.K, g.N - n0,
                                     g.K, wave, lds, acc);
   // The distinct adapters of a tile's rows, shared out over the 4 / MT waves that hold the
-  // tile: four adapters' loads side by side, 4 chunks of 8 columns at a time (R/8 high
-  // ones, then R/8 low ones).
-  uint64_t left = __ballot(ad >= 0);
+  // tile.  Every row is multiplied with each of them and takes only its own one's result (a
+  // product of 0 with another adapter's infinity would be NaN): four adapters' loads side by side, WIDE times 4 chunks of 8 columns at a time (R/8
+  // high ones, then R/8 low ones).
+  uint64_t left = __ballot(ad.x >= 0);
   if (left) {
+    constexpr int WIDE = NT == 1 ? 2 : 1;
     const int chunks = g.R / 8;
     const short *hp = g.h + int64_t(min(my_row, g.rows - 1)) * (2 * g.R);
     f32x4 sum[NT] = {};
@@ -220,39 +246,64 @@ __global__ void __launch_bounds__(256) k_linear_few(LinArgs g) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         while (left) {
-          const int32_t a = __builtin_amdgcn_readlane(ad, __builtin_ctzll(left));
-          left &= ~__ballot(ad == a);
+          const int first = __builtin_ctzll(left);
+          const int32_t a = __builtin_amdgcn_readlane(ad.x, first);
+          left &= ~__ballot(ad.x == a);
           if (turn++ % (4 / MT) == wave / MT) {
             who[i] = a;
-            rank[i] = rank_of(g, a);
+            rank[i] = __builtin_amdgcn_readlane(ad.y, first);
             ++found;
             break;
           }
         }
       }
       if (found == 0) break;
-      for (int c = lane >> 4; c < (2 * chunks + 3) / 4 * 4; c += 4) {
-        const bool in = c < 2 * chunks;
-        const s16x8 hv = in ? *reinterpret_cast<const s16x8 *>(hp + c * 8) : zero;
-        const int j = in ? (c < chunks ? c : c - chunks) * 8 : g.R;
-        s16x8 bv[4][NT];
+      const short *bp[4][NT];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
-            bv[i][n] = load_b(g, max(who[i], 0), rank[i], min(n0 + n * 16 + r, g.N - 1), j);
+        for (int n = 0; n < NT; ++n) {
+          const int col = min(n0 + n * 16 + r, g.N - 1);
+          bp[i][n] = g.b + (int64_t(max(who[i], 0)) * g.N + col) * g.R;
+        }
+      f32x4 one[4][NT] = {};
+      for (int c0 = g4; c0 < (2 * chunks + 3) / 4 * 4; c0 += 4 * WIDE) {
+        s16x8 hv[WIDE], bv[WIDE][4][NT];
+        int j[WIDE];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int u = 0; u < WIDE; ++u) {
+          const int c = c0 + u * 4;
+          const bool in = c < 2 * chunks;
+          j[u] = in ? (c < chunks ? c : c - chunks) * 8 : g.R;
+          hv[u] = *reinterpret_cast<const s16x8 *>(hp + (in ? c : 0) * 8);
+          hv[u] = in ? hv[u] : zero;
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
-            sum[n] = mfma_16x16x32<BF>(bv[i][n], ad >= 0 && ad == who[i] ? hv : zero, sum[n]);
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+              bv[u][i][n] = *reinterpret_cast<const s16x8 *>(bp[i][n] + min(j[u], g.R - 8));
+        }
+#pragma unroll
+        for (int u = 0; u < WIDE; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+              one[i][n] =
+                  mfma_16x16x32<BF>(within_rank(bv[u][i][n], j[u], rank[i]), hv[u], one[i][n]);
       }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          if (ad.x >= 0 && ad.x == who[i]) sum[n] += one[i][n];
     }
+    const float unit = !BF && ad.x >= 0 ? g.row_unit[my_row] : 1.f;
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int n = 0; n < NT; ++n)
-        if (m == my) acc[m][n] += sum[n];
+        if (m == my) acc[m][n] += sum[n] * unit;
   }
   __syncthreads();
   f32x4 *part = reinterpret_cast<f32x4 *>(lds);
@@ -275,10 +326,41 @@ __global__ void __launch_bounds__(256) k_linear_few(LinArgs g) {
   }
 }
 
+// The distinct adapters of a wave's 32 rows in steps of two chunks of 8 columns (R/8 chunks of
+// h's high parts, then R/8 of its low ones).
+struct Steps {
+  int2 ad;        // the lane's row's adapter and rank
+  uint64_t left;  // lanes whose adapter is still to come
+  int each, at;   // an adapter's steps, the next one
+  int32_t who = -1, rank = 0;
+  __device__ Steps(const LinArgs &g, int2 row_ad) : ad(row_ad) {
+    left = __ballot(ad.x >= 0);
+    each = at = g.R / 8;
+  }
+  __device__ bool done() const { return at == each && !left; }
+  // The next step's adapter (-1, at step 0: none is left), its step and its rank.
+  __device__ int32_t next(int &step, int32_t &its_rank) {
+    if (at == each) {
+      who = -1;
+      if (left) {
+        const int first = __builtin_ctzll(left);
+        who = __builtin_amdgcn_readlane(ad.x, first);
+        rank = __builtin_amdgcn_readlane(ad.y, first);
+        left &= ~__ballot(ad.x == who);
+        at = 0;
+      }
+    }
+    step = who < 0 ? 0 : at;
+    its_rank = rank;
+    at += who >= 0;
+    return who;
+  }
+};
+
 // ---- many rows: BM rows by BN columns a work-group, K in steps of BK through STAGES LDS
 // buffers that are filled STAGES - 1 steps ahead; a wave takes WM rows by WN columns.
 template <bool BF, int BM, int BN, int WM, int WN, int BK, int STAGES>
-__global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) k_linear_tile(LinArgs g) {
+__global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) k_linear_tile(LinArgs g) {
   constexpr int WAVES = (BM / WM) * (BN / WN);
   constexpr int MT = WM / 32, NT = WN / 32;
   constexpr int CH = BK / 8, RW = 64 / CH;  // chunks of a row, rows of a wave's load
@@ -315,11 +397,11 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) k_linear_tile(LinA
     wc[i] = place_of<BK>(r, lane % CH) * 8;
     wo[i] = uint32_t((min(n0 + r, g.N - 1) - n0) * g.K + wc[i]) * 2;
   }
-  int32_t ad[MT];
+  int2 ad[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     const int row = m0 + wm + m * 32 + r32;
-    ad[m] = g.n_adapters > 0 && row < g.rows ? __ldg(g.row_ad + row) : -1;
+    ad[m] = g.n_adapters > 0 && row < g.rows ? g.row_ad[row] : int2{-1, 0};
   }
   const short *x0 = g.x + int64_t(m0) * g.x_stride, *w0 = g.w + int64_t(n0) * g.K;
   const uint32_t xs_at = lds_address(&xs[0][wave * LX * RW * BK]),
@@ -400,52 +482,67 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) k_linear_tile(LinA
     wait_loads<0>();
     multiply(step, step < full, [] {});
   }
-  const s16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
-  // The distinct adapters of a tile's rows, two at a time: the loads of both, and of two
-  // chunks of 8 columns (R/8 high ones, then R/8 low ones), go side by side.
   const int chunks = g.R / 8;
+  constexpr int UNITS = MT * NT == 1 ? 4 : 2;  // steps whose loads go side by side
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     const int row = m0 + wm + m * 32 + r32;
     const short *hp = g.h + int64_t(min(row, g.rows - 1)) * (2 * g.R);
-    uint64_t left = __ballot(ad[m] >= 0);
-    while (left) {
-      int32_t who[2] = {-1, -1}, rank[2] = {0, 0};
+    Steps adapters(g, ad[m]);
+    if (!adapters.left) continue;
+    const float unit = !BF && ad[m].x >= 0 ? g.row_unit[row] : 1.f;
+    int32_t who[UNITS], rank[UNITS];
+    int at[UNITS], j[UNITS];
+    s16x8 hv[UNITS], bv[UNITS][NT];
+    auto fetch = [&] {
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-        if (left) {
-          who[i] = __builtin_amdgcn_readlane(ad[m], __builtin_ctzll(left));
-          left &= ~__ballot(ad[m] == who[i]);
-          rank[i] = rank_of(g, who[i]);
-        }
-      for (int c0 = h2; c0 < 2 * chunks; c0 += 4) {
-        s16x8 hv[2], bv[2][2][NT];
-        int j[2];
+      for (int i = 0; i < UNITS; ++i) who[i] = adapters.next(at[i], rank[i]);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int c = c0 + u * 2;
-          const bool in = c < 2 * chunks;
-          hv[u] = in ? *reinterpret_cast<const s16x8 *>(hp + c * 8) : zero;
-          j[u] = in ? (c < chunks ? c : c - chunks) * 8 : g.R;
-        }
+      for (int i = 0; i < UNITS; ++i) {
+        const int c = at[i] * 2 + h2;
+        hv[i] = *reinterpret_cast<const s16x8 *>(hp + c * 8);
+        j[i] = (c < chunks ? c : c - chunks) * 8;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int n = 0; n < NT; ++n)
+          bv[i][n] = load_b(g, max(who[i], 0), min(n0 + wn + n * 32 + r32, g.N - 1), j[i]);
+      }
+    };
+    const int32_t first = __builtin_amdgcn_readlane(ad[m].x, __builtin_ctzll(adapters.left));
+    if (__all(ad[m].x == first || row >= g.rows)) {  // all in one sum
+      if (!BF)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[m][n] *= 1.f / unit;
+      while (!adapters.done()) {
+        fetch();
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i)
           if (who[i] >= 0)
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int n = 0; n < NT; ++n)
+              acc[m][n] =
+                  mfma_32x32x16<BF>(within_rank(bv[i][n], j[i], rank[i]), hv[i], acc[m][n]);
+      }
+      if (!BF)
 #pragma unroll
-              for (int n = 0; n < NT; ++n)
-                bv[i][u][n] =
-                    load_b(g, who[i], rank[i], min(n0 + wn + n * 32 + r32, g.N - 1), j[u]);
+        for (int n = 0; n < NT; ++n) acc[m][n] *= unit;
+      continue;
+    }
+    // every row with each adapter; it takes only its own one's result
+    f32x16 one[NT] = {};
+    while (!adapters.done()) {
+      fetch();
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          if (who[i] >= 0)
+      for (int i = 0; i < UNITS; ++i) {
+        if (who[i] < 0) continue;
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+        for (int n = 0; n < NT; ++n)
+          one[n] = mfma_32x32x16<BF>(within_rank(bv[i][n], j[i], rank[i]), hv[i], one[n]);
+        if (at[i] + 1 < adapters.each) continue;
 #pragma unroll
-              for (int n = 0; n < NT; ++n)
-                acc[m][n] =
-                    mfma_32x32x16<BF>(bv[i][u][n], ad[m] == who[i] ? hv[u] : zero, acc[m][n]);
+        for (int n = 0; n < NT; ++n) {
+          if (ad[m].x == who[i]) acc[m][n] += one[n] * unit;
+          one[n] = f32x16{};
+        }
       }
     }
   }
@@ -547,7 +644,8 @@ void run(const LinArgs &g, const fs_step *st, hipStream_t stream) {
 
 size_t adapter_workspace_bytes(const fs_step *s, const fs_adapters *ad) {
   if (ad->n_adapters == 0) return 0;
-  return size_t(s->q_off_h[s->n_seqs]) * (ad->max_rank + 1) * 4;
+  const size_t rows = s->q_off_h[s->n_seqs], whole = (rows + 15) / 16 * 16;
+  return rows * ad->max_rank * 4 + whole * 8 + (ad->dtype == FS_F16 ? rows * 4 : 0);
 }
 
 hipError_t launch_adapter_linear(const fs_step *s, const fs_adapters *ad, const void *x,
@@ -570,7 +668,8 @@ hipError_t launch_adapter_linear(const fs_step *s, const fs_adapters *ad, const 
   g.b = static_cast<const short *>(ad->b);
   g.y = static_cast<short *>(y);
   g.h = static_cast<short *>(ws);
-  g.row_ad = static_cast<int32_t *>(ws) + size_t(g.rows) * g.R;
+  g.row_ad = reinterpret_cast<int2 *>(g.h + size_t(g.rows) * g.R * 2);
+  g.row_unit = reinterpret_cast<float *>(g.row_ad + (size_t(g.rows) + 15) / 16 * 16);
   g.x_stride = x_stride;
   g.y_stride = y_stride;
   g.err = err;

@@ -98,6 +98,51 @@ def test_linear_few_rows_many_columns(rows, N):
     within(fs.fs_adapter_linear(fs.Step(q_off), ad, x.cuda(), w.cuda()), want, bound, "y")
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows,N", [(1, 64), (20, 136), (50, 9000), (130, 520), (1200, 2056), (5000, 4000)])
+def test_linear_of_a_broken_adapter_is_its_own(rows, N, dtype):
+    """Infinities and NaN in one adapter reach the rows of its requests alone."""
+    g = gen(rows + N)
+    K, R = 72, 24
+    lens = [1] * min(rows, 40) + ([rows - 40] if rows > 40 else [])
+    q_off = offsets(lens)
+    x, w = normal(g, rows, K, dtype=dtype), normal(g, N, K, dtype=dtype, std=K ** -0.5)
+    a, b = normal(g, 5, R, K, dtype=dtype, std=K ** -0.5), normal(g, 5, N, R, dtype=dtype)
+    adapter = torch.randint(-1, 5, (len(lens),), generator=g, dtype=torch.int32)
+    whole = fs.fs_adapter_linear(fs.Step(q_off), fs.Adapters(a.cuda(), b.cuda(), adapter.cuda()),
+                                 x.cuda(), w.cuda())
+    assert bool(torch.isfinite(whole).all())
+    bad_a, bad_b = a.clone(), b.clone()
+    bad_a[0, 3], bad_b[1], bad_b[2, :, 5] = math.inf, math.nan, -math.inf
+    bad = fs.Adapters(bad_a.cuda(), bad_b.cuda(), adapter.cuda())
+    y = fs.fs_adapter_linear(fs.Step(q_off), bad, x.cuda(), w.cuda())
+    for s in range(len(lens)):
+        rows_s = slice(q_off[s], q_off[s + 1])
+        if int(adapter[s]) in (0, 1, 2):
+            assert not bool(torch.isfinite(y[rows_s]).any()), s
+        else:
+            assert torch.equal(y[rows_s], whole[rows_s]), s
+
+
+@pytest.mark.parametrize("size", [3e-5, 1e-2, 3e3])
+@pytest.mark.parametrize("rows", [3, 200])
+def test_linear_half_precision_beyond_its_range(rows, size):
+    """x a^T from far below half precision's smallest numbers to far above its largest."""
+    g = gen(rows)
+    K, N, R = 512, 136, 16
+    q_off = [0, 1, rows]
+    x = normal(g, rows, K, dtype=HF, std=size)
+    a = (normal(g, 2, R, K).abs() + 1).to(HF) * min(size, 10)
+    b = normal(g, 2, N, R, dtype=HF, std=1e-4 if size > 1 else 1.0)
+    w = torch.zeros(N, K, dtype=HF)
+    x[:, :300] = x[:, :300].abs()
+    adapter = torch.tensor([1, 0], dtype=torch.int32)
+    want, bound = ref.linear(x, w, a, b, q_off, adapter)
+    y = fs.fs_adapter_linear(fs.Step(q_off), fs.Adapters(a.cuda(), b.cuda(), adapter.cuda()),
+                             x.cuda(), w.cuda())
+    within(y, want, bound, "y")
+
+
 def test_linear_without_adapters_and_defaults():
     g = gen(5)
     lens, K, N = [5, 1, 70], 128, 200
