@@ -232,8 +232,9 @@ __global__ void __launch_bounds__(256) k_linear_few(LinArgs g) {
                                     g.K, wave, lds, acc);
   // The distinct adapters of a tile's rows, shared out over the 4 / MT waves that hold the
   // tile.  Every row is multiplied with each of them and takes only its own one's result (a
-  // product of 0 with another adapter's infinity would be NaN): four adapters' loads side by side, WIDE times 4 chunks of 8 columns at a time (R/8
-  // high ones, then R/8 low ones).
+  // product of 0 with another adapter's infinity would be NaN).  Four adapters' loads go side
+  // by side, for WIDE times 4 chunks of 8 columns (R/8 high ones, then R/8 low ones): 3 us of
+  // 20 at 64 rows of 8 adapters of rank 16, 9 at rank 64.
   uint64_t left = __ballot(ad.x >= 0);
   if (left) {
     constexpr int WIDE = NT == 1 ? 2 : 1;
