@@ -66,9 +66,10 @@ __device__ inline int place_of(int r, int c) {
 // w.  The waves take 64 of K in turn, each through STAGES buffers of its own that are filled
 // STAGES - 1 steps ahead, so they never wait for each other.  (Straight from memory in the
 // matrix cores' layout, 16 lanes would touch 16 rows: a quarter of the cache's rate.)
-template <bool BF, int MT, int NT, int WAVES, int STAGES>
+// `meanwhile` runs once the first loads are under way.
+template <bool BF, int MT, int NT, int WAVES, int STAGES, class F>
 __device__ void share_of_k(const short *x, int64_t x_stride, int x_rows, const short *w, int w_rows,
-                           int K, int wave, short *lds, f32x4 (&acc)[MT][NT]) {
+                           int K, int wave, short *lds, f32x4 (&acc)[MT][NT], F meanwhile) {
   constexpr int TILE = 16 * 64, STEP = (MT + NT) * TILE, LOADS = 2 * (MT + NT);
   const int lane = threadIdx.x & 63, r16 = lane & 15, g4 = lane >> 4;
   short *mine = lds + wave * (STAGES * STEP);
@@ -124,6 +125,7 @@ __device__ void share_of_k(const short *x, int64_t x_stride, int x_rows, const s
 #pragma unroll
   for (int t = 0; t < STAGES - 1; ++t)
     if (t < n) issue(t);
+  meanwhile();
   int t = 0;
   for (; t + STAGES - 1 < n; ++t) {
     reads_done();
@@ -155,7 +157,8 @@ __global__ void __launch_bounds__(WAVES * 64) k_shrink(LinArgs g) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   f32x4 acc[1][JT] = {};
   share_of_k<BF, 1, JT, WAVES, STAGES>(g.x + int64_t(t.row0) * g.x_stride, g.x_stride, t.rows,
-                                        g.a + int64_t(ad) * g.R * g.K, rank, g.K, wave, lds, acc);
+                                       g.a + int64_t(ad) * g.R * g.K, rank, g.K, wave, lds, acc,
+                                       [] {});
   __syncthreads();
   f32x4 *part = reinterpret_cast<f32x4 *>(lds);
 #pragma unroll
@@ -228,84 +231,87 @@ __global__ void __launch_bounds__(256) k_linear_few(LinArgs g) {
   const int my = wave % MT, my_row = my * 16 + r;
   const int2 ad = g.n_adapters > 0 && my_row < g.rows ? g.row_ad[my_row] : int2{-1, 0};
   f32x4 acc[MT][NT] = {};
-  share_of_k<BF, MT, NT, 4, STAGES>(g.x, g.x_stride, g.rows, g.w + int64_t(n0) * g.K, g.N - n0,
-                                    g.K, wave, lds, acc);
   // The distinct adapters of a tile's rows, shared out over the 4 / MT waves that hold the
-  // tile.  Every row is multiplied with each of them and takes only its own one's result (a
-  // product of 0 with another adapter's infinity would be NaN).  Four adapters' loads go side
-  // by side, for WIDE times 4 chunks of 8 columns (R/8 high ones, then R/8 low ones): 3 us of
-  // 20 at 64 rows of 8 adapters of rank 16, 9 at rank 64.
-  uint64_t left = __ballot(ad.x >= 0);
-  if (left) {
-    constexpr int WIDE = NT == 1 ? 2 : 1;
-    const int chunks = g.R / 8;
-    const short *hp = g.h + int64_t(min(my_row, g.rows - 1)) * (2 * g.R);
-    f32x4 sum[NT] = {};
-    for (int turn = 0; left;) {
-      int32_t who[4] = {-1, -1, -1, -1}, rank[4] = {0, 0, 0, 0};
-      int found = 0;
+  // tile, while the first loads for the product over K are under way.  Every row is multiplied
+  // with each of them and takes only its own one's result (a product of 0 with another
+  // adapter's infinity would be NaN).  Four adapters' loads go side by side, for WIDE times 4
+  // chunks of 8 columns (R/8 high ones, then R/8 low ones): 3 us of 20 at 64 rows of 8
+  // adapters of rank 16, 9 at rank 64.
+  auto adapters = [&] {
+    uint64_t left = __ballot(ad.x >= 0);
+    if (left) {
+      constexpr int WIDE = NT == 1 ? 2 : 1;
+      const int chunks = g.R / 8;
+      const short *hp = g.h + int64_t(min(my_row, g.rows - 1)) * (2 * g.R);
+      f32x4 sum[NT] = {};
+      for (int turn = 0; left;) {
+        int32_t who[4] = {-1, -1, -1, -1}, rank[4] = {0, 0, 0, 0};
+        int found = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        while (left) {
-          const int first = __builtin_ctzll(left);
-          const int32_t a = __builtin_amdgcn_readlane(ad.x, first);
-          left &= ~__ballot(ad.x == a);
-          if (turn++ % (4 / MT) == wave / MT) {
-            who[i] = a;
-            rank[i] = __builtin_amdgcn_readlane(ad.y, first);
-            ++found;
-            break;
+        for (int i = 0; i < 4; ++i) {
+          while (left) {
+            const int first = __builtin_ctzll(left);
+            const int32_t a = __builtin_amdgcn_readlane(ad.x, first);
+            left &= ~__ballot(ad.x == a);
+            if (turn++ % (4 / MT) == wave / MT) {
+              who[i] = a;
+              rank[i] = __builtin_amdgcn_readlane(ad.y, first);
+              ++found;
+              break;
+            }
           }
         }
-      }
-      if (found == 0) break;
-      const short *bp[4][NT];
+        if (found == 0) break;
+        const short *bp[4][NT];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const int col = min(n0 + n * 16 + r, g.N - 1);
-          bp[i][n] = g.b + (int64_t(max(who[i], 0)) * g.N + col) * g.R;
+          for (int n = 0; n < NT; ++n) {
+            const int col = min(n0 + n * 16 + r, g.N - 1);
+            bp[i][n] = g.b + (int64_t(max(who[i], 0)) * g.N + col) * g.R;
+          }
+        f32x4 one[4][NT] = {};
+        for (int c0 = g4; c0 < (2 * chunks + 3) / 4 * 4; c0 += 4 * WIDE) {
+          s16x8 hv[WIDE], bv[WIDE][4][NT];
+          int j[WIDE];
+#pragma unroll
+          for (int u = 0; u < WIDE; ++u) {
+            const int c = c0 + u * 4;
+            const bool in = c < 2 * chunks;
+            j[u] = in ? (c < chunks ? c : c - chunks) * 8 : g.R;
+            hv[u] = *reinterpret_cast<const s16x8 *>(hp + (in ? c : 0) * 8);
+            hv[u] = in ? hv[u] : zero;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int n = 0; n < NT; ++n)
+                bv[u][i][n] = *reinterpret_cast<const s16x8 *>(bp[i][n] + min(j[u], g.R - 8));
+          }
+#pragma unroll
+          for (int u = 0; u < WIDE; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int n = 0; n < NT; ++n)
+                one[i][n] =
+                    mfma_16x16x32<BF>(within_rank(bv[u][i][n], j[u], rank[i]), hv[u], one[i][n]);
         }
-      f32x4 one[4][NT] = {};
-      for (int c0 = g4; c0 < (2 * chunks + 3) / 4 * 4; c0 += 4 * WIDE) {
-        s16x8 hv[WIDE], bv[WIDE][4][NT];
-        int j[WIDE];
 #pragma unroll
-        for (int u = 0; u < WIDE; ++u) {
-          const int c = c0 + u * 4;
-          const bool in = c < 2 * chunks;
-          j[u] = in ? (c < chunks ? c : c - chunks) * 8 : g.R;
-          hv[u] = *reinterpret_cast<const s16x8 *>(hp + (in ? c : 0) * 8);
-          hv[u] = in ? hv[u] : zero;
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-              bv[u][i][n] = *reinterpret_cast<const s16x8 *>(bp[i][n] + min(j[u], g.R - 8));
-        }
-#pragma unroll
-        for (int u = 0; u < WIDE; ++u)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-              one[i][n] =
-                  mfma_16x16x32<BF>(within_rank(bv[u][i][n], j[u], rank[i]), hv[u], one[i][n]);
+          for (int n = 0; n < NT; ++n)
+            if (ad.x >= 0 && ad.x == who[i]) sum[n] += one[i][n];
       }
+      const float unit = !BF && ad.x >= 0 ? g.row_unit[my_row] : 1.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-          if (ad.x >= 0 && ad.x == who[i]) sum[n] += one[i][n];
+          if (m == my) acc[m][n] += sum[n] * unit;
     }
-    const float unit = !BF && ad.x >= 0 ? g.row_unit[my_row] : 1.f;
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-        if (m == my) acc[m][n] += sum[n] * unit;
-  }
+  };
+  share_of_k<BF, MT, NT, 4, STAGES>(g.x, g.x_stride, g.rows, g.w + int64_t(n0) * g.K, g.N - n0,
+                                    g.K, wave, lds, acc, adapters);
   __syncthreads();
   f32x4 *part = reinterpret_cast<f32x4 *>(lds);
 #pragma unroll
