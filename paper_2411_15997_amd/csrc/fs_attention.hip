@@ -750,12 +750,15 @@ void run(const AttnArgs &a, const Plan &p, hipStream_t stream) {
   const int few = p.few_seqs > 0 ? a.n_seqs * a.c.n_kv_heads * p.few_splits : 0;
   const int tiles = p.chunk_tiles * a.c.n_kv_heads;
   const int chunk = p.chunk_seqs > 0 ? tiles * p.chunk_splits : 0;
+  // In one launch where one kernel holds both without spilling registers.
+  const bool mixed = few > 0 && chunk > 0 && p.chunk_rows == 128 && (D == 64 || p.few_rows <= 32);
   auto by_rows = [&](auto nt) {
     constexpr int NT = decltype(nt)::value;
-    if (few > 0 && chunk > 0 && p.chunk_rows == 128)
-      hipLaunchKernelGGL((k_attn_mixed<BF, D, NT>), dim3(chunk + few), block, 0, stream, a, chunk,
-                         tiles);
-    else if (few > 0)
+    if constexpr (D == 64 || NT <= 2)
+      if (mixed)
+        hipLaunchKernelGGL((k_attn_mixed<BF, D, NT>), dim3(chunk + few), block, 0, stream, a, chunk,
+                           tiles);
+    if (few > 0 && !mixed)
       hipLaunchKernelGGL((k_attn_few<BF, D, NT>), dim3(few), block, 0, stream, a);
   };
   if (p.few_rows <= 16)
@@ -764,12 +767,12 @@ void run(const AttnArgs &a, const Plan &p, hipStream_t stream) {
     by_rows(std::integral_constant<int, 2>());
   else
     by_rows(std::integral_constant<int, 4>());
-  if (chunk > 0) {
+  if (chunk > 0 && !mixed) {
     const dim3 grid(tiles, p.chunk_splits);
     if constexpr (D == 128)
       if (p.chunk_rows == 256)
         hipLaunchKernelGGL((k_attn_chunk<BF, D, 8>), grid, dim3(512), 0, stream, a);
-    if (few == 0 && p.chunk_rows == 128)
+    if (p.chunk_rows == 128)
       hipLaunchKernelGGL((k_attn_chunk<BF, D, 4>), grid, block, 0, stream, a);
   }
   if (p.few_splits > 1)
