@@ -32,8 +32,9 @@ struct LinArgs {
   const short *x, *w, *a, *b;
   short *y;
   short *h;         // [rows][2R]: high parts, low parts
-  int2 *row_ad;     // [rows up to a multiple of 16]: the row's adapter (-1: none), its rank
-  float *row_unit;  // [rows]: what h counts in (half precision; 1 in bfloat16)
+  // [rows up to a multiple of 16]: the row's adapter (-1: none); its rank, and from bit 8 on
+  // the exponent of what h counts in (half precision; 1 in bfloat16)
+  int2 *row_ad;
   int64_t x_stride, y_stride;
   int32_t *err;
 };
@@ -152,8 +153,10 @@ __global__ void __launch_bounds__(WAVES * 64) k_shrink(LinArgs g) {
   int32_t code = 0, rank;
   const int32_t ad = adapter_of(g, t.s, rank, code);
   if (threadIdx.x == 0) raise_err(g.err, code);
-  if (threadIdx.x < t.rows) g.row_ad[t.row0 + threadIdx.x] = {rank > 0 ? ad : -1, rank};
-  if (ad < 0 || rank == 0) return;  // h of such rows is not looked at
+  if (ad < 0 || rank == 0) {  // h of such rows is not looked at
+    if (threadIdx.x < t.rows) g.row_ad[t.row0 + threadIdx.x] = {-1, 0};
+    return;
+  }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   f32x4 acc[1][JT] = {};
   share_of_k<BF, 1, JT, WAVES, STAGES>(g.x + int64_t(t.row0) * g.x_stride, g.x_stride, t.rows,
@@ -193,7 +196,7 @@ __global__ void __launch_bounds__(WAVES * 64) k_shrink(LinArgs g) {
     // (a unit of at least 2^-40: sums are divided by it)
     const uint32_t top = BF ? 0 : most[row] >> 23, ex = top < 101 ? 101 : top;
     const float up = BF || ex == 255 ? 1.f : __uint_as_float((268 - ex) << 23);
-    const float unit = BF || ex == 255 ? 1.f : __uint_as_float((ex - 14) << 23);
+    const uint32_t unit = BF || ex == 255 ? 127 : ex - 14;
     s16x4 hi, lo;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -205,9 +208,12 @@ __global__ void __launch_bounds__(WAVES * 64) k_shrink(LinArgs g) {
     short *hp = g.h + int64_t(t.row0 + row) * (2 * g.R) + j0;
     *reinterpret_cast<s16x4 *>(hp) = hi;
     *reinterpret_cast<s16x4 *>(hp + g.R) = lo;
-    if (!BF && j0 == 0) g.row_unit[t.row0 + row] = unit;
+    if (j0 == 0) g.row_ad[t.row0 + row] = {ad, int32_t(rank | unit << 8)};
   }
 }
+
+__device__ inline int32_t rank_in(int32_t packed) { return packed & 255; }
+__device__ inline float unit_in(int32_t packed) { return __uint_as_float(packed >> 8 << 23); }
 
 // B_a[n][j .. j + 7] (another place's at j = R), and 0 for its columns at and beyond the rank.
 __device__ inline s16x8 load_b(const LinArgs &g, int32_t ad, int32_t n, int j) {
@@ -255,7 +261,7 @@ __global__ void __launch_bounds__(256) k_linear_few(LinArgs g) {
             left &= ~__ballot(ad.x == a);
             if (turn++ % (4 / MT) == wave / MT) {
               who[i] = a;
-              rank[i] = __builtin_amdgcn_readlane(ad.y, first);
+              rank[i] = rank_in(__builtin_amdgcn_readlane(ad.y, first));
               ++found;
               break;
             }
@@ -302,7 +308,7 @@ __global__ void __launch_bounds__(256) k_linear_few(LinArgs g) {
           for (int n = 0; n < NT; ++n)
             if (ad.x >= 0 && ad.x == who[i]) sum[n] += one[i][n];
       }
-      const float unit = !BF && ad.x >= 0 ? g.row_unit[my_row] : 1.f;
+      const float unit = !BF && ad.x >= 0 ? unit_in(ad.y) : 1.f;
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -352,7 +358,7 @@ struct Steps {
       if (left) {
         const int first = __builtin_ctzll(left);
         who = __builtin_amdgcn_readlane(ad.x, first);
-        rank = __builtin_amdgcn_readlane(ad.y, first);
+        rank = rank_in(__builtin_amdgcn_readlane(ad.y, first));
         left &= ~__ballot(ad.x == who);
         at = 0;
       }
@@ -497,7 +503,7 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) k_linear_tile(L
     const short *hp = g.h + int64_t(min(row, g.rows - 1)) * (2 * g.R);
     Steps adapters(g, ad[m]);
     if (!adapters.left) continue;
-    const float unit = !BF && ad[m].x >= 0 ? g.row_unit[row] : 1.f;
+    const float unit = !BF && ad[m].x >= 0 ? unit_in(ad[m].y) : 1.f;
     int32_t who[UNITS], rank[UNITS];
     int at[UNITS], j[UNITS];
     s16x8 hv[UNITS], bv[UNITS][NT];
@@ -652,7 +658,7 @@ void run(const LinArgs &g, const fs_step *st, hipStream_t stream) {
 size_t adapter_workspace_bytes(const fs_step *s, const fs_adapters *ad) {
   if (ad->n_adapters == 0) return 0;
   const size_t rows = s->q_off_h[s->n_seqs], whole = (rows + 15) / 16 * 16;
-  return rows * ad->max_rank * 4 + whole * 8 + (ad->dtype == FS_F16 ? rows * 4 : 0);
+  return rows * ad->max_rank * 4 + whole * 8;
 }
 
 hipError_t launch_adapter_linear(const fs_step *s, const fs_adapters *ad, const void *x,
@@ -676,7 +682,6 @@ hipError_t launch_adapter_linear(const fs_step *s, const fs_adapters *ad, const 
   g.y = static_cast<short *>(y);
   g.h = static_cast<short *>(ws);
   g.row_ad = reinterpret_cast<int2 *>(g.h + size_t(g.rows) * g.R * 2);
-  g.row_unit = reinterpret_cast<float *>(g.row_ad + (size_t(g.rows) + 15) / 16 * 16);
   g.x_stride = x_stride;
   g.y_stride = y_stride;
   g.err = err;
