@@ -640,15 +640,25 @@ void run(const LinArgs &g, const fs_step *st, hipStream_t stream) {
   }
   // The largest tiles that still occupy three quarters of the compute units (K = 4,096: 1,024
   // tiles of 256 take 516 us, of 128 587 and of 64 902; 2,048 rows by 4,096 columns, 128 tiles
-  // of 256, 106, 75 and 114 us; K = 2,048, 500 rows by 2,560 columns: - , 34.0 and 22.7).
+  // of 256, 106, 75 and 114 us; K = 2,048, 500 rows by 2,560 columns: - , 34.0 and 22.7,
+  // and 1,000 rows 34.7 with 64 and 32.2 with 128 by 96).
   auto tiles = [&](int64_t t) { return ((g.rows + t - 1) / t) * ((g.N + t - 1) / t); };
+  const int64_t narrow = (g.rows + 127) / 128 * int64_t((g.N + 95) / 96);  // of 128 by 96
   if (tiles(256) >= 192)
     hipLaunchKernelGGL((k_linear_tile<BF, 256, 256, 128, 64, 64, 2>), dim3(tiles(256)), dim3(512),
                        0, stream, g);
-  else if (tiles(128) >= 192)
-    hipLaunchKernelGGL((k_linear_tile<BF, 128, 128, 64, 64, 64, 2>), dim3(tiles(128)), dim3(256), 0,
-                       stream, g);
-  else
+  else if (narrow >= 192) {
+    // 96 columns for 128 where that takes no more rounds of two work-groups a compute unit, or
+    // few enough (a round of theirs takes 0.9 of the other's time a column: K = 2,048, 1,999
+    // rows by 2,560 columns 39.7 and 42.3 us; K = N = 4,096: 1,500 rows 98 and 68.5, 2,500 107
+    // and 115.5)
+    if ((narrow + 511) / 512 * 115 < (tiles(128) + 511) / 512 * 128)
+      hipLaunchKernelGGL((k_linear_tile<BF, 128, 96, 32, 96, 64, 2>), dim3(narrow), dim3(256), 0,
+                         stream, g);
+    else
+      hipLaunchKernelGGL((k_linear_tile<BF, 128, 128, 64, 64, 64, 2>), dim3(tiles(128)), dim3(256),
+                         0, stream, g);
+  } else
     hipLaunchKernelGGL((k_linear_tile<BF, 64, 64, 32, 32, 64, 4>), dim3(tiles(64)), dim3(256), 0,
                        stream, g);
 }

@@ -143,6 +143,19 @@ def test_linear_half_precision_beyond_its_range(rows, size):
     within(y, want, bound, "y")
 
 
+@pytest.mark.parametrize("lens,N", [([700, 1, 1297], 2568), ([1400, 150], 4096), ([2000, 501], 4104)])
+def test_linear_tiles_of_the_middle(lens, N):
+    """Row and column counts whose tiles are 128 rows by 96 or 128 columns."""
+    g = gen(N)
+    K, q_off, T = 200, offsets(lens), sum(lens)
+    x, w = normal(g, T, K, dtype=HF), normal(g, N, K, dtype=HF, std=K ** -0.5)
+    a, b = normal(g, 2, 8, K, dtype=HF, std=K ** -0.5), normal(g, 2, N, 8, dtype=HF)
+    adapter = torch.tensor([1, -1, 0][:len(lens)], dtype=torch.int32)
+    want, bound = ref.linear(x, w, a, b, q_off, adapter)
+    ad = fs.Adapters(a.cuda(), b.cuda(), adapter.cuda())
+    within(fs.fs_adapter_linear(fs.Step(q_off), ad, x.cuda(), w.cuda()), want, bound, "y")
+
+
 def test_linear_without_adapters_and_defaults():
     g = gen(5)
     lens, K, N = [5, 1, 70], 128, 200
