@@ -14,7 +14,7 @@
 //                  and join in LDS.
 //   k_linear_tile  more rows: bound by the matrix cores and LDS together.  W and x go through
 //                  LDS in tiles (16,384 x 4,096 x 4,096: 470 to 490 us and the shrink's 38,
-//                  1.1 PFLOP/s, the matrix cores busy for 58 % of the cycles; its loads alone
+//                  1.1 PFLOP/s, the matrix cores busy for 63 % of the cycles; its loads alone
 //                  take 404 us, its products alone 419).  Eight waves with tiles of 128 x 64
 //                  each read LDS least for a product.
 // W is the first operand (its rows are y's columns), so a lane holds neighbouring columns
@@ -649,7 +649,7 @@ void run(const LinArgs &g, const fs_step *st, hipStream_t stream) {
                        0, stream, g);
   else if (narrow >= 192) {
     // 96 columns for 128 where that takes no more rounds of two work-groups a compute unit, or
-    // few enough (a round of theirs takes 0.9 of the other's time a column: K = 2,048, 1,999
+    // few enough (a round of them takes 0.9 of the time of one of the others: K = 2,048, 1,999
     // rows by 2,560 columns 39.7 and 42.3 us; K = N = 4,096: 1,500 rows 98 and 68.5, 2,500 107
     // and 115.5)
     if ((narrow + 511) / 512 * 115 < (tiles(128) + 511) / 512 * 128)
