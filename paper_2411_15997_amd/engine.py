@@ -53,8 +53,7 @@ class fs_sampling(C.Structure):
 
 def signatures():
     P, I32, I64, SZ, F, D = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t, C.c_float, C.c_double
-    S, K, A, R, G = (C.POINTER(t) for t in (fs_step, fs_kv_cache, fs_adapters, fs_rope,
-                                            fs_sampling))
+    S = K = A = R = G = P  # the descriptors' addresses
     return {
         "fs_clear_status": ([P, P], I32),
         "fs_adapter_workspace": ([S, A], SZ),
@@ -111,8 +110,15 @@ def _want(cond, what):
         raise ValueError(what)
 
 
+def _raw_stream(gpu):
+    """The current stream of the GPU of that index; itself looked up once."""
+    global _raw_stream
+    _raw_stream = _torch()._C._cuda_getCurrentRawStream
+    return _raw_stream(gpu)
+
+
 def _stream(t):
-    return _torch()._C._cuda_getCurrentRawStream(t.get_device())
+    return _raw_stream(t.get_device())
 
 
 def _one_device(*tensors):
@@ -125,8 +131,10 @@ def _one_device(*tensors):
 def _on(index, *tensors):
     """The tensors given are on the GPU of that index (what the host could not read the GPU
     would fault on)."""
+    if index is None:
+        raise ValueError("every tensor of a call on one GPU")
     for t in tensors:
-        if t is not None and t.get_device() != index or index is None:
+        if t is not None and t.get_device() != index:
             raise ValueError("every tensor of a call on one GPU")
 
 
@@ -147,7 +155,9 @@ def _rows(t, name, shape):
     inner = shape[-1]
     if st[-1] != 1 and inner != 1 or len(st) == 3 and st[1] != inner and shape[1] != 1:
         raise ValueError(f"{name}: inner dimensions are not packed")
-    return t.data_ptr(), (st[0] if shape[0] > 1 else inner if len(st) == 2 else inner * shape[1])
+    if shape[0] > 1:
+        return t.data_ptr(), st[0]
+    return t.data_ptr(), (inner if len(st) == 2 else inner * shape[1])
 
 
 def _new(shape, dtype, device):
@@ -197,7 +207,7 @@ class Step:
         self.s = fs_step(n, self.q_off_h.ctypes.data,
                          _vector(self.q_off, torch.int32, n + 1, "q_off"),
                          _vector(kv_len, torch.int32, n, "kv_len"), int(max_kv))
-        self.ref = C.byref(self.s)
+        self.ref = C.addressof(self.s)
 
 
 class KVCache:
@@ -213,10 +223,11 @@ class KVCache:
               (table.shape[1] <= 1 or table.stride(1) == 1), "table: int32 [n][width]")
         self.k, self.v, self.table, self.gpu = k, v, table, _one_device(k, v, table)
         self.n_kv_heads, self.head_dim, self.dtype = k.shape[1], k.shape[3], k.dtype
+        self.n_seqs = table.shape[0]
         self.s = fs_kv_cache(_dtype_code(k), k.shape[1], k.shape[3], k.shape[2], k.shape[0],
                              k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
                              table.data_ptr(), self._table_stride(table))
-        self.ref = C.byref(self.s)
+        self.ref = C.addressof(self.s)
 
     @staticmethod
     def _table_stride(table):
@@ -243,7 +254,7 @@ class Adapters:
                              _vector(rank, torch.int32, n, "rank"),
                              _vector(scale, torch.float32, n, "scale"),
                              _vector(adapter, torch.int32, 0, "adapter"))
-        self.ref = C.byref(self.s)
+        self.ref = C.addressof(self.s)
 
 
 class Rope:
@@ -252,11 +263,12 @@ class Rope:
 
     def __init__(self, inv_freq, interleaved=False, factor=1.0, pos=None):
         torch = _torch()
+        self.rows = None if pos is None else pos.shape[0]
         self.inv_freq, self.pos, self.gpu = inv_freq, pos, _one_device(inv_freq, pos)
         n = inv_freq.shape[0]
         self.s = fs_rope(2 * n, int(bool(interleaved)), _vector(inv_freq, torch.float32, n, "inv_freq"),
                          float(factor), _vector(pos, torch.int32, 0, "pos"))
-        self.ref = C.byref(self.s)
+        self.ref = C.addressof(self.s)
 
 
 class Sampling:
@@ -271,29 +283,36 @@ class Sampling:
                              _vector(top_k, torch.int32, 0, "top_k"),
                              _vector(top_p, torch.float32, 0, "top_p"),
                              _vector(min_p, torch.float32, 0, "min_p"))
-        self.ref = C.byref(self.s)
+        self.ref = C.addressof(self.s)
 
 
 def fs_adapter_linear(step: Step, adapters: Adapters, x, w, y=None, ws=None, err=None, check=True):
     """y = x w^T plus every request's adapter; x [rows][K], w [N][K], returns y [rows][N]."""
-    K, N = adapters.K, adapters.N
-    xp, xs = _rows(x, "x", (step.rows, K))
-    _want(w.shape == (N, K) and w.is_contiguous(), "w: packed [N][K]")
-    _want(x.dtype == adapters.dtype and w.dtype == adapters.dtype, "x, w and adapters: one dtype")
-    _want(adapters.n_seqs >= step.n, "adapter: an id for every request")
-    _on(step.gpu, x, w, y, ws, err)
-    _want(adapters.gpu == step.gpu, "adapters and step: one GPU")
+    K, N, dtype, gpu, T = adapters.K, adapters.N, adapters.dtype, step.gpu, step.rows
+    xp, xs = _rows(x, "x", (T, K))
+    if w.shape != (N, K) or not w.is_contiguous():
+        raise ValueError("w: packed [N][K]")
+    if x.dtype != dtype or w.dtype != dtype:
+        raise ValueError("x, w and adapters: one dtype")
+    if adapters.n_seqs < step.n:
+        raise ValueError("adapter: an id for every request")
+    if adapters.gpu != gpu:
+        raise ValueError("adapters and step: one GPU")
+    _on(gpu, x, w, y, ws, err)
     if y is None:
-        y = _new((step.rows, N), x.dtype, x.device)
+        y = _new((T, N), dtype, x.device)
         yp, ys = y.data_ptr(), N
     else:
-        _want(y.dtype == x.dtype, "y: the dtype of x")
-        yp, ys = _rows(y, "y", (step.rows, N))
-    err = cleared_err_word(x.device) if err is None else err
+        _want(y.dtype == dtype, "y: the dtype of x")
+        yp, ys = _rows(y, "y", (T, N))
+    if err is None:
+        err = cleared_err_word(x.device)
     L = _lib()
     ws, wp, wn = _workspace(ws, L.fs_adapter_workspace(step.ref, adapters.ref), x)
-    _done(L.fs_adapter_linear(step.ref, adapters.ref, xp, xs, w.data_ptr(), yp, ys, wp, wn,
-                              err.data_ptr(), _stream(x)), "fs_adapter_linear", err, check)
+    code = L.fs_adapter_linear(step.ref, adapters.ref, xp, xs, w.data_ptr(), yp, ys, wp, wn,
+                               err.data_ptr(), _raw_stream(gpu))
+    if code or check:
+        _done(code, "fs_adapter_linear", err, check)
     return y
 
 
@@ -314,13 +333,16 @@ def fs_rope_append(step: Step, cache: KVCache, rope: Rope, q, k, v, q_out=None, 
                    check=True):
     """Turns q [rows][heads][dim] and k, appends k and v [rows][kv_heads][dim] to the cache;
     returns the turned q (q_out, which may be q itself)."""
-    T, HK, D = step.rows, cache.n_kv_heads, cache.head_dim
-    _want(k.dtype == cache.dtype and v.dtype == cache.dtype and
-          (q is None or q.dtype == cache.dtype), "q, k, v: the cache's dtype")
-    _want(cache.table.shape[0] >= step.n, "table: a row for every request")
-    _want(rope.pos is None or rope.pos.shape[0] >= T, "pos: a position for every row")
-    _on(step.gpu, q, k, v, q_out, err)
-    _want(cache.gpu == rope.gpu == step.gpu, "cache, rope and step: one GPU")
+    T, HK, D, dtype, gpu = step.rows, cache.n_kv_heads, cache.head_dim, cache.dtype, step.gpu
+    if k.dtype != dtype or v.dtype != dtype or (q is not None and q.dtype != dtype):
+        raise ValueError("q, k, v: the cache's dtype")
+    if cache.n_seqs < step.n:
+        raise ValueError("table: a row for every request")
+    if rope.rows is not None and rope.rows < T:
+        raise ValueError("pos: a position for every row")
+    if cache.gpu != gpu or rope.gpu != gpu:
+        raise ValueError("cache, rope and step: one GPU")
+    _on(gpu, q, k, v, q_out, err)
     kp, ks = _rows(k, "k", (T, HK, D))
     vp, vs = _rows(v, "v", (T, HK, D))
     H, qp, qs, op, os_ = 0, None, 0, None, 0
@@ -333,9 +355,12 @@ def fs_rope_append(step: Step, cache: KVCache, rope: Rope, q, k, v, q_out=None, 
         else:
             _want(q_out.dtype == q.dtype, "q_out: the dtype of q")
             op, os_ = _rows(q_out, "q_out", (T, H, D))
-    err = cleared_err_word(k.device) if err is None else err
-    _done(_lib().fs_rope_append(step.ref, cache.ref, rope.ref, H, qp, qs, kp, ks, vp, vs, op, os_,
-                                err.data_ptr(), _stream(k)), "fs_rope_append", err, check)
+    if err is None:
+        err = cleared_err_word(k.device)
+    code = _lib().fs_rope_append(step.ref, cache.ref, rope.ref, H, qp, qs, kp, ks, vp, vs, op, os_,
+                                 err.data_ptr(), _raw_stream(gpu))
+    if code or check:
+        _done(code, "fs_rope_append", err, check)
     return q_out
 
 
@@ -343,30 +368,39 @@ def fs_paged_attention(step: Step, cache: KVCache, q, scale, window=0, out=None,
                        want_lse=False, ws=None, err=None, check=True):
     """Attention of q [rows][heads][dim] over the cache; returns out, or (out, lse) when the
     log-sum-exp [rows][heads] is wanted."""
-    T, H, D = q.shape
-    _want(q.dtype == cache.dtype and D == cache.head_dim, "q: the cache's dtype and head_dim")
-    _want(cache.table.shape[0] >= step.n, "table: a row for every request")
-    _on(step.gpu, q, out, lse, ws, err)
-    _want(cache.gpu == step.gpu, "cache and step: one GPU")
+    shape, gpu = q.shape, step.gpu
+    T, H, D = shape
+    if q.dtype != cache.dtype or D != cache.head_dim:
+        raise ValueError("q: the cache's dtype and head_dim")
+    if cache.n_seqs < step.n:
+        raise ValueError("table: a row for every request")
+    if cache.gpu != gpu:
+        raise ValueError("cache and step: one GPU")
+    _on(gpu, q, out, lse, ws, err)
     qp, qs = _rows(q, "q", (step.rows, H, D))
-    torch = _torch()
     if out is None:
-        out = torch.empty_like(q)  # packed, whatever q's row stride
+        out = _torch().empty_like(q)  # packed, whatever q's row stride
         op, os_ = out.data_ptr(), H * D
     else:
         _want(out.dtype == q.dtype, "out: the dtype of q")
         op, os_ = _rows(out, "out", (T, H, D))
-    if lse is None:
-        lse = _new((T, H), torch.float32, q.device) if want_lse else None
-    else:
-        _want(lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == T * H,
+    lp = None
+    if lse is not None:
+        _want(lse.dtype == _torch().float32 and lse.is_contiguous() and lse.numel() == T * H,
               "lse: packed float32 [rows][heads]")
-    err = cleared_err_word(q.device) if err is None else err
+        lp = lse.data_ptr()
+    elif want_lse:
+        lse = _new((T, H), _torch().float32, q.device)
+        lp = lse.data_ptr()
+    if err is None:
+        err = cleared_err_word(q.device)
     L = _lib()
-    ws, wp, wn = _workspace(ws, L.fs_attention_workspace(step.ref, cache.ref, H, int(window)), q)
-    _done(L.fs_paged_attention(step.ref, cache.ref, H, scale, int(window), qp, qs, op, os_,
-                               None if lse is None else lse.data_ptr(), wp, wn, err.data_ptr(),
-                               _stream(q)), "fs_paged_attention", err, check)
+    window = int(window)
+    ws, wp, wn = _workspace(ws, L.fs_attention_workspace(step.ref, cache.ref, H, window), q)
+    code = L.fs_paged_attention(step.ref, cache.ref, H, scale, window, qp, qs, op, os_, lp, wp, wn,
+                                err.data_ptr(), _raw_stream(gpu))
+    if code or check:
+        _done(code, "fs_paged_attention", err, check)
     return out if lse is None else (out, lse)
 
 
