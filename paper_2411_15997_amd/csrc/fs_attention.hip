@@ -6,8 +6,8 @@
 //   k_attn_few    requests of at most 64 rows (single tokens, small chunks): bound by the
 //                 cache's bytes (64 requests of up to 16,384 tokens: 121 us, 4.97 TB/s; one of
 //                 200,001: 80 us and 7 for the join, 5.1 TB/s).  The keys are spread over
-//                 work-groups (splits of up to 1,024) and over the four waves of each, which
-//                 load 32 keys at a time into LDS of their own and never wait for each other.
+//                 work-groups (splits of up to 1,024) and over the waves of each, which load 32
+//                 keys at a time into LDS of their own and never wait for each other.
 //   k_attn_chunk  larger chunks: bound by the waits of a tile's chain (scores, maximum,
 //                 exponentials, products) at two waves a SIMD; the matrix cores are busy for
 //                 half of the cycles (4,096 rows over 32,768 keys, head_dim 128: 1.9 ms, 1.08
@@ -103,8 +103,8 @@ __device__ inline float max_of_halves(float x) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// ---- few rows: NT tiles of 16 rows
-template <bool BF, int D, int NT>
+// ---- few rows: NT tiles of 16 rows, WAVES waves
+template <bool BF, int D, int NT, int WAVES>
 __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *lds) {
   constexpr int KS = D / 32;  // matrix steps of a score
   constexpr int DB = D / 16;  // 16-column blocks of an output row
@@ -112,7 +112,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
   constexpr int RW = 64 / CH, LD = 32 / RW;  // rows of a wave's load, loads of 32 keys' K (or V)
   constexpr int kIds = 512;   // page ids kept in LDS
   auto kv_lds = reinterpret_cast<short(*)[2][32 * D]>(lds);  // a wave's K and V
-  __shared__ float wm[4][NT * 16], wl[4][NT * 16];
+  __shared__ float wm[WAVES][NT * 16], wl[WAVES][NT * 16];
   __shared__ uint32_t ids[kIds];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, g4 = lane >> 4;
@@ -167,7 +167,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
     const int32_t p0 = from >> a.c.page_shift;
     const int32_t end = int32_t(min(int64_t(hi), int64_t(p0 + kIds) << a.c.page_shift));
     __syncthreads();
-    for (int i = tid; i < ((end - 1) >> a.c.page_shift) - p0 + 1; i += 256) {
+    for (int i = tid; i < ((end - 1) >> a.c.page_shift) - p0 + 1; i += WAVES * 64) {
       const uint32_t page = __ldg(table + p0 + i);
       if (page >= a.c.n_pages) code = FS_E_RANGE;
       ids[i] = page < a.c.n_pages ? page : 0;
@@ -175,9 +175,9 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
     __syncthreads();
     // the waves take 32 keys in turn
     const int32_t first = from + wave * 32;
-    const int32_t tiles = first < end ? (end - first + 127) / 128 : 0;
+    const int32_t tiles = first < end ? (end - first + WAVES * 32 - 1) / (WAVES * 32) : 0;
     auto issue = [&](int32_t t) {
-      const int32_t j0 = first + t * 128;
+      const int32_t j0 = first + t * (WAVES * 32);
       uint64_t at[LD];
 #pragma unroll
       for (int i = 0; i < LD; ++i) {
@@ -191,7 +191,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
     };
     if (tiles > 0) issue(0);
     for (int32_t t = 0; t < tiles; ++t) {
-      const int32_t j0 = first + t * 128;
+      const int32_t j0 = first + t * (WAVES * 32);
       wait_own<0>();
       const short *kb = kv_lds[wave][0], *vb = kv_lds[wave][1];
       f32x4 sc[NT][2] = {};
@@ -261,7 +261,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
     l[t] += __shfl_xor(l[t], 32, 64);
     if (g4 == 0) wm[wave][t * 16 + r16] = m[t], wl[wave][t * 16 + r16] = l[t];
   }
-  float *buf = reinterpret_cast<float *>(kv_lds);  // [4][16][D / 2]: half of the columns at a time
+  float *buf = reinterpret_cast<float *>(kv_lds);  // [WAVES][16][D / 2]: half of the columns
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     if (t * 16 >= R) break;
@@ -274,17 +274,17 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
             buf + (wave * 16 + r16) * (D / 2) + ((d * 16 + g4 * 4) ^ ((r16 & 3) * 4))) =
             o[t][half * (DB / 2) + d];
       __syncthreads();
-      for (int e = tid; e < 16 * D / 8; e += 256) {
+      for (int e = tid; e < 16 * D / 8; e += WAVES * 64) {
         const int r = e / (D / 8), col = (e - r * (D / 8)) * 4;
         if (t * 16 + r >= R) continue;
         const int tr = t * 16 + r;
         float top = wm[0][tr];
 #pragma unroll
-        for (int w = 1; w < 4; ++w) top = fmaxf(top, wm[w][tr]);
+        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, wm[w][tr]);
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
         float sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
           const float f = wm[w][tr] == -INFINITY ? 0.f : exp2_fast((wm[w][tr] - top) * a.c2);
           sum += f * wl[w][tr];
           acc += f * *reinterpret_cast<const f32x4 *>(buf + (w * 16 + r) * (D / 2) +
@@ -520,10 +520,10 @@ __device__ __forceinline__ void attn_chunk(const AttnArgs &a, int block, int z, 
   }
 }
 
-template <bool BF, int D, int NT>
-__global__ void __launch_bounds__(256) k_attn_few(AttnArgs a) {
-  __shared__ __align__(16) short lds[256 * D];
-  attn_few<BF, D, NT>(a, blockIdx.x, lds);
+template <bool BF, int D, int NT, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64) k_attn_few(AttnArgs a) {
+  __shared__ __align__(16) short lds[WAVES * 64 * D];
+  attn_few<BF, D, NT, WAVES>(a, blockIdx.x, lds);
 }
 template <bool BF, int D, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64, 2) k_attn_chunk(AttnArgs a) {
@@ -542,7 +542,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_mixed(AttnArgs a, int chunk, in
   if (block < chunk)
     attn_chunk<BF, D, 4>(a, block % tiles, block / tiles, lds);
   else
-    attn_few<BF, D, NT>(a, block - chunk, lds);
+    attn_few<BF, D, NT, 4>(a, block - chunk, lds);
 }
 
 // ---- the splits of a row and head, joined in split order by 16-byte columns.
@@ -649,7 +649,7 @@ __global__ void __launch_bounds__(256) k_attn_join_chunk(AttnArgs a) {
 
 // How a call's work is split: from the step's shape and the bound on lengths alone.
 struct Plan {
-  int32_t few_seqs, few_rows, few_tokens, few_split, few_splits;
+  int32_t few_seqs, few_rows, few_tokens, few_waves, few_split, few_splits;
   int32_t chunk_seqs, chunk_rows, chunk_tiles, chunk_split, chunk_splits;
 };
 
@@ -695,9 +695,22 @@ Plan plan(const fs_step *s, const fs_kv_cache *c, int32_t n_heads, int32_t windo
   // 8 heads: 9.7 us whole, 13.0 in two splits of 256, and 3,000 keys 15.5 and 14.1; 64 of up
   // to 16,384: 121 us with 1,024 keys at most, 125 with 512, 127 with 2,048; one of 200,001
   // over 4 heads: 86 us, 94 with 2,048 work-groups, 90 with 512)
-  if (p.few_seqs > 0)
-    split_of(int64_t(p.few_seqs) * c->n_kv_heads, keys(p.few_tokens), 1024, 512, 1024,
-             int64_t(s->n_seqs) * p.few_tokens, p.few_split, p.few_splits);
+  p.few_waves = 4;
+  if (p.few_seqs > 0) {
+    const int64_t blocks = int64_t(p.few_seqs) * c->n_kv_heads;
+    const int32_t len = keys(p.few_tokens);
+    split_of(blocks, len, 1024, 512, 1024, int64_t(s->n_seqs) * p.few_tokens, p.few_split,
+             p.few_splits);
+    // Up to 1,024 keys with a compute unit for each work-group: eight waves and no join (4
+    // requests, 8 heads: 500 keys 8.9 us, 9.8 with four waves; 1,000 keys 11.5 and, in two
+    // splits, 14; 30 requests of 1,000 13.4 and 17.2.  3,000 keys in splits of 1,024 by eight
+    // waves 17.2, as above 15.9.)
+    if (p.chunk_seqs == 0 && p.few_rows <= 32 && len <= 1024 && blocks <= 256) {
+      p.few_waves = 8;
+      p.few_split = 1024;
+      p.few_splits = 1;
+    }
+  }
   if (p.chunk_seqs > 0) {
     auto tiles = [&](int32_t rows) {
       return int32_t(int64_t(s->q_off_h[s->n_seqs]) * G / rows + s->n_seqs);
@@ -758,8 +771,11 @@ void run(const AttnArgs &a, const Plan &p, hipStream_t stream) {
       if (mixed)
         hipLaunchKernelGGL((k_attn_mixed<BF, D, NT>), dim3(chunk + few), block, 0, stream, a, chunk,
                            tiles);
-    if (few > 0 && !mixed)
-      hipLaunchKernelGGL((k_attn_few<BF, D, NT>), dim3(few), block, 0, stream, a);
+    if constexpr (NT <= 2)
+      if (p.few_waves == 8)
+        hipLaunchKernelGGL((k_attn_few<BF, D, NT, 8>), dim3(few), dim3(512), 0, stream, a);
+    if (few > 0 && !mixed && p.few_waves == 4)
+      hipLaunchKernelGGL((k_attn_few<BF, D, NT, 4>), dim3(few), block, 0, stream, a);
   };
   if (p.few_rows <= 16)
     by_rows(std::integral_constant<int, 1>());
