@@ -701,13 +701,14 @@ Plan plan(const fs_step *s, const fs_kv_cache *c, int32_t n_heads, int32_t windo
     const int32_t len = keys(p.few_tokens);
     split_of(blocks, len, 1024, 512, 1024, int64_t(s->n_seqs) * p.few_tokens, p.few_split,
              p.few_splits);
-    // Up to 1,024 keys with a compute unit for each work-group: eight waves and no join (4
-    // requests, 8 heads: 500 keys 8.9 us, 9.8 with four waves; 1,000 keys 11.5 and, in two
-    // splits, 14; 30 requests of 1,000 13.4 and 17.2.  3,000 keys in splits of 1,024 by eight
-    // waves 17.2, as above 15.9.)
-    if (p.chunk_seqs == 0 && p.few_rows <= 32 && len <= 1024 && blocks <= 256) {
+    // Up to 1,024 keys (2,048 of head_dim 64) with a compute unit for each work-group: eight
+    // waves and no join.  (4 requests, 8 heads of 128: 500 keys 8.9 us, 9.8 with four waves;
+    // 1,000 keys 11.5 and, in two splits, 13.5; 30 requests of 1,000 13.4 and 17.1; 1,500 keys
+    // whole 14.5, in splits 13.8.  Of 64: 1,400 keys 10.3 and 13.2, 2,000 12.9 and 14.1.)
+    const int32_t whole = 131072 / c->head_dim;
+    if (p.chunk_seqs == 0 && p.few_rows <= 32 && len <= whole && blocks <= 256) {
       p.few_waves = 8;
-      p.few_split = 1024;
+      p.few_split = whole;
       p.few_splits = 1;
     }
   }

@@ -382,6 +382,21 @@ def test_attention_of_many_requests(lens):
     within(fs.fs_paged_attention(step_of(lens, kv), on_gpu(k, v, table), q.cuda(), 0.1), want, tol, "out")
 
 
+@pytest.mark.parametrize("most", [1023, 1024, 1025, 2047, 2048, 2049])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_around_the_longest_whole_request(D, most):
+    """Lengths and bounds at which single tokens go from one work-group a head to splits."""
+    g = gen(most + D)
+    lens, kv = [1, 1, 2, 1], [most, 1, most - 200, 257]
+    k, v, table = make_cache(g, kv, 2, D, 16, BF)
+    q_off = offsets(lens)
+    q = normal(g, q_off[-1], 8, D)
+    want, tol, lse, ltol = ref.attention(q, k, v, table, q_off, kv, 0.1, 0)
+    got, l = fs.fs_paged_attention(step_of(lens, kv), on_gpu(k, v, table), q.cuda(), 0.1, want_lse=True)
+    within(got, want, tol, "out")
+    within(l, lse, ltol, "lse")
+
+
 @pytest.mark.parametrize("window", [0, 150])
 @pytest.mark.parametrize("dtype", [BF, HF])
 def test_attention_of_many_rows_without_small_requests(dtype, window):
