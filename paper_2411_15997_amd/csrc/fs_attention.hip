@@ -621,14 +621,15 @@ __global__ void __launch_bounds__(256) k_attn_join_few(AttnArgs a) {
 }
 
 // Many rows, few splits: D / 4 lanes for a row and head.  (1,000 tokens of 32 heads in 2
-// splits, head_dim 128: 10.5 us; with a work-group for each row and head 43.)
+// splits, head_dim 128: 10.5 us; with a work-group for each row and head 43.)  A wave holds
+// several items, whose rows may belong to several requests.
 template <bool BF, int D>
 __global__ void __launch_bounds__(256) k_attn_join_chunk(AttnArgs a) {
   constexpr int LANES = D / 4;
   const int32_t it = blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
   if (it >= a.rows * a.n_heads) return;
   const int32_t t = it / a.n_heads, h = it - t * a.n_heads, c = threadIdx.x % LANES;
-  const int32_t s = seq_of_row(a.q_off, a.n_seqs, t);
+  const int32_t s = seq_of_own_row(a.q_off, a.n_seqs, t);
   const int32_t q0 = __ldg(a.q_off + s), n = __ldg(a.q_off + s + 1) - q0;
   if (n * a.group <= kFewRows) return;
   int32_t code = 0;

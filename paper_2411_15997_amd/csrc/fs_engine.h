@@ -93,7 +93,9 @@ __device__ inline void wait_own() {
 }
 
 // The last of the requests 0 .. n - 1 whose first(s) is at most b, by the whole wave: 64
-// probes a round instead of one.  first is non-decreasing and first(0) <= b.
+// probes a round instead of one.  first is non-decreasing and first(0) <= b.  All 64 lanes
+// take part, with the same b: lanes that have left, or that look for another b, would make
+// the count of hits wrong.
 template <class F>
 __device__ inline int32_t last_at_most(int32_t n, int32_t b, F first) {
   int32_t lo = 0, len = n;
@@ -106,9 +108,22 @@ __device__ inline int32_t last_at_most(int32_t n, int32_t b, F first) {
   }
   return lo;
 }
-// The request whose rows contain row t (t < q_off[n]), by the whole wave.
+// The request whose rows contain row t (t < q_off[n]), by the whole wave (one t for all 64
+// lanes).
 __device__ inline int32_t seq_of_row(const int32_t *q_off, int32_t n, int32_t t) {
   return last_at_most(n, t, [&](int32_t s) { return __ldg(q_off + s); });
+}
+// The same by each lane for a t of its own, whatever the other lanes do.
+__device__ inline int32_t seq_of_own_row(const int32_t *q_off, int32_t n, int32_t t) {
+  int32_t lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int32_t mid = (lo + hi + 1) >> 1;
+    if (__ldg(q_off + mid) <= t)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  return lo;
 }
 
 // Row tiles that never span two requests.  Request s owns the tile numbers from
