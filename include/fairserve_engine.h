@@ -144,7 +144,8 @@ fs_status fs_rope_append(const fs_step *s, const fs_kv_cache *c, const fs_rope *
  *   out[t][h] = sum_j softmax_j(scale * q[t][h] . k_j) v_j
  * over the cached tokens j <= p, j < kv_len and, with window > 0, j > p - window.  A row with no
  * such token gets 0 (lse -inf).  lse [T][n_heads] fp32 (NULL: not wanted) is
- * ln sum_j exp(scale q . k_j), which joins results over parts of a context.
+ * ln sum_j exp(scale q . k_j), which joins results over parts of a context: NaN where a score
+ * is NaN, inf where one is inf and none is NaN (out is NaN in both).
  *   q, out: [T][n_heads][head_dim] of the cache's dtype (token strides q_stride,
  *   out_stride); head_dim 64 or 128; n_heads a multiple of n_kv_heads, at most 64 times it;
  *   rows times n_heads at most 2^30, n_seqs times n_kv_heads at most 2^20.

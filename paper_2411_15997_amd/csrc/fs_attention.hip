@@ -103,6 +103,22 @@ __device__ inline float max_of_halves(float x) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+// A reference of the exponentials as they use it: 0 while there is none and where it is
+// infinite, so that a score of inf makes the sum inf (inf - inf would make it NaN).
+__device__ inline float reference(float m, float c2) {
+  return fabsf(m) == INFINITY ? 0.f : m * c2;
+}
+// What a part with the maximum m weighs where the largest of the parts' is `top` (inf less
+// inf is no number; a part without a maximum holds sums of 0).
+__device__ inline float part_factor(float m, float top, float c2) {
+  return exp2_fast(m == top ? 0.f : (m - top) * c2);
+}
+// ln of a row's sum of exponentials: -inf only where nothing was summed (a NaN score makes
+// the sum NaN, one of inf makes it inf).
+__device__ inline float log_sum(float top, float sum, float c2) {
+  return sum == 0.f ? -INFINITY : (top * c2 + __log2f(sum)) * kLn2;
+}
+
 // ---- few rows: NT tiles of 16 rows, WAVES waves
 template <bool BF, int D, int NT, int WAVES>
 __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *lds) {
@@ -227,7 +243,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
           for (int d = 0; d < DB; ++d) o[r][d] *= f;
           m[r] = m2;
         }
-        const float mc = m[r] == -INFINITY ? 0.f : m[r] * a.c2;
+        const float mc = reference(m[r], a.c2);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           p[i] = exp2_fast(fmaf(p[i], a.c2, -mc));
@@ -285,7 +301,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
         float sum = 0.f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-          const float f = wm[w][tr] == -INFINITY ? 0.f : exp2_fast((wm[w][tr] - top) * a.c2);
+          const float f = part_factor(wm[w][tr], top, a.c2);
           sum += f * wl[w][tr];
           acc += f * *reinterpret_cast<const f32x4 *>(buf + (w * 16 + r) * (D / 2) +
                                                       (col ^ ((r & 3) * 4)));
@@ -298,8 +314,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
           for (int i = 0; i < 4; ++i) v[i] = to_16<BF>(acc[i] * inv);
           *reinterpret_cast<s16x4 *>(a.out + (q0 + tok) * a.out_stride + h * D + cc) = v;
           if (cc == 0 && a.lse)
-            a.lse[int64_t(q0 + tok) * a.n_heads + h] =
-                sum > 0.f ? (top * a.c2 + __log2f(sum)) * kLn2 : -INFINITY;
+            a.lse[int64_t(q0 + tok) * a.n_heads + h] = log_sum(top, sum, a.c2);
         } else {
           const int64_t idx =
               ((int64_t(z) * a.n_seqs + s) * a.few_tokens + tok) * a.n_heads + h;
@@ -465,7 +480,7 @@ __device__ __forceinline__ void attn_chunk(const AttnArgs &a, int block, int z, 
       for (int d = 0; d < DB; ++d) o[d] *= f;
       m = m2;
     }
-    const float mc = m == -INFINITY ? 0.f : m * a.c2;
+    const float mc = reference(m, a.c2);
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -505,8 +520,7 @@ __device__ __forceinline__ void attn_chunk(const AttnArgs &a, int block, int z, 
         *reinterpret_cast<s16x4 *>(op + d * 32 + i * 8 + h2 * 4) = v;
       }
     if (h2 == 0 && a.lse)
-      a.lse[int64_t(q0 + tok) * a.n_heads + h] =
-          l > 0.f ? (m * a.c2 + __log2f(l)) * kLn2 : -INFINITY;
+      a.lse[int64_t(q0 + tok) * a.n_heads + h] = log_sum(m, l, a.c2);
   } else {
     const int64_t idx = (int64_t(z) * a.rows + q0 + tok) * a.n_heads + h;
     float *op = a.chunk_o + idx * D;
@@ -560,7 +574,7 @@ __device__ inline void add_splits(const AttnArgs &a, const Parts &p, int first, 
   for (int i = first; i < p.splits; i += PER) {
     const int64_t idx = p.idx0 + i * p.step;
     const float mi = p.ml[idx * 2];
-    const float f = mi == -INFINITY ? 0.f : exp2_fast((mi - top) * a.c2);
+    const float f = part_factor(mi, top, a.c2);
     sum += f * p.ml[idx * 2 + 1];
     acc += f * *reinterpret_cast<const f32x4 *>(p.o + idx * D + c * 4);
   }
@@ -583,8 +597,7 @@ __device__ inline void put_joined(const AttnArgs &a, int64_t t, int32_t h, int c
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = to_16<BF>(acc[i] * inv);
   *reinterpret_cast<s16x4 *>(a.out + t * a.out_stride + h * D + c * 4) = v;
-  if (c == 0 && a.lse)
-    a.lse[t * a.n_heads + h] = sum > 0.f ? (top * a.c2 + __log2f(sum)) * kLn2 : -INFINITY;
+  if (c == 0 && a.lse) a.lse[t * a.n_heads + h] = log_sum(top, sum, a.c2);
 }
 
 // Few rows, often many splits: a work-group for a row and head, the splits side by side.

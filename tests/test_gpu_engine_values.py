@@ -1,0 +1,99 @@
+"""Attention of values that are not finite, or far apart: NaN and infinities in queries and
+keys, in every form of the call (single tokens and chunks, whole and split over keys)."""
+import math
+
+import pytest
+import torch
+
+import engine_ref as ref
+import paper_2411_15997_amd as fs
+from gpu_common import say
+from test_gpu_engine import BF, HF, gen, make_cache, normal, offsets, on_gpu, step_of, within
+
+pytestmark = pytest.mark.gpu
+
+FORMS = [
+    # rows, cached lengths, heads, kv heads, dim: whole and split, few rows and many, both at once
+    ([1, 1, 1], [300, 90, 301], 8, 2, 128),
+    ([1, 2, 1], [5000, 90, 2500], 4, 4, 64),
+    ([40, 30], [200, 333], 6, 2, 128),
+    ([90, 80], [1500, 4000], 3, 1, 64),
+    ([90, 1, 2], [1500, 3000, 90], 6, 2, 64),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("lens,kv,H,HK,D", FORMS)
+def test_rows_with_scores_that_are_not_finite(lens, kv, H, HK, D, dtype):
+    """A NaN score makes out and lse NaN; one of +inf makes out NaN (inf / inf) and lse +inf;
+    scores of -inf weigh nothing.  Other heads and rows are as they were."""
+    say("not finite", lens, kv, H, HK, D, dtype)
+    g = gen(D + H)
+    q_off, grp = offsets(lens), H // HK
+    T = q_off[-1]
+    k, v, table = make_cache(g, kv, HK, D, 16, dtype)
+    q = normal(g, T, H, D, dtype=dtype)
+    # element 0 of the queries is 1, and -1 in one row: a key's element 0 of inf then makes its
+    # scores inf, and -inf in that row
+    q[:, :, 0] = 1.0
+    q[0, 0, 0] = -1.0
+    nan_row = T - 1
+    q[nan_row, H - 1, 3] = math.nan
+    bad = min(kv[0] - lens[0], 7)                   # a key that every row of request 0 sees
+    page = int(table[0, bad // 16])
+    k[page, 0, bad % 16, 0] = math.inf
+    if HK > 1:
+        k[page, 1, bad % 16, 5] = math.nan
+    scale = D ** -0.5
+    out, lse = fs.fs_paged_attention(step_of(lens, kv), on_gpu(k, v, table), q.cuda(), scale,
+                                     want_lse=True)
+    out, lse = out.double().cpu(), lse.double().cpu()
+    # what must not have changed: the oracle on finite inputs, the key of -inf scores left out
+    kf, qf = k.clone(), q.clone()
+    kf[page, 0, bad % 16, 0] = 0.0
+    if HK > 1:
+        kf[page, 1, bad % 16, 5] = 0.0
+    qf[nan_row, H - 1, 3] = 0.0
+    want, tol, wl, ltol = ref.attention(qf, kf, v, table, q_off, kv, scale, 0)
+    for t in range(T):
+        for h in range(H):
+            first = t < lens[0]
+            if (t, h) == (nan_row, H - 1) or (first and HK > 1 and h // grp == 1):
+                assert bool(out[t, h].isnan().all()) and bool(lse[t, h].isnan()), (t, h, lse[t, h])
+            elif first and h // grp == 0 and (t, h) != (0, 0):
+                assert bool(out[t, h].isnan().all()) and lse[t, h] == math.inf, (t, h, lse[t, h])
+            elif (t, h) != (0, 0):
+                within(out[t, h], want[t, h], tol[t, h], f"out {t} {h}")
+                within(lse[t, h], wl[t, h], ltol[t, h], f"lse {t} {h}")
+    # row 0, head 0: without the key whose score is -inf
+    p = kv[0] - lens[0]
+    K = ref.kv_rows(kf, table[0], p + 1, 16, 0)
+    sc = scale * K @ q[0, 0].double()
+    sc[bad] = -math.inf
+    V = ref.kv_rows(v, table[0], p + 1, 16, 0)
+    prob = torch.softmax(sc, 0)
+    u = ref.U16[dtype]
+    rel = u + 2 * (D + 4) * ref.E32 * scale * float((K.abs() @ q[0, 0].double().abs()).max()) + \
+        (p + 9) * ref.E32 + 2.0 ** -20
+    bound = u * (prob @ V).abs() + rel * (prob @ V.abs()) + ref.TINY[dtype]
+    if p > 0:
+        within(out[0, 0], prob @ V, bound, "out without a key")
+        within(lse[0, 0], torch.logsumexp(sc, 0), rel + 2 * ref.E32 * float(lse[0, 0].abs()), "lse")
+    else:
+        assert lse[0, 0] == -math.inf
+
+
+def test_rows_without_a_key_are_empty_and_nothing_else():
+    """-inf is the log-sum-exp of rows that see nothing, and of rows whose scores are all -inf."""
+    g = gen(5)
+    k, v, table = make_cache(g, [3, 40], 1, 64, 16, BF)
+    k[int(table[1, 0]), 0, 0:16, 0] = -math.inf
+    k[int(table[1, 1]), 0, 0:16, 0] = -math.inf
+    k[int(table[1, 2]), 0, 0:8, 0] = -math.inf
+    q = normal(g, 6, 2, 64)
+    q[:, :, 0] = 1.0
+    out, lse = fs.fs_paged_attention(step_of([5, 1], [3, 40]), on_gpu(k, v, table), q.cuda(), 0.1,
+                                     want_lse=True)
+    assert bool((lse[:2] == -math.inf).all()) and bool((out[:2] == 0).all())
+    assert bool(torch.isfinite(lse[2:5]).all())
+    assert bool((lse[5] == -math.inf).all())
