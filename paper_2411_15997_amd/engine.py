@@ -15,6 +15,7 @@ import numpy as np
 
 FS_BF16, FS_F16, FS_F32 = 0, 1, 2
 FS_ROPE_PLAIN, FS_ROPE_LINEAR, FS_ROPE_BASE, FS_ROPE_PARTS = 0, 1, 2, 3
+FS_E_ARG = 1
 ALIGN = 256
 
 EXPORTED_ENGINE = ("fs_clear_status", "fs_adapter_workspace", "fs_adapter_linear",
@@ -202,17 +203,18 @@ class Step:
         _want(n >= 0, "q_off: at least one value")
         self.n, self.rows = n, int(self.q_off_h[-1])
         self.q_off = torch.from_numpy(self.q_off_h.copy()).to(device) if q_off is None else q_off
-        self.kv_len = kv_len
+        self.kv_len, self.max_kv = kv_len, int(max_kv)
         self.gpu = _one_device(self.q_off, kv_len)
         self.s = fs_step(n, self.q_off_h.ctypes.data,
                          _vector(self.q_off, torch.int32, n + 1, "q_off"),
-                         _vector(kv_len, torch.int32, n, "kv_len"), int(max_kv))
+                         _vector(kv_len, torch.int32, n, "kv_len"), self.max_kv)
         self.ref = C.addressof(self.s)
 
 
 class KVCache:
     """A paged cache: k and v [pages][kv_heads][page_size][head_dim] (any strides with the
-    last dimension packed; k and v alike), table [n][width] int32 of page ids."""
+    last dimension packed; k and v alike), table [n][width] int32 of page ids (rows may be
+    further apart than their width; a step's max_kv keeps to the width)."""
 
     def __init__(self, k, v, table):
         torch = _torch()
@@ -223,7 +225,7 @@ class KVCache:
               (table.shape[1] <= 1 or table.stride(1) == 1), "table: int32 [n][width]")
         self.k, self.v, self.table, self.gpu = k, v, table, _one_device(k, v, table)
         self.n_kv_heads, self.head_dim, self.dtype = k.shape[1], k.shape[3], k.dtype
-        self.n_seqs = table.shape[0]
+        self.n_seqs, self.most_kv = table.shape[0], table.shape[1] * k.shape[2]
         self.s = fs_kv_cache(_dtype_code(k), k.shape[1], k.shape[3], k.shape[2], k.shape[0],
                              k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
                              table.data_ptr(), self._table_stride(table))
@@ -235,6 +237,14 @@ class KVCache:
             _want(table.stride(0) >= table.shape[1], "table: rows overlap")
             return table.stride(0)
         return table.shape[1]
+
+    def check(self, step, where):
+        """A page id for every token that a request of the step may hold (the library knows
+        how far apart the table's rows are, not their width)."""
+        if self.n_seqs < step.n:
+            raise ValueError("table: a row for every request")
+        if step.max_kv > self.most_kv and step.n > 0:
+            _fail(FS_E_ARG, where)
 
 
 class Adapters:
@@ -336,8 +346,7 @@ def fs_rope_append(step: Step, cache: KVCache, rope: Rope, q, k, v, q_out=None, 
     T, HK, D, dtype, gpu = step.rows, cache.n_kv_heads, cache.head_dim, cache.dtype, step.gpu
     if k.dtype != dtype or v.dtype != dtype or (q is not None and q.dtype != dtype):
         raise ValueError("q, k, v: the cache's dtype")
-    if cache.n_seqs < step.n:
-        raise ValueError("table: a row for every request")
+    cache.check(step, "fs_rope_append")
     if rope.rows is not None and rope.rows < T:
         raise ValueError("pos: a position for every row")
     if cache.gpu != gpu or rope.gpu != gpu:
@@ -372,8 +381,7 @@ def fs_paged_attention(step: Step, cache: KVCache, q, scale, window=0, out=None,
     T, H, D = shape
     if q.dtype != cache.dtype or D != cache.head_dim:
         raise ValueError("q: the cache's dtype and head_dim")
-    if cache.n_seqs < step.n:
-        raise ValueError("table: a row for every request")
+    cache.check(step, "fs_paged_attention")
     if cache.gpu != gpu:
         raise ValueError("cache and step: one GPU")
     _on(gpu, q, out, lse, ws, err)

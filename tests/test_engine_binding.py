@@ -1,0 +1,36 @@
+"""The binding of the engine step's operators: what it refuses before anything is enqueued,
+because the library could not see it (no GPU needed)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2411_15997_amd as fs
+
+BF = torch.bfloat16
+
+
+def cache(width, page=16, rows=2, of=None, at=0):
+    """A cache whose page table is `width` columns of a table of `of` columns."""
+    k = torch.zeros(4, 2, page, 64, dtype=BF)
+    table = torch.zeros(rows, of or width, dtype=torch.int32)[:, at:at + width]
+    return fs.KVCache(k, k.clone(), table)
+
+
+def step(max_kv, rows=2):
+    return fs.Step(list(range(rows + 1)), kv_len=torch.ones(rows, dtype=torch.int32), max_kv=max_kv,
+                   device="cpu")
+
+
+@pytest.mark.parametrize("width,of,at", [(4, 9, 0), (4, 9, 5), (4, 4, 0), (0, 3, 1)])
+def test_lengths_keep_to_the_page_tables_width(width, of, at):
+    """Columns of a wider table: its rows' distance is no width."""
+    q, kv = torch.zeros(2, 4, 64, dtype=BF), torch.zeros(2, 2, 64, dtype=BF)
+    rope = fs.Rope(torch.ones(32))
+    calls = (lambda s, c: fs.fs_paged_attention(s, c, q, 1.0),
+             lambda s, c: fs.fs_rope_append(s, c, rope, q, kv, kv))
+    for call in calls:
+        with pytest.raises(fs.FairServeError) as e:
+            call(step(width * 16 + 1), cache(width, of=of, at=at))
+        assert e.value.code == fs.FS_E_ARG
+        with pytest.raises(ValueError, match="on one GPU"):           # up to the width: goes on
+            call(step(width * 16), cache(width, of=of, at=at))
