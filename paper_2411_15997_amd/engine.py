@@ -198,7 +198,8 @@ class Step:
 
     def __init__(self, q_off_h, q_off=None, kv_len=None, max_kv=0, device="cuda"):
         torch = _torch()
-        self.q_off_h = np.ascontiguousarray(q_off_h, np.int32)
+        # a copy: the grids and the outputs' sizes are taken from it at every call
+        self.q_off_h = np.array(q_off_h, np.int32)
         n = self.q_off_h.shape[0] - 1
         _want(n >= 0, "q_off: at least one value")
         self.n, self.rows = n, int(self.q_off_h[-1])

@@ -34,3 +34,12 @@ def test_lengths_keep_to_the_page_tables_width(width, of, at):
         assert e.value.code == fs.FS_E_ARG
         with pytest.raises(ValueError, match="on one GPU"):           # up to the width: goes on
             call(step(width * 16), cache(width, of=of, at=at))
+
+
+def test_a_steps_offsets_are_its_own():
+    """A serving loop fills one array of offsets again for each step."""
+    off = np.array([0, 1, 3], np.int32)
+    s = fs.Step(off, kv_len=torch.ones(2, dtype=torch.int32), max_kv=4, device="cpu")
+    off[:] = [0, 500, 1000]
+    assert s.q_off_h.tolist() == [0, 1, 3] and s.rows == 3
+    assert s.s.q_off_h == s.q_off_h.ctypes.data
