@@ -111,6 +111,11 @@ def _want(cond, what):
         raise ValueError(what)
 
 
+def _want_32(what, *sizes):
+    """Sizes that the library takes as int32 (ctypes would cut larger ones down to 32 bits)."""
+    _want(all(-1 << 31 <= n < 1 << 31 for n in sizes), f"{what}: beyond 32 bits")
+
+
 def _raw_stream(gpu):
     """The current stream of the GPU of that index; itself looked up once."""
     global _raw_stream
@@ -199,12 +204,15 @@ class Step:
     def __init__(self, q_off_h, q_off=None, kv_len=None, max_kv=0, device="cuda"):
         torch = _torch()
         # a copy: the grids and the outputs' sizes are taken from it at every call
-        self.q_off_h = np.array(q_off_h, np.int32)
+        given = np.asarray(q_off_h)
+        self.q_off_h = given.astype(np.int32)  # astype copies
+        _want((self.q_off_h == given).all(), "q_off: beyond 32 bits")
         n = self.q_off_h.shape[0] - 1
         _want(n >= 0, "q_off: at least one value")
         self.n, self.rows = n, int(self.q_off_h[-1])
         self.q_off = torch.from_numpy(self.q_off_h.copy()).to(device) if q_off is None else q_off
         self.kv_len, self.max_kv = kv_len, int(max_kv)
+        _want_32("max_kv", self.max_kv)
         self.gpu = _one_device(self.q_off, kv_len)
         self.s = fs_step(n, self.q_off_h.ctypes.data,
                          _vector(self.q_off, torch.int32, n + 1, "q_off"),
@@ -224,6 +232,7 @@ class KVCache:
         _want(k.shape[3] == 1 or k.stride(3) == 1, "k, v: the last dimension is not packed")
         _want(table.dim() == 2 and table.dtype == torch.int32 and
               (table.shape[1] <= 1 or table.stride(1) == 1), "table: int32 [n][width]")
+        _want_32("k, v", *k.shape[1:])
         self.k, self.v, self.table, self.gpu = k, v, table, _one_device(k, v, table)
         self.n_kv_heads, self.head_dim, self.dtype = k.shape[1], k.shape[3], k.dtype
         self.n_seqs, self.most_kv = table.shape[0], table.shape[1] * k.shape[2]
@@ -258,6 +267,7 @@ class Adapters:
               a.dtype == b.dtype and a.shape[0] == b.shape[0] and a.shape[1] == b.shape[2],
               "a [n][max_rank][K] and b [n][N][max_rank]: packed, of one dtype")
         n, r, k = a.shape
+        _want_32("a, b", n, r, k, b.shape[1])
         self.keep = (a, b, adapter, rank, scale)
         self.gpu = _one_device(*self.keep)
         self.dtype, self.K, self.N, self.n_seqs = a.dtype, k, b.shape[1], adapter.shape[0]
@@ -277,6 +287,7 @@ class Rope:
         self.rows = None if pos is None else pos.shape[0]
         self.inv_freq, self.pos, self.gpu = inv_freq, pos, _one_device(inv_freq, pos)
         n = inv_freq.shape[0]
+        _want_32("inv_freq", 2 * n)
         self.s = fs_rope(2 * n, int(bool(interleaved)), _vector(inv_freq, torch.float32, n, "inv_freq"),
                          float(factor), _vector(pos, torch.int32, 0, "pos"))
         self.ref = C.addressof(self.s)
@@ -358,6 +369,8 @@ def fs_rope_append(step: Step, cache: KVCache, rope: Rope, q, k, v, q_out=None, 
     H, qp, qs, op, os_ = 0, None, 0, None, 0
     if q is not None:
         H = q.shape[1]
+        if H >= 1 << 31:
+            raise ValueError("q: beyond 32 bits")
         qp, qs = _rows(q, "q", (T, H, D))
         if q_out is None:
             q_out = _torch().empty_like(q)  # packed, whatever q's row stride
@@ -404,7 +417,7 @@ def fs_paged_attention(step: Step, cache: KVCache, q, scale, window=0, out=None,
     if err is None:
         err = cleared_err_word(q.device)
     L = _lib()
-    window = int(window)
+    window = max(-1, min(int(window), 0x7fffffff))  # one beyond every length is none
     ws, wp, wn = _workspace(ws, L.fs_attention_workspace(step.ref, cache.ref, H, window), q)
     code = L.fs_paged_attention(step.ref, cache.ref, H, scale, window, qp, qs, op, os_, lp, wp, wn,
                                 err.data_ptr(), _raw_stream(gpu))
@@ -419,6 +432,8 @@ def fs_sample(logits, u, sampling: Sampling, token=None, logprob=None, kept=None
     returns (token int32, logprob float32, kept int32), each [rows]."""
     torch = _torch()
     n, V = logits.shape
+    if n >= 1 << 31 or V >= 1 << 31:
+        raise ValueError("logits: beyond 32 bits")
     stride = logits.stride()
     _want(n <= 1 or stride[0] >= V, "logits: rows overlap")
     _want(V == 1 or stride[1] == 1, "logits: rows are not packed")

@@ -43,3 +43,26 @@ def test_a_steps_offsets_are_its_own():
     off[:] = [0, 500, 1000]
     assert s.q_off_h.tolist() == [0, 1, 3] and s.rows == 3
     assert s.s.q_off_h == s.q_off_h.ctypes.data
+
+
+BIG = 1 << 32
+
+
+@pytest.mark.parametrize("make", [
+    lambda: fs.Step([0, BIG + 1], kv_len=torch.ones(1, dtype=torch.int32), max_kv=4, device="cpu"),
+    lambda: fs.Step(np.array([0, 1, BIG + 2]), max_kv=4, device="cpu"),
+    lambda: fs.Step([0, 1], kv_len=torch.ones(1, dtype=torch.int32), max_kv=BIG + 16, device="cpu"),
+    lambda: fs.KVCache(*[torch.empty(1, BIG + 1, 1, 8, dtype=BF, device="meta")] * 2,
+                       torch.empty(1, 1, dtype=torch.int32, device="meta")),
+    lambda: fs.Adapters(torch.empty(1, 8, BIG + 8, dtype=BF, device="meta"),
+                        torch.empty(1, 64, 8, dtype=BF, device="meta"),
+                        torch.empty(1, dtype=torch.int32, device="meta")),
+    lambda: fs.Rope(torch.empty(BIG // 2 + 32, device="meta")),
+    lambda: fs.fs_sample(torch.empty(BIG + 3, 1, dtype=BF, device="meta"),
+                         torch.empty(BIG + 3, device="meta"), fs.Sampling()),
+    lambda: fs.fs_sample(torch.empty(1, BIG + 3, dtype=BF, device="meta"),
+                         torch.empty(1, device="meta"), fs.Sampling()),
+])
+def test_sizes_beyond_32_bits_are_refused(make):
+    with pytest.raises(ValueError, match="beyond 32 bits"):
+        make()

@@ -97,3 +97,18 @@ def test_rows_without_a_key_are_empty_and_nothing_else():
     assert bool((lse[:2] == -math.inf).all()) and bool((out[:2] == 0).all())
     assert bool(torch.isfinite(lse[2:5]).all())
     assert bool((lse[5] == -math.inf).all())
+
+
+@pytest.mark.parametrize("lens", [[1, 1], [90, 1]])
+def test_a_window_beyond_32_bits_is_none(lens):
+    g = gen(6)
+    k, v, table = make_cache(g, [200, 33], 2, 64, 16, BF)
+    q = normal(g, sum(lens), 4, 64).cuda()
+    step, cache = step_of(lens, [200, 33]), on_gpu(k, v, table)
+    plain = fs.fs_paged_attention(step, cache, q, 0.2)
+    for window in ((1 << 31), (1 << 32) + 3, 1 << 40):
+        assert torch.equal(fs.fs_paged_attention(step, cache, q, 0.2, window=window), plain)
+    for window in (-1, -(1 << 32) + 3):
+        with pytest.raises(fs.FairServeError) as e:
+            fs.fs_paged_attention(step, cache, q, 0.2, window=window)
+        assert e.value.code == fs.FS_E_ARG
