@@ -176,6 +176,8 @@ def _workspace(ws, need, like):
         return None, None, 0
     if ws is None:
         ws = _torch().empty(need, dtype=_torch().uint8, device=like.device)
+    elif not ws.is_contiguous():
+        raise ValueError("ws: packed (its size is that of its values)")
     return ws, ws.data_ptr(), ws.numel() * ws.element_size()
 
 

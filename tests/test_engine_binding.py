@@ -66,3 +66,13 @@ BIG = 1 << 32
 def test_sizes_beyond_32_bits_are_refused(make):
     with pytest.raises(ValueError, match="beyond 32 bits"):
         make()
+
+
+def test_a_workspace_is_as_large_as_it_says():
+    """A view that repeats one byte has many values and little memory."""
+    like = torch.zeros(1)
+    _, _, n = fs.engine._workspace(torch.zeros(1000, dtype=torch.uint8), 500, like)
+    assert n == 1000
+    for ws in (torch.zeros(1, dtype=torch.uint8).expand(1000), torch.zeros(2000, dtype=torch.uint8)[::2]):
+        with pytest.raises(ValueError, match="ws: packed"):
+            fs.engine._workspace(ws, 500, like)
