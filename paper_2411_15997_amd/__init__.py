@@ -202,6 +202,9 @@ def err_word(device="cuda"):
 
 
 def fs_sync_status(err) -> int:
+    if err.get_device() not in (-1, _torch().cuda.current_device()):
+        with _torch().cuda.device(err.device):       # the stream that raised it is there
+            return fs_sync_status(err)
     return int(_lib().fs_sync_status(_stream(), _ptr(err)))
 
 

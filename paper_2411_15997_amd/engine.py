@@ -123,8 +123,18 @@ def _raw_stream(gpu):
     return _raw_stream(gpu)
 
 
-def _stream(t):
-    return _raw_stream(t.get_device())
+def _current_gpu():
+    """The index of the current GPU; itself looked up once."""
+    global _current_gpu
+    _current_gpu = _torch()._C._cuda_getDevice
+    return _current_gpu()
+
+
+def _there(gpu, call, *args):
+    """The call with its tensors' GPU current.  (The handle of a default stream names no GPU:
+    kernels would go to the current one.)"""
+    with _torch().cuda.device(gpu):
+        return call(*args)
 
 
 def _one_device(*tensors):
@@ -186,7 +196,11 @@ def cleared_err_word(device="cuda"):
 
 
 def fs_clear_status(err):
-    code = _lib().fs_clear_status(err.data_ptr(), _stream(err))
+    gpu = err.get_device()
+    _on(None if gpu < 0 else gpu, err)
+    if gpu != _current_gpu():
+        return _there(gpu, fs_clear_status, err)
+    code = _lib().fs_clear_status(err.data_ptr(), _raw_stream(gpu))
     if code:
         _fail(code, "fs_clear_status")
 
@@ -323,6 +337,8 @@ def fs_adapter_linear(step: Step, adapters: Adapters, x, w, y=None, ws=None, err
     if adapters.gpu != gpu:
         raise ValueError("adapters and step: one GPU")
     _on(gpu, x, w, y, ws, err)
+    if gpu != _current_gpu():
+        return _there(gpu, fs_adapter_linear, step, adapters, x, w, y, ws, err, check)
     if y is None:
         y = _new((T, N), dtype, x.device)
         yp, ys = y.data_ptr(), N
@@ -366,6 +382,8 @@ def fs_rope_append(step: Step, cache: KVCache, rope: Rope, q, k, v, q_out=None, 
     if cache.gpu != gpu or rope.gpu != gpu:
         raise ValueError("cache, rope and step: one GPU")
     _on(gpu, q, k, v, q_out, err)
+    if gpu != _current_gpu():
+        return _there(gpu, fs_rope_append, step, cache, rope, q, k, v, q_out, err, check)
     kp, ks = _rows(k, "k", (T, HK, D))
     vp, vs = _rows(v, "v", (T, HK, D))
     H, qp, qs, op, os_ = 0, None, 0, None, 0
@@ -401,6 +419,9 @@ def fs_paged_attention(step: Step, cache: KVCache, q, scale, window=0, out=None,
     if cache.gpu != gpu:
         raise ValueError("cache and step: one GPU")
     _on(gpu, q, out, lse, ws, err)
+    if gpu != _current_gpu():
+        return _there(gpu, fs_paged_attention, step, cache, q, scale, window, out, lse, want_lse, ws,
+                      err, check)
     qp, qs = _rows(q, "q", (step.rows, H, D))
     if out is None:
         out = _torch().empty_like(q)  # packed, whatever q's row stride
@@ -444,6 +465,8 @@ def fs_sample(logits, u, sampling: Sampling, token=None, logprob=None, kept=None
     dev = logits.device
     _on(dev.index, u, token, logprob, kept, ws, err)
     _want(sampling.gpu is None or sampling.gpu == dev.index, "logits and sampling: one GPU")
+    if dev.index != _current_gpu():
+        return _there(dev.index, fs_sample, logits, u, sampling, token, logprob, kept, ws, err, check)
     like = u if u.shape[0] == n else u[:n]
 
     def output(t, dtype, name):
@@ -460,6 +483,6 @@ def fs_sample(logits, u, sampling: Sampling, token=None, logprob=None, kept=None
     L = _lib()
     ws, wp, wn = _workspace(ws, L.fs_sample_workspace(code, n, V), logits)
     _done(L.fs_sample(code, n, V, logits.data_ptr(), stride[0] if n > 1 else V,
-                      sampling.ref, up, tp, lp, kp, wp, wn, err.data_ptr(), _stream(logits)),
+                      sampling.ref, up, tp, lp, kp, wp, wn, err.data_ptr(), _raw_stream(dev.index)),
           "fs_sample", err, check)
     return token, logprob, kept

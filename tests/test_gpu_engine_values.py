@@ -112,3 +112,43 @@ def test_a_window_beyond_32_bits_is_none(lens):
         with pytest.raises(fs.FairServeError) as e:
             fs.fs_paged_attention(step, cache, q, 0.2, window=window)
         assert e.value.code == fs.FS_E_ARG
+
+
+def test_calls_go_to_their_tensors_gpu(monkeypatch):
+    """With another GPU current, each call makes its tensors' own one current: the handle of a
+    default stream names no GPU.  (One GPU is enough to see that the call asks for it.)"""
+    g = gen(7)
+    k, v, table = make_cache(g, [30, 9], 2, 64, 16, BF)
+    step, cache = step_of([1, 2], [30, 9]), on_gpu(k, v, table)
+    qkv = normal(g, 3, 8, 64).cuda()
+    q, kn, vn = qkv[:, :4], qkv[:, 4:6], qkv[:, 6:]
+    x, w = normal(g, 3, 64).cuda(), normal(g, 72, 64).cuda()
+    ad = fs.Adapters(normal(g, 1, 8, 64).cuda(), normal(g, 1, 72, 8).cuda(),
+                     torch.tensor([0, -1], dtype=torch.int32).cuda())
+    rope = fs.Rope(torch.ones(32).cuda())
+    err = fs.cleared_err_word()
+    calls = (lambda: fs.fs_adapter_linear(step, ad, x, w, err=err, check=False),
+             lambda: fs.fs_rope_append(step, cache, rope, q, kn, vn, err=err, check=False),
+             lambda: fs.fs_paged_attention(step, cache, q, 0.1, err=err, check=False),
+             lambda: fs.fs_sample(x, torch.rand(3).cuda() * 0, fs.Sampling(), err=err, check=False)[0],
+             lambda: fs.fs_clear_status(err))
+    want = [c() for c in calls]
+    entered, current, device = [], [0], torch.cuda.device
+
+    class Spy(device):
+        def __enter__(self):
+            entered.append(self.idx)
+            current[0] = self.idx
+            return super().__enter__()
+
+        def __exit__(self, *a):
+            current[0] = 1
+            return super().__exit__(*a)
+
+    monkeypatch.setattr(fs.engine, "_current_gpu", lambda: current[0], raising=False)
+    monkeypatch.setattr(torch.cuda, "device", Spy)
+    for i, c in enumerate(calls):
+        current[0], entered[:] = 1, []
+        got = c()
+        assert entered == [0], (i, entered)
+        assert got is None or torch.equal(got, want[i]), i
