@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(256) k_rope_append(RopeArgs a) {
       const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
       const int32_t p = kv - (__ldg(a.q_off + s + 1) - t);
       int64_t at = -1;
-      if (p >= 0) {
+      if (p >= 0 && !code) {  // a length that is none says nothing of a token's place
         const uint32_t id = __ldg(a.c.table + s * a.c.table_stride + (p >> a.c.page_shift));
         if (id < a.c.n_pages)
           at = row_at(a.c, id, p, 0, code);
