@@ -63,6 +63,8 @@ __device__ inline f32x16 mfma_32x32x16(s16x8 a, s16x8 b, f32x16 c) {
 // Counted by vmcnt, in order; wait_loads() before use.  Written out because the compiler
 // would wait for all such loads before any LDS read.  No register is loaded: nothing of
 // the wave's own can be overwritten while it is under way.
+// (m0 is reserved: the compiler keeps no value of its own there from one statement to the
+// next, and wants it on no list of clobbered registers.)
 __device__ inline void load_to_lds(const void *base, uint32_t offset, uint32_t at) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at),
                "v"(offset), "s"(base)
