@@ -12,9 +12,11 @@
  * kept, bit-deterministic results) with one difference: a step makes hundreds of these
  * calls, so they RAISE the device status word `err` and do not clear it.  One word
  * collects a whole step; the caller clears it with fs_clear_status before the step and
- * reads it with fs_sync_status after.  Every index read from device memory is checked
- * before it is used as an address, so a wrong one ends in FS_E_RANGE, not in a fault;
- * outputs are unspecified after an error.
+ * reads it with fs_sync_status after.  Every index read from device memory (page and
+ * adapter ids, ranks, cached lengths) is checked before it is used as an address, so a wrong
+ * one ends in FS_E_RANGE, not in a fault; outputs are unspecified after an error.  Not
+ * checked is the device copy of fs_step's q_off, as little as that of fs_trace's rep_off: it
+ * has to hold the host copy's values, from which grids and workspaces are sized.
  *
  * Every call may be captured into a HIP graph: what a replay may change is device data
  * (kv_len, the page table, adapter ids, sampling parameters); shapes, q_off and max_kv
@@ -35,7 +37,7 @@ typedef enum fs_dtype { FS_BF16 = 0, FS_F16 = 1, FS_F32 = 2 } fs_dtype;
  * the step's token matrices (a chunk of its prompt, one decoded token, or none).
  *   n_seqs   in [0, 65535]; at most 2^24 rows in all
  *   q_off_h  host   [n_seqs+1] int32, q_off_h[0] = 0, non-decreasing
- *   q_off    device [n_seqs+1] int32, same values
+ *   q_off    device [n_seqs+1] int32, same values (the caller's word: they are not compared)
  *   kv_len   device [n_seqs] int32: the request's tokens in the cache once this step's
  *            are appended; row i of its n rows has position kv_len - n + i.  A negative
  *            position marks a padding row: nothing is appended for it and its attention

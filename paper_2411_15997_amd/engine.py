@@ -215,7 +215,8 @@ def _done(code, where, err, check):
 
 class Step:
     """The requests of one engine step: q_off (host sequence and its int32 device copy,
-    made when not given), kv_len [n] int32 on the device and the host bound max_kv."""
+    made when not given; one that is given has to hold the same values, they are not
+    compared), kv_len [n] int32 on the device and the host bound max_kv."""
 
     def __init__(self, q_off_h, q_off=None, kv_len=None, max_kv=0, device="cuda"):
         torch = _torch()
