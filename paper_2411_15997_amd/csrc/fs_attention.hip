@@ -95,6 +95,11 @@ __device__ inline s16x8 pack8(const float *p) {
 // that its sums are seldom scaled; probabilities then reach 2^kSlack, which costs no
 // precision.
 constexpr float kSlack = 8.f;
+// In half precision the exponentials count in units of 2^-kLift (sums and products alike, so
+// that it cancels): with kSlack they stay below 2^16, and a probability is lost to the type's
+// smallest number from 2^-32 of the reference on, not from 2^-25.  (No change in time.)
+template <bool BF>
+constexpr float kLift = BF ? 0.f : 7.f;
 
 // The larger of the two halves' values, in both.
 __device__ inline float max_of_halves(float x) {
@@ -115,8 +120,9 @@ __device__ inline float part_factor(float m, float top, float c2) {
 }
 // ln of a row's sum of exponentials: -inf only where nothing was summed (a NaN score makes
 // the sum NaN, one of inf makes it inf).
+template <bool BF>
 __device__ inline float log_sum(float top, float sum, float c2) {
-  return sum == 0.f ? -INFINITY : (top * c2 + __log2f(sum)) * kLn2;
+  return sum == 0.f ? -INFINITY : (top * c2 + (__log2f(sum) - kLift<BF>)) * kLn2;
 }
 
 // ---- few rows: NT tiles of 16 rows, WAVES waves
@@ -243,7 +249,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
           for (int d = 0; d < DB; ++d) o[r][d] *= f;
           m[r] = m2;
         }
-        const float mc = reference(m[r], a.c2);
+        const float mc = reference(m[r], a.c2) - kLift<BF>;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           p[i] = exp2_fast(fmaf(p[i], a.c2, -mc));
@@ -314,7 +320,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
           for (int i = 0; i < 4; ++i) v[i] = to_16<BF>(acc[i] * inv);
           *reinterpret_cast<s16x4 *>(a.out + (q0 + tok) * a.out_stride + h * D + cc) = v;
           if (cc == 0 && a.lse)
-            a.lse[int64_t(q0 + tok) * a.n_heads + h] = log_sum(top, sum, a.c2);
+            a.lse[int64_t(q0 + tok) * a.n_heads + h] = log_sum<BF>(top, sum, a.c2);
         } else {
           const int64_t idx =
               ((int64_t(z) * a.n_seqs + s) * a.few_tokens + tok) * a.n_heads + h;
@@ -480,7 +486,7 @@ __device__ __forceinline__ void attn_chunk(const AttnArgs &a, int block, int z, 
       for (int d = 0; d < DB; ++d) o[d] *= f;
       m = m2;
     }
-    const float mc = reference(m, a.c2);
+    const float mc = reference(m, a.c2) - kLift<BF>;
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -520,7 +526,7 @@ __device__ __forceinline__ void attn_chunk(const AttnArgs &a, int block, int z, 
         *reinterpret_cast<s16x4 *>(op + d * 32 + i * 8 + h2 * 4) = v;
       }
     if (h2 == 0 && a.lse)
-      a.lse[int64_t(q0 + tok) * a.n_heads + h] = log_sum(m, l, a.c2);
+      a.lse[int64_t(q0 + tok) * a.n_heads + h] = log_sum<BF>(m, l, a.c2);
   } else {
     const int64_t idx = (int64_t(z) * a.rows + q0 + tok) * a.n_heads + h;
     float *op = a.chunk_o + idx * D;
@@ -597,7 +603,7 @@ __device__ inline void put_joined(const AttnArgs &a, int64_t t, int32_t h, int c
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = to_16<BF>(acc[i] * inv);
   *reinterpret_cast<s16x4 *>(a.out + t * a.out_stride + h * D + c * 4) = v;
-  if (c == 0 && a.lse) a.lse[t * a.n_heads + h] = log_sum(top, sum, a.c2);
+  if (c == 0 && a.lse) a.lse[t * a.n_heads + h] = log_sum<BF>(top, sum, a.c2);
 }
 
 // Few rows, often many splits: a work-group for a row and head, the splits side by side.

@@ -152,3 +152,32 @@ def test_calls_go_to_their_tensors_gpu(monkeypatch):
         got = c()
         assert entered == [0], (i, entered)
         assert got is None or torch.equal(got, want[i]), i
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows,D", [(1, 128), (1, 64), (70, 128), (70, 64)])
+def test_many_small_probabilities_are_not_lost(rows, D, dtype):
+    """One key of weight 1 and value 0, and 1,000 of weight 2^-26 and value 64: all of the result
+    is theirs.  The bound: a probability of half precision counts in units of 2^-31, and is
+    rounded to half of that; a result to its own unit; sums of fp32; 2^-20 for exponentials."""
+    n, small = 1000, 2.0 ** -26
+    kv = [n + 1 + rows - 1]
+    k, v, table = make_cache(gen(9), kv, 1, D, 16, dtype)
+    for j in range(kv[0]):
+        at = (int(table[0, j // 16]), 0, j % 16)
+        k[at], v[at] = 0.0, 64.0
+        k[at][0] = -13.0
+        if j == 0:
+            k[at][0], v[at] = 13.0, 0.0
+    q = torch.zeros(rows, 1, D, dtype=dtype)
+    q[:, 0, 0] = 1.0
+    out, lse = fs.fs_paged_attention(step_of([rows], kv), on_gpu(k, v, table), q.cuda(), math.log(2.0),
+                                     want_lse=True)
+    count = torch.arange(n, n + rows, dtype=torch.float64)[:, None, None]
+    want = (64 * small * count / (1 + small * count)).expand(rows, 1, D)
+    u = ref.U16[dtype]
+    off = 2.0 ** -32 if dtype == HF else u * small
+    rel = u + 2 * 30 * ref.E32 + (n + rows) * ref.E32 + 2.0 ** -20
+    within(out, want, want * rel + 64 * count * off + ref.TINY[dtype], "out")
+    within(lse[:, 0], 13 * math.log(2.0) + torch.log1p(small * count[:, 0, 0]),
+           torch.full((rows,), 2 * 30 * ref.E32 + (n + rows) * ref.E32 + 2.0 ** -20), "lse")
