@@ -83,6 +83,12 @@ __device__ inline int tile_at(int r, int c) {
     return r * 64 + ((c ^ (((r >> 1) & 1) << 2 | ((r >> 2) & 3))) * 8);
 }
 
+// Probabilities enter the second product in 16 bits.  Up to 32 few rows, where the bytes of the
+// cache are the bound, as the sum of two values: the error against 64 bits is that of rounding
+// the result alone (64 requests of up to 16,384 tokens 122.4 us, 122.0 with one value; 32
+// requests of 32 rows 119 and 118).  In k_attn_chunk and for more few rows as one value, with
+// 1.1 to 1.4 times that error: a second product would take 4,096 rows over 32,768 keys from
+// 1.92 to 2.65 ms, 24 mixed requests from 89 to 113 us, 32 of 64 rows from 180 to 192.
 template <bool BF>
 __device__ inline s16x8 pack8(const float *p) {
   s16x8 v;
@@ -133,6 +139,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
   constexpr int CH = D / 8;   // 16-byte chunks of a key row
   constexpr int RW = 64 / CH, LD = 32 / RW;  // rows of a wave's load, loads of 32 keys' K (or V)
   constexpr int kIds = 512;   // page ids kept in LDS
+  constexpr bool kTwoParts = NT <= 2;  // of a probability
   auto kv_lds = reinterpret_cast<short(*)[2][32 * D]>(lds);  // a wave's K and V
   __shared__ float wm[WAVES][NT * 16], wl[WAVES][NT * 16];
   __shared__ uint32_t ids[kIds];
@@ -226,7 +233,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
 #pragma unroll
           for (int r = 0; r < NT; ++r) sc[r][b] = mfma_16x16x32<BF>(kf, qf[r][k], sc[r][b]);
         }
-      s16x8 pf[NT];
+      s16x8 pf[NT], pl[NT];
 #pragma unroll
       for (int r = 0; r < NT; ++r) {
         float p[8], top = -INFINITY;
@@ -256,6 +263,9 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
           l[r] += p[i];
         }
         pf[r] = pack8<BF>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (kTwoParts) pl[r][i] = to_16<BF>(p[i] - to_f32<BF>(pf[r][i]));
       }
       // keys 4 g4 .. + 3 and 16 + 4 g4 .. + 3 of the tile, 16 columns at a time
 #pragma unroll
@@ -265,7 +275,10 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
         const s16x4 v1 = read_tr(vb + tile_at<D>(row + 16, col >> 3) + (col & 7));
         const s16x8 vv = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-        for (int r = 0; r < NT; ++r) o[r][d] = mfma_16x16x32<BF>(vv, pf[r], o[r][d]);
+        for (int r = 0; r < NT; ++r) {
+          o[r][d] = mfma_16x16x32<BF>(vv, pf[r], o[r][d]);
+          if (kTwoParts) o[r][d] = mfma_16x16x32<BF>(vv, pl[r], o[r][d]);
+        }
       }
       if (t + 1 < tiles) {
         reads_done();

@@ -99,6 +99,26 @@ def test_rows_without_a_key_are_empty_and_nothing_else():
     assert bool((lse[5] == -math.inf).all())
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("lens,H,HK,D", [([1, 1], 4, 1, 128), ([1, 3], 16, 2, 64), ([4, 2], 8, 1, 128)])
+def test_few_rows_keep_their_probabilities_to_two_parts(lens, H, HK, D, dtype):
+    """Up to 32 rows: no rounding of a probability to 16 bits shows, only one of what a first
+    rounding left (u^2) and the result's own."""
+    g = gen(D + H)
+    kv = [40, 33]
+    k, v, table = make_cache(g, kv, HK, D, 16, dtype)
+    q = normal(g, sum(lens), H, D, dtype=dtype)
+    q_off = offsets(lens)
+    want, tol, _, _ = ref.attention(q, k, v, table, q_off, kv, D ** -0.5, 0)
+    u = ref.U16[dtype]
+    mag, _, _, _ = ref.attention(q, k, v.abs(), table, q_off, kv, D ** -0.5, 0)
+    # ref's bound has u |out| + (u + rel) (prob |V|): u^2 in the place of the second u
+    bound = tol - (u - u * u) * mag
+    assert bool((bound > 0).all())
+    got = fs.fs_paged_attention(step_of(lens, kv), on_gpu(k, v, table), q.cuda(), D ** -0.5)
+    within(got, want, bound, "out")
+
+
 @pytest.mark.parametrize("lens", [[1, 1], [90, 1]])
 def test_a_window_beyond_32_bits_is_none(lens):
     g = gen(6)
