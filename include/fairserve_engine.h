@@ -153,8 +153,8 @@ fs_status fs_rope_append(const fs_step *s, const fs_kv_cache *c, const fs_rope *
  *   rows times n_heads at most 2^30, n_seqs times n_kv_heads at most 2^20.
  * Scores, softmax statistics and sums are fp32; the probabilities enter the second
  * product as the sum of two values of the cache's dtype (requests of up to 32 rows times
- * query heads of a key/value head, unless others of the call have up to 64) or as one.  Values at positions that a row's mask excludes have to
- * be finite if they lie below kv_len (they meet a probability of 0).
+ * query heads of a key/value head, unless others of the call have up to 64) or as one.
+ * Keys and values that a row does not see do not reach it, whatever they hold.
  * ws: fs_attention_workspace(...) bytes, 256-byte aligned (may be NULL when that is 0). */
 size_t fs_attention_workspace(const fs_step *s, const fs_kv_cache *c, int32_t n_heads,
                               int32_t window);

@@ -131,6 +131,113 @@ __device__ inline float log_sum(float top, float sum, float c2) {
   return sum == 0.f ? -INFINITY : (top * c2 + (__log2f(sum) - kLift<BF>)) * kLn2;
 }
 
+// A value that is not finite meets a probability of 0 in the rows of its tile that do not see
+// it, and 0 times it is NaN.  Rows that end so, where a key that some rows do not see holds
+// such values, are gone through again by whole waves, with the keys they see alone: lane j of
+// 64 takes the score of key j, then each lane sums its own columns.  (4,096 rows over 32,768
+// keys: 115 ms where the newest key is such a one, 2.3 where all rows see it; looking for NaN in
+// the results costs nothing that shows, 2 % with 33 to 64 few rows.)
+__device__ inline bool not_finite(float x) { return !(fabsf(x) < INFINITY); }
+
+// Whether a value of the keys lo .. hi - 1 is not finite, by the whole wave.
+template <bool BF, int D>
+__device__ bool broken_values(const AttnArgs &a, const int32_t *table, uint32_t head, int32_t lo,
+                              int32_t hi) {
+  constexpr short kAll = BF ? 0x7f80 : 0x7c00;  // the exponent of what is not
+  bool any = false;
+  int32_t code = 0;
+  for (int32_t j = lo + int32_t(threadIdx.x & 63); j < hi; j += 64) {
+    const uint64_t at = 2 * row_at(a.c, __ldg(table + (j >> a.c.page_shift)), j, head, code);
+#pragma unroll 4
+    for (int c = 0; c < D / 8; ++c) {
+      const s16x8 v = *reinterpret_cast<const s16x8 *>(a.c.v + at + c * 16);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) any |= (v[i] & kAll) == kAll;
+    }
+  }
+  return __any(any);
+}
+
+// Keys lo .. hi - 1 (each seen) for one row and head, by the whole wave: the exponentials' sum
+// l and reference m, and the products' sums of this lane's columns D / 64 lane .. .
+template <bool BF, int D>
+__device__ void row_by_key(const AttnArgs &a, const int32_t *table, uint32_t head, const short *q,
+                           int32_t lo, int32_t hi, float (&acc)[D / 64], float &m, float &l) {
+  constexpr int N = D / 64;
+  typedef __attribute__((ext_vector_type(N))) short Cols;
+  const int lane = threadIdx.x & 63;
+  int32_t code = 0;
+  m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) acc[i] = 0.f;
+#pragma unroll 1
+  for (int32_t j0 = lo; j0 < hi; j0 += 64) {
+    const int32_t j = min(j0 + lane, hi - 1);
+    const uint64_t at = 2 * row_at(a.c, __ldg(table + (j >> a.c.page_shift)), j, head, code);
+    float s = 0.f;
+#pragma unroll 8
+    for (int c = 0; c < D / 8; ++c) {
+      const s16x8 kv = *reinterpret_cast<const s16x8 *>(a.c.k + at + c * 16);
+      const s16x8 qv = *reinterpret_cast<const s16x8 *>(q + c * 8);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s = fmaf(to_f32<BF>(qv[i]), to_f32<BF>(kv[i]), s);
+    }
+    s = j0 + lane >= hi ? -INFINITY : a.flip ? -s : s;
+    float top = fmaxf(m, s);
+#pragma unroll
+    for (int w = 32; w; w >>= 1) top = fmaxf(top, __shfl_xor(top, w, 64));
+    const float f = part_factor(m, top, a.c2), mc = reference(top, a.c2) - kLift<BF>;
+    const float p = exp2_fast(fmaf(s, a.c2, -mc));
+    float sum = p;
+#pragma unroll
+    for (int w = 32; w; w >>= 1) sum += __shfl_xor(sum, w, 64);
+    l = l * f + sum;
+    m = top;
+#pragma unroll
+    for (int i = 0; i < N; ++i) acc[i] *= f;
+    // (a key past the last is the last one, which the row sees, with a weight of 0)
+#pragma unroll 1
+    for (int k0 = 0; k0 < 64; k0 += 16) {
+      if (j0 + k0 >= hi) break;
+      Cols v[16];
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const uint32_t lo32 = __builtin_amdgcn_readlane(int(at), k0 + k),
+                       hi32 = __builtin_amdgcn_readlane(int(at >> 32), k0 + k);
+        v[k] = reinterpret_cast<const Cols *>(a.c.v + (uint64_t(hi32) << 32 | lo32))[lane];
+      }
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const float pk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(p), k0 + k));
+#pragma unroll
+        for (int i = 0; i < N; ++i) acc[i] = fmaf(pk, to_f32<BF>(v[k][i]), acc[i]);
+      }
+    }
+  }
+}
+
+// The same, written: to out and lse, or as partial results (o, ml) at idx.
+template <bool BF, int D>
+__device__ void put_row_by_key(const AttnArgs &a, const int32_t *table, uint32_t head, int32_t t,
+                               int32_t h, int32_t pos, int32_t lo, int32_t hi, bool single, float *o,
+                               float *ml, int64_t idx) {
+  const int lane = threadIdx.x & 63;
+  float acc[D / 64], top, sum;
+  row_by_key<BF, D>(a, table, head, a.q + t * a.q_stride + h * D,
+                    a.window ? max(lo, pos - a.window + 1) : lo, min(hi, pos + 1), acc, top, sum);
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) {
+    const int col = lane * (D / 64) + i;
+    if (single)
+      a.out[t * a.out_stride + h * D + col] = to_16<BF>(sum > 0.f ? acc[i] / sum : 0.f);
+    else
+      o[idx * D + col] = acc[i];
+  }
+  if (lane) return;
+  if (single && a.lse) a.lse[int64_t(t) * a.n_heads + h] = log_sum<BF>(top, sum, a.c2);
+  if (!single) ml[idx * 2] = top, ml[idx * 2 + 1] = sum;
+}
+
 // ---- few rows: NT tiles of 16 rows, WAVES waves
 template <bool BF, int D, int NT, int WAVES>
 __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *lds) {
@@ -143,6 +250,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
   auto kv_lds = reinterpret_cast<short(*)[2][32 * D]>(lds);  // a wave's K and V
   __shared__ float wm[WAVES][NT * 16], wl[WAVES][NT * 16];
   __shared__ uint32_t ids[kIds];
+  __shared__ uint32_t broken[NT * 16];  // a row to be gone through again
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, g4 = lane >> 4;
   // Work-groups go to the 8 dies in turn: heads fastest, and each split shifts the
@@ -296,6 +404,8 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
     l[t] += __shfl_xor(l[t], 32, 64);
     if (g4 == 0) wm[wave][t * 16 + r16] = m[t], wl[wave][t * 16 + r16] = l[t];
   }
+  bool any = false;
+  if (n > 1 && tid < NT * 16) broken[tid] = 0;
   float *buf = reinterpret_cast<float *>(kv_lds);  // [WAVES][16][D / 2]: half of the columns
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -329,8 +439,9 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
         if (single) {
           const float inv = sum > 0.f ? 1.f / sum : 0.f;
           s16x4 v;
+          acc *= inv;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = to_16<BF>(acc[i] * inv);
+          for (int i = 0; i < 4; ++i) v[i] = to_16<BF>(acc[i]);
           *reinterpret_cast<s16x4 *>(a.out + (q0 + tok) * a.out_stride + h * D + cc) = v;
           if (cc == 0 && a.lse)
             a.lse[int64_t(q0 + tok) * a.n_heads + h] = log_sum<BF>(top, sum, a.c2);
@@ -340,8 +451,28 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
           *reinterpret_cast<f32x4 *>(a.few_o + idx * D + cc) = acc;
           if (cc == 0) a.few_ml[idx * 2] = top, a.few_ml[idx * 2 + 1] = sum;
         }
+        if (n > 1 && !not_finite(sum)) {
+          float zero = 0.f;  // NaN where a result is not finite
+#pragma unroll
+          for (int i = 0; i < 4; ++i) zero = fmaf(acc[i], 0.f, zero);
+          if (zero != 0.f) broken[tr] = 1, any = true;
+        }
       }
     }
+  }
+  if (n == 1 || !__syncthreads_or(any)) return;  // (one token's rows see every key)
+  if (!broken_values<BF, D>(a, table, head, max(lo, kv - n + 1), hi) &&
+      !(a.window && broken_values<BF, D>(a, table, head, lo, min(hi, kv - a.window))))
+    return;
+  wait_own<0>();  // what was stored above comes first
+  __syncthreads();
+#pragma unroll 1
+  for (int r = wave; r < R; r += WAVES) {
+    if (!broken[r]) continue;
+    const int tok = r / G, h = hk * G + (r - tok * G);
+    put_row_by_key<BF, D>(a, table, head, q0 + tok, h, kv - n + tok, lo, hi, single, a.few_o,
+                          a.few_ml,
+                          ((int64_t(z) * a.n_seqs + s) * a.few_tokens + tok) * a.n_heads + h);
   }
 }
 
@@ -427,6 +558,7 @@ __device__ __forceinline__ void attn_chunk(const AttnArgs &a, int block, int z, 
   }
   f32x16 o[DB] = {};
   float m = -INFINITY, l = 0.f;
+  bool hidden = false;  // from some row of the wave, some key
 
   // This lane's row and 16-byte chunk of each of the wave's loads, RW rows at a time.
   int32_t lrow[LD];
@@ -478,6 +610,7 @@ __device__ __forceinline__ void attn_chunk(const AttnArgs &a, int block, int z, 
             sc[c]);
     // keys that some row of the wave does not see
     if (j0 + 63 > pos_lo || j0 + 64 > hi || j0 <= win_hi) {
+      hidden = true;
 #pragma unroll
       for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -525,31 +658,53 @@ __device__ __forceinline__ void attn_chunk(const AttnArgs &a, int block, int z, 
   }
   raise_err(a.err, code);
   l += __shfl_xor(l, 32, 64);
-  if (row >= R) return;
-  if (single) {
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    short *op = a.out + (q0 + tok) * a.out_stride + h * D;
+  float zero = 0.f;  // NaN once a result is not finite
+  if (row < R) {
+    if (single) {
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      short *op = a.out + (q0 + tok) * a.out_stride + h * D;
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
+      for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s16x4 v;
+        for (int i = 0; i < 4; ++i) {
+          s16x4 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = to_16<BF>(o[d][i * 4 + e] * inv);
-        *reinterpret_cast<s16x4 *>(op + d * 32 + i * 8 + h2 * 4) = v;
-      }
-    if (h2 == 0 && a.lse)
-      a.lse[int64_t(q0 + tok) * a.n_heads + h] = log_sum<BF>(m, l, a.c2);
-  } else {
-    const int64_t idx = (int64_t(z) * a.rows + q0 + tok) * a.n_heads + h;
-    float *op = a.chunk_o + idx * D;
+          for (int e = 0; e < 4; ++e) {
+            const float x = o[d][i * 4 + e] * inv;
+            zero = fmaf(x, 0.f, zero);
+            v[e] = to_16<BF>(x);
+          }
+          *reinterpret_cast<s16x4 *>(op + d * 32 + i * 8 + h2 * 4) = v;
+        }
+      if (h2 == 0 && a.lse)
+        a.lse[int64_t(q0 + tok) * a.n_heads + h] = log_sum<BF>(m, l, a.c2);
+    } else {
+      const int64_t idx = (int64_t(z) * a.rows + q0 + tok) * a.n_heads + h;
+      float *op = a.chunk_o + idx * D;
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
+      for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<f32x4 *>(op + d * 32 + i * 8 + h2 * 4) =
-            f32x4{o[d][i * 4], o[d][i * 4 + 1], o[d][i * 4 + 2], o[d][i * 4 + 3]};
-    if (h2 == 0) a.chunk_ml[idx * 2] = m, a.chunk_ml[idx * 2 + 1] = l;
+        for (int i = 0; i < 4; ++i) {
+          const f32x4 x = {o[d][i * 4], o[d][i * 4 + 1], o[d][i * 4 + 2], o[d][i * 4 + 3]};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) zero = fmaf(x[e], 0.f, zero);
+          *reinterpret_cast<f32x4 *>(op + d * 32 + i * 8 + h2 * 4) = x;
+        }
+      if (h2 == 0) a.chunk_ml[idx * 2] = m, a.chunk_ml[idx * 2 + 1] = l;
+    }
+  }
+  if (!hidden) return;
+  uint64_t again = __ballot(zero != 0.f && !not_finite(l));
+  again = (again | again >> 32) & 0xffffffffu;  // rows of the wave
+  if (!again || !(broken_values<BF, D>(a, table, head, max(lo, pos_lo + 1), hi) ||
+                  (a.window && broken_values<BF, D>(a, table, head, lo, min(hi, win_hi + 1)))))
+    return;
+  wait_own<0>();  // what was stored above comes first
+#pragma unroll 1
+  for (; again; again &= again - 1) {
+    const int r = r0 + wave * 32 + __builtin_ctzll(again), t = r / G, hh = hk * G + (r - t * G);
+    put_row_by_key<BF, D>(a, table, head, q0 + t, hh, kv - n + t, lo, hi, single, a.chunk_o,
+                          a.chunk_ml, (int64_t(z) * a.rows + q0 + t) * a.n_heads + hh);
   }
 }
 

@@ -201,3 +201,47 @@ def test_many_small_probabilities_are_not_lost(rows, D, dtype):
     within(out, want, want * rel + 64 * count * off + ref.TINY[dtype], "out")
     within(lse[:, 0], 13 * math.log(2.0) + torch.log1p(small * count[:, 0, 0]),
            torch.full((rows,), 2 * 30 * ref.E32 + (n + rows) * ref.E32 + 2.0 ** -20), "lse")
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("lens,kv,H,HK,D,window", [
+    ([3, 1], [40, 9], 8, 2, 128, 0),
+    ([5, 7], [3, 60], 4, 4, 64, 0),                     # padding rows
+    ([8, 20], [5000, 900], 8, 4, 64, 0),                # few rows, split
+    ([30, 9], [2500, 70], 4, 2, 128, 1100),             # the same with a window
+    ([16, 2], [100, 300], 16, 4, 128, 0),               # 64 rows
+    ([90, 70], [90, 400], 6, 3, 128, 0),
+    ([150, 2, 1], [3000, 30, 3], 3, 1, 64, 0),          # chunks, split, beside few rows
+    ([150, 2], [3100, 1300], 4, 1, 128, 1050),
+    ([300], [300], 2, 1, 64, 40),
+    ([130, 300], [130, 700], 64, 32, 128, 0),           # 256 rows a work-group
+])
+def test_values_that_are_not_finite_stay_with_the_rows_that_see_them(lens, kv, H, HK, D, window, dtype):
+    """V of NaN or infinities at places that some rows see and others do not."""
+    say("values not finite", lens, kv, H, HK, D, window, dtype)
+    g = gen(D + H + len(lens))
+    k, v, table = make_cache(g, kv, HK, D, 16, dtype)
+    q_off = offsets(lens)
+    q = normal(g, q_off[-1], H, D, dtype=dtype)
+    for s, (n, c) in enumerate(zip(lens, kv)):
+        def put(j, head, cols, value):
+            if 0 <= j < c:
+                v[int(table[s, j // 16]), head, j % 16, cols] = value
+        put(c - 1, 0, slice(3, 4), math.nan)                       # the newest token
+        put(c - 1 - n // 2, HK - 1, slice(0, D), math.inf)         # one of the middle
+        put(c - n // 3, HK - 1, slice(9, 11), -math.inf)
+        if window:
+            put(c - n - window + 2, 0, slice(20, 30), math.nan)    # in the first rows' windows alone
+    want, tol, lse, ltol = ref.attention(q, k, v, table, q_off, kv, D ** -0.5, window)
+    out = torch.full((q_off[-1], H, D), 99.0, dtype=dtype, device="cuda")
+    out, got = fs.fs_paged_attention(step_of(lens, kv), on_gpu(k, v, table), q.cuda(), D ** -0.5, window,
+                                     out=out, want_lse=True)
+    out = out.double().cpu()
+    fine = torch.isfinite(want)
+    assert bool(fine.any()) and not bool(fine.all())
+    assert not bool(torch.isfinite(out[~fine]).any())
+    within(out[fine], want[fine], tol[fine], "out")
+    some = torch.isfinite(lse)
+    within(got.cpu()[some], lse[some], ltol[some], "lse")
+    again = fs.fs_paged_attention(step_of(lens, kv), on_gpu(k, v, table), q.cuda(), D ** -0.5, window)
+    assert torch.equal(again.double().cpu()[fine], out[fine])
