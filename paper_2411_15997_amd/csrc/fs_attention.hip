@@ -6,12 +6,14 @@
 //   k_attn_few    requests of at most 64 rows (single tokens, small chunks): bound by the
 //                 cache's bytes (64 requests of up to 16,384 tokens: 121 us, 4.97 TB/s; one of
 //                 200,001: 80 us and 7 for the join, 5.1 TB/s).  The keys are spread over
-//                 work-groups (splits of up to 1,024) and over the waves of each, which load 32
-//                 keys at a time into LDS of their own and never wait for each other.
+//                 work-groups (splits of 512 to 1,024, more where their results would take too
+//                 much memory; up to 131,072 / head_dim keys whole where the card has a unit
+//                 for each request and head) and over the waves of each, which load 32 keys at
+//                 a time into LDS of their own and never wait for each other.
 //   k_attn_chunk  larger chunks: bound by the waits of a tile's chain (scores, maximum,
 //                 exponentials, products) at two waves a SIMD; the matrix cores are busy for
-//                 half of the cycles (4,096 rows over 32,768 keys, head_dim 128: 1.9 ms, 1.08
-//                 PFLOP/s; head_dim 64: 0.84).  128 or 256 rows a work-group share each tile
+//                 half of the cycles (4,096 rows over 32,768 keys, head_dim 128: 1.91 ms, 1.08
+//                 PFLOP/s, 1.84 to 2.04 ms from card to card; head_dim 64: 0.84 PFLOP/s).  128 or 256 rows a work-group share each tile
 //                 of 64 keys.
 //   k_attn_join_* join the splits' results with their maxima and sums, in split order.
 // Both products run with the keys as rows of the first operand (S^T = K Q^T,
@@ -808,7 +810,7 @@ __global__ void __launch_bounds__(256) k_attn_join_few(AttnArgs a) {
 }
 
 // Many rows, few splits: D / 4 lanes for a row and head.  (1,000 tokens of 32 heads in 2
-// splits, head_dim 128: 10.5 us; with a work-group for each row and head 43.)  A wave holds
+// splits, head_dim 128: 10.8 us; with a work-group for each row and head 43.)  A wave holds
 // several items, whose rows may belong to several requests.
 template <bool BF, int D>
 __global__ void __launch_bounds__(256) k_attn_join_chunk(AttnArgs a) {

@@ -13,10 +13,10 @@
 //                  us).  A work-group takes 16 to 64 columns of y; its four waves share out K
 //                  and join in LDS.
 //   k_linear_tile  more rows: bound by the matrix cores and LDS together.  W and x go through
-//                  LDS in tiles (16,384 x 4,096 x 4,096: 470 to 490 us and the shrink's 38,
-//                  1.1 PFLOP/s, the matrix cores busy for 63 % of the cycles; its loads alone
-//                  take 404 us, its products alone 419).  Eight waves with tiles of 128 x 64
-//                  each read LDS least for a product.
+//                  LDS in tiles (16,384 x 4,096 x 4,096: 467 us and the shrink's 37, 487 to
+//                  510 a call from card to card, 1.1 PFLOP/s, the matrix cores busy for 63 %
+//                  of the cycles; its loads alone take 404 us, its products alone 419).  Eight
+//                  waves with tiles of 128 x 64 each read LDS least for a product.
 // W is the first operand (its rows are y's columns), so a lane holds neighbouring columns
 // of one row of y.
 #include "fs_engine.h"

@@ -47,7 +47,7 @@ __device__ inline void turn8(s16x8 &a, s16x8 &b, const float *cs, const float *s
 template <bool BF, bool INTER, bool VEC>
 __global__ void __launch_bounds__(256) k_rope_append(RopeArgs a) {
   __shared__ float cs[kTok][128], sn[kTok][128];
-  __shared__ int64_t slot[kTok];  // byte offset of the token's cache row (head 0), -1: none
+  __shared__ int64_t slot[kTok];  // the token's cache row (head 0), in elements; -1: none
   __shared__ int32_t where[kTok];
   const int32_t t0 = blockIdx.x * kTok;
   const int32_t nt = min(kTok, a.rows - t0);
