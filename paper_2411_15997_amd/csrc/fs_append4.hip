@@ -1,0 +1,336 @@
+// Rotary positions of the step's queries and keys, and the append of its keys and values to
+// a cache held in 4 bits; and the step's rows of such a cache, read back.
+//
+//   (a, b) -> (a cos t - b sin t, b cos t + a sin t) * factor,  t = p * inv_freq[i];
+//   a group x of 32 values: E least with max |x| <= 7 * 2^E, codes of x / 2^E.
+// Keys are turned in fp64 (the angle, its sine and cosine, the products) and rounded to fp32
+// once: next to the border of two codes an error of fp32 would pick the other one, half of the
+// value away, and the cache would hang on the order of operations.  A key value costs two
+// fp64 products, which the card does at half of its fp32 rate.
+#include <type_traits>
+
+#include "fs_cache.h"
+
+namespace fs {
+
+namespace {
+
+struct Append4Args {
+  const int32_t *q_off, *kv_len;
+  int32_t n_seqs, max_kv, rows;
+  DevCache c;
+  DevScales sc;
+  char *kw, *vw;  // the codes, for writing
+  uint8_t *ksw, *vsw;
+  const short *q, *k, *v;
+  short *q_out, *k_out, *v_out;
+  int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride, v_out_stride;
+  const float *inv_freq;
+  const int32_t *pos;
+  float factor;
+  int32_t n_heads, rotary;
+  int32_t *err;
+};
+
+constexpr int kTok = 4;  // tokens per work-group
+
+// A token's place: its cache rows of head 0 (bytes; -1: none) and its position.
+struct Place {
+  int64_t code, scale;
+  int32_t pos;
+};
+// Of row t, by the whole wave.
+__device__ inline Place place_of(const Append4Args &a, int32_t t, int32_t &code) {
+  const int32_t s = seq_of_row(a.q_off, a.n_seqs, t);
+  const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
+  const int32_t p = kv - (__ldg(a.q_off + s + 1) - t);
+  Place w = {-1, -1, p};
+  if (p >= 0 && !code) {  // a length that is none says nothing of a token's place
+    const uint32_t id = __ldg(a.c.table + s * a.c.table_stride + (p >> a.c.page_shift));
+    if (id < a.c.n_pages) {
+      const uint32_t slot = uint32_t(p & ((1 << a.c.page_shift) - 1));
+      w.code = int64_t(id) * a.c.page_stride + int64_t(slot) * a.c.token_stride;
+      w.scale = int64_t(id) * a.sc.page_stride + int64_t(slot) * a.sc.token_stride;
+    } else {
+      code = FS_E_RANGE;
+    }
+  }
+  return w;
+}
+
+// Eight of a group's values, the others with the next three lanes: their codes, and the group's
+// scale byte.
+template <bool BF>
+__device__ inline uint32_t codes8(const float *x, uint32_t &byte) {
+  uint32_t top = 0;  // of the absolute values' bits: what is not finite is above all others
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+  top = max(top, uint32_t(__shfl_xor(int(top), 1, 64)));
+  top = max(top, uint32_t(__shfl_xor(int(top), 2, 64)));
+  if (top >= 0x7f800000u) {
+    byte = 255;
+    return 0;
+  }
+  // top = f 2^e <= 7 * 2^E = 1.75 * 2^(E + 2)
+  const int32_t e = int32_t(top >> 23) - 2 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
+  byte = uint32_t(min(max(e, 1), int32_t(kTopScale<BF>)));
+  const float unit = __uint_as_float(byte << 23);
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], unit, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], unit, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], unit, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], unit, 3);
+  return w;
+}
+
+// Element d of a row turned: x with the other element of its pair.
+template <class F, bool INTER>
+__device__ inline float turned(int d, int half, float x, float other, const double *cs,
+                               const double *sn) {
+  const int f = INTER ? d >> 1 : d < half ? d : d - half;
+  const bool second = INTER ? d & 1 : d >= half;
+  const F c = F(cs[f]), s = F(sn[f]);
+  return float(second ? F(x) * c + F(other) * s : F(x) * c - F(other) * s);
+}
+
+// VEC: pairs lie in whole 16-byte chunks (rotary_dim a multiple of 16, or of 8 when
+// interleaved).  A key's chunk is turned by one lane, which reads the chunk of the pairs' other
+// elements too; queries may be turned in place, so there a lane takes both (one pair or one
+// element per item without VEC).
+template <bool BF, bool INTER, bool VEC>
+__global__ void __launch_bounds__(256) k_rope_append4(Append4Args a) {
+  __shared__ double cs[kTok][128], sn[kTok][128];
+  __shared__ Place place[kTok];
+  const int32_t t0 = blockIdx.x * kTok;
+  const int32_t nt = min(kTok, a.rows - t0);
+  const int tid = threadIdx.x;
+  // a wave for each token
+  if (tid >> 6 < nt) {
+    const int32_t i = tid >> 6, t = t0 + i;
+    int32_t code = 0;
+    Place w = place_of(a, t, code);
+    if ((tid & 63) == 0) {
+      w.pos = a.pos ? __ldg(a.pos + t) : max(w.pos, 0);
+      place[i] = w;
+      raise_err(a.err, code);
+    }
+  }
+  __syncthreads();
+  const int half = a.rotary / 2, D = a.c.head_dim, HK = a.c.n_kv_heads;
+  for (int i = tid; i < nt * half; i += 256) {
+    const int tok = i / half, f = i - tok * half;
+    double sv, cv;
+    sincos(double(place[tok].pos) * double(__ldg(a.inv_freq + f)), &sv, &cv);
+    cs[tok][f] = cv * double(a.factor);
+    sn[tok][f] = sv * double(a.factor);
+  }
+  __syncthreads();
+
+  const int CH = D / 8;  // 8-element chunks of a head
+  const int kv_items = HK * CH;
+  const int q_turned = VEC ? (INTER ? a.rotary / 8 : a.rotary / 16) : half;
+  const int per = q_turned + (VEC ? (D - a.rotary) / 8 : D - a.rotary);
+  const int q_items = a.n_heads * per, all_kv = nt * 2 * kv_items;
+  for (int it = tid; it < all_kv + nt * q_items; it += 256) {
+    // keys and values of all tokens first: a group is four neighbouring lanes' (CH is a multiple of 4)
+    const bool kv = it < all_kv;
+    const int tok = kv ? it / (2 * kv_items) : (it - all_kv) / q_items;
+    const int64_t t = t0 + tok;
+    const double *c = cs[tok], *s = sn[tok];
+    if (kv) {
+      const int r0 = it - tok * 2 * kv_items;
+      const Place at = place[tok];
+      if (at.code < 0) continue;
+      const bool val = r0 >= kv_items;
+      const int r = val ? r0 - kv_items : r0, h = r / CH, ch = r - h * CH;
+      const short *row = (val ? a.v + t * a.v_stride : a.k + t * a.k_stride) + h * D;
+      const s16x8 v = *reinterpret_cast<const s16x8 *>(row + ch * 8);
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = to_f32<BF>(v[i]);
+      if (!val && ch * 8 < a.rotary) {
+        if constexpr (INTER) {
+#pragma unroll
+          for (int i = 0; i < 8; i += 2)
+            if (VEC || ch * 8 + i < a.rotary) {
+              const float p = x[i], q = x[i + 1];
+              x[i] = turned<double, INTER>(ch * 8 + i, half, p, q, c, s);
+              x[i + 1] = turned<double, INTER>(ch * 8 + i + 1, half, q, p, c, s);
+            }
+        } else if constexpr (VEC) {
+          const s16x8 o = *reinterpret_cast<const s16x8 *>(
+              row + (ch * 8 < half ? ch * 8 + half : ch * 8 - half));
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            x[i] = turned<double, INTER>(ch * 8 + i, half, x[i], to_f32<BF>(o[i]), c, s);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int d = ch * 8 + i;
+            if (d < a.rotary)
+              x[i] = turned<double, INTER>(d, half, x[i],
+                                           to_f32<BF>(row[d < half ? d + half : d - half]), c, s);
+          }
+        }
+      }
+      uint32_t byte;
+      const uint32_t w = codes8<BF>(x, byte);
+      *reinterpret_cast<uint32_t *>((val ? a.vw : a.kw) + at.code + int64_t(h) * a.c.head_stride +
+                                    ch * 4) = w;
+      if ((ch & 3) == 0)
+        ((val ? a.vsw : a.ksw) + at.scale + int64_t(h) * a.sc.head_stride)[ch >> 2] = uint8_t(byte);
+      continue;
+    }
+    const int r = it - all_kv - tok * q_items, h = r / per, j = r - h * per;
+    const short *src = a.q + t * a.q_stride + h * D;
+    short *dst = a.q_out + t * a.q_out_stride + h * D;
+    if constexpr (VEC) {
+      if (j >= q_turned) {
+        const int e = a.rotary + (j - q_turned) * 8;
+        *reinterpret_cast<s16x8 *>(dst + e) = *reinterpret_cast<const s16x8 *>(src + e);
+      } else if constexpr (INTER) {
+        const s16x8 x = *reinterpret_cast<const s16x8 *>(src + 8 * j);
+        s16x8 y;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          y[i] = to_16<BF>(turned<float, INTER>(8 * j + i, half, to_f32<BF>(x[i]),
+                                                to_f32<BF>(x[i ^ 1]), c, s));
+        *reinterpret_cast<s16x8 *>(dst + 8 * j) = y;
+      } else {
+        const s16x8 x = *reinterpret_cast<const s16x8 *>(src + 8 * j);
+        const s16x8 y = *reinterpret_cast<const s16x8 *>(src + 8 * j + half);
+        s16x8 u, w;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float p = to_f32<BF>(x[i]), q = to_f32<BF>(y[i]);
+          u[i] = to_16<BF>(turned<float, INTER>(8 * j + i, half, p, q, c, s));
+          w[i] = to_16<BF>(turned<float, INTER>(8 * j + i + half, half, q, p, c, s));
+        }
+        *reinterpret_cast<s16x8 *>(dst + 8 * j) = u;
+        *reinterpret_cast<s16x8 *>(dst + 8 * j + half) = w;
+      }
+    } else if (j >= q_turned) {
+      dst[a.rotary + j - q_turned] = src[a.rotary + j - q_turned];
+    } else {
+      const int e0 = INTER ? 2 * j : j, e1 = INTER ? 2 * j + 1 : j + half;
+      const float p = to_f32<BF>(src[e0]), q = to_f32<BF>(src[e1]);
+      dst[e0] = to_16<BF>(turned<float, INTER>(e0, half, p, q, c, s));
+      dst[e1] = to_16<BF>(turned<float, INTER>(e1, half, q, p, c, s));
+    }
+  }
+}
+
+// What the cache holds at the step's rows.
+template <bool BF>
+__global__ void __launch_bounds__(256) k_cache4_rows(Append4Args a) {
+  __shared__ Place place[kTok];
+  const int32_t t0 = blockIdx.x * kTok;
+  const int32_t nt = min(kTok, a.rows - t0);
+  const int tid = threadIdx.x;
+  if (tid >> 6 < nt) {
+    int32_t code = 0;
+    const Place w = place_of(a, t0 + (tid >> 6), code);
+    if ((tid & 63) == 0) {
+      place[tid >> 6] = w;
+      raise_err(a.err, code);
+    }
+  }
+  __syncthreads();
+  const int D = a.c.head_dim, CH = D / 8, kv_items = a.c.n_kv_heads * CH;
+  for (int it = tid; it < nt * 2 * kv_items; it += 256) {
+    const int tok = it / (2 * kv_items), r0 = it - tok * 2 * kv_items;
+    const bool val = r0 >= kv_items;
+    const int r = val ? r0 - kv_items : r0, h = r / CH, ch = r - h * CH;
+    short *out = val ? a.v_out : a.k_out;
+    if (!out) continue;
+    const Place at = place[tok];
+    s16x8 x = {};
+    if (at.code >= 0) {
+      const uint32_t w = *reinterpret_cast<const uint32_t *>(
+          (val ? a.c.v : a.c.k) + at.code + int64_t(h) * a.c.head_stride + ch * 4);
+      const uint32_t byte =
+          ((val ? a.sc.v : a.sc.k) + at.scale + int64_t(h) * a.sc.head_stride)[ch >> 2];
+      x = values8<BF>(w, scale_of<BF>(byte));
+      if (byte > kTopScale<BF>) x = BF ? 0x7fc0 : 0x7e00;  // NaN
+    }
+    *reinterpret_cast<s16x8 *>(out + int64_t(t0 + tok) * (val ? a.v_out_stride : a.k_out_stride) +
+                               h * D + ch * 8) = x;
+  }
+}
+
+Append4Args step_args(const fs_step *s, const fs_kv_cache4 *c, int32_t *err) {
+  Append4Args a = {};
+  a.q_off = s->q_off;
+  a.kv_len = s->kv_len;
+  a.n_seqs = s->n_seqs;
+  a.max_kv = s->max_kv;
+  a.rows = s->q_off_h[s->n_seqs];
+  a.c = dev_codes(c);
+  a.sc = dev_scales(c);
+  a.kw = static_cast<char *>(c->k);
+  a.vw = static_cast<char *>(c->v);
+  a.ksw = static_cast<uint8_t *>(c->k_scale);
+  a.vsw = static_cast<uint8_t *>(c->v_scale);
+  a.err = err;
+  return a;
+}
+
+}  // namespace
+
+hipError_t launch_rope_append4(const fs_step *s, const fs_kv_cache4 *c, const fs_rope *r,
+                               int32_t dtype, int32_t n_heads, const void *q, int64_t q_stride,
+                               const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                               void *q_out, int64_t q_out_stride, int32_t *err,
+                               hipStream_t stream) {
+  Append4Args a = step_args(s, c, err);
+  a.q = static_cast<const short *>(q);
+  a.k = static_cast<const short *>(k);
+  a.v = static_cast<const short *>(v);
+  a.q_out = static_cast<short *>(q_out);
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.q_out_stride = q_out_stride;
+  a.inv_freq = r->inv_freq;
+  a.pos = r->pos;
+  a.factor = r->factor;
+  a.n_heads = n_heads;
+  a.rotary = r->rotary_dim;
+  const bool inter = r->interleaved != 0;
+  const bool vec = r->rotary_dim % (inter ? 8 : 16) == 0;
+  const dim3 grid((a.rows + kTok - 1) / kTok), block(256);
+  auto go = [&](auto bf) {
+    constexpr bool BF = decltype(bf)::value;
+    if (inter && vec)
+      hipLaunchKernelGGL((k_rope_append4<BF, true, true>), grid, block, 0, stream, a);
+    else if (inter)
+      hipLaunchKernelGGL((k_rope_append4<BF, true, false>), grid, block, 0, stream, a);
+    else if (vec)
+      hipLaunchKernelGGL((k_rope_append4<BF, false, true>), grid, block, 0, stream, a);
+    else
+      hipLaunchKernelGGL((k_rope_append4<BF, false, false>), grid, block, 0, stream, a);
+  };
+  if (dtype == FS_BF16)
+    go(std::true_type());
+  else
+    go(std::false_type());
+  return hipGetLastError();
+}
+
+hipError_t launch_cache4_rows(const fs_step *s, const fs_kv_cache4 *c, int32_t dtype, void *k_out,
+                              int64_t k_stride, void *v_out, int64_t v_stride, int32_t *err,
+                              hipStream_t stream) {
+  Append4Args a = step_args(s, c, err);
+  a.k_out = static_cast<short *>(k_out);
+  a.v_out = static_cast<short *>(v_out);
+  a.k_out_stride = k_stride;
+  a.v_out_stride = v_stride;
+  const dim3 grid((a.rows + kTok - 1) / kTok), block(256);
+  if (dtype == FS_BF16)
+    hipLaunchKernelGGL((k_cache4_rows<true>), grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_cache4_rows<false>), grid, block, 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace fs

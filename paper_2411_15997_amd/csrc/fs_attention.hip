@@ -23,115 +23,11 @@
 // one leaves them; V is read from LDS transposed, in that same order.
 #include <type_traits>
 
-#include "fs_engine.h"
+#include "fs_attn.h"
 
 namespace fs {
 
 namespace {
-
-constexpr int kFewRows = 64;    // rows (tokens times group) that k_attn_few takes
-constexpr int64_t kMostPartial = int64_t(1) << 28;  // bytes of partial results, about
-constexpr float kLn2 = 0.693147180559945309f;
-
-struct AttnArgs {
-  const int32_t *q_off, *kv_len;
-  int32_t n_seqs, max_kv, rows, n_heads, window, group;
-  DevCache c;
-  const short *q;
-  short *out;
-  int64_t q_stride, out_stride;
-  float *lse;
-  float c2;            // |scale| * log2(e)
-  uint32_t flip;       // sign of the scale, applied to the queries
-  int32_t few_split;   // keys of a split (k_attn_few)
-  int32_t few_tokens;  // most tokens of a request that k_attn_few takes
-  int32_t chunk_rows;  // rows of a work-group of k_attn_chunk
-  int32_t chunk_split;
-  float *few_o, *few_ml;      // [splits][n_seqs][few_tokens][heads][D], [..][2]
-  float *chunk_o, *chunk_ml;  // [splits][rows][heads][D], [..][2]
-  int32_t *err;
-};
-
-// Keys that the tokens tok0 .. tok1 of a request with n new and kv cached ones see.
-struct KeyRange {
-  int32_t lo, hi;
-};
-__device__ inline KeyRange key_range(const AttnArgs &a, int32_t n, int32_t kv, int32_t tok0,
-                                     int32_t tok1) {
-  KeyRange r;
-  r.lo = a.window ? max(0, kv - n + tok0 - a.window + 1) : 0;
-  r.hi = max(0, kv - n + tok1 + 1);
-  return r;
-}
-
-__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-// Four keys by sixteen columns of V per 16 lanes, transposed: lane i of the 16 names the
-// 8 bytes (key i / 4, columns 4 (i % 4) ..) and gets column i of the four keys.
-__device__ inline s16x4 read_tr(const short *p) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-      (lds_s16x4 *)(__attribute__((address_space(3))) short *)(p));
-}
-
-// Where 16-byte chunk `c` of key row `r` lies in an LDS tile with D-element rows: chunks
-// are exchanged so that 16 rows' chunks, and 4 rows' transposed reads, fall on different
-// banks.
-template <int D>
-__device__ inline int tile_at(int r, int c) {
-  if constexpr (D == 128)
-    return r * 128 + ((c ^ ((r & 3) << 2 | ((r >> 2) & 3))) * 8);
-  else
-    return r * 64 + ((c ^ (((r >> 1) & 1) << 2 | ((r >> 2) & 3))) * 8);
-}
-
-// Probabilities enter the second product in 16 bits.  Up to 32 few rows, where the bytes of the
-// cache are the bound, as the sum of two values: the error against 64 bits is that of rounding
-// the result alone (64 requests of up to 16,384 tokens 122.4 us, 122.0 with one value; 32
-// requests of 32 rows 119 and 118).  In k_attn_chunk and for more few rows as one value, with
-// 1.1 to 1.4 times that error: a second product would take 4,096 rows over 32,768 keys from
-// 1.92 to 2.65 ms, 24 mixed requests from 89 to 113 us, 32 of 64 rows from 180 to 192.
-template <bool BF>
-__device__ inline s16x8 pack8(const float *p) {
-  s16x8 v;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = to_16<BF>(p[i]);
-  return v;
-}
-
-// A row keeps the reference of its exponentials until a score passes it by 2^kSlack, so
-// that its sums are seldom scaled; probabilities then reach 2^kSlack, which costs no
-// precision.
-constexpr float kSlack = 8.f;
-// In half precision the exponentials count in units of 2^-kLift (sums and products alike, so
-// that it cancels): with kSlack they stay below 2^16, and a probability is lost to the type's
-// smallest number from 2^-32 of the reference on, not from 2^-25.  (No change in time.)
-template <bool BF>
-constexpr float kLift = BF ? 0.f : 7.f;
-
-// The larger of the two halves' values, in both.
-__device__ inline float max_of_halves(float x) {
-  const uint32_t b = __float_as_uint(x);
-  const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-
-// A reference of the exponentials as they use it: 0 while there is none and where it is
-// infinite, so that a score of inf makes the sum inf (inf - inf would make it NaN).
-__device__ inline float reference(float m, float c2) {
-  return fabsf(m) == INFINITY ? 0.f : m * c2;
-}
-// What a part with the maximum m weighs where the largest of the parts' is `top` (inf less
-// inf is no number; a part without a maximum holds sums of 0).
-__device__ inline float part_factor(float m, float top, float c2) {
-  return exp2_fast(m == top ? 0.f : (m - top) * c2);
-}
-// ln of a row's sum of exponentials: -inf only where nothing was summed (a NaN score makes
-// the sum NaN, one of inf makes it inf).
-template <bool BF>
-__device__ inline float log_sum(float top, float sum, float c2) {
-  return sum == 0.f ? -INFINITY : (top * c2 + (__log2f(sum) - kLift<BF>)) * kLn2;
-}
 
 // A value that is not finite meets a probability of 0 in the rows of its tile that do not see
 // it, and 0 times it is NaN.  Rows that end so, where a key that some rows do not see holds
@@ -160,11 +56,35 @@ __device__ bool broken_values(const AttnArgs &a, const int32_t *table, uint32_t 
   return __any(any);
 }
 
-// Keys lo .. hi - 1 (each seen) for one row and head, by the whole wave: the exponentials' sum
+// Keys that one row sees of a split: `first` of them from a0 on, then those of b0 .. .
+struct RowKeys {
+  int32_t a0, first, b0, n;
+  __device__ int32_t key(int32_t i) const { return i < first ? a0 + i : b0 + (i - first); }
+};
+// Those of the places lo .. hi - 1 for the row at `pos` (without sinks places are keys).
+template <bool SINK>
+__device__ RowKeys row_keys(const AttnArgs &a, const KeyRange &kr, int32_t lo, int32_t hi,
+                            int32_t pos) {
+  RowKeys r;
+  if constexpr (!SINK) {
+    r.a0 = r.first = 0;
+    r.b0 = a.window ? max(lo, pos - a.window + 1) : lo;
+    r.n = max(0, min(hi, pos + 1) - r.b0);
+  } else {
+    const int32_t end = lo < hi ? min(kr.key(hi - 1), pos) + 1 : 0;
+    r.a0 = kr.key(lo);
+    r.first = max(0, min(end, a.sinks) - r.a0);
+    r.b0 = max(max(lo < kr.sink ? kr.lo : r.a0, a.sinks), pos - a.window + 1);
+    r.n = r.first + max(0, end - r.b0);
+  }
+  return r;
+}
+
+// The keys `keys` (each seen) for one row and head, by the whole wave: the exponentials' sum
 // l and reference m, and the products' sums of this lane's columns D / 64 lane .. .
 template <bool BF, int D>
 __device__ void row_by_key(const AttnArgs &a, const int32_t *table, uint32_t head, const short *q,
-                           int32_t lo, int32_t hi, float (&acc)[D / 64], float &m, float &l) {
+                           const RowKeys &keys, float (&acc)[D / 64], float &m, float &l) {
   constexpr int N = D / 64;
   typedef __attribute__((ext_vector_type(N))) short Cols;
   const int lane = threadIdx.x & 63;
@@ -173,8 +93,8 @@ __device__ void row_by_key(const AttnArgs &a, const int32_t *table, uint32_t hea
 #pragma unroll
   for (int i = 0; i < N; ++i) acc[i] = 0.f;
 #pragma unroll 1
-  for (int32_t j0 = lo; j0 < hi; j0 += 64) {
-    const int32_t j = min(j0 + lane, hi - 1);
+  for (int32_t j0 = 0; j0 < keys.n; j0 += 64) {
+    const int32_t j = keys.key(min(j0 + lane, keys.n - 1));
     const uint64_t at = 2 * row_at(a.c, __ldg(table + (j >> a.c.page_shift)), j, head, code);
     float s = 0.f;
 #pragma unroll 8
@@ -184,7 +104,7 @@ __device__ void row_by_key(const AttnArgs &a, const int32_t *table, uint32_t hea
 #pragma unroll
       for (int i = 0; i < 8; ++i) s = fmaf(to_f32<BF>(qv[i]), to_f32<BF>(kv[i]), s);
     }
-    s = j0 + lane >= hi ? -INFINITY : a.flip ? -s : s;
+    s = j0 + lane >= keys.n ? -INFINITY : a.flip ? -s : s;
     float top = fmaxf(m, s);
 #pragma unroll
     for (int w = 32; w; w >>= 1) top = fmaxf(top, __shfl_xor(top, w, 64));
@@ -200,7 +120,7 @@ __device__ void row_by_key(const AttnArgs &a, const int32_t *table, uint32_t hea
     // (a key past the last is the last one, which the row sees, with a weight of 0)
 #pragma unroll 1
     for (int k0 = 0; k0 < 64; k0 += 16) {
-      if (j0 + k0 >= hi) break;
+      if (j0 + k0 >= keys.n) break;
       Cols v[16];
 #pragma unroll
       for (int k = 0; k < 16; ++k) {
@@ -221,12 +141,11 @@ __device__ void row_by_key(const AttnArgs &a, const int32_t *table, uint32_t hea
 // The same, written: to out and lse, or as partial results (o, ml) at idx.
 template <bool BF, int D>
 __device__ void put_row_by_key(const AttnArgs &a, const int32_t *table, uint32_t head, int32_t t,
-                               int32_t h, int32_t pos, int32_t lo, int32_t hi, bool single, float *o,
-                               float *ml, int64_t idx) {
+                               int32_t h, const RowKeys &keys, bool single, float *o, float *ml,
+                               int64_t idx) {
   const int lane = threadIdx.x & 63;
   float acc[D / 64], top, sum;
-  row_by_key<BF, D>(a, table, head, a.q + t * a.q_stride + h * D,
-                    a.window ? max(lo, pos - a.window + 1) : lo, min(hi, pos + 1), acc, top, sum);
+  row_by_key<BF, D>(a, table, head, a.q + t * a.q_stride + h * D, keys, acc, top, sum);
 #pragma unroll
   for (int i = 0; i < D / 64; ++i) {
     const int col = lane * (D / 64) + i;
@@ -236,12 +155,14 @@ __device__ void put_row_by_key(const AttnArgs &a, const int32_t *table, uint32_t
       o[idx * D + col] = acc[i];
   }
   if (lane) return;
-  if (single && a.lse) a.lse[int64_t(t) * a.n_heads + h] = log_sum<BF>(top, sum, a.c2);
+  if (single && a.lse) a.lse[int64_t(t) * a.n_heads + h] = log_sum(top, sum, a.c2, kLift<BF>);
   if (!single) ml[idx * 2] = top, ml[idx * 2 + 1] = sum;
 }
 
-// ---- few rows: NT tiles of 16 rows, WAVES waves
-template <bool BF, int D, int NT, int WAVES>
+// ---- few rows: NT tiles of 16 rows, WAVES waves.  SINK: the first keys stay visible beyond a
+// window; lo, hi and what counts between them are then places of the keys seen (KeyRange), and
+// a tile may hold the last sinks beside the window's first keys.
+template <bool BF, int D, int NT, int WAVES, bool SINK>
 __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *lds) {
   constexpr int KS = D / 32;  // matrix steps of a score
   constexpr int DB = D / 16;  // 16-column blocks of an output row
@@ -265,10 +186,12 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
   int32_t code = 0;
   const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
   const KeyRange kr = key_range(a, n, kv, 0, n - 1);
-  const bool single = kr.hi - kr.lo <= a.few_split;
-  const int32_t lo = kr.lo + z * a.few_split;
-  if (z > 0 && lo >= kr.hi) return;
-  const int32_t hi = min(kr.hi, lo + a.few_split);
+  const int32_t from0 = SINK ? 0 : kr.lo, to0 = SINK ? kr.length() : kr.hi;
+  const bool single = to0 - from0 <= a.few_split;
+  const int32_t lo = from0 + z * a.few_split;
+  if (z > 0 && lo >= to0) return;
+  const int32_t hi = min(to0, lo + a.few_split);
+  auto key = [&](int32_t place) { return SINK ? kr.key(place) : place; };
   const int32_t *table = a.c.table + s * a.c.table_stride;
   const uint32_t head = hk * a.c.head_stride;
 
@@ -301,13 +224,13 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
   }
   const uint32_t to = lds_address(kv_lds[wave][0]);
 
-  // the page ids of up to kIds pages at a time
+  // the ids of up to kIds pages at a time
   for (int32_t from = lo; from < hi;) {
-    const int32_t p0 = from >> a.c.page_shift;
-    const int32_t end = int32_t(min(int64_t(hi), int64_t(p0 + kIds) << a.c.page_shift));
+    const PageIds span = page_ids<SINK>(kr, from, hi, a.c.page_shift, kIds);
+    const int32_t end = span.end;
     __syncthreads();
-    for (int i = tid; i < ((end - 1) >> a.c.page_shift) - p0 + 1; i += WAVES * 64) {
-      const uint32_t page = __ldg(table + p0 + i);
+    for (int i = tid; i < span.n; i += WAVES * 64) {
+      const uint32_t page = __ldg(table + span.page(i));
       if (page >= a.c.n_pages) code = FS_E_RANGE;
       ids[i] = page < a.c.n_pages ? page : 0;
     }
@@ -320,8 +243,8 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
       uint64_t at[LD];
 #pragma unroll
       for (int i = 0; i < LD; ++i) {
-        const int32_t j = min(j0 + i * RW + lane / CH, end - 1);
-        at[i] = 2 * row_at(a.c, ids[(j >> a.c.page_shift) - p0], j, lcol[i], code);
+        const int32_t j = key(min(j0 + i * RW + lane / CH, end - 1));
+        at[i] = 2 * row_at(a.c, ids[span.slot(j)], j, lcol[i], code);
       }
 #pragma unroll
       for (int i = 0; i < LD; ++i) load_to_lds(a.c.k + at[i], to + i * 1024);
@@ -351,8 +274,9 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int32_t j = j0 + b * 16 + g4 * 4 + i;
-            const bool see = j <= pos[r] && j < end && (a.window == 0 || j > pos[r] - a.window);
+            const int32_t v = j0 + b * 16 + g4 * 4 + i, j = key(v);
+            const bool see = j <= pos[r] && v < end &&
+                             (a.window == 0 || j > pos[r] - a.window || (SINK && j < a.sinks));
             p[b * 4 + i] = see ? sc[r][b][i] : -INFINITY;
             top = fmaxf(top, p[b * 4 + i]);
           }
@@ -446,7 +370,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
           for (int i = 0; i < 4; ++i) v[i] = to_16<BF>(acc[i]);
           *reinterpret_cast<s16x4 *>(a.out + (q0 + tok) * a.out_stride + h * D + cc) = v;
           if (cc == 0 && a.lse)
-            a.lse[int64_t(q0 + tok) * a.n_heads + h] = log_sum<BF>(top, sum, a.c2);
+            a.lse[int64_t(q0 + tok) * a.n_heads + h] = log_sum(top, sum, a.c2, kLift<BF>);
         } else {
           const int64_t idx =
               ((int64_t(z) * a.n_seqs + s) * a.few_tokens + tok) * a.n_heads + h;
@@ -463,59 +387,28 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
     }
   }
   if (n == 1 || !__syncthreads_or(any)) return;  // (one token's rows see every key)
-  if (!broken_values<BF, D>(a, table, head, max(lo, kv - n + 1), hi) &&
-      !(a.window && broken_values<BF, D>(a, table, head, lo, min(hi, kv - a.window))))
+  if constexpr (SINK) {  // (all keys of the split: a superset of the hidden ones)
+    if (!broken_values<BF, D>(a, table, head, lo, min(hi, kr.sink)) &&
+        !broken_values<BF, D>(a, table, head, key(max(lo, kr.sink)), key(hi - 1) + 1))
+      return;
+  } else if (!broken_values<BF, D>(a, table, head, max(lo, kv - n + 1), hi) &&
+             !(a.window && broken_values<BF, D>(a, table, head, lo, min(hi, kv - a.window)))) {
     return;
+  }
   wait_own<0>();  // what was stored above comes first
   __syncthreads();
 #pragma unroll 1
   for (int r = wave; r < R; r += WAVES) {
     if (!broken[r]) continue;
     const int tok = r / G, h = hk * G + (r - tok * G);
-    put_row_by_key<BF, D>(a, table, head, q0 + tok, h, kv - n + tok, lo, hi, single, a.few_o,
-                          a.few_ml,
+    put_row_by_key<BF, D>(a, table, head, q0 + tok, h,
+                          row_keys<SINK>(a, kr, lo, hi, kv - n + tok), single, a.few_o, a.few_ml,
                           ((int64_t(z) * a.n_seqs + s) * a.few_tokens + tok) * a.n_heads + h);
   }
 }
 
-// Row tile number b of k_attn_chunk, a request's last rows (which see the most keys) first.
-// Up to 64 requests are taken in the order of the keys they see, the most first, so that
-// the work ends evenly; more in their own order, request s owning the tile numbers from
-// q_off[s] * G / chunk_rows + s on.  r0 < 0: no rows.
-__device__ inline void chunk_tile(const AttnArgs &a, int32_t b, int32_t &s, int32_t &r0) {
-  if (a.n_seqs <= 64) {
-    const int32_t i = min(int32_t(__lane_id()), a.n_seqs - 1);
-    const int32_t n = __ldg(a.q_off + i + 1) - __ldg(a.q_off + i), R = n * a.group;
-    const int32_t kv = __ldg(a.kv_len + i);
-    const int32_t keys = a.window ? min(kv, a.window + n) : kv;
-    const int32_t mine = R > kFewRows ? (R + a.chunk_rows - 1) / a.chunk_rows : 0;
-    int32_t before = 0;
-    for (int j = 0; j < a.n_seqs; ++j) {
-      const int32_t other = __builtin_amdgcn_readlane(keys, j);
-      if (other > keys || (other == keys && j < i)) before += __builtin_amdgcn_readlane(mine, j);
-    }
-    const uint64_t hit =
-        __ballot(int32_t(__lane_id()) < a.n_seqs && before <= b && b < before + mine);
-    if (!hit) {
-      s = 0;
-      r0 = -1;
-      return;
-    }
-    s = __builtin_ctzll(hit);
-    r0 = (__builtin_amdgcn_readlane(mine, s) - 1 - (b - __builtin_amdgcn_readlane(before, s))) *
-         a.chunk_rows;
-    return;
-  }
-  s = last_at_most(a.n_seqs, b, [&](int32_t i) {
-    return __ldg(a.q_off + i) * a.group / a.chunk_rows + i;
-  });
-  const int32_t q0 = __ldg(a.q_off + s), R = (__ldg(a.q_off + s + 1) - q0) * a.group;
-  const int32_t tiles = (R + a.chunk_rows - 1) / a.chunk_rows;
-  r0 = (tiles - 1 - (b - q0 * a.group / a.chunk_rows - s)) * a.chunk_rows;
-}
-
 // ---- chunks: WAVES waves of 32 rows, 64 keys at a time through two buffers
-template <bool BF, int D, int WAVES>
+template <bool BF, int D, int WAVES, bool SINK>
 __device__ __forceinline__ void attn_chunk(const AttnArgs &a, int block, int z, short *lds) {
   constexpr int KS = D / 16;       // matrix steps of a score
   constexpr int DB = D / 32;       // 32-column blocks of an output row
@@ -535,10 +428,12 @@ __device__ __forceinline__ void attn_chunk(const AttnArgs &a, int block, int z, 
   int32_t code = 0;
   const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
   const KeyRange kr = key_range(a, n, kv, r0 / G, (min(r0 + WAVES * 32, R) - 1) / G);
-  const bool single = kr.hi - kr.lo <= a.chunk_split;
-  const int32_t lo = kr.lo + z * a.chunk_split;
-  if (z > 0 && lo >= kr.hi) return;
-  const int32_t hi = min(kr.hi, lo + a.chunk_split);
+  const int32_t from0 = SINK ? 0 : kr.lo, to0 = SINK ? kr.length() : kr.hi;
+  const bool single = to0 - from0 <= a.chunk_split;
+  const int32_t lo = from0 + z * a.chunk_split;
+  if (z > 0 && lo >= to0) return;
+  const int32_t hi = min(to0, lo + a.chunk_split);
+  auto key = [&](int32_t place) { return SINK ? kr.key(place) : place; };
   const int32_t *table = a.c.table + s * a.c.table_stride;
   const uint32_t head = hk * a.c.head_stride;
 
@@ -574,7 +469,7 @@ __device__ __forceinline__ void attn_chunk(const AttnArgs &a, int block, int z, 
   auto pages = [&](int32_t j0) {
 #pragma unroll
     for (int i = 0; i < LD; ++i)
-      page[i] = __ldg(table + (min(j0 + lrow[i], hi - 1) >> a.c.page_shift));
+      page[i] = __ldg(table + (key(min(j0 + lrow[i], hi - 1)) >> a.c.page_shift));
   };
   const uint32_t k_to = lds_address(kt[0] + wave * LD * RW * D),
                  v_to = lds_address(vt[0] + wave * LD * RW * D);
@@ -584,7 +479,8 @@ __device__ __forceinline__ void attn_chunk(const AttnArgs &a, int block, int z, 
     for (int i = 0; i < LD; ++i) asm volatile("" : "+v"(page[i]));
 #pragma unroll
     for (int i = 0; i < LD; ++i) {
-      const uint64_t at = 2 * row_at(a.c, page[i], min(j0 + lrow[i], hi - 1), lcol[i], code);
+      const uint64_t at =
+          2 * row_at(a.c, page[i], key(min(j0 + lrow[i], hi - 1)), lcol[i], code);
       load_to_lds(a.c.k + at, k_to + (buf * 64 + i * RW) * D * 2);
       load_to_lds(a.c.v + at, v_to + (buf * 64 + i * RW) * D * 2);
     }
@@ -611,14 +507,16 @@ __device__ __forceinline__ void attn_chunk(const AttnArgs &a, int block, int z, 
             *reinterpret_cast<const s16x8 *>(kb + tile_at<D>(c * 32 + r32, k * 2 + h2)), qf[k],
             sc[c]);
     // keys that some row of the wave does not see
-    if (j0 + 63 > pos_lo || j0 + 64 > hi || j0 <= win_hi) {
+    if (key(j0 + 63) > pos_lo || j0 + 64 > hi || key(j0) <= win_hi) {
       hidden = true;
 #pragma unroll
       for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int32_t j = j0 + c * 32 + 8 * (i >> 2) + 4 * h2 + (i & 3);
-          if (j > pos || j >= hi || (a.window && j <= pos - a.window)) sc[c][i] = -INFINITY;
+          const int32_t v = j0 + c * 32 + 8 * (i >> 2) + 4 * h2 + (i & 3), j = key(v);
+          if (j > pos || v >= hi ||
+              (a.window && j <= pos - a.window && !(SINK && j < a.sinks)))
+            sc[c][i] = -INFINITY;
         }
     }
     float top = sc[0][0];
@@ -679,7 +577,7 @@ __device__ __forceinline__ void attn_chunk(const AttnArgs &a, int block, int z, 
           *reinterpret_cast<s16x4 *>(op + d * 32 + i * 8 + h2 * 4) = v;
         }
       if (h2 == 0 && a.lse)
-        a.lse[int64_t(q0 + tok) * a.n_heads + h] = log_sum<BF>(m, l, a.c2);
+        a.lse[int64_t(q0 + tok) * a.n_heads + h] = log_sum(m, l, a.c2, kLift<BF>);
     } else {
       const int64_t idx = (int64_t(z) * a.rows + q0 + tok) * a.n_heads + h;
       float *op = a.chunk_o + idx * D;
@@ -698,257 +596,50 @@ __device__ __forceinline__ void attn_chunk(const AttnArgs &a, int block, int z, 
   if (!hidden) return;
   uint64_t again = __ballot(zero != 0.f && !not_finite(l));
   again = (again | again >> 32) & 0xffffffffu;  // rows of the wave
-  if (!again || !(broken_values<BF, D>(a, table, head, max(lo, pos_lo + 1), hi) ||
-                  (a.window && broken_values<BF, D>(a, table, head, lo, min(hi, win_hi + 1)))))
+  if (!again) return;
+  if constexpr (SINK) {  // (all keys of the split: a superset of the hidden ones)
+    if (!broken_values<BF, D>(a, table, head, lo, min(hi, kr.sink)) &&
+        !broken_values<BF, D>(a, table, head, key(max(lo, kr.sink)), key(hi - 1) + 1))
+      return;
+  } else if (!broken_values<BF, D>(a, table, head, max(lo, pos_lo + 1), hi) &&
+             !(a.window && broken_values<BF, D>(a, table, head, lo, min(hi, win_hi + 1)))) {
     return;
+  }
   wait_own<0>();  // what was stored above comes first
 #pragma unroll 1
   for (; again; again &= again - 1) {
     const int r = r0 + wave * 32 + __builtin_ctzll(again), t = r / G, hh = hk * G + (r - t * G);
-    put_row_by_key<BF, D>(a, table, head, q0 + t, hh, kv - n + t, lo, hi, single, a.chunk_o,
-                          a.chunk_ml, (int64_t(z) * a.rows + q0 + t) * a.n_heads + hh);
+    put_row_by_key<BF, D>(a, table, head, q0 + t, hh, row_keys<SINK>(a, kr, lo, hi, kv - n + t),
+                          single, a.chunk_o, a.chunk_ml, (int64_t(z) * a.rows + q0 + t) * a.n_heads + hh);
   }
 }
 
-template <bool BF, int D, int NT, int WAVES>
+template <bool BF, int D, int NT, int WAVES, bool SINK>
 __global__ void __launch_bounds__(WAVES * 64) k_attn_few(AttnArgs a) {
   __shared__ __align__(16) short lds[WAVES * 64 * D];
-  attn_few<BF, D, NT, WAVES>(a, blockIdx.x, lds);
+  attn_few<BF, D, NT, WAVES, SINK>(a, blockIdx.x, lds);
 }
-template <bool BF, int D, int WAVES>
+template <bool BF, int D, int WAVES, bool SINK>
 __global__ void __launch_bounds__(WAVES * 64, 2) k_attn_chunk(AttnArgs a) {
   __shared__ __align__(16) short lds[256 * D];
-  attn_chunk<BF, D, WAVES>(a, blockIdx.x, blockIdx.y, lds);
+  attn_chunk<BF, D, WAVES, SINK>(a, blockIdx.x, blockIdx.y, lds);
 }
 // Both kinds of requests in one launch: the single tokens' loads fill what the chunks' last
 // work-groups leave of the card.  (24 requests of up to 8,192 tokens, 16 heads of 64, a window
 // of 3,000: 82 us, 99 one after the other, 102 with the chunks last; 24 of up to 16,000, most
 // of them chunks of 400 or less: 216 us, 232 one after the other, 301 with the chunks last,
 // 275 with the two evenly mixed.)
-template <bool BF, int D, int NT>
+template <bool BF, int D, int NT, bool SINK>
 __global__ void __launch_bounds__(256, 2) k_attn_mixed(AttnArgs a, int chunk, int tiles) {
   __shared__ __align__(16) short lds[256 * D];
   const int block = blockIdx.x;
   if (block < chunk)
-    attn_chunk<BF, D, 4>(a, block % tiles, block / tiles, lds);
+    attn_chunk<BF, D, 4, SINK>(a, block % tiles, block / tiles, lds);
   else
-    attn_few<BF, D, NT, 4>(a, block - chunk, lds);
+    attn_few<BF, D, NT, 4, SINK>(a, block - chunk, lds);
 }
 
-// ---- the splits of a row and head, joined in split order by 16-byte columns.
-// A row's splits, `step` rows apart from idx0 on.
-struct Parts {
-  const float *o, *ml;
-  int64_t idx0, step;
-  int splits;
-};
-// Adds every PER-th split from `first` on to the four columns of `acc`.
-template <int D, int PER>
-__device__ inline void add_splits(const AttnArgs &a, const Parts &p, int first, int c, float top,
-                                  f32x4 &acc, float &sum) {
-#pragma unroll 4
-  for (int i = first; i < p.splits; i += PER) {
-    const int64_t idx = p.idx0 + i * p.step;
-    const float mi = p.ml[idx * 2];
-    const float f = part_factor(mi, top, a.c2);
-    sum += f * p.ml[idx * 2 + 1];
-    acc += f * *reinterpret_cast<const f32x4 *>(p.o + idx * D + c * 4);
-  }
-}
-// The largest of the splits' maxima, by LANES neighbouring lanes.
-template <int LANES>
-__device__ inline float top_of(const Parts &p) {
-  float top = -INFINITY;
-  for (int i = threadIdx.x % LANES; i < p.splits; i += LANES)
-    top = fmaxf(top, p.ml[(p.idx0 + i * p.step) * 2]);
-#pragma unroll
-  for (int w = LANES / 2; w; w >>= 1) top = fmaxf(top, __shfl_xor(top, w, 64));
-  return top;
-}
-template <bool BF, int D>
-__device__ inline void put_joined(const AttnArgs &a, int64_t t, int32_t h, int c, f32x4 acc,
-                                  float sum, float top) {
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
-  s16x4 v;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = to_16<BF>(acc[i] * inv);
-  *reinterpret_cast<s16x4 *>(a.out + t * a.out_stride + h * D + c * 4) = v;
-  if (c == 0 && a.lse) a.lse[t * a.n_heads + h] = log_sum<BF>(top, sum, a.c2);
-}
-
-// Few rows, often many splits: a work-group for a row and head, the splits side by side.
-template <bool BF, int D>
-__global__ void __launch_bounds__(256) k_attn_join_few(AttnArgs a) {
-  constexpr int PER = 256 / (D / 4);  // splits side by side
-  __shared__ f32x4 part[PER][D / 4];
-  __shared__ float ls[PER];
-  const int32_t h = blockIdx.x, s = blockIdx.y, tok = blockIdx.z;
-  const int32_t q0 = __ldg(a.q_off + s), n = __ldg(a.q_off + s + 1) - q0;
-  if (tok >= n || n * a.group > kFewRows) return;
-  int32_t code = 0;
-  const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
-  const KeyRange kr = key_range(a, n, kv, 0, n - 1);
-  const int32_t len = kr.hi - kr.lo;
-  if (len <= a.few_split) return;  // written whole
-  const Parts p{a.few_o, a.few_ml, (int64_t(s) * a.few_tokens + tok) * a.n_heads + h,
-                int64_t(a.n_seqs) * a.few_tokens * a.n_heads,
-                (len + a.few_split - 1) / a.few_split};
-  const float top = top_of<64>(p);
-  const int g = threadIdx.x / (D / 4), c = threadIdx.x % (D / 4);
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  float sum = 0.f;
-  add_splits<D, PER>(a, p, g, c, top, acc, sum);
-  part[g][c] = acc;
-  if (c == 0) ls[g] = sum;
-  __syncthreads();
-  if (g) return;
-  sum = 0.f;
-  acc = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < PER; ++i) acc += part[i][c], sum += ls[i];
-  put_joined<BF, D>(a, q0 + tok, h, c, acc, sum, top);
-}
-
-// Many rows, few splits: D / 4 lanes for a row and head.  (1,000 tokens of 32 heads in 2
-// splits, head_dim 128: 10.8 us; with a work-group for each row and head 43.)  A wave holds
-// several items, whose rows may belong to several requests.
-template <bool BF, int D>
-__global__ void __launch_bounds__(256) k_attn_join_chunk(AttnArgs a) {
-  constexpr int LANES = D / 4;
-  const int32_t it = blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-  if (it >= a.rows * a.n_heads) return;
-  const int32_t t = it / a.n_heads, h = it - t * a.n_heads, c = threadIdx.x % LANES;
-  const int32_t s = seq_of_own_row(a.q_off, a.n_seqs, t);
-  const int32_t q0 = __ldg(a.q_off + s), n = __ldg(a.q_off + s + 1) - q0;
-  if (n * a.group <= kFewRows) return;
-  int32_t code = 0;
-  const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
-  const int32_t r0 = ((t - q0) * a.group + h % a.group) / a.chunk_rows * a.chunk_rows;
-  const KeyRange kr = key_range(a, n, kv, r0 / a.group,
-                                (min(r0 + a.chunk_rows, n * a.group) - 1) / a.group);
-  const int32_t len = kr.hi - kr.lo;
-  if (len <= a.chunk_split) return;  // written whole
-  const Parts p{a.chunk_o, a.chunk_ml, it, int64_t(a.rows) * a.n_heads,
-                (len + a.chunk_split - 1) / a.chunk_split};
-  const float top = top_of<LANES>(p);
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  float sum = 0.f;
-  add_splits<D, 1>(a, p, 0, c, top, acc, sum);
-  put_joined<BF, D>(a, t, h, c, acc, sum, top);
-}
-
-// How a call's work is split: from the step's shape and the bound on lengths alone.
-struct Plan {
-  int32_t few_seqs, few_rows, few_tokens, few_waves, few_split, few_splits;
-  int32_t chunk_seqs, chunk_rows, chunk_tiles, chunk_split, chunk_splits;
-};
-
-// A window that no length can fill is none (and positions less a window stay in 32 bits).
-int32_t limited(int32_t window, const fs_step *s) { return window >= s->max_kv ? 0 : window; }
-
-Plan plan(const fs_step *s, const fs_kv_cache *c, int32_t n_heads, int32_t window) {
-  window = limited(window, s);
-  Plan p = {};
-  const int32_t G = n_heads / c->n_kv_heads;
-  int32_t most = 0;
-  for (int32_t i = 0; i < s->n_seqs; ++i) {
-    const int32_t n = s->q_off_h[i + 1] - s->q_off_h[i];
-    if (n == 0) continue;
-    if (int64_t(n) * G <= kFewRows) {
-      ++p.few_seqs;
-      p.few_tokens = n > p.few_tokens ? n : p.few_tokens;
-    } else {
-      ++p.chunk_seqs;
-      most = n > most ? n : most;
-    }
-  }
-  p.few_rows = p.few_tokens * G;
-  auto keys = [&](int32_t tokens) {  // most keys that a tile of rows sees
-    const int64_t k = window ? int64_t(window) + tokens : s->max_kv;
-    return int32_t(k < s->max_kv ? k : s->max_kv);
-  };
-  auto split_of = [&](int64_t blocks, int32_t len, int32_t want, int32_t least, int32_t most,
-                      int64_t rows, int32_t &split, int32_t &splits) {
-    const int64_t bytes = rows * n_heads * (c->head_dim + 2) * 4;  // of one split
-    int64_t most_splits = kMostPartial / bytes;
-    most_splits = most_splits < 4 ? 4 : most_splits > 512 ? 512 : most_splits;
-    int64_t each = (int64_t(len) * blocks + want - 1) / want;
-    each = (each + 127) / 128 * 128;
-    each = each < least ? least : each > most ? most : each;
-    // no more splits than their partial results may take, whatever the bound on lengths
-    const int64_t few = (int64_t(len) + most_splits - 1) / most_splits;
-    if (each < few) each = (few + 127) / 128 * 128;
-    split = int32_t(each);
-    splits = len > split ? (len + split - 1) / split : 1;
-  };
-  // few rows: 1,024 work-groups wanted, of 512 to 1,024 keys (4 requests of up to 500 keys,
-  // 8 heads: 9.7 us whole, 13.0 in two splits of 256, and 3,000 keys 15.5 and 14.1; 64 of up
-  // to 16,384: 121 us with 1,024 keys at most, 125 with 512, 127 with 2,048; one of 200,001
-  // over 4 heads: 86 us, 94 with 2,048 work-groups, 90 with 512)
-  p.few_waves = 4;
-  if (p.few_seqs > 0) {
-    const int64_t blocks = int64_t(p.few_seqs) * c->n_kv_heads;
-    const int32_t len = keys(p.few_tokens);
-    split_of(blocks, len, 1024, 512, 1024, int64_t(s->n_seqs) * p.few_tokens, p.few_split,
-             p.few_splits);
-    // Up to 1,024 keys (2,048 of head_dim 64) with a compute unit for each work-group: eight
-    // waves and no join.  (4 requests, 8 heads of 128: 500 keys 8.9 us, 9.8 with four waves;
-    // 1,000 keys 11.5 and, in two splits, 13.5; 30 requests of 1,000 13.4 and 17.1; 1,500 keys
-    // whole 14.5, in splits 13.8.  Of 64: 1,400 keys 10.3 and 13.2, 2,000 12.9 and 14.1.)
-    const int32_t whole = 131072 / c->head_dim;
-    if (p.chunk_seqs == 0 && p.few_rows <= 32 && len <= whole && blocks <= 256) {
-      p.few_waves = 8;
-      p.few_split = whole;
-      p.few_splits = 1;
-    }
-  }
-  if (p.chunk_seqs > 0) {
-    auto tiles = [&](int32_t rows) {
-      return int32_t(int64_t(s->q_off_h[s->n_seqs]) * G / rows + s->n_seqs);
-    };
-    // 256 rows share each key tile where that still gives every compute unit a work-group
-    // (head_dim 128: 4,096 rows over 32,768 keys 2.03 ms with 128 rows, 1.89 ms with 256; the
-    // lighter tiles of head_dim 64 gain more from four work-groups a unit, 145 against 109 us)
-    // and no request of few rows is there to run beside them (100 requests, chunks of up to
-    // 300 of 8 x 4 heads and single tokens: 466 us with 256 rows, 356 with 128 and one launch;
-    // chunks of up to 4,000 over 20,000 keys: 2.23 ms and 2.30)
-    p.chunk_rows = c->head_dim == 128 && p.few_seqs == 0 &&
-                           int64_t(tiles(256)) * c->n_kv_heads >= 256
-                       ? 256
-                       : 128;
-    p.chunk_tiles = tiles(p.chunk_rows);
-    // 512 work-groups wanted, of at least 1,024 keys (300 rows over 20,000 keys: 134 us, 154
-    // with 256 work-groups, 144 with 1,024)
-    const int32_t toks = p.chunk_rows / G + 2;
-    split_of(int64_t(p.chunk_tiles) * c->n_kv_heads, keys(most < toks ? most : toks), 512, 1024,
-             1 << 30, s->q_off_h[s->n_seqs], p.chunk_split, p.chunk_splits);
-  }
-  return p;
-}
-
-size_t round256(size_t x) { return (x + 255) / 256 * 256; }
-
-// Bytes of the partial results: [rows][D] and [rows][2] floats of each kind.
-struct Space {
-  size_t few_o, few_ml, chunk_o, chunk_ml;
-  size_t total() const { return few_o + few_ml + chunk_o + chunk_ml; }
-};
-Space space(const Plan &p, const fs_step *s, const fs_kv_cache *c, int32_t n_heads) {
-  Space w = {};
-  if (p.few_splits > 1) {
-    const size_t r = size_t(p.few_splits) * s->n_seqs * p.few_tokens * n_heads;
-    w.few_o = round256(r * c->head_dim * 4);
-    w.few_ml = round256(r * 8);
-  }
-  if (p.chunk_splits > 1) {
-    const size_t r = size_t(p.chunk_splits) * s->q_off_h[s->n_seqs] * n_heads;
-    w.chunk_o = round256(r * c->head_dim * 4);
-    w.chunk_ml = round256(r * 8);
-  }
-  return w;
-}
-
-template <bool BF, int D>
+template <bool BF, int D, bool SINK>
 void run(const AttnArgs &a, const Plan &p, hipStream_t stream) {
   const dim3 block(256);
   const int few = p.few_seqs > 0 ? a.n_seqs * a.c.n_kv_heads * p.few_splits : 0;
@@ -960,13 +651,13 @@ void run(const AttnArgs &a, const Plan &p, hipStream_t stream) {
     constexpr int NT = decltype(nt)::value;
     if constexpr (D == 64 || NT <= 2)
       if (mixed)
-        hipLaunchKernelGGL((k_attn_mixed<BF, D, NT>), dim3(chunk + few), block, 0, stream, a, chunk,
+        hipLaunchKernelGGL((k_attn_mixed<BF, D, NT, SINK>), dim3(chunk + few), block, 0, stream, a, chunk,
                            tiles);
     if constexpr (NT <= 2)
       if (p.few_waves == 8)
-        hipLaunchKernelGGL((k_attn_few<BF, D, NT, 8>), dim3(few), dim3(512), 0, stream, a);
+        hipLaunchKernelGGL((k_attn_few<BF, D, NT, 8, SINK>), dim3(few), dim3(512), 0, stream, a);
     if (few > 0 && !mixed && p.few_waves == 4)
-      hipLaunchKernelGGL((k_attn_few<BF, D, NT, 4>), dim3(few), block, 0, stream, a);
+      hipLaunchKernelGGL((k_attn_few<BF, D, NT, 4, SINK>), dim3(few), block, 0, stream, a);
   };
   if (p.few_rows <= 16)
     by_rows(std::integral_constant<int, 1>());
@@ -978,9 +669,9 @@ void run(const AttnArgs &a, const Plan &p, hipStream_t stream) {
     const dim3 grid(tiles, p.chunk_splits);
     if constexpr (D == 128)
       if (p.chunk_rows == 256)
-        hipLaunchKernelGGL((k_attn_chunk<BF, D, 8>), grid, dim3(512), 0, stream, a);
+        hipLaunchKernelGGL((k_attn_chunk<BF, D, 8, SINK>), grid, dim3(512), 0, stream, a);
     if (p.chunk_rows == 128)
-      hipLaunchKernelGGL((k_attn_chunk<BF, D, 4>), grid, block, 0, stream, a);
+      hipLaunchKernelGGL((k_attn_chunk<BF, D, 4, SINK>), grid, block, 0, stream, a);
   }
   if (p.few_splits > 1)
     hipLaunchKernelGGL((k_attn_join_few<BF, D>), dim3(a.n_heads, a.n_seqs, p.few_tokens), block, 0,
@@ -994,54 +685,35 @@ void run(const AttnArgs &a, const Plan &p, hipStream_t stream) {
 }  // namespace
 
 size_t attention_workspace_bytes(const fs_step *s, const fs_kv_cache *c, int32_t n_heads,
-                                 int32_t window) {
-  return space(plan(s, c, n_heads, window), s, c, n_heads).total();
+                                 int32_t window, int32_t sinks) {
+  const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks);
+  return space(plan(s, sh), s, sh).total();
 }
 
 hipError_t launch_attention(const fs_step *s, const fs_kv_cache *c, int32_t n_heads, float scale,
-                            int32_t window, const void *q, int64_t q_stride, void *out,
-                            int64_t out_stride, float *lse, void *ws, int32_t *err,
+                            int32_t window, int32_t sinks, const void *q, int64_t q_stride,
+                            void *out, int64_t out_stride, float *lse, void *ws, int32_t *err,
                             hipStream_t stream) {
-  const Plan p = plan(s, c, n_heads, window);
-  const Space w = space(p, s, c, n_heads);
+  const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks);
+  const Plan p = plan(s, sh);
   AttnArgs a;
-  a.q_off = s->q_off;
-  a.kv_len = s->kv_len;
-  a.n_seqs = s->n_seqs;
-  a.max_kv = s->max_kv;
-  a.rows = s->q_off_h[s->n_seqs];
-  a.n_heads = n_heads;
-  a.window = limited(window, s);
-  a.group = n_heads / c->n_kv_heads;
+  fill_args(a, p, space(p, s, sh), sh, s, scale, q, q_stride, out, out_stride, lse, ws, err);
   a.c = dev_cache(c);
-  a.q = static_cast<const short *>(q);
-  a.out = static_cast<short *>(out);
-  a.q_stride = q_stride;
-  a.out_stride = out_stride;
-  a.lse = lse;
-  // a scale of 0 makes every visible score equal; a factor of 0 would turn -inf into NaN
-  const float c2 = (scale < 0.f ? -scale : scale) * 1.44269504088896341f;
-  a.c2 = c2 > 1.2e-38f ? c2 : 1.2e-38f;
-  a.flip = scale < 0.f;
-  a.few_split = p.few_split;
-  a.few_tokens = p.few_tokens;
-  a.chunk_rows = p.chunk_rows;
-  a.chunk_split = p.chunk_split;
-  char *at = static_cast<char *>(ws);
-  a.few_o = reinterpret_cast<float *>(at);
-  a.few_ml = reinterpret_cast<float *>(at + w.few_o);
-  a.chunk_o = reinterpret_cast<float *>(at + w.few_o + w.few_ml);
-  a.chunk_ml = reinterpret_cast<float *>(at + w.few_o + w.few_ml + w.chunk_o);
-  a.err = err;
-  const bool bf = c->dtype == FS_BF16;
-  if (bf && c->head_dim == 128)
-    run<true, 128>(a, p, stream);
-  else if (bf)
-    run<true, 64>(a, p, stream);
-  else if (c->head_dim == 128)
-    run<false, 128>(a, p, stream);
+  a.lift = c->dtype == FS_BF16 ? kLift<true> : kLift<false>;
+  auto go = [&](auto bf, auto dim) {
+    constexpr bool BF = decltype(bf)::value;
+    constexpr int D = decltype(dim)::value;
+    if (sh.sinks > 0)
+      run<BF, D, true>(a, p, stream);
+    else
+      run<BF, D, false>(a, p, stream);
+  };
+  const std::integral_constant<int, 64> d64;
+  const std::integral_constant<int, 128> d128;
+  if (c->dtype == FS_BF16)
+    c->head_dim == 128 ? go(std::true_type(), d128) : go(std::true_type(), d64);
   else
-    run<false, 64>(a, p, stream);
+    c->head_dim == 128 ? go(std::false_type(), d128) : go(std::false_type(), d64);
   return hipGetLastError();
 }
 

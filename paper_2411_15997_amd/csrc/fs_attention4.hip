@@ -1,0 +1,616 @@
+// Attention of the step's rows over a paged cache held in 4 bits: the softmax, the split of
+// the work and the joins of the kernels over the 16-bit cache, with codes in place of values.
+//
+// A group of 32 values and its scale become 16-bit values exactly (one conversion
+// instruction for two of them), so both products are those of the 16-bit cache.
+//   K  feeds the first product from registers: the sum over a head's dimensions may be taken
+//      in any order, so each lane takes 32 (or 16) neighbouring ones of a key, 16 bytes of
+//      codes with one scale, and a wave's load is 16 whole keys without a gap.
+//   V  is wanted with keys along a lane, while its codes and scales lie along dimensions:
+//      it goes through LDS as 16-bit values and is read back transposed.
+#include <type_traits>
+
+#include "fs_attn.h"
+#include "fs_cache.h"
+
+namespace fs {
+
+namespace {
+
+struct Attn4Args : AttnArgs {  // `c` is the cache's codes, in bytes
+  DevScales sc;
+};
+
+// The units of the exponentials (fs_attn.h).  Scales reach 2^125 for bfloat16: with 2^-18 the
+// sums of 1,000 such values stay in fp32's range, and values down to 2^-100 above its smallest.
+template <bool BF>
+constexpr float kLift4 = BF ? -18.f : 7.f;
+
+// Codes of N neighbouring values: 16 bytes for 32 of them, 8 for 16.
+template <int N>
+using Codes = uint32_t __attribute__((ext_vector_type(N / 8)));
+
+// A group that counts as NaN is multiplied as zeros; the rows that see such a key get NaN in
+// the group's columns at the end: bit g of `poison` for the columns 32 g .. .
+template <int N, class Acc>
+__device__ inline void put_poison(uint32_t poison, int group, Acc &o) {
+  if (poison >> group & 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = NAN;
+}
+
+// ---- few rows: NT tiles of 16 rows, WAVES waves, which take 32 keys each in turn
+template <bool BF, int D, int NT, int WAVES>
+__device__ __forceinline__ void attn4_few(const Attn4Args &a, int block, short *lds) {
+  constexpr int KS = D / 32;  // matrix steps of a score
+  constexpr int DB = D / 16;  // 16-column blocks of an output row
+  constexpr int DL = D / 4;   // neighbouring dimensions of a key that a lane takes
+  constexpr int kIds = 512;   // page ids kept in LDS
+  constexpr bool kTwoParts = NT <= 2;  // of a probability
+  auto v_lds = reinterpret_cast<short(*)[32 * D]>(lds);  // a wave's V
+  __shared__ float wm[WAVES][NT * 16], wl[WAVES][NT * 16];
+  __shared__ uint32_t ids[kIds];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r16 = lane & 15, g4 = lane >> 4;
+  // (heads fastest, and each split shifts the requests by one: see the 16-bit kernel)
+  const int hk = block % a.c.n_kv_heads, sz = block / a.c.n_kv_heads;
+  const int z = sz / a.n_seqs, s = (sz + z) % a.n_seqs;
+  const int32_t q0 = __ldg(a.q_off + s), n = __ldg(a.q_off + s + 1) - q0;
+  const int G = a.group, R = n * G;
+  if (R <= 0 || R > kFewRows) return;
+  int32_t code = 0;
+  const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
+  const KeyRange kr = key_range(a, n, kv, 0, n - 1);
+  const bool single = kr.length() <= a.few_split;
+  const int32_t lo = z * a.few_split;
+  if (z > 0 && lo >= kr.length()) return;
+  const int32_t hi = min(kr.length(), lo + a.few_split);
+  const int32_t *table = a.c.table + s * a.c.table_stride;
+  // where this lane's part of a key row begins
+  const uint32_t inside = hk * a.c.head_stride + g4 * (DL / 2);
+  const uint32_t s_inside = hk * a.sc.head_stride + g4 * DL / 32;
+
+  // queries: row r16 of each tile, 8 of this lane's dimensions at each step
+  s16x8 qf[NT][KS];
+  int32_t pos[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int r = min(t * 16 + r16, R - 1), tok = r / G, h = hk * G + (r - tok * G);
+    pos[t] = t * 16 + r16 < R ? kv - n + tok : -1;
+    const short *qp = a.q + (q0 + tok) * a.q_stride + h * D + g4 * DL;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      qf[t][k] = *reinterpret_cast<const s16x8 *>(qp + k * 8);
+      if (a.flip) qf[t][k] ^= short(0x8000);
+    }
+  }
+  f32x4 o[NT][DB] = {};
+  float m[NT], l[NT];
+  uint32_t poison[NT] = {};
+#pragma unroll
+  for (int t = 0; t < NT; ++t) m[t] = -INFINITY, l[t] = 0.f;
+
+  struct Tile {
+    Codes<DL> k[2], v[2];
+    uint32_t ks[2], vs[2];
+  };
+  short *vb = v_lds[wave];
+
+  for (int32_t from = lo; from < hi;) {
+    const PageIds span = page_ids<true>(kr, from, hi, a.c.page_shift, kIds);
+    const int32_t end = span.end;
+    __syncthreads();
+    for (int i = tid; i < span.n; i += WAVES * 64) {
+      const uint32_t page = __ldg(table + span.page(i));
+      if (page >= a.c.n_pages) code = FS_E_RANGE;
+      ids[i] = page < a.c.n_pages ? page : 0;
+    }
+    __syncthreads();
+    const int32_t first = from + wave * 32;
+    const int32_t tiles = first < end ? (end - first + WAVES * 32 - 1) / (WAVES * 32) : 0;
+    auto load = [&](int32_t t, Tile &x) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int32_t j = kr.key(min(first + t * (WAVES * 32) + b * 16 + r16, end - 1));
+        const uint32_t page = ids[span.slot(j)], slot = j & ((1 << a.c.page_shift) - 1);
+        const uint64_t at =
+            uint64_t(page) * a.c.page_stride + (inside + slot * a.c.token_stride);
+        const uint64_t sat =
+            uint64_t(page) * a.sc.page_stride + (s_inside + slot * a.sc.token_stride);
+        x.k[b] = *reinterpret_cast<const Codes<DL> *>(a.c.k + at);
+        x.v[b] = *reinterpret_cast<const Codes<DL> *>(a.c.v + at);
+        x.ks[b] = a.sc.k[sat];
+        x.vs[b] = a.sc.v[sat];
+      }
+    };
+    Tile x, next;
+    if (tiles > 0) load(0, next);
+    for (int32_t t = 0; t < tiles; ++t) {
+      const int32_t j0 = first + t * (WAVES * 32);
+      x = next;
+      if (t + 1 < tiles) load(t + 1, next);
+      f32x4 sc[NT][2] = {};
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const float unit = scale_of<BF>(x.ks[b]);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          const s16x8 kf = values8<BF>(x.k[b][k], unit);
+#pragma unroll
+          for (int r = 0; r < NT; ++r) sc[r][b] = mfma_16x16x32<BF>(kf, qf[r][k], sc[r][b]);
+        }
+      }
+      // V: this lane's dimensions of two keys, as chunks of 8
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const float unit = scale_of<BF>(x.vs[b]);
+        const bool bad = x.vs[b] > kTopScale<BF>;
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+          *reinterpret_cast<s16x8 *>(vb + tile_at<D>(b * 16 + r16, g4 * KS + k)) =
+              values8<BF>(bad ? 0 : x.v[b][k], unit);
+      }
+      const int32_t key0 = kr.key(j0), key31 = kr.key(j0 + 31);
+      const bool odd = max(max(x.ks[0], x.ks[1]), max(x.vs[0], x.vs[1])) > kTopScale<BF>;
+      const uint64_t odd_any = __ballot(odd);
+      // keys that some row does not see
+      const bool edge = j0 + 32 > end || key31 > kv - n || (a.window && key0 <= kv - 1 - a.window);
+      s16x8 pf[NT], pl[NT];
+#pragma unroll
+      for (int r = 0; r < NT; ++r) {
+        float p[8], top = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[b * 4 + i] = sc[r][b][i];
+        if (odd_any) {
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            uint64_t bad = __ballot(x.ks[b] > kTopScale<BF>);
+            bad |= bad >> 32;
+            bad |= bad >> 16;  // bit i: key i of the 16
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (bad >> (g4 * 4 + i) & 1) p[b * 4 + i] = NAN;
+            for (uint64_t vbad = __ballot(x.vs[b] > kTopScale<BF>); vbad; vbad &= vbad - 1) {
+              const int i = __builtin_ctzll(vbad);
+              const int32_t v = j0 + b * 16 + (i & 15), j = kr.key(v);
+              if (j <= pos[r] && v < end &&
+                  (a.window == 0 || j > pos[r] - a.window || j < a.sinks))
+                poison[r] |= 1u << ((i >> 4) * DL / 32);
+            }
+          }
+        }
+        if (edge || pos[r] < 0) {
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int32_t v = j0 + b * 16 + g4 * 4 + i, j = kr.key(v);
+              const bool see = j <= pos[r] && v < end &&
+                               (a.window == 0 || j > pos[r] - a.window || j < a.sinks);
+              if (!see) p[b * 4 + i] = -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, p[i]);
+        top = max_of_halves(fmaxf(top, __shfl_xor(top, 16, 64)));
+        const float m2 = fmaxf(m[r], top);
+        // (-inf less -inf is no number and asks for nothing)
+        if (__any((m2 - m[r]) * a.c2 > kSlack)) {
+          const float f = m[r] == -INFINITY ? 0.f : exp2_fast((m[r] - m2) * a.c2);
+          l[r] *= f;
+#pragma unroll
+          for (int d = 0; d < DB; ++d) o[r][d] *= f;
+          m[r] = m2;
+        }
+        const float mc = reference(m[r], a.c2) - kLift4<BF>;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          p[i] = exp2_fast(fmaf(p[i], a.c2, -mc));
+          l[r] += p[i];
+        }
+        pf[r] = pack8<BF>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (kTwoParts) pl[r][i] = to_16<BF>(p[i] - to_f32<BF>(pf[r][i]));
+      }
+      // keys 4 g4 .. + 3 and 16 + 4 g4 .. + 3 of the tile, 16 columns at a time
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        const int row = 4 * g4 + (r16 >> 2), col = d * 16 + (r16 & 3) * 4;
+        const s16x4 v0 = read_tr(vb + tile_at<D>(row, col >> 3) + (col & 7));
+        const s16x4 v1 = read_tr(vb + tile_at<D>(row + 16, col >> 3) + (col & 7));
+        const s16x8 vv = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+        for (int r = 0; r < NT; ++r) {
+          o[r][d] = mfma_16x16x32<BF>(vv, pf[r], o[r][d]);
+          if (kTwoParts) o[r][d] = mfma_16x16x32<BF>(vv, pl[r], o[r][d]);
+        }
+      }
+    }
+    from = end;
+  }
+  raise_err(a.err, code);
+
+  // the waves' results, joined in LDS a tile of rows at a time
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    l[t] += __shfl_xor(l[t], 16, 64);
+    l[t] += __shfl_xor(l[t], 32, 64);
+    if (g4 == 0) wm[wave][t * 16 + r16] = m[t], wl[wave][t * 16 + r16] = l[t];
+    if (__any(poison[t] != 0))
+#pragma unroll
+      for (int d = 0; d < DB; ++d) put_poison<4>(poison[t], d / 2, o[t][d]);
+  }
+  float *buf = reinterpret_cast<float *>(lds);  // [WAVES][16][D / 2]: half of the columns
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    if (t * 16 >= R) break;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      __syncthreads();
+#pragma unroll
+      for (int d = 0; d < DB / 2; ++d)
+        *reinterpret_cast<f32x4 *>(
+            buf + (wave * 16 + r16) * (D / 2) + ((d * 16 + g4 * 4) ^ ((r16 & 3) * 4))) =
+            o[t][half * (DB / 2) + d];
+      __syncthreads();
+      for (int e = tid; e < 16 * D / 8; e += WAVES * 64) {
+        const int r = e / (D / 8), col = (e - r * (D / 8)) * 4;
+        if (t * 16 + r >= R) continue;
+        const int tr = t * 16 + r;
+        float top = wm[0][tr];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, wm[w][tr]);
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+          const float f = part_factor(wm[w][tr], top, a.c2);
+          sum += f * wl[w][tr];
+          acc += f * *reinterpret_cast<const f32x4 *>(buf + (w * 16 + r) * (D / 2) +
+                                                      (col ^ ((r & 3) * 4)));
+        }
+        const int tok = tr / G, h = hk * G + (tr - tok * G), cc = half * (D / 2) + col;
+        if (single) {
+          const float inv = sum > 0.f ? 1.f / sum : 0.f;
+          s16x4 v;
+          acc *= inv;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = to_16<BF>(acc[i]);
+          *reinterpret_cast<s16x4 *>(a.out + (q0 + tok) * a.out_stride + h * D + cc) = v;
+          if (cc == 0 && a.lse)
+            a.lse[int64_t(q0 + tok) * a.n_heads + h] = log_sum(top, sum, a.c2, kLift4<BF>);
+        } else {
+          const int64_t idx =
+              ((int64_t(z) * a.n_seqs + s) * a.few_tokens + tok) * a.n_heads + h;
+          *reinterpret_cast<f32x4 *>(a.few_o + idx * D + cc) = acc;
+          if (cc == 0) a.few_ml[idx * 2] = top, a.few_ml[idx * 2 + 1] = sum;
+        }
+      }
+    }
+  }
+}
+
+// ---- chunks: WAVES waves of 32 rows, 64 keys at a time through two buffers of 16-bit values
+template <bool BF, int D, int WAVES>
+__device__ __forceinline__ void attn4_chunk(const Attn4Args &a, int block, int z, short *lds,
+                                            uint8_t *scales, int *odd) {
+  constexpr int KS = D / 16;       // matrix steps of a score
+  constexpr int DB = D / 32;       // 32-column blocks of an output row: groups
+  constexpr int RW = 64 / DB;      // keys of a wave's load: a lane takes a group of one key
+  constexpr int LD = 2 * 64 / RW / WAVES;  // a wave's loads of K and V for 64 keys
+  static_assert(LD >= 1, "a wave loads whole rows");
+  auto kt = reinterpret_cast<short(*)[64 * D]>(lds), vt = kt + 2;
+  auto sb = reinterpret_cast<uint8_t(*)[2][64 * DB]>(scales);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r32 = lane & 31, h2 = lane >> 5;
+  const int hk = block % a.c.n_kv_heads;
+  int32_t s, r0;
+  chunk_tile(a, block / a.c.n_kv_heads, s, r0);
+  const int32_t q0 = __ldg(a.q_off + s), n = __ldg(a.q_off + s + 1) - q0;
+  const int G = a.group, R = n * G;
+  if (r0 < 0 || R <= kFewRows) return;
+  int32_t code = 0;
+  const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
+  const KeyRange kr = key_range(a, n, kv, r0 / G, (min(r0 + WAVES * 32, R) - 1) / G);
+  const bool single = kr.length() <= a.chunk_split;
+  const int32_t lo = z * a.chunk_split;
+  if (z > 0 && lo >= kr.length()) return;
+  const int32_t hi = min(kr.length(), lo + a.chunk_split);
+  const int32_t *table = a.c.table + s * a.c.table_stride;
+
+  const int row = r0 + wave * 32 + r32;
+  const int tok = min(row, R - 1) / G, h = hk * G + (min(row, R - 1) - tok * G);
+  const int32_t pos = kv - n + tok;
+  // the wave's first row, and the first key that its last row's window leaves
+  const int32_t pos_lo = kv - n + min(r0 + wave * 32, R - 1) / G;
+  const int32_t win_hi =
+      a.window ? kv - n + min(r0 + wave * 32 + 31, R - 1) / G - a.window : INT32_MIN;
+  s16x8 qf[KS];
+  {
+    const short *qp = a.q + (q0 + tok) * a.q_stride + h * D + h2 * 8;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      qf[k] = *reinterpret_cast<const s16x8 *>(qp + k * 16);
+      if (a.flip) qf[k] ^= short(0x8000);
+    }
+  }
+  f32x16 o[DB] = {};
+  float m = -INFINITY, l = 0.f;
+  uint32_t poison = 0;
+
+  // Load i of the wave: 64 / DB keys' K (then V) rows, the keys along the lanes, so that 16
+  // lanes write 16 rows of a tile (and no two of them the same banks).
+  const int group = lane / RW;
+  int32_t lrow[LD];
+  uint32_t page[LD];
+  bool val[LD];
+#pragma unroll
+  for (int i = 0; i < LD; ++i) {
+    const int u = i * WAVES + wave;
+    val[i] = u >= 64 / RW;
+    lrow[i] = (val[i] ? u - 64 / RW : u) * RW + lane % RW;
+  }
+  auto pages = [&](int32_t j0) {
+#pragma unroll
+    for (int i = 0; i < LD; ++i)
+      page[i] = __ldg(table + (kr.key(min(j0 + lrow[i], hi - 1)) >> a.c.page_shift));
+  };
+  Codes<32> w[LD];
+  uint32_t ws[LD];
+  auto load = [&](int32_t j0) {
+#pragma unroll
+    for (int i = 0; i < LD; ++i) {
+      const int32_t j = kr.key(min(j0 + lrow[i], hi - 1));
+      uint32_t id = page[i];
+      if (id >= a.c.n_pages) {
+        code = FS_E_RANGE;
+        id = 0;
+      }
+      const uint32_t slot = j & ((1 << a.c.page_shift) - 1);
+      const uint64_t at = uint64_t(id) * a.c.page_stride +
+                          (hk * a.c.head_stride + group * 16 + slot * a.c.token_stride);
+      const uint64_t sat = uint64_t(id) * a.sc.page_stride +
+                           (hk * a.sc.head_stride + group + slot * a.sc.token_stride);
+      w[i] = *reinterpret_cast<const Codes<32> *>((val[i] ? a.c.v : a.c.k) + at);
+      ws[i] = (val[i] ? a.sc.v : a.sc.k)[sat];
+    }
+  };
+  auto put = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < LD; ++i) {
+      const bool bad = ws[i] > kTopScale<BF>;
+      const float unit = scale_of<BF>(ws[i]);
+      short *tile = val[i] ? vt[buf] : kt[buf];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        *reinterpret_cast<s16x8 *>(tile + tile_at<D>(lrow[i], group * 4 + k)) =
+            values8<BF>(bad ? 0 : w[i][k], unit);
+      sb[buf][val[i]][lrow[i] * DB + group] = uint8_t(ws[i]);
+      if (bad) *odd = 1;
+    }
+  };
+  if (tid == 0) *odd = 0;
+  __syncthreads();
+  if (lo < hi) {
+    pages(lo);
+    load(lo);
+    pages(lo + 64);
+    put(0);
+    load(lo + 64);  // (past the end: the last key)
+    pages(lo + 128);
+  }
+  __syncthreads();
+  int buf = 0;
+  for (int32_t j0 = lo; j0 < hi; j0 += 64, buf ^= 1) {
+    if (j0 + 64 < hi) {
+      put(buf ^ 1);
+      load(j0 + 128);
+      pages(j0 + 192);
+    }
+    const short *kb = kt[buf], *vb = vt[buf];
+    f32x16 sc[2] = {};
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        sc[c] = mfma_32x32x16<BF>(
+            *reinterpret_cast<const s16x8 *>(kb + tile_at<D>(c * 32 + r32, k * 2 + h2)), qf[k],
+            sc[c]);
+    if (__builtin_amdgcn_readfirstlane(*reinterpret_cast<volatile int *>(odd))) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = c * 32 + 8 * (i >> 2) + 4 * h2 + (i & 3);
+#pragma unroll
+          for (int g = 0; g < DB; ++g)
+            if (sb[buf][0][key * DB + g] > kTopScale<BF>) sc[c][i] = NAN;
+        }
+#pragma unroll 1
+      for (int key = 0; key < 64; ++key) {
+        const int32_t v = j0 + key, j = kr.key(v);
+        if (j > pos || v >= hi || (a.window && j <= pos - a.window && j >= a.sinks)) continue;
+#pragma unroll
+        for (int g = 0; g < DB; ++g)
+          if (sb[buf][1][key * DB + g] > kTopScale<BF>) poison |= 1u << g;
+      }
+    }
+    // keys that some row of the wave does not see
+    if (kr.key(j0 + 63) > pos_lo || j0 + 64 > hi || kr.key(j0) <= win_hi) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int32_t v = j0 + c * 32 + 8 * (i >> 2) + 4 * h2 + (i & 3), j = kr.key(v);
+          if (j > pos || v >= hi || (a.window && j <= pos - a.window && j >= a.sinks))
+            sc[c][i] = -INFINITY;
+        }
+    }
+    float top = sc[0][0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[0][i]);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[1][i]);
+    const float m2 = fmaxf(m, max_of_halves(top));
+    if (__any((m2 - m) * a.c2 > kSlack)) {
+      const float f = m == -INFINITY ? 0.f : exp2_fast((m - m2) * a.c2);
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) o[d] *= f;
+      m = m2;
+    }
+    const float mc = reference(m, a.c2) - kLift4<BF>;
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          p[i] = exp2_fast(fmaf(sc[c][u * 8 + i], a.c2, -mc));
+          l += p[i];
+        }
+        const s16x8 pf = pack8<BF>(p);
+        // keys 4 h2 .. + 3 and 8 + 4 h2 .. + 3 of this 16
+        const int vr = c * 32 + u * 16 + 4 * h2 + ((lane & 15) >> 2);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const int col = d * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+          const s16x4 v0 = read_tr(vb + tile_at<D>(vr, col >> 3) + (col & 7));
+          const s16x4 v1 = read_tr(vb + tile_at<D>(vr + 8, col >> 3) + (col & 7));
+          o[d] = mfma_32x32x16<BF>(__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7), pf,
+                                   o[d]);
+        }
+      }
+    __syncthreads();
+  }
+  raise_err(a.err, code);
+  l += __shfl_xor(l, 32, 64);
+  if (__any(poison != 0))
+#pragma unroll
+    for (int d = 0; d < DB; ++d) put_poison<16>(poison, d, o[d]);
+  if (row >= R) return;
+  if (single) {
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    short *op = a.out + (q0 + tok) * a.out_stride + h * D;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s16x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = to_16<BF>(o[d][i * 4 + e] * inv);
+        *reinterpret_cast<s16x4 *>(op + d * 32 + i * 8 + h2 * 4) = v;
+      }
+    if (h2 == 0 && a.lse) a.lse[int64_t(q0 + tok) * a.n_heads + h] = log_sum(m, l, a.c2, kLift4<BF>);
+  } else {
+    const int64_t idx = (int64_t(z) * a.rows + q0 + tok) * a.n_heads + h;
+    float *op = a.chunk_o + idx * D;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4 *>(op + d * 32 + i * 8 + h2 * 4) =
+            f32x4{o[d][i * 4], o[d][i * 4 + 1], o[d][i * 4 + 2], o[d][i * 4 + 3]};
+    if (h2 == 0) a.chunk_ml[idx * 2] = m, a.chunk_ml[idx * 2 + 1] = l;
+  }
+}
+
+template <bool BF, int D, int NT, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64) k_attn4_few(Attn4Args a) {
+  __shared__ __align__(16) short lds[WAVES * 32 * D];
+  attn4_few<BF, D, NT, WAVES>(a, blockIdx.x, lds);
+}
+template <bool BF, int D, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64, 2) k_attn4_chunk(Attn4Args a) {
+  __shared__ __align__(16) short lds[256 * D];
+  __shared__ uint8_t scales[4 * 64 * (D / 32)];
+  __shared__ int odd;
+  attn4_chunk<BF, D, WAVES>(a, blockIdx.x, blockIdx.y, lds, scales, &odd);
+}
+// Both kinds of requests in one launch, as over the 16-bit cache.
+template <bool BF, int D, int NT>
+__global__ void __launch_bounds__(256, 2) k_attn4_mixed(Attn4Args a, int chunk, int tiles) {
+  __shared__ __align__(16) short lds[256 * D];
+  __shared__ uint8_t scales[4 * 64 * (D / 32)];
+  __shared__ int odd;
+  const int block = blockIdx.x;
+  if (block < chunk)
+    attn4_chunk<BF, D, 4>(a, block % tiles, block / tiles, lds, scales, &odd);
+  else
+    attn4_few<BF, D, NT, 4>(a, block - chunk, lds);
+}
+
+template <bool BF, int D>
+void run(const Attn4Args &a, const Plan &p, hipStream_t stream) {
+  const dim3 block(256);
+  const int few = p.few_seqs > 0 ? a.n_seqs * a.c.n_kv_heads * p.few_splits : 0;
+  const int tiles = p.chunk_tiles * a.c.n_kv_heads;
+  const int chunk = p.chunk_seqs > 0 ? tiles * p.chunk_splits : 0;
+  // In one launch where one kernel holds both without spilling registers.
+  const bool mixed = few > 0 && chunk > 0 && p.chunk_rows == 128 && (D == 64 || p.few_rows <= 32);
+  auto by_rows = [&](auto nt) {
+    constexpr int NT = decltype(nt)::value;
+    if constexpr (D == 64 || NT <= 2)
+      if (mixed)
+        hipLaunchKernelGGL((k_attn4_mixed<BF, D, NT>), dim3(chunk + few), block, 0, stream, a,
+                           chunk, tiles);
+    if constexpr (NT <= 2)
+      if (p.few_waves == 8)
+        hipLaunchKernelGGL((k_attn4_few<BF, D, NT, 8>), dim3(few), dim3(512), 0, stream, a);
+    if (few > 0 && !mixed && p.few_waves == 4)
+      hipLaunchKernelGGL((k_attn4_few<BF, D, NT, 4>), dim3(few), block, 0, stream, a);
+  };
+  if (p.few_rows <= 16)
+    by_rows(std::integral_constant<int, 1>());
+  else if (p.few_rows <= 32)
+    by_rows(std::integral_constant<int, 2>());
+  else
+    by_rows(std::integral_constant<int, 4>());
+  if (chunk > 0 && !mixed) {
+    const dim3 grid(tiles, p.chunk_splits);
+    if constexpr (D == 128)
+      if (p.chunk_rows == 256)
+        hipLaunchKernelGGL((k_attn4_chunk<BF, D, 8>), grid, dim3(512), 0, stream, a);
+    if (p.chunk_rows == 128)
+      hipLaunchKernelGGL((k_attn4_chunk<BF, D, 4>), grid, block, 0, stream, a);
+  }
+  if (p.few_splits > 1)
+    hipLaunchKernelGGL((k_attn_join_few<BF, D>), dim3(a.n_heads, a.n_seqs, p.few_tokens), block, 0,
+                       stream, a);
+  if (p.chunk_splits > 1) {
+    const int64_t lanes = int64_t(a.rows) * a.n_heads * (D / 4);
+    hipLaunchKernelGGL((k_attn_join_chunk<BF, D>), dim3((lanes + 255) / 256), block, 0, stream, a);
+  }
+}
+
+}  // namespace
+
+size_t attention4_workspace_bytes(const fs_step *s, const fs_kv_cache4 *c, int32_t n_heads,
+                                  int32_t window, int32_t sinks) {
+  const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks);
+  return space(plan(s, sh), s, sh).total();
+}
+
+hipError_t launch_attention4(const fs_step *s, const fs_kv_cache4 *c, int32_t dtype,
+                             int32_t n_heads, float scale, int32_t window, int32_t sinks,
+                             const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                             float *lse, void *ws, int32_t *err, hipStream_t stream) {
+  const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks);
+  const Plan p = plan(s, sh);
+  Attn4Args a;
+  fill_args(a, p, space(p, s, sh), sh, s, scale, q, q_stride, out, out_stride, lse, ws, err);
+  a.c = dev_codes(c);
+  a.sc = dev_scales(c);
+  a.lift = dtype == FS_BF16 ? kLift4<true> : kLift4<false>;
+  if (dtype == FS_BF16)
+    c->head_dim == 128 ? run<true, 128>(a, p, stream) : run<true, 64>(a, p, stream);
+  else
+    c->head_dim == 128 ? run<false, 128>(a, p, stream) : run<false, 64>(a, p, stream);
+  return hipGetLastError();
+}
+
+}  // namespace fs

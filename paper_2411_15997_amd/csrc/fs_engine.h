@@ -211,10 +211,10 @@ hipError_t launch_rope_append(const fs_step *s, const fs_kv_cache *c, const fs_r
                               int64_t q_out_stride, int32_t *err, hipStream_t stream);
 
 size_t attention_workspace_bytes(const fs_step *s, const fs_kv_cache *c, int32_t n_heads,
-                                 int32_t window);
+                                 int32_t window, int32_t sinks);
 hipError_t launch_attention(const fs_step *s, const fs_kv_cache *c, int32_t n_heads, float scale,
-                            int32_t window, const void *q, int64_t q_stride, void *out,
-                            int64_t out_stride, float *lse, void *ws, int32_t *err,
+                            int32_t window, int32_t sinks, const void *q, int64_t q_stride,
+                            void *out, int64_t out_stride, float *lse, void *ws, int32_t *err,
                             hipStream_t stream);
 
 size_t sample_workspace_bytes(int32_t dtype, int32_t rows, int32_t vocab);

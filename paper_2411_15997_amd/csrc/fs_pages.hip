@@ -1,0 +1,475 @@
+// The pages of a cache: letting rows go, forking rows that share a prompt's pages, moving the
+// pages in use together, and copying pages.
+//
+// A page's state is its count of holders.  Free pages are taken, and pages are moved, in the
+// order of ids: a page's place is its rank among its kind, the sum of a block's count before it
+// (k_count, then each block adds up the counts of those before it) and of ballots inside the
+// block.  So no result hangs on the order of atomics; those used (claims by the lowest index,
+// counts of holders) end the same in any order.
+// Bound by launches at the usual sizes (thousands of pages: three kernels of 2 to 4 us); the
+// copies by their bytes.
+#include "fs_cache.h"
+
+namespace fs {
+
+namespace {
+
+constexpr int kBlock = 1024;          // threads
+constexpr int kPer = 2 * kBlock;      // pages of a work-group
+
+struct PoolArgs {
+  int32_t n_pages, page_shift, n_rows, width;
+  int32_t *refs, *table, *held;
+  int64_t stride;
+  int32_t n, blocks;
+  const int32_t *rows, *parent, *child, *shared, *room;
+  int32_t *src, *dst, *count, *refs_out, *table_out;
+  int64_t out_stride;
+  int32_t *claim;            // [n_rows]
+  int32_t *first;            // [n + 1]: new pages of the forks before; -1 - that for a refused one
+  int32_t *block_sum;        // [blocks]
+  int32_t *list;             // [n_pages]: free pages in order; of a compaction: a moved page's rank
+  int32_t *word;             // fork: whether the pages suffice; compaction: L and the moves
+  int32_t *err;
+};
+
+// Sum over the work-group of x, in every thread.
+template <class T>
+__device__ inline T block_total(T x, T *lds) {
+#pragma unroll
+  for (int w = 32; w; w >>= 1) x += __shfl_xor(x, w, 64);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+  __syncthreads();
+  T sum = 0;
+#pragma unroll
+  for (int i = 0; i < kBlock / 64; ++i) sum += lds[i];
+  return sum;
+}
+// The sum of x over the threads before this one.
+template <class T>
+__device__ inline T block_before(T x, T *lds) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  T run = x;
+#pragma unroll
+  for (int w = 1; w < 64; w <<= 1) {
+    const T y = __shfl_up(run, w, 64);
+    if (lane >= w) run += y;
+  }
+  __syncthreads();
+  if (lane == 63) lds[wave] = run;
+  __syncthreads();
+  T before = run - x;
+  for (int i = 0; i < wave; ++i) before += lds[i];
+  return before;
+}
+
+// The pages of block b that are in use (LIVE) or free, and for a fork, in a block of its own,
+// which forks are sound and how many new pages each takes.
+template <bool LIVE>
+__global__ void __launch_bounds__(kBlock) k_pages_count(PoolArgs a) {
+  __shared__ int32_t lds[kBlock / 64];
+  const int tid = threadIdx.x;
+  if (int32_t(blockIdx.x) < a.blocks) {
+    int32_t x = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int32_t p = blockIdx.x * kPer + i * kBlock + tid;
+      if (p < a.n_pages) x += (a.refs[p] > 0) == LIVE;
+    }
+    x = block_total(x, lds);
+    if (tid == 0) a.block_sum[blockIdx.x] = x;
+    return;
+  }
+  // a child belongs to the lowest index that names it
+  for (int32_t i = tid; i < a.n; i += kBlock)
+    if (uint32_t(a.child[i]) < uint32_t(a.n_rows))
+      __hip_atomic_store(a.claim + a.child[i], INT32_MAX, __ATOMIC_RELAXED,
+                         __HIP_MEMORY_SCOPE_AGENT);
+  __threadfence();
+  __syncthreads();
+  for (int32_t i = tid; i < a.n; i += kBlock)
+    if (uint32_t(a.child[i]) < uint32_t(a.n_rows)) atomicMin(a.claim + a.child[i], i);
+  __threadfence();
+  __syncthreads();
+  __shared__ int64_t lds64[kBlock / 64];
+  const int64_t most = int64_t(a.n_pages) + 1;  // more than there are is as many as that
+  int64_t before = 0;
+  for (int32_t i0 = 0; i0 < a.n; i0 += kBlock) {
+    const int32_t i = i0 + tid;
+    int64_t need = 0;
+    bool ok = false;
+    if (i < a.n) {
+      const int32_t p = a.parent[i], c = a.child[i], sh = a.shared[i], room = a.room[i];
+      const int32_t size = 1 << a.page_shift;
+      ok = p >= -1 && p < a.n_rows && uint32_t(c) < uint32_t(a.n_rows) && sh >= 0 && room >= sh;
+      if (ok)
+        ok = __hip_atomic_load(a.claim + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == i &&
+             a.held[c] == 0;
+      const int32_t pages = int32_t((int64_t(room) + size - 1) >> a.page_shift);
+      if (ok) ok = pages <= a.width;
+      if (ok && sh > 0)
+        ok = p >= 0 && a.held[p] >= 0 && a.held[p] <= a.width &&
+             int32_t((int64_t(sh) + size - 1) >> a.page_shift) <= a.held[p];
+      if (ok)
+        need = pages - (sh >> a.page_shift);
+      else
+        raise_err(a.err, FS_E_RANGE);
+    }
+    const int64_t f = min(before + block_before(need, lds64), most);
+    before += block_total(need, lds64);
+    if (i < a.n) a.first[i] = int32_t(ok ? f : -1 - f);
+  }
+  if (tid == 0) a.first[a.n] = int32_t(min(before, most));
+}
+
+// The first free pages, as many as the forks take, in order of ids.
+__global__ void __launch_bounds__(kBlock) k_pages_list(PoolArgs a) {
+  __shared__ int32_t lds[kBlock / 64];
+  const int tid = threadIdx.x;
+  const int32_t wanted = a.first[a.n];
+  int32_t before = 0, all = 0;
+  for (int32_t b = tid; b < a.blocks; b += kBlock) {
+    const int32_t x = a.block_sum[b];
+    all += x;
+    if (b < int32_t(blockIdx.x)) before += x;
+  }
+  before = block_total(before, lds);
+  all = block_total(all, lds);
+  if (blockIdx.x == 0 && tid == 0) {
+    *a.word = wanted <= all;
+    if (wanted > all) raise_err(a.err, FS_E_OVERFLOW);
+  }
+  if (wanted > all || before >= wanted) return;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int32_t p = blockIdx.x * kPer + i * kBlock + tid;
+    const int32_t is = p < a.n_pages && a.refs[p] <= 0;
+    const int32_t at = before + block_before(is, lds);
+    if (is && at < wanted) a.list[at] = p;
+    before += block_total(is, lds);
+  }
+}
+
+// A work-group for a fork: the child's row, counts and the page to be copied.
+__global__ void __launch_bounds__(256) k_pages_fork(PoolArgs a) {
+  const int32_t i = blockIdx.x;
+  const int tid = threadIdx.x;
+  int32_t first = a.first[i];
+  bool go = first >= 0 && *a.word;
+  const int32_t p = go ? a.parent[i] : 0, c = go ? a.child[i] : 0, sh = go ? a.shared[i] : 0;
+  const int32_t size = 1 << a.page_shift, full = sh >> a.page_shift;
+  const int32_t pages = go ? int32_t((int64_t(a.room[i]) + size - 1) >> a.page_shift) : 0;
+  const bool part = sh & (size - 1);
+  const int32_t *from = a.table + int64_t(max(p, 0)) * a.stride;
+  bool bad = false;
+  for (int32_t j = tid; j < full + part; j += 256) bad |= uint32_t(from[j]) >= uint32_t(a.n_pages);
+  if (__syncthreads_or(bad)) {
+    raise_err(a.err, FS_E_RANGE);
+    go = false;
+  }
+  if (tid == 0) {
+    a.src[i] = go && part ? from[full] : -1;
+    a.dst[i] = go && part ? a.list[first] : -1;
+    if (go) a.held[c] = pages;
+  }
+  if (!go) return;
+  int32_t *to = a.table + int64_t(c) * a.stride;
+  for (int32_t j = tid; j < pages; j += 256) {
+    const int32_t id = j < full ? from[j] : a.list[first + j - full];
+    to[j] = id;
+    atomicAdd(a.refs + id, 1);
+  }
+}
+
+__global__ void __launch_bounds__(256) k_pages_free(PoolArgs a) {
+  __shared__ int32_t got;
+  const int32_t r = a.rows[blockIdx.x];
+  const int tid = threadIdx.x;
+  if (uint32_t(r) >= uint32_t(a.n_rows)) {
+    if (tid == 0) raise_err(a.err, FS_E_RANGE);
+    return;
+  }
+  if (tid == 0) got = atomicExch(a.held + r, 0);  // of a row named twice, one gets them
+  __syncthreads();
+  int32_t n = got;
+  bool bad = n < 0 || n > a.width;
+  if (bad) n = 0;
+  const int32_t *row = a.table + int64_t(r) * a.stride;
+  for (int32_t j = tid; j < n; j += 256) {
+    const int32_t id = row[j];
+    if (uint32_t(id) >= uint32_t(a.n_pages)) {
+      bad = true;
+    } else if (atomicSub(a.refs + id, 1) <= 0) {
+      atomicAdd(a.refs + id, 1);
+      bad = true;
+    }
+  }
+  if (bad) raise_err(a.err, FS_E_RANGE);
+}
+
+// The pages in use with ids from L on, and the free ones below, in order of ids: src and dst.
+__global__ void __launch_bounds__(kBlock) k_pages_moves(PoolArgs a) {
+  __shared__ int32_t lds[kBlock / 64];
+  const int tid = threadIdx.x;
+  int32_t before = 0, L = 0;
+  for (int32_t b = tid; b < a.blocks; b += kBlock) {
+    const int32_t x = a.block_sum[b];
+    L += x;
+    if (b < int32_t(blockIdx.x)) before += x;
+  }
+  before = block_total(before, lds);
+  L = block_total(L, lds);
+  // of the pages in use, those below L
+  const int32_t lb = L / kPer;
+  int32_t below = 0;
+  for (int32_t b = tid; b < lb; b += kBlock) below += a.block_sum[b];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int32_t p = lb * kPer + i * kBlock + tid;
+    if (p < L) below += a.refs[p] > 0;
+  }
+  below = block_total(below, lds);
+  const int32_t moves = L - below;
+  if (blockIdx.x == 0 && tid == 0) {
+    *a.count = moves;
+    a.word[0] = L;
+    a.word[1] = moves;
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int32_t p = blockIdx.x * kPer + i * kBlock + tid;
+    const int32_t refs = p < a.n_pages ? a.refs[p] : 0;
+    const int32_t live = refs > 0;
+    const int32_t rank = before + block_before(live, lds);  // pages in use before p
+    before += block_total(live, lds);
+    if (p >= a.n_pages) continue;
+    if (p < L) {
+      if (!live) a.dst[p - rank] = p;
+    } else {
+      a.list[p] = live ? rank - below : -1;
+      if (live) a.src[rank - below] = p;
+    }
+    if (a.refs_out != a.refs) a.refs_out[p] = p < L ? refs : 0;
+    if (p >= moves && p < a.n_pages / 2) a.src[p] = a.dst[p] = -1;
+  }
+}
+
+// Counts of moved pages, and the table's ids.  The first table_blocks work-groups, `per_row` a
+// row, take the table.
+__global__ void __launch_bounds__(256) k_pages_remap(PoolArgs a, int32_t table_blocks,
+                                                     int32_t per_row) {
+  const int32_t L = a.word[0], moves = a.word[1];
+  const int tid = threadIdx.x;
+  if (int32_t(blockIdx.x) >= table_blocks) {
+    const int32_t step = (gridDim.x - table_blocks) * 256;
+    for (int32_t i = (blockIdx.x - table_blocks) * 256 + tid; i < moves; i += step) {
+      const int32_t s = a.src[i], d = a.dst[i];
+      const int32_t x = a.refs[s];
+      a.refs_out[s] = 0;
+      a.refs_out[d] = x;
+    }
+    return;
+  }
+  const int32_t r = blockIdx.x / per_row, part = blockIdx.x - r * per_row;
+  int32_t held = a.held[r];
+  bool bad = held < 0 || held > a.width;
+  if (bad) held = 0;
+  for (int32_t j = part * 256 + tid; j < held; j += per_row * 256) {
+    int32_t id = a.table[int64_t(r) * a.stride + j];
+    if (uint32_t(id) >= uint32_t(a.n_pages)) {
+      bad = true;
+    } else if (id >= L) {
+      const int32_t m = a.list[id];
+      if (m >= 0)
+        id = a.dst[m];
+      else
+        bad = true;  // a held page that is free
+    }
+    a.table_out[int64_t(r) * a.out_stride + j] = id;
+  }
+  if (bad) raise_err(a.err, FS_E_RANGE);
+}
+
+// ---- copies
+struct CopyArgs {
+  PageArrays arrays;
+  PageShape codes, scales;
+  int32_t n_layers, n_kinds, n_pages, n;
+  int32_t code_parts, scale_parts;  // work-groups' shares of a page
+  const int32_t *src, *dst, *count;
+  int32_t *err;
+};
+
+constexpr int kUnroll = 4;  // loads of a thread under way
+
+// Bytes by T from the pieces of one page to another's: share `part` of `parts`.
+template <class T>
+__device__ inline void copy_page(char *base, const PageShape &s, int64_t from, int64_t to,
+                                 int32_t part) {
+  const uint32_t per = s.bytes / sizeof(T), total = s.heads * s.tokens * per;
+  const uint32_t begin = uint32_t(part) * (256 * kUnroll);
+  T x[kUnroll];
+  int64_t at[kUnroll];
+#pragma unroll
+  for (int i = 0; i < kUnroll; ++i) {
+    const uint32_t e = begin + i * 256 + threadIdx.x;
+    at[i] = -1;
+    if (e >= total) continue;
+    if (per == total) {  // the page is one piece
+      at[i] = int64_t(e) * sizeof(T);
+    } else {
+      const uint32_t piece = e / per, h = piece / s.tokens;
+      at[i] = int64_t(h) * s.head_stride + int64_t(piece - h * s.tokens) * s.token_stride +
+              int64_t(e - piece * per) * sizeof(T);
+    }
+    x[i] = *reinterpret_cast<const T *>(base + from + at[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kUnroll; ++i)
+    if (at[i] >= 0) *reinterpret_cast<T *>(base + to + at[i]) = x[i];
+}
+
+template <bool VEC_SCALES>
+__global__ void __launch_bounds__(256) k_pages_copy(CopyArgs a) {
+  typedef uint32_t __attribute__((ext_vector_type(4))) V;
+  const int32_t n = a.count ? min(max(*a.count, 0), a.n) : a.n;
+  const int32_t each = 2 * a.code_parts + (a.n_kinds > 2 ? 2 * a.scale_parts : 0);
+  const int32_t per = each * a.n_layers;
+  for (int64_t u = blockIdx.x; u < int64_t(n) * per; u += gridDim.x) {
+    const int32_t i = int32_t(u / per), r = int32_t(u - int64_t(i) * per);
+    const int32_t src = a.src[i], dst = a.dst[i];
+    if (src == -1 && dst == -1) continue;
+    if (uint32_t(src) >= uint32_t(a.n_pages) || uint32_t(dst) >= uint32_t(a.n_pages)) {
+      if (r == 0 && threadIdx.x == 0) raise_err(a.err, FS_E_RANGE);
+      continue;
+    }
+    const int32_t layer = r / each, w = r - layer * each;
+    if (w < 2 * a.code_parts) {
+      const int32_t kind = w >= a.code_parts;
+      copy_page<V>(a.arrays.at[layer][kind], a.codes, src * a.codes.page_stride,
+                   dst * a.codes.page_stride, w - kind * a.code_parts);
+    } else {
+      const int32_t ws = w - 2 * a.code_parts, kind = ws >= a.scale_parts;
+      char *base = a.arrays.at[layer][2 + kind];
+      const int64_t from = src * a.scales.page_stride, to = dst * a.scales.page_stride;
+      if constexpr (VEC_SCALES)
+        copy_page<V>(base, a.scales, from, to, ws - kind * a.scale_parts);
+      else
+        copy_page<uint8_t>(base, a.scales, from, to, ws - kind * a.scale_parts);
+    }
+  }
+}
+
+size_t round256(size_t x) { return (x + 255) / 256 * 256; }
+int32_t page_blocks(const fs_pages *p) { return (p->n_pages + kPer - 1) / kPer; }
+
+PoolArgs pool_args(const fs_pages *p, int32_t n, void *ws, int32_t *err) {
+  PoolArgs a = {};
+  a.n_pages = p->n_pages;
+  a.page_shift = __builtin_ctz(unsigned(p->page_size));
+  a.n_rows = p->n_rows;
+  a.width = p->width;
+  a.refs = p->refs;
+  a.table = p->table;
+  a.held = p->held;
+  a.stride = p->table_stride;
+  a.n = n;
+  a.blocks = page_blocks(p);
+  a.err = err;
+  char *at = static_cast<char *>(ws);
+  auto take = [&](size_t values) {
+    int32_t *x = reinterpret_cast<int32_t *>(at);
+    at += round256(values * 4);
+    return x;
+  };
+  a.word = take(2);
+  a.block_sum = take(a.blocks);
+  a.list = take(p->n_pages);
+  a.claim = take(p->n_rows);
+  a.first = take(size_t(n) + 1);
+  return a;
+}
+
+}  // namespace
+
+size_t pages_workspace_bytes(const fs_pages *p, int32_t n) {
+  return 256 + round256(size_t(page_blocks(p)) * 4) + round256(size_t(p->n_pages) * 4) +
+         round256(size_t(p->n_rows) * 4) + round256((size_t(n) + 1) * 4);
+}
+
+hipError_t launch_pages_free(const fs_pages *p, int32_t n, const int32_t *rows, int32_t *err,
+                             hipStream_t stream) {
+  PoolArgs a = pool_args(p, 0, nullptr, err);
+  a.rows = rows;
+  hipLaunchKernelGGL(k_pages_free, dim3(n), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_fork(const fs_pages *p, int32_t n, const int32_t *parent,
+                             const int32_t *child, const int32_t *shared, const int32_t *room,
+                             int32_t *src, int32_t *dst, void *ws, int32_t *err,
+                             hipStream_t stream) {
+  PoolArgs a = pool_args(p, n, ws, err);
+  a.parent = parent;
+  a.child = child;
+  a.shared = shared;
+  a.room = room;
+  a.src = src;
+  a.dst = dst;
+  hipLaunchKernelGGL((k_pages_count<false>), dim3(a.blocks + 1), dim3(kBlock), 0, stream, a);
+  hipLaunchKernelGGL(k_pages_list, dim3(a.blocks), dim3(kBlock), 0, stream, a);
+  hipLaunchKernelGGL(k_pages_fork, dim3(n), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_compact(const fs_pages *p, int32_t *refs_out, int32_t *table_out,
+                                int64_t table_out_stride, int32_t *src, int32_t *dst,
+                                int32_t *count, void *ws, int32_t *err, hipStream_t stream) {
+  PoolArgs a = pool_args(p, 0, ws, err);
+  a.refs_out = refs_out;
+  a.table_out = table_out;
+  a.out_stride = table_out_stride;
+  a.src = src;
+  a.dst = dst;
+  a.count = count;
+  hipLaunchKernelGGL((k_pages_count<true>), dim3(a.blocks), dim3(kBlock), 0, stream, a);
+  hipLaunchKernelGGL(k_pages_moves, dim3(a.blocks), dim3(kBlock), 0, stream, a);
+  const int32_t per_row = p->width <= 1024 ? 1 : p->width <= 65536 ? (p->width + 1023) / 1024 : 64;
+  const int32_t table_blocks = p->n_rows * per_row;
+  const int32_t moves = p->n_pages / 2 / 256 + 1;
+  hipLaunchKernelGGL(k_pages_remap, dim3(table_blocks + (moves < 256 ? moves : 256)), dim3(256), 0,
+                     stream, a, table_blocks, per_row);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_copy(const PageArrays &arrays, int32_t n_layers, int32_t n_kinds,
+                             const PageShape &codes, const PageShape &scales, int32_t n_pages,
+                             int32_t n, const int32_t *src, const int32_t *dst,
+                             const int32_t *count, int32_t *err, hipStream_t stream) {
+  CopyArgs a = {arrays, codes, scales, n_layers, n_kinds, n_pages, n, 0, 0, src, dst, count, err};
+  bool vec = true;
+  auto parts = [](const PageShape &s, uint32_t unit) {
+    const int64_t units = int64_t(s.heads) * s.tokens * (s.bytes / unit);
+    return int32_t((units + 256 * kUnroll - 1) / (256 * kUnroll));
+  };
+  a.code_parts = parts(codes, 16);
+  if (n_kinds > 2) {
+    int64_t all = scales.page_stride | scales.bytes | scales.head_stride | scales.token_stride;
+    for (int32_t i = 0; i < n_layers; ++i)
+      all |= int64_t(reinterpret_cast<uintptr_t>(arrays.at[i][2])) |
+             int64_t(reinterpret_cast<uintptr_t>(arrays.at[i][3]));
+    vec = all % 16 == 0;
+    a.scale_parts = parts(scales, vec ? 16 : 1);
+  }
+  const int64_t units =
+      int64_t(n) * n_layers * (2 * a.code_parts + (n_kinds > 2 ? 2 * a.scale_parts : 0));
+  const dim3 grid(uint32_t(units < 4096 ? units : 4096)), block(256);
+  if (vec)
+    hipLaunchKernelGGL((k_pages_copy<true>), grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_pages_copy<false>), grid, block, 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace fs

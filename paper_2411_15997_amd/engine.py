@@ -408,10 +408,15 @@ def fs_rope_append(step: Step, cache: KVCache, rope: Rope, q, k, v, q_out=None, 
     return q_out
 
 
+def _bounded(n):
+    """A window or a count of sinks: one beyond every length is like the largest."""
+    return max(-1, min(int(n), 0x7fffffff))
+
+
 def fs_paged_attention(step: Step, cache: KVCache, q, scale, window=0, out=None, lse=None,
-                       want_lse=False, ws=None, err=None, check=True):
+                       want_lse=False, ws=None, err=None, check=True, sinks=0):
     """Attention of q [rows][heads][dim] over the cache; returns out, or (out, lse) when the
-    log-sum-exp [rows][heads] is wanted."""
+    log-sum-exp [rows][heads] is wanted.  A window leaves the first `sinks` tokens visible."""
     shape, gpu = q.shape, step.gpu
     T, H, D = shape
     if q.dtype != cache.dtype or D != cache.head_dim:
@@ -422,7 +427,7 @@ def fs_paged_attention(step: Step, cache: KVCache, q, scale, window=0, out=None,
     _on(gpu, q, out, lse, ws, err)
     if gpu != _current_gpu():
         return _there(gpu, fs_paged_attention, step, cache, q, scale, window, out, lse, want_lse, ws,
-                      err, check)
+                      err, check, sinks)
     qp, qs = _rows(q, "q", (step.rows, H, D))
     if out is None:
         out = _torch().empty_like(q)  # packed, whatever q's row stride
@@ -441,10 +446,17 @@ def fs_paged_attention(step: Step, cache: KVCache, q, scale, window=0, out=None,
     if err is None:
         err = cleared_err_word(q.device)
     L = _lib()
-    window = max(-1, min(int(window), 0x7fffffff))  # one beyond every length is none
-    ws, wp, wn = _workspace(ws, L.fs_attention_workspace(step.ref, cache.ref, H, window), q)
-    code = L.fs_paged_attention(step.ref, cache.ref, H, scale, window, qp, qs, op, os_, lp, wp, wn,
-                                err.data_ptr(), _raw_stream(gpu))
+    window = _bounded(window)
+    if sinks:
+        sinks = _bounded(sinks)
+        ws, wp, wn = _workspace(
+            ws, L.fs_attention_sinks_workspace(step.ref, cache.ref, H, window, sinks), q)
+        code = L.fs_paged_attention_sinks(step.ref, cache.ref, H, scale, window, sinks, qp, qs, op,
+                                          os_, lp, wp, wn, err.data_ptr(), _raw_stream(gpu))
+    else:
+        ws, wp, wn = _workspace(ws, L.fs_attention_workspace(step.ref, cache.ref, H, window), q)
+        code = L.fs_paged_attention(step.ref, cache.ref, H, scale, window, qp, qs, op, os_, lp, wp,
+                                    wn, err.data_ptr(), _raw_stream(gpu))
     if code or check:
         _done(code, "fs_paged_attention", err, check)
     return out if lse is None else (out, lse)
