@@ -26,6 +26,9 @@ struct Attn4Args : AttnArgs {  // `c` is the cache's codes, in bytes
 template <bool BF>
 constexpr float kLift4 = BF ? -18.f : 7.f;
 
+// Keys of a split of few rows, at most: a quarter of the bytes of the 16-bit cache's.
+constexpr int32_t kFewMost4 = 2048;
+
 // Codes of N neighbouring values: 16 bytes for 32 of them, 8 for 16.
 template <int N>
 using Codes = uint32_t __attribute__((ext_vector_type(N / 8)));
@@ -39,6 +42,17 @@ __device__ inline void put_poison(uint32_t poison, int group, Acc &o) {
     for (int i = 0; i < N; ++i) o[i] = NAN;
 }
 
+// A wave's V tile: key rows further apart than their D values, so that 16 rows' chunks, and 4
+// rows' transposed reads, fall on different banks at addresses that differ by constants.
+template <int D>
+constexpr int kVRow = D == 128 ? 144 : 72;
+template <int D>
+constexpr int kVTile = 32 * kVRow<D> + 8;
+template <int D>
+__device__ inline int v_row(int r) {
+  return r * kVRow<D> + (D == 128 ? (r >> 3 & 1) * 8 : 0);
+}
+
 // ---- few rows: NT tiles of 16 rows, WAVES waves, which take 32 keys each in turn
 template <bool BF, int D, int NT, int WAVES>
 __device__ __forceinline__ void attn4_few(const Attn4Args &a, int block, short *lds) {
@@ -47,7 +61,7 @@ __device__ __forceinline__ void attn4_few(const Attn4Args &a, int block, short *
   constexpr int DL = D / 4;   // neighbouring dimensions of a key that a lane takes
   constexpr int kIds = 512;   // page ids kept in LDS
   constexpr bool kTwoParts = NT <= 2;  // of a probability
-  auto v_lds = reinterpret_cast<short(*)[32 * D]>(lds);  // a wave's V
+  constexpr int VB = 4;       // 16-column blocks of V read at once
   __shared__ float wm[WAVES][NT * 16], wl[WAVES][NT * 16];
   __shared__ uint32_t ids[kIds];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -75,8 +89,9 @@ __device__ __forceinline__ void attn4_few(const Attn4Args &a, int block, short *
   int32_t pos[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
+    // (rows past the last are that one again)
     const int r = min(t * 16 + r16, R - 1), tok = r / G, h = hk * G + (r - tok * G);
-    pos[t] = t * 16 + r16 < R ? kv - n + tok : -1;
+    pos[t] = kv - n + tok;
     const short *qp = a.q + (q0 + tok) * a.q_stride + h * D + g4 * DL;
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
@@ -90,11 +105,9 @@ __device__ __forceinline__ void attn4_few(const Attn4Args &a, int block, short *
 #pragma unroll
   for (int t = 0; t < NT; ++t) m[t] = -INFINITY, l[t] = 0.f;
 
-  struct Tile {
-    Codes<DL> k[2], v[2];
-    uint32_t ks[2], vs[2];
-  };
-  short *vb = v_lds[wave];
+  short *const v_to = lds + wave * kVTile<D> + v_row<D>(r16) + g4 * DL;
+  const short *const v_from =
+      lds + wave * kVTile<D> + v_row<D>(4 * g4 + (r16 >> 2)) + (r16 & 3) * 4;
 
   for (int32_t from = lo; from < hi;) {
     const PageIds span = page_ids<true>(kr, from, hi, a.c.page_shift, kIds);
@@ -108,7 +121,10 @@ __device__ __forceinline__ void attn4_few(const Attn4Args &a, int block, short *
     __syncthreads();
     const int32_t first = from + wave * 32;
     const int32_t tiles = first < end ? (end - first + WAVES * 32 - 1) / (WAVES * 32) : 0;
-    auto load = [&](int32_t t, Tile &x) {
+    // this lane's part of two keys
+    Codes<DL> kc[2], vc[2];
+    uint32_t ks[2], vs[2];
+    auto load = [&](int32_t t) {
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const int32_t j = kr.key(min(first + t * (WAVES * 32) + b * 16 + r16, end - 1));
@@ -117,25 +133,22 @@ __device__ __forceinline__ void attn4_few(const Attn4Args &a, int block, short *
             uint64_t(page) * a.c.page_stride + (inside + slot * a.c.token_stride);
         const uint64_t sat =
             uint64_t(page) * a.sc.page_stride + (s_inside + slot * a.sc.token_stride);
-        x.k[b] = *reinterpret_cast<const Codes<DL> *>(a.c.k + at);
-        x.v[b] = *reinterpret_cast<const Codes<DL> *>(a.c.v + at);
-        x.ks[b] = a.sc.k[sat];
-        x.vs[b] = a.sc.v[sat];
+        kc[b] = *reinterpret_cast<const Codes<DL> *>(a.c.k + at);
+        vc[b] = *reinterpret_cast<const Codes<DL> *>(a.c.v + at);
+        ks[b] = a.sc.k[sat];
+        vs[b] = a.sc.v[sat];
       }
     };
-    Tile x, next;
-    if (tiles > 0) load(0, next);
+    if (tiles > 0) load(0);
     for (int32_t t = 0; t < tiles; ++t) {
       const int32_t j0 = first + t * (WAVES * 32);
-      x = next;
-      if (t + 1 < tiles) load(t + 1, next);
       f32x4 sc[NT][2] = {};
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const float unit = scale_of<BF>(x.ks[b]);
+        const float unit = scale_of<BF>(ks[b]);
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-          const s16x8 kf = values8<BF>(x.k[b][k], unit);
+          const s16x8 kf = values8<BF>(kc[b][k], unit);
 #pragma unroll
           for (int r = 0; r < NT; ++r) sc[r][b] = mfma_16x16x32<BF>(kf, qf[r][k], sc[r][b]);
         }
@@ -143,16 +156,39 @@ __device__ __forceinline__ void attn4_few(const Attn4Args &a, int block, short *
       // V: this lane's dimensions of two keys, as chunks of 8
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const float unit = scale_of<BF>(x.vs[b]);
-        const bool bad = x.vs[b] > kTopScale<BF>;
+        const float unit = scale_of<BF>(vs[b]);
+        const bool bad = vs[b] > kTopScale<BF>;
 #pragma unroll
         for (int k = 0; k < KS; ++k)
-          *reinterpret_cast<s16x8 *>(vb + tile_at<D>(b * 16 + r16, g4 * KS + k)) =
-              values8<BF>(bad ? 0 : x.v[b][k], unit);
+          *reinterpret_cast<s16x8 *>(v_to + b * 16 * kVRow<D> + k * 8) =
+              values8<BF>(bad ? 0 : vc[b][k], unit);
       }
+      if (__any(max(max(ks[0], ks[1]), max(vs[0], vs[1])) > kTopScale<BF>)) {
+#pragma unroll 1
+        for (int b = 0; b < 2; ++b) {
+          uint64_t bad = __ballot((b ? ks[1] : ks[0]) > kTopScale<BF>);
+          bad |= bad >> 32;
+          bad |= bad >> 16;  // bit i: key i of the 16
+#pragma unroll
+          for (int r = 0; r < NT; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (bad >> (g4 * 4 + i) & 1) (b ? sc[r][1] : sc[r][0])[i] = NAN;
+          for (uint64_t vbad = __ballot((b ? vs[1] : vs[0]) > kTopScale<BF>); vbad;
+               vbad &= vbad - 1) {
+            const int i = __builtin_ctzll(vbad);
+            const int32_t v = j0 + b * 16 + (i & 15), j = kr.key(v);
+#pragma unroll
+            for (int r = 0; r < NT; ++r)
+              if (j <= pos[r] && v < end &&
+                  (a.window == 0 || j > pos[r] - a.window || j < a.sinks))
+                poison[r] |= 1u << ((i >> 4) * DL / 32);
+          }
+        }
+      }
+      // the codes have been used: the next ones come while the rest is computed
+      if (t + 1 < tiles) load(t + 1);
       const int32_t key0 = kr.key(j0), key31 = kr.key(j0 + 31);
-      const bool odd = max(max(x.ks[0], x.ks[1]), max(x.vs[0], x.vs[1])) > kTopScale<BF>;
-      const uint64_t odd_any = __ballot(odd);
       // keys that some row does not see
       const bool edge = j0 + 32 > end || key31 > kv - n || (a.window && key0 <= kv - 1 - a.window);
       s16x8 pf[NT], pl[NT];
@@ -163,25 +199,7 @@ __device__ __forceinline__ void attn4_few(const Attn4Args &a, int block, short *
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int i = 0; i < 4; ++i) p[b * 4 + i] = sc[r][b][i];
-        if (odd_any) {
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            uint64_t bad = __ballot(x.ks[b] > kTopScale<BF>);
-            bad |= bad >> 32;
-            bad |= bad >> 16;  // bit i: key i of the 16
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (bad >> (g4 * 4 + i) & 1) p[b * 4 + i] = NAN;
-            for (uint64_t vbad = __ballot(x.vs[b] > kTopScale<BF>); vbad; vbad &= vbad - 1) {
-              const int i = __builtin_ctzll(vbad);
-              const int32_t v = j0 + b * 16 + (i & 15), j = kr.key(v);
-              if (j <= pos[r] && v < end &&
-                  (a.window == 0 || j > pos[r] - a.window || j < a.sinks))
-                poison[r] |= 1u << ((i >> 4) * DL / 32);
-            }
-          }
-        }
-        if (edge || pos[r] < 0) {
+        if (edge) {
 #pragma unroll
           for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -194,7 +212,7 @@ __device__ __forceinline__ void attn4_few(const Attn4Args &a, int block, short *
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) top = fmaxf(top, p[i]);
-        top = max_of_halves(fmaxf(top, __shfl_xor(top, 16, 64)));
+        top = max_of_halves(max_of_16s(top));
         const float m2 = fmaxf(m[r], top);
         // (-inf less -inf is no number and asks for nothing)
         if (__any((m2 - m[r]) * a.c2 > kSlack)) {
@@ -217,15 +235,21 @@ __device__ __forceinline__ void attn4_few(const Attn4Args &a, int block, short *
       }
       // keys 4 g4 .. + 3 and 16 + 4 g4 .. + 3 of the tile, 16 columns at a time
 #pragma unroll
-      for (int d = 0; d < DB; ++d) {
-        const int row = 4 * g4 + (r16 >> 2), col = d * 16 + (r16 & 3) * 4;
-        const s16x4 v0 = read_tr(vb + tile_at<D>(row, col >> 3) + (col & 7));
-        const s16x4 v1 = read_tr(vb + tile_at<D>(row + 16, col >> 3) + (col & 7));
-        const s16x8 vv = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+      for (int d0 = 0; d0 < DB; d0 += VB) {
+        s16x8 vv[VB];
+#pragma unroll
+        for (int d = 0; d < VB; ++d)
+          vv[d] = __builtin_shufflevector(read_tr(v_from + (d0 + d) * 16),
+                                          read_tr(v_from + 16 * kVRow<D> + (d0 + d) * 16), 0, 1, 2,
+                                          3, 4, 5, 6, 7);
 #pragma unroll
         for (int r = 0; r < NT; ++r) {
-          o[r][d] = mfma_16x16x32<BF>(vv, pf[r], o[r][d]);
-          if (kTwoParts) o[r][d] = mfma_16x16x32<BF>(vv, pl[r], o[r][d]);
+#pragma unroll
+          for (int d = 0; d < VB; ++d) o[r][d0 + d] = mfma_16x16x32<BF>(vv[d], pf[r], o[r][d0 + d]);
+          if (kTwoParts)
+#pragma unroll
+            for (int d = 0; d < VB; ++d)
+              o[r][d0 + d] = mfma_16x16x32<BF>(vv[d], pl[r], o[r][d0 + d]);
         }
       }
     }
@@ -520,8 +544,9 @@ __device__ __forceinline__ void attn4_chunk(const Attn4Args &a, int block, int z
 }
 
 template <bool BF, int D, int NT, int WAVES>
-__global__ void __launch_bounds__(WAVES * 64) k_attn4_few(Attn4Args a) {
-  __shared__ __align__(16) short lds[WAVES * 32 * D];
+__global__ void __launch_bounds__(WAVES * 64, NT == 1 ? 4 : NT == 2 ? (D == 64 ? 3 : 2) : D == 64 ? 2 : 1)
+k_attn4_few(Attn4Args a) {
+  __shared__ __align__(16) short lds[WAVES * kVTile<D>];
   attn4_few<BF, D, NT, WAVES>(a, blockIdx.x, lds);
 }
 template <bool BF, int D, int WAVES>
@@ -542,6 +567,41 @@ __global__ void __launch_bounds__(256, 2) k_attn4_mixed(Attn4Args a, int chunk, 
     attn4_chunk<BF, D, 4>(a, block % tiles, block / tiles, lds, scales, &odd);
   else
     attn4_few<BF, D, NT, 4>(a, block - chunk, lds);
+}
+
+// The join of few rows in very many splits: a work-group for 32 columns of a row and head, 32
+// splits side by side.  (One request of 200,001 tokens, 32 heads in 224 splits: JOINUS)
+constexpr int kManySplits = 128;
+template <bool BF, int D>
+__global__ void __launch_bounds__(256) k_attn4_join_many(Attn4Args a) {
+  __shared__ f32x4 part[4][8];
+  __shared__ float ls[4];
+  const int32_t h = blockIdx.x / (D / 32), s = blockIdx.y, tok = blockIdx.z;
+  const int32_t q0 = __ldg(a.q_off + s), n = __ldg(a.q_off + s + 1) - q0;
+  if (tok >= n || n * a.group > kFewRows) return;
+  int32_t code = 0;
+  const int32_t kv = checked_len(a.kv_len, s, a.max_kv, code);
+  const int32_t len = key_range(a, n, kv, 0, n - 1).length();
+  if (len <= a.few_split) return;  // written whole
+  const Parts p{a.few_o, a.few_ml, (int64_t(s) * a.few_tokens + tok) * a.n_heads + h,
+                int64_t(a.n_seqs) * a.few_tokens * a.n_heads,
+                (len + a.few_split - 1) / a.few_split};
+  const float top = top_of<64>(p);
+  const int tid = threadIdx.x, c = blockIdx.x % (D / 32) * 8 + tid % 8;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  float sum = 0.f;
+  add_splits<D, 32>(a, p, tid / 8, c, top, acc, sum);
+#pragma unroll
+  for (int w = 8; w < 64; w <<= 1) {
+    sum += __shfl_xor(sum, w, 64);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], w, 64);
+  }
+  if ((tid & 63) < 8) part[tid >> 6][tid & 63] = acc, ls[tid >> 6] = sum;
+  __syncthreads();
+  if (tid >= 8) return;
+  acc = part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid];
+  put_joined<BF, D>(a, q0 + tok, h, c, acc, ls[0] + ls[1] + ls[2] + ls[3], top);
 }
 
 template <bool BF, int D>
@@ -578,7 +638,10 @@ void run(const Attn4Args &a, const Plan &p, hipStream_t stream) {
     if (p.chunk_rows == 128)
       hipLaunchKernelGGL((k_attn4_chunk<BF, D, 4>), grid, block, 0, stream, a);
   }
-  if (p.few_splits > 1)
+  if (p.few_splits >= kManySplits)
+    hipLaunchKernelGGL((k_attn4_join_many<BF, D>), dim3(a.n_heads * (D / 32), a.n_seqs, p.few_tokens),
+                       block, 0, stream, a);
+  else if (p.few_splits > 1)
     hipLaunchKernelGGL((k_attn_join_few<BF, D>), dim3(a.n_heads, a.n_seqs, p.few_tokens), block, 0,
                        stream, a);
   if (p.chunk_splits > 1) {
@@ -591,7 +654,7 @@ void run(const Attn4Args &a, const Plan &p, hipStream_t stream) {
 
 size_t attention4_workspace_bytes(const fs_step *s, const fs_kv_cache4 *c, int32_t n_heads,
                                   int32_t window, int32_t sinks) {
-  const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks);
+  const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks, kFewMost4);
   return space(plan(s, sh), s, sh).total();
 }
 
@@ -599,7 +662,7 @@ hipError_t launch_attention4(const fs_step *s, const fs_kv_cache4 *c, int32_t dt
                              int32_t n_heads, float scale, int32_t window, int32_t sinks,
                              const void *q, int64_t q_stride, void *out, int64_t out_stride,
                              float *lse, void *ws, int32_t *err, hipStream_t stream) {
-  const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks);
+  const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks, kFewMost4);
   const Plan p = plan(s, sh);
   Attn4Args a;
   fill_args(a, p, space(p, s, sh), sh, s, scale, q, q_stride, out, out_stride, lse, ws, err);

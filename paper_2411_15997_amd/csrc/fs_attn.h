@@ -149,6 +149,13 @@ __device__ inline float max_of_halves(float x) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+// The larger of the values of lanes 16 apart, in both.
+__device__ inline float max_of_16s(float x) {
+  const uint32_t b = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 // A reference of the exponentials as they use it: 0 while there is none and where it is
 // infinite, so that a score of inf makes the sum inf (inf - inf would make it NaN).
 __device__ inline float reference(float m, float c2) {
@@ -315,12 +322,13 @@ int32_t limited(int32_t window, const fs_step *s) { return window >= s->max_kv ?
 // What a plan goes by beside the step.
 struct Shape {
   int32_t n_heads, n_kv_heads, head_dim, window, sinks;
+  int32_t few_most;  // keys of a split of few rows, at most
 };
 Shape shape_of(const fs_step *s, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
-               int32_t window, int32_t sinks) {
+               int32_t window, int32_t sinks, int32_t few_most) {
   window = limited(window, s);
   sinks = window == 0 ? 0 : sinks < s->max_kv ? sinks : s->max_kv;
-  return {n_heads, n_kv_heads, head_dim, window, sinks};
+  return {n_heads, n_kv_heads, head_dim, window, sinks, few_most};
 }
 
 Plan plan(const fs_step *s, const Shape &c) {
@@ -365,7 +373,7 @@ Plan plan(const fs_step *s, const Shape &c) {
   if (p.few_seqs > 0) {
     const int64_t blocks = int64_t(p.few_seqs) * c.n_kv_heads;
     const int32_t len = keys(p.few_tokens);
-    split_of(blocks, len, 1024, 512, 1024, int64_t(s->n_seqs) * p.few_tokens, p.few_split,
+    split_of(blocks, len, 1024, 512, c.few_most, int64_t(s->n_seqs) * p.few_tokens, p.few_split,
              p.few_splits);
     // Up to 1,024 keys (2,048 of head_dim 64) with a compute unit for each work-group: eight
     // waves and no join.  (4 requests, 8 heads of 128: 500 keys 8.9 us, 9.8 with four waves;
