@@ -108,7 +108,7 @@ class CacheLayers:
               "caches: all KVCache or all KVCache4")
         _want(len({c.gpu for c in caches}) == 1, "caches: one GPU")
         self.caches, self.gpu, self.n = caches, caches[0].gpu, len(caches)
-        self.fn = "fs_pages_copy4" if kind is KVCache4 else "fs_pages_copy"
+        self.four = kind is KVCache4
         self.s = (type(caches[0].s) * self.n)(*(c.s for c in caches))
         self.ref = C.addressof(self.s)
 
@@ -131,6 +131,14 @@ class PagePool:
                           table.data_ptr(), _vector(held, torch.int32, self.n_rows, "held"),
                           KVCache._table_stride(table))
         self.ref = C.addressof(self.s)
+        self._bytes = {}
+
+    def workspace(self, n):
+        """Bytes of workspace that a fork of n rows (0: a compaction) takes."""
+        need = self._bytes.get(n)
+        if need is None:
+            need = self._bytes[n] = _lib().fs_pages_workspace(self.ref, n)
+        return need
 
 
 def fs_rope_append4(step: Step, cache: KVCache4, rope: Rope, q, k, v, q_out=None, err=None,
@@ -176,24 +184,27 @@ def fs_cache4_rows(step: Step, cache: KVCache4, dtype=None, k=None, v=None, err=
     where not given; bfloat16 unless k, v or dtype say otherwise)."""
     torch = _torch()
     T, HK, D, gpu = step.rows, cache.n_kv_heads, cache.head_dim, step.gpu
-    given = [x for x in (k, v) if x is not None]
-    dtype = dtype or (given[0].dtype if given else torch.bfloat16)
+    if dtype is None:
+        dtype = k.dtype if k is not None else v.dtype if v is not None else torch.bfloat16
     code = _row_type(dtype)
-    _want(all(x.dtype == dtype for x in given), "k, v: the dtype asked for")
+    if (k is not None and k.dtype != dtype) or (v is not None and v.dtype != dtype):
+        raise ValueError("k, v: the dtype asked for")
     cache.check(step, "fs_cache4_rows")
     if cache.gpu != gpu:
         raise ValueError("cache and step: one GPU")
     _on(gpu, step.q_off, k, v, err)
     if gpu != engine._current_gpu():
         return _there(gpu, fs_cache4_rows, step, cache, dtype, k, v, err, check)
-
-    def rows(x, name):
-        if x is None:
-            x = torch.empty((T, HK, D), dtype=dtype, device=cache.k.device)
-            return x, x.data_ptr(), HK * D
-        return x, *_rows(x, name, (T, HK, D))
-
-    (k, kp, ks), (v, vp, vs) = rows(k, "k"), rows(v, "v")
+    if k is None:
+        k = torch.empty((T, HK, D), dtype=dtype, device=cache.k.device)
+        kp, ks = k.data_ptr(), HK * D
+    else:
+        kp, ks = _rows(k, "k", (T, HK, D))
+    if v is None:
+        v = torch.empty((T, HK, D), dtype=dtype, device=cache.k.device)
+        vp, vs = v.data_ptr(), HK * D
+    else:
+        vp, vs = _rows(v, "v", (T, HK, D))
     if err is None:
         err = cleared_err_word(cache.k.device)
     code = _lib().fs_cache4_rows(step.ref, cache.ref, code, kp, ks, vp, vs, err.data_ptr(),
@@ -246,10 +257,17 @@ def fs_paged_attention4(step: Step, cache: KVCache4, q, scale, window=0, sinks=0
     return out if lse is None else (out, lse)
 
 
+_i32 = None
+
+
 def _ids(t, n, name):
-    if t.dim() != 1 or t.shape[0] != n:
-        raise ValueError(f"{name}: {n} values")
-    return _vector(t, _torch().int32, n, name)
+    """A contiguous int32 vector of n values."""
+    global _i32
+    if _i32 is None:
+        _i32 = _torch().int32
+    if t.dtype is not _i32 or t.dim() != 1 or t.size(0) != n or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous int32 vector of {n} values")
+    return t.data_ptr()
 
 
 def fs_pages_free(pool: PagePool, rows, err=None, check=True):
@@ -258,7 +276,7 @@ def fs_pages_free(pool: PagePool, rows, err=None, check=True):
     _on(gpu, rows, err)
     if gpu != engine._current_gpu():
         return _there(gpu, fs_pages_free, pool, rows, err, check)
-    n = rows.shape[0]
+    n = rows.size(0)
     _want_32("rows", n)
     rp = _ids(rows, n, "rows")
     if err is None:
@@ -277,17 +295,24 @@ def fs_pages_fork(pool: PagePool, parent, child, shared, room, src=None, dst=Non
     _on(gpu, parent, child, shared, room, src, dst, ws, err)
     if gpu != engine._current_gpu():
         return _there(gpu, fs_pages_fork, pool, parent, child, shared, room, src, dst, ws, err, check)
-    n = child.shape[0]
+    n = child.size(0)
     _want_32("child", n)
-    pp, cp, sp, mp = (_ids(t, n, name) for t, name in
-                      ((parent, "parent"), (child, "child"), (shared, "shared"), (room, "room")))
-    src = torch.empty_like(child) if src is None else src
-    dst = torch.empty_like(child) if dst is None else dst
-    srcp, dstp = _ids(src, n, "src"), _ids(dst, n, "dst")
+    pp, cp = _ids(parent, n, "parent"), _ids(child, n, "child")
+    sp, mp = _ids(shared, n, "shared"), _ids(room, n, "room")
+    if src is None:
+        src = torch.empty_like(child)
+        srcp = src.data_ptr()
+    else:
+        srcp = _ids(src, n, "src")
+    if dst is None:
+        dst = torch.empty_like(child)
+        dstp = dst.data_ptr()
+    else:
+        dstp = _ids(dst, n, "dst")
     if err is None:
         err = cleared_err_word(child.device)
     L = _lib()
-    ws, wp, wn = _workspace(ws, L.fs_pages_workspace(pool.ref, n), child)
+    ws, wp, wn = _workspace(ws, pool.workspace(n), child)
     code = L.fs_pages_fork(pool.ref, n, pp, cp, sp, mp, srcp, dstp, wp, wn, err.data_ptr(),
                            engine._raw_stream(gpu))
     if code or check:
@@ -304,22 +329,23 @@ def fs_pages_compact(pool: PagePool, refs_out=None, table_out=None, src=None, ds
     _on(gpu, refs_out, table_out, src, dst, count, ws, err)
     if gpu != engine._current_gpu():
         return _there(gpu, fs_pages_compact, pool, refs_out, table_out, src, dst, count, ws, err, check)
-    refs_out = pool.refs if refs_out is None else refs_out
-    table_out = pool.table if table_out is None else table_out
-    _want(table_out.dtype == torch.int32 and table_out.shape == pool.table.shape and
-          (pool.width <= 1 or table_out.stride(1) == 1), "table_out: like the table")
-    stride = KVCache._table_stride(table_out)
-    rp = _ids(refs_out, pool.n_pages, "refs_out")
+    rp = pool.s.refs if refs_out is None else _ids(refs_out, pool.n_pages, "refs_out")
+    if table_out is None:
+        tp, stride = pool.s.table, pool.s.table_stride
+    else:
+        _want(table_out.dtype == torch.int32 and table_out.shape == pool.table.shape and
+              (pool.width <= 1 or table_out.stride(1) == 1), "table_out: like the table")
+        tp, stride = table_out.data_ptr(), KVCache._table_stride(table_out)
     like = pool.refs
-    src = torch.empty(n, dtype=torch.int32, device=like.device) if src is None else src
-    dst = torch.empty_like(src) if dst is None else dst
-    count = torch.empty(1, dtype=torch.int32, device=like.device) if count is None else count
+    src = like.new_empty(n) if src is None else src
+    dst = like.new_empty(n) if dst is None else dst
+    count = like.new_empty(1) if count is None else count
     sp, dp, cp = _ids(src, n, "src"), _ids(dst, n, "dst"), _ids(count, 1, "count")
     if err is None:
         err = cleared_err_word(like.device)
     L = _lib()
-    ws, wp, wn = _workspace(ws, L.fs_pages_workspace(pool.ref, 0), like)
-    code = L.fs_pages_compact(pool.ref, rp, table_out.data_ptr(), stride, sp, dp, cp, wp, wn,
+    ws, wp, wn = _workspace(ws, pool.workspace(0), like)
+    code = L.fs_pages_compact(pool.ref, rp, tp, stride, sp, dp, cp, wp, wn,
                               err.data_ptr(), engine._raw_stream(gpu))
     if code or check:
         _done(code, "fs_pages_compact", err, check)
@@ -334,14 +360,15 @@ def fs_pages_copy(caches, src, dst, count=None, err=None, check=True):
     _on(gpu, src, dst, count, err)
     if gpu != engine._current_gpu():
         return _there(gpu, fs_pages_copy, layers, src, dst, count, err, check)
-    n = src.shape[0]
+    n = src.size(0)
     _want_32("src", n)
     sp, dp = _ids(src, n, "src"), _ids(dst, n, "dst")
     cp = None if count is None else _ids(count, 1, "count")
     if err is None:
         err = cleared_err_word(src.device)
-    code = getattr(_lib(), layers.fn)(layers.ref, layers.n, n, sp, dp, cp, err.data_ptr(),
-                                      engine._raw_stream(gpu))
+    L = _lib()
+    copy = L.fs_pages_copy4 if layers.four else L.fs_pages_copy
+    code = copy(layers.ref, layers.n, n, sp, dp, cp, err.data_ptr(), engine._raw_stream(gpu))
     if code or check:
         _done(code, "fs_pages_copy", err, check)
 

@@ -32,8 +32,6 @@ struct Append4Args {
   int32_t *err;
 };
 
-constexpr int kTok = 4;  // tokens per work-group
-
 // A token's place: its cache rows of head 0 (bytes; -1: none) and its position.
 struct Place {
   int64_t code, scale;
@@ -83,26 +81,26 @@ __device__ inline uint32_t codes8(const float *x, uint32_t &byte) {
   return w;
 }
 
-// Element d of a row turned: x with the other element of its pair.
+// Element d of a row turned in F: x with the other element of its pair.
 template <class F, bool INTER>
-__device__ inline float turned(int d, int half, float x, float other, const double *cs,
-                               const double *sn) {
+__device__ inline float turned(int d, int half, float x, float other, const F *cs, const F *sn) {
   const int f = INTER ? d >> 1 : d < half ? d : d - half;
   const bool second = INTER ? d & 1 : d >= half;
-  const F c = F(cs[f]), s = F(sn[f]);
-  return float(second ? F(x) * c + F(other) * s : F(x) * c - F(other) * s);
+  return float(second ? F(x) * cs[f] + F(other) * sn[f] : F(x) * cs[f] - F(other) * sn[f]);
 }
 
 // VEC: pairs lie in whole 16-byte chunks (rotary_dim a multiple of 16, or of 8 when
 // interleaved).  A key's chunk is turned by one lane, which reads the chunk of the pairs' other
 // elements too; queries may be turned in place, so there a lane takes both (one pair or one
 // element per item without VEC).
-template <bool BF, bool INTER, bool VEC>
+// TOK tokens a work-group.
+template <bool BF, bool INTER, bool VEC, int TOK>
 __global__ void __launch_bounds__(256) k_rope_append4(Append4Args a) {
-  __shared__ double cs[kTok][128], sn[kTok][128];
-  __shared__ Place place[kTok];
-  const int32_t t0 = blockIdx.x * kTok;
-  const int32_t nt = min(kTok, a.rows - t0);
+  __shared__ double cs[TOK][128], sn[TOK][128];
+  __shared__ float csf[TOK][128], snf[TOK][128];  // rounded, for the queries
+  __shared__ Place place[TOK];
+  const int32_t t0 = blockIdx.x * TOK;
+  const int32_t nt = min(TOK, a.rows - t0);
   const int tid = threadIdx.x;
   // a wave for each token
   if (tid >> 6 < nt) {
@@ -121,8 +119,9 @@ __global__ void __launch_bounds__(256) k_rope_append4(Append4Args a) {
     const int tok = i / half, f = i - tok * half;
     double sv, cv;
     sincos(double(place[tok].pos) * double(__ldg(a.inv_freq + f)), &sv, &cv);
-    cs[tok][f] = cv * double(a.factor);
-    sn[tok][f] = sv * double(a.factor);
+    cv *= double(a.factor), sv *= double(a.factor);
+    cs[tok][f] = cv, sn[tok][f] = sv;
+    csf[tok][f] = float(cv), snf[tok][f] = float(sv);
   }
   __syncthreads();
 
@@ -136,8 +135,8 @@ __global__ void __launch_bounds__(256) k_rope_append4(Append4Args a) {
     const bool kv = it < all_kv;
     const int tok = kv ? it / (2 * kv_items) : (it - all_kv) / q_items;
     const int64_t t = t0 + tok;
-    const double *c = cs[tok], *s = sn[tok];
     if (kv) {
+      const double *c = cs[tok], *s = sn[tok];
       const int r0 = it - tok * 2 * kv_items;
       const Place at = place[tok];
       if (at.code < 0) continue;
@@ -181,6 +180,7 @@ __global__ void __launch_bounds__(256) k_rope_append4(Append4Args a) {
         ((val ? a.vsw : a.ksw) + at.scale + int64_t(h) * a.sc.head_stride)[ch >> 2] = uint8_t(byte);
       continue;
     }
+    const float *c = csf[tok], *s = snf[tok];
     const int r = it - all_kv - tok * q_items, h = r / per, j = r - h * per;
     const short *src = a.q + t * a.q_stride + h * D;
     short *dst = a.q_out + t * a.q_out_stride + h * D;
@@ -221,11 +221,11 @@ __global__ void __launch_bounds__(256) k_rope_append4(Append4Args a) {
 }
 
 // What the cache holds at the step's rows.
-template <bool BF>
+template <bool BF, int TOK>
 __global__ void __launch_bounds__(256) k_cache4_rows(Append4Args a) {
-  __shared__ Place place[kTok];
-  const int32_t t0 = blockIdx.x * kTok;
-  const int32_t nt = min(kTok, a.rows - t0);
+  __shared__ Place place[TOK];
+  const int32_t t0 = blockIdx.x * TOK;
+  const int32_t nt = min(TOK, a.rows - t0);
   const int tid = threadIdx.x;
   if (tid >> 6 < nt) {
     int32_t code = 0;
@@ -256,6 +256,18 @@ __global__ void __launch_bounds__(256) k_cache4_rows(Append4Args a) {
     *reinterpret_cast<s16x8 *>(out + int64_t(t0 + tok) * (val ? a.v_out_stride : a.k_out_stride) +
                                h * D + ch * 8) = x;
   }
+}
+
+// One token a work-group up to 1,024 rows, where a work-group's items would only follow each
+// other (8 rows: ROWSUS), and four beyond, which look for their places side by side.
+template <class F>
+void by_rows(int32_t rows, int32_t dtype, F f) {
+  const std::integral_constant<int, 1> one;
+  const std::integral_constant<int, 4> four;
+  if (dtype == FS_BF16)
+    rows <= 1024 ? f(std::true_type(), one) : f(std::true_type(), four);
+  else
+    rows <= 1024 ? f(std::false_type(), one) : f(std::false_type(), four);
 }
 
 Append4Args step_args(const fs_step *s, const fs_kv_cache4 *c, int32_t *err) {
@@ -298,22 +310,19 @@ hipError_t launch_rope_append4(const fs_step *s, const fs_kv_cache4 *c, const fs
   a.rotary = r->rotary_dim;
   const bool inter = r->interleaved != 0;
   const bool vec = r->rotary_dim % (inter ? 8 : 16) == 0;
-  const dim3 grid((a.rows + kTok - 1) / kTok), block(256);
-  auto go = [&](auto bf) {
+  by_rows(a.rows, dtype, [&](auto bf, auto tok) {
     constexpr bool BF = decltype(bf)::value;
+    constexpr int TOK = decltype(tok)::value;
+    const dim3 grid((a.rows + TOK - 1) / TOK), block(256);
     if (inter && vec)
-      hipLaunchKernelGGL((k_rope_append4<BF, true, true>), grid, block, 0, stream, a);
+      hipLaunchKernelGGL((k_rope_append4<BF, true, true, TOK>), grid, block, 0, stream, a);
     else if (inter)
-      hipLaunchKernelGGL((k_rope_append4<BF, true, false>), grid, block, 0, stream, a);
+      hipLaunchKernelGGL((k_rope_append4<BF, true, false, TOK>), grid, block, 0, stream, a);
     else if (vec)
-      hipLaunchKernelGGL((k_rope_append4<BF, false, true>), grid, block, 0, stream, a);
+      hipLaunchKernelGGL((k_rope_append4<BF, false, true, TOK>), grid, block, 0, stream, a);
     else
-      hipLaunchKernelGGL((k_rope_append4<BF, false, false>), grid, block, 0, stream, a);
-  };
-  if (dtype == FS_BF16)
-    go(std::true_type());
-  else
-    go(std::false_type());
+      hipLaunchKernelGGL((k_rope_append4<BF, false, false, TOK>), grid, block, 0, stream, a);
+  });
   return hipGetLastError();
 }
 
@@ -325,11 +334,11 @@ hipError_t launch_cache4_rows(const fs_step *s, const fs_kv_cache4 *c, int32_t d
   a.v_out = static_cast<short *>(v_out);
   a.k_out_stride = k_stride;
   a.v_out_stride = v_stride;
-  const dim3 grid((a.rows + kTok - 1) / kTok), block(256);
-  if (dtype == FS_BF16)
-    hipLaunchKernelGGL((k_cache4_rows<true>), grid, block, 0, stream, a);
-  else
-    hipLaunchKernelGGL((k_cache4_rows<false>), grid, block, 0, stream, a);
+  by_rows(a.rows, dtype, [&](auto bf, auto tok) {
+    constexpr int TOK = decltype(tok)::value;
+    hipLaunchKernelGGL((k_cache4_rows<decltype(bf)::value, TOK>), dim3((a.rows + TOK - 1) / TOK),
+                       dim3(256), 0, stream, a);
+  });
   return hipGetLastError();
 }
 

@@ -16,6 +16,9 @@ namespace {
 
 constexpr int kBlock = 1024;          // threads
 constexpr int kPer = 2 * kBlock;      // pages of a work-group
+constexpr int kFewPages = 2 * kBlock;  // a pool that one work-group looks through
+constexpr int kFewForks = 32;         // forks, and rows, that the same one finishes
+constexpr int kClaims = 8192;         // rows whose claims LDS holds
 
 struct PoolArgs {
   int32_t n_pages, page_shift, n_rows, width;
@@ -64,8 +67,151 @@ __device__ inline T block_before(T x, T *lds) {
   return before;
 }
 
-// The pages of block b that are in use (LIVE) or free, and for a fork, in a block of its own,
-// which forks are sound and how many new pages each takes.
+// Which forks are sound and how many new pages come before each one's, by one work-group; the
+// sum, at most n_pages + 1.
+__device__ inline int32_t plan_forks(const PoolArgs &a) {
+  __shared__ int64_t lds64[kBlock / 64];
+  __shared__ int32_t lds_claim[kClaims];
+  const int tid = threadIdx.x;
+  // A child belongs to the lowest index that names it.  (Atomics alone, in LDS where that holds
+  // the rows: no other work-group looks at the claims, so nothing has to be flushed.)
+  int32_t *const claim = a.n_rows <= kClaims ? lds_claim : a.claim;
+  for (int32_t i = tid; i < a.n; i += kBlock)
+    if (uint32_t(a.child[i]) < uint32_t(a.n_rows)) atomicExch(claim + a.child[i], INT32_MAX);
+  __syncthreads();
+  for (int32_t i = tid; i < a.n; i += kBlock)
+    if (uint32_t(a.child[i]) < uint32_t(a.n_rows)) atomicMin(claim + a.child[i], i);
+  __syncthreads();
+  const int64_t most = int64_t(a.n_pages) + 1;  // more than there are is as many as that
+  int64_t before = 0;
+  for (int32_t i0 = 0; i0 < a.n; i0 += kBlock) {
+    const int32_t i = i0 + tid;
+    int64_t need = 0;
+    bool ok = false;
+    if (i < a.n) {
+      const int32_t p = a.parent[i], c = a.child[i], sh = a.shared[i], room = a.room[i];
+      const int32_t size = 1 << a.page_shift;
+      ok = p >= -1 && p < a.n_rows && uint32_t(c) < uint32_t(a.n_rows) && sh >= 0 && room >= sh;
+      const int32_t has = ok && p >= 0 ? a.held[p] : 0, own = ok ? a.held[c] : 0;
+      if (ok) ok = atomicMin(claim + c, INT32_MAX) == i && own == 0;
+      const int32_t pages = int32_t((int64_t(room) + size - 1) >> a.page_shift);
+      if (ok) ok = pages <= a.width;
+      if (ok && sh > 0)
+        ok = p >= 0 && has >= 0 && has <= a.width &&
+             int32_t((int64_t(sh) + size - 1) >> a.page_shift) <= has;
+      if (ok)
+        need = pages - (sh >> a.page_shift);
+      else
+        raise_err(a.err, FS_E_RANGE);
+    }
+    const int64_t f = min(before + block_before(need, lds64), most);
+    before += block_total(need, lds64);
+    if (i < a.n) a.first[i] = int32_t(ok ? f : -1 - f);
+  }
+  return int32_t(min(before, most));
+}
+__device__ inline bool enough(const PoolArgs &a, int32_t wanted, int32_t free) {
+  if (threadIdx.x == 0) {
+    *a.word = wanted <= free;  // (read by k_pages_fork)
+    if (wanted > free) raise_err(a.err, FS_E_OVERFLOW);
+  }
+  return wanted <= free;
+}
+
+// Fork i by THREADS threads (a wave, or a work-group): the child's row, counts and the page to be
+// copied.
+template <int THREADS>
+__device__ inline void fork_row(const PoolArgs &a, int32_t i) {
+  const int tid = threadIdx.x % THREADS;
+  const int32_t first = a.first[i];
+  bool go = first >= 0 && *a.word;
+  const int32_t p = go ? a.parent[i] : 0, c = go ? a.child[i] : 0, sh = go ? a.shared[i] : 0;
+  const int32_t size = 1 << a.page_shift, full = sh >> a.page_shift;
+  const int32_t pages = go ? int32_t((int64_t(a.room[i]) + size - 1) >> a.page_shift) : 0;
+  const bool part = sh & (size - 1);
+  const int32_t *from = a.table + int64_t(max(p, 0)) * a.stride;
+  bool bad = false;
+  for (int32_t j = tid; j < full + part; j += THREADS)
+    bad |= uint32_t(from[j]) >= uint32_t(a.n_pages);
+  if (THREADS == 64 ? __any(bad) : __syncthreads_or(bad)) {
+    raise_err(a.err, FS_E_RANGE);
+    go = false;
+  }
+  if (tid == 0) {
+    a.src[i] = go && part ? from[full] : -1;
+    a.dst[i] = go && part ? a.list[first] : -1;
+    if (go) a.held[c] = pages;
+  }
+  if (!go) return;
+  int32_t *to = a.table + int64_t(c) * a.stride;
+  for (int32_t j = tid; j < pages; j += THREADS) {
+    const int32_t id = j < full ? from[j] : a.list[first + j - full];
+    to[j] = id;
+    atomicAdd(a.refs + id, 1);
+  }
+}
+
+// Pools of few pages, by one work-group: a wave goes through its share of the ids 64 at a time.
+// f(p, refs) of the share's pages (refs 0 past the last).
+template <class F>
+__device__ inline void my_pages(const PoolArgs &a, F f) {
+  const int32_t share = (a.n_pages + kBlock - 1) / kBlock * 64;  // of a wave
+  const int32_t from = int32_t(threadIdx.x >> 6) * share, to = min(from + share, a.n_pages);
+  for (int32_t p0 = from; p0 < to; p0 += 64 * 8) {  // eight loads under way
+    const int32_t p = p0 + int32_t(threadIdx.x & 63);
+    int32_t refs[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) refs[i] = p + 64 * i < a.n_pages ? a.refs[p + 64 * i] : 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (p0 + 64 * i < to) f(p + 64 * i, refs[i]);
+  }
+}
+__device__ inline int32_t lanes_before(uint64_t lanes) {
+  return __popcll(lanes & ((uint64_t(1) << (threadIdx.x & 63)) - 1));
+}
+// The sum over the waves before this one of x (one for all lanes of a wave), and over all.
+__device__ inline int32_t waves_before(int32_t x, int32_t *lds, int32_t &all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __syncthreads();
+  if (lane == 0) lds[wave] = x;
+  __syncthreads();
+  int32_t before = 0;
+  all = 0;
+#pragma unroll
+  for (int i = 0; i < kBlock / 64; ++i) {
+    if (i < wave) before += lds[i];
+    all += lds[i];
+  }
+  return before;
+}
+
+// The forks, and the list of the first free pages, as many as they take, in order of ids.  WHOLE:
+// the rows of few forks too, two for each wave.  (Eight forks of 28 pages, a pool of 256: PLANUS)
+template <bool WHOLE>
+__global__ void __launch_bounds__(kBlock) k_pages_plan(PoolArgs a) {
+  __shared__ int32_t lds[kBlock / 64];
+  int32_t mine = 0, all;
+  my_pages(a, [&](int32_t p, int32_t refs) {
+    mine += __popcll(__ballot(p < a.n_pages && refs <= 0));
+  });
+  const int32_t wanted = plan_forks(a);
+  int32_t at = waves_before(mine, lds, all);
+  if (enough(a, wanted, all))
+    my_pages(a, [&](int32_t p, int32_t refs) {
+      const uint64_t free = __ballot(p < a.n_pages && refs <= 0);
+      const int32_t to = at + lanes_before(free);
+      if (p < a.n_pages && refs <= 0 && to < wanted) a.list[to] = p;
+      at += __popcll(free);
+    });
+  if constexpr (WHOLE) {
+    __syncthreads();  // what the waves have written is read by others of this work-group
+    for (int32_t i = threadIdx.x >> 6; i < a.n; i += kBlock / 64) fork_row<64>(a, i);
+  }
+}
+
+// Pools of many pages: the pages of block b that are in use (LIVE) or free, and for a fork, in
+// a block of its own, the forks.
 template <bool LIVE>
 __global__ void __launch_bounds__(kBlock) k_pages_count(PoolArgs a) {
   __shared__ int32_t lds[kBlock / 64];
@@ -81,49 +227,13 @@ __global__ void __launch_bounds__(kBlock) k_pages_count(PoolArgs a) {
     if (tid == 0) a.block_sum[blockIdx.x] = x;
     return;
   }
-  // a child belongs to the lowest index that names it
-  for (int32_t i = tid; i < a.n; i += kBlock)
-    if (uint32_t(a.child[i]) < uint32_t(a.n_rows))
-      __hip_atomic_store(a.claim + a.child[i], INT32_MAX, __ATOMIC_RELAXED,
-                         __HIP_MEMORY_SCOPE_AGENT);
-  __threadfence();
-  __syncthreads();
-  for (int32_t i = tid; i < a.n; i += kBlock)
-    if (uint32_t(a.child[i]) < uint32_t(a.n_rows)) atomicMin(a.claim + a.child[i], i);
-  __threadfence();
-  __syncthreads();
-  __shared__ int64_t lds64[kBlock / 64];
-  const int64_t most = int64_t(a.n_pages) + 1;  // more than there are is as many as that
-  int64_t before = 0;
-  for (int32_t i0 = 0; i0 < a.n; i0 += kBlock) {
-    const int32_t i = i0 + tid;
-    int64_t need = 0;
-    bool ok = false;
-    if (i < a.n) {
-      const int32_t p = a.parent[i], c = a.child[i], sh = a.shared[i], room = a.room[i];
-      const int32_t size = 1 << a.page_shift;
-      ok = p >= -1 && p < a.n_rows && uint32_t(c) < uint32_t(a.n_rows) && sh >= 0 && room >= sh;
-      if (ok)
-        ok = __hip_atomic_load(a.claim + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == i &&
-             a.held[c] == 0;
-      const int32_t pages = int32_t((int64_t(room) + size - 1) >> a.page_shift);
-      if (ok) ok = pages <= a.width;
-      if (ok && sh > 0)
-        ok = p >= 0 && a.held[p] >= 0 && a.held[p] <= a.width &&
-             int32_t((int64_t(sh) + size - 1) >> a.page_shift) <= a.held[p];
-      if (ok)
-        need = pages - (sh >> a.page_shift);
-      else
-        raise_err(a.err, FS_E_RANGE);
-    }
-    const int64_t f = min(before + block_before(need, lds64), most);
-    before += block_total(need, lds64);
-    if (i < a.n) a.first[i] = int32_t(ok ? f : -1 - f);
+  if constexpr (!LIVE) {
+    const int32_t wanted = plan_forks(a);
+    if (tid == 0) a.first[a.n] = wanted;
   }
-  if (tid == 0) a.first[a.n] = int32_t(min(before, most));
 }
 
-// The first free pages, as many as the forks take, in order of ids.
+// The list of the first free pages.
 __global__ void __launch_bounds__(kBlock) k_pages_list(PoolArgs a) {
   __shared__ int32_t lds[kBlock / 64];
   const int tid = threadIdx.x;
@@ -136,10 +246,7 @@ __global__ void __launch_bounds__(kBlock) k_pages_list(PoolArgs a) {
   }
   before = block_total(before, lds);
   all = block_total(all, lds);
-  if (blockIdx.x == 0 && tid == 0) {
-    *a.word = wanted <= all;
-    if (wanted > all) raise_err(a.err, FS_E_OVERFLOW);
-  }
+  if (blockIdx.x == 0) enough(a, wanted, all);
   if (wanted > all || before >= wanted) return;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -151,36 +258,7 @@ __global__ void __launch_bounds__(kBlock) k_pages_list(PoolArgs a) {
   }
 }
 
-// A work-group for a fork: the child's row, counts and the page to be copied.
-__global__ void __launch_bounds__(256) k_pages_fork(PoolArgs a) {
-  const int32_t i = blockIdx.x;
-  const int tid = threadIdx.x;
-  int32_t first = a.first[i];
-  bool go = first >= 0 && *a.word;
-  const int32_t p = go ? a.parent[i] : 0, c = go ? a.child[i] : 0, sh = go ? a.shared[i] : 0;
-  const int32_t size = 1 << a.page_shift, full = sh >> a.page_shift;
-  const int32_t pages = go ? int32_t((int64_t(a.room[i]) + size - 1) >> a.page_shift) : 0;
-  const bool part = sh & (size - 1);
-  const int32_t *from = a.table + int64_t(max(p, 0)) * a.stride;
-  bool bad = false;
-  for (int32_t j = tid; j < full + part; j += 256) bad |= uint32_t(from[j]) >= uint32_t(a.n_pages);
-  if (__syncthreads_or(bad)) {
-    raise_err(a.err, FS_E_RANGE);
-    go = false;
-  }
-  if (tid == 0) {
-    a.src[i] = go && part ? from[full] : -1;
-    a.dst[i] = go && part ? a.list[first] : -1;
-    if (go) a.held[c] = pages;
-  }
-  if (!go) return;
-  int32_t *to = a.table + int64_t(c) * a.stride;
-  for (int32_t j = tid; j < pages; j += 256) {
-    const int32_t id = j < full ? from[j] : a.list[first + j - full];
-    to[j] = id;
-    atomicAdd(a.refs + id, 1);
-  }
-}
+__global__ void __launch_bounds__(256) k_pages_fork(PoolArgs a) { fork_row<256>(a, blockIdx.x); }
 
 __global__ void __launch_bounds__(256) k_pages_free(PoolArgs a) {
   __shared__ int32_t got;
@@ -208,7 +286,82 @@ __global__ void __launch_bounds__(256) k_pages_free(PoolArgs a) {
   if (bad) raise_err(a.err, FS_E_RANGE);
 }
 
+// Page p of a compaction, `rank` pages in use before it, L in all and `below` of them below L.
+__device__ inline void place_page(const PoolArgs &a, int32_t p, int32_t refs, int32_t rank, int32_t L,
+                                  int32_t below) {
+  const int32_t moves = L - below;
+  if (p < L) {
+    if (refs <= 0) a.dst[p - rank] = p;
+  } else {
+    a.list[p] = refs > 0 ? rank - below : -1;
+    if (refs > 0) a.src[rank - below] = p;
+  }
+  if (a.refs_out != a.refs) a.refs_out[p] = p < L && refs > 0 ? refs : 0;
+  if (p >= moves && p < a.n_pages / 2) a.src[p] = a.dst[p] = -1;
+}
+__device__ inline void put_moves(const PoolArgs &a, int32_t L, int32_t below) {
+  *a.count = L - below;
+  a.word[0] = L;
+  a.word[1] = L - below;
+}
+
 // The pages in use with ids from L on, and the free ones below, in order of ids: src and dst.
+// Counts of the moved pages `from`, `from` + step .. .
+__device__ inline void move_counts(const PoolArgs &a, int32_t moves, int32_t from, int32_t step) {
+  for (int32_t i = from; i < moves; i += step) {
+    const int32_t s = a.src[i], d = a.dst[i];
+    const int32_t x = a.refs[s];
+    a.refs_out[s] = 0;
+    a.refs_out[d] = x;
+  }
+}
+// The ids of row r, entries `from`, `from` + step .. .
+__device__ inline void remap_row(const PoolArgs &a, int32_t L, int32_t r, int32_t from,
+                                 int32_t step) {
+  int32_t held = a.held[r];
+  bool bad = held < 0 || held > a.width;
+  if (bad) held = 0;
+  for (int32_t j = from; j < held; j += step) {
+    int32_t id = a.table[int64_t(r) * a.stride + j];
+    if (uint32_t(id) >= uint32_t(a.n_pages)) {
+      bad = true;
+    } else if (id >= L) {
+      const int32_t m = a.list[id];
+      if (m >= 0)
+        id = a.dst[m];
+      else
+        bad = true;  // a held page that is free
+    }
+    a.table_out[int64_t(r) * a.out_stride + j] = id;
+  }
+  if (bad) raise_err(a.err, FS_E_RANGE);
+}
+
+// Pools of few pages.  WHOLE: the counts and few rows of the table too, two for each wave.
+template <bool WHOLE>
+__global__ void __launch_bounds__(kBlock) k_pages_moves_few(PoolArgs a) {
+  __shared__ int32_t lds[kBlock / 64];
+  int32_t mine = 0, L, below = 0;
+  my_pages(a, [&](int32_t, int32_t refs) { mine += __popcll(__ballot(refs > 0)); });
+  int32_t rank = waves_before(mine, lds, L);
+  my_pages(a, [&](int32_t p, int32_t refs) { below += __popcll(__ballot(p < L && refs > 0)); });
+  int32_t all_below;
+  waves_before(below, lds, all_below);
+  if (threadIdx.x == 0) put_moves(a, L, all_below);
+  my_pages(a, [&](int32_t p, int32_t refs) {
+    const uint64_t live = __ballot(refs > 0);
+    if (p < a.n_pages) place_page(a, p, refs, rank + lanes_before(live), L, all_below);
+    rank += __popcll(live);
+  });
+  if constexpr (WHOLE) {
+    __syncthreads();
+    move_counts(a, L - all_below, threadIdx.x, kBlock);
+    for (int32_t r = threadIdx.x >> 6; r < a.n_rows; r += kBlock / 64)
+      remap_row(a, L, r, threadIdx.x & 63, 64);
+  }
+}
+
+// The same for pools of many pages.
 __global__ void __launch_bounds__(kBlock) k_pages_moves(PoolArgs a) {
   __shared__ int32_t lds[kBlock / 64];
   const int tid = threadIdx.x;
@@ -230,65 +383,29 @@ __global__ void __launch_bounds__(kBlock) k_pages_moves(PoolArgs a) {
     if (p < L) below += a.refs[p] > 0;
   }
   below = block_total(below, lds);
-  const int32_t moves = L - below;
-  if (blockIdx.x == 0 && tid == 0) {
-    *a.count = moves;
-    a.word[0] = L;
-    a.word[1] = moves;
-  }
+  if (blockIdx.x == 0 && tid == 0) put_moves(a, L, below);
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int32_t p = blockIdx.x * kPer + i * kBlock + tid;
     const int32_t refs = p < a.n_pages ? a.refs[p] : 0;
     const int32_t live = refs > 0;
-    const int32_t rank = before + block_before(live, lds);  // pages in use before p
+    const int32_t rank = before + block_before(live, lds);
     before += block_total(live, lds);
-    if (p >= a.n_pages) continue;
-    if (p < L) {
-      if (!live) a.dst[p - rank] = p;
-    } else {
-      a.list[p] = live ? rank - below : -1;
-      if (live) a.src[rank - below] = p;
-    }
-    if (a.refs_out != a.refs) a.refs_out[p] = p < L ? refs : 0;
-    if (p >= moves && p < a.n_pages / 2) a.src[p] = a.dst[p] = -1;
+    if (p < a.n_pages) place_page(a, p, refs, rank, L, below);
   }
 }
 
-// Counts of moved pages, and the table's ids.  The first table_blocks work-groups, `per_row` a
-// row, take the table.
+// The first table_blocks work-groups, `per_row` a row, take the table, the others the counts.
 __global__ void __launch_bounds__(256) k_pages_remap(PoolArgs a, int32_t table_blocks,
                                                      int32_t per_row) {
-  const int32_t L = a.word[0], moves = a.word[1];
+  const int32_t L = a.word[0], moves = a.word[1], b = blockIdx.x;
   const int tid = threadIdx.x;
-  if (int32_t(blockIdx.x) >= table_blocks) {
-    const int32_t step = (gridDim.x - table_blocks) * 256;
-    for (int32_t i = (blockIdx.x - table_blocks) * 256 + tid; i < moves; i += step) {
-      const int32_t s = a.src[i], d = a.dst[i];
-      const int32_t x = a.refs[s];
-      a.refs_out[s] = 0;
-      a.refs_out[d] = x;
-    }
-    return;
+  if (b >= table_blocks) {
+    move_counts(a, moves, (b - table_blocks) * 256 + tid, (gridDim.x - table_blocks) * 256);
+  } else {
+    const int32_t r = b / per_row;
+    remap_row(a, L, r, (b - r * per_row) * 256 + tid, per_row * 256);
   }
-  const int32_t r = blockIdx.x / per_row, part = blockIdx.x - r * per_row;
-  int32_t held = a.held[r];
-  bool bad = held < 0 || held > a.width;
-  if (bad) held = 0;
-  for (int32_t j = part * 256 + tid; j < held; j += per_row * 256) {
-    int32_t id = a.table[int64_t(r) * a.stride + j];
-    if (uint32_t(id) >= uint32_t(a.n_pages)) {
-      bad = true;
-    } else if (id >= L) {
-      const int32_t m = a.list[id];
-      if (m >= 0)
-        id = a.dst[m];
-      else
-        bad = true;  // a held page that is free
-    }
-    a.table_out[int64_t(r) * a.out_stride + j] = id;
-  }
-  if (bad) raise_err(a.err, FS_E_RANGE);
 }
 
 // ---- copies
@@ -417,8 +534,16 @@ hipError_t launch_pages_fork(const fs_pages *p, int32_t n, const int32_t *parent
   a.room = room;
   a.src = src;
   a.dst = dst;
-  hipLaunchKernelGGL((k_pages_count<false>), dim3(a.blocks + 1), dim3(kBlock), 0, stream, a);
-  hipLaunchKernelGGL(k_pages_list, dim3(a.blocks), dim3(kBlock), 0, stream, a);
+  if (p->n_pages <= kFewPages) {
+    if (n <= kFewForks) {
+      hipLaunchKernelGGL((k_pages_plan<true>), dim3(1), dim3(kBlock), 0, stream, a);
+      return hipGetLastError();
+    }
+    hipLaunchKernelGGL((k_pages_plan<false>), dim3(1), dim3(kBlock), 0, stream, a);
+  } else {
+    hipLaunchKernelGGL((k_pages_count<false>), dim3(a.blocks + 1), dim3(kBlock), 0, stream, a);
+    hipLaunchKernelGGL(k_pages_list, dim3(a.blocks), dim3(kBlock), 0, stream, a);
+  }
   hipLaunchKernelGGL(k_pages_fork, dim3(n), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
@@ -433,8 +558,16 @@ hipError_t launch_pages_compact(const fs_pages *p, int32_t *refs_out, int32_t *t
   a.src = src;
   a.dst = dst;
   a.count = count;
-  hipLaunchKernelGGL((k_pages_count<true>), dim3(a.blocks), dim3(kBlock), 0, stream, a);
-  hipLaunchKernelGGL(k_pages_moves, dim3(a.blocks), dim3(kBlock), 0, stream, a);
+  if (p->n_pages <= kFewPages) {
+    if (p->n_rows <= kFewForks && p->width <= 1024) {
+      hipLaunchKernelGGL((k_pages_moves_few<true>), dim3(1), dim3(kBlock), 0, stream, a);
+      return hipGetLastError();
+    }
+    hipLaunchKernelGGL((k_pages_moves_few<false>), dim3(1), dim3(kBlock), 0, stream, a);
+  } else {
+    hipLaunchKernelGGL((k_pages_count<true>), dim3(a.blocks), dim3(kBlock), 0, stream, a);
+    hipLaunchKernelGGL(k_pages_moves, dim3(a.blocks), dim3(kBlock), 0, stream, a);
+  }
   const int32_t per_row = p->width <= 1024 ? 1 : p->width <= 65536 ? (p->width + 1023) / 1024 : 64;
   const int32_t table_blocks = p->n_rows * per_row;
   const int32_t moves = p->n_pages / 2 / 256 + 1;
