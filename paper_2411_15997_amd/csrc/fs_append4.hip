@@ -129,25 +129,34 @@ __global__ void __launch_bounds__(256) k_rope_append4(Append4Args a) {
   const int kv_items = HK * CH;
   const int q_turned = VEC ? (INTER ? a.rotary / 8 : a.rotary / 16) : half;
   const int per = q_turned + (VEC ? (D - a.rotary) / 8 : D - a.rotary);
-  const int q_items = a.n_heads * per, all_kv = nt * 2 * kv_items;
-  for (int it = tid; it < all_kv + nt * q_items; it += 256) {
-    // keys and values of all tokens first: a group is four neighbouring lanes' (CH is a multiple of 4)
-    const bool kv = it < all_kv;
-    const int tok = kv ? it / (2 * kv_items) : (it - all_kv) / q_items;
-    const int64_t t = t0 + tok;
-    if (kv) {
-      const double *c = cs[tok], *s = sn[tok];
-      const int r0 = it - tok * 2 * kv_items;
-      const Place at = place[tok];
+  // A thread has the same item of all the work-group's tokens under way: one look for its place
+  // in the row, and TOK loads before the first is waited for.  (Items one after the other,
+  // 5,726 rows of 32 + 2 x 8 heads: STEPUS)
+  for (int it = tid; it < 2 * kv_items; it += 256) {
+    const bool val = it >= kv_items;
+    const int r = val ? it - kv_items : it, h = r / CH, ch = r - h * CH;
+    const int64_t stride = val ? a.v_stride : a.k_stride;
+    const short *row = (val ? a.v : a.k) + t0 * stride + h * D;
+    const bool turn = !val && ch * 8 < a.rotary;
+    s16x8 in[TOK], other[TOK];
+#pragma unroll
+    for (int u = 0; u < TOK; ++u) {
+      const short *from = row + min(u, nt - 1) * stride;
+      in[u] = *reinterpret_cast<const s16x8 *>(from + ch * 8);
+      if (!INTER && VEC && turn)  // the pairs' other elements
+        other[u] = *reinterpret_cast<const s16x8 *>(
+            from + (ch * 8 < half ? ch * 8 + half : ch * 8 - half));
+    }
+#pragma unroll
+    for (int u = 0; u < TOK; ++u) {
+      if (u >= nt) break;
+      const Place at = place[u];
       if (at.code < 0) continue;
-      const bool val = r0 >= kv_items;
-      const int r = val ? r0 - kv_items : r0, h = r / CH, ch = r - h * CH;
-      const short *row = (val ? a.v + t * a.v_stride : a.k + t * a.k_stride) + h * D;
-      const s16x8 v = *reinterpret_cast<const s16x8 *>(row + ch * 8);
+      const double *c = cs[u], *s = sn[u];
       float x[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = to_f32<BF>(v[i]);
-      if (!val && ch * 8 < a.rotary) {
+      for (int i = 0; i < 8; ++i) x[i] = to_f32<BF>(in[u][i]);
+      if (turn) {
         if constexpr (INTER) {
 #pragma unroll
           for (int i = 0; i < 8; i += 2)
@@ -157,65 +166,80 @@ __global__ void __launch_bounds__(256) k_rope_append4(Append4Args a) {
               x[i + 1] = turned<double, INTER>(ch * 8 + i + 1, half, q, p, c, s);
             }
         } else if constexpr (VEC) {
-          const s16x8 o = *reinterpret_cast<const s16x8 *>(
-              row + (ch * 8 < half ? ch * 8 + half : ch * 8 - half));
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            x[i] = turned<double, INTER>(ch * 8 + i, half, x[i], to_f32<BF>(o[i]), c, s);
+            x[i] = turned<double, INTER>(ch * 8 + i, half, x[i], to_f32<BF>(other[u][i]), c, s);
         } else {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int d = ch * 8 + i;
             if (d < a.rotary)
-              x[i] = turned<double, INTER>(d, half, x[i],
-                                           to_f32<BF>(row[d < half ? d + half : d - half]), c, s);
+              x[i] = turned<double, INTER>(
+                  d, half, x[i], to_f32<BF>(row[u * stride + (d < half ? d + half : d - half)]), c,
+                  s);
           }
         }
       }
-      uint32_t byte;
+      uint32_t byte;  // (a group is four neighbouring lanes': CH is a multiple of 4)
       const uint32_t w = codes8<BF>(x, byte);
       *reinterpret_cast<uint32_t *>((val ? a.vw : a.kw) + at.code + int64_t(h) * a.c.head_stride +
                                     ch * 4) = w;
       if ((ch & 3) == 0)
         ((val ? a.vsw : a.ksw) + at.scale + int64_t(h) * a.sc.head_stride)[ch >> 2] = uint8_t(byte);
-      continue;
     }
-    const float *c = csf[tok], *s = snf[tok];
-    const int r = it - all_kv - tok * q_items, h = r / per, j = r - h * per;
-    const short *src = a.q + t * a.q_stride + h * D;
-    short *dst = a.q_out + t * a.q_out_stride + h * D;
+  }
+
+  for (int it = tid; it < a.n_heads * per; it += 256) {
+    const int h = it / per, j = it - h * per;
     if constexpr (VEC) {
-      if (j >= q_turned) {
-        const int e = a.rotary + (j - q_turned) * 8;
-        *reinterpret_cast<s16x8 *>(dst + e) = *reinterpret_cast<const s16x8 *>(src + e);
-      } else if constexpr (INTER) {
-        const s16x8 x = *reinterpret_cast<const s16x8 *>(src + 8 * j);
-        s16x8 y;
+      // the chunk's first element: turned below rotary
+      const int e = j >= q_turned ? a.rotary + (j - q_turned) * 8 : 8 * j;
+      const short *src = a.q + t0 * a.q_stride + h * D + e;
+      short *dst = a.q_out + t0 * a.q_out_stride + h * D + e;
+      s16x8 in[TOK], other[TOK];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          y[i] = to_16<BF>(turned<float, INTER>(8 * j + i, half, to_f32<BF>(x[i]),
-                                                to_f32<BF>(x[i ^ 1]), c, s));
-        *reinterpret_cast<s16x8 *>(dst + 8 * j) = y;
-      } else {
-        const s16x8 x = *reinterpret_cast<const s16x8 *>(src + 8 * j);
-        const s16x8 y = *reinterpret_cast<const s16x8 *>(src + 8 * j + half);
-        s16x8 u, w;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float p = to_f32<BF>(x[i]), q = to_f32<BF>(y[i]);
-          u[i] = to_16<BF>(turned<float, INTER>(8 * j + i, half, p, q, c, s));
-          w[i] = to_16<BF>(turned<float, INTER>(8 * j + i + half, half, q, p, c, s));
-        }
-        *reinterpret_cast<s16x8 *>(dst + 8 * j) = u;
-        *reinterpret_cast<s16x8 *>(dst + 8 * j + half) = w;
+      for (int u = 0; u < TOK; ++u) {
+        const short *from = src + min(u, nt - 1) * a.q_stride;
+        in[u] = *reinterpret_cast<const s16x8 *>(from);
+        if (!INTER && e < half) other[u] = *reinterpret_cast<const s16x8 *>(from + half);
       }
-    } else if (j >= q_turned) {
-      dst[a.rotary + j - q_turned] = src[a.rotary + j - q_turned];
+#pragma unroll
+      for (int u = 0; u < TOK; ++u) {
+        if (u >= nt) break;
+        const float *c = csf[u], *s = snf[u];
+        s16x8 v = in[u];
+        if (e < a.rotary) {
+          if constexpr (INTER) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              v[i] = to_16<BF>(turned<float, INTER>(e + i, half, to_f32<BF>(in[u][i]),
+                                                    to_f32<BF>(in[u][i ^ 1]), c, s));
+          } else {
+            s16x8 w;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float p = to_f32<BF>(in[u][i]), q = to_f32<BF>(other[u][i]);
+              v[i] = to_16<BF>(turned<float, INTER>(e + i, half, p, q, c, s));
+              w[i] = to_16<BF>(turned<float, INTER>(e + i + half, half, q, p, c, s));
+            }
+            *reinterpret_cast<s16x8 *>(dst + u * a.q_out_stride + half) = w;
+          }
+        }
+        *reinterpret_cast<s16x8 *>(dst + u * a.q_out_stride) = v;
+      }
     } else {
       const int e0 = INTER ? 2 * j : j, e1 = INTER ? 2 * j + 1 : j + half;
-      const float p = to_f32<BF>(src[e0]), q = to_f32<BF>(src[e1]);
-      dst[e0] = to_16<BF>(turned<float, INTER>(e0, half, p, q, c, s));
-      dst[e1] = to_16<BF>(turned<float, INTER>(e1, half, q, p, c, s));
+      for (int u = 0; u < nt; ++u) {
+        const short *src = a.q + (t0 + u) * a.q_stride + h * D;
+        short *dst = a.q_out + (t0 + u) * a.q_out_stride + h * D;
+        if (j >= q_turned) {
+          dst[a.rotary + j - q_turned] = src[a.rotary + j - q_turned];
+          continue;
+        }
+        const float p = to_f32<BF>(src[e0]), q = to_f32<BF>(src[e1]);
+        dst[e0] = to_16<BF>(turned<float, INTER>(e0, half, p, q, csf[u], snf[u]));
+        dst[e1] = to_16<BF>(turned<float, INTER>(e1, half, q, p, csf[u], snf[u]));
+      }
     }
   }
 }
@@ -237,24 +261,30 @@ __global__ void __launch_bounds__(256) k_cache4_rows(Append4Args a) {
   }
   __syncthreads();
   const int D = a.c.head_dim, CH = D / 8, kv_items = a.c.n_kv_heads * CH;
-  for (int it = tid; it < nt * 2 * kv_items; it += 256) {
-    const int tok = it / (2 * kv_items), r0 = it - tok * 2 * kv_items;
-    const bool val = r0 >= kv_items;
-    const int r = val ? r0 - kv_items : r0, h = r / CH, ch = r - h * CH;
+  for (int it = tid; it < 2 * kv_items; it += 256) {
+    const bool val = it >= kv_items;
+    const int r = val ? it - kv_items : it, h = r / CH, ch = r - h * CH;
+    const int64_t stride = val ? a.v_out_stride : a.k_out_stride;
     short *out = val ? a.v_out : a.k_out;
     if (!out) continue;
-    const Place at = place[tok];
-    s16x8 x = {};
-    if (at.code >= 0) {
-      const uint32_t w = *reinterpret_cast<const uint32_t *>(
-          (val ? a.c.v : a.c.k) + at.code + int64_t(h) * a.c.head_stride + ch * 4);
-      const uint32_t byte =
-          ((val ? a.sc.v : a.sc.k) + at.scale + int64_t(h) * a.sc.head_stride)[ch >> 2];
-      x = values8<BF>(w, scale_of<BF>(byte));
-      if (byte > kTopScale<BF>) x = BF ? 0x7fc0 : 0x7e00;  // NaN
+    out += t0 * stride + h * D + ch * 8;
+    uint32_t w[TOK], byte[TOK];
+#pragma unroll
+    for (int u = 0; u < TOK; ++u) {
+      const Place at = place[min(u, nt - 1)];
+      w[u] = byte[u] = 0;
+      if (at.code < 0) continue;
+      w[u] = *reinterpret_cast<const uint32_t *>((val ? a.c.v : a.c.k) + at.code +
+                                                 int64_t(h) * a.c.head_stride + ch * 4);
+      byte[u] = ((val ? a.sc.v : a.sc.k) + at.scale + int64_t(h) * a.sc.head_stride)[ch >> 2];
     }
-    *reinterpret_cast<s16x8 *>(out + int64_t(t0 + tok) * (val ? a.v_out_stride : a.k_out_stride) +
-                               h * D + ch * 8) = x;
+#pragma unroll
+    for (int u = 0; u < TOK; ++u) {
+      if (u >= nt) break;
+      s16x8 x = values8<BF>(w[u], scale_of<BF>(byte[u]));
+      if (byte[u] > kTopScale<BF>) x = BF ? 0x7fc0 : 0x7e00;  // NaN
+      *reinterpret_cast<s16x8 *>(out + u * stride) = x;
+    }
   }
 }
 
