@@ -5,13 +5,18 @@ one more token; this example is the engine that does it, with the package's oper
 
   per layer   fs_adapter_linear (q, k, v; every app has its own adapter), fs_rope_append,
               fs_paged_attention, fs_adapter_linear (output), two plain projections
+              (with --cache4 fs_rope_append4 and fs_paged_attention4 on a cache in 4 bits)
   at the end  fs_adapter_linear (logits), fs_sample
+  per step    fs_pages_fork and fs_pages_copy for the calls that begin, fs_pages_free for
+              those that end, fs_pages_compact and fs_pages_copy from time to time
 
 Weights and token ids are random; lengths, apps, admissions and the KV capacity are the
 trace's.  A call is prefilled in its admission step and holds its pages until it has
-L_O output tokens, as the engine model says.
+L_O output tokens, as the engine model says.  With --system N the calls of an app begin
+with the same N tokens, which are prefilled once and whose whole pages they share.
 
-    python examples/engine_steps.py [--requests N] [--layers L] [--users U]
+    python examples/engine_steps.py [--requests N] [--layers L] [--users U] [--cache4]
+                                    [--system N] [--window N --sinks N]
 """
 import argparse
 import os
@@ -48,15 +53,24 @@ def schedule(requests, users=8, step_ms=250.0, cap_tokens=8192):
 
 class Decoder:
     """Random weights of a small decoder with an adapter for each app on its attention
-    projections, and its paged caches."""
+    projections, and its paged caches (16 bits or, with cache4, 4 bits a value); attention over
+    all cached tokens, or over a window and the first `sinks`."""
 
     def __init__(self, apps, pages, layers=2, width=512, heads=8, kv_heads=2, dim=64, vocab=2048,
-                 rank=16, seed=0, dtype=torch.bfloat16, device="cuda"):
+                 rank=16, seed=0, dtype=torch.bfloat16, device="cuda", cache4=False, window=0,
+                 sinks=0):
         g = torch.Generator(device).manual_seed(seed)
 
         def normal(*shape, std):
             return torch.empty(shape, dtype=dtype, device=device).normal_(0, std, generator=g)
 
+        def cache():
+            if not cache4:
+                return [normal(pages, kv_heads, PAGE, dim, std=1.0) for _ in range(2)]
+            return [torch.zeros(pages, kv_heads, PAGE, n, dtype=torch.uint8, device=device)
+                    for n in (dim // 2, dim // 2, dim // 32, dim // 32)]
+
+        self.cache4, self.window, self.sinks = cache4, window, sinks
         self.heads, self.kv_heads, self.dim, self.width, self.vocab = heads, kv_heads, dim, width, vocab
         qkv, hd = (heads + 2 * kv_heads) * dim, heads * dim
         self.embed = normal(vocab, width, std=1.0)
@@ -67,8 +81,7 @@ class Decoder:
             down=normal(width, 4 * width, std=0.5 * width ** -0.5),
             a_qkv=normal(apps, rank, width, std=width ** -0.5), b_qkv=normal(apps, qkv, rank, std=0.1),
             a_out=normal(apps, rank, hd, std=hd ** -0.5), b_out=normal(apps, width, rank, std=0.1),
-            k=normal(pages, kv_heads, PAGE, dim, std=1.0), v=normal(pages, kv_heads, PAGE, dim, std=1.0))
-            for _ in range(layers)]
+            cache=cache()) for _ in range(layers)]
         freq, factor = fs.fs_rope_frequencies(dim, 10000.0)
         self.rope = fs.Rope(torch.from_numpy(freq).to(device), False, factor)
         self.scale = dim ** -0.5
@@ -79,13 +92,18 @@ class Decoder:
         f = x.float()
         return (f * torch.rsqrt(f.square().mean(-1, keepdim=True) + 1e-6)).to(x.dtype)
 
+    def caches(self, table):
+        """Each layer's cache under a page table."""
+        kind = fs.KVCache4 if self.cache4 else fs.KVCache
+        return [kind(*L["cache"], table) for L in self.layers]
+
     def step(self, ids, q_off, kv_len, table, app, u, sampling, err):
         """One engine step: token ids of its rows, where each request's rows begin, its cached
         length with them, its pages and its app -> each request's next token, its logits."""
         dev = self.device
         step = fs.Step(q_off, kv_len=torch.tensor(kv_len, dtype=torch.int32, device=dev),
                        max_kv=max(kv_len), device=dev)
-        table = torch.from_numpy(table).to(dev)
+        table = torch.as_tensor(table).to(dev)
         app = torch.tensor(app, dtype=torch.int32, device=dev)
         h, hk, T = self.heads, self.kv_heads, step.rows
         x = self.embed[torch.tensor(ids, device=dev)]
@@ -95,12 +113,14 @@ class Decoder:
                 a, b = x.new_empty(0, 8, w.shape[1]), x.new_empty(0, w.shape[0], 8)
             return fs.fs_adapter_linear(step, fs.Adapters(a, b, app), x, w, err=err, check=False)
 
-        for L in self.layers:
-            cache = fs.KVCache(L["k"], L["v"], table)
+        append = fs.fs_rope_append4 if self.cache4 else fs.fs_rope_append
+        attend = fs.fs_paged_attention4 if self.cache4 else fs.fs_paged_attention
+        for L, cache in zip(self.layers, self.caches(table)):
             qkv = linear(self.norm(x), L["qkv"], L["a_qkv"], L["b_qkv"]).view(T, h + 2 * hk, self.dim)
-            q = fs.fs_rope_append(step, cache, self.rope, qkv[:, :h], qkv[:, h:h + hk],
-                                  qkv[:, h + hk:], err=err, check=False)
-            o = fs.fs_paged_attention(step, cache, q, self.scale, err=err, check=False)
+            q = append(step, cache, self.rope, qkv[:, :h], qkv[:, h:h + hk], qkv[:, h + hk:], err=err,
+                       check=False)
+            o = attend(step, cache, q, self.scale, window=self.window, sinks=self.sinks, err=err,
+                       check=False)
             x = x + linear(o.view(T, -1), L["out"], L["a_out"], L["b_out"])
             x = x + linear(torch.nn.functional.silu(linear(self.norm(x), L["up"])), L["down"])
         last = torch.tensor(q_off[1:], device=dev) - 1
@@ -112,7 +132,34 @@ class Decoder:
         return token, logits
 
 
-def play(requests=120, layers=2, users=8, seed=0, greedy=False):
+class Pages:
+    """Rows of a page table and the pages behind them, of all layers' caches at once."""
+
+    def __init__(self, model, pages, rows, width):
+        i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=model.device)  # noqa: E731
+        self.pool = fs.PagePool(i32(pages), i32(rows, width), i32(rows), PAGE)
+        self.layers = fs.CacheLayers(model.caches(self.pool.table))
+        self.device = model.device
+
+    def ids(self, x):
+        return torch.tensor(x, dtype=torch.int32, device=self.device)
+
+    def begin(self, forks, err):
+        """forks: (parent row or -1, row, shared tokens, room in tokens) each."""
+        src, dst = fs.fs_pages_fork(self.pool, *(self.ids(list(x)) for x in zip(*forks)), err=err,
+                                    check=False)
+        fs.fs_pages_copy(self.layers, src, dst, err=err, check=False)
+
+    def end(self, rows, err):
+        fs.fs_pages_free(self.pool, self.ids(rows), err=err, check=False)
+
+    def compact(self, err):
+        src, dst, count = fs.fs_pages_compact(self.pool, err=err, check=False)
+        fs.fs_pages_copy(self.layers, src, dst, count, err=err, check=False)
+
+
+def play(requests=120, layers=2, users=8, seed=0, greedy=False, system=0, cache4=False, window=0,
+         sinks=0, compact_every=50):
     """Plays the schedule; returns what was generated and how the cache was used."""
     tr, h, cap = schedule(requests, users)
     n = tr.n
@@ -122,50 +169,76 @@ def play(requests=120, layers=2, users=8, seed=0, greedy=False):
     answer = np.maximum(np.asarray(tr.len_out), 1).astype(int)
     size = len_in + np.asarray(tr.len_out)
     admitted = np.nonzero(status == 0)[0]
-    pages = max(2 * cap, 2 * int(size.max(initial=1))) // PAGE + 2 * len(admitted) + 1
-    model = Decoder(tr.n_apps, pages, layers, seed=seed)
+    apps = tr.n_apps
+    pages = max(2 * cap, 2 * int(size.max(initial=1))) // PAGE + 2 * len(admitted) + 1 + \
+        apps * (-(-system // PAGE))
+    model = Decoder(apps, pages, layers, seed=seed, cache4=cache4, window=window, sinks=sinks)
     rng = np.random.default_rng(seed)
-    free, running, done = list(range(pages))[::-1], [], {}
+    most = max(system, int((prompt + answer).max(initial=1)))
+    store = Pages(model, pages, apps + len(admitted), -(-most // PAGE))
+    slots = list(range(apps, apps + len(admitted)))[::-1]
+    running, done = [], {}
     by_step = {}
     for g in admitted:
         by_step.setdefault(int(admit[g]), []).append(int(g))
     err = fs.cleared_err_word()
-    stats = dict(steps=0, rows=0, most_tokens=0, most_running=0)
+
+    def step(rows, new, kv, app, u, sampling):
+        q_off = [0] + list(np.cumsum([len(x) for x in new]))
+        table = store.pool.table[store.ids(rows).long()]
+        return model.step([t for x in new for t in x], q_off, kv, table, app, u, sampling, err)[0]
+
+    # the apps' prompts, prefilled once
+    shared = [rng.integers(0, model.vocab, system).tolist() for _ in range(apps)]
+    if system:
+        store.begin([(-1, a, 0, system) for a in range(apps)], err)
+        step(range(apps), shared, [system] * apps, list(range(apps)), torch.zeros(apps, device="cuda"),
+             fs.Sampling())
+    stats = dict(steps=0, rows=0, most_tokens=0, most_running=0, most_pages=0)
     torch.cuda.synchronize()
     began = time.perf_counter()
     last_step = max((int(admit[g]) + answer[g] for g in admitted), default=0)
     for s in range(last_step):
+        forks = []
         for g in by_step.get(s, []):           # prefilled in this step
-            ids = rng.integers(0, model.vocab, prompt[g]).tolist()
-            need = -(-(prompt[g] + answer[g]) // PAGE)
-            running.append(dict(g=g, ids=ids, new=ids, pages=[free.pop() for _ in range(need)], out=[]))
+            # (the last token of a prompt is always the call's own: its logits are wanted)
+            common = min(system, int(prompt[g]) - 1)
+            app = int(tr.app[g])
+            own = rng.integers(0, model.vocab, prompt[g] - common).tolist()
+            row = slots.pop()
+            forks.append((app if common else -1, row, common, int(prompt[g] + answer[g])))
+            running.append(dict(g=g, ids=shared[app][:common] + own, new=own, row=row, app=app, out=[]))
         if not running:
             continue
-        q_off = [0] + list(np.cumsum([len(r["new"]) for r in running]))
+        if forks:
+            store.begin(forks, err)
         kv = [len(r["ids"]) for r in running]
-        table = np.zeros((len(running), max(len(r["pages"]) for r in running)), np.int32)
-        for i, r in enumerate(running):
-            table[i, :len(r["pages"])] = r["pages"]
         u = torch.from_numpy(rng.random(len(running), np.float32)).cuda()
         top_p = torch.full((len(running),), 0.9, device="cuda")
         temp = torch.full((len(running),), 0.0 if greedy else 0.8, device="cuda")
-        token, _ = model.step([t for r in running for t in r["new"]], q_off, kv, table,
-                              [int(tr.app[r["g"]]) for r in running], u,
-                              fs.Sampling(temperature=temp, top_p=top_p), err)
+        token = step([r["row"] for r in running], [r["new"] for r in running], kv,
+                     [r["app"] for r in running], u, fs.Sampling(temperature=temp, top_p=top_p))
         stats["steps"] += 1
-        stats["rows"] += q_off[-1]
+        stats["rows"] += sum(len(r["new"]) for r in running)
         stats["most_running"] = max(stats["most_running"], len(running))
         stats["most_tokens"] = max(stats["most_tokens"], int(sum(size[r["g"]] for r in running)))
         for r, t in zip(running, token.tolist()):
             r["out"].append(t)
             r["ids"], r["new"] = r["ids"] + [t], [t]
-        for r in [r for r in running if len(r["out"]) == answer[r["g"]]]:
+        ended = [r for r in running if len(r["out"]) == answer[r["g"]]]
+        if ended:
+            stats["most_pages"] = max(stats["most_pages"], int((store.pool.refs > 0).sum()))
+            store.end([r["row"] for r in ended], err)
+        for r in ended:
             running.remove(r)
-            free.extend(r["pages"])
+            slots.append(r["row"])
             done[r["g"]] = r
+        if compact_every and s % compact_every == compact_every - 1:
+            store.compact(err)
     fs.sync_check(err, "engine steps")
     stats.update(seconds=time.perf_counter() - began, tokens=sum(len(r["out"]) for r in done.values()),
-                 admitted=len(admitted), requests=n, cap=cap, largest=int(size.max(initial=0)))
+                 admitted=len(admitted), requests=n, cap=cap, largest=int(size.max(initial=0)),
+                 held=int((store.pool.refs > 0).sum()), pages=pages)
     return model, tr, done, stats
 
 
@@ -174,8 +247,13 @@ def main():
     ap.add_argument("--requests", type=int, default=120)
     ap.add_argument("--layers", type=int, default=2)
     ap.add_argument("--users", type=int, default=8)
+    ap.add_argument("--cache4", action="store_true", help="a cache of 4 bits a value")
+    ap.add_argument("--system", type=int, default=0, help="tokens that an app's calls begin with")
+    ap.add_argument("--window", type=int, default=0, help="newest tokens that attention sees (0: all)")
+    ap.add_argument("--sinks", type=int, default=0, help="first tokens that it sees beside them")
     a = ap.parse_args()
-    _, _, done, s = play(a.requests, a.layers, a.users)
+    _, _, done, s = play(a.requests, a.layers, a.users, system=a.system, cache4=a.cache4,
+                         window=a.window, sinks=a.sinks)
     print(f"{s['requests']} requests, {s['admitted']} admitted; {s['steps']} engine steps, {s['rows']} "
           f"token rows, {s['tokens']} tokens generated; at most {s['most_running']} calls and "
           f"{s['most_tokens']} of {s['cap']} KV tokens at once; {s['seconds']:.2f} s, "

@@ -26,8 +26,11 @@ struct Attn4Args : AttnArgs {  // `c` is the cache's codes, in bytes
 template <bool BF>
 constexpr float kLift4 = BF ? -18.f : 7.f;
 
-// Keys of a split of few rows, at most: a quarter of the bytes of the 16-bit cache's.
+// A quarter of the 16-bit cache's bytes: twice its longest splits (64 requests of 16,384 tokens:
+// 219 us, 233 with 1,024 keys) and whole requests (30 of 2,000 tokens: 19.4 us, 23.3 in splits; 8 of
+// 1,100 11.7 and 15.0; 4 of 2,000 16.6 and 15.7).
 constexpr int32_t kFewMost4 = 2048;
+constexpr int32_t kFewWhole4 = 262144;
 
 // Codes of N neighbouring values: 16 bytes for 32 of them, 8 for 16.
 template <int N>
@@ -570,7 +573,9 @@ __global__ void __launch_bounds__(256, 2) k_attn4_mixed(Attn4Args a, int chunk, 
 }
 
 // The join of few rows in very many splits: a work-group for 32 columns of a row and head, 32
-// splits side by side.  (One request of 200,001 tokens, 32 heads in 224 splits: JOINUS)
+// splits side by side.  (One request of 200,001 tokens, 32 heads in 224
+// splits: 34.5 us, 35.9 with a work-group for a row and head; 8 of 32,768 in 64 splits 43.8
+// and 43.3.)
 constexpr int kManySplits = 128;
 template <bool BF, int D>
 __global__ void __launch_bounds__(256) k_attn4_join_many(Attn4Args a) {
@@ -654,7 +659,8 @@ void run(const Attn4Args &a, const Plan &p, hipStream_t stream) {
 
 size_t attention4_workspace_bytes(const fs_step *s, const fs_kv_cache4 *c, int32_t n_heads,
                                   int32_t window, int32_t sinks) {
-  const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks, kFewMost4);
+  const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks, kFewMost4,
+                            kFewWhole4);
   return space(plan(s, sh), s, sh).total();
 }
 
@@ -662,7 +668,8 @@ hipError_t launch_attention4(const fs_step *s, const fs_kv_cache4 *c, int32_t dt
                              int32_t n_heads, float scale, int32_t window, int32_t sinks,
                              const void *q, int64_t q_stride, void *out, int64_t out_stride,
                              float *lse, void *ws, int32_t *err, hipStream_t stream) {
-  const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks, kFewMost4);
+  const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks, kFewMost4,
+                            kFewWhole4);
   const Plan p = plan(s, sh);
   Attn4Args a;
   fill_args(a, p, space(p, s, sh), sh, s, scale, q, q_stride, out, out_stride, lse, ws, err);

@@ -322,13 +322,15 @@ int32_t limited(int32_t window, const fs_step *s) { return window >= s->max_kv ?
 // What a plan goes by beside the step.
 struct Shape {
   int32_t n_heads, n_kv_heads, head_dim, window, sinks;
-  int32_t few_most;  // keys of a split of few rows, at most
+  int32_t few_most;   // keys of a split of few rows, at most
+  int32_t few_whole;  // keys times head_dim that eight waves take without a split
 };
 Shape shape_of(const fs_step *s, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
-               int32_t window, int32_t sinks, int32_t few_most) {
+               int32_t window, int32_t sinks, int32_t few_most,
+               int32_t few_whole) {
   window = limited(window, s);
   sinks = window == 0 ? 0 : sinks < s->max_kv ? sinks : s->max_kv;
-  return {n_heads, n_kv_heads, head_dim, window, sinks, few_most};
+  return {n_heads, n_kv_heads, head_dim, window, sinks, few_most, few_whole};
 }
 
 Plan plan(const fs_step *s, const Shape &c) {
@@ -379,7 +381,7 @@ Plan plan(const fs_step *s, const Shape &c) {
     // waves and no join.  (4 requests, 8 heads of 128: 500 keys 8.9 us, 9.8 with four waves;
     // 1,000 keys 11.5 and, in two splits, 13.5; 30 requests of 1,000 13.4 and 17.1; 1,500 keys
     // whole 14.5, in splits 13.8.  Of 64: 1,400 keys 10.3 and 13.2, 2,000 12.9 and 14.1.)
-    const int32_t whole = 131072 / c.head_dim;
+    const int32_t whole = c.few_whole / c.head_dim;
     if (p.chunk_seqs == 0 && p.few_rows <= 32 && len <= whole && blocks <= 256) {
       p.few_waves = 8;
       p.few_split = whole;

@@ -187,7 +187,8 @@ __device__ inline int32_t waves_before(int32_t x, int32_t *lds, int32_t &all) {
 }
 
 // The forks, and the list of the first free pages, as many as they take, in order of ids.  WHOLE:
-// the rows of few forks too, two for each wave.  (Eight forks of 28 pages, a pool of 256: PLANUS)
+// the rows of few forks too, two for each wave.  (Eight forks in a pool of 247 pages: 7.8 us,
+// 14 and two more launches with the kernels for many.)
 template <bool WHOLE>
 __global__ void __launch_bounds__(kBlock) k_pages_plan(PoolArgs a) {
   __shared__ int32_t lds[kBlock / 64];

@@ -277,6 +277,59 @@ def test_few_rows_keep_their_probabilities_to_two_parts(lens, H, HK, D, dtype):
     within(got, want, bound, "out")
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("lens,kv,HK,D", [([1], [70001], 1, 64), ([2, 1], [66000, 130], 1, 128),
+                                          ([1, 3], [140000, 90000], 1, 128)])
+def test_attention4_of_very_many_splits(lens, kv, HK, D, dtype):
+    g = gen(D + kv[0])
+    c = make_cache4(g, kv, HK, D, 64, dtype)
+    k, v = both_values(c, dtype)
+    q, q_off = normal(g, sum(lens), 4, D, dtype=dtype), offsets(lens)
+    want, tol, lse, ltol = cref.attention(q, k, v, c[4], q_off, kv, D ** -0.5, 0, 0)
+    o, l = fs.fs_paged_attention4(step_of(lens, kv), on_gpu4(*c), q.cuda(), D ** -0.5, want_lse=True)
+    within(o, want, tol, "out")
+    within(l, lse, ltol, "lse")
+
+
+@pytest.mark.parametrize("lens,kv", [([1, 1], [3000, 50]), ([60], [90])])
+def test_attention4_with_a_loose_bound(lens, kv):
+    """A host bound far above the lengths, and scores in the thousands."""
+    g = gen(31)
+    c = make_cache4(g, kv, 2, 128, 16, BF, spread=1)
+    k, v = both_values(c, BF)
+    q, q_off = normal(g, sum(lens), 8, 128, std=60.0), offsets(lens)
+    want, tol, lse, ltol = cref.attention(q, k, v, c[4], q_off, kv, 0.5, 0, 0)
+    wide = torch.full((len(kv), 4000), -1, dtype=torch.int32)
+    wide[:, :c[4].shape[1]] = c[4]
+    step = fs.Step(q_off, kv_len=torch.tensor(kv, dtype=torch.int32).cuda(), max_kv=60000)
+    o, l = fs.fs_paged_attention4(step, on_gpu4(*c[:4], wide), q.cuda(), 0.5, want_lse=True)
+    # Values are whole codes: where the largest score's one is 0, what is left is the others', whose
+    # weights may lie beyond fp32.  An exponential is held in units of 2^-18 (and of up to 2^8
+    # of the row's largest), so one below 2^-126 * 2^18 * 2^8 = 2^-100 of the largest may become
+    # 0: each key loses less than 2^-100 of its value, at most 6 here (the scale bytes are at
+    # most 2^-1), and the weights sum to one at least.
+    tol = tol + max(kv) * 2.0 ** -100 * 6
+    within(o, want, tol, "out")
+    within(l, lse, ltol, "lse")
+
+
+@pytest.mark.parametrize("lens,kv", [([1, 1, 1], [300, 90, 5000]), ([90, 80, 1], [150, 400, 40])])
+def test_queries_that_are_not_finite_stay_in_their_rows(lens, kv):
+    g = gen(32)
+    c = make_cache4(g, kv, 2, 64, 16, HF)
+    q = normal(g, sum(lens), 4, 64, dtype=HF)
+    step, cache = step_of(lens, kv), on_gpu4(*c)
+    want, wl = fs.fs_paged_attention4(step, cache, q.cuda(), 0.1, want_lse=True)
+    q[0, 1, 3], q[sum(lens) - 1, 0, 60] = math.nan, math.inf
+    out, lse = fs.fs_paged_attention4(step, cache, q.cuda(), 0.1, want_lse=True)
+    touched = torch.zeros(sum(lens), 4, dtype=torch.bool)
+    touched[0, 1] = touched[-1, 0] = True
+    assert bool(out.cpu()[0, 1].isnan().all()) and bool(lse[0, 1].isnan())
+    assert not bool(torch.isfinite(out.cpu()[-1, 0]).any())
+    assert torch.equal(out.cpu()[~touched], want.cpu()[~touched])
+    assert torch.equal(lse.cpu()[~touched], wl.cpu()[~touched])
+
+
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("byte", [1, 0, 30, 200, 252])
 def test_attention4_of_far_scales(D, byte):

@@ -62,6 +62,8 @@ POOLS = [
     (2049, 4096, 65, 31, 0.3),
     (5000, 32, 300, 20, 0.6),
     (70001, 16, 50, 1300, 0.4),
+    (3000, 8, 9000, 2, 0.5),                  # more rows than claims fit beside each other
+    (2000, 8, 31, 1100, 0.9),                 # few pages and rows, wide ones
 ]
 
 
