@@ -26,6 +26,11 @@ struct Attn4Args : AttnArgs {  // `c` is the cache's codes, in bytes
 template <bool BF>
 constexpr float kLift4 = BF ? -18.f : 7.f;
 
+// The most that a lane's 32 probabilities of a tile may sum to before its reference is moved:
+// 2^14 times the reference's own, and below half precision's 65,504.
+template <bool BF>
+constexpr float kMostSum = BF ? 0x1p-4f : 0x1p15f;
+
 // A quarter of the 16-bit cache's bytes: twice its longest splits (64 requests of 16,384 tokens:
 // 219 us, 233 with 1,024 keys) and whole requests (30 of 2,000 tokens: 19.4 us, 23.3 in splits; 8 of
 // 1,100 11.7 and 15.0; 4 of 2,000 16.6 and 15.7).
@@ -45,15 +50,16 @@ __device__ inline void put_poison(uint32_t poison, int group, Acc &o) {
     for (int i = 0; i < N; ++i) o[i] = NAN;
 }
 
-// A wave's V tile: key rows further apart than their D values, so that 16 rows' chunks, and 4
-// rows' transposed reads, fall on different banks at addresses that differ by constants.
+// Tiles of 16-bit values: key rows further apart than their D values, so that 16 rows' chunks,
+// and 4 rows' transposed reads, fall on different banks at addresses that differ by constants
+// (places swapped by row, as over the 16-bit cache, take a register for each address).
 template <int D>
-constexpr int kVRow = D == 128 ? 144 : 72;
+constexpr int kRow = D == 128 ? 144 : 72;
+template <int D, int KEYS>
+constexpr int kTile = KEYS * kRow<D> + 8;
 template <int D>
-constexpr int kVTile = 32 * kVRow<D> + 8;
-template <int D>
-__device__ inline int v_row(int r) {
-  return r * kVRow<D> + (D == 128 ? (r >> 3 & 1) * 8 : 0);
+__device__ inline int tile_row(int r) {
+  return r * kRow<D> + (D == 128 ? (r >> 3 & 1) * 8 : 0);
 }
 
 // ---- few rows: NT tiles of 16 rows, WAVES waves, which take 32 keys each in turn
@@ -108,9 +114,9 @@ __device__ __forceinline__ void attn4_few(const Attn4Args &a, int block, short *
 #pragma unroll
   for (int t = 0; t < NT; ++t) m[t] = -INFINITY, l[t] = 0.f;
 
-  short *const v_to = lds + wave * kVTile<D> + v_row<D>(r16) + g4 * DL;
+  short *const v_to = lds + wave * kTile<D, 32> + tile_row<D>(r16) + g4 * DL;
   const short *const v_from =
-      lds + wave * kVTile<D> + v_row<D>(4 * g4 + (r16 >> 2)) + (r16 & 3) * 4;
+      lds + wave * kTile<D, 32> + tile_row<D>(4 * g4 + (r16 >> 2)) + (r16 & 3) * 4;
 
   for (int32_t from = lo; from < hi;) {
     const PageIds span = page_ids<true>(kr, from, hi, a.c.page_shift, kIds);
@@ -163,7 +169,7 @@ __device__ __forceinline__ void attn4_few(const Attn4Args &a, int block, short *
         const bool bad = vs[b] > kTopScale<BF>;
 #pragma unroll
         for (int k = 0; k < KS; ++k)
-          *reinterpret_cast<s16x8 *>(v_to + b * 16 * kVRow<D> + k * 8) =
+          *reinterpret_cast<s16x8 *>(v_to + b * 16 * kRow<D> + k * 8) =
               values8<BF>(bad ? 0 : vc[b][k], unit);
       }
       if (__any(max(max(ks[0], ks[1]), max(vs[0], vs[1])) > kTopScale<BF>)) {
@@ -216,10 +222,11 @@ __device__ __forceinline__ void attn4_few(const Attn4Args &a, int block, short *
 #pragma unroll
         for (int i = 0; i < 8; ++i) top = fmaxf(top, p[i]);
         top = max_of_halves(max_of_16s(top));
-        const float m2 = fmaxf(m[r], top);
-        // (-inf less -inf is no number and asks for nothing)
-        if (__any((m2 - m[r]) * a.c2 > kSlack)) {
-          const float f = m[r] == -INFINITY ? 0.f : exp2_fast((m[r] - m2) * a.c2);
+        // a row's reference moves by its own scores alone (-inf less -inf is no number and asks for
+        // nothing)
+        const float m2 = (top - m[r]) * a.c2 > kSlack ? top : m[r];
+        if (__any(m2 != m[r])) {
+          const float f = m[r] == -INFINITY ? 0.f : part_factor(m[r], m2, a.c2);
           l[r] *= f;
 #pragma unroll
           for (int d = 0; d < DB; ++d) o[r][d] *= f;
@@ -243,7 +250,7 @@ __device__ __forceinline__ void attn4_few(const Attn4Args &a, int block, short *
 #pragma unroll
         for (int d = 0; d < VB; ++d)
           vv[d] = __builtin_shufflevector(read_tr(v_from + (d0 + d) * 16),
-                                          read_tr(v_from + 16 * kVRow<D> + (d0 + d) * 16), 0, 1, 2,
+                                          read_tr(v_from + 16 * kRow<D> + (d0 + d) * 16), 0, 1, 2,
                                           3, 4, 5, 6, 7);
 #pragma unroll
         for (int r = 0; r < NT; ++r) {
@@ -322,15 +329,15 @@ __device__ __forceinline__ void attn4_few(const Attn4Args &a, int block, short *
 
 // ---- chunks: WAVES waves of 32 rows, 64 keys at a time through two buffers of 16-bit values
 template <bool BF, int D, int WAVES>
-__device__ __forceinline__ void attn4_chunk(const Attn4Args &a, int block, int z, short *lds,
-                                            uint8_t *scales, int *odd) {
+__device__ __forceinline__ void attn4_chunk(const Attn4Args &a, int block, int z, short *lds) {
+  __shared__ uint8_t sb[2][2][64 * (D / 32)];  // the scale bytes of K's and V's tiles
+  __shared__ int odd;                          // whether one of them counts as NaN
   constexpr int KS = D / 16;       // matrix steps of a score
   constexpr int DB = D / 32;       // 32-column blocks of an output row: groups
   constexpr int RW = 64 / DB;      // keys of a wave's load: a lane takes a group of one key
   constexpr int LD = 2 * 64 / RW / WAVES;  // a wave's loads of K and V for 64 keys
   static_assert(LD >= 1, "a wave loads whole rows");
-  auto kt = reinterpret_cast<short(*)[64 * D]>(lds), vt = kt + 2;
-  auto sb = reinterpret_cast<uint8_t(*)[2][64 * DB]>(scales);
+  constexpr int VT = 2 * kTile<D, 64>;  // K's two buffers, then V's
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r32 = lane & 31, h2 = lane >> 5;
   const int hk = block % a.c.n_kv_heads;
@@ -365,7 +372,7 @@ __device__ __forceinline__ void attn4_chunk(const Attn4Args &a, int block, int z
     }
   }
   f32x16 o[DB] = {};
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, mc = 0.f, l = 0.f;
   uint32_t poison = 0;
 
   // Load i of the wave: 64 / DB keys' K (then V) rows, the keys along the lanes, so that 16
@@ -410,16 +417,15 @@ __device__ __forceinline__ void attn4_chunk(const Attn4Args &a, int block, int z
     for (int i = 0; i < LD; ++i) {
       const bool bad = ws[i] > kTopScale<BF>;
       const float unit = scale_of<BF>(ws[i]);
-      short *tile = val[i] ? vt[buf] : kt[buf];
+      short *to = lds + (val[i] ? VT : 0) + buf * kTile<D, 64> + tile_row<D>(lrow[i]) + group * 32;
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        *reinterpret_cast<s16x8 *>(tile + tile_at<D>(lrow[i], group * 4 + k)) =
-            values8<BF>(bad ? 0 : w[i][k], unit);
+        *reinterpret_cast<s16x8 *>(to + k * 8) = values8<BF>(bad ? 0 : w[i][k], unit);
       sb[buf][val[i]][lrow[i] * DB + group] = uint8_t(ws[i]);
-      if (bad) *odd = 1;
+      if (bad) odd = 1;
     }
   };
-  if (tid == 0) *odd = 0;
+  if (tid == 0) odd = 0;
   __syncthreads();
   if (lo < hi) {
     pages(lo);
@@ -437,16 +443,22 @@ __device__ __forceinline__ void attn4_chunk(const Attn4Args &a, int block, int z
       load(j0 + 128);
       pages(j0 + 192);
     }
-    const short *kb = kt[buf], *vb = vt[buf];
     f32x16 sc[2] = {};
+    const short *const kb = lds + buf * kTile<D, 64> + tile_row<D>(r32) + h2 * 8;
 #pragma unroll
-    for (int k = 0; k < KS; ++k)
+    for (int k0 = 0; k0 < KS; k0 += 4) {
+      s16x8 kf[4][2];
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
-        sc[c] = mfma_32x32x16<BF>(
-            *reinterpret_cast<const s16x8 *>(kb + tile_at<D>(c * 32 + r32, k * 2 + h2)), qf[k],
-            sc[c]);
-    if (__builtin_amdgcn_readfirstlane(*reinterpret_cast<volatile int *>(odd))) {
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+          kf[k][c] = *reinterpret_cast<const s16x8 *>(kb + c * 32 * kRow<D> + (k0 + k) * 16);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) sc[c] = mfma_32x32x16<BF>(kf[k][c], qf[k0 + k], sc[c]);
+    }
+    if (__builtin_amdgcn_readfirstlane(odd)) {
 #pragma unroll
       for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -476,43 +488,57 @@ __device__ __forceinline__ void attn4_chunk(const Attn4Args &a, int block, int z
             sc[c][i] = -INFINITY;
         }
     }
-    float top = sc[0][0];
+    // Probabilities, and their sum, by the reference of the tiles before; only where a row has
+    // none yet, or a sum shows that a score passes it by far, the row's maximum is looked for.
+    // (Rows keep their own: what one holds does not show in another's rounding.)
+    s16x8 pf[4];
+    float sum;
+    bool moves = m == -INFINITY;
+    for (bool again = false;; again = true) {
+      if (__any(moves)) {
+        float top = sc[0][0];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[0][i]);
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[0][i]);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[1][i]);
-    const float m2 = fmaxf(m, max_of_halves(top));
-    if (__any((m2 - m) * a.c2 > kSlack)) {
-      const float f = m == -INFINITY ? 0.f : exp2_fast((m - m2) * a.c2);
-      l *= f;
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[1][i]);
+        top = max_of_halves(top);
+        const float m2 = moves ? fmaxf(m, top) : m;
+        const float f = m == -INFINITY ? 0.f : part_factor(m, m2, a.c2);
+        l *= f;
 #pragma unroll
-      for (int d = 0; d < DB; ++d) o[d] *= f;
-      m = m2;
-    }
-    const float mc = reference(m, a.c2) - kLift4<BF>;
+        for (int d = 0; d < DB; ++d) o[d] *= f;
+        m = m2;
+        mc = reference(m, a.c2) - kLift4<BF>;
+      }
+      sum = 0.f;
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < 4; ++u) {
         float p[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          p[i] = exp2_fast(fmaf(sc[c][u * 8 + i], a.c2, -mc));
-          l += p[i];
+          p[i] = exp2_fast(fmaf(sc[u >> 1][(u & 1) * 8 + i], a.c2, -mc));
+          sum += p[i];
         }
-        const s16x8 pf = pack8<BF>(p);
-        // keys 4 h2 .. + 3 and 8 + 4 h2 .. + 3 of this 16
-        const int vr = c * 32 + u * 16 + 4 * h2 + ((lane & 15) >> 2);
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          const int col = d * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-          const s16x4 v0 = read_tr(vb + tile_at<D>(vr, col >> 3) + (col & 7));
-          const s16x4 v1 = read_tr(vb + tile_at<D>(vr + 8, col >> 3) + (col & 7));
-          o[d] = mfma_32x32x16<BF>(__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7), pf,
-                                   o[d]);
-        }
+        pf[u] = pack8<BF>(p);
       }
-    __syncthreads();
+      if (again || !__any(sum > kMostSum<BF>)) break;
+      moves = max_of_halves(sum) > kMostSum<BF>;
+    }
+    l += sum;
+    const short *const vb = lds + VT + buf * kTile<D, 64> + tile_row<D>(4 * h2 + ((lane & 15) >> 2)) +
+                            (lane >> 4 & 1) * 16 + (lane & 3) * 4;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      // keys 4 h2 .. + 3 and 8 + 4 h2 .. + 3 of the 16
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        const short *from = vb + u * 16 * kRow<D> + d * 32;
+        o[d] = mfma_32x32x16<BF>(__builtin_shufflevector(read_tr(from), read_tr(from + tile_row<D>(8)),
+                                                         0, 1, 2, 3, 4, 5, 6, 7),
+                                 pf[u], o[d]);
+      }
+    // (what the wave has read and written is done; loads from memory stay under way)
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   }
   raise_err(a.err, code);
   l += __shfl_xor(l, 32, 64);
@@ -549,25 +575,21 @@ __device__ __forceinline__ void attn4_chunk(const Attn4Args &a, int block, int z
 template <bool BF, int D, int NT, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64, NT == 1 ? 4 : NT == 2 ? (D == 64 ? 3 : 2) : D == 64 ? 2 : 1)
 k_attn4_few(Attn4Args a) {
-  __shared__ __align__(16) short lds[WAVES * kVTile<D>];
+  __shared__ __align__(16) short lds[WAVES * kTile<D, 32>];
   attn4_few<BF, D, NT, WAVES>(a, blockIdx.x, lds);
 }
 template <bool BF, int D, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64, 2) k_attn4_chunk(Attn4Args a) {
-  __shared__ __align__(16) short lds[256 * D];
-  __shared__ uint8_t scales[4 * 64 * (D / 32)];
-  __shared__ int odd;
-  attn4_chunk<BF, D, WAVES>(a, blockIdx.x, blockIdx.y, lds, scales, &odd);
+  __shared__ __align__(16) short lds[4 * kTile<D, 64>];
+  attn4_chunk<BF, D, WAVES>(a, blockIdx.x, blockIdx.y, lds);
 }
 // Both kinds of requests in one launch, as over the 16-bit cache.
 template <bool BF, int D, int NT>
 __global__ void __launch_bounds__(256, 2) k_attn4_mixed(Attn4Args a, int chunk, int tiles) {
-  __shared__ __align__(16) short lds[256 * D];
-  __shared__ uint8_t scales[4 * 64 * (D / 32)];
-  __shared__ int odd;
+  __shared__ __align__(16) short lds[4 * kTile<D, 64>];
   const int block = blockIdx.x;
   if (block < chunk)
-    attn4_chunk<BF, D, 4>(a, block % tiles, block / tiles, lds, scales, &odd);
+    attn4_chunk<BF, D, 4>(a, block % tiles, block / tiles, lds);
   else
     attn4_few<BF, D, NT, 4>(a, block - chunk, lds);
 }
