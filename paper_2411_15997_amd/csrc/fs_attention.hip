@@ -284,7 +284,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs &a, int block, short *ld
         const float m2 = fmaxf(m[r], top);
         // (-inf less -inf is no number and asks for nothing)
         if (__any((m2 - m[r]) * a.c2 > kSlack)) {
-          const float f = m[r] == -INFINITY ? 0.f : exp2_fast((m[r] - m2) * a.c2);
+          const float f = m[r] == -INFINITY ? 0.f : part_factor(m[r], m2, a.c2);
           l[r] *= f;
 #pragma unroll
           for (int d = 0; d < DB; ++d) o[r][d] *= f;
@@ -526,7 +526,7 @@ __device__ __forceinline__ void attn_chunk(const AttnArgs &a, int block, int z, 
     for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[1][i]);
     const float m2 = fmaxf(m, max_of_halves(top));
     if (__any((m2 - m) * a.c2 > kSlack)) {
-      const float f = m == -INFINITY ? 0.f : exp2_fast((m - m2) * a.c2);
+      const float f = m == -INFINITY ? 0.f : part_factor(m, m2, a.c2);
       l *= f;
 #pragma unroll
       for (int d = 0; d < DB; ++d) o[d] *= f;

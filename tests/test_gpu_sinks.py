@@ -111,6 +111,36 @@ def test_values_that_are_not_finite_stay_with_the_rows_that_see_them(lens, kv, H
                 within(out[t, h][~nan], want[t, h][~nan], tol[t, h][~nan], f"out {t} {h}")
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (150, 4)])
+@pytest.mark.parametrize("n", [3, 40])
+def test_a_score_of_inf_keeps_the_rows_sum_inf_while_its_neighbours_sums_grow(n, window, sinks, dtype):
+    """lse is inf for a row that sees a score of inf, also when later keys move the references of
+    the rows beside it, whose own results stay theirs."""
+    kv, D, scale = 400, 64, 0.25
+    k = torch.zeros(kv, D)
+    k[:, 1] = torch.arange(kv) // 8      # scores that grow by more than any slack
+    k[0, 0] = math.inf
+    q = torch.zeros(n, 1, D)
+    q[:, :, 0], q[:, :, 1] = -1, 8       # (the others' score of the first key is -inf)
+    q[0, :, 0], q[0, :, 1] = 1, 0
+    kb, vb, table = make_cache(gen(29), [kv], 1, D, 16, dtype)
+    for j in range(kv):
+        kb[int(table[0, j // 16]), 0, j % 16] = k[j].to(dtype)
+    out, lse = fs.fs_paged_attention(step_of([n], [kv]), on_gpu(kb, vb, table), q.to(dtype).cuda(), scale,
+                                     window, want_lse=True, sinks=sinks)
+    assert float(lse[0, 0]) == math.inf and not bool(torch.isfinite(out[0]).any())
+    assert bool(torch.isfinite(out[1:]).all())
+    for t in range(1, n):
+        pos = kv - n + t
+        seen = [j for j in range(1, pos + 1) if window == 0 or j > pos - window or j < sinks]
+        want = float(torch.logsumexp(k[seen, 1].double() * 8 * scale, 0))
+        # scores are exact; a sum of at most 400 terms is off by 400 * 2^-24 < 3e-5, its
+        # exponents (up to 145 = 100 / ln 2) by 145 * 2^-23 < 2e-5, and lse <= 106 itself by
+        # 106 * 2^-23 < 2e-5
+        assert abs(float(lse[t, 0]) - want) < 1e-4, (t, float(lse[t, 0]), want)
+
+
 def test_sinks_in_a_graph_with_lengths_that_grow():
     g = gen(23)
     k, v, table = make_cache(g, [1300, 200], 2, 128, 16, BF)
