@@ -76,8 +76,13 @@ fs_status fs_cache4_rows(const fs_step *s, const fs_kv_cache4 *c, int32_t dtype,
 /* fs_paged_attention over a cache of 4 bits, with a window and sinks as above; q and out of
  * `dtype`.  head_dim 64 or 128 and the other limits as there.  The values that codes and
  * scales stand for are exact in `dtype` (FS_F16: in its range); the rest is as in
- * fs_paged_attention, the rounding of the probabilities included.  A group that counts as NaN
- * reaches the rows that see it alone. */
+ * fs_paged_attention, the rounding of the probabilities included, but for FS_BF16 and a request
+ * whose tokens times n_heads / n_kv_heads are more than 64: there a query's group of 32 values
+ * is multiplied with the codes in two 8-bit parts of each value, which are exact down to 2^-13
+ * of the group's largest value and below that off by at most 2^-21 of it.
+ * A group of the cache that counts as NaN makes out and lse of the rows that see it NaN (k), or
+ * its 32 values of out (v); so does a query with a value that is not finite make those of its
+ * own row, where the row sees any token.  Sums stay finite while |v| < 2^100 (FS_BF16). */
 size_t fs_attention4_workspace(const fs_step *s, const fs_kv_cache4 *c, int32_t n_heads,
                                int32_t window, int32_t sinks);
 fs_status fs_paged_attention4(const fs_step *s, const fs_kv_cache4 *c, int32_t dtype,
@@ -137,8 +142,8 @@ fs_status fs_pages_compact(const fs_pages *p, int32_t *refs_out, int32_t *table_
 
 /* Copies page src[i] to page dst[i] in k and v (scales included) of n_layers caches,
  * i < min(n, *count) (count device, NULL: n); pairs of -1 are passed over.  `layers` is a host
- * array of caches (head_dim at most 256) alike in all but their k, v (and scale) addresses (their tables are not
- * read), n_layers in [0, 2^16], n in [0, 2^24].
+ * array of caches (head_dim at most 256) alike in all but their k, v (and scale) addresses
+ * (their tables are not read), n_layers in [0, 2^16], n in [0, 2^24].
  * No dst may be another pair's src or dst, else those pages' contents are unspecified.
  * FS_E_RANGE for an id outside [-1, n_pages) or a pair with one -1. */
 fs_status fs_pages_copy(const fs_kv_cache *layers, int32_t n_layers, int32_t n, const int32_t *src,

@@ -89,13 +89,15 @@ __device__ inline float turned(int d, int half, float x, float other, const F *c
   return float(second ? F(x) * cs[f] + F(other) * sn[f] : F(x) * cs[f] - F(other) * sn[f]);
 }
 
-// VEC: pairs lie in whole 16-byte chunks (rotary_dim a multiple of 16, or of 8 when
-// interleaved).  A key's chunk is turned by one lane, which reads the chunk of the pairs' other
-// elements too; queries may be turned in place, so there a lane takes both (one pair or one
-// element per item without VEC).
+// A key's chunk of 8 elements is turned by one lane, which reads the pairs' other elements too;
+// queries may be turned in place, so there a lane takes both.  Without INTER these lie half of
+// rotary_dim apart, and PW of them (8, 4 or 1, which divides that) are one load; with INTER PW is 8
+// where whole chunks are turned.  (6,629 rows of 32 + 2 x 8 heads, 24 of 128 elements turned, and
+// the rows read back: 45.6 us, 102.6 by single elements; 6,916 rows and 22 elements 82, 40.7 interleaved.)
 // TOK tokens a work-group.
-template <bool BF, bool INTER, bool VEC, int TOK>
+template <bool BF, bool INTER, int PW, int TOK>
 __global__ void __launch_bounds__(256) k_rope_append4(Append4Args a) {
+  typedef short __attribute__((ext_vector_type(PW))) Side;  // one side of the pairs of a lane
   __shared__ double cs[TOK][128], sn[TOK][128];
   __shared__ float csf[TOK][128], snf[TOK][128];  // rounded, for the queries
   __shared__ Place place[TOK];
@@ -127,8 +129,6 @@ __global__ void __launch_bounds__(256) k_rope_append4(Append4Args a) {
 
   const int CH = D / 8;  // 8-element chunks of a head
   const int kv_items = HK * CH;
-  const int q_turned = VEC ? (INTER ? a.rotary / 8 : a.rotary / 16) : half;
-  const int per = q_turned + (VEC ? (D - a.rotary) / 8 : D - a.rotary);
   // A thread has the same item of all the work-group's tokens under way: one look for its place
   // in the row, and TOK loads before the first is waited for.  (5,726 rows of
   // 32 + 2 x 8 heads: 31 us, 36 with one item after the other.)
@@ -138,14 +138,18 @@ __global__ void __launch_bounds__(256) k_rope_append4(Append4Args a) {
     const int64_t stride = val ? a.v_stride : a.k_stride;
     const short *row = (val ? a.v : a.k) + t0 * stride + h * D;
     const bool turn = !val && ch * 8 < a.rotary;
-    s16x8 in[TOK], other[TOK];
+    s16x8 in[TOK];
+    Side other[TOK][8 / PW];
 #pragma unroll
     for (int u = 0; u < TOK; ++u) {
       const short *from = row + min(u, nt - 1) * stride;
       in[u] = *reinterpret_cast<const s16x8 *>(from + ch * 8);
-      if (!INTER && VEC && turn)  // the pairs' other elements
-        other[u] = *reinterpret_cast<const s16x8 *>(
-            from + (ch * 8 < half ? ch * 8 + half : ch * 8 - half));
+      if (!INTER && PW > 1 && turn)  // the pairs' other elements
+#pragma unroll
+        for (int g = 0; g < 8 / PW; ++g) {
+          const int d = ch * 8 + g * PW;
+          other[u][g] = *reinterpret_cast<const Side *>(from + (d < half ? d + half : d - half));
+        }
     }
 #pragma unroll
     for (int u = 0; u < TOK; ++u) {
@@ -160,15 +164,16 @@ __global__ void __launch_bounds__(256) k_rope_append4(Append4Args a) {
         if constexpr (INTER) {
 #pragma unroll
           for (int i = 0; i < 8; i += 2)
-            if (VEC || ch * 8 + i < a.rotary) {
+            if (PW == 8 || ch * 8 + i < a.rotary) {
               const float p = x[i], q = x[i + 1];
               x[i] = turned<double, INTER>(ch * 8 + i, half, p, q, c, s);
               x[i + 1] = turned<double, INTER>(ch * 8 + i + 1, half, q, p, c, s);
             }
-        } else if constexpr (VEC) {
+        } else if constexpr (PW > 1) {
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            x[i] = turned<double, INTER>(ch * 8 + i, half, x[i], to_f32<BF>(other[u][i]), c, s);
+            x[i] = turned<double, INTER>(ch * 8 + i, half, x[i],
+                                         to_f32<BF>(other[u][i / PW][i % PW]), c, s);
         } else {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
@@ -189,57 +194,66 @@ __global__ void __launch_bounds__(256) k_rope_append4(Append4Args a) {
     }
   }
 
+  // of a head's items: turned ones, single elements up to a whole chunk, chunks that stay
+  const int q_turned = INTER ? (a.rotary + 7) / 8 : half / PW;
+  const int edge = !INTER && PW == 1 ? -a.rotary & 7 : 0, rest = (a.rotary + 7) & ~7;
+  const int per = q_turned + edge + (D - rest) / 8;
   for (int it = tid; it < a.n_heads * per; it += 256) {
     const int h = it / per, j = it - h * per;
-    if constexpr (VEC) {
-      // the chunk's first element: turned below rotary
-      const int e = j >= q_turned ? a.rotary + (j - q_turned) * 8 : 8 * j;
-      const short *src = a.q + t0 * a.q_stride + h * D + e;
-      short *dst = a.q_out + t0 * a.q_out_stride + h * D + e;
-      s16x8 in[TOK], other[TOK];
+    const bool turn = j < q_turned;
+    const short *src = a.q + t0 * a.q_stride + h * D;
+    short *dst = a.q_out + t0 * a.q_out_stride + h * D;
+    if (edge && !turn && j < q_turned + edge) {
+      const int e = a.rotary + j - q_turned;
+      for (int u = 0; u < nt; ++u) dst[u * a.q_out_stride + e] = src[u * a.q_stride + e];
+      continue;
+    }
+    const int e = turn ? (INTER ? 8 : PW) * j : rest + (j - q_turned - edge) * 8;
+    src += e, dst += e;
+    s16x8 in[TOK];
+    Side other[TOK];
 #pragma unroll
-      for (int u = 0; u < TOK; ++u) {
-        const short *from = src + min(u, nt - 1) * a.q_stride;
+    for (int u = 0; u < TOK; ++u) {
+      const short *from = src + min(u, nt - 1) * a.q_stride;
+      if (INTER || PW == 8 || !turn) {
         in[u] = *reinterpret_cast<const s16x8 *>(from);
-        if (!INTER && e < half) other[u] = *reinterpret_cast<const s16x8 *>(from + half);
+      } else {
+        const Side x = *reinterpret_cast<const Side *>(from);
+#pragma unroll
+        for (int i = 0; i < PW; ++i) in[u][i] = x[i];
       }
+      if (!INTER && turn) other[u] = *reinterpret_cast<const Side *>(from + half);
+    }
 #pragma unroll
-      for (int u = 0; u < TOK; ++u) {
-        if (u >= nt) break;
-        const float *c = csf[u], *s = snf[u];
-        s16x8 v = in[u];
-        if (e < a.rotary) {
-          if constexpr (INTER) {
+    for (int u = 0; u < TOK; ++u) {
+      if (u >= nt) break;
+      const float *c = csf[u], *s = snf[u];
+      short *to = dst + u * a.q_out_stride;
+      s16x8 v = in[u];
+      if (INTER && turn) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              v[i] = to_16<BF>(turned<float, INTER>(e + i, half, to_f32<BF>(in[u][i]),
-                                                    to_f32<BF>(in[u][i ^ 1]), c, s));
-          } else {
-            s16x8 w;
+        for (int i = 0; i < 8; ++i)
+          if (PW == 8 || e + i < a.rotary)
+            v[i] = to_16<BF>(turned<float, INTER>(e + i, half, to_f32<BF>(in[u][i]),
+                                                  to_f32<BF>(in[u][i ^ 1]), c, s));
+      } else if (turn) {
+        Side w;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float p = to_f32<BF>(in[u][i]), q = to_f32<BF>(other[u][i]);
-              v[i] = to_16<BF>(turned<float, INTER>(e + i, half, p, q, c, s));
-              w[i] = to_16<BF>(turned<float, INTER>(e + i + half, half, q, p, c, s));
-            }
-            *reinterpret_cast<s16x8 *>(dst + u * a.q_out_stride + half) = w;
-          }
+        for (int i = 0; i < PW; ++i) {
+          const float p = to_f32<BF>(in[u][i]), q = to_f32<BF>(other[u][i]);
+          v[i] = to_16<BF>(turned<float, INTER>(e + i, half, p, q, c, s));
+          w[i] = to_16<BF>(turned<float, INTER>(e + i + half, half, q, p, c, s));
         }
-        *reinterpret_cast<s16x8 *>(dst + u * a.q_out_stride) = v;
-      }
-    } else {
-      const int e0 = INTER ? 2 * j : j, e1 = INTER ? 2 * j + 1 : j + half;
-      for (int u = 0; u < nt; ++u) {
-        const short *src = a.q + (t0 + u) * a.q_stride + h * D;
-        short *dst = a.q_out + (t0 + u) * a.q_out_stride + h * D;
-        if (j >= q_turned) {
-          dst[a.rotary + j - q_turned] = src[a.rotary + j - q_turned];
+        *reinterpret_cast<Side *>(to + half) = w;
+        if constexpr (PW < 8) {
+          Side x;
+#pragma unroll
+          for (int i = 0; i < PW; ++i) x[i] = v[i];
+          *reinterpret_cast<Side *>(to) = x;
           continue;
         }
-        const float p = to_f32<BF>(src[e0]), q = to_f32<BF>(src[e1]);
-        dst[e0] = to_16<BF>(turned<float, INTER>(e0, half, p, q, csf[u], snf[u]));
-        dst[e1] = to_16<BF>(turned<float, INTER>(e1, half, q, p, csf[u], snf[u]));
       }
+      *reinterpret_cast<s16x8 *>(to) = v;
     }
   }
 }
@@ -338,20 +352,21 @@ hipError_t launch_rope_append4(const fs_step *s, const fs_kv_cache4 *c, const fs
   a.factor = r->factor;
   a.n_heads = n_heads;
   a.rotary = r->rotary_dim;
-  const bool inter = r->interleaved != 0;
-  const bool vec = r->rotary_dim % (inter ? 8 : 16) == 0;
+  const int half = r->rotary_dim / 2;
   by_rows(a.rows, dtype, [&](auto bf, auto tok) {
     constexpr bool BF = decltype(bf)::value;
     constexpr int TOK = decltype(tok)::value;
     const dim3 grid((a.rows + TOK - 1) / TOK), block(256);
-    if (inter && vec)
-      hipLaunchKernelGGL((k_rope_append4<BF, true, true, TOK>), grid, block, 0, stream, a);
-    else if (inter)
-      hipLaunchKernelGGL((k_rope_append4<BF, true, false, TOK>), grid, block, 0, stream, a);
-    else if (vec)
-      hipLaunchKernelGGL((k_rope_append4<BF, false, true, TOK>), grid, block, 0, stream, a);
+    if (r->interleaved && r->rotary_dim % 8 == 0)
+      hipLaunchKernelGGL((k_rope_append4<BF, true, 8, TOK>), grid, block, 0, stream, a);
+    else if (r->interleaved)
+      hipLaunchKernelGGL((k_rope_append4<BF, true, 1, TOK>), grid, block, 0, stream, a);
+    else if (half % 8 == 0)
+      hipLaunchKernelGGL((k_rope_append4<BF, false, 8, TOK>), grid, block, 0, stream, a);
+    else if (half % 4 == 0)
+      hipLaunchKernelGGL((k_rope_append4<BF, false, 4, TOK>), grid, block, 0, stream, a);
     else
-      hipLaunchKernelGGL((k_rope_append4<BF, false, false, TOK>), grid, block, 0, stream, a);
+      hipLaunchKernelGGL((k_rope_append4<BF, false, 1, TOK>), grid, block, 0, stream, a);
   });
   return hipGetLastError();
 }

@@ -45,7 +45,7 @@ using Codes = uint32_t __attribute__((ext_vector_type(N / 8)));
 // significant bits, which two numbers of 4 (sign, 4 bits of exponent, 3 of fraction) hold
 // exactly.  A group of 32 has the power of two that brings its largest value to 2^7 .. 2^8; its
 // second parts are in units of 2^-4 of the first ones'.  Exact down to 2^-13 of the group's
-// largest value; below, a value is off by at most 2^-22 of that.
+// largest value; below, a value is off by at most 2^-21 of that.
 struct Parts8 {
   uint32_t hi[4], lo[4];  // of 16 neighbouring values
 };

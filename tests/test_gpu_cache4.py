@@ -105,6 +105,12 @@ APPEND = [
     ([13], [200], 1, 1, 32, 1, 2, False),
     ([6], [6], 3, 3, 96, 32, 0, False),                            # nothing turns
     ([40, 3], [1 << 20, 900], 2, 2, 128, 4096, 128, False),
+    # four tokens a work-group, the last one's not all there; sides of 4, of 1, chunks turned in part
+    ([1021, 5], [1021, 300], 3, 1, 64, 16, 24, False),
+    ([5, 1021], [3, 2000], 2, 2, 96, 16, 22, False),
+    ([1027], [1500], 1, 1, 32, 64, 20, False),
+    ([1, 1026], [9, 1026], 3, 1, 64, 16, 20, True),
+    ([1030], [1030], 2, 1, 128, 8, 128, False),
 ]
 
 
