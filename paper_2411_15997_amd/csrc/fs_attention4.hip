@@ -36,6 +36,11 @@ constexpr float kMostSum = BF ? 0x1p-4f : 0x1p15f;
 // 1,100 11.7 and 15.0; 4 of 2,000 16.6 and 15.7).
 constexpr int32_t kFewMost4 = 2048;
 constexpr int32_t kFewWhole4 = 262144;
+// Splits go by the bound on lengths, and chunks of several requests seldom all reach it: twice the
+// work-groups.  (4 chunks of 300 rows over 20,000, 3,000, 1,000 and 500 keys: 215 us, 320 with 512
+// work-groups, all over 20,000 438 and 462; 8 of 100 over 100 to 8,000, head_dim 64: 39 and 63, all
+// over 8,000 64 and 87; but 3 of 1,000 over 9,000 457 and 414, 16 of 64 over 4,000 105 and 88.)
+constexpr int32_t kChunkWant4 = 1024;
 
 // Codes of N neighbouring values: 16 bytes for 32 of them, 8 for 16.
 template <int N>
@@ -807,7 +812,7 @@ void run(const Attn4Args &a, const Plan &p, hipStream_t stream) {
 size_t attention4_workspace_bytes(const fs_step *s, const fs_kv_cache4 *c, int32_t n_heads,
                                   int32_t window, int32_t sinks) {
   const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks, kFewMost4,
-                            kFewWhole4);
+                            kFewWhole4, kChunkWant4);
   return space(plan(s, sh), s, sh).total();
 }
 
@@ -816,7 +821,7 @@ hipError_t launch_attention4(const fs_step *s, const fs_kv_cache4 *c, int32_t dt
                              const void *q, int64_t q_stride, void *out, int64_t out_stride,
                              float *lse, void *ws, int32_t *err, hipStream_t stream) {
   const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks, kFewMost4,
-                            kFewWhole4);
+                            kFewWhole4, kChunkWant4);
   const Plan p = plan(s, sh);
   Attn4Args a;
   fill_args(a, p, space(p, s, sh), sh, s, scale, q, q_stride, out, out_stride, lse, ws, err);
