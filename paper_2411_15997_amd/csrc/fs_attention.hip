@@ -686,7 +686,8 @@ void run(const AttnArgs &a, const Plan &p, hipStream_t stream) {
 
 size_t attention_workspace_bytes(const fs_step *s, const fs_kv_cache *c, int32_t n_heads,
                                  int32_t window, int32_t sinks) {
-  const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks, 1024, 131072, 512);
+  const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks, 1024, 131072, 512,
+                            1024);
   return space(plan(s, sh), s, sh).total();
 }
 
@@ -694,7 +695,8 @@ hipError_t launch_attention(const fs_step *s, const fs_kv_cache *c, int32_t n_he
                             int32_t window, int32_t sinks, const void *q, int64_t q_stride,
                             void *out, int64_t out_stride, float *lse, void *ws, int32_t *err,
                             hipStream_t stream) {
-  const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks, 1024, 131072, 512);
+  const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks, 1024, 131072, 512,
+                            1024);
   const Plan p = plan(s, sh);
   AttnArgs a;
   fill_args(a, p, space(p, s, sh), sh, s, scale, q, q_stride, out, out_stride, lse, ws, err);

@@ -41,6 +41,9 @@ constexpr int32_t kFewWhole4 = 262144;
 // work-groups, all over 20,000 438 and 462; 8 of 100 over 100 to 8,000, head_dim 64: 39 and 63, all
 // over 8,000 64 and 87; but 3 of 1,000 over 9,000 457 and 414, 16 of 64 over 4,000 105 and 88.)
 constexpr int32_t kChunkWant4 = 1024;
+// (100 rows over 4,000 keys 31.7 us, 38.7 in splits of 1,024 keys, 33.5 of 256; 255 rows over 11,191,
+// head_dim 64, 32.1, 36.6 and 32.2; 300 over 20,000 take longer splits.)
+constexpr int32_t kChunkLeast4 = 512;
 
 // Codes of N neighbouring values: 16 bytes for 32 of them, 8 for 16.
 template <int N>
@@ -812,7 +815,7 @@ void run(const Attn4Args &a, const Plan &p, hipStream_t stream) {
 size_t attention4_workspace_bytes(const fs_step *s, const fs_kv_cache4 *c, int32_t n_heads,
                                   int32_t window, int32_t sinks) {
   const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks, kFewMost4,
-                            kFewWhole4, kChunkWant4);
+                            kFewWhole4, kChunkWant4, kChunkLeast4);
   return space(plan(s, sh), s, sh).total();
 }
 
@@ -821,7 +824,7 @@ hipError_t launch_attention4(const fs_step *s, const fs_kv_cache4 *c, int32_t dt
                              const void *q, int64_t q_stride, void *out, int64_t out_stride,
                              float *lse, void *ws, int32_t *err, hipStream_t stream) {
   const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks, kFewMost4,
-                            kFewWhole4, kChunkWant4);
+                            kFewWhole4, kChunkWant4, kChunkLeast4);
   const Plan p = plan(s, sh);
   Attn4Args a;
   fill_args(a, p, space(p, s, sh), sh, s, scale, q, q_stride, out, out_stride, lse, ws, err);

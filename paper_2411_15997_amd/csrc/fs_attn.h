@@ -324,14 +324,15 @@ struct Shape {
   int32_t n_heads, n_kv_heads, head_dim, window, sinks;
   int32_t few_most;   // keys of a split of few rows, at most
   int32_t few_whole;  // keys times head_dim that eight waves take without a split
-  int32_t chunk_want;  // work-groups wanted of several requests' chunks
+  int32_t chunk_want;   // work-groups wanted of several requests' chunks
+  int32_t chunk_least;  // keys of a split of chunks, at least
 };
 Shape shape_of(const fs_step *s, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                int32_t window, int32_t sinks, int32_t few_most, int32_t few_whole,
-               int32_t chunk_want) {
+               int32_t chunk_want, int32_t chunk_least) {
   window = limited(window, s);
   sinks = window == 0 ? 0 : sinks < s->max_kv ? sinks : s->max_kv;
-  return {n_heads, n_kv_heads, head_dim, window, sinks, few_most, few_whole, chunk_want};
+  return {n_heads, n_kv_heads, head_dim, window, sinks, few_most, few_whole, chunk_want, chunk_least};
 }
 
 Plan plan(const fs_step *s, const Shape &c) {
@@ -408,7 +409,7 @@ Plan plan(const fs_step *s, const Shape &c) {
     // with 256 work-groups, 144 with 1,024)
     const int32_t toks = p.chunk_rows / G + 2;
     split_of(int64_t(p.chunk_tiles) * c.n_kv_heads, keys(most < toks ? most : toks),
-             p.chunk_seqs > 1 ? c.chunk_want : 512, 1024, 1 << 30, s->q_off_h[s->n_seqs], p.chunk_split, p.chunk_splits);
+             p.chunk_seqs > 1 ? c.chunk_want : 512, c.chunk_least, 1 << 30, s->q_off_h[s->n_seqs], p.chunk_split, p.chunk_splits);
   }
   return p;
 }
