@@ -7,6 +7,9 @@
 // once: next to the border of two codes an error of fp32 would pick the other one, half of the
 // value away, and the cache would hang on the order of operations.  A key value costs two
 // fp64 products, which the card does at half of its fp32 rate.
+// Bound by HBM in steps of thousands of rows (7,616 of 32 + 2 x 8 heads of 128: 31.5 us, 5.2 TB/s,
+// and 8.7, 4.5 TB/s, to read them back), by the chain from lengths to pages to rows in small ones
+// (8 rows: 5.0 us and 3.2).
 #include <type_traits>
 
 #include "fs_cache.h"
@@ -91,9 +94,10 @@ __device__ inline float turned(int d, int half, float x, float other, const F *c
 
 // A key's chunk of 8 elements is turned by one lane, which reads the pairs' other elements too;
 // queries may be turned in place, so there a lane takes both.  Without INTER these lie half of
-// rotary_dim apart, and PW of them (8, 4 or 1, which divides that) are one load; with INTER PW is 8
-// where whole chunks are turned.  (6,629 rows of 32 + 2 x 8 heads, 24 of 128 elements turned, and
-// the rows read back: 45.6 us, 102.6 by single elements; 6,916 rows and 22 elements 82, 40.7 interleaved.)
+// rotary_dim apart, and PW of them (8, 4 or 1, which divides that) are one load; with INTER PW is
+// 8 where whole chunks are turned.  (6,629 rows of 32 + 2 x 8 heads, 24 of 128 elements turned,
+// and the rows read back: 45.6 us, 102.6 by single elements; 6,916 rows and 22 elements 82, 40.7
+// interleaved.)
 // TOK tokens a work-group.
 template <bool BF, bool INTER, int PW, int TOK>
 __global__ void __launch_bounds__(256) k_rope_append4(Append4Args a) {
@@ -130,8 +134,8 @@ __global__ void __launch_bounds__(256) k_rope_append4(Append4Args a) {
   const int CH = D / 8;  // 8-element chunks of a head
   const int kv_items = HK * CH;
   // A thread has the same item of all the work-group's tokens under way: one look for its place
-  // in the row, and TOK loads before the first is waited for.  (5,726 rows of
-  // 32 + 2 x 8 heads: 31 us, 36 with one item after the other.)
+  // in the row, and TOK loads before the first is waited for.  (7,616 rows of
+  // 32 + 2 x 8 heads: 31.5 us, 36 with one item after the other.)
   for (int it = tid; it < 2 * kv_items; it += 256) {
     const bool val = it >= kv_items;
     const int r = val ? it - kv_items : it, h = r / CH, ch = r - h * CH;

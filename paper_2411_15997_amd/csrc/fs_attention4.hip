@@ -1,13 +1,23 @@
-// Attention of the step's rows over a paged cache held in 4 bits: the softmax, the split of
-// the work and the joins of the kernels over the 16-bit cache, with codes in place of values.
-//
-// A group of 32 values and its scale become 16-bit values exactly (one conversion
-// instruction for two of them), so both products are those of the 16-bit cache.
-//   K  feeds the first product from registers: the sum over a head's dimensions may be taken
-//      in any order, so each lane takes 32 (or 16) neighbouring ones of a key, 16 bytes of
-//      codes with one scale, and a wave's load is 16 whole keys without a gap.
-//   V  is wanted with keys along a lane, while its codes and scales lie along dimensions:
-//      it goes through LDS as 16-bit values and is read back transposed.
+// Attention of the step's rows over a paged cache held in 4 bits:
+//   o = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q . k_j - m),  over the keys a row sees,
+// with the softmax's running reference, the split of the work and the joins of the kernels over
+// the 16-bit cache, and codes in place of values.  A group of 32 values and its scale become
+// 16-bit values exactly (one conversion instruction for two of them).
+//   k_attn4_few    requests of at most 64 rows: bound by the cache's bytes where many are long
+//                  (64 of 16,384 tokens: 219 us, 5.2 TB/s; 128 of up to 16,384, 229,312 in all,
+//                  70 us, 3.6 TB/s, 60 and 4.2 without the join and the launch), by the chain from
+//                  lengths to pages to keys where few are (4 of 500: 8.6 us).  K feeds the first
+//                  product from registers: the sum over a head's dimensions may be taken in any
+//                  order, so each lane takes 32 (or 16) neighbouring ones of a key, 16 bytes of
+//                  codes with one scale, and a wave's load is 16 whole keys without a gap.  V is
+//                  wanted with keys along a lane, while its codes and scales lie along dimensions:
+//                  it goes through LDS as 16-bit values and is read back transposed.
+//   k_attn4_chunk  larger chunks: bound by the products and the tile's steps between them (4,096
+//                  rows over 32,768 keys 1.64 to 1.74 ms from card to card, up to 1.25 PFLOP/s; in
+//                  half precision 1.88 to 1.98).  V as above; K stays in codes for bfloat16
+//                  queries, which are multiplied as two 8-bit parts, and is made values for others.
+//   k_attn4_mixed  both in one launch; the joins are those of the 16-bit cache, or
+//   k_attn4_join_many for few rows in very many splits.
 #include <type_traits>
 
 #include "fs_attn.h"
@@ -32,8 +42,10 @@ template <bool BF>
 constexpr float kMostSum = BF ? 0x1p-4f : 0x1p15f;
 
 // A quarter of the 16-bit cache's bytes: twice its longest splits (64 requests of 16,384 tokens:
-// 219 us, 233 with 1,024 keys) and whole requests (30 of 2,000 tokens: 19.4 us, 23.3 in splits; 8 of
-// 1,100 11.7 and 15.0; 4 of 2,000 16.6 and 15.7).
+// 219 us, 233 with 1,024 keys) and whole requests (30 of 2,000 tokens: 19.4 us, 23.3 in splits; 8
+// of 1,100 11.7 and 15.0; 4 of 2,000 16.6 and 15.7).  (Finer splits, 4,096 work-groups wanted,
+// help a few requests of which one is long, 9 of 2 to 18,596 tokens 27 us and 45, and cost those
+// that are alike, 32 of 8,000 46 and 41, 8 of 32,768 51 and 44.)
 constexpr int32_t kFewMost4 = 2048;
 constexpr int32_t kFewWhole4 = 262144;
 // Splits go by the bound on lengths, and chunks of several requests seldom all reach it: twice the
@@ -41,8 +53,8 @@ constexpr int32_t kFewWhole4 = 262144;
 // work-groups, all over 20,000 438 and 462; 8 of 100 over 100 to 8,000, head_dim 64: 39 and 63, all
 // over 8,000 64 and 87; but 3 of 1,000 over 9,000 457 and 414, 16 of 64 over 4,000 105 and 88.)
 constexpr int32_t kChunkWant4 = 1024;
-// (100 rows over 4,000 keys 31.7 us, 38.7 in splits of 1,024 keys, 33.5 of 256; 255 rows over 11,191,
-// head_dim 64, 32.1, 36.6 and 32.2; 300 over 20,000 take longer splits.)
+// (100 rows over 4,000 keys 31.7 us, 38.7 in splits of 1,024 keys, 33.5 of 256; 255 rows over
+// 11,191, head_dim 64, 32.1, 36.6 and 32.2; 300 over 20,000 take longer splits.)
 constexpr int32_t kChunkLeast4 = 512;
 
 // Codes of N neighbouring values: 16 bytes for 32 of them, 8 for 16.
@@ -391,9 +403,10 @@ __device__ __forceinline__ void attn4_chunk(const Attn4Args &a, int block, int z
   static_assert(LD >= 1, "a wave loads whole rows");
   // K's two buffers, then V's.  K stays in codes where the queries are bfloat16: the matrix
   // cores multiply them with the queries' two parts, at the rate of one product of 16-bit
-  // values, a quarter of the reads from LDS and no conversion.  (4,096 rows over 32,768 keys: 1,657 us, 1,843
-  // with K as values; 24 mixed requests of head_dim 128 706 and 773, of 64 284 and 294.
-  // In half precision three parts would cost more than they save.)
+  // values, a quarter of the reads from LDS and no conversion.  (4,096 rows over 32,768 keys:
+  // 1,657 us, 1,843 with K as values; 24 mixed requests of head_dim 128 706 and 773, of 64 284
+  // and 294.  In half precision three parts would cost more than they save; with few rows, which
+  // wait for memory, the codes change nothing.)
   constexpr int KB = BF ? kCodeTile<D> / 2 : kTile<D, 64>, VT = 2 * KB;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r32 = lane & 31, h2 = lane >> 5;

@@ -405,11 +405,12 @@ Plan plan(const fs_step *s, const Shape &c) {
                        ? 256
                        : 128;
     p.chunk_tiles = tiles(p.chunk_rows);
-    // 512 work-groups wanted, of at least 1,024 keys (300 rows over 20,000 keys: 134 us, 154
-    // with 256 work-groups, 144 with 1,024)
+    // 512 work-groups wanted, of at least 1,024 keys over the 16-bit cache (300 rows over 20,000
+    // keys: 134 us, 154 with 256 work-groups, 144 with 1,024)
     const int32_t toks = p.chunk_rows / G + 2;
     split_of(int64_t(p.chunk_tiles) * c.n_kv_heads, keys(most < toks ? most : toks),
-             p.chunk_seqs > 1 ? c.chunk_want : 512, c.chunk_least, 1 << 30, s->q_off_h[s->n_seqs], p.chunk_split, p.chunk_splits);
+             p.chunk_seqs > 1 ? c.chunk_want : 512, c.chunk_least, 1 << 30,
+             s->q_off_h[s->n_seqs], p.chunk_split, p.chunk_splits);
   }
   return p;
 }

@@ -236,6 +236,9 @@ ATTENTION = [
     ([257], [771], 5, 1, 128, 16, 0, 0),
     ([300, 1, 3], [900, 2000, 700], 4, 2, 64, 16, 64, 40),
     ([261, 0, 77], [500, 9, 333], 64, 16, 128, 16, 150, 9),
+    ([100], [4000], 4, 1, 128, 16, 0, 0),                 # chunks over split keys
+    ([90, 80, 1], [2600, 700, 1500], 3, 3, 64, 32, 0, 0),
+    ([65] * 67 + [1] * 3, [66 + 9 * i for i in range(66)] + [2500, 3, 0, 1400], 1, 1, 64, 16, 0, 0),  # > 64 requests
 ]
 
 
@@ -263,6 +266,21 @@ def test_attention4(lens, kv, H, HK, D, page, window, sinks, dtype):
     # a scale of the other sign
     want, tol, _, _ = cref.attention(q, k, v, c[4], q_off, kv, -scale, window, sinks)
     within(fs.fs_paged_attention4(step, cache, qd, -scale, window, sinks), want, tol, "out, flipped")
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("lens,kv", [([1, 2], [700, 30]), ([70, 1], [900, 40])])
+def test_attention4_with_a_scale_of_zero(lens, kv, dtype):
+    """Every visible token counts alike."""
+    g = gen(41)
+    c = make_cache4(g, kv, 1, 128, 16, dtype)
+    k, v = both_values(c, dtype)
+    q = normal(g, sum(lens), 2, 128, dtype=dtype)
+    for scale in (0.0, -0.0):
+        want, tol, lse, ltol = cref.attention(q, k, v, c[4], offsets(lens), kv, scale, 0, 0)
+        o, l = fs.fs_paged_attention4(step_of(lens, kv), on_gpu4(*c), q.cuda(), scale, want_lse=True)
+        within(o, want, tol, "out")
+        within(l, lse, ltol, "lse")
 
 
 @pytest.mark.parametrize("dtype", [BF, HF])
