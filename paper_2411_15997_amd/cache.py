@@ -196,12 +196,12 @@ def fs_cache4_rows(step: Step, cache: KVCache4, dtype=None, k=None, v=None, err=
     if gpu != engine._current_gpu():
         return _there(gpu, fs_cache4_rows, step, cache, dtype, k, v, err, check)
     if k is None:
-        k = torch.empty((T, HK, D), dtype=dtype, device=cache.k.device)
+        k = torch.empty_strided((T, HK, D), (HK * D, D, 1), dtype=dtype, device=cache.k.device)
         kp, ks = k.data_ptr(), HK * D
     else:
         kp, ks = _rows(k, "k", (T, HK, D))
     if v is None:
-        v = torch.empty((T, HK, D), dtype=dtype, device=cache.k.device)
+        v = torch.empty_strided((T, HK, D), (HK * D, D, 1), dtype=dtype, device=cache.k.device)
         vp, vs = v.data_ptr(), HK * D
     else:
         vp, vs = _rows(v, "v", (T, HK, D))
