@@ -48,6 +48,7 @@ constexpr float kMostSum = BF ? 0x1p-4f : 0x1p15f;
 // that are alike, 32 of 8,000 46 and 41, 8 of 32,768 51 and 44.)
 constexpr int32_t kFewMost4 = 2048;
 constexpr int32_t kFewWhole4 = 262144;
+constexpr int32_t kOnce4 = 2048;
 // Splits go by the bound on lengths, and chunks of several requests seldom all reach it: twice the
 // work-groups.  (4 chunks of 300 rows over 20,000, 3,000, 1,000 and 500 keys: 215 us, 320 with 512
 // work-groups, all over 20,000 438 and 462; 8 of 100 over 100 to 8,000, head_dim 64: 39 and 63, all
@@ -828,7 +829,7 @@ void run(const Attn4Args &a, const Plan &p, hipStream_t stream) {
 size_t attention4_workspace_bytes(const fs_step *s, const fs_kv_cache4 *c, int32_t n_heads,
                                   int32_t window, int32_t sinks) {
   const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks, kFewMost4,
-                            kFewWhole4, kChunkWant4, kChunkLeast4);
+                            kFewWhole4, kOnce4, kChunkWant4, kChunkLeast4);
   return space(plan(s, sh), s, sh).total();
 }
 
@@ -837,7 +838,7 @@ hipError_t launch_attention4(const fs_step *s, const fs_kv_cache4 *c, int32_t dt
                              const void *q, int64_t q_stride, void *out, int64_t out_stride,
                              float *lse, void *ws, int32_t *err, hipStream_t stream) {
   const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks, kFewMost4,
-                            kFewWhole4, kChunkWant4, kChunkLeast4);
+                            kFewWhole4, kOnce4, kChunkWant4, kChunkLeast4);
   const Plan p = plan(s, sh);
   Attn4Args a;
   fill_args(a, p, space(p, s, sh), sh, s, scale, q, q_stride, out, out_stride, lse, ws, err);

@@ -324,15 +324,17 @@ struct Shape {
   int32_t n_heads, n_kv_heads, head_dim, window, sinks;
   int32_t few_most;   // keys of a split of few rows, at most
   int32_t few_whole;  // keys times head_dim that eight waves take without a split
+  int32_t few_once;     // keys that are not split where the card is full without, at most
   int32_t chunk_want;   // work-groups wanted of several requests' chunks
   int32_t chunk_least;  // keys of a split of chunks, at least
 };
 Shape shape_of(const fs_step *s, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                int32_t window, int32_t sinks, int32_t few_most, int32_t few_whole,
-               int32_t chunk_want, int32_t chunk_least) {
+               int32_t few_once, int32_t chunk_want, int32_t chunk_least) {
   window = limited(window, s);
   sinks = window == 0 ? 0 : sinks < s->max_kv ? sinks : s->max_kv;
-  return {n_heads, n_kv_heads, head_dim, window, sinks, few_most, few_whole, chunk_want, chunk_least};
+  return {n_heads, n_kv_heads, head_dim, window, sinks, few_most, few_whole, few_once, chunk_want,
+          chunk_least};
 }
 
 Plan plan(const fs_step *s, const Shape &c) {
@@ -379,6 +381,16 @@ Plan plan(const fs_step *s, const Shape &c) {
     const int32_t len = keys(p.few_tokens);
     split_of(blocks, len, 1024, 512, c.few_most, int64_t(s->n_seqs) * p.few_tokens, p.few_split,
              p.few_splits);
+    // Not split where every compute unit has a work-group without, and the longest few enough
+    // keys for them: no join.  (4 bits: 64 requests of up to 16,384 tokens, 8 heads of 128, a
+    // window of 700 14.2 us, 16.2 in two splits, of 1,500 19.1 and 21.6; 40 of 1,500, 16 heads,
+    // 33 and 40; 64 of 2,000 34.6 and 39.3, but 33 of 2,000 27.2 and 24.6.  16 bits with sinks:
+    // a window of 1,000 30.0 and 32.0, and of 1,500 over 264 work-groups 29.3 and 25.2.)
+    const int64_t once = 1024 + 2 * blocks;
+    if (blocks > 256 && p.few_splits > 1 && len <= (once < c.few_once ? once : c.few_once)) {
+      p.few_split = c.few_once;
+      p.few_splits = 1;
+    }
     // Up to 1,024 keys (2,048 of head_dim 64) with a compute unit for each work-group: eight
     // waves and no join.  (4 requests, 8 heads of 128: 500 keys 8.9 us, 9.8 with four waves;
     // 1,000 keys 11.5 and, in two splits, 13.5; 30 requests of 1,000 13.4 and 17.1; 1,500 keys
