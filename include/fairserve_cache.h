@@ -81,8 +81,9 @@ fs_status fs_cache4_rows(const fs_step *s, const fs_kv_cache4 *c, int32_t dtype,
  * is multiplied with the codes in two 8-bit parts of each value, which are exact down to 2^-13
  * of the group's largest value and below that off by at most 2^-21 of it.
  * A group of the cache that counts as NaN makes out and lse of the rows that see it NaN (k), or
- * its 32 values of out (v); so does a query with a value that is not finite make those of its
- * own row, where the row sees any token.  Sums stay finite while |v| < 2^100 (FS_BF16). */
+ * its 32 values of out (v).  A query with a value that is not finite reaches its own row alone:
+ * out and lse are NaN where it is multiplied in parts and the row sees a token, else what its
+ * scores make of them.  Sums stay finite while |v| < 2^100 (FS_BF16). */
 size_t fs_attention4_workspace(const fs_step *s, const fs_kv_cache4 *c, int32_t n_heads,
                                int32_t window, int32_t sinks);
 fs_status fs_paged_attention4(const fs_step *s, const fs_kv_cache4 *c, int32_t dtype,
