@@ -62,44 +62,6 @@ constexpr int32_t kChunkLeast4 = 512;
 template <int N>
 using Codes = uint32_t __attribute__((ext_vector_type(N / 8)));
 
-// Queries as the matrix cores' products with 4-bit numbers take them: a bfloat16 number has 8
-// significant bits, which two numbers of 4 (sign, 4 bits of exponent, 3 of fraction) hold
-// exactly.  A group of 32 has the power of two that brings its largest value to 2^7 .. 2^8; its
-// second parts are in units of 2^-4 of the first ones'.  Exact down to 2^-13 of the group's
-// largest value; below, a value is off by at most 2^-21 of that.
-struct Parts8 {
-  uint32_t hi[4], lo[4];  // of 16 neighbouring values
-};
-// The scale byte of a group whose values' absolute bits are at most `top` (finite).
-__device__ inline uint32_t query_scale(uint32_t top) { return max(top >> 23, 12u) - 7; }
-__device__ inline Parts8 query_parts(const float *x, uint32_t scale) {
-  const float inv = __uint_as_float((254 - scale) << 23);
-  Parts8 p;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    float y[4], r[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = x[w * 4 + i] * inv;
-    int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-    hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], hi, true);
-    r[0] = (y[0] - __builtin_amdgcn_cvt_f32_fp8(hi, 0)) * 16.f;
-    r[1] = (y[1] - __builtin_amdgcn_cvt_f32_fp8(hi, 1)) * 16.f;
-    r[2] = (y[2] - __builtin_amdgcn_cvt_f32_fp8(hi, 2)) * 16.f;
-    r[3] = (y[3] - __builtin_amdgcn_cvt_f32_fp8(hi, 3)) * 16.f;
-    int lo = __builtin_amdgcn_cvt_pk_fp8_f32(r[0], r[1], 0, false);
-    lo = __builtin_amdgcn_cvt_pk_fp8_f32(r[2], r[3], lo, true);
-    p.hi[w] = uint32_t(hi);
-    p.lo[w] = uint32_t(lo);
-  }
-  return p;
-}
-__device__ inline uint32_t abs_bits(const float *x, int n) {
-  uint32_t top = 0;
-  for (int i = 0; i < n; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-  return top;
-}
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-
 // A group that counts as NaN is multiplied as zeros; the rows that see such a key get NaN in
 // the group's columns at the end: bit g of `poison` for the columns 32 g .. .
 template <int N, class Acc>
@@ -116,11 +78,6 @@ template <int D>
 constexpr int kRow = D == 128 ? 144 : 72;
 template <int D, int KEYS>
 constexpr int kTile = KEYS * kRow<D> + 8;
-// Bytes of a tile of 64 keys' codes: rows 16 bytes further apart, for the same reason.
-template <int D>
-constexpr int kCodeRow = D / 2 + 16;
-template <int D>
-constexpr int kCodeTile = 64 * kCodeRow<D>;
 template <int D>
 __device__ inline int tile_row(int r) {
   return r * kRow<D> + (D == 128 ? (r >> 3 & 1) * 8 : 0);
@@ -396,19 +353,16 @@ template <bool BF, int D, int WAVES>
 __device__ __forceinline__ void attn4_chunk(const Attn4Args &a, int block, int z, short *lds) {
   __shared__ __align__(16) uint8_t sb[2][2][64 * (D / 32)];  // the scale bytes of K's and V's tiles
   __shared__ int odd;                          // whether one of them counts as NaN
-  constexpr int KS = D / 16;       // matrix steps of a score, by 16-bit values
-  constexpr int K4 = D / 64;       // the same by codes
+  constexpr int KS = D / 16;       // matrix steps of a score
   constexpr int DB = D / 32;       // 32-column blocks of an output row: groups
   constexpr int RW = 64 / DB;      // keys of a wave's load: a lane takes a group of one key
   constexpr int LD = 2 * 64 / RW / WAVES;  // a wave's loads of K and V for 64 keys
   static_assert(LD >= 1, "a wave loads whole rows");
-  // K's two buffers, then V's.  K stays in codes where the queries are bfloat16: the matrix
-  // cores multiply them with the queries' two parts, at the rate of one product of 16-bit
-  // values, a quarter of the reads from LDS and no conversion.  (4,096 rows over 32,768 keys:
-  // 1,657 us, 1,843 with K as values; 24 mixed requests of head_dim 128 706 and 773, of 64 284
-  // and 294.  In half precision three parts would cost more than they save; with few rows, which
-  // wait for memory, the codes change nothing.)
-  constexpr int KB = BF ? kCodeTile<D> / 2 : kTile<D, 64>, VT = 2 * KB;
+  // K's two buffers, then V's, as 16-bit values.  (The matrix cores' products of 4-bit numbers
+  // would take K's codes as they are, with the queries as two 8-bit parts, in 1,657 us for 4,096
+  // rows over 32,768 keys; but they drop what lies 2^-14 below the largest of the products that
+  // they add at once, and scores are sums of 32 bits.)
+  constexpr int VT = 2 * kTile<D, 64>;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r32 = lane & 31, h2 = lane >> 5;
   const int hk = block % a.c.n_kv_heads;
@@ -433,47 +387,12 @@ __device__ __forceinline__ void attn4_chunk(const Attn4Args &a, int block, int z
   const int32_t pos_lo = kv - n + min(r0 + wave * 32, R - 1) / G;
   const int32_t win_hi =
       a.window ? kv - n + min(r0 + wave * 32 + 31, R - 1) / G - a.window : INT32_MIN;
-  s16x8 qf[BF ? 1 : KS];
-  i32x8 q_hi[BF ? K4 : 1], q_lo[BF ? K4 : 1];  // 16 dimensions of each of two groups
-  uint32_t q_scale = 0;  // bytes: the first parts' scale of group h2 of each step, the second's
-  bool broken = false;   // a value of the row's query is not finite
-  if constexpr (BF) {
-    const short *qp = a.q + (q0 + tok) * a.q_stride + h * D + h2 * 16;
+  s16x8 qf[KS];
+  const short *qp = a.q + (q0 + tok) * a.q_stride + h * D + h2 * 8;
 #pragma unroll
-    for (int k = 0; k < K4; ++k) {
-      uint32_t scale[2];
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        float x[16];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const s16x8 v = *reinterpret_cast<const s16x8 *>(qp + k * 64 + g * 32 + i * 8);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[i * 8 + e] = a.flip ? -to_f32<BF>(v[e]) : to_f32<BF>(v[e]);
-        }
-        uint32_t top = abs_bits(x, 16);
-        top = max(top, uint32_t(__shfl_xor(int(top), 32, 64)));
-        if (top >= 0x7f800000u) {
-          broken = true;
-          top = 0;
-#pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] = 0.f;
-        }
-        scale[g] = query_scale(top);
-        const Parts8 p = query_parts(x, scale[g]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) q_hi[k][g * 4 + e] = p.hi[e], q_lo[k][g * 4 + e] = p.lo[e];
-      }
-      const uint32_t mine = h2 ? scale[1] : scale[0];
-      q_scale |= (mine | (mine - 4) << 8) << (16 * k);
-    }
-  } else {
-    const short *qp = a.q + (q0 + tok) * a.q_stride + h * D + h2 * 8;
-#pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      qf[k] = *reinterpret_cast<const s16x8 *>(qp + k * 16);
-      if (a.flip) qf[k] ^= short(0x8000);
-    }
+  for (int k = 0; k < KS; ++k) {
+    qf[k] = *reinterpret_cast<const s16x8 *>(qp + k * 16);
+    if (a.flip) qf[k] ^= short(0x8000);
   }
   f32x16 o[DB] = {};
   float m = -INFINITY, mc = 0.f, l = 0.f;
@@ -521,17 +440,11 @@ __device__ __forceinline__ void attn4_chunk(const Attn4Args &a, int block, int z
     for (int i = 0; i < LD; ++i) {
       const bool bad = ws[i] > kTopScale<BF>;
       const float unit = scale_of<BF>(ws[i]);
-      if (BF && !val[i]) {
-        *reinterpret_cast<Codes<32> *>(reinterpret_cast<char *>(lds) + buf * kCodeTile<D> +
-                                       lrow[i] * kCodeRow<D> + group * 16) = w[i];
-      } else {
-        short *to = lds + (val[i] ? VT + buf * kTile<D, 64> : buf * KB) + tile_row<D>(lrow[i]) +
-                    group * 32;
+      short *to = lds + (val[i] ? VT : 0) + buf * kTile<D, 64> + tile_row<D>(lrow[i]) + group * 32;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          *reinterpret_cast<s16x8 *>(to + k * 8) = values8<BF>(bad ? 0 : w[i][k], unit);
-      }
-      sb[buf][val[i]][lrow[i] * DB + group] = uint8_t(max(ws[i], 1u));
+      for (int k = 0; k < 4; ++k)
+        *reinterpret_cast<s16x8 *>(to + k * 8) = values8<BF>(bad ? 0 : w[i][k], unit);
+      sb[buf][val[i]][lrow[i] * DB + group] = uint8_t(ws[i]);
       if (bad) odd = 1;
     }
   };
@@ -554,52 +467,19 @@ __device__ __forceinline__ void attn4_chunk(const Attn4Args &a, int block, int z
       pages(j0 + 192);
     }
     f32x16 sc[2] = {};
-    if constexpr (BF) {
-      const char *const kb = reinterpret_cast<const char *>(lds) + buf * kCodeTile<D> +
-                             r32 * kCodeRow<D> + h2 * 16;
-      i32x8 kf[2][K4] = {};  // 32 codes: the first half
-      uint32_t unit[2];      // scale bytes of groups h2, 2 + h2 in bytes 0, 2
+    const short *const kb = lds + buf * kTile<D, 64> + tile_row<D>(r32) + h2 * 8;
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
+    for (int k0 = 0; k0 < KS; k0 += 4) {
+      s16x8 kf[4][2];
 #pragma unroll
-        for (int k = 0; k < K4; ++k) {
-          const Codes<32> x =
-              *reinterpret_cast<const Codes<32> *>(kb + c * 32 * kCodeRow<D> + k * 32);
+      for (int k = 0; k < 4; ++k)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) kf[c][k][e] = int(x[e]);
-        }
-        const uint8_t *b = &sb[buf][0][(c * 32 + r32) * DB];
-        unit[c] = (D == 128 ? *reinterpret_cast<const uint32_t *>(b)
-                            : *reinterpret_cast<const uint16_t *>(b)) >> (8 * h2);
-      }
+        for (int c = 0; c < 2; ++c)
+          kf[k][c] = *reinterpret_cast<const s16x8 *>(kb + c * 32 * kRow<D> + (k0 + k) * 16);
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {  // (the formats: A codes of 4 bits, B of 8)
-        sc[c] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf[c][0], q_hi[0], sc[c], 4, 0, 0,
-                                                                unit[c], 0, q_scale);
-        sc[c] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf[c][0], q_lo[0], sc[c], 4, 0, 0,
-                                                                unit[c], 1, q_scale);
-        if constexpr (K4 == 2) {
-          sc[c] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf[c][1], q_hi[1], sc[c], 4, 0, 2,
-                                                                  unit[c], 2, q_scale);
-          sc[c] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf[c][1], q_lo[1], sc[c], 4, 0, 2,
-                                                                  unit[c], 3, q_scale);
-        }
-      }
-    } else {
-      const short *const kb = lds + buf * KB + tile_row<D>(r32) + h2 * 8;
+      for (int k = 0; k < 4; ++k)
 #pragma unroll
-      for (int k0 = 0; k0 < KS; k0 += 4) {
-        s16x8 kf[4][2];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
-            kf[k][c] = *reinterpret_cast<const s16x8 *>(kb + c * 32 * kRow<D> + (k0 + k) * 16);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) sc[c] = mfma_32x32x16<BF>(kf[k][c], qf[k0 + k], sc[c]);
-      }
+        for (int c = 0; c < 2; ++c) sc[c] = mfma_32x32x16<BF>(kf[k][c], qf[k0 + k], sc[c]);
     }
     if (__builtin_amdgcn_readfirstlane(odd)) {
 #pragma unroll
@@ -685,10 +565,6 @@ __device__ __forceinline__ void attn4_chunk(const Attn4Args &a, int block, int z
   }
   raise_err(a.err, code);
   l += __shfl_xor(l, 32, 64);
-  if (BF && broken && l > 0.f) {  // (one that sees nothing is 0 all the same)
-    l = NAN;
-    poison = (1u << DB) - 1;
-  }
   if (__any(poison != 0))
 #pragma unroll
     for (int d = 0; d < DB; ++d) put_poison<16>(poison, d, o[d]);
@@ -727,13 +603,13 @@ k_attn4_few(Attn4Args a) {
 }
 template <bool BF, int D, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64, 2) k_attn4_chunk(Attn4Args a) {
-  __shared__ __align__(16) short lds[BF ? kCodeTile<D> + 2 * kTile<D, 64> : 4 * kTile<D, 64>];
+  __shared__ __align__(16) short lds[4 * kTile<D, 64>];
   attn4_chunk<BF, D, WAVES>(a, blockIdx.x, blockIdx.y, lds);
 }
 // Both kinds of requests in one launch, as over the 16-bit cache.
 template <bool BF, int D, int NT>
 __global__ void __launch_bounds__(256, 2) k_attn4_mixed(Attn4Args a, int chunk, int tiles) {
-  __shared__ __align__(16) short lds[BF ? kCodeTile<D> + 2 * kTile<D, 64> : 4 * kTile<D, 64>];
+  __shared__ __align__(16) short lds[4 * kTile<D, 64>];
   const int block = blockIdx.x;
   if (block < chunk)
     attn4_chunk<BF, D, 4>(a, block % tiles, block / tiles, lds);

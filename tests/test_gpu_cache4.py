@@ -355,6 +355,43 @@ def test_queries_that_are_not_finite_stay_in_their_rows(lens, kv):
 
 
 @pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("large", [1.0, 256.0, 2.0 ** 100])
+def test_queries_of_chunks_keep_what_lies_far_below_their_largest_value(D, large):
+    """The largest value of each group meets keys of 0, so the scores are the others'."""
+    g, lens, kv = gen(D), [80], [150]
+    c = make_cache4(g, kv, 1, D, 16, BF)
+    c[0][..., ::16] &= 0xf0             # value 0 of each group of 32 is a zero
+    q = normal(g, 80, 1, D, dtype=BF) * torch.exp2(-(torch.arange(D) % 23).float()).to(BF)
+    q[..., ::32] = large
+    k, v = both_values(c, BF)
+    want, _, lse, ltol = cref.attention(q, k, v, c[4], [0, 80], kv, 1.0, 0, 0)
+    _, l = fs.fs_paged_attention4(step_of(lens, kv), on_gpu4(*c), q.cuda(), 1.0, want_lse=True)
+    within(l, lse, ltol, "lse")
+
+
+@pytest.mark.parametrize("lens,kv", [([70, 1], [200, 40]), ([90], [3000]), ([70, 3], [64, 2])])
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_nan_query_of_a_chunk_gives_nan_to_its_row(lens, kv, D):
+    """A row that sees no token is 0 all the same."""
+    g = gen(D + kv[0])
+    c = make_cache4(g, kv, 1, D, 16, BF)
+    q = normal(g, sum(lens), 1, D, dtype=BF)
+    step, cache = step_of(lens, kv), on_gpu4(*c)
+    want, wl = fs.fs_paged_attention4(step, cache, q.cuda(), 0.1, want_lse=True)
+    rows = [0, 33, lens[0] - 1]
+    for t, d in zip(rows, (0, D // 2 + 5, D - 1)):
+        q[t, 0, d] = math.nan
+    out, lse = fs.fs_paged_attention4(step, cache, q.cuda(), 0.1, want_lse=True)
+    for t in range(sum(lens)):
+        if t in rows and t + kv[0] - lens[0] >= 0:
+            assert bool(out[t].isnan().all()) and bool(lse[t].isnan().all()), t
+        else:
+            assert torch.equal(out[t], want[t]) and torch.equal(lse[t], wl[t]), t
+    if kv[0] < lens[0]:
+        assert bool((out[0] == 0).all()) and float(lse[0, 0]) == -math.inf
+
+
+@pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("byte", [1, 0, 30, 200, 252])
 def test_attention4_of_far_scales(D, byte):
     """Keys of 0 weigh all values alike, however large or small these are (bfloat16's range)."""
