@@ -76,14 +76,10 @@ fs_status fs_cache4_rows(const fs_step *s, const fs_kv_cache4 *c, int32_t dtype,
 /* fs_paged_attention over a cache of 4 bits, with a window and sinks as above; q and out of
  * `dtype`.  head_dim 64 or 128 and the other limits as there.  The values that codes and
  * scales stand for are exact in `dtype` (FS_F16: in its range); the rest is as in
- * fs_paged_attention, the rounding of the probabilities included, but for FS_BF16 and a request
- * whose tokens times n_heads / n_kv_heads are more than 64: there a query's group of 32 values
- * is multiplied with the codes in two 8-bit parts of each value, which are exact down to 2^-13
- * of the group's largest value and below that off by at most 2^-21 of it.
- * A group of the cache that counts as NaN makes out and lse of the rows that see it NaN (k), or
- * its 32 values of out (v).  A query with a value that is not finite reaches its own row alone:
- * out and lse are NaN where it is multiplied in parts and the row sees a token, else what its
- * scores make of them.  Sums stay finite while |v| < 2^100 (FS_BF16). */
+ * fs_paged_attention, the rounding of the probabilities included.  A group of the cache that
+ * counts as NaN makes out and lse of the rows that see it NaN (k), or its 32 values of out (v);
+ * a query with a value that is not finite reaches its own row alone.  Sums stay finite while
+ * |v| < 2^100 (FS_BF16). */
 size_t fs_attention4_workspace(const fs_step *s, const fs_kv_cache4 *c, int32_t n_heads,
                                int32_t window, int32_t sinks);
 fs_status fs_paged_attention4(const fs_step *s, const fs_kv_cache4 *c, int32_t dtype,

@@ -12,10 +12,10 @@
 //                  codes with one scale, and a wave's load is 16 whole keys without a gap.  V is
 //                  wanted with keys along a lane, while its codes and scales lie along dimensions:
 //                  it goes through LDS as 16-bit values and is read back transposed.
-//   k_attn4_chunk  larger chunks: bound by the products and the tile's steps between them (4,096
-//                  rows over 32,768 keys 1.64 to 1.74 ms from card to card, up to 1.25 PFLOP/s; in
-//                  half precision 1.88 to 1.98).  V as above; K stays in codes for bfloat16
-//                  queries, which are multiplied as two 8-bit parts, and is made values for others.
+//   k_attn4_chunk  larger chunks: bound by the chain of a tile's steps (scores, exponentials,
+//                  products) at two waves a SIMD (4,096 rows over 32,768 keys 1.84 to 1.95 ms from
+//                  card to card, 1.11 PFLOP/s; in half precision 1.88 to 2.01).  K and V go through
+//                  LDS as 16-bit values.
 //   k_attn4_mixed  both in one launch; the joins are those of the 16-bit cache, or
 //   k_attn4_join_many for few rows in very many splits.
 #include <type_traits>
@@ -50,12 +50,12 @@ constexpr int32_t kFewMost4 = 2048;
 constexpr int32_t kFewWhole4 = 262144;
 constexpr int32_t kOnce4 = 2048;
 // Splits go by the bound on lengths, and chunks of several requests seldom all reach it: twice the
-// work-groups.  (4 chunks of 300 rows over 20,000, 3,000, 1,000 and 500 keys: 215 us, 320 with 512
-// work-groups, all over 20,000 438 and 462; 8 of 100 over 100 to 8,000, head_dim 64: 39 and 63, all
-// over 8,000 64 and 87; but 3 of 1,000 over 9,000 457 and 414, 16 of 64 over 4,000 105 and 88.)
+// work-groups.  (4 chunks of 300 rows over 20,000, 3,000, 1,000 and 500 keys: 245 us, 342 with 512
+// work-groups, all over 20,000 492 and 527; 8 of 100 over 100 to 8,000, head_dim 64: 40 and 67, all
+// over 8,000 67 and 94; but 3 of 1,000 over 9,000 488 and 462, 16 of 64 over 4,000 108 and 94.)
 constexpr int32_t kChunkWant4 = 1024;
-// (100 rows over 4,000 keys 31.7 us, 38.7 in splits of 1,024 keys, 33.5 of 256; 255 rows over
-// 11,191, head_dim 64, 32.1, 36.6 and 32.2; 300 over 20,000 take longer splits.)
+// (100 rows over 4,000 keys 31.2 us, 38.8 in splits of 1,024 keys, 33.4 of 256; 255 rows over
+// 11,191, head_dim 64, 31.9, 37.2 and 31.6; 300 over 20,000 take longer splits.)
 constexpr int32_t kChunkLeast4 = 512;
 
 // Codes of N neighbouring values: 16 bytes for 32 of them, 8 for 16.
