@@ -263,9 +263,8 @@ __global__ void __launch_bounds__(kBlock) k_pages_list(PoolArgs a) {
 
 __global__ void __launch_bounds__(256) k_pages_fork(PoolArgs a) { fork_row<256>(a, blockIdx.x); }
 
-__global__ void __launch_bounds__(256) k_pages_free(PoolArgs a) {
-  __shared__ int32_t got;
-  const int32_t r = a.rows[blockIdx.x];
+// Row r let go, by the work-group.
+__device__ inline void free_row(const PoolArgs &a, int32_t r, int32_t &got) {
   const int tid = threadIdx.x;
   if (uint32_t(r) >= uint32_t(a.n_rows)) {
     if (tid == 0) raise_err(a.err, FS_E_RANGE);
@@ -287,6 +286,14 @@ __global__ void __launch_bounds__(256) k_pages_free(PoolArgs a) {
     }
   }
   if (bad) raise_err(a.err, FS_E_RANGE);
+  __syncthreads();  // (got is the next row's)
+}
+
+// (A launch counts its threads in 32 bits: 2^24 work-groups would be none.)
+constexpr int kFreeBlocks = 65536;
+__global__ void __launch_bounds__(256) k_pages_free(PoolArgs a) {
+  __shared__ int32_t got;
+  for (uint32_t i = blockIdx.x; i < uint32_t(a.n); i += kFreeBlocks) free_row(a, a.rows[i], got);
 }
 
 // Page p of a compaction, `rank` pages in use before it, L in all and `below` of them below L.
@@ -521,8 +528,9 @@ size_t pages_workspace_bytes(const fs_pages *p, int32_t n) {
 hipError_t launch_pages_free(const fs_pages *p, int32_t n, const int32_t *rows, int32_t *err,
                              hipStream_t stream) {
   PoolArgs a = pool_args(p, 0, nullptr, err);
+  a.n = n;
   a.rows = rows;
-  hipLaunchKernelGGL(k_pages_free, dim3(n), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(k_pages_free, dim3(n < kFreeBlocks ? n : kFreeBlocks), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
