@@ -683,14 +683,22 @@ void run(const AttnArgs &a, const Plan &p, hipStream_t stream) {
   }
 }
 
-}  // namespace
+constexpr int32_t kOnceSinks = 1024;
 
-constexpr int32_t kOnceSinks = 1024;  // (without sinks a window is split as ever)
+// Without a window, or with one that no length can fill, sinks are none: the call is then
+// fs_paged_attention's, split as ever, and its sums are taken in the same order.
+Shape shape16(const fs_step *s, const fs_kv_cache *c, int32_t n_heads, int32_t window,
+              int32_t sinks) {
+  Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks, 1024, 131072, 0, 512, 1024);
+  if (sh.sinks > 0) sh.few_once = kOnceSinks;
+  return sh;
+}
+
+}  // namespace
 
 size_t attention_workspace_bytes(const fs_step *s, const fs_kv_cache *c, int32_t n_heads,
                                  int32_t window, int32_t sinks) {
-  const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks, 1024, 131072,
-                            sinks ? kOnceSinks : 0, 512, 1024);
+  const Shape sh = shape16(s, c, n_heads, window, sinks);
   return space(plan(s, sh), s, sh).total();
 }
 
@@ -698,8 +706,7 @@ hipError_t launch_attention(const fs_step *s, const fs_kv_cache *c, int32_t n_he
                             int32_t window, int32_t sinks, const void *q, int64_t q_stride,
                             void *out, int64_t out_stride, float *lse, void *ws, int32_t *err,
                             hipStream_t stream) {
-  const Shape sh = shape_of(s, n_heads, c->n_kv_heads, c->head_dim, window, sinks, 1024, 131072,
-                            sinks ? kOnceSinks : 0, 512, 1024);
+  const Shape sh = shape16(s, c, n_heads, window, sinks);
   const Plan p = plan(s, sh);
   AttnArgs a;
   fill_args(a, p, space(p, s, sh), sh, s, scale, q, q_stride, out, out_stride, lse, ws, err);
