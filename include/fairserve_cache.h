@@ -118,8 +118,9 @@ fs_status fs_pages_free(const fs_pages *p, int32_t n, const int32_t *rows, int32
  * to be made in each layer by fs_pages_copy: src[i] -> dst[i] (otherwise both -1).
  * So a page that is held twice is whole and is not written again.
  * Parents and free pages are those before the call.  FS_E_RANGE, and no pages, src = dst = -1
- * for the i in question: a parent, child or length out of range, a child that holds pages or
- * is named by a lower i, a parent that does not hold the shared tokens, a room beyond width
+ * for the i in question, the others getting theirs as if it were not there: a parent, child or
+ * length out of range, a child that holds pages or is named by a lower i, a parent that does
+ * not hold the shared tokens, a page id out of range among the shared ones, a room beyond width
  * pages.  FS_E_OVERFLOW, and nothing at all is given, where the free pages do not suffice.
  * ws: fs_pages_workspace(p, n) bytes, 256-byte aligned; so for fs_pages_compact (n = 0). */
 size_t fs_pages_workspace(const fs_pages *p, int32_t n);

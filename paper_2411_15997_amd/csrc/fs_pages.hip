@@ -20,6 +20,7 @@ constexpr int kBlock = 1024;          // threads
 constexpr int kPer = 2 * kBlock;      // pages of a work-group
 constexpr int kFewPages = 2 * kBlock;  // a pool that one work-group looks through
 constexpr int kFewForks = 32;         // forks, and rows, that the same one finishes
+constexpr int kSomeForks = 1024;      // forks that it plans
 constexpr int kClaims = 8192;         // rows whose claims LDS holds
 
 struct PoolArgs {
@@ -31,9 +32,10 @@ struct PoolArgs {
   int32_t *src, *dst, *count, *refs_out, *table_out;
   int64_t out_stride;
   int32_t *claim;            // [n_rows]
-  int32_t *first;            // [n + 1]: new pages of the forks before; -1 - that for a refused one
+  int32_t *first;            // [n]: new pages of the forks before; -1 - that for a refused one
   int32_t *block_sum;        // [blocks]
   int32_t *list;             // [n_pages]: free pages in order; of a compaction: a moved page's rank
+  int32_t most;              // free pages that a fork can take
   int32_t *word;             // fork: whether the pages suffice; compaction: L and the moves
   int32_t *err;
 };
@@ -69,8 +71,28 @@ __device__ inline T block_before(T x, T *lds) {
   return before;
 }
 
-// Which forks are sound and how many new pages come before each one's, by one work-group; the
-// sum, at most n_pages + 1.
+// Which forks would share a page id out of range: their first[i] is -1, that of the others 0.  Seen
+// before the plan: a refused fork takes no free pages from the others.  By `groups` groups of
+// `lanes` neighbouring lanes (a power of two up to 64), this thread in number `group`.
+__device__ inline void check_shared(const PoolArgs &a, int32_t group, int32_t groups, int lanes) {
+  const int lane = threadIdx.x & (lanes - 1);
+  for (int32_t i = group; i < a.n; i += groups) {
+    const int32_t p = a.parent[i], sh = a.shared[i];
+    const bool any = p >= 0 && p < a.n_rows && sh > 0;
+    // (what the parent does not hold is refused for that)
+    const int32_t pages =
+        any ? int32_t(min((int64_t(sh) + (1 << a.page_shift) - 1) >> a.page_shift, int64_t(a.width)))
+            : 0;
+    const int32_t *from = a.table + int64_t(any ? p : 0) * a.stride;
+    int32_t bad = 0;
+    for (int32_t j = lane; j < pages; j += lanes) bad |= uint32_t(from[j]) >= uint32_t(a.n_pages);
+    for (int w = lanes >> 1; w; w >>= 1) bad |= __shfl_xor(bad, w, 64);
+    if (lane == 0) a.first[i] = -bad;
+  }
+}
+
+// Which forks are sound (first[i] says which share sound pages) and how many new pages come before
+// each one's, by one work-group; the sum, at most n_pages + 1.
 __device__ inline int32_t plan_forks(const PoolArgs &a) {
   __shared__ int64_t lds64[kBlock / 64];
   __shared__ int32_t lds_claim[kClaims];
@@ -100,7 +122,7 @@ __device__ inline int32_t plan_forks(const PoolArgs &a) {
       if (ok) ok = pages <= a.width;
       if (ok && sh > 0)
         ok = p >= 0 && has >= 0 && has <= a.width &&
-             int32_t((int64_t(sh) + size - 1) >> a.page_shift) <= has;
+             int32_t((int64_t(sh) + size - 1) >> a.page_shift) <= has && a.first[i] == 0;
       if (ok)
         need = pages - (sh >> a.page_shift);
       else
@@ -126,19 +148,12 @@ template <int THREADS>
 __device__ inline void fork_row(const PoolArgs &a, int32_t i) {
   const int tid = threadIdx.x % THREADS;
   const int32_t first = a.first[i];
-  bool go = first >= 0 && *a.word;
+  const bool go = first >= 0 && *a.word;
   const int32_t p = go ? a.parent[i] : 0, c = go ? a.child[i] : 0, sh = go ? a.shared[i] : 0;
   const int32_t size = 1 << a.page_shift, full = sh >> a.page_shift;
   const int32_t pages = go ? int32_t((int64_t(a.room[i]) + size - 1) >> a.page_shift) : 0;
   const bool part = sh & (size - 1);
-  const int32_t *from = a.table + int64_t(max(p, 0)) * a.stride;
-  bool bad = false;
-  for (int32_t j = tid; j < full + part; j += THREADS)
-    bad |= uint32_t(from[j]) >= uint32_t(a.n_pages);
-  if (THREADS == 64 ? __any(bad) : __syncthreads_or(bad)) {
-    raise_err(a.err, FS_E_RANGE);
-    go = false;
-  }
+  const int32_t *from = a.table + int64_t(max(p, 0)) * a.stride;  // (ids looked at before the plan)
   if (tid == 0) {
     a.src[i] = go && part ? from[full] : -1;
     a.dst[i] = go && part ? a.list[first] : -1;
@@ -195,6 +210,9 @@ template <bool WHOLE>
 __global__ void __launch_bounds__(kBlock) k_pages_plan(PoolArgs a) {
   __shared__ int32_t lds[kBlock / 64];
   int32_t mine = 0, all;
+  int lanes = 64;
+  while (lanes * a.n > kBlock) lanes >>= 1;
+  check_shared(a, threadIdx.x / lanes, kBlock / lanes, lanes);
   my_pages(a, [&](int32_t p, int32_t refs) {
     mine += __popcll(__ballot(p < a.n_pages && refs <= 0));
   });
@@ -214,49 +232,46 @@ __global__ void __launch_bounds__(kBlock) k_pages_plan(PoolArgs a) {
 }
 
 // Pools of many pages: the pages of block b that are in use (LIVE) or free, and for a fork, in
-// a block of its own, the forks.
+// blocks of their own, the shared pages of a fork for each wave.
 template <bool LIVE>
 __global__ void __launch_bounds__(kBlock) k_pages_count(PoolArgs a) {
   __shared__ int32_t lds[kBlock / 64];
-  const int tid = threadIdx.x;
-  if (int32_t(blockIdx.x) < a.blocks) {
+  const int tid = threadIdx.x, b = blockIdx.x;
+  if (LIVE || b < a.blocks) {
     int32_t x = 0;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int32_t p = blockIdx.x * kPer + i * kBlock + tid;
+      const int32_t p = b * kPer + i * kBlock + tid;
       if (p < a.n_pages) x += (a.refs[p] > 0) == LIVE;
     }
     x = block_total(x, lds);
-    if (tid == 0) a.block_sum[blockIdx.x] = x;
-    return;
-  }
-  if constexpr (!LIVE) {
-    const int32_t wanted = plan_forks(a);
-    if (tid == 0) a.first[a.n] = wanted;
+    if (tid == 0) a.block_sum[b] = x;
+  } else {
+    check_shared(a, (b - a.blocks) * (kBlock / 64) + (tid >> 6),
+                 (int32_t(gridDim.x) - a.blocks) * (kBlock / 64), 64);
   }
 }
 
-// The list of the first free pages.
+// The list of the first free pages, as many as can be asked for, and, in a block of its own, the
+// forks.
 __global__ void __launch_bounds__(kBlock) k_pages_list(PoolArgs a) {
   __shared__ int32_t lds[kBlock / 64];
   const int tid = threadIdx.x;
-  const int32_t wanted = a.first[a.n];
-  int32_t before = 0, all = 0;
-  for (int32_t b = tid; b < a.blocks; b += kBlock) {
-    const int32_t x = a.block_sum[b];
-    all += x;
-    if (b < int32_t(blockIdx.x)) before += x;
-  }
+  const bool plans = int32_t(blockIdx.x) == a.blocks;
+  int32_t before = 0;  // free pages of the blocks before: for the forks, all
+  for (int32_t b = tid; b < int32_t(blockIdx.x); b += kBlock) before += a.block_sum[b];
   before = block_total(before, lds);
-  all = block_total(all, lds);
-  if (blockIdx.x == 0) enough(a, wanted, all);
-  if (wanted > all || before >= wanted) return;
+  if (plans) {
+    enough(a, plan_forks(a), before);
+    return;
+  }
+  if (before >= a.most) return;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int32_t p = blockIdx.x * kPer + i * kBlock + tid;
     const int32_t is = p < a.n_pages && a.refs[p] <= 0;
     const int32_t at = before + block_before(is, lds);
-    if (is && at < wanted) a.list[at] = p;
+    if (is && at < a.most) a.list[at] = p;
     before += block_total(is, lds);
   }
 }
@@ -514,7 +529,7 @@ PoolArgs pool_args(const fs_pages *p, int32_t n, void *ws, int32_t *err) {
   a.block_sum = take(a.blocks);
   a.list = take(p->n_pages);
   a.claim = take(p->n_rows);
-  a.first = take(size_t(n) + 1);
+  a.first = take(n);
   return a;
 }
 
@@ -522,7 +537,7 @@ PoolArgs pool_args(const fs_pages *p, int32_t n, void *ws, int32_t *err) {
 
 size_t pages_workspace_bytes(const fs_pages *p, int32_t n) {
   return 256 + round256(size_t(page_blocks(p)) * 4) + round256(size_t(p->n_pages) * 4) +
-         round256(size_t(p->n_rows) * 4) + round256((size_t(n) + 1) * 4);
+         round256(size_t(p->n_rows) * 4) + round256(size_t(n) * 4);
 }
 
 hipError_t launch_pages_free(const fs_pages *p, int32_t n, const int32_t *rows, int32_t *err,
@@ -545,15 +560,18 @@ hipError_t launch_pages_fork(const fs_pages *p, int32_t n, const int32_t *parent
   a.room = room;
   a.src = src;
   a.dst = dst;
-  if (p->n_pages <= kFewPages) {
+  const int64_t most = int64_t(n) * p->width;
+  a.most = int32_t(most < p->n_pages ? most : p->n_pages);
+  if (p->n_pages <= kFewPages && n <= kSomeForks) {
     if (n <= kFewForks) {
       hipLaunchKernelGGL((k_pages_plan<true>), dim3(1), dim3(kBlock), 0, stream, a);
       return hipGetLastError();
     }
     hipLaunchKernelGGL((k_pages_plan<false>), dim3(1), dim3(kBlock), 0, stream, a);
   } else {
-    hipLaunchKernelGGL((k_pages_count<false>), dim3(a.blocks + 1), dim3(kBlock), 0, stream, a);
-    hipLaunchKernelGGL(k_pages_list, dim3(a.blocks), dim3(kBlock), 0, stream, a);
+    const int32_t checks = (n + kBlock / 64 - 1) / (kBlock / 64);
+    hipLaunchKernelGGL((k_pages_count<false>), dim3(a.blocks + checks), dim3(kBlock), 0, stream, a);
+    hipLaunchKernelGGL(k_pages_list, dim3(a.blocks + 1), dim3(kBlock), 0, stream, a);
   }
   hipLaunchKernelGGL(k_pages_fork, dim3(n), dim3(256), 0, stream, a);
   return hipGetLastError();
