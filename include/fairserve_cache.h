@@ -120,8 +120,9 @@ fs_status fs_pages_free(const fs_pages *p, int32_t n, const int32_t *rows, int32
  * Parents and free pages are those before the call.  FS_E_RANGE, and no pages, src = dst = -1
  * for the i in question, the others getting theirs as if it were not there: a parent, child or
  * length out of range, a child that holds pages or is named by a lower i, a parent that does
- * not hold the shared tokens, a page id out of range among the shared ones, a room beyond width
- * pages.  FS_E_OVERFLOW, and nothing at all is given, where the free pages do not suffice.
+ * not hold the shared tokens, a page id out of range or a free page among the shared ones, a
+ * room beyond width pages.  FS_E_OVERFLOW, and nothing at all is given, where the free pages do
+ * not suffice.
  * ws: fs_pages_workspace(p, n) bytes, 256-byte aligned; so for fs_pages_compact (n = 0). */
 size_t fs_pages_workspace(const fs_pages *p, int32_t n);
 fs_status fs_pages_fork(const fs_pages *p, int32_t n, const int32_t *parent, const int32_t *child,

@@ -71,9 +71,10 @@ __device__ inline T block_before(T x, T *lds) {
   return before;
 }
 
-// Which forks would share a page id out of range: their first[i] is -1, that of the others 0.  Seen
-// before the plan: a refused fork takes no free pages from the others.  By `groups` groups of
-// `lanes` neighbouring lanes (a power of two up to 64), this thread in number `group`.
+// Which forks would share a page id out of range, or a free page (which another one may get as a new
+// one): their first[i] is -1, that of the others 0.  Seen before the plan: a refused fork takes no
+// free pages from the others.  By `groups` groups of `lanes` neighbouring lanes (a power of two up
+// to 64), this thread in number `group`.
 __device__ inline void check_shared(const PoolArgs &a, int32_t group, int32_t groups, int lanes) {
   const int lane = threadIdx.x & (lanes - 1);
   for (int32_t i = group; i < a.n; i += groups) {
@@ -85,7 +86,10 @@ __device__ inline void check_shared(const PoolArgs &a, int32_t group, int32_t gr
             : 0;
     const int32_t *from = a.table + int64_t(any ? p : 0) * a.stride;
     int32_t bad = 0;
-    for (int32_t j = lane; j < pages; j += lanes) bad |= uint32_t(from[j]) >= uint32_t(a.n_pages);
+    for (int32_t j = lane; j < pages; j += lanes) {
+      const uint32_t id = from[j];
+      bad |= id >= uint32_t(a.n_pages) || a.refs[id] <= 0;
+    }
     for (int w = lanes >> 1; w; w >>= 1) bad |= __shfl_xor(bad, w, 64);
     if (lane == 0) a.first[i] = -bad;
   }

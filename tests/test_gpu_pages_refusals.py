@@ -1,6 +1,6 @@
 """What the calls of a pool of pages do at their limits, and what they refuse beside what they do
-not: rows named more often than a launch has work-groups, a page id out of range among the shared
-pages of some forks."""
+not: rows named more often than a launch has work-groups, a page id out of range or a free page
+among the shared pages of some forks."""
 import pytest
 import torch
 
@@ -87,3 +87,20 @@ def test_a_bad_page_behind_the_shared_ones_refuses_nothing():
     src, dst, err = fork_all(p, forks)
     assert err == 0 and (src, dst) == pool.fork(*zip(*forks))
     alike(p, pool)
+
+
+@pytest.mark.parametrize("n_pages,rows,n", SIZES)
+def test_a_free_page_among_the_shared_refuses_its_own_forks_alone(n_pages, rows, n):
+    """A page that no row is counted for may be given out as a new one: to share it as well would
+    make two rows write it."""
+    say("free shared page", n_pages, rows, n)
+    pool, forks = a_pool(n_pages, rows, n)
+    lost = pool.table[1][2]
+    pool.refs[lost] = 0                    # (free now, and the lowest)
+    p = on_gpu(pool)
+    src, dst, err = fork_all(p, forks)
+    assert err == fs.FS_E_RANGE
+    s, d = pool.fork(*zip(*forks[0::2]))
+    alike(p, pool)
+    assert src[0::2] == s and dst[0::2] == d and d[0] == lost
+    assert set(src[1::2]) == set(dst[1::2]) == {-1}
