@@ -133,8 +133,9 @@ fs_status fs_pages_fork(const fs_pages *p, int32_t n, const int32_t *parent, con
  * >= L moves to the i-th free id < L, src[i] -> dst[i], i < *count <= n_pages / 2; src and dst
  * [n_pages / 2] are -1 from *count on.  refs_out [n_pages] and table_out (row stride
  * table_out_stride >= width, entries from held on left as they were) get the new ids; each
- * may be the pool's own, and else does not overlap it.  The pages' contents are moved in each
- * layer by fs_pages_copy. */
+ * may be the pool's own, and else does not overlap it.  FS_E_RANGE for a held page that is free,
+ * whose entry keeps its id (other contents may move there).  The pages' contents are moved in
+ * each layer by fs_pages_copy. */
 fs_status fs_pages_compact(const fs_pages *p, int32_t *refs_out, int32_t *table_out,
                            int64_t table_out_stride, int32_t *src, int32_t *dst, int32_t *count,
                            void *ws, size_t ws_bytes, int32_t *err, hipStream_t stream);

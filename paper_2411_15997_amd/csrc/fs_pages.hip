@@ -34,7 +34,8 @@ struct PoolArgs {
   int32_t *claim;            // [n_rows]
   int32_t *first;            // [n]: new pages of the forks before; -1 - that for a refused one
   int32_t *block_sum;        // [blocks]
-  int32_t *list;             // [n_pages]: free pages in order; of a compaction: a moved page's rank
+  int32_t *list;             // [n_pages]: free pages in order; of a compaction: which moved page it
+                             // is, 0 for one that stays, -1 for a free one
   int32_t most;              // free pages that a fork can take
   int32_t *word;             // fork: whether the pages suffice; compaction: L and the moves
   int32_t *err;
@@ -315,16 +316,14 @@ __global__ void __launch_bounds__(256) k_pages_free(PoolArgs a) {
   for (uint32_t i = blockIdx.x; i < uint32_t(a.n); i += kFreeBlocks) free_row(a, a.rows[i], got);
 }
 
-// Page p of a compaction, `rank` pages in use before it, L in all and `below` of them below L.
+// Page p of a compaction, `rank` pages in use before it, L in all and `below` of them below L: the
+// pages in use with ids from L on, and the free ones below, in order of ids are src and dst.
 __device__ inline void place_page(const PoolArgs &a, int32_t p, int32_t refs, int32_t rank, int32_t L,
                                   int32_t below) {
   const int32_t moves = L - below;
-  if (p < L) {
-    if (refs <= 0) a.dst[p - rank] = p;
-  } else {
-    a.list[p] = refs > 0 ? rank - below : -1;
-    if (refs > 0) a.src[rank - below] = p;
-  }
+  a.list[p] = refs <= 0 ? -1 : p < L ? 0 : rank - below;
+  if (p < L && refs <= 0) a.dst[p - rank] = p;
+  if (p >= L && refs > 0) a.src[rank - below] = p;
   if (a.refs_out != a.refs) a.refs_out[p] = p < L && refs > 0 ? refs : 0;
   if (p >= moves && p < a.n_pages / 2) a.src[p] = a.dst[p] = -1;
 }
@@ -334,7 +333,6 @@ __device__ inline void put_moves(const PoolArgs &a, int32_t L, int32_t below) {
   a.word[1] = L - below;
 }
 
-// The pages in use with ids from L on, and the free ones below, in order of ids: src and dst.
 // Counts of the moved pages `from`, `from` + step .. .
 __device__ inline void move_counts(const PoolArgs &a, int32_t moves, int32_t from, int32_t step) {
   for (int32_t i = from; i < moves; i += step) {
@@ -354,12 +352,12 @@ __device__ inline void remap_row(const PoolArgs &a, int32_t L, int32_t r, int32_
     int32_t id = a.table[int64_t(r) * a.stride + j];
     if (uint32_t(id) >= uint32_t(a.n_pages)) {
       bad = true;
-    } else if (id >= L) {
+    } else {
       const int32_t m = a.list[id];
-      if (m >= 0)
+      if (m < 0)
+        bad = true;  // a held page that is free: its id may be another's now
+      else if (id >= L)
         id = a.dst[m];
-      else
-        bad = true;  // a held page that is free
     }
     a.table_out[int64_t(r) * a.out_stride + j] = id;
   }

@@ -1,6 +1,6 @@
 """What the calls of a pool of pages do at their limits, and what they refuse beside what they do
 not: rows named more often than a launch has work-groups, a page id out of range or a free page
-among the shared pages of some forks."""
+among the shared pages of some forks, a free page held by a row that is renumbered."""
 import pytest
 import torch
 
@@ -104,3 +104,33 @@ def test_a_free_page_among_the_shared_refuses_its_own_forks_alone(n_pages, rows,
     alike(p, pool)
     assert src[0::2] == s and dst[0::2] == d and d[0] == lost
     assert set(src[1::2]) == set(dst[1::2]) == {-1}
+
+
+@pytest.mark.parametrize("other", [False, True])
+@pytest.mark.parametrize("n_pages,rows,width", [(40, 3, 6), (2000, 50, 6), (3000, 3, 6), (3000, 9, 1500)])
+def test_compaction_refuses_a_held_page_that_is_free(n_pages, rows, width, other):
+    """Below L as from there on: FS_E_RANGE, and the entry keeps its id; the other entries and the
+    counts are renumbered."""
+    say("held but free", n_pages, rows, width, other)
+    # row 0 holds the pool's last pages, row 1 its first ones; L = 8
+    for low, at in ((True, 2), (False, 2), (True, 0), (False, 3)):
+        pool = cref.Pool(n_pages, 4, rows, width)
+        pool.table[0][:5] = range(n_pages - 5, n_pages)
+        pool.table[1][:4] = range(4)
+        pool.held[:2] = [5, 4]
+        for q in pool.table[0][:5] + pool.table[1][:4]:
+            pool.refs[q] = 1
+        row = 1 if low else 0
+        lost = pool.table[row][at]
+        pool.refs[lost] = 0
+        p = on_gpu(pool)
+        out = dict(refs_out=torch.full_like(p.refs, 9), table_out=p.table.clone()) if other else {}
+        err = fs.cleared_err_word()
+        src, dst, count = fs.fs_pages_compact(p, err=err, check=False, **out)
+        assert int(err) == fs.FS_E_RANGE, (low, at)
+        s, d = pool.compact()
+        pool.table[row][at] = lost
+        n = int(count)
+        assert (src[:n].tolist(), dst[:n].tolist()) == (s, d)
+        refs, table = (out["refs_out"], out["table_out"]) if other else (p.refs, p.table)
+        assert refs.tolist() == pool.refs and table.tolist() == pool.table, (low, at)
