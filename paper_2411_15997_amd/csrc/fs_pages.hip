@@ -3,11 +3,11 @@
 //
 // A page's state is its count of holders.  Free pages are taken, and pages are moved, in the
 // order of ids: a page's place is its rank among its kind, the sum of a block's count before it
-// (k_count, then each block adds up the counts of those before it) and of ballots inside the
+// (k_pages_count, then each block adds up the counts of those before it) and of ballots inside the
 // block.  So no result hangs on the order of atomics; those used (claims by the lowest index,
 // counts of holders) end the same in any order.
 // Bound by launches and chains of a few dependent loads: pools of up to 2,048 pages take one kernel
-// of 4 to 8 us, larger ones three of 4 to 6 (256 forks among 9,425 pages 16 us, 9,559 pages moved
+// of 4 to 8 us, larger ones three of 3 to 6 (256 forks among 9,425 pages 13 us, 9,559 pages moved
 // together 15); the copies by their bytes (277 MB: 46 us, 6.0 TB/s, some of it from the cache before
 // memory).
 #include "fs_cache.h"
@@ -20,7 +20,7 @@ constexpr int kBlock = 1024;          // threads
 constexpr int kPer = 2 * kBlock;      // pages of a work-group
 constexpr int kFewPages = 2 * kBlock;  // a pool that one work-group looks through
 constexpr int kFewForks = 32;         // forks, and rows, that the same one finishes
-constexpr int kSomeForks = 1024;      // forks that it plans
+constexpr int kSomeForks = 256;       // forks that it plans
 constexpr int kClaims = 8192;         // rows whose claims LDS holds
 
 struct PoolArgs {
@@ -72,28 +72,25 @@ __device__ inline T block_before(T x, T *lds) {
   return before;
 }
 
-// Which forks would share a page id out of range, or a free page (which another one may get as a new
-// one): their first[i] is -1, that of the others 0.  Seen before the plan: a refused fork takes no
-// free pages from the others.  By `groups` groups of `lanes` neighbouring lanes (a power of two up
-// to 64), this thread in number `group`.
-__device__ inline void check_shared(const PoolArgs &a, int32_t group, int32_t groups, int lanes) {
+// Whether fork i (parent p, sh shared tokens) would share a page id out of range, or a free page
+// (which another one may get as a new one): first[i] is then -1, else 0.  Seen before the plan: a
+// refused fork takes no free pages from the others.  By `lanes` neighbouring lanes (a power of two up
+// to 64) of threads that all come here.
+__device__ inline void check_shared(const PoolArgs &a, int32_t i, int32_t p, int32_t sh, int lanes) {
   const int lane = threadIdx.x & (lanes - 1);
-  for (int32_t i = group; i < a.n; i += groups) {
-    const int32_t p = a.parent[i], sh = a.shared[i];
-    const bool any = p >= 0 && p < a.n_rows && sh > 0;
-    // (what the parent does not hold is refused for that)
-    const int32_t pages =
-        any ? int32_t(min((int64_t(sh) + (1 << a.page_shift) - 1) >> a.page_shift, int64_t(a.width)))
-            : 0;
-    const int32_t *from = a.table + int64_t(any ? p : 0) * a.stride;
-    int32_t bad = 0;
-    for (int32_t j = lane; j < pages; j += lanes) {
-      const uint32_t id = from[j];
-      bad |= id >= uint32_t(a.n_pages) || a.refs[id] <= 0;
-    }
-    for (int w = lanes >> 1; w; w >>= 1) bad |= __shfl_xor(bad, w, 64);
-    if (lane == 0) a.first[i] = -bad;
+  const bool any = i < a.n && p >= 0 && p < a.n_rows && sh > 0;
+  // (what the parent does not hold is refused for that)
+  const int32_t pages =
+      any ? int32_t(min((int64_t(sh) + (1 << a.page_shift) - 1) >> a.page_shift, int64_t(a.width)))
+          : 0;
+  const int32_t *from = a.table + int64_t(any ? p : 0) * a.stride;
+  int32_t bad = 0;
+  for (int32_t j = lane; j < pages; j += lanes) {
+    const uint32_t id = from[j];
+    bad |= id >= uint32_t(a.n_pages) || a.refs[id] <= 0;
   }
+  for (int w = lanes >> 1; w; w >>= 1) bad |= __shfl_xor(bad, w, 64);
+  if (lane == 0 && i < a.n) a.first[i] = -bad;
 }
 
 // Which forks are sound (first[i] says which share sound pages) and how many new pages come before
@@ -209,18 +206,21 @@ __device__ inline int32_t waves_before(int32_t x, int32_t *lds, int32_t &all) {
 }
 
 // The forks, and the list of the first free pages, as many as they take, in order of ids.  WHOLE:
-// the rows of few forks too, two for each wave.  (Eight forks in a pool of 247 pages: 7.8 us,
-// 14 and two more launches with the kernels for many.)
+// the rows of few forks too, two for each wave.  (Eight forks in a pool of 247 pages: 8.1 us, 11.3
+// and two more launches with the kernels for many.  256 forks that share 7 pages each in a pool of
+// 2,000: 12.4 with k_pages_fork, 13.1 and one more launch; 1,024 that share 75: 35.3 and 19.8.)
 template <bool WHOLE>
 __global__ void __launch_bounds__(kBlock) k_pages_plan(PoolArgs a) {
   __shared__ int32_t lds[kBlock / 64];
   int32_t mine = 0, all;
-  int lanes = 64;
-  while (lanes * a.n > kBlock) lanes >>= 1;
-  check_shared(a, threadIdx.x / lanes, kBlock / lanes, lanes);
+  // this thread's fork to be checked (2^shift lanes for each), its loads under way with the pages'
+  const int shift = min(6, __clz(a.n - 1) - (32 - 10));
+  const int32_t i = int32_t(threadIdx.x) >> shift;
+  const int32_t parent = i < a.n ? a.parent[i] : -1, shared = i < a.n ? a.shared[i] : 0;
   my_pages(a, [&](int32_t p, int32_t refs) {
     mine += __popcll(__ballot(p < a.n_pages && refs <= 0));
   });
+  check_shared(a, i, parent, shared, 1 << shift);
   const int32_t wanted = plan_forks(a);
   int32_t at = waves_before(mine, lds, all);
   if (enough(a, wanted, all))
@@ -252,8 +252,8 @@ __global__ void __launch_bounds__(kBlock) k_pages_count(PoolArgs a) {
     x = block_total(x, lds);
     if (tid == 0) a.block_sum[b] = x;
   } else {
-    check_shared(a, (b - a.blocks) * (kBlock / 64) + (tid >> 6),
-                 (int32_t(gridDim.x) - a.blocks) * (kBlock / 64), 64);
+    const int32_t i = (b - a.blocks) * (kBlock / 64) + (tid >> 6);
+    check_shared(a, i, i < a.n ? a.parent[i] : -1, i < a.n ? a.shared[i] : 0, 64);
   }
 }
 
@@ -306,14 +306,17 @@ __device__ inline void free_row(const PoolArgs &a, int32_t r, int32_t &got) {
     }
   }
   if (bad) raise_err(a.err, FS_E_RANGE);
-  __syncthreads();  // (got is the next row's)
 }
 
 // (A launch counts its threads in 32 bits: 2^24 work-groups would be none.)
 constexpr int kFreeBlocks = 65536;
 __global__ void __launch_bounds__(256) k_pages_free(PoolArgs a) {
   __shared__ int32_t got;
-  for (uint32_t i = blockIdx.x; i < uint32_t(a.n); i += kFreeBlocks) free_row(a, a.rows[i], got);
+  free_row(a, a.rows[blockIdx.x], got);
+  for (uint32_t i = blockIdx.x + kFreeBlocks; i < uint32_t(a.n); i += kFreeBlocks) {
+    __syncthreads();  // (got was the last row's)
+    free_row(a, a.rows[i], got);
+  }
 }
 
 // Page p of a compaction, `rank` pages in use before it, L in all and `below` of them below L: the
@@ -447,7 +450,7 @@ struct CopyArgs {
 
 constexpr int kUnroll = 4;  // loads of a thread under way
 
-// Bytes by T from the pieces of one page to another's: share `part` of `parts`.
+// Bytes by T from the pieces of one page to another's: its `part`-th 256 * kUnroll values of T.
 template <class T>
 __device__ inline void copy_page(char *base, const PageShape &s, int64_t from, int64_t to,
                                  int32_t part) {
