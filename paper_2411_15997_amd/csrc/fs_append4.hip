@@ -7,8 +7,8 @@
 // once: next to the border of two codes an error of fp32 would pick the other one, half of the
 // value away, and the cache would hang on the order of operations.  A key value costs two
 // fp64 products, which the card does at half of its fp32 rate.
-// Bound by HBM in steps of thousands of rows (7,616 of 32 + 2 x 8 heads of 128: 31.5 us, 5.2 TB/s,
-// and 8.7, 4.5 TB/s, to read them back), by the chain from lengths to pages to rows in small ones
+// Bound by HBM in steps of thousands of rows (7,616 of 32 + 2 x 8 heads of 128: 30 us, 5.4 TB/s,
+// and 9, 4.4 TB/s, to read them back), by the chain from lengths to pages to rows in small ones
 // (8 rows: 5.0 us and 3.2).
 #include <type_traits>
 

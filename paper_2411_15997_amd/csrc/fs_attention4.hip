@@ -4,18 +4,18 @@
 // the 16-bit cache, and codes in place of values.  A group of 32 values and its scale become
 // 16-bit values exactly (one conversion instruction for two of them).
 //   k_attn4_few    requests of at most 64 rows: bound by the cache's bytes where many are long
-//                  (64 of 16,384 tokens: 219 us, 5.2 TB/s; 128 of up to 16,384, 229,312 in all,
-//                  70 us, 3.6 TB/s, 60 and 4.2 without the join and the launch), by the chain from
-//                  lengths to pages to keys where few are (4 of 500: 8.6 us).  K feeds the first
-//                  product from registers: the sum over a head's dimensions may be taken in any
-//                  order, so each lane takes 32 (or 16) neighbouring ones of a key, 16 bytes of
-//                  codes with one scale, and a wave's load is 16 whole keys without a gap.  V is
-//                  wanted with keys along a lane, while its codes and scales lie along dimensions:
-//                  it goes through LDS as 16-bit values and is read back transposed.
+//                  (64 of 16,384 tokens: 219 to 227 us, 5.0 to 5.2 TB/s; 128 of up to 16,384,
+//                  229,312 in all, 70 us, 3.6 TB/s, 61 and 4.1 without the join and the launch), by
+//                  the chain from lengths to pages to keys where few are (4 of 500: 9.0 us).  K
+//                  feeds the first product from registers: the sum over a head's dimensions may be
+//                  taken in any order, so each lane takes 32 (or 16) neighbouring ones of a key, 16
+//                  bytes of codes with one scale, and a wave's load is 16 whole keys without a gap.
+//                  V is wanted with keys along a lane, while its codes and scales lie along
+//                  dimensions: it goes through LDS as 16-bit values and is read back transposed.
 //   k_attn4_chunk  larger chunks: bound by the chain of a tile's steps (scores, exponentials,
-//                  products) at two waves a SIMD (4,096 rows over 32,768 keys 1.84 to 1.95 ms from
-//                  card to card, 1.11 PFLOP/s; in half precision 1.88 to 2.01).  K and V go through
-//                  LDS as 16-bit values.
+//                  products) at two waves a SIMD (4,096 rows over 32,768 keys 1.84 to 1.96 ms from
+//                  card to card, 1.05 to 1.12 PFLOP/s; in half precision 1.88 to 2.01; head_dim 64
+//                  1.25, 0.82 PFLOP/s).  K and V go through LDS as 16-bit values.
 //   k_attn4_mixed  both in one launch; the joins are those of the 16-bit cache, or
 //   k_attn4_join_many for few rows in very many splits.
 #include <type_traits>
@@ -36,8 +36,8 @@ struct Attn4Args : AttnArgs {  // `c` is the cache's codes, in bytes
 template <bool BF>
 constexpr float kLift4 = BF ? -18.f : 7.f;
 
-// The most that a lane's 32 probabilities of a tile may sum to before its reference is moved:
-// 2^14 times the reference's own, and below half precision's 65,504.
+// The most that a lane's 32 probabilities of a tile may sum to before its reference is moved: 2^14
+// times the reference's own for bfloat16, and 2^8 times for half precision, below its 65,504.
 template <bool BF>
 constexpr float kMostSum = BF ? 0x1p-4f : 0x1p15f;
 
@@ -552,9 +552,9 @@ __device__ __forceinline__ void attn4_chunk(const Attn4Args &a, int block, int z
                             (lane >> 4 & 1) * 16 + (lane & 3) * 4;
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-      // keys 4 h2 .. + 3 and 8 + 4 h2 .. + 3 of the 16
 #pragma unroll
       for (int d = 0; d < DB; ++d) {
+        // keys 4 h2 .. + 3 and 8 + 4 h2 .. + 3 of the 16
         const short *from = vb + u * 16 * kRow<D> + d * 32;
         o[d] = mfma_32x32x16<BF>(__builtin_shufflevector(read_tr(from), read_tr(from + tile_row<D>(8)),
                                                          0, 1, 2, 3, 4, 5, 6, 7),
@@ -618,9 +618,9 @@ __global__ void __launch_bounds__(256, 2) k_attn4_mixed(Attn4Args a, int chunk, 
 }
 
 // The join of few rows in very many splits: a work-group for 32 columns of a row and head, 32
-// splits side by side.  (One request of 200,001 tokens, 32 heads in 224
-// splits: 34.5 us, 35.9 with a work-group for a row and head; 8 of 32,768 in 64 splits 43.8
-// and 43.3.)
+// splits side by side.  (One request of 200,001 tokens, 32 heads in 224 splits: 34.5 us, 32.5 to
+// 36.6 from card to card, 35.9 on the first with a work-group for a row and head; 8 of 32,768 in 64
+// splits 43.8 and 43.3.)
 constexpr int kManySplits = 128;
 template <bool BF, int D>
 __global__ void __launch_bounds__(256) k_attn4_join_many(Attn4Args a) {
@@ -660,7 +660,9 @@ void run(const Attn4Args &a, const Plan &p, hipStream_t stream) {
   const int few = p.few_seqs > 0 ? a.n_seqs * a.c.n_kv_heads * p.few_splits : 0;
   const int tiles = p.chunk_tiles * a.c.n_kv_heads;
   const int chunk = p.chunk_seqs > 0 ? tiles * p.chunk_splits : 0;
-  // In one launch where one kernel holds both without spilling registers.
+  // In one launch where one kernel holds both: at head_dim 128 it takes all 256 registers, and what
+  // it spills, 5 of them, is stored ahead of the chunks' loop and loaded after it, as 3 are by
+  // k_attn4_chunk alone.
   const bool mixed = few > 0 && chunk > 0 && p.chunk_rows == 128 && (D == 64 || p.few_rows <= 32);
   auto by_rows = [&](auto nt) {
     constexpr int NT = decltype(nt)::value;

@@ -385,7 +385,7 @@ Plan plan(const fs_step *s, const Shape &c) {
     // keys for them: no join.  (4 bits: 64 requests of up to 16,384 tokens, 8 heads of 128, a
     // window of 700 14.2 us, 16.2 in two splits, of 1,500 19.1 and 21.6; 40 of 1,500, 16 heads,
     // 33 and 40; 64 of 2,000 34.6 and 39.3, but 33 of 2,000 27.2 and 24.6.  16 bits with sinks:
-    // a window of 1,000 30.0 and 32.0, and of 1,500 over 264 work-groups 29.3 and 25.2.)
+    // a window of 1,000 30.2 and 33.4, and of 1,500 over 264 work-groups 29.3 and 25.2.)
     const int64_t once = 1024 + 2 * blocks;
     if (blocks > 256 && p.few_splits > 1 && len <= (once < c.few_once ? once : c.few_once)) {
       p.few_split = c.few_once;
